@@ -330,6 +330,80 @@ typedef struct {
 int kn_profile_enable(kn_ctx *ctx, int on);
 int kn_profile_read(kn_ctx *ctx, kn_profile *out /*host*/, int reset);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Networks chosen per row: what training such networks, or serving them behind a learned router, takes besides the
+ * path above.  E networks, M rows; the rows are in the order of their networks, network e has rows offsets[e] ..
+ * offsets[e+1]-1 (offsets: dev, E+1 entries, offsets[0] = 0, never falling, at most M), and rows offsets[E] .. M-1 belong
+ * to no network (what kn_bucket and kn_route leave: kn_bucket's offsets are one entry longer).  All calls are
+ * asynchronous on `stream`, read nothing back and may be captured into a HIP graph.  Sums, softmax statistics and
+ * scales are held in 32 bits whatever the type; results are rounded once.  The same inputs give the same bits.
+ * Entries of offsets beyond 0 .. M are taken as 0 or M; an entry of `rows` / `slots` outside its range counts as a row of zeros.
+ * Limits (KN_E_UNSUPPORTED beyond): 65535 networks, 2^30 rows, widths of 2^20; kn_route: 1024 networks, k <= 32. */
+
+/* Weights of the grouped products in memory: W[e][in][out] (the canonical layout's order), or W[e][out][in]. */
+typedef enum { KN_W_IN_OUT = 0, KN_W_OUT_IN = 1 } kn_w_layout;
+
+typedef struct {
+    int32_t dtype;          /* kn_dtype of x, w, bias, y and the gradients (kn_grouped_linear_f8: of bias and y)       */
+    int32_t w_layout;       /* kn_w_layout of w and dw                                                                 */
+    int32_t experts;        /* E >= 1 networks                                                                         */
+    int32_t n_in, n_out;    /* widths K and N of the layer                                                             */
+    int64_t rows;           /* M: rows of y (and dy, dx)                                                               */
+    int64_t x_rows;         /* rows of x: at least M unless `rows` is given                                            */
+    int64_t ldx;            /* elements from one row of x to the next, >= n_in                                         */
+} kn_linear_desc;
+
+/* The router: for each of T rows of E logits the k largest (ties: the lower index), their weights, and the order of the
+ * M = T*k pairs (row t, choice j), pair number t*k + j, by network, stable.  A logit of -infinity is never chosen; a row with
+ * fewer than k others has ids -1 and weights 0 in the remaining places.  renormalize != 0: the weights are the softmax over
+ * the row's chosen logits; else the softmax over all its logits, at the chosen ones.  A NaN among a row's logits is not
+ * chosen and makes the row's weights NaN.
+ * slots[t*k + j] = place of the pair in the order (a permutation of 0 .. M-1; pairs with id -1 come last, from offsets[E] on),
+ * rows[place] = t.  Workspace: kn_route_workspace_bytes, dev, 256-byte aligned. */
+int kn_route_workspace_bytes(int64_t T, int32_t experts, int32_t k, int64_t *out_bytes);
+int kn_route(void *stream, const void *logits /*dev T rows*/, int32_t dtype, int64_t T, int32_t experts, int64_t ld /*elements*/,
+             int32_t k, int32_t renormalize, float *weights /*dev T*k*/, int32_t *ids /*dev T*k*/, int32_t *slots /*dev T*k*/,
+             int32_t *rows /*dev T*k*/, int32_t *offsets /*dev E+1*/, void *workspace, int64_t workspace_bytes);
+/* Gradient of kn_route's weights: dlogits (dev, T*E, contiguous, of the logits' type) from dweights (dev, T*k), with kn_route's
+ * logits, weights and ids.  dweights of a pair with id -1 are not looked at. */
+int kn_route_backward(void *stream, const void *logits, int32_t dtype, int64_t T, int32_t experts, int64_t ld, int32_t k,
+                      int32_t renormalize, const float *weights, const int32_t *ids, const float *dweights, void *dlogits);
+
+/* One layer of all networks: y[i] = act(x[r] W_e + b_e) for the rows i of network e, r = rows[i] (i itself where rows is
+ * NULL); act is a ReLU or nothing.  Rows of no network: zeros. */
+int kn_grouped_linear(void *stream, const kn_linear_desc *desc, const void *x /*dev*/, const void *w /*dev E*K*N*/,
+                      const void *bias /*dev E*N, nullable*/, const int32_t *offsets, const int32_t *rows /*dev M, nullable*/,
+                      int32_t relu, void *y /*dev M*N*/);
+/* Gradient of its inputs, a row per row of y: dx[i] = dy[i] W_e^T (with `rows`: sum them with kn_combine).  x_relu (nullable):
+ * the layer's x where that is a ReLU's result; dx is then 0 where x[r] is not above 0, which is the gradient before that ReLU. */
+int kn_grouped_linear_dx(void *stream, const kn_linear_desc *desc, const void *dy /*dev M*N*/, const void *w, const void *x_relu,
+                         const int32_t *offsets, const int32_t *rows, void *dx /*dev M*K*/);
+/* Gradients of its weights and biases: dw[e] = sum over the network's rows of x[r]^T dy[i], in w's layout, and db[e] = sum of
+ * dy[i]; zeros for a network without rows. */
+int kn_grouped_linear_dw(void *stream, const kn_linear_desc *desc, const void *x, const void *dy, const int32_t *offsets,
+                         const int32_t *rows, void *dw /*dev E*K*N*/, void *db /*dev E*N, nullable*/);
+
+/* The same layer in 8 bits (e4m3).  kb = ceil(K / 128) blocks of inputs, zeros behind the K-th.
+ * kn_quantize_f8: rows x (R, K) -> q (dev, R * kb*128 bytes) and scales (dev, R * kb): s = max(amax, 2^-100) / 448 over a row's
+ * block, q the e4m3 nearest to x / s.  A NaN stays one; an infinity makes its block zeros and NaN.
+ * kn_quantize_f8_weights: w -> q (dev, E * N * kb*128 bytes, input innermost) and scales (dev, E * ceil(N/128) * kb), one per
+ * 128 outputs x 128 inputs.  To be done once per weights.  q 16-byte aligned.
+ * kn_grouped_linear_f8: y[i] = act(sum over blocks of s_x s_w (q_x q_w) + b_e); sums in fp32, y of desc's dtype. */
+int kn_quantize_f8(void *stream, const void *x, int32_t dtype, int64_t R, int32_t K, int64_t ld, void *q, float *scales);
+int kn_quantize_f8_weights(void *stream, const void *w, int32_t dtype, int32_t w_layout, int32_t experts, int32_t n_in,
+                           int32_t n_out, void *q, float *scales);
+int kn_grouped_linear_f8(void *stream, const kn_linear_desc *desc, const void *xq, const float *x_scales, const void *wq,
+                         const float *w_scales, const void *bias, const int32_t *offsets, const int32_t *rows, int32_t relu, void *y);
+
+/* The networks' results brought back to their rows: out[t] = sum over j < k of weights[t*k + j] y[slots[t*k + j]] (weights NULL:
+ * ones, which is the gradient of reading x through `rows`).  y (dev, M rows of `width`), out (dev, T rows). */
+int kn_combine(void *stream, const void *y, int32_t dtype, int64_t M, int32_t width, const int32_t *slots /*dev T*k*/,
+               const float *weights /*dev T*k, nullable*/, int64_t T, int32_t k, void *out);
+/* Its gradients: dy[slots[t*k + j]] = weights[t*k + j] dout[t] (rows of dy that no slot names are left as they are), and
+ * dweights[t*k + j] = <dout[t], y[slots[t*k + j]]> (nullable; then y may be NULL). */
+int kn_combine_backward(void *stream, const void *dout, const void *y, int32_t dtype, int64_t M, int32_t width, const int32_t *slots,
+                        const float *weights, int64_t T, int32_t k, void *dy, float *dweights);
+
 #ifdef __cplusplus
 }
 #endif

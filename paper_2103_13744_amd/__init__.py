@@ -22,7 +22,9 @@ EXPORTS = ["kn_error_string", "kn_last_hip_error", "kn_params_per_net", "kn_crea
            "kn_scene_bytes", "kn_scene_create", "kn_scene_destroy",
            "kn_extract_workspace_bytes", "kn_extract_occupancy", "kn_layered_workspace_bytes", "kn_eval_grouped_layered",
            "kn_workspace_bytes", "kn_cell_ids", "kn_bucket", "kn_eval_grouped", "kn_eval_grouped_static", "kn_march", "kn_composite",
-           "kn_render", "kn_composite_deltas", "kn_march_stratified", "kn_render_stratified", "kn_set_render_params", "kn_profile_enable", "kn_profile_read"]
+           "kn_render", "kn_composite_deltas", "kn_march_stratified", "kn_render_stratified", "kn_set_render_params", "kn_profile_enable", "kn_profile_read",
+           "kn_route_workspace_bytes", "kn_route", "kn_route_backward", "kn_grouped_linear", "kn_grouped_linear_dx", "kn_grouped_linear_dw",
+           "kn_quantize_f8", "kn_quantize_f8_weights", "kn_grouped_linear_f8", "kn_combine", "kn_combine_backward"]
 
 
 class KnError(RuntimeError):
@@ -39,6 +41,11 @@ class SceneDesc(C.Structure):
 class RenderStats(C.Structure):
     _fields_ = [("rays", C.c_int64), ("waves", C.c_int64), ("samples_evaluated", C.c_int64),
                 ("samples_blended", C.c_int64), ("slots", C.c_int64)]
+
+
+class LinearDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("w_layout", C.c_int32), ("experts", C.c_int32), ("n_in", C.c_int32), ("n_out", C.c_int32),
+                ("rows", C.c_int64), ("x_rows", C.c_int64), ("ldx", C.c_int64)]
 
 
 class Profile(C.Structure):
@@ -98,6 +105,18 @@ def load_library(build_if_missing: bool = True):
     L.kn_set_render_params.argtypes = [vp, i32, i32, i32]
     L.kn_profile_enable.argtypes = [vp, C.c_int]
     L.kn_profile_read.argtypes = [vp, C.POINTER(Profile), C.c_int]
+    desc = C.POINTER(LinearDesc)
+    L.kn_route_workspace_bytes.argtypes = [i64, i32, i32, C.POINTER(i64)]
+    L.kn_route.argtypes = [vp, vp, i32, i64, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, i64]
+    L.kn_route_backward.argtypes = [vp, vp, i32, i64, i32, i64, i32, i32, vp, vp, vp, vp]
+    L.kn_grouped_linear.argtypes = [vp, desc, vp, vp, vp, vp, vp, i32, vp]
+    L.kn_grouped_linear_dx.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp]
+    L.kn_grouped_linear_dw.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp]
+    L.kn_quantize_f8.argtypes = [vp, vp, i32, i64, i32, i64, vp, vp]
+    L.kn_quantize_f8_weights.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp]
+    L.kn_grouped_linear_f8.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp, vp, i32, vp]
+    L.kn_combine.argtypes = [vp, vp, i32, i64, i32, vp, vp, i64, i32, vp]
+    L.kn_combine_backward.argtypes = [vp, vp, vp, i32, i64, i32, vp, vp, i64, i32, vp, vp]
     _lib = L
     return L
 
@@ -432,3 +451,180 @@ def composite(sigma, rgb, offsets, step, term_eps=0.0, bg=(0.0, 0.0, 0.0)):
                           _ptr(offsets, torch.int32), R, float(step), float(term_eps), C.byref(bgc), _ptr(out), _ptr(T),
                           _ptr(used)), "kn_composite")
     return out, T, used
+
+
+# ---------------------------------------------------------------------------------------------
+# networks chosen per row: router, grouped products, weighted sum
+def _dtype_id(dtype) -> int:
+    wd = {torch.float32: KN_F32, torch.float16: KN_F16, torch.bfloat16: KN_BF16}.get(dtype)
+    if wd is None:
+        raise KnError("unsupported dtype %s" % dtype)
+    return wd
+
+
+def _rows_ptr(t, shape):
+    """Pointer and row stride of a matrix whose rows are contiguous but may lie apart (a slice of the columns of a wider one)."""
+    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise KnError("expected a device matrix with contiguous rows")
+    if any(w is not None and int(w) != int(h) for w, h in zip(shape, t.shape)):
+        raise KnError("expected shape %s, got %s" % (tuple(shape), tuple(t.shape)))
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _weights_layout(w):
+    """kn_w_layout of (E, n_in, n_out) weights: contiguous, or the transpose of contiguous (E, n_out, n_in) ones."""
+    if w.dim() != 3 or not w.is_cuda:
+        raise KnError("weights must be a device tensor (experts, n_in, n_out)")
+    if w.is_contiguous():
+        return 0
+    if w.transpose(1, 2).is_contiguous():
+        return 1
+    raise KnError("weights must be contiguous, or a transpose of contiguous (experts, n_out, n_in) ones")
+
+
+def route(logits, k, renormalize=True):
+    """Top-k router on (T, E) logits: (weights (T, k) float32, ids (T, k), slots (T, k), rows (T*k,), offsets (E + 1,)), int32
+    all but the first: what ``grouped_linear`` takes as ``rows`` and ``offsets`` and ``combine`` as ``slots`` and ``weights``."""
+    L = load_library()
+    T, E = logits.shape
+    ptr, ld = _rows_ptr(logits, (None, None))
+    dt, k, dev, i32 = _dtype_id(logits.dtype), int(k), logits.device, torch.int32
+    need = C.c_int64()
+    _check(L.kn_route_workspace_bytes(T, E, k, C.byref(need)), "kn_route_workspace_bytes")
+    weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+    ids, slots = torch.empty((T, k), dtype=i32, device=dev), torch.empty((T, k), dtype=i32, device=dev)
+    rows, offsets = torch.empty(T * k, dtype=i32, device=dev), torch.empty(E + 1, dtype=i32, device=dev)
+    ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+    _check(L.kn_route(_stream(), ptr, dt, T, E, ld, k, 1 if renormalize else 0, weights.data_ptr(), ids.data_ptr(), slots.data_ptr(),
+                      rows.data_ptr(), offsets.data_ptr(), ws.data_ptr(), need.value), "kn_route")
+    return weights, ids, slots, rows, offsets
+
+
+def route_backward(logits, weights, ids, dweights, renormalize=True):
+    """Gradient of ``route``'s weights by its logits: (T, E) of the logits' type."""
+    L = load_library()
+    T, E = logits.shape
+    k = ids.shape[1]
+    ptr, ld = _rows_ptr(logits, (None, None))
+    out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+    f = torch.float32
+    _check(L.kn_route_backward(_stream(), ptr, _dtype_id(logits.dtype), T, E, ld, k, 1 if renormalize else 0, _ptr(weights, f, shape=(T, k)),
+                               _ptr(ids, torch.int32, shape=(T, k)), _ptr(dweights, f, shape=(T, k)), out.data_ptr()), "kn_route_backward")
+    return out
+
+
+def _linear_desc(x, w, rows):
+    """(desc, M, pointers of x, w, rows): x (X, n_in) with contiguous rows, w (E, n_in, n_out), rows (M,) int32 or None."""
+    E, n_in, n_out = w.shape
+    if x.dtype is not w.dtype:
+        raise KnError("inputs and weights must have one dtype, got %s and %s" % (x.dtype, w.dtype))
+    px, ld = _rows_ptr(x, (None, n_in))
+    M = x.shape[0] if rows is None else rows.shape[0]
+    pr = None if rows is None else _ptr(rows, torch.int32, shape=(M,))
+    return LinearDesc(_dtype_id(x.dtype), _weights_layout(w), E, n_in, n_out, M, x.shape[0], ld), M, px, w.data_ptr(), pr
+
+
+def grouped_linear(x, w, offsets, rows=None, bias=None, relu=False, out=None):
+    """One layer of all networks: row i of the result, of network e with offsets[e] <= i < offsets[e + 1], is
+    x[rows[i]] @ w[e] + bias[e], then a ReLU where asked for; rows from offsets[E] on are zeros.  ``w``: (E, n_in, n_out),
+    contiguous or the transpose of contiguous (E, n_out, n_in) weights."""
+    L = load_library()
+    d, M, px, pw, pr = _linear_desc(x, w, rows)
+    if out is None:
+        out = torch.empty((M, d.n_out), dtype=x.dtype, device=x.device)
+    _check(L.kn_grouped_linear(_stream(), C.byref(d), px, pw, _ptr(bias, x.dtype, allow_none=True, shape=(d.experts, d.n_out)),
+                               _ptr(offsets, torch.int32, shape=(d.experts + 1,)), pr, 1 if relu else 0, _ptr(out, x.dtype, shape=(M, d.n_out))),
+           "kn_grouped_linear")
+    return out
+
+
+def grouped_linear_dx(dy, x, w, offsets, rows=None, relu_in=False):
+    """Gradient of ``grouped_linear``'s inputs, (M, n_in): a row per row of dy (sum them with ``combine`` where ``rows`` read a row
+    of x several times).  ``relu_in``: x is a ReLU's result, and the gradient is that before the ReLU."""
+    L = load_library()
+    d, M, px, pw, pr = _linear_desc(x, w, rows)
+    dx = torch.empty((M, d.n_in), dtype=x.dtype, device=x.device)
+    _check(L.kn_grouped_linear_dx(_stream(), C.byref(d), _ptr(dy, x.dtype, shape=(M, d.n_out)), pw, px if relu_in else None,
+                                  _ptr(offsets, torch.int32, shape=(d.experts + 1,)), pr if relu_in else None, dx.data_ptr()), "kn_grouped_linear_dx")
+    return dx
+
+
+def grouped_linear_dw(dy, x, w, offsets, rows=None, want_bias=True):
+    """Gradients of ``grouped_linear``'s weights, laid out as ``w``, and biases ((E, n_out), or None): sums over each network's rows."""
+    L = load_library()
+    d, M, px, _, pr = _linear_desc(x, w, rows)
+    dw = torch.empty_like(w)  # (keeps the layout of dense weights)
+    db = torch.empty((d.experts, d.n_out), dtype=x.dtype, device=x.device) if want_bias else None
+    _check(L.kn_grouped_linear_dw(_stream(), C.byref(d), px, _ptr(dy, x.dtype, shape=(M, d.n_out)), _ptr(offsets, torch.int32, shape=(d.experts + 1,)),
+                                  pr, dw.data_ptr(), None if db is None else db.data_ptr()), "kn_grouped_linear_dw")
+    return dw, db
+
+
+def grouped_linear_backward(dy, x, w, offsets, rows=None, relu_in=False, want_bias=True):
+    """(dx, dw, db) of ``grouped_linear``: see ``grouped_linear_dx`` and ``grouped_linear_dw``.  dy is the gradient before the layer's
+    own ReLU, if it has one (the next layer's ``relu_in``)."""
+    return (grouped_linear_dx(dy, x, w, offsets, rows, relu_in), *grouped_linear_dw(dy, x, w, offsets, rows, want_bias))
+
+
+def quantize_f8(x):
+    """Rows in 8 bits: (R, K) -> (float8_e4m3fn (R, kb * 128), zeros behind the K-th; float32 scales (R, kb)), kb = ceil(K / 128)."""
+    L = load_library()
+    R, K = x.shape
+    ptr, ld = _rows_ptr(x, (None, None))
+    kb = -(-K // 128)
+    q = torch.empty((R, kb * 128), dtype=torch.float8_e4m3fn, device=x.device)
+    s = torch.empty((R, kb), dtype=torch.float32, device=x.device)
+    _check(L.kn_quantize_f8(_stream(), ptr, _dtype_id(x.dtype), R, K, ld, q.data_ptr(), s.data_ptr()), "kn_quantize_f8")
+    return q, s
+
+
+def quantize_f8_weights(w):
+    """(E, n_in, n_out) weights in 8 bits: (float8_e4m3fn (E, n_out, kb * 128), float32 scales (E, ceil(n_out / 128), kb))."""
+    L = load_library()
+    E, K, N = w.shape
+    layout = _weights_layout(w)
+    kb = -(-K // 128)
+    q = torch.empty((E, N, kb * 128), dtype=torch.float8_e4m3fn, device=w.device)
+    s = torch.empty((E, -(-N // 128), kb), dtype=torch.float32, device=w.device)
+    _check(L.kn_quantize_f8_weights(_stream(), w.data_ptr(), _dtype_id(w.dtype), layout, E, K, N, q.data_ptr(), s.data_ptr()), "kn_quantize_f8_weights")
+    return q, s
+
+
+def grouped_linear_f8(xq, xs, wq, ws, offsets, rows=None, bias=None, relu=False, dtype=None, out=None):
+    """``grouped_linear`` on what ``quantize_f8`` and ``quantize_f8_weights`` gave; the result is of ``dtype`` (bfloat16)."""
+    L = load_library()
+    E, N, kp = wq.shape
+    X, kb, f8, f = xq.shape[0], kp // 128, torch.float8_e4m3fn, torch.float32
+    dtype = (torch.bfloat16 if dtype is None else dtype) if out is None else out.dtype
+    M = X if rows is None else rows.shape[0]
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype, device=xq.device)
+    d = LinearDesc(_dtype_id(dtype), 1, E, kp, N, M, X, kp)
+    _check(L.kn_grouped_linear_f8(_stream(), C.byref(d), _ptr(xq, f8, shape=(X, kb * 128)), _ptr(xs, f, shape=(X, kb)), _ptr(wq, f8),
+                                  _ptr(ws, f, shape=(E, -(-N // 128), kb)), _ptr(bias, dtype, allow_none=True, shape=(E, N)),
+                                  _ptr(offsets, torch.int32, shape=(E + 1,)), None if rows is None else _ptr(rows, torch.int32, shape=(M,)),
+                                  1 if relu else 0, _ptr(out, dtype, shape=(M, N))), "kn_grouped_linear_f8")
+    return out
+
+
+def combine(y, slots, weights=None):
+    """out[t] = sum over j of weights[t, j] * y[slots[t, j]] (ones where ``weights`` is None): (T, width) of y's type."""
+    L = load_library()
+    M, D = y.shape
+    T, k = slots.shape
+    out = torch.empty((T, D), dtype=y.dtype, device=y.device)
+    _check(L.kn_combine(_stream(), _ptr(y), _dtype_id(y.dtype), M, D, _ptr(slots, torch.int32), _ptr(weights, torch.float32, allow_none=True, shape=(T, k)),
+                        T, k, out.data_ptr()), "kn_combine")
+    return out
+
+
+def combine_backward(dout, y, slots, weights=None):
+    """Gradients of ``combine``: (dy, dweights (T, k) float32).  slots names every row of y (what ``route`` gives)."""
+    L = load_library()
+    M, D = y.shape
+    T, k = slots.shape
+    dy = torch.empty_like(y)
+    dw = torch.empty((T, k), dtype=torch.float32, device=y.device)
+    _check(L.kn_combine_backward(_stream(), _ptr(dout, y.dtype, shape=(T, D)), _ptr(y), _dtype_id(y.dtype), M, D, _ptr(slots, torch.int32),
+                                 _ptr(weights, torch.float32, allow_none=True, shape=(T, k)), T, k, dy.data_ptr(), dw.data_ptr()), "kn_combine_backward")
+    return dy, dw

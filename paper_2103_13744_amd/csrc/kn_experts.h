@@ -1,0 +1,102 @@
+// What the operators of per-row networks share (router, grouped products, weighted sum): element types, the look-up of a
+// workgroup's rows among groups of ragged sizes, the description of a grouped product.
+#pragma once
+
+#include "kn_common.h"
+
+typedef float kn_f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 kn_f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 kn_bf16x8 __attribute__((ext_vector_type(8)));
+typedef int kn_i32x4 __attribute__((ext_vector_type(4)));
+typedef int kn_i32x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t kn_u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int32_t KN_MAX_EXPERTS = 65535;
+constexpr int32_t KN_MAX_WIDTH = 1 << 20;
+constexpr int64_t KN_MAX_ROWS = 1ll << 30;
+
+template <typename T> struct KnType;
+template <> struct KnType<float> { static constexpr int id = KN_F32; };
+template <> struct KnType<_Float16> { static constexpr int id = KN_F16; };
+template <> struct KnType<__bf16> { static constexpr int id = KN_BF16; };
+
+static inline int kn_item(int32_t dtype) { return dtype == KN_F32 ? 4 : 2; }
+static inline bool kn_dtype_ok(int32_t dtype) { return dtype == KN_F32 || dtype == KN_F16 || dtype == KN_BF16; }
+
+// Calls `f` with a value of the element type that `dtype` names (which has been checked).
+template <typename F> static inline int kn_with_type(int32_t dtype, F &&f)
+{
+    if (dtype == KN_F32) return f(float());
+    if (dtype == KN_F16) return f((_Float16)0);
+    return f((__bf16)0.0f);
+}
+
+// Rows of one network among the sorted rows: where a workgroup's piece lies.
+struct KnPiece {
+    int32_t group;   // the network, or E: rows of no network
+    int32_t begin;   // first row of the piece
+    int32_t end;     // end of the group's rows (begin >= end: nothing to do)
+};
+
+// offsets[e] as far as it can be used: callers' arrays are not looked at on the host
+__device__ __forceinline__ int32_t kn_offset(const int32_t *__restrict__ offsets, int32_t e, int32_t M)
+{
+    return min(max(offsets[e], 0), M);
+}
+
+// Group e gets the pieces of `len` rows numbered from offsets[e] / len + e on: these first numbers grow strictly with e and
+// leave every group room for all its pieces, so a workgroup finds its group by a search in the offsets alone, with no list
+// of pieces to be made before.  64 offsets a step, one per lane: one step for up to 64 groups, three for 65,535.
+// Piece numbers run from 0 to M / len + E (the last group, E, is that of the rows without a network).
+__device__ __forceinline__ KnPiece kn_find_piece(const int32_t *__restrict__ offsets, int32_t E, int32_t M, int32_t len, int32_t number)
+{
+    const int lane = kn_thread() & (KN_WAVE - 1);
+    int32_t lo = 0, n = E + 1; // the group lies in [lo, lo + n)
+    while (n > 1) {
+        const int32_t step = (n + KN_WAVE - 1) / KN_WAVE;
+        const int32_t e = lo + lane * step;
+        const bool there = lane * step < n;
+        const bool upto = there && kn_offset(offsets, min(e, E), M) / len + e <= number;
+        const int32_t hits = __popcll(__ballot(upto)); // (the first is always one: number >= first number of lo)
+        const int32_t at = max(hits, 1) - 1;
+        lo += at * step;
+        n = min(step, n - at * step);
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    const int32_t o = kn_offset(offsets, lo, M);
+    KnPiece p;
+    p.group = lo;
+    const int32_t first = o / len + lo;
+    p.end = lo < E ? kn_offset(offsets, lo + 1, M) : M;
+    p.begin = number >= first ? o + (number - first) * len : p.end; // (always, where offsets start at 0 and do not fall)
+    return p;
+}
+static inline int64_t kn_pieces(int64_t M, int64_t E, int64_t len) { return M / len + E + 1; }
+
+// 16 x 16 products of fragments of 8 values a lane: lane l holds row (or column) l % 16 and the contraction's 8 (l / 16) .. + 7
+// of 32; results: column l % 16, rows 4 (l / 16) .. + 3.
+__device__ __forceinline__ kn_f32x4 kn_mfma(kn_f16x8 a, kn_f16x8 b, kn_f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ kn_f32x4 kn_mfma(kn_bf16x8 a, kn_bf16x8 b, kn_f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// the same for 4 values a lane of fp32: four products over 4 each, contraction 4 (l / 16) + j in the order j = 0 .. 3
+__device__ __forceinline__ kn_f32x4 kn_mfma(kn_f32x4 a, kn_f32x4 b, kn_f32x4 c)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+
+// A grouped product as the kernels see it.
+//   forward:         out(i, j) = sum over c of a(i, c) b_e(c, j), a = x (rows through `rows`), b_e = w[e], out = y, c < K
+//   input gradient:  the same with a = dy, b_e = w[e] transposed, out = dx, c < N
+//   weight gradient: out_e(i, j) = sum over the network's rows r of a(r, i) b(r, j), a = x (rows through `rows`), b = dy
+struct KnProduct {
+    const void *a, *b, *bias, *mask; // mask: out(i, j) becomes 0 where mask(row i, j) <= 0 (a ReLU's result)
+    void *out, *out_bias;            // out_bias (weight gradient): sum over the rows r of b(r, j)
+    const int32_t *offsets, *rows, *mask_rows; // rows: of a, mask_rows: of the mask, both nullable
+    int64_t lda, ldb, ldm;           // row strides in elements: a, b (weight gradient), mask
+    int64_t b_group, b_c, b_j;       // strides of b_e: network, contraction, column
+    int64_t o_group, o_i, o_j;       // strides of out: network (weight gradient), row, column
+    int32_t M, E, I, J, C;           // rows, networks; weight gradient: rows of out_e; columns of out; contraction
+    int32_t a_rows, m_rows;          // rows that a and the mask have (an index outside is a row of zeros)
+    int32_t relu;
+};
