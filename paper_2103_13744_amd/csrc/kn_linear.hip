@@ -1,6 +1,6 @@
 // Products grouped by network with ragged sizes, and their gradients: kn_grouped_linear, kn_grouped_linear_dx,
 // kn_grouped_linear_dw.
-#include "kn_experts.h"
+#include "kn_tile.h"
 
 namespace {
 
@@ -111,6 +111,140 @@ __global__ void __launch_bounds__(256) k_product_any(KnProduct p)
             }
 }
 
+// Rows of 16-byte pieces throughout: tiles of BM x BN results, WR x WC wavefronts, two stages in the LDS, of which one is
+// fetched while the other is multiplied.  COLS: b's columns are contiguous in memory (else its contraction is).
+// Fragments of b are the products' first operand, so that a lane holds four neighbouring results of a row; they go through
+// the LDS once more to leave in pieces of 8.
+template <typename T, bool COLS, int BM, int BN, int WR, int WC>
+__global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int32_t blocks)
+{
+    constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16, CS = 128 / sizeof(T);
+    typedef typename KnFrag<T>::Type Frag;
+    typedef KnRowLoader<T, BM, NW> LoadA;
+    __shared__ __align__(16) char lds_[2 * STAGE];
+    KN_LDS char *lds = (KN_LDS char *)lds_;
+    const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ntiles = (p.J + BN - 1) / BN;
+    const int32_t number = kn_xcd_order(kn_block(), blocks);
+    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, BM, number / ntiles);
+    const int j0 = number % ntiles * BN;
+    if (piece.begin >= piece.end) return;
+    const bool some = piece.group < p.E;
+    const int64_t group = some ? piece.group : 0;
+    const T *a = (const T *)p.a, *b = (const T *)p.b + group * p.b_group;
+    LoadA la;
+    la.start(wave, lane, [&](int r) {
+        const int32_t i = min(piece.begin + r, piece.end - 1);
+        const int32_t src = p.rows ? p.rows[i] : i;
+        return a + (int64_t)((uint32_t)src < (uint32_t)p.a_rows ? src : 0) * p.lda;
+    });
+    KnRowLoader<T, BN, NW> lbr;
+    KnColLoader<T, BN, NW> lbc;
+    constexpr int LOADS = LoadA::N + (COLS ? lbc.N : lbr.N);
+    if constexpr (COLS) lbc.start(wave, lane, b + j0, p.b_c, (p.J - j0) * (int)sizeof(T) / 16);
+    else lbr.start(wave, lane, [&](int r) { return b + (int64_t)min(j0 + r, p.J - 1) * p.b_j; });
+    const int32_t C = some ? p.C : 0, steps = (C + CS - 1) / CS;
+    auto fetch = [&](int s) {
+        KN_LDS char *tile = lds + (s & 1) * STAGE;
+        la.fetch(tile, wave, C - s * CS);
+        if constexpr (COLS) lbc.fetch(tile + BM * 128, wave, lane, C - s * CS);
+        else lbr.fetch(tile + BM * 128, wave, C - s * CS);
+    };
+    const int wi = (wave / WC) * (BM / WR), wj = (wave % WC) * (BN / WC);
+    kn_f32x4 acc[U][V] = {};
+    if (steps > 0) fetch(0);
+    for (int s = 0; s < steps; ++s) {
+        if (s + 1 < steps) {
+            fetch(s + 1);
+            KN_WAIT_LOADS(LOADS);
+        } else {
+            KN_WAIT_LOADS(0);
+        }
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const KN_LDS char *ta = lds + (s & 1) * STAGE, *tb = ta + BM * 128;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            Frag fa[U], fb[V];
+#pragma unroll
+            for (int u = 0; u < U; ++u) fa[u] = kn_row_frag<T>(ta, wi + 16 * u, kk, lane);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if constexpr (COLS) fb[v] = kn_col_frag<T, BN>(tb, wj + 16 * v, kk, lane);
+                else fb[v] = kn_row_frag<T>(tb, wj + 16 * v, kk, lane);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[v], fa[u], acc[u][v]);
+        }
+        kn_lds_read_barrier();
+    }
+    // 16 rows of the wavefront's results at a time, in LDS of its own
+    constexpr int WN = BN / WC, LD = WN + 4, LR = WN / 8; // LR lanes take a row
+    KN_LDS float *mine = (KN_LDS float *)(lds + wave * (16 * LD * 4));
+    const T *bias = (const T *)p.bias, *mask = (const T *)p.mask;
+    typedef T Out __attribute__((ext_vector_type(8)));
+    const int32_t j = j0 + wj + lane % LR * 8;
+    float add[8] = {};
+    if (bias && some && j < p.J) {
+        const Out v = *(const Out *)(bias + group * p.J + j);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) add[q] = (float)v[q];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) *(KN_LDS kn_f32x4 *)(mine + (lane & 15) * LD + 16 * v + (lane >> 4) * 4) = acc[u][v];
+#pragma unroll
+        for (int h = 0; h < 16 * LR / 64; ++h) {
+            const int r = h * (64 / LR) + lane / LR;
+            const int32_t i = piece.begin + wi + 16 * u + r;
+            const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + lane % LR * 8), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + lane % LR * 8 + 4);
+            if (i >= piece.end || j >= p.J) continue;
+            float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if (p.rows && (uint32_t)p.rows[i] >= (uint32_t)p.a_rows) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) y[q] = 0.0f;
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                y[q] += add[q];
+                if (p.relu) y[q] = y[q] > 0.0f || y[q] != y[q] ? y[q] : 0.0f; // (a NaN stays one)
+            }
+            if (mask && some) {
+                const int32_t src = p.mask_rows ? p.mask_rows[i] : i;
+                const bool there = (uint32_t)src < (uint32_t)p.m_rows;
+                const Out m = *(const Out *)(mask + (int64_t)(there ? src : 0) * p.ldm + j);
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    if (!there || !((float)m[q] > 0.0f)) y[q] = 0.0f;
+            }
+            Out o;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) o[q] = (T)y[q];
+            *(Out *)((T *)p.out + (int64_t)i * p.o_i + j) = o;
+        }
+    }
+}
+
+// Whether every row is made of whole 16-byte pieces that lie on multiples of 16 bytes, as k_product_rows takes them
+template <typename T> bool rows_of_pieces(const KnProduct &p)
+{
+    constexpr int64_t V = 16 / sizeof(T);
+    const uintptr_t at = (uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)p.bias | (uintptr_t)p.mask | (uintptr_t)p.out;
+    return (at & 15) == 0 && p.C % V == 0 && p.J % 8 == 0 && p.lda % V == 0 && (!p.mask || p.ldm % V == 0) && p.a_rows > 0 && (!p.mask || p.m_rows > 0);
+}
+
+template <typename T, bool COLS, int BM, int BN, int WR, int WC> int launch_rows(hipStream_t st, const KnProduct &p)
+{
+    const int64_t blocks = kn_pieces(p.M, p.E, BM) * kn_div_up(p.J, BN);
+    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
+    hipLaunchKernelGGL((k_product_rows<T, COLS, BM, BN, WR, WC>), dim3((unsigned)blocks), dim3(WR * WC * 64), 0, st, p, (int32_t)blocks);
+    KN_CHECK_LAUNCH();
+    return KN_OK;
+}
+
 template <typename T, bool REDUCE> int launch_any(hipStream_t st, const KnProduct &p)
 {
     const int64_t groups = REDUCE ? (int64_t)p.E * kn_div_up(p.I, ANY_TILE) : kn_pieces(p.M, p.E, ANY_TILE);
@@ -119,6 +253,12 @@ template <typename T, bool REDUCE> int launch_any(hipStream_t st, const KnProduc
     hipLaunchKernelGGL((k_product_any<T, REDUCE>), dim3((unsigned)blocks), dim3(256), 0, st, p);
     KN_CHECK_LAUNCH();
     return KN_OK;
+}
+
+template <typename T> int launch_forward(hipStream_t st, const KnProduct &p)
+{
+    if (!rows_of_pieces<T>(p)) return launch_any<T, false>(st, p);
+    return p.b_j == 1 ? launch_rows<T, true, 128, 128, 2, 2>(st, p) : launch_rows<T, false, 128, 128, 2, 2>(st, p);
 }
 
 // What the three calls check alike
@@ -148,7 +288,7 @@ extern "C" int kn_grouped_linear(void *stream, const kn_linear_desc *d, const vo
     p.o_i = d->n_out; p.o_j = 1;
     p.M = (int32_t)d->rows; p.E = d->experts; p.J = d->n_out; p.C = d->n_in;
     p.a_rows = (int32_t)d->x_rows; p.relu = relu != 0;
-    return kn_with_type(d->dtype, [&](auto v) { return launch_any<decltype(v), false>((hipStream_t)stream, p); });
+    return kn_with_type(d->dtype, [&](auto v) { return launch_forward<decltype(v)>((hipStream_t)stream, p); });
 }
 
 extern "C" int kn_grouped_linear_dx(void *stream, const kn_linear_desc *d, const void *dy, const void *w, const void *x_relu,
@@ -166,7 +306,7 @@ extern "C" int kn_grouped_linear_dx(void *stream, const kn_linear_desc *d, const
     p.M = (int32_t)d->rows; p.E = d->experts; p.J = d->n_in; p.C = d->n_out;
     p.a_rows = p.M; p.m_rows = (int32_t)d->x_rows;
     p.mask_rows = x_relu ? rows : nullptr;
-    return kn_with_type(d->dtype, [&](auto v) { return launch_any<decltype(v), false>((hipStream_t)stream, p); });
+    return kn_with_type(d->dtype, [&](auto v) { return launch_forward<decltype(v)>((hipStream_t)stream, p); });
 }
 
 extern "C" int kn_grouped_linear_dw(void *stream, const kn_linear_desc *d, const void *x, const void *dy, const int32_t *offsets,
