@@ -97,6 +97,6 @@ struct KnProduct {
     int64_t b_group, b_c, b_j;       // strides of b_e: network, contraction, column
     int64_t o_group, o_i, o_j;       // strides of out: network (weight gradient), row, column
     int32_t M, E, I, J, C;           // rows, networks; weight gradient: rows of out_e; columns of out; contraction
-    int32_t a_rows, m_rows;          // rows that a and the mask have (an index outside is a row of zeros)
+    int32_t a_rows, b_rows, m_rows;  // rows that a, b (weight gradient) and the mask have (an index outside is a row of zeros)
     int32_t relu;
 };

@@ -140,7 +140,6 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
     });
     KnRowLoader<T, BN, NW> lbr;
     KnColLoader<T, BN, NW> lbc;
-    constexpr int LOADS = LoadA::N + (COLS ? lbc.N : lbr.N);
     if constexpr (COLS) lbc.start(wave, lane, b + j0, p.b_c, (p.J - j0) * (int)sizeof(T) / 16);
     else lbr.start(wave, lane, [&](int r) { return b + (int64_t)min(j0 + r, p.J - 1) * p.b_j; });
     const int32_t C = some ? p.C : 0, steps = (C + CS - 1) / CS;
@@ -154,14 +153,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
     kn_f32x4 acc[U][V] = {};
     if (steps > 0) fetch(0);
     for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) {
-            fetch(s + 1);
-            KN_WAIT_LOADS(LOADS);
-        } else {
-            KN_WAIT_LOADS(0);
-        }
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        kn_stage_barrier();
+        if (s + 1 < steps) fetch(s + 1);
         const KN_LDS char *ta = lds + (s & 1) * STAGE, *tb = ta + BM * 128;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
@@ -178,8 +171,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
 #pragma unroll
                 for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[v], fa[u], acc[u][v]);
         }
-        kn_lds_read_barrier();
     }
+    kn_stage_barrier(); // (the tiles' LDS is used again)
     // 16 rows of the wavefront's results at a time, in LDS of its own
     constexpr int WN = BN / WC, LD = WN + 4, LR = WN / 8; // LR lanes take a row
     KN_LDS float *mine = (KN_LDS float *)(lds + wave * (16 * LD * 4));
@@ -261,6 +254,128 @@ template <typename T> int launch_forward(hipStream_t st, const KnProduct &p)
     return p.b_j == 1 ? launch_rows<T, true, 128, 128, 2, 2>(st, p) : launch_rows<T, false, 128, 128, 2, 2>(st, p);
 }
 
+// The weight gradient on tiles: both operands column-wise, the contraction is the network's rows, 128 bytes' worth a stage.  GATHER: 1,
+// 2: a's, b's rows are read through the index.  The columns' sums (gradient of the biases) are products with ones of the
+// fragments that are there anyway, in the workgroups of the first tile: SUM_B the columns of b, SUM_A those of a.
+enum { SUM_NONE, SUM_A, SUM_B };
+template <typename T, int GATHER, int BM, int BN, int WR, int WC>
+__global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, int32_t blocks, int32_t sum)
+{
+    constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16, CS = 128 / sizeof(T);
+    typedef typename KnFrag<T>::Type Frag;
+    __shared__ __align__(16) char lds_[2 * STAGE];
+    KN_LDS char *lds = (KN_LDS char *)lds_;
+    const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int jtiles = (p.J + BN - 1) / BN, itiles = (p.I + BM - 1) / BM;
+    int32_t number = kn_xcd_order(kn_block(), blocks);
+    const int j0 = number % jtiles * BN;
+    number /= jtiles;
+    const int i0 = number % itiles * BM, group = number / itiles;
+    const int32_t c0 = kn_offset(p.offsets, group, p.M), cend = max(c0, kn_offset(p.offsets, group + 1, p.M));
+    const int32_t steps = (cend - c0 + CS - 1) / CS;
+    const bool sum_a = sum == SUM_A && j0 == 0, sum_b = sum == SUM_B && i0 == 0;
+    KnGroupLoader<T, BM, NW, GATHER == 1> la;
+    KnGroupLoader<T, BN, NW, GATHER == 2> lb;
+    const int wi = (wave / WC) * (BM / WR), wj = (wave % WC) * (BN / WC);
+    kn_f32x4 acc[U][V] = {}, side[U > V ? U : V] = {};
+    Frag ones;
+#pragma unroll
+    for (int q = 0; q < (int)(sizeof(Frag) / sizeof(T)); ++q) ones[q] = (T)1.0f;
+    if (steps > 0) {
+        la.start(wave, lane, (const T *)p.a + i0, p.lda, (p.I - i0) * (int)sizeof(T) / 16, p.rows, p.a_rows, c0, cend);
+        lb.start(wave, lane, (const T *)p.b + j0, p.ldb, (p.J - j0) * (int)sizeof(T) / 16, p.rows, p.b_rows, c0, cend);
+        la.fetch(lds, wave, lane, c0);
+        lb.fetch(lds + BM * 128, wave, lane, c0);
+    }
+    for (int s = 0; s < steps; ++s) {
+        kn_stage_barrier();
+        if (s + 1 < steps) {
+            KN_LDS char *tile = lds + ((s + 1) & 1) * STAGE;
+            la.fetch(tile, wave, lane, c0 + (s + 1) * CS);
+            lb.fetch(tile + BM * 128, wave, lane, c0 + (s + 1) * CS);
+        }
+        const KN_LDS char *ta = lds + (s & 1) * STAGE, *tb = ta + BM * 128;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            Frag fa[U], fb[V];
+#pragma unroll
+            for (int u = 0; u < U; ++u) fa[u] = kn_col_frag<T, BM>(ta, wi + 16 * u, kk, lane);
+#pragma unroll
+            for (int v = 0; v < V; ++v) fb[v] = kn_col_frag<T, BN>(tb, wj + 16 * v, kk, lane);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[v], fa[u], acc[u][v]);
+            if (sum_a && wj == 0) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) side[u] = kn_mfma(ones, fa[u], side[u]);
+            }
+            if (sum_b && wi == 0) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) side[v] = kn_mfma(fb[v], ones, side[v]);
+            }
+        }
+    }
+    kn_stage_barrier(); // (the tiles' LDS is used again)
+    if (sum_a && wj == 0 && lane < 16) { // (each column of the product is alike: its 16 rows are the sums of 16 columns of a)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i0 + wi + 16 * u + lane < p.I) ((T *)p.out_bias)[(int64_t)group * p.I + i0 + wi + 16 * u + lane] = (T)side[u][0];
+    }
+    if (sum_b && wi == 0 && (lane & 15) == 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int j = j0 + wj + 16 * v + (lane >> 4) * 4 + r;
+                if (j < p.J) ((T *)p.out_bias)[(int64_t)group * p.J + j] = (T)side[v][r];
+            }
+    }
+    constexpr int WN = BN / WC, LD = WN + 4, LR = WN / 8;
+    KN_LDS float *mine = (KN_LDS float *)(lds + wave * (16 * LD * 4));
+    typedef T Out __attribute__((ext_vector_type(8)));
+    T *out = (T *)p.out + (int64_t)group * p.o_group;
+    const int32_t j = j0 + wj + lane % LR * 8;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) *(KN_LDS kn_f32x4 *)(mine + (lane & 15) * LD + 16 * v + (lane >> 4) * 4) = acc[u][v];
+#pragma unroll
+        for (int h = 0; h < 16 * LR / 64; ++h) {
+            const int r = h * (64 / LR) + lane / LR;
+            const int32_t i = i0 + wi + 16 * u + r;
+            const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + lane % LR * 8), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + lane % LR * 8 + 4);
+            if (i >= p.I || j >= p.J) continue;
+            const Out o = {(T)lo[0], (T)lo[1], (T)lo[2], (T)lo[3], (T)hi[0], (T)hi[1], (T)hi[2], (T)hi[3]};
+            *(Out *)(out + (int64_t)i * p.o_i + j) = o;
+        }
+    }
+}
+
+template <typename T, int GATHER> int launch_reduce(hipStream_t st, const KnProduct &p, int32_t sum)
+{
+    const int64_t blocks = (int64_t)p.E * kn_div_up(p.I, 128) * kn_div_up(p.J, 128);
+    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
+    hipLaunchKernelGGL((k_product_reduce<T, GATHER, 128, 128, 2, 2>), dim3((unsigned)blocks), dim3(256), 0, st, p, (int32_t)blocks, sum);
+    KN_CHECK_LAUNCH();
+    return KN_OK;
+}
+
+// q: the product with out's contiguous index as columns
+template <typename T> int launch_dw(hipStream_t st, const KnProduct &p)
+{
+    constexpr int64_t V = 16 / sizeof(T);
+    const uintptr_t at = (uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)p.out;
+    const bool pieces = (at & 15) == 0 && p.I % 8 == 0 && p.J % 8 == 0 && p.lda % V == 0 && p.ldb % V == 0;
+    if (!pieces) return launch_any<T, true>(st, p);
+    KnProduct q = p;
+    q.b_rows = p.M;
+    if (p.o_j == 1) return p.rows ? launch_reduce<T, 1>(st, q, p.out_bias ? SUM_B : SUM_NONE) : launch_reduce<T, 0>(st, q, p.out_bias ? SUM_B : SUM_NONE);
+    q.a = p.b; q.b = p.a; q.lda = p.ldb; q.ldb = p.lda; q.a_rows = p.M; q.b_rows = p.a_rows;
+    q.I = p.J; q.J = p.I; q.o_i = p.o_j; q.o_j = p.o_i;
+    return p.rows ? launch_reduce<T, 2>(st, q, p.out_bias ? SUM_A : SUM_NONE) : launch_reduce<T, 0>(st, q, p.out_bias ? SUM_A : SUM_NONE);
+}
+
 // What the three calls check alike
 int check(const kn_linear_desc *d)
 {
@@ -321,5 +436,5 @@ extern "C" int kn_grouped_linear_dw(void *stream, const kn_linear_desc *d, const
     p.o_group = (int64_t)d->n_in * d->n_out; p.o_i = io ? d->n_out : 1; p.o_j = io ? 1 : d->n_in;
     p.M = (int32_t)d->rows; p.E = d->experts; p.I = d->n_in; p.J = d->n_out;
     p.a_rows = (int32_t)d->x_rows;
-    return kn_with_type(d->dtype, [&](auto v) { return launch_any<decltype(v), true>((hipStream_t)stream, p); });
+    return kn_with_type(d->dtype, [&](auto v) { return launch_dw<decltype(v)>((hipStream_t)stream, p); });
 }

@@ -116,12 +116,56 @@ template <typename T, int W, int NW> struct KnColLoader {
     }
 };
 
-// Everything this wavefront has asked for but the last `n` loads is there
-#define KN_WAIT_LOADS(n) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory")
-// what this wavefront reads from the LDS has arrived; every wavefront of the workgroup is here
-__device__ __forceinline__ void kn_lds_read_barrier()
+// A column-wise tile whose rows are those of one network, through an index or not: the numbers of the next stage's rows are
+// asked for before this stage's values, so that they are there when that stage is fetched.
+template <typename T, int W, int NW, bool INDEX> struct KnGroupLoader {
+    static constexpr int CS = 128 / sizeof(T), PR = W * sizeof(T) / 16, RP = 64 / PR, N = CS / RP / NW;
+    int32_t next[N];
+    int at[N]; // bytes of this lane's piece in a row
+    const char *base;
+    const int32_t *index;
+    int64_t stride;
+    int32_t rows, last; // rows that there are; the network's last
+    __device__ __forceinline__ int row(int wave, int lane, int t) const { return (wave * N + t) * RP + lane / PR; }
+    __device__ __forceinline__ void ask(int wave, int lane, int32_t c0)
+    {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const int32_t c = min(c0 + row(wave, lane, t), last);
+            next[t] = INDEX ? index[c] : c;
+        }
+    }
+    // first: the tile's first column; c0: the network's first row
+    __device__ __forceinline__ void start(int wave, int lane, const T *first, int64_t ld, int pieces, const int32_t *idx, int32_t n, int32_t c0, int32_t cend)
+    {
+        base = (const char *)first;
+        stride = ld * (int64_t)sizeof(T);
+        index = idx;
+        rows = n;
+        last = cend - 1;
+#pragma unroll
+        for (int t = 0; t < N; ++t) at[t] = min((lane % PR) ^ kn_col_swizzle<T>(row(wave, lane, t)), pieces - 1) * 16;
+        ask(wave, lane, c0);
+    }
+    __device__ __forceinline__ void fetch(KN_LDS char *tile, int wave, int lane, int32_t c0)
+    {
+        int32_t now[N];
+#pragma unroll
+        for (int t = 0; t < N; ++t) now[t] = next[t];
+        ask(wave, lane, c0 + CS);
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const bool there = c0 + row(wave, lane, t) <= last && (uint32_t)now[t] < (uint32_t)rows;
+            kn_fetch(there ? base + (int64_t)now[t] * stride + at[t] : (const char *)&kn_zeros, tile + (wave * N + t) * 1024);
+        }
+    }
+};
+
+// Between two stages: what this wavefront asked for has arrived in the LDS, what it read there has arrived in registers, and so for every
+// wavefront of the workgroup.  The buffer read before may be fetched into again, the one fetched may be read.
+__device__ __forceinline__ void kn_stage_barrier()
 {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
