@@ -111,6 +111,45 @@ __global__ void __launch_bounds__(256) k_product_any(KnProduct p)
             }
 }
 
+// What is added to columns j .. j + 7 of a network's results (j a multiple of 8)
+template <typename T> __device__ __forceinline__ void bias_of(const KnProduct &p, bool some, int64_t group, int32_t j, float add[8])
+{
+    typedef T Piece __attribute__((ext_vector_type(8)));
+#pragma unroll
+    for (int q = 0; q < 8; ++q) add[q] = 0.0f;
+    if (p.bias && some && j < p.J) {
+        const Piece v = *(const Piece *)((const T *)p.bias + group * p.J + j);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) add[q] = (float)v[q];
+    }
+}
+// The end of 8 neighbouring results of row i: zeros for a row that x does not have, bias, ReLU, the mask of a ReLU before; one rounding
+template <typename T> __device__ __forceinline__ void finish(const KnProduct &p, bool some, int64_t group, int32_t i, int32_t j, const float add[8], float y[8])
+{
+    typedef T Piece __attribute__((ext_vector_type(8)));
+    if (p.rows && (uint32_t)p.rows[i] >= (uint32_t)p.a_rows) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) y[q] = 0.0f;
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        y[q] += add[q];
+        if (p.relu) y[q] = y[q] > 0.0f || y[q] != y[q] ? y[q] : 0.0f; // (a NaN stays one)
+    }
+    if (p.mask && some) {
+        const int32_t src = p.mask_rows ? p.mask_rows[i] : i;
+        const bool there = (uint32_t)src < (uint32_t)p.m_rows;
+        const Piece m = *(const Piece *)((const T *)p.mask + (int64_t)(there ? src : 0) * p.ldm + j);
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (!there || !((float)m[q] > 0.0f)) y[q] = 0.0f;
+    }
+    Piece o;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) o[q] = (T)y[q];
+    *(Piece *)((T *)p.out + (int64_t)i * p.o_i + j) = o;
+}
+
 // Rows of 16-byte pieces throughout: tiles of BM x BN results, WR x WC wavefronts, two stages in the LDS, of which one is
 // fetched while the other is multiplied.  COLS: b's columns are contiguous in memory (else its contraction is).
 // Fragments of b are the products' first operand, so that a lane holds four neighbouring results of a row; they go through
@@ -151,40 +190,47 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
     };
     const int wi = (wave / WC) * (BM / WR), wj = (wave % WC) * (BN / WC);
     kn_f32x4 acc[U][V] = {};
-    if (steps > 0) fetch(0);
-    for (int s = 0; s < steps; ++s) {
-        kn_stage_barrier();
-        if (s + 1 < steps) fetch(s + 1);
+    Frag fa[2][U], fb[2][V];
+    auto read = [&](int s, int kk) {
         const KN_LDS char *ta = lds + (s & 1) * STAGE, *tb = ta + BM * 128;
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            Frag fa[U], fb[V];
+        for (int u = 0; u < U; ++u) fa[kk][u] = kn_row_frag<T>(ta, wi + 16 * u, kk, lane);
 #pragma unroll
-            for (int u = 0; u < U; ++u) fa[u] = kn_row_frag<T>(ta, wi + 16 * u, kk, lane);
+        for (int v = 0; v < V; ++v) {
+            if constexpr (COLS) fb[kk][v] = kn_col_frag<T, BN>(tb, wj + 16 * v, kk, lane);
+            else fb[kk][v] = kn_row_frag<T>(tb, wj + 16 * v, kk, lane);
+        }
+    };
+    auto multiply = [&](int kk) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if constexpr (COLS) fb[v] = kn_col_frag<T, BN>(tb, wj + 16 * v, kk, lane);
-                else fb[v] = kn_row_frag<T>(tb, wj + 16 * v, kk, lane);
-            }
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[v], fa[u], acc[u][v]);
+            for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[kk][v], fa[kk][u], acc[u][v]);
+    };
+    // Half a stage's fragments are read while the other half's are multiplied; the barrier between stages lies in between.
+    if (steps > 0) {
+        fetch(0);
+        kn_stage_barrier();
+        if (steps > 1) fetch(1);
+        read(0, 0);
+        for (int s = 0; s < steps; ++s) {
+            read(s, 1);
+            multiply(0);
+            kn_interleave<U, V, T, COLS>();
+            kn_stage_barrier();
+            if (s + 2 < steps) fetch(s + 2);
+            read(s + 1, 0); // (behind the last stage: what happens to lie there, unused)
+            multiply(1);
+            kn_interleave<U, V, T, COLS>();
         }
     }
     kn_stage_barrier(); // (the tiles' LDS is used again)
     // 16 rows of the wavefront's results at a time, in LDS of its own
     constexpr int WN = BN / WC, LD = WN + 4, LR = WN / 8; // LR lanes take a row
     KN_LDS float *mine = (KN_LDS float *)(lds + wave * (16 * LD * 4));
-    const T *bias = (const T *)p.bias, *mask = (const T *)p.mask;
-    typedef T Out __attribute__((ext_vector_type(8)));
     const int32_t j = j0 + wj + lane % LR * 8;
-    float add[8] = {};
-    if (bias && some && j < p.J) {
-        const Out v = *(const Out *)(bias + group * p.J + j);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) add[q] = (float)v[q];
-    }
+    float add[8];
+    bias_of<T>(p, some, group, j, add);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -196,27 +242,131 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
             const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + lane % LR * 8), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + lane % LR * 8 + 4);
             if (i >= piece.end || j >= p.J) continue;
             float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            if (p.rows && (uint32_t)p.rows[i] >= (uint32_t)p.a_rows) {
+            finish<T>(p, some, group, i, j, add, y);
+        }
+    }
+}
+
+// Few rows per network: the weights are read once, straight into the registers they are multiplied from, 16 bytes a lane and load,
+// and no tile is kept.  A workgroup makes 16 MB rows of FEW_COLS results; its FEW_WAVES wavefronts take every FEW_WAVES-th step of the
+// contraction and are summed at the end, in the order of their numbers.
+//  - COLS (columns contiguous): lane l takes R = 16 / sizeof(T) columns from R (l % 16) on, of the R rows of the contraction from
+//    R (l / 16) on: an R x R square, whose transpose is, per column j of it, one product's fragment: column j of every lane's square.
+//    16-bit squares are turned by byte permutations of register pairs, fp32 ones by naming.
+//  - else (contraction contiguous): lane l takes R values of the contraction of column l % 16 of a tile of 16.
+constexpr int FEW_WAVES = 8;
+template <typename T, bool COLS> struct FewCols { static constexpr int N = COLS ? 256 / sizeof(T) : 64; };
+template <typename T, bool COLS, int MB>
+__global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p, int32_t blocks)
+{
+    constexpr int R = 16 / sizeof(T), BN = FewCols<T, COLS>::N, SETS = BN / 16; // SETS products per fragment of a
+    constexpr int KS = COLS ? 4 * R : 8 * R;      // contraction of a step: 8 loads of 16 bytes (fp32 columns: 4)
+    constexpr int PARTS = COLS ? 1 : 2, LOADS = COLS ? R : SETS * PARTS, LD = BN + 4;
+    typedef typename KnFrag<T>::Type Frag;
+    __shared__ __align__(16) float red[FEW_WAVES * 16 * LD];
+    const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ntiles = (p.J + BN - 1) / BN;
+    const int32_t number = kn_xcd_order(kn_block(), blocks);
+    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, 16 * MB, number / ntiles);
+    const int j0 = number % ntiles * BN;
+    if (piece.begin >= piece.end) return;
+    const bool some = piece.group < p.E;
+    const int64_t group = some ? piece.group : 0;
+    const T *b = (const T *)p.b + group * p.b_group;
+    const int col = lane & 15, g = lane >> 4;
+    const T *arow[MB];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) y[q] = 0.0f;
+    for (int m = 0; m < MB; ++m) {
+        const int32_t i = min(piece.begin + 16 * m + col, piece.end - 1);
+        const int32_t src = p.rows ? p.rows[i] : i;
+        arow[m] = (const T *)p.a + (int64_t)((uint32_t)src < (uint32_t)p.a_rows ? src : 0) * p.lda;
+    }
+    const T *bat[COLS ? 1 : SETS];
+    if constexpr (COLS) bat[0] = b + min(j0 + R * col, p.J - R);
+    else
+#pragma unroll
+        for (int v = 0; v < SETS; ++v) bat[v] = b + (int64_t)min(j0 + 16 * v + col, p.J - 1) * p.b_j;
+    const int32_t C = some ? p.C : 0, steps = (C + KS - 1) / KS;
+    kn_f32x4 acc[MB][SETS] = {};
+    struct Step { kn_u32x4 a[MB][PARTS], b[LOADS]; };
+    auto load = [&](Step &x, int s) {
+        const int32_t c = s * KS;
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) { // (pieces behind the contraction's end: zeros, both of a and b)
+            const int32_t k = c + q * 4 * R + R * g;
+            const bool there = k < C;
+            const kn_u32x4 none = {0, 0, 0, 0};
+#pragma unroll
+            for (int m = 0; m < MB; ++m) x.a[m][q] = there ? *(const kn_u32x4 *)(arow[m] + k) : none;
+            if constexpr (COLS) {
+#pragma unroll
+                for (int t = 0; t < R; ++t) x.b[t] = there ? *(const kn_u32x4 *)(bat[0] + (int64_t)(k + t) * p.b_c) : none;
+            } else {
+#pragma unroll
+                for (int v = 0; v < SETS; ++v) x.b[v * PARTS + q] = there ? *(const kn_u32x4 *)(bat[v] + k) : none;
             }
+        }
+    };
+    auto multiply = [&](const Step &x) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                y[q] += add[q];
-                if (p.relu) y[q] = y[q] > 0.0f || y[q] != y[q] ? y[q] : 0.0f; // (a NaN stays one)
+        for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+            for (int v = 0; v < SETS; ++v) {
+                union { kn_u32x4 u; Frag f; } fb, fa;
+                if constexpr (!COLS) fb.u = x.b[v * PARTS + q];
+                else if constexpr (sizeof(T) == 4) fb.u = kn_u32x4{x.b[0][v], x.b[1][v], x.b[2][v], x.b[3][v]};
+                else
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) // columns 2 (v / 2) and + 1 of rows 2 t and 2 t + 1: the lower or the upper halves
+                        fb.u[t] = __builtin_amdgcn_perm(x.b[2 * t + 1][v / 2], x.b[2 * t][v / 2], v & 1 ? 0x07060302 : 0x05040100);
+#pragma unroll
+                for (int m = 0; m < MB; ++m) {
+                    fa.u = x.a[m][q];
+                    acc[m][v] = kn_mfma(fb.f, fa.f, acc[m][v]);
+                }
             }
-            if (mask && some) {
-                const int32_t src = p.mask_rows ? p.mask_rows[i] : i;
-                const bool there = (uint32_t)src < (uint32_t)p.m_rows;
-                const Out m = *(const Out *)(mask + (int64_t)(there ? src : 0) * p.ldm + j);
+    };
+    Step even, odd;
+    int s = wave;
+    if (s < steps) load(even, s);
+    while (s < steps) {
+        if (s + FEW_WAVES < steps) load(odd, s + FEW_WAVES);
+        multiply(even);
+        s += FEW_WAVES;
+        if (s >= steps) break;
+        if (s + FEW_WAVES < steps) load(even, s + FEW_WAVES);
+        multiply(odd);
+        s += FEW_WAVES;
+    }
 #pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    if (!there || !((float)m[q] > 0.0f)) y[q] = 0.0f;
+    for (int m = 0; m < MB; ++m) {
+        if (m) __syncthreads();
+        float *mine = red + (wave * 16 + col) * LD;
+        if constexpr (COLS) { // register r of set v: column R (4 g + r) + v
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int v = 0; v < SETS; v += 4)
+                    *(kn_f32x4 *)(mine + R * (4 * g + r) + v) = kn_f32x4{acc[m][v][r], acc[m][v + 1][r], acc[m][v + 2][r], acc[m][v + 3][r]};
+        } else {
+#pragma unroll
+            for (int v = 0; v < SETS; ++v) *(kn_f32x4 *)(mine + 16 * v + 4 * g) = acc[m][v];
+        }
+        __syncthreads();
+        for (int q = tid; q < 16 * BN / 8; q += FEW_WAVES * 64) {
+            const int r = q / (BN / 8), cj = q % (BN / 8) * 8;
+            const int32_t i = piece.begin + 16 * m + r, j = j0 + cj;
+            if (i >= piece.end || j >= p.J) continue;
+            float y[8] = {};
+#pragma unroll
+            for (int w = 0; w < FEW_WAVES; ++w) {
+                const kn_f32x4 lo = *(const kn_f32x4 *)(red + (w * 16 + r) * LD + cj), hi = *(const kn_f32x4 *)(red + (w * 16 + r) * LD + cj + 4);
+#pragma unroll
+                for (int n = 0; n < 4; ++n) { y[n] += lo[n]; y[n + 4] += hi[n]; }
             }
-            Out o;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) o[q] = (T)y[q];
-            *(Out *)((T *)p.out + (int64_t)i * p.o_i + j) = o;
+            float add[8];
+            bias_of<T>(p, some, group, j, add);
+            finish<T>(p, some, group, i, j, add, y);
         }
     }
 }
@@ -248,10 +398,27 @@ template <typename T, bool REDUCE> int launch_any(hipStream_t st, const KnProduc
     return KN_OK;
 }
 
+template <typename T, bool COLS, int MB> int launch_few(hipStream_t st, const KnProduct &p)
+{
+    const int64_t blocks = kn_pieces(p.M, p.E, 16 * MB) * kn_div_up(p.J, FewCols<T, COLS>::N);
+    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
+    hipLaunchKernelGGL((k_product_few<T, COLS, MB>), dim3((unsigned)blocks), dim3(FEW_WAVES * 64), 0, st, p, (int32_t)blocks);
+    KN_CHECK_LAUNCH();
+    return KN_OK;
+}
+
+template <typename T, bool COLS> int launch_pieces(hipStream_t st, const KnProduct &p)
+{
+    const int64_t each = p.M / p.E; // rows of a network, on average
+    if (each <= 16) return launch_few<T, COLS, 1>(st, p);
+    if (each <= 32) return launch_few<T, COLS, 2>(st, p);
+    return launch_rows<T, COLS, 128, 128, 2, 2>(st, p);
+}
+
 template <typename T> int launch_forward(hipStream_t st, const KnProduct &p)
 {
     if (!rows_of_pieces<T>(p)) return launch_any<T, false>(st, p);
-    return p.b_j == 1 ? launch_rows<T, true, 128, 128, 2, 2>(st, p) : launch_rows<T, false, 128, 128, 2, 2>(st, p);
+    return p.b_j == 1 ? launch_pieces<T, true>(st, p) : launch_pieces<T, false>(st, p);
 }
 
 // The weight gradient on tiles: both operands column-wise, the contraction is the network's rows, 128 bytes' worth a stage.  GATHER: 1,
@@ -281,39 +448,53 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
     Frag ones;
 #pragma unroll
     for (int q = 0; q < (int)(sizeof(Frag) / sizeof(T)); ++q) ones[q] = (T)1.0f;
+    Frag fa[2][U], fb[2][V];
+    auto fetch = [&](int s) {
+        KN_LDS char *tile = lds + (s & 1) * STAGE;
+        la.fetch(tile, wave, lane, c0 + s * CS);
+        lb.fetch(tile + BM * 128, wave, lane, c0 + s * CS);
+    };
+    auto read = [&](int s, int kk) {
+        const KN_LDS char *ta = lds + (s & 1) * STAGE, *tb = ta + BM * 128;
+#pragma unroll
+        for (int u = 0; u < U; ++u) fa[kk][u] = kn_col_frag<T, BM>(ta, wi + 16 * u, kk, lane);
+#pragma unroll
+        for (int v = 0; v < V; ++v) fb[kk][v] = kn_col_frag<T, BN>(tb, wj + 16 * v, kk, lane);
+    };
+    auto multiply = [&](int kk) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[kk][v], fa[kk][u], acc[u][v]);
+    };
+    auto add_up = [&](int kk) {
+        if (sum_a && wj == 0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) side[u] = kn_mfma(ones, fa[kk][u], side[u]);
+        }
+        if (sum_b && wi == 0) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) side[v] = kn_mfma(fb[kk][v], ones, side[v]);
+        }
+    };
     if (steps > 0) {
         la.start(wave, lane, (const T *)p.a + i0, p.lda, (p.I - i0) * (int)sizeof(T) / 16, p.rows, p.a_rows, c0, cend);
         lb.start(wave, lane, (const T *)p.b + j0, p.ldb, (p.J - j0) * (int)sizeof(T) / 16, p.rows, p.b_rows, c0, cend);
-        la.fetch(lds, wave, lane, c0);
-        lb.fetch(lds + BM * 128, wave, lane, c0);
-    }
-    for (int s = 0; s < steps; ++s) {
+        fetch(0);
         kn_stage_barrier();
-        if (s + 1 < steps) {
-            KN_LDS char *tile = lds + ((s + 1) & 1) * STAGE;
-            la.fetch(tile, wave, lane, c0 + (s + 1) * CS);
-            lb.fetch(tile + BM * 128, wave, lane, c0 + (s + 1) * CS);
-        }
-        const KN_LDS char *ta = lds + (s & 1) * STAGE, *tb = ta + BM * 128;
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            Frag fa[U], fb[V];
-#pragma unroll
-            for (int u = 0; u < U; ++u) fa[u] = kn_col_frag<T, BM>(ta, wi + 16 * u, kk, lane);
-#pragma unroll
-            for (int v = 0; v < V; ++v) fb[v] = kn_col_frag<T, BN>(tb, wj + 16 * v, kk, lane);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[v], fa[u], acc[u][v]);
-            if (sum_a && wj == 0) {
-#pragma unroll
-                for (int u = 0; u < U; ++u) side[u] = kn_mfma(ones, fa[u], side[u]);
-            }
-            if (sum_b && wi == 0) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) side[v] = kn_mfma(fb[v], ones, side[v]);
-            }
+        if (steps > 1) fetch(1);
+        read(0, 0);
+        for (int s = 0; s < steps; ++s) {
+            add_up(0);
+            read(s, 1);
+            multiply(0);
+            kn_interleave<U, V, T, true, true>();
+            kn_stage_barrier();
+            if (s + 2 < steps) fetch(s + 2);
+            add_up(1);
+            read(s + 1, 0); // (behind the last stage: what happens to lie there, unused)
+            multiply(1);
+            kn_interleave<U, V, T, true, true>();
         }
     }
     kn_stage_barrier(); // (the tiles' LDS is used again)

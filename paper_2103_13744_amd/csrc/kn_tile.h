@@ -170,6 +170,18 @@ __device__ __forceinline__ void kn_stage_barrier()
     asm volatile("" ::: "memory");
 }
 
+// Order of the instructions since the last such mark: the fragments' reads spread among the products.
+template <int U, int V, typename T, bool COLS_B, bool COLS_A = false> __device__ __forceinline__ void kn_interleave()
+{
+    constexpr int PER_COL = sizeof(T) == 2 ? 2 : 4, READS = U * (COLS_A ? PER_COL : 1) + V * (COLS_B ? PER_COL : 1);
+    constexpr int PRODUCTS = U * V * (sizeof(T) == 2 ? 1 : 4), EACH = PRODUCTS / READS > 0 ? PRODUCTS / READS : 1;
+#pragma unroll
+    for (int i = 0; i < READS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0); // an LDS read
+        __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0); // products
+    }
+}
+
 // A workgroup's number such that those of one XCD (every eighth) are neighbours and share what they read in its L2
 __device__ __forceinline__ int32_t kn_xcd_order(int32_t b, int32_t n)
 {
