@@ -154,13 +154,14 @@ template <typename T> __device__ __forceinline__ void finish(const KnProduct &p,
 // fetched while the other is multiplied.  COLS: b's columns are contiguous in memory (else its contraction is).
 // Fragments of b are the products' first operand, so that a lane holds four neighbouring results of a row; they go through
 // the LDS once more to leave in pieces of 8.
-template <typename T, bool COLS, int BM, int BN, int WR, int WC>
+template <typename T, bool COLS, int BM, int BN, int WR, int WC, int NB>
 __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int32_t blocks)
 {
     constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16, CS = 128 / sizeof(T);
     typedef typename KnFrag<T>::Type Frag;
     typedef KnRowLoader<T, BM, NW> LoadA;
-    __shared__ __align__(16) char lds_[2 * STAGE];
+    constexpr int BYTES = NB * STAGE > NW * 16 * (BN / WC + 4) * 4 ? NB * STAGE : NW * 16 * (BN / WC + 4) * 4;
+    __shared__ __align__(16) char lds_[BYTES];
     KN_LDS char *lds = (KN_LDS char *)lds_;
     const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ntiles = (p.J + BN - 1) / BN;
@@ -182,8 +183,9 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
     if constexpr (COLS) lbc.start(wave, lane, b + j0, p.b_c, (p.J - j0) * (int)sizeof(T) / 16);
     else lbr.start(wave, lane, [&](int r) { return b + (int64_t)min(j0 + r, p.J - 1) * p.b_j; });
     const int32_t C = some ? p.C : 0, steps = (C + CS - 1) / CS;
-    auto fetch = [&](int s) {
-        KN_LDS char *tile = lds + (s & 1) * STAGE;
+    constexpr int LOADS = LoadA::N + (COLS ? lbc.N : lbr.N); // a wavefront's, per stage
+    auto fetch = [&](int s, int at) {
+        KN_LDS char *tile = lds + at * STAGE;
         la.fetch(tile, wave, C - s * CS);
         if constexpr (COLS) lbc.fetch(tile + BM * 128, wave, lane, C - s * CS);
         else lbr.fetch(tile + BM * 128, wave, C - s * CS);
@@ -191,8 +193,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
     const int wi = (wave / WC) * (BM / WR), wj = (wave % WC) * (BN / WC);
     kn_f32x4 acc[U][V] = {};
     Frag fa[2][U], fb[2][V];
-    auto read = [&](int s, int kk) {
-        const KN_LDS char *ta = lds + (s & 1) * STAGE, *tb = ta + BM * 128;
+    auto read = [&](int at, int kk) {
+        const KN_LDS char *ta = lds + at * STAGE, *tb = ta + BM * 128;
 #pragma unroll
         for (int u = 0; u < U; ++u) fa[kk][u] = kn_row_frag<T>(ta, wi + 16 * u, kk, lane);
 #pragma unroll
@@ -207,28 +209,34 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
 #pragma unroll
             for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[kk][v], fa[kk][u], acc[u][v]);
     };
-    // Half a stage's fragments are read while the other half's are multiplied; the barrier between stages lies in between.
+    // Half a stage's fragments are read while the other half's are multiplied; in between, the next stage has to have arrived, and the
+    // one behind the NB that lie in the LDS takes the place of the one that everybody has just read.
     if (steps > 0) {
-        fetch(0);
-        kn_stage_barrier();
-        if (steps > 1) fetch(1);
+        for (int s = 0; s < NB && s < steps; ++s) fetch(s, s);
+        if (steps >= NB) kn_stage_barrier<(NB - 1) * LOADS>();
+        else kn_stage_barrier<0>();
         read(0, 0);
-        for (int s = 0; s < steps; ++s) {
-            read(s, 1);
+        for (int s = 0, at = 0; s < steps; ++s) {
+            const int next = at + 1 == NB ? 0 : at + 1;
+            read(at, 1);
             multiply(0);
             kn_interleave<U, V, T, COLS>();
-            kn_stage_barrier();
-            if (s + 2 < steps) fetch(s + 2);
-            read(s + 1, 0); // (behind the last stage: what happens to lie there, unused)
+            if (s + NB <= steps) kn_stage_barrier<(NB - 2) * LOADS>();
+            else kn_stage_barrier<0>();
+            if (s + NB < steps) fetch(s + NB, at);
+            read(next, 0); // (behind the last stage: what happens to lie there, unused)
             multiply(1);
             kn_interleave<U, V, T, COLS>();
+            at = next;
         }
     }
     kn_stage_barrier(); // (the tiles' LDS is used again)
     // 16 rows of the wavefront's results at a time, in LDS of its own
     constexpr int WN = BN / WC, LD = WN + 4, LR = WN / 8; // LR lanes take a row
     KN_LDS float *mine = (KN_LDS float *)(lds + wave * (16 * LD * 4));
-    const int32_t j = j0 + wj + lane % LR * 8;
+    static_assert(64 % LR == 0, "");
+    const int cj = lane % LR * 8;
+    const int32_t j = j0 + wj + cj;
     float add[8];
     bias_of<T>(p, some, group, j, add);
 #pragma unroll
@@ -236,95 +244,65 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
 #pragma unroll
         for (int v = 0; v < V; ++v) *(KN_LDS kn_f32x4 *)(mine + (lane & 15) * LD + 16 * v + (lane >> 4) * 4) = acc[u][v];
 #pragma unroll
-        for (int h = 0; h < 16 * LR / 64; ++h) {
+        for (int h = 0; h < (16 * LR + 63) / 64; ++h) {
             const int r = h * (64 / LR) + lane / LR;
             const int32_t i = piece.begin + wi + 16 * u + r;
-            const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + lane % LR * 8), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + lane % LR * 8 + 4);
-            if (i >= piece.end || j >= p.J) continue;
+            if (r >= 16 || i >= piece.end || j >= p.J) continue;
+            const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj + 4);
             float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
             finish<T>(p, some, group, i, j, add, y);
         }
     }
 }
 
-// Few rows per network: the weights are read once, straight into the registers they are multiplied from, 16 bytes a lane and load,
-// and no tile is kept.  A workgroup makes 16 MB rows of FEW_COLS results; its FEW_WAVES wavefronts take every FEW_WAVES-th step of the
-// contraction and are summed at the end, in the order of their numbers.
-//  - COLS (columns contiguous): lane l takes R = 16 / sizeof(T) columns from R (l % 16) on, of the R rows of the contraction from
-//    R (l / 16) on: an R x R square, whose transpose is, per column j of it, one product's fragment: column j of every lane's square.
-//    16-bit squares are turned by byte permutations of register pairs, fp32 ones by naming.
-//  - else (contraction contiguous): lane l takes R values of the contraction of column l % 16 of a tile of 16.
+// A row or none per network: the weights are read once, straight into the registers they are multiplied from, 16 bytes a lane and load.
+// A workgroup makes 16 rows of FEW_COLS results; its FEW_WAVES wavefronts take every FEW_WAVES-th step of the contraction and are
+// summed at the end, in the order of their numbers.  Columns contiguous in memory: lane l takes R = 16 / sizeof(T) columns from
+// R (l % 16) on, of the R rows of the contraction from R (l / 16) on: an R x R square, whose transpose is, per column j of it, one
+// product's fragment: column j of every lane's square.  16-bit squares are turned by byte permutations of register pairs, fp32
+// ones by naming.
 constexpr int FEW_WAVES = 8;
-template <typename T, bool COLS> struct FewCols { static constexpr int N = COLS ? 256 / sizeof(T) : 64; };
-template <typename T, bool COLS, int MB>
+template <typename T>
 __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p, int32_t blocks)
 {
-    constexpr int R = 16 / sizeof(T), BN = FewCols<T, COLS>::N, SETS = BN / 16; // SETS products per fragment of a
-    constexpr int KS = COLS ? 4 * R : 8 * R;      // contraction of a step: 8 loads of 16 bytes (fp32 columns: 4)
-    constexpr int PARTS = COLS ? 1 : 2, LOADS = COLS ? R : SETS * PARTS, LD = BN + 4;
+    constexpr int R = 16 / sizeof(T), BN = 16 * R, KS = 4 * R, LD = BN + 4;
     typedef typename KnFrag<T>::Type Frag;
     __shared__ __align__(16) float red[FEW_WAVES * 16 * LD];
     const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ntiles = (p.J + BN - 1) / BN;
     const int32_t number = kn_xcd_order(kn_block(), blocks);
-    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, 16 * MB, number / ntiles);
+    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, 16, number / ntiles);
     const int j0 = number % ntiles * BN;
     if (piece.begin >= piece.end) return;
     const bool some = piece.group < p.E;
     const int64_t group = some ? piece.group : 0;
-    const T *b = (const T *)p.b + group * p.b_group;
     const int col = lane & 15, g = lane >> 4;
-    const T *arow[MB];
-#pragma unroll
-    for (int m = 0; m < MB; ++m) {
-        const int32_t i = min(piece.begin + 16 * m + col, piece.end - 1);
-        const int32_t src = p.rows ? p.rows[i] : i;
-        arow[m] = (const T *)p.a + (int64_t)((uint32_t)src < (uint32_t)p.a_rows ? src : 0) * p.lda;
-    }
-    const T *bat[COLS ? 1 : SETS];
-    if constexpr (COLS) bat[0] = b + min(j0 + R * col, p.J - R);
-    else
-#pragma unroll
-        for (int v = 0; v < SETS; ++v) bat[v] = b + (int64_t)min(j0 + 16 * v + col, p.J - 1) * p.b_j;
+    const int32_t row = min(piece.begin + col, piece.end - 1), src = p.rows ? p.rows[row] : row;
+    const T *arow = (const T *)p.a + (int64_t)((uint32_t)src < (uint32_t)p.a_rows ? src : 0) * p.lda;
+    const T *brow = (const T *)p.b + group * p.b_group + min(j0 + R * col, p.J - R);
     const int32_t C = some ? p.C : 0, steps = (C + KS - 1) / KS;
-    kn_f32x4 acc[MB][SETS] = {};
-    struct Step { kn_u32x4 a[MB][PARTS], b[LOADS]; };
+    kn_f32x4 acc[R] = {};
+    struct Step { kn_u32x4 a, b[R]; };
     auto load = [&](Step &x, int s) {
-        const int32_t c = s * KS;
+        const int32_t k = s * KS + R * g;
+        const kn_u32x4 none = {0, 0, 0, 0}; // (behind the contraction's end: zeros, of a and of b)
+        const bool there = k < C;
+        x.a = there ? *(const kn_u32x4 *)(arow + k) : none;
 #pragma unroll
-        for (int q = 0; q < PARTS; ++q) { // (pieces behind the contraction's end: zeros, both of a and b)
-            const int32_t k = c + q * 4 * R + R * g;
-            const bool there = k < C;
-            const kn_u32x4 none = {0, 0, 0, 0};
-#pragma unroll
-            for (int m = 0; m < MB; ++m) x.a[m][q] = there ? *(const kn_u32x4 *)(arow[m] + k) : none;
-            if constexpr (COLS) {
-#pragma unroll
-                for (int t = 0; t < R; ++t) x.b[t] = there ? *(const kn_u32x4 *)(bat[0] + (int64_t)(k + t) * p.b_c) : none;
-            } else {
-#pragma unroll
-                for (int v = 0; v < SETS; ++v) x.b[v * PARTS + q] = there ? *(const kn_u32x4 *)(bat[v] + k) : none;
-            }
-        }
+        for (int t = 0; t < R; ++t) x.b[t] = there ? *(const kn_u32x4 *)(brow + (int64_t)(k + t) * p.b_c) : none;
     };
     auto multiply = [&](const Step &x) {
+        union { kn_u32x4 u; Frag f; } fa, fb;
+        fa.u = x.a;
 #pragma unroll
-        for (int q = 0; q < PARTS; ++q)
+        for (int v = 0; v < R; ++v) {
+            if constexpr (sizeof(T) == 4) fb.u = kn_u32x4{x.b[0][v], x.b[1][v], x.b[2][v], x.b[3][v]};
+            else
 #pragma unroll
-            for (int v = 0; v < SETS; ++v) {
-                union { kn_u32x4 u; Frag f; } fb, fa;
-                if constexpr (!COLS) fb.u = x.b[v * PARTS + q];
-                else if constexpr (sizeof(T) == 4) fb.u = kn_u32x4{x.b[0][v], x.b[1][v], x.b[2][v], x.b[3][v]};
-                else
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) // columns 2 (v / 2) and + 1 of rows 2 t and 2 t + 1: the lower or the upper halves
-                        fb.u[t] = __builtin_amdgcn_perm(x.b[2 * t + 1][v / 2], x.b[2 * t][v / 2], v & 1 ? 0x07060302 : 0x05040100);
-#pragma unroll
-                for (int m = 0; m < MB; ++m) {
-                    fa.u = x.a[m][q];
-                    acc[m][v] = kn_mfma(fb.f, fa.f, acc[m][v]);
-                }
-            }
+                for (int t = 0; t < 4; ++t) // column v of rows 2 t and 2 t + 1: the lower or the upper halves of word v / 2
+                    fb.u[t] = __builtin_amdgcn_perm(x.b[2 * t + 1][v / 2], x.b[2 * t][v / 2], v & 1 ? 0x07060302 : 0x05040100);
+            acc[v] = kn_mfma(fb.f, fa.f, acc[v]);
+        }
     };
     Step even, odd;
     int s = wave;
@@ -338,36 +316,25 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p, int
         multiply(odd);
         s += FEW_WAVES;
     }
+    float *mine = red + (wave * 16 + col) * LD; // register r of product v: column R (4 g + r) + v
 #pragma unroll
-    for (int m = 0; m < MB; ++m) {
-        if (m) __syncthreads();
-        float *mine = red + (wave * 16 + col) * LD;
-        if constexpr (COLS) { // register r of set v: column R (4 g + r) + v
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+        for (int v = 0; v < R; v += 4) *(kn_f32x4 *)(mine + R * (4 * g + r) + v) = kn_f32x4{acc[v][r], acc[v + 1][r], acc[v + 2][r], acc[v + 3][r]};
+    __syncthreads();
+    for (int q = tid; q < 16 * BN / 8; q += FEW_WAVES * 64) {
+        const int r = q / (BN / 8), cj = q % (BN / 8) * 8;
+        const int32_t i = piece.begin + r, j = j0 + cj;
+        if (i >= piece.end || j >= p.J) continue;
+        float y[8] = {}, add[8];
 #pragma unroll
-                for (int v = 0; v < SETS; v += 4)
-                    *(kn_f32x4 *)(mine + R * (4 * g + r) + v) = kn_f32x4{acc[m][v][r], acc[m][v + 1][r], acc[m][v + 2][r], acc[m][v + 3][r]};
-        } else {
+        for (int w = 0; w < FEW_WAVES; ++w) {
+            const kn_f32x4 lo = *(const kn_f32x4 *)(red + (w * 16 + r) * LD + cj), hi = *(const kn_f32x4 *)(red + (w * 16 + r) * LD + cj + 4);
 #pragma unroll
-            for (int v = 0; v < SETS; ++v) *(kn_f32x4 *)(mine + 16 * v + 4 * g) = acc[m][v];
+            for (int n = 0; n < 4; ++n) { y[n] += lo[n]; y[n + 4] += hi[n]; }
         }
-        __syncthreads();
-        for (int q = tid; q < 16 * BN / 8; q += FEW_WAVES * 64) {
-            const int r = q / (BN / 8), cj = q % (BN / 8) * 8;
-            const int32_t i = piece.begin + 16 * m + r, j = j0 + cj;
-            if (i >= piece.end || j >= p.J) continue;
-            float y[8] = {};
-#pragma unroll
-            for (int w = 0; w < FEW_WAVES; ++w) {
-                const kn_f32x4 lo = *(const kn_f32x4 *)(red + (w * 16 + r) * LD + cj), hi = *(const kn_f32x4 *)(red + (w * 16 + r) * LD + cj + 4);
-#pragma unroll
-                for (int n = 0; n < 4; ++n) { y[n] += lo[n]; y[n + 4] += hi[n]; }
-            }
-            float add[8];
-            bias_of<T>(p, some, group, j, add);
-            finish<T>(p, some, group, i, j, add, y);
-        }
+        bias_of<T>(p, some, group, j, add);
+        finish<T>(p, some, group, i, j, add, y);
     }
 }
 
@@ -379,11 +346,11 @@ template <typename T> bool rows_of_pieces(const KnProduct &p)
     return (at & 15) == 0 && p.C % V == 0 && p.J % 8 == 0 && p.lda % V == 0 && (!p.mask || p.ldm % V == 0) && p.a_rows > 0 && (!p.mask || p.m_rows > 0);
 }
 
-template <typename T, bool COLS, int BM, int BN, int WR, int WC> int launch_rows(hipStream_t st, const KnProduct &p)
+template <typename T, bool COLS, int BM, int BN, int WR, int WC, int NB> int launch_rows(hipStream_t st, const KnProduct &p)
 {
     const int64_t blocks = kn_pieces(p.M, p.E, BM) * kn_div_up(p.J, BN);
     if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_product_rows<T, COLS, BM, BN, WR, WC>), dim3((unsigned)blocks), dim3(WR * WC * 64), 0, st, p, (int32_t)blocks);
+    hipLaunchKernelGGL((k_product_rows<T, COLS, BM, BN, WR, WC, NB>), dim3((unsigned)blocks), dim3(WR * WC * 64), 0, st, p, (int32_t)blocks);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }
@@ -398,21 +365,27 @@ template <typename T, bool REDUCE> int launch_any(hipStream_t st, const KnProduc
     return KN_OK;
 }
 
-template <typename T, bool COLS, int MB> int launch_few(hipStream_t st, const KnProduct &p)
+template <typename T> int launch_few(hipStream_t st, const KnProduct &p)
 {
-    const int64_t blocks = kn_pieces(p.M, p.E, 16 * MB) * kn_div_up(p.J, FewCols<T, COLS>::N);
+    const int64_t blocks = kn_pieces(p.M, p.E, 16) * kn_div_up(p.J, 256 / (int)sizeof(T));
     if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_product_few<T, COLS, MB>), dim3((unsigned)blocks), dim3(FEW_WAVES * 64), 0, st, p, (int32_t)blocks);
+    hipLaunchKernelGGL((k_product_few<T>), dim3((unsigned)blocks), dim3(FEW_WAVES * 64), 0, st, p, (int32_t)blocks);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }
 
+// Which tile, by the rows that a network has on average.
 template <typename T, bool COLS> int launch_pieces(hipStream_t st, const KnProduct &p)
 {
-    const int64_t each = p.M / p.E; // rows of a network, on average
-    if (each <= 16) return launch_few<T, COLS, 1>(st, p);
-    if (each <= 32) return launch_few<T, COLS, 2>(st, p);
-    return launch_rows<T, COLS, 128, 128, 2, 2>(st, p);
+    const int64_t each = p.M / p.E;
+    if (each >= 384) return launch_rows<T, COLS, 192, 128, 2, 2, 2>(st, p);
+    if (each >= 64) return launch_rows<T, COLS, 128, 128, 2, 4, 2>(st, p);
+    if constexpr (COLS) {
+        if (p.M <= 32 || p.M < p.E) return launch_few<T>(st, p);
+        return launch_rows<T, COLS, 64, 256 / (sizeof(T) / 2), 1, 8 / (sizeof(T) / 2), 2>(st, p);
+    } else {
+        return launch_rows<T, COLS, 32, 64, 1, 4, 4>(st, p);
+    }
 }
 
 template <typename T> int launch_forward(hipStream_t st, const KnProduct &p)
@@ -537,7 +510,7 @@ template <typename T, int GATHER> int launch_reduce(hipStream_t st, const KnProd
 {
     const int64_t blocks = (int64_t)p.E * kn_div_up(p.I, 128) * kn_div_up(p.J, 128);
     if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_product_reduce<T, GATHER, 128, 128, 2, 2>), dim3((unsigned)blocks), dim3(256), 0, st, p, (int32_t)blocks, sum);
+    hipLaunchKernelGGL((k_product_reduce<T, GATHER, 128, 128, 2, 4>), dim3((unsigned)blocks), dim3(512), 0, st, p, (int32_t)blocks, sum);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }

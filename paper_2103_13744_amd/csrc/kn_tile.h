@@ -46,7 +46,7 @@ template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type kn_row
     return *(const KN_LDS typename KnFrag<T>::Type *)(tile + kn_row_byte(r, kk * 4 + (lane >> 4)));
 }
 // the same of the 16 columns from j0 on in a column-wise tile W wide
-template <typename T, int W> __device__ __forceinline__ typename KnFrag<T>::Type kn_col_frag(const KN_LDS char *tile, int j0, int kk, int lane)
+template <typename T, int W> __device__ __forceinline__ typename KnFrag<T>::Type kn_col_frag(const KN_LDS char *__restrict tile, int j0, int kk, int lane)
 {
     if constexpr (sizeof(T) == 2) {
         const int g = lane >> 4, i = lane & 15, c = kk * 32 + 8 * g + (i >> 2);
@@ -163,9 +163,12 @@ template <typename T, int W, int NW, bool INDEX> struct KnGroupLoader {
 
 // Between two stages: what this wavefront asked for has arrived in the LDS, what it read there has arrived in registers, and so for every
 // wavefront of the workgroup.  The buffer read before may be fetched into again, the one fetched may be read.
-__device__ __forceinline__ void kn_stage_barrier()
+// LATER: so many of the loads that this wavefront asked for last need not have arrived.
+template <int LATER = 0> __device__ __forceinline__ void kn_stage_barrier()
 {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    static_assert(LATER < 64, "");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((LATER & 15) | (LATER >> 4) << 14 | 7 << 4); // vmcnt(LATER), lgkmcnt(0); expcnt is not waited for
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
@@ -175,6 +178,7 @@ template <int U, int V, typename T, bool COLS_B, bool COLS_A = false> __device__
 {
     constexpr int PER_COL = sizeof(T) == 2 ? 2 : 4, READS = U * (COLS_A ? PER_COL : 1) + V * (COLS_B ? PER_COL : 1);
     constexpr int PRODUCTS = U * V * (sizeof(T) == 2 ? 1 : 4), EACH = PRODUCTS / READS > 0 ? PRODUCTS / READS : 1;
+    __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0); // (a product first: what it waits for is not asked for behind a new read)
 #pragma unroll
     for (int i = 0; i < READS; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0); // an LDS read

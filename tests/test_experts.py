@@ -81,7 +81,7 @@ def dev(t):
 SIZES = [  # rows, networks, inputs, outputs
     (0, 3, 16, 16), (1, 1, 1, 1), (1, 4, 64, 64), (2, 70, 128, 136), (5, 2, 2, 3), (16, 8, 256, 64), (17, 3, 33, 65), (64, 1, 64, 64),
     (65, 2, 63, 32), (129, 5, 91, 64), (200, 65, 32, 33), (257, 3, 72, 200), (300, 130, 64, 3), (500, 4, 320, 520), (1000, 7, 129, 127),
-    (1100, 3, 512, 256), (3000, 4200, 32, 32), (2100, 2, 136, 264),
+    (1100, 3, 512, 256), (3000, 4200, 32, 32), (2100, 2, 136, 264), (300, 20, 200, 328), (1000, 30, 520, 256), (40, 2, 72, 520), (1300, 3, 40, 72),
 ]
 
 
