@@ -71,6 +71,19 @@ __device__ __forceinline__ KnPiece kn_find_piece(const int32_t *__restrict__ off
     p.begin = number >= first ? o + (number - first) * len : p.end; // (always, where offsets start at 0 and do not fall)
     return p;
 }
+// The network with the `turn`-th most rows (ties: the lower number first), of up to 64: long ones begin first, short ones fill the end.
+__device__ __forceinline__ int32_t kn_longest(const int32_t *__restrict__ offsets, int32_t E, int32_t M, int32_t turn)
+{
+    const int lane = kn_thread() & (KN_WAVE - 1);
+    const int32_t o = kn_offset(offsets, min(lane, E), M);
+    const int32_t n = lane < E ? max(0, kn_offset(offsets, min(lane + 1, E), M) - o) : -1;
+    int32_t rank = 0;
+    for (int e = 0; e < E; ++e) {
+        const int32_t other = __builtin_amdgcn_readlane(n, e);
+        rank += other > n || (other == n && e < lane) ? 1 : 0;
+    }
+    return __builtin_amdgcn_readfirstlane((int32_t)__ffsll((unsigned long long)__ballot(lane < E && rank == turn)) - 1);
+}
 static inline int64_t kn_pieces(int64_t M, int64_t E, int64_t len) { return M / len + E + 1; }
 
 // 16 x 16 products of fragments of 8 values a lane: lane l holds row (or column) l % 16 and the contraction's 8 (l / 16) .. + 7

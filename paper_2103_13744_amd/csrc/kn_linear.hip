@@ -338,6 +338,136 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p, int
     }
 }
 
+// Layers of the small networks' kind (contraction up to KF fragments, columns up to V of 16, or a few such tiles of columns), of any
+// sizes, strides and alignment: a wavefront takes SMALL_ROWS rows of one network by itself, with the network's fragments in its
+// registers; nothing goes through the LDS and no wavefront waits for another.  Such calls are bound by their bytes, or rather by the
+// latency of one look-up, one fetch and one store per piece: what is under way at a time is what counts, so all of a piece is
+// asked for at once.
+constexpr int SMALL_ROWS = 64, SMALL_WAVES = 4;
+template <typename T> struct SmallFrag {
+    static constexpr int W = 16 / sizeof(T), KS = 4 * W;
+    typedef T Any __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T)))); // a piece wherever it lies
+};
+// values k .. k + W - 1 of a row of C (zeros behind its end; k is a multiple of W)
+template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type small_row(const T *row, int32_t k, int32_t C)
+{
+    constexpr int W = SmallFrag<T>::W;
+    typename KnFrag<T>::Type f;
+    if (k + W <= C) {
+        f = *(const typename SmallFrag<T>::Any *)(row + k);
+    } else {
+#pragma unroll
+        for (int q = 0; q < W; ++q) {
+            const T v = row[min(k + q, C - 1)];
+            f[q] = k + q < C ? v : (T)0.0f;
+        }
+    }
+    return f;
+}
+template <typename T, bool COLS, int KF, int V>
+__global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p, int32_t pieces)
+{
+    constexpr int W = SmallFrag<T>::W, KS = SmallFrag<T>::KS, SUBS = SMALL_ROWS / 16;
+    typedef typename KnFrag<T>::Type Frag;
+    typedef T Four __attribute__((ext_vector_type(4)));
+    const int lane = kn_thread() & 63, col = lane & 15, g = lane >> 4;
+    const int32_t number = __builtin_amdgcn_readfirstlane(kn_block() * SMALL_WAVES + (kn_thread() >> 6));
+    const int ntiles = (p.J + 16 * V - 1) / (16 * V);
+    if (number / ntiles >= pieces) return;
+    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, SMALL_ROWS, number / ntiles);
+    const int32_t j0 = number % ntiles * 16 * V;
+    if (piece.begin >= piece.end) return;
+    const bool some = piece.group < p.E;
+    const int64_t group = some ? piece.group : 0;
+    const int32_t C = p.C;
+    Frag fa[SUBS][KF], fb[KF][V];
+    bool there[SUBS];
+    if (some) {
+        const T *arow[SUBS];
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) {
+            const int32_t i = min(piece.begin + 16 * s + col, piece.end - 1), src = p.rows ? p.rows[i] : i;
+            there[s] = (uint32_t)src < (uint32_t)p.a_rows;
+            arow[s] = (const T *)p.a + (int64_t)(there[s] ? src : 0) * p.lda;
+        }
+        const T *b = (const T *)p.b + group * p.b_group;
+#pragma unroll
+        for (int k = 0; k < KF; ++k)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int32_t c = k * KS + g * W, j = min(j0 + 16 * v + col, p.J - 1);
+                if constexpr (COLS) {
+#pragma unroll
+                    for (int q = 0; q < W; ++q) {
+                        const T w = b[(int64_t)min(c + q, C - 1) * p.b_c + j];
+                        fb[k][v][q] = c + q < C ? w : (T)0.0f;
+                    }
+                } else {
+                    fb[k][v] = small_row<T>(b + (int64_t)j * p.b_j, c, C);
+                }
+            }
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+            for (int k = 0; k < KF; ++k) fa[s][k] = small_row<T>(arow[s], k * KS + g * W, C);
+    }
+    const T *bias = (const T *)p.bias, *mask = (const T *)p.mask;
+    const bool fours = p.J % 4 == 0 && (((uintptr_t)p.out | (uintptr_t)bias | (uintptr_t)mask) & (4 * sizeof(T) - 1)) == 0 && (!mask || p.ldm % 4 == 0);
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
+        const int32_t i = piece.begin + 16 * s + col;
+        if (piece.begin + 16 * s >= piece.end) break;
+        kn_f32x4 acc[V] = {};
+        const T *mrow = nullptr;
+        if (some) {
+#pragma unroll
+            for (int k = 0; k < KF; ++k)
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[v] = kn_mfma(fb[k][v], fa[s][k], acc[v]);
+            if (!there[s])
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[v] = kn_f32x4{0, 0, 0, 0};
+            if (mask) {
+                const int32_t m = min(i, piece.end - 1), src = p.mask_rows ? p.mask_rows[m] : m;
+                mrow = (uint32_t)src < (uint32_t)p.m_rows ? mask + (int64_t)src * p.ldm : nullptr;
+            }
+        }
+        if (i >= piece.end) continue;
+        T *out = (T *)p.out + (int64_t)i * p.o_i;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int32_t j = j0 + 16 * v + 4 * g; // this lane's columns j .. j + 3
+            if (j >= p.J) continue;
+            float y[4] = {acc[v][0], acc[v][1], acc[v][2], acc[v][3]};
+            Four m = {}, o, add = {};
+            if (some && bias) {
+                if (fours) add = *(const Four *)(bias + group * p.J + j);
+                else
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) add[r] = bias[group * p.J + min(j + r, p.J - 1)];
+            }
+            if (mrow) {
+                if (fours) m = *(const Four *)(mrow + j);
+                else
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) m[r] = mrow[min(j + r, p.J - 1)];
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (some && bias) y[r] += (float)add[r];
+                if (p.relu) y[r] = y[r] > 0.0f || y[r] != y[r] ? y[r] : 0.0f; // (a NaN stays one)
+                if (mask && !((float)m[r] > 0.0f)) y[r] = 0.0f;
+                o[r] = (T)y[r];
+            }
+            if (fours) *(Four *)(out + j) = o;
+            else
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (j + r < p.J) out[j + r] = o[r];
+        }
+    }
+}
+
 // Whether every row is made of whole 16-byte pieces that lie on multiples of 16 bytes, as k_product_rows takes them
 template <typename T> bool rows_of_pieces(const KnProduct &p)
 {
@@ -388,8 +518,32 @@ template <typename T, bool COLS> int launch_pieces(hipStream_t st, const KnProdu
     }
 }
 
+template <typename T, bool COLS, int KF, int V> int launch_small(hipStream_t st, const KnProduct &p)
+{
+    const int64_t pieces = kn_pieces(p.M, p.E, SMALL_ROWS), waves = pieces * kn_div_up(p.J, 16 * V);
+    if (waves > 0x7fffffffLL) return KN_E_UNSUPPORTED;
+    hipLaunchKernelGGL((k_product_small<T, COLS, KF, V>), dim3((unsigned)kn_div_up(waves, SMALL_WAVES)), dim3(SMALL_WAVES * 64), 0, st, p, (int32_t)pieces);
+    KN_CHECK_LAUNCH();
+    return KN_OK;
+}
+constexpr int SMALL_MOST = 128; // widest contraction and most columns that k_product_small takes
+template <typename T, bool COLS> int launch_small_widths(hipStream_t st, const KnProduct &p)
+{
+    const int kf = (p.C + SmallFrag<T>::KS - 1) / SmallFrag<T>::KS;
+    if constexpr (sizeof(T) == 4) {
+        if (kf > 4) return launch_small<T, COLS, 8, 2>(st, p);
+        if (kf > 2) return p.J <= 32 ? launch_small<T, COLS, 4, 2>(st, p) : launch_small<T, COLS, 4, 4>(st, p);
+        return p.J <= 32 ? launch_small<T, COLS, 2, 2>(st, p) : launch_small<T, COLS, 2, 4>(st, p);
+    } else {
+        if (kf > 2) return launch_small<T, COLS, 4, 4>(st, p);
+        if (kf > 1) return p.J <= 32 ? launch_small<T, COLS, 2, 2>(st, p) : launch_small<T, COLS, 2, 4>(st, p);
+        return p.J <= 32 ? launch_small<T, COLS, 1, 2>(st, p) : launch_small<T, COLS, 1, 4>(st, p);
+    }
+}
+
 template <typename T> int launch_forward(hipStream_t st, const KnProduct &p)
 {
+    if (p.C <= SMALL_MOST && p.J <= SMALL_MOST) return p.b_j == 1 ? launch_small_widths<T, true>(st, p) : launch_small_widths<T, false>(st, p);
     if (!rows_of_pieces<T>(p)) return launch_any<T, false>(st, p);
     return p.b_j == 1 ? launch_pieces<T, true>(st, p) : launch_pieces<T, false>(st, p);
 }
@@ -399,7 +553,7 @@ template <typename T> int launch_forward(hipStream_t st, const KnProduct &p)
 // fragments that are there anyway, in the workgroups of the first tile: SUM_B the columns of b, SUM_A those of a.
 enum { SUM_NONE, SUM_A, SUM_B };
 template <typename T, int GATHER, int BM, int BN, int WR, int WC>
-__global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, int32_t blocks, int32_t sum)
+__global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, int32_t sum)
 {
     constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16, CS = 128 / sizeof(T);
     typedef typename KnFrag<T>::Type Frag;
@@ -407,10 +561,10 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
     KN_LDS char *lds = (KN_LDS char *)lds_;
     const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int jtiles = (p.J + BN - 1) / BN, itiles = (p.I + BM - 1) / BM;
-    int32_t number = kn_xcd_order(kn_block(), blocks);
-    const int j0 = number % jtiles * BN;
-    number /= jtiles;
-    const int i0 = number % itiles * BM, group = number / itiles;
+    // (a network's tiles go to all XCDs, neighbours among them to one: networks differ in rows, XCDs should not)
+    const int32_t tiles = itiles * jtiles, turn = kn_block() / tiles, number = kn_xcd_order(kn_block() % tiles, tiles);
+    const int32_t group = p.E <= KN_WAVE ? kn_longest(p.offsets, p.E, p.M, turn) : turn;
+    const int j0 = number % jtiles * BN, i0 = number / jtiles * BM;
     const int32_t c0 = kn_offset(p.offsets, group, p.M), cend = max(c0, kn_offset(p.offsets, group + 1, p.M));
     const int32_t steps = (cend - c0 + CS - 1) / CS;
     const bool sum_a = sum == SUM_A && j0 == 0, sum_b = sum == SUM_B && i0 == 0;
@@ -510,7 +664,7 @@ template <typename T, int GATHER> int launch_reduce(hipStream_t st, const KnProd
 {
     const int64_t blocks = (int64_t)p.E * kn_div_up(p.I, 128) * kn_div_up(p.J, 128);
     if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_product_reduce<T, GATHER, 128, 128, 2, 4>), dim3((unsigned)blocks), dim3(512), 0, st, p, (int32_t)blocks, sum);
+    hipLaunchKernelGGL((k_product_reduce<T, GATHER, 128, 128, 2, 4>), dim3((unsigned)blocks), dim3(512), 0, st, p, sum);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }
