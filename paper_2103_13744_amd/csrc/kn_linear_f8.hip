@@ -1,6 +1,6 @@
 // Products grouped by network in 8-bit floating point (e4m3) with fp32 scales: kn_quantize_f8 (a scale per row and 128 inputs),
 // kn_quantize_f8_weights (a scale per 128 x 128), kn_grouped_linear_f8.
-#include "kn_experts.h"
+#include "kn_tile.h"
 
 namespace {
 
@@ -111,87 +111,143 @@ struct F8Args {
     int32_t M, E, N, kb, x_rows, relu;
 };
 
-// 128 x 128 results per workgroup of four wavefronts, 64 x 64 each; a step is a block of 128 inputs, which is one instruction's
-// contraction, so that every product starts from zero and is scaled, in fp32, as it is added.
-template <typename T>
-__global__ void __launch_bounds__(256) k_linear_f8(F8Args p)
+// Tiles of BM x BN results, WR x WC wavefronts, NB stages in the LDS, fetched ahead.  A stage is a block of 128 inputs, which is one
+// instruction's contraction, so that every product starts from zero and is scaled, in fp32, as it is added.  Fragments of the
+// weights are the first operand: a lane's four results are neighbours in a row, and one factor, the product of the row's
+// scale and the weights', serves all of them.  The four lanes of a row hold the factors of four blocks and hand them to each other:
+// in the LDS they took the place of a workgroup.
+template <typename T, int BM, int BN, int WR, int WC, int NB>
+__global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t blocks)
 {
-    constexpr int TILE = 128;
-    __shared__ kn_u32x4 as[TILE * 8], bs[TILE * 8]; // rows of 128 bytes; 16-byte piece c of row r lies at c ^ (r & 7)
-    __shared__ float sa[TILE];
-    const int tid = kn_thread(), lane = tid & 63, wave = tid >> 6;
-    const int ntiles = (p.N + TILE - 1) / TILE;
-    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, TILE, kn_block() / ntiles);
-    const int j0 = (kn_block() % ntiles) * TILE;
+    constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16;
+    static_assert(F8_BLOCK % BN == 0, "a tile's columns share a scale");
+    typedef KnRowLoader<uint8_t, BM, NW> LoadA;
+    typedef KnRowLoader<uint8_t, BN, NW> LoadB;
+    constexpr int WN = BN / WC, LD = WN + 4, LR = WN / 8;
+    constexpr int BYTES = NB * STAGE > NW * 16 * LD * 4 ? NB * STAGE : NW * 16 * LD * 4;
+    __shared__ __align__(16) char lds_[BYTES];
+    KN_LDS char *lds = (KN_LDS char *)lds_;
+    const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ntiles = (p.N + BN - 1) / BN;
+    const int32_t number = kn_xcd_order(kn_block(), blocks);
+    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, BM, number / ntiles);
+    const int j0 = number % ntiles * BN;
     if (piece.begin >= piece.end) return;
     const int64_t kp = (int64_t)p.kb * F8_BLOCK;
     const bool some = piece.group < p.E;
     const int64_t group = some ? piece.group : 0;
-    const uint8_t *arow[4], *brow[4];
+    LoadA la;
+    LoadB lb;
+    la.start(wave, lane, [&](int r) {
+        const int32_t i = min(piece.begin + r, piece.end - 1), src = p.rows ? p.rows[i] : i;
+        return p.x + ((uint32_t)src < (uint32_t)p.x_rows ? src : 0) * kp;
+    });
+    lb.start(wave, lane, [&](int r) { return p.w + (group * p.N + min(j0 + r, p.N - 1)) * kp; });
+    const int32_t steps = some ? p.kb : 0;
+    constexpr int LOADS = LoadA::N + LoadB::N;
+    auto fetch = [&](int s, int at) {
+        la.fetch(lds + at * STAGE, wave, F8_BLOCK);
+        lb.fetch(lds + at * STAGE + BM * 128, wave, F8_BLOCK);
+    };
+    const float *ws = p.ws + (group * ((p.N + F8_BLOCK - 1) / F8_BLOCK) + j0 / F8_BLOCK) * p.kb;
+    const int wi = (wave / WC) * (BM / WR), wj = (wave % WC) * WN;
+    const float *xs[U]; // this lane's row's scales, from its own of four on
+    bool there[U];      // (rows that x does not have count as zeros)
 #pragma unroll
-    for (int t = 0; t < 4; ++t) { // thread's pieces: row t * 32 + tid / 8, 16 bytes tid % 8
-        const int r = t * 32 + tid / 8;
-        const int32_t i = piece.begin + r;
-        int32_t src = -1;
-        if (i < piece.end) src = p.rows ? p.rows[i] : i;
-        arow[t] = (uint32_t)src < (uint32_t)p.x_rows ? p.x + src * kp + tid % 8 * 16 : nullptr;
-        brow[t] = j0 + r < p.N ? p.w + (group * p.N + j0 + r) * kp + tid % 8 * 16 : nullptr;
+    for (int u = 0; u < U; ++u) {
+        const int32_t i = min(piece.begin + wi + 16 * u + (lane & 15), piece.end - 1), src = p.rows ? p.rows[i] : i;
+        there[u] = (uint32_t)src < (uint32_t)p.x_rows;
+        xs[u] = p.xs + (int64_t)(there[u] ? src : 0) * p.kb;
     }
-    int32_t srow = -1; // threads 0 .. 127: the row whose scale they fetch
-    if (tid < TILE && piece.begin + tid < piece.end) {
-        srow = p.rows ? p.rows[piece.begin + tid] : piece.begin + tid;
-        if ((uint32_t)srow >= (uint32_t)p.x_rows) srow = -1;
-    }
-    const float *ws = p.ws + (group * ntiles + j0 / TILE) * p.kb;
-    const int wi = (wave >> 1) * 64, wj = (wave & 1) * 64;
-    kn_f32x4 acc[4][4] = {};
-    for (int b = 0; b < (some ? p.kb : 0); ++b) {
-        __syncthreads();
+    float asked[U], asked_w, factor[U];
+    auto ask = [&](int s) { // (behind the last block: the last one's, unused)
+        const int b = min(s + (lane >> 4), steps - 1);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int r = t * 32 + tid / 8, at = r * 8 + ((tid & 7) ^ (r & 7));
-            as[at] = arow[t] ? *(const kn_u32x4 *)(arow[t] + b * F8_BLOCK) : kn_u32x4{0, 0, 0, 0};
-            bs[at] = brow[t] ? *(const kn_u32x4 *)(brow[t] + b * F8_BLOCK) : kn_u32x4{0, 0, 0, 0};
-        }
-        if (tid < TILE) sa[tid] = srow >= 0 ? p.xs[(int64_t)srow * p.kb + b] * ws[b] : 0.0f;
-        __syncthreads();
-        union Frag { kn_u32x4 h[2]; kn_i32x8 v; } fa[4], fb[4];
+        for (int u = 0; u < U; ++u) asked[u] = xs[u][b];
+        asked_w = ws[b];
+    };
+    kn_f32x4 acc[U][V] = {};
+    if (steps > 0) {
+        ask(0);
+        for (int s = 0; s < NB - 1 && s < steps; ++s) fetch(s, s);
+        for (int s = 0, at = 0; s < steps; ++s) {
+            if (s + NB - 1 <= steps) kn_stage_barrier<(NB - 2) * LOADS>();
+            else kn_stage_barrier();
+            if (s + NB - 1 < steps) fetch(s + NB - 1, at == 0 ? NB - 1 : at - 1);
+            if (s % 4 == 0) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int ra = wi + 16 * u + (lane & 15), rb = wj + 16 * u + (lane & 15), c = lane >> 4;
-            fa[u].h[0] = as[ra * 8 + (c ^ (ra & 7))];
-            fa[u].h[1] = as[ra * 8 + ((c + 4) ^ (ra & 7))];
-            fb[u].h[0] = bs[rb * 8 + (c ^ (rb & 7))];
-            fb[u].h[1] = bs[rb * 8 + ((c + 4) ^ (rb & 7))];
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const kn_f32x4 s = *(const kn_f32x4 *)(sa + wi + 16 * u + (lane >> 4) * 4);
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const kn_f32x4 r = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[u].v, fb[v].v, kn_f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[u][v][i] = fmaf(r[i], s[i], acc[u][v][i]);
+                for (int u = 0; u < U; ++u) factor[u] = there[u] ? asked[u] * asked_w : 0.0f;
+                if (s + 4 < steps) ask(s + 4);
             }
+            const KN_LDS char *ta = lds + at * STAGE, *tb = ta + BM * 128;
+            union Frag { kn_u32x4 h[2]; kn_i32x8 v; } fa[U], fb[V];
+            float f[U];
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) fb[v].h[h] = *(const KN_LDS kn_u32x4 *)(tb + kn_row_byte(wj + 16 * v + (lane & 15), h * 4 + (lane >> 4)));
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) fa[u].h[h] = *(const KN_LDS kn_u32x4 *)(ta + kn_row_byte(wi + 16 * u + (lane & 15), h * 4 + (lane >> 4)));
+                f[u] = __shfl(factor[u], (lane & 15) + 16 * (s & 3));
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const kn_f32x4 r = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[v].v, fa[u].v, kn_f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[u][v][i] = fmaf(r[i], f[u], acc[u][v][i]);
+                }
+            at = at + 1 == NB ? 0 : at + 1;
         }
     }
+    kn_stage_barrier(); // (the tiles' LDS is used again)
+    KN_LDS float *mine = (KN_LDS float *)(lds + wave * (16 * LD * 4));
     T *y = (T *)p.y;
     const T *bias = (const T *)p.bias;
+    const int cj = lane % LR * 8;
+    const int32_t j = j0 + wj + cj;
+    const bool wide = p.N % 8 == 0 && ((uintptr_t)y & 15) == 0;
+    typedef T Out __attribute__((ext_vector_type(8)));
+    float add[8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int q = 0; q < 8; ++q) add[q] = bias && some && j + q < p.N ? (float)bias[group * p.N + j + q] : 0.0f;
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
+    for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int32_t i = piece.begin + wi + 16 * u + (lane >> 4) * 4 + r, j = j0 + wj + 16 * v + (lane & 15);
-                if (i >= piece.end || j >= p.N) continue;
-                float o = acc[u][v][r];
-                if (some) {
-                    if (bias) o += (float)bias[group * p.N + j];
-                    if (p.relu) o = o > 0.0f || o != o ? o : 0.0f;
-                }
-                y[(int64_t)i * p.N + j] = (T)o;
+        for (int v = 0; v < V; ++v) *(KN_LDS kn_f32x4 *)(mine + (lane & 15) * LD + 16 * v + (lane >> 4) * 4) = acc[u][v];
+#pragma unroll
+        for (int h = 0; h < (16 * LR + 63) / 64; ++h) {
+            const int r = h * (64 / LR) + lane / LR;
+            const int32_t i = piece.begin + wi + 16 * u + r;
+            if (r >= 16 || i >= piece.end || j >= p.N) continue;
+            const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj + 4);
+            const float s[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            Out o;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                float t = s[q] + add[q];
+                if (p.relu) t = t > 0.0f || t != t ? t : 0.0f; // (a NaN stays one)
+                o[q] = (T)t;
             }
+            if (wide) *(Out *)(y + (int64_t)i * p.N + j) = o;
+            else
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    if (j + q < p.N) y[(int64_t)i * p.N + j + q] = o[q];
+        }
+    }
+}
+
+template <typename T, int BM, int BN, int WR, int WC, int NB> int launch_f8(hipStream_t st, const F8Args &p)
+{
+    const int64_t blocks = kn_pieces(p.M, p.E, BM) * kn_div_up(p.N, BN);
+    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
+    hipLaunchKernelGGL((k_linear_f8<T, BM, BN, WR, WC, NB>), dim3((unsigned)blocks), dim3(WR * WC * 64), 0, st, p, (int32_t)blocks);
+    KN_CHECK_LAUNCH();
+    return KN_OK;
 }
 
 } // namespace
@@ -245,11 +301,12 @@ extern "C" int kn_grouped_linear_f8(void *stream, const kn_linear_desc *d, const
         return KN_E_INVALID_ARG;
     F8Args p = {(const uint8_t *)xq, (const uint8_t *)wq, xs, ws, bias, y, offsets, rows, (int32_t)d->rows, d->experts, d->n_out,
                 (int32_t)kn_div_up(d->n_in, F8_BLOCK), (int32_t)d->x_rows, relu != 0};
-    const int64_t blocks = kn_pieces(d->rows, d->experts, 128) * kn_div_up(d->n_out, 128);
-    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
+    const int64_t each = p.M / p.E; // rows of a network, on average
     return kn_with_type(d->dtype, [&](auto v) -> int {
-        hipLaunchKernelGGL((k_linear_f8<decltype(v)>), dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, p);
-        KN_CHECK_LAUNCH();
-        return KN_OK;
+        typedef decltype(v) E_;
+        hipStream_t st = (hipStream_t)stream;
+        if (each >= 512) return launch_f8<E_, 192, 128, 2, 2, 2>(st, p);
+        if (each >= 32) return launch_f8<E_, 64, 128, 1, 4, 2>(st, p);
+        return launch_f8<E_, 32, 128, 1, 4, 2>(st, p);
     });
 }

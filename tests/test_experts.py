@@ -395,7 +395,7 @@ def test_quantize_f8_weights(dtype):
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("size", [(0, 2, 128, 128), (1, 1, 1, 1), (1, 3, 256, 128), (8, 40, 384, 200), (16, 4, 640, 256), (33, 2, 100, 70), (130, 3, 130, 129),
-                                  (300, 5, 512, 384), (700, 2, 257, 520), (900, 100, 128, 64)], ids=str)
+                                  (300, 5, 512, 384), (700, 2, 257, 520), (900, 100, 128, 64), (1500, 2, 640, 264)], ids=str)
 def test_linear_f8(size, dtype):
     """The products of the 8-bit values are exact in fp32; what is rounded is their sum, the scales' product and the result."""
     m, e, k, n = size
