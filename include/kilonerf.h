@@ -384,8 +384,8 @@ int kn_grouped_linear_dw(void *stream, const kn_linear_desc *desc, const void *x
                          const int32_t *rows, void *dw /*dev E*K*N*/, void *db /*dev E*N, nullable*/);
 
 /* The same layer in 8 bits (e4m3).  kb = ceil(K / 128) blocks of inputs, zeros behind the K-th.
- * kn_quantize_f8: rows x (R, K) -> q (dev, R * kb*128 bytes) and scales (dev, R * kb): s = max(amax, 2^-100) / 448 over a row's
- * block, q the e4m3 nearest to x / s.  A NaN stays one; an infinity makes its block zeros and NaN.
+ * kn_quantize_f8: rows x (R, K) -> q (dev, R * kb*128 bytes) and scales (dev, R * kb): s = max(amax, 2^-100) * (1/448), in fp32, over a
+ * row's block, q the e4m3 nearest to the fp32 x / s.  A NaN stays one; an infinity makes its block zeros and NaN.
  * kn_quantize_f8_weights: w -> q (dev, E * N * kb*128 bytes, input innermost) and scales (dev, E * ceil(N/128) * kb), one per
  * 128 outputs x 128 inputs.  To be done once per weights.  q 16-byte aligned.
  * kn_grouped_linear_f8: y[i] = act(sum over blocks of s_x s_w (q_x q_w) + b_e); sums in fp32, y of desc's dtype. */

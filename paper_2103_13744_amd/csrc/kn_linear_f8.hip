@@ -5,12 +5,13 @@
 namespace {
 
 constexpr int F8_BLOCK = 128;
-constexpr float F8_LARGEST = 448.0f, F8_TINY = 0x1p-100f;
+constexpr float F8_INVERSE = 1.0f / 448.0f, F8_TINY = 0x1p-100f; // 448: the type's largest value
 
-// Scale of a block whose largest magnitude is `amax`, and a value's 8 bits: x / s is at most 448 but for the last bit of the
-// quotient, which rounds to 448.  Both are divisions, not products with a reciprocal: the nearest e4m3 of the exact quotient's
-// fp32 form.  A block of zeros keeps a finite scale.
-__device__ __forceinline__ float f8_scale(float amax) { return fmaxf(amax, F8_TINY) / F8_LARGEST; }
+// Scale of a block whose largest magnitude is `amax`: amax times the fp32 next to 1 / 448, rounded once.  A value's 8 bits are the
+// nearest e4m3 (ties to even) of the fp32 quotient x / s; the quotient of amax may pass 448 by its last bit and rounds to 448.  Both
+// roundings matter to the bit: inputs of 16 bits lie on ties of the 8-bit type now and then, which an s one bit off breaks the
+// other way.  A block of zeros keeps a finite scale.
+__device__ __forceinline__ float f8_scale(float amax) { return fmaxf(amax, F8_TINY) * F8_INVERSE; }
 __device__ __forceinline__ uint32_t f8_pack(float a, float b, float c, float d, float s)
 {
     int v = __builtin_amdgcn_cvt_pk_fp8_f32(a / s, b / s, 0, false);

@@ -351,7 +351,7 @@ def test_combine(size, dtype):
 
 # ---------------------------------------------------------------------------------------------
 def ref_quantize(v, dims):
-    s = torch.maximum(v.float().abs().amax(dim=dims, keepdim=True), torch.tensor(2.0 ** -100)) / 448.0
+    s = torch.maximum(v.float().abs().amax(dim=dims, keepdim=True), torch.tensor(2.0 ** -100)) * torch.tensor(1.0 / 448.0)
     return (v.float() / s).to(torch.float8_e4m3fn), s
 
 
