@@ -359,7 +359,7 @@ typedef struct {
  * the row's chosen logits; else the softmax over all its logits, at the chosen ones.  A NaN among a row's logits is not
  * chosen and makes the row's weights NaN.
  * slots[t*k + j] = place of the pair in the order (a permutation of 0 .. M-1; pairs with id -1 come last, from offsets[E] on),
- * rows[place] = t.  Workspace: kn_route_workspace_bytes, dev, 256-byte aligned. */
+ * rows[place] = t.  Workspace: kn_route_workspace_bytes (0 for up to 64 rows: then NULL will do), dev, 256-byte aligned. */
 int kn_route_workspace_bytes(int64_t T, int32_t experts, int32_t k, int64_t *out_bytes);
 int kn_route(void *stream, const void *logits /*dev T rows*/, int32_t dtype, int64_t T, int32_t experts, int64_t ld /*elements*/,
              int32_t k, int32_t renormalize, float *weights /*dev T*k*/, int32_t *ids /*dev T*k*/, int32_t *slots /*dev T*k*/,

@@ -488,15 +488,20 @@ def route(logits, k, renormalize=True):
     L = load_library()
     T, E = logits.shape
     ptr, ld = _rows_ptr(logits, (None, None))
-    dt, k, dev, i32 = _dtype_id(logits.dtype), int(k), logits.device, torch.int32
-    need = C.c_int64()
-    _check(L.kn_route_workspace_bytes(T, E, k, C.byref(need)), "kn_route_workspace_bytes")
-    weights = torch.empty((T, k), dtype=torch.float32, device=dev)
-    ids, slots = torch.empty((T, k), dtype=i32, device=dev), torch.empty((T, k), dtype=i32, device=dev)
-    rows, offsets = torch.empty(T * k, dtype=i32, device=dev), torch.empty(E + 1, dtype=i32, device=dev)
-    ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
-    _check(L.kn_route(_stream(), ptr, dt, T, E, ld, k, 1 if renormalize else 0, weights.data_ptr(), ids.data_ptr(), slots.data_ptr(),
-                      rows.data_ptr(), offsets.data_ptr(), ws.data_ptr(), need.value), "kn_route")
+    dt, k, i32 = _dtype_id(logits.dtype), int(k), torch.int32
+    if k < 1 or k > E:
+        raise KnError("expected 1 <= k <= %d experts, got %d" % (E, k))
+    weights = logits.new_empty((T, k), dtype=torch.float32)
+    ids = torch.empty_like(weights, dtype=i32)
+    slots, rows, offsets = torch.empty_like(ids), ids.new_empty(T * k), ids.new_empty(E + 1)
+    args = (_stream(), ptr, dt, T, E, ld, k, 1 if renormalize else 0, weights.data_ptr(), ids.data_ptr(), slots.data_ptr(), rows.data_ptr(), offsets.data_ptr())
+    rc = L.kn_route(*args, None, 0)  # (a few rows need no workspace)
+    if rc == KN_E_WORKSPACE:
+        need = C.c_int64()
+        _check(L.kn_route_workspace_bytes(T, E, k, C.byref(need)), "kn_route_workspace_bytes")
+        ws = torch.empty(need.value, dtype=torch.uint8, device=logits.device)
+        rc = L.kn_route(*args, ws.data_ptr(), need.value)
+    _check(rc, "kn_route")
     return weights, ids, slots, rows, offsets
 
 
@@ -506,7 +511,7 @@ def route_backward(logits, weights, ids, dweights, renormalize=True):
     T, E = logits.shape
     k = ids.shape[1]
     ptr, ld = _rows_ptr(logits, (None, None))
-    out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+    out = logits.new_empty((T, E))
     f = torch.float32
     _check(L.kn_route_backward(_stream(), ptr, _dtype_id(logits.dtype), T, E, ld, k, 1 if renormalize else 0, _ptr(weights, f, shape=(T, k)),
                                _ptr(ids, torch.int32, shape=(T, k)), _ptr(dweights, f, shape=(T, k)), out.data_ptr()), "kn_route_backward")
@@ -531,7 +536,7 @@ def grouped_linear(x, w, offsets, rows=None, bias=None, relu=False, out=None):
     L = load_library()
     d, M, px, pw, pr = _linear_desc(x, w, rows)
     if out is None:
-        out = torch.empty((M, d.n_out), dtype=x.dtype, device=x.device)
+        out = x.new_empty((M, d.n_out))
     _check(L.kn_grouped_linear(_stream(), C.byref(d), px, pw, _ptr(bias, x.dtype, allow_none=True, shape=(d.experts, d.n_out)),
                                _ptr(offsets, torch.int32, shape=(d.experts + 1,)), pr, 1 if relu else 0, _ptr(out, x.dtype, shape=(M, d.n_out))),
            "kn_grouped_linear")
@@ -543,7 +548,7 @@ def grouped_linear_dx(dy, x, w, offsets, rows=None, relu_in=False):
     of x several times).  ``relu_in``: x is a ReLU's result, and the gradient is that before the ReLU."""
     L = load_library()
     d, M, px, pw, pr = _linear_desc(x, w, rows)
-    dx = torch.empty((M, d.n_in), dtype=x.dtype, device=x.device)
+    dx = x.new_empty((M, d.n_in))
     _check(L.kn_grouped_linear_dx(_stream(), C.byref(d), _ptr(dy, x.dtype, shape=(M, d.n_out)), pw, px if relu_in else None,
                                   _ptr(offsets, torch.int32, shape=(d.experts + 1,)), pr if relu_in else None, dx.data_ptr()), "kn_grouped_linear_dx")
     return dx
@@ -554,7 +559,7 @@ def grouped_linear_dw(dy, x, w, offsets, rows=None, want_bias=True):
     L = load_library()
     d, M, px, _, pr = _linear_desc(x, w, rows)
     dw = torch.empty_like(w)  # (keeps the layout of dense weights)
-    db = torch.empty((d.experts, d.n_out), dtype=x.dtype, device=x.device) if want_bias else None
+    db = x.new_empty((d.experts, d.n_out)) if want_bias else None
     _check(L.kn_grouped_linear_dw(_stream(), C.byref(d), px, _ptr(dy, x.dtype, shape=(M, d.n_out)), _ptr(offsets, torch.int32, shape=(d.experts + 1,)),
                                   pr, dw.data_ptr(), None if db is None else db.data_ptr()), "kn_grouped_linear_dw")
     return dw, db
@@ -572,8 +577,7 @@ def quantize_f8(x):
     R, K = x.shape
     ptr, ld = _rows_ptr(x, (None, None))
     kb = -(-K // 128)
-    q = torch.empty((R, kb * 128), dtype=torch.float8_e4m3fn, device=x.device)
-    s = torch.empty((R, kb), dtype=torch.float32, device=x.device)
+    q, s = x.new_empty((R, kb * 128), dtype=torch.float8_e4m3fn), x.new_empty((R, kb), dtype=torch.float32)
     _check(L.kn_quantize_f8(_stream(), ptr, _dtype_id(x.dtype), R, K, ld, q.data_ptr(), s.data_ptr()), "kn_quantize_f8")
     return q, s
 
@@ -598,7 +602,7 @@ def grouped_linear_f8(xq, xs, wq, ws, offsets, rows=None, bias=None, relu=False,
     dtype = (torch.bfloat16 if dtype is None else dtype) if out is None else out.dtype
     M = X if rows is None else rows.shape[0]
     if out is None:
-        out = torch.empty((M, N), dtype=dtype, device=xq.device)
+        out = xq.new_empty((M, N), dtype=dtype)
     d = LinearDesc(_dtype_id(dtype), 1, E, kp, N, M, X, kp)
     _check(L.kn_grouped_linear_f8(_stream(), C.byref(d), _ptr(xq, f8, shape=(X, kb * 128)), _ptr(xs, f, shape=(X, kb)), _ptr(wq, f8),
                                   _ptr(ws, f, shape=(E, -(-N // 128), kb)), _ptr(bias, dtype, allow_none=True, shape=(E, N)),
@@ -612,7 +616,7 @@ def combine(y, slots, weights=None):
     L = load_library()
     M, D = y.shape
     T, k = slots.shape
-    out = torch.empty((T, D), dtype=y.dtype, device=y.device)
+    out = y.new_empty((T, D))
     _check(L.kn_combine(_stream(), _ptr(y), _dtype_id(y.dtype), M, D, _ptr(slots, torch.int32), _ptr(weights, torch.float32, allow_none=True, shape=(T, k)),
                         T, k, out.data_ptr()), "kn_combine")
     return out
@@ -624,7 +628,7 @@ def combine_backward(dout, y, slots, weights=None):
     M, D = y.shape
     T, k = slots.shape
     dy = torch.empty_like(y)
-    dw = torch.empty((T, k), dtype=torch.float32, device=y.device)
+    dw = y.new_empty((T, k), dtype=torch.float32)
     _check(L.kn_combine_backward(_stream(), _ptr(dout, y.dtype, shape=(T, D)), _ptr(y), _dtype_id(y.dtype), M, D, _ptr(slots, torch.int32),
                                  _ptr(weights, torch.float32, allow_none=True, shape=(T, k)), T, k, dy.data_ptr(), dw.data_ptr()), "kn_combine_backward")
     return dy, dw

@@ -5,8 +5,9 @@
 namespace {
 
 constexpr int ROUTE_MAX_EXPERTS = 1024, ROUTE_MAX_K = 32;
-constexpr int ROUTE_PAIRS = 2048; // pairs (row, choice) that a workgroup orders by itself
 constexpr int ROUTE_THREADS = 512;
+constexpr int ROUTE_TOKENS = 64;                          // rows of logits of a workgroup
+constexpr int ROUTE_PAIRS = ROUTE_TOKENS * ROUTE_MAX_K;   // pairs (row, choice) that it orders at most
 
 template <typename T> __device__ __forceinline__ float to_float(T v) { return (float)v; }
 
@@ -57,35 +58,48 @@ struct RouteArgs {
     int64_t ld;
     int32_t T, E, k, renorm;
     float *weights;
-    int32_t *ids, *slots, *rows, *offsets, *hist; // hist: a histogram per workgroup, ROUTE_PAIRS / k rows of logits each
-    int32_t tokens_per_block;
+    int32_t *ids, *slots, *rows, *offsets;
+    int32_t *hist;   // (E + 1, workgroups): pairs of each expert in each workgroup, then those before it
+    int32_t *totals; // E + 1
+    int32_t wide;    // a lane's logits are one aligned piece
 };
+
+// The V logits of row t that lane `at` holds: neighbours, -infinity behind the end
+template <typename T, int V> __device__ __forceinline__ void load_logits(const RouteArgs &p, int32_t t, bool there, int at, float v[V])
+{
+    typedef T Piece __attribute__((ext_vector_type(V)));
+    const T *l = (const T *)p.logits + (int64_t)t * p.ld + at * V;
+    if (p.wide) {
+        const bool in = there && at * V < p.E;
+        Piece x = {};
+        if (in) x = *(const Piece *)l;
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = in ? to_float((T)x[i]) : -INFINITY;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = there && at * V + i < p.E ? to_float(l[i]) : -INFINITY;
+    }
+}
 
 // Top-k of the rows [t0, t1) of logits: G lanes a row, each with V neighbouring logits in registers, so that the first lane of
 // a ballot holds the lowest index among equal values.  k times the largest is taken out; the statistics of the softmax are
-// held in 32 bits.  `count`: a histogram in the LDS.
+// held in 32 bits.  In the LDS: `count`, a histogram; `chosen`, the experts of the rows that are being worked on.
 template <typename T, int G, int V>
-__device__ void choose(const RouteArgs &p, int32_t t0, int32_t t1, int32_t *count)
+__device__ void choose(const RouteArgs &p, int32_t t0, int32_t t1, int32_t *count, int32_t *chosen)
 {
     const int lane = kn_thread() & 63, at = lane & (G - 1);
-    const T *logits = (const T *)p.logits;
-    const int per_round = (int)blockDim.x / G;
-    for (int32_t base = t0; base < t1; base += per_round) {
+    constexpr int PER_ROUND = ROUTE_THREADS / G;
+    int32_t *mine = chosen + kn_thread() / G * ROUTE_MAX_K; // (of one wavefront alone)
+    for (int32_t base = t0; base < t1; base += PER_ROUND) {
         const int32_t t = base + kn_thread() / G;
         const bool there = t < t1; // (lanes without a row stay: the whole wavefront takes part in the ballots)
         float v[V];
+        load_logits<T, V>(p, t, there, at, v);
         bool nan = false;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int32_t e = at * V + i;
-            v[i] = there && e < p.E ? to_float(logits[(int64_t)t * p.ld + e]) : -INFINITY;
-            nan |= v[i] != v[i];
-        }
+        for (int i = 0; i < V; ++i) nan |= v[i] != v[i];
         const bool poisoned = group_ballot<G>(nan, lane) != 0;
-        float top = -INFINITY, total = 0.0f, mine = 0.0f; // mine: the value of choice `at` (choices G * n + at: k <= 32, G >= 16)
-        float all = 0.0f;
-        int32_t chosen = -1, chosen2 = -1;
-        float mine2 = 0.0f;
+        float top = -INFINITY, all = 0.0f, value[2] = {-INFINITY, -INFINITY}; // value: the logits of choices at and at + G
         for (int j = 0; j < p.k; ++j) {
             float best = v[0];
 #pragma unroll
@@ -102,58 +116,42 @@ __device__ void choose(const RouteArgs &p, int32_t t0, int32_t t1, int32_t *coun
             }
             const bool some = m > -INFINITY; // (uniform in the group)
             const uint64_t holds = group_ballot<G>(some && best == m, lane);
-            const int owner = (int)__ffsll((unsigned long long)holds) - 1;
-            int32_t e = -1;
-            if (at == owner) {
+            if (at == (int)__ffsll((unsigned long long)holds) - 1) {
+                int i0 = 0;
 #pragma unroll
-                for (int i = V - 1; i >= 0; --i)
-                    if (v[i] == m) e = at * V + i;
+                for (int i = V - 1; i >= 0; --i) i0 = v[i] == m ? i : i0;
 #pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (at * V + i == e) v[i] = -INFINITY;
+                for (int i = 0; i < V; ++i) v[i] = i == i0 ? -INFINITY : v[i];
+                mine[j] = at * V + i0;
             }
-            e = __shfl(e, owner < 0 ? lane : (lane & ~(G - 1)) + owner);
-            const float w = some ? expf(m - top) : 0.0f;
-            total += w;
-            if (at == (j & (G - 1))) {
-                if (j < G) { mine = w; chosen = e; } else { mine2 = w; chosen2 = e; }
+            if (at == (j & (G - 1))) value[j / G] = some ? m : -INFINITY;
+        }
+        const float z[2] = {value[0] > -INFINITY ? expf(value[0] - top) : 0.0f, value[1] > -INFINITY ? expf(value[1] - top) : 0.0f};
+        const float scale = p.renorm ? group_sum<G>(z[0] + z[1]) : all;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (there)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const int j = at + n * G;
+                if (j >= p.k) break;
+                const int32_t e = value[n] > -INFINITY ? mine[j] : -1;
+                const int64_t pair = (int64_t)t * p.k + j;
+                p.weights[pair] = poisoned ? NAN : e >= 0 ? z[n] / scale : 0.0f;
+                p.ids[pair] = e;
+                atomicAdd(&count[e >= 0 ? e : p.E], 1); // (a sum of whole numbers: any order gives the same)
             }
-        }
-        if (!there) continue;
-        const float scale = p.renorm ? total : all;
-        for (int n = 0; n < 2; ++n) {
-            const int j = at + n * G;
-            if (j >= p.k) break;
-            const int32_t e = n ? chosen2 : chosen;
-            const int64_t pair = (int64_t)t * p.k + j;
-            float w = e >= 0 ? (n ? mine2 : mine) / scale : 0.0f;
-            if (poisoned) w = NAN;
-            p.weights[pair] = w;
-            p.ids[pair] = e;
-            atomicAdd(&count[e >= 0 ? e : p.E], 1); // (a sum of whole numbers: any order gives the same)
-        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
-template <typename T, int G, int V>
-__global__ void __launch_bounds__(ROUTE_THREADS) k_route_choose(RouteArgs p)
-{
-    __shared__ int32_t count[ROUTE_MAX_EXPERTS + 1];
-    for (int e = kn_thread(); e <= p.E; e += ROUTE_THREADS) count[e] = 0;
-    __syncthreads();
-    const int32_t t0 = kn_block() * p.tokens_per_block;
-    choose<T, G, V>(p, t0, min(p.T, t0 + p.tokens_per_block), count);
-    __syncthreads();
-    for (int e = kn_thread(); e <= p.E; e += ROUTE_THREADS) p.hist[(int64_t)kn_block() * (p.E + 1) + e] = count[e];
-}
-
-// Places of the pairs of one workgroup: start[e] in the LDS is the place of its first pair of expert e.  Stable: wavefront w
+// Places of the pairs [p0, p1) of one workgroup: start[e] in the LDS is the place of its first pair of expert e.  Stable: wavefront w
 // takes the w-th part of the pairs, 64 neighbours a step; a pair's rank among its step's comes from ballots over the
 // bits of the expert's number.  `seen`: (wavefronts, E + 1) counts.
-__device__ void place(const RouteArgs &p, int32_t p0, int32_t p1, int32_t *start, int32_t *seen)
+__device__ void place(const RouteArgs &p, int32_t p0, int32_t p1, const int32_t *start, int32_t *seen)
 {
     constexpr int WAVES = ROUTE_THREADS / 64, STEPS = ROUTE_PAIRS / ROUTE_THREADS;
     const int lane = kn_thread() & 63, wave = kn_thread() >> 6, bins = p.E + 1;
+    const int steps = (p1 - p0 + ROUTE_THREADS - 1) / ROUTE_THREADS; // (of a wavefront)
     for (int i = kn_thread(); i < WAVES * bins; i += ROUTE_THREADS) seen[i] = 0;
     __syncthreads();
     int32_t rank[STEPS], key[STEPS];
@@ -161,7 +159,10 @@ __device__ void place(const RouteArgs &p, int32_t p0, int32_t p1, int32_t *start
     const int bits = 32 - __clz(p.E);
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-        const int32_t q = p0 + (wave * STEPS + s) * 64 + lane;
+        key[s] = -1;
+        rank[s] = 0;
+        if (s >= steps) continue;
+        const int32_t q = p0 + (wave * steps + s) * 64 + lane;
         const bool there = q < p1;
         int32_t e = there ? p.ids[q] : -1;
         e = there && e < 0 ? p.E : e;
@@ -171,10 +172,8 @@ __device__ void place(const RouteArgs &p, int32_t p0, int32_t p1, int32_t *start
             const uint64_t set = __ballot((e >> b) & 1);
             same &= (e >> b) & 1 ? set : ~set;
         }
-        rank[s] = 0;
         if (there) {
-            const uint64_t below = same & ((1ull << lane) - 1);
-            rank[s] = own[e] + __popcll(below); // (the wavefront's lanes read before the last of them writes: one wavefront, in order)
+            rank[s] = own[e] + __popcll(same & ((1ull << lane) - 1)); // (every lane has read before one of them writes: one wavefront)
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             if ((same >> lane) == 1ull) own[e] = rank[s] + 1;
         }
@@ -193,44 +192,81 @@ __device__ void place(const RouteArgs &p, int32_t p0, int32_t p1, int32_t *start
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
         if (key[s] < 0) continue;
-        const int32_t q = p0 + (wave * STEPS + s) * 64 + lane;
+        const int32_t q = p0 + (wave * steps + s) * 64 + lane;
         const int32_t at = own[key[s]] + rank[s];
         p.slots[q] = at;
         p.rows[at] = q / p.k;
     }
 }
 
-// Every workgroup sums the histograms of those before it, and all of them, by itself: they lie in the L2, and a launch
-// between the two kernels costs more than reading them does.
-__global__ void __launch_bounds__(ROUTE_THREADS) k_route_place(RouteArgs p, int32_t blocks)
+// start[e] += the sum of counts before e, offsets where asked for
+__device__ void scan_counts(const RouteArgs &p, const int32_t *counts, int32_t *start, int32_t *scratch, bool store)
 {
-    extern __shared__ int32_t lds[];
-    const int bins = p.E + 1;
-    int32_t *start = lds, *total = start + bins, *seen = total + bins, *scan = seen + (ROUTE_THREADS / 64) * bins;
-    for (int e = kn_thread(); e < bins; e += ROUTE_THREADS) {
-        int32_t before = 0, all = 0;
-        for (int b = 0; b < blocks; ++b) {
-            const int32_t n = p.hist[(int64_t)b * bins + e];
-            before += b < kn_block() ? n : 0;
-            all += n;
-        }
-        start[e] = before;
-        total[e] = all;
-    }
-    __syncthreads();
     int32_t carry = 0;
-    for (int e0 = 0; e0 < bins; e0 += ROUTE_THREADS) {
+    for (int e0 = 0; e0 <= p.E; e0 += ROUTE_THREADS) {
         const int e = e0 + kn_thread();
         int32_t sum;
-        const int32_t ex = kn_block_exclusive_scan(e < bins ? total[e] : 0, scan, sum);
-        if (e < bins) {
-            start[e] += carry + ex;
-            if (kn_block() == 0) p.offsets[e] = carry + ex; // (offsets[E]: where the pairs without an expert begin)
+        const int32_t before = kn_block_exclusive_scan(e <= p.E ? counts[e] : 0, scratch, sum);
+        if (e <= p.E) {
+            start[e] += carry + before;
+            if (store) p.offsets[e] = carry + before; // (offsets[E]: where the pairs without an expert begin)
         }
         carry += sum;
     }
-    const int32_t p0 = kn_block() * p.tokens_per_block * p.k;
-    place(p, p0, (int32_t)min((int64_t)p.T * p.k, (int64_t)p0 + (int64_t)p.tokens_per_block * p.k), start, seen);
+}
+
+// ONE: all rows are one workgroup's, which places them too; else its histogram is left for k_route_scan and k_route_place
+template <typename T, int G, int V, bool ONE>
+__global__ void __launch_bounds__(ROUTE_THREADS) k_route_choose(RouteArgs p)
+{
+    extern __shared__ int32_t lds[];
+    __shared__ int32_t chosen[ROUTE_THREADS / G * ROUTE_MAX_K], scratch[16];
+    const int bins = p.E + 1;
+    int32_t *count = lds, *start = count + bins, *seen = start + bins; // (start, seen: ONE only)
+    for (int e = kn_thread(); e < bins; e += ROUTE_THREADS) count[e] = 0;
+    __syncthreads();
+    const int32_t t0 = kn_block() * ROUTE_TOKENS, t1 = min(p.T, t0 + ROUTE_TOKENS);
+    choose<T, G, V>(p, t0, t1, count, chosen);
+    __syncthreads();
+    if constexpr (ONE) {
+        for (int e = kn_thread(); e < bins; e += ROUTE_THREADS) start[e] = 0;
+        __threadfence_block(); // (this workgroup's ids are read again below)
+        __syncthreads();
+        scan_counts(p, count, start, scratch, true);
+        __syncthreads();
+        place(p, 0, p.T * p.k, start, seen);
+    } else {
+        for (int e = kn_thread(); e < bins; e += ROUTE_THREADS) p.hist[(int64_t)e * gridDim.x + kn_block()] = count[e];
+    }
+}
+
+// One workgroup per expert: its pairs before each workgroup, and in all
+__global__ void __launch_bounds__(256) k_route_scan(RouteArgs p, int32_t blocks)
+{
+    __shared__ int32_t scratch[16];
+    int32_t *h = p.hist + (int64_t)kn_block() * blocks;
+    int32_t carry = 0;
+    for (int32_t b0 = 0; b0 < blocks; b0 += 256) {
+        const int32_t b = b0 + kn_thread();
+        int32_t sum;
+        const int32_t before = kn_block_exclusive_scan(b < blocks ? h[b] : 0, scratch, sum);
+        if (b < blocks) h[b] = carry + before;
+        carry += sum;
+    }
+    if (kn_thread() == 0) p.totals[kn_block()] = carry;
+}
+
+__global__ void __launch_bounds__(ROUTE_THREADS) k_route_place(RouteArgs p, int32_t blocks)
+{
+    extern __shared__ int32_t lds[];
+    __shared__ int32_t scratch[16];
+    const int bins = p.E + 1;
+    int32_t *start = lds, *seen = start + bins;
+    for (int e = kn_thread(); e < bins; e += ROUTE_THREADS) start[e] = p.hist[(int64_t)e * blocks + kn_block()];
+    scan_counts(p, p.totals, start, scratch, kn_block() == 0);
+    __syncthreads();
+    const int32_t p0 = kn_block() * ROUTE_TOKENS * p.k;
+    place(p, p0, (int32_t)min((int64_t)p.T * p.k, (int64_t)p0 + ROUTE_TOKENS * p.k), start, seen);
 }
 
 __global__ void k_route_none(int32_t *offsets, int32_t n)
@@ -239,55 +275,69 @@ __global__ void k_route_none(int32_t *offsets, int32_t n)
     if (i < n) offsets[i] = 0;
 }
 
-// One wavefront per row of logits.  renormalised: dl_j = w_j (g_j - sum of w g), zeros elsewhere; else with the softmax over all
-// p_e: dl_e = p_e ([e chosen] g_e - sum of w g).
-template <typename T>
+// Rows of logits as in `choose`.  The chosen experts' gradients are brought to their places through a row in the LDS.  renormalised:
+// dl_j = w_j (g_j - sum of w g), zeros elsewhere; else, with the softmax p over all: dl_e = p_e ([e chosen] g_e - sum of w g).
+template <typename T, int G, int V>
 __global__ void __launch_bounds__(256) k_route_backward(RouteArgs p, const float *__restrict__ dweights, T *__restrict__ dlogits)
 {
-    const int lane = kn_thread() & 63;
-    const int32_t t = kn_block() * 4 + (kn_thread() >> 6);
-    if (t >= p.T) return;
-    const T *l = (const T *)p.logits + (int64_t)t * p.ld;
-    T *d = dlogits + (int64_t)t * p.E;
-    const int64_t pair = (int64_t)t * p.k + lane;
-    int32_t e = -1;
-    float w = 0.0f, g = 0.0f;
-    if (lane < p.k) {
-        e = p.ids[pair];
-        if ((uint32_t)e >= (uint32_t)p.E) e = -1;
-        if (e >= 0) { w = p.weights[pair]; g = dweights[pair]; }
+    __shared__ float lds[256 * V];
+    const int lane = kn_thread() & 63, at = lane & (G - 1);
+    float *row = lds + (kn_thread() & ~(G - 1)) * V; // (of one wavefront alone)
+    const int32_t t = kn_block() * (256 / G) + kn_thread() / G;
+    const bool there = t < p.T;
+    const float other = __int_as_float(0x7fc00001); // marks an expert that was not chosen (no product here has these bits)
+#pragma unroll
+    for (int i = 0; i < V; ++i) row[at * V + i] = p.renorm ? 0.0f : other;
+    int32_t e[2] = {-1, -1};
+    float w[2] = {0.0f, 0.0f}, g[2] = {0.0f, 0.0f}, part = 0.0f;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const int j = at + n * G;
+        if (there && j < p.k) {
+            const int64_t pair = (int64_t)t * p.k + j;
+            e[n] = p.ids[pair];
+            if ((uint32_t)e[n] >= (uint32_t)p.E) e[n] = -1;
+            if (e[n] >= 0) { w[n] = p.weights[pair]; g[n] = dweights[pair]; }
+            part += w[n] * g[n];
+        }
     }
-    float mean = group_sum<64>(w * g);
-    float top = -INFINITY, all = 0.0f;
+    const float mean = group_sum<G>(part);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+        if (e[n] >= 0) row[e[n]] = w[n] * (g[n] - mean);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    float d[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) d[i] = row[at * V + i];
     if (!p.renorm) {
-        for (int i = lane; i < p.E; i += 64) top = fmaxf(top, to_float(l[i]));
-        top = group_max<64>(top);
-        for (int i = lane; i < p.E; i += 64) {
-            const float v = to_float(l[i]);
-            all += v == -INFINITY ? 0.0f : expf(v - top);
+        float v[V], best = -INFINITY, s = 0.0f;
+        load_logits<T, V>(p, t, there, at, v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) best = fmaxf(best, v[i]);
+        const float top = group_max<G>(best);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            v[i] = v[i] == -INFINITY ? 0.0f : expf(v[i] - top);
+            s += v[i];
         }
-        all = group_sum<64>(all);
+        const float all = group_sum<G>(s);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (__float_as_int(d[i]) == __float_as_int(other)) d[i] = top > -INFINITY ? v[i] / all * -mean : 0.0f;
     }
-    for (int i0 = 0; i0 < p.E; i0 += 64) {
-        const int i = i0 + lane;
-        float gi = 0.0f, wi = 0.0f;
-        bool hit = false;
-        for (int j = 0; j < p.k; ++j) {
-            const int32_t ej = __builtin_amdgcn_readlane(e, j);
-            const float gj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), j));
-            const float wj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), j));
-            if (ej == i) { gi = gj; wi = wj; hit = true; }
-        }
-        if (i >= p.E) continue;
-        float v = 0.0f;
-        if (p.renorm) {
-            if (hit) v = wi * (gi - mean);
-        } else if (top > -INFINITY) {
-            const float z = to_float(l[i]);
-            const float pi = hit ? wi : z == -INFINITY ? 0.0f : expf(z - top) / all;
-            v = pi * (gi - mean);
-        }
-        d[i] = (T)v;
+    if (!there) return;
+    typedef T Piece __attribute__((ext_vector_type(V)));
+    T *out = dlogits + (int64_t)t * p.E + at * V;
+    if (p.wide) {
+        Piece x;
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = (T)d[i];
+        if (at * V < p.E) *(Piece *)out = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (at * V + i < p.E) out[i] = (T)d[i];
     }
 }
 
@@ -360,19 +410,22 @@ __global__ void __launch_bounds__(256) k_combine_backward(const T *__restrict__ 
 
 bool route_supported(int64_t T, int32_t E, int32_t k) { return E <= ROUTE_MAX_EXPERTS && k <= ROUTE_MAX_K && T * k <= KN_MAX_ROWS; }
 bool route_valid(int64_t T, int32_t E, int32_t k) { return T >= 0 && E >= 1 && k >= 1 && k <= E; }
-int32_t route_tokens_per_block(int32_t k) { return ROUTE_PAIRS / k; }
 
-template <typename T> int route_choose(hipStream_t st, const RouteArgs &p, int32_t blocks)
+// Calls f with the lanes that take a row of E logits and the logits that each of them holds.
+template <int N> struct Int { static constexpr int n = N; };
+template <typename F> int route_shape(int32_t E, F &&f)
 {
-#define KN_CHOOSE(G, V) hipLaunchKernelGGL((k_route_choose<T, G, V>), dim3(blocks), dim3(ROUTE_THREADS), 0, st, p)
-    if (p.E <= 16) KN_CHOOSE(16, 1);
-    else if (p.E <= 64) KN_CHOOSE(16, 4);
-    else if (p.E <= 128) KN_CHOOSE(16, 8);
-    else if (p.E <= 256) KN_CHOOSE(16, 16);
-    else KN_CHOOSE(64, 16);
-#undef KN_CHOOSE
-    KN_CHECK_LAUNCH();
-    return KN_OK;
+    if (E <= 16) return f(Int<16>(), Int<1>());
+    if (E <= 64) return f(Int<16>(), Int<4>());
+    if (E <= 128) return f(Int<16>(), Int<8>());
+    if (E <= 256) return f(Int<16>(), Int<16>());
+    return f(Int<64>(), Int<16>());
+}
+// Whether every lane's V values are one aligned piece, in each of the rows
+bool route_wide(const void *at, int64_t ld, int32_t E, int V, int item)
+{
+    const int bytes = V * item, align = bytes < 16 ? bytes : 16;
+    return E % V == 0 && ((uintptr_t)at & (align - 1)) == 0 && ld * item % align == 0;
 }
 
 } // namespace
@@ -381,7 +434,7 @@ extern "C" int kn_route_workspace_bytes(int64_t T, int32_t E, int32_t k, int64_t
 {
     if (!out_bytes || !route_valid(T, E, k)) return KN_E_INVALID_ARG;
     if (!route_supported(T, E, k)) return KN_E_UNSUPPORTED;
-    *out_bytes = kn_align_up(kn_div_up(T > 0 ? T : 1, route_tokens_per_block(k)) * (E + 1) * 4, 256);
+    *out_bytes = T <= ROUTE_TOKENS ? 0 : kn_align_up((kn_div_up(T, ROUTE_TOKENS) + 1) * (E + 1) * 4, 256);
     return KN_OK;
 }
 
@@ -399,12 +452,25 @@ extern "C" int kn_route(void *stream, const void *logits, int32_t dtype, int64_t
     }
     int64_t need = 0;
     KN_TRY(kn_route_workspace_bytes(T, E, k, &need));
-    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return KN_E_WORKSPACE;
-    RouteArgs p = {logits, ld, (int32_t)T, E, k, renormalize != 0, weights, ids, slots, rows, offsets, (int32_t *)workspace, route_tokens_per_block(k)};
-    const int32_t blocks = (int32_t)kn_div_up(T, p.tokens_per_block);
-    KN_TRY(kn_with_type(dtype, [&](auto v) -> int { return route_choose<decltype(v)>(st, p, blocks); }));
-    const size_t lds = (size_t)((2 + ROUTE_THREADS / 64) * (E + 1) + 16) * 4;
-    hipLaunchKernelGGL(k_route_place, dim3(blocks), dim3(ROUTE_THREADS), lds, st, p, blocks);
+    if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return KN_E_WORKSPACE;
+    const int32_t blocks = (int32_t)kn_div_up(T, ROUTE_TOKENS);
+    RouteArgs p = {logits, ld, (int32_t)T, E, k, renormalize != 0, weights, ids, slots, rows, offsets, (int32_t *)workspace, (int32_t *)workspace + (int64_t)blocks * (E + 1), 0};
+    const size_t seen = (size_t)(ROUTE_THREADS / 64) * (E + 1) * 4, bins = (size_t)(E + 1) * 4;
+    KN_TRY(kn_with_type(dtype, [&](auto v) -> int {
+        typedef decltype(v) E_;
+        return route_shape(E, [&](auto g, auto n) -> int {
+            constexpr int G = decltype(g)::n, V = decltype(n)::n;
+            p.wide = route_wide(logits, ld, E, V, sizeof(E_));
+            if (blocks == 1) hipLaunchKernelGGL((k_route_choose<E_, G, V, true>), dim3(1), dim3(ROUTE_THREADS), 2 * bins + seen, st, p);
+            else hipLaunchKernelGGL((k_route_choose<E_, G, V, false>), dim3(blocks), dim3(ROUTE_THREADS), bins, st, p);
+            KN_CHECK_LAUNCH();
+            return KN_OK;
+        });
+    }));
+    if (blocks == 1) return KN_OK;
+    hipLaunchKernelGGL(k_route_scan, dim3(E + 1), dim3(256), 0, st, p, blocks);
+    KN_CHECK_LAUNCH();
+    hipLaunchKernelGGL(k_route_place, dim3(blocks), dim3(ROUTE_THREADS), bins + seen, st, p, blocks);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }
@@ -415,12 +481,16 @@ extern "C" int kn_route_backward(void *stream, const void *logits, int32_t dtype
     if (!route_valid(T, E, k) || !kn_dtype_ok(dtype) || ld < E || (T > 0 && (!logits || !weights || !ids || !dweights || !dlogits))) return KN_E_INVALID_ARG;
     if (!route_supported(T, E, k)) return KN_E_UNSUPPORTED;
     if (T == 0) return KN_OK;
-    RouteArgs p = {logits, ld, (int32_t)T, E, k, renormalize != 0, const_cast<float *>(weights), const_cast<int32_t *>(ids), nullptr, nullptr, nullptr, nullptr, 0};
+    RouteArgs p = {logits, ld, (int32_t)T, E, k, renormalize != 0, const_cast<float *>(weights), const_cast<int32_t *>(ids), nullptr, nullptr, nullptr, nullptr, nullptr, 0};
     return kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
-        hipLaunchKernelGGL((k_route_backward<E_>), dim3((unsigned)kn_div_up(T, 4)), dim3(256), 0, (hipStream_t)stream, p, dweights, (E_ *)dlogits);
-        KN_CHECK_LAUNCH();
-        return KN_OK;
+        return route_shape(E, [&](auto g, auto n) -> int {
+            constexpr int G = decltype(g)::n, V = decltype(n)::n;
+            p.wide = route_wide(logits, ld, E, V, sizeof(E_)) && route_wide(dlogits, E, E, V, sizeof(E_));
+            hipLaunchKernelGGL((k_route_backward<E_, G, V>), dim3((unsigned)kn_div_up(T, 256 / G)), dim3(256), 0, (hipStream_t)stream, p, dweights, (E_ *)dlogits);
+            KN_CHECK_LAUNCH();
+            return KN_OK;
+        });
     });
 }
 
