@@ -495,13 +495,11 @@ def route(logits, k, renormalize=True):
     ids = torch.empty_like(weights, dtype=i32)
     slots, rows, offsets = torch.empty_like(ids), ids.new_empty(T * k), ids.new_empty(E + 1)
     args = (_stream(), ptr, dt, T, E, ld, k, 1 if renormalize else 0, weights.data_ptr(), ids.data_ptr(), slots.data_ptr(), rows.data_ptr(), offsets.data_ptr())
-    rc = L.kn_route(*args, None, 0)  # (a few rows need no workspace)
-    if rc == KN_E_WORKSPACE:
-        need = C.c_int64()
+    need, ws = C.c_int64(), None
+    if T > 64:  # (fewer need no workspace)
         _check(L.kn_route_workspace_bytes(T, E, k, C.byref(need)), "kn_route_workspace_bytes")
-        ws = torch.empty(need.value, dtype=torch.uint8, device=logits.device)
-        rc = L.kn_route(*args, ws.data_ptr(), need.value)
-    _check(rc, "kn_route")
+        ws = ids.new_empty(need.value // 4)
+    _check(L.kn_route(*args, None if ws is None else ws.data_ptr(), need.value), "kn_route")
     return weights, ids, slots, rows, offsets
 
 

@@ -53,6 +53,25 @@ template <int G> __device__ __forceinline__ uint64_t group_ballot(bool v, int la
     return G == 64 ? b : (b >> (lane & 48)) & 0xffffull;
 }
 
+// The same for whole numbers of 16 lanes
+__device__ __forceinline__ int32_t row_max_i32(int32_t v)
+{
+    constexpr int ROW_ROR = 0x120;
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, ROW_ROR + 8, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, ROW_ROR + 4, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(v, v, ROW_ROR + 2, 0xf, 0xf, false));
+    return max(v, __builtin_amdgcn_update_dpp(v, v, ROW_ROR + 1, 0xf, 0xf, false));
+}
+template <int G> __device__ __forceinline__ int32_t group_max_i32(int32_t v)
+{
+    v = row_max_i32(v);
+    if constexpr (G == 64) {
+        v = max(v, __shfl_xor(v, 16));
+        v = max(v, __shfl_xor(v, 32));
+    }
+    return v;
+}
+
 struct RouteArgs {
     const void *logits;
     int64_t ld;
@@ -81,52 +100,69 @@ template <typename T, int V> __device__ __forceinline__ void load_logits(const R
     }
 }
 
+// Logits as whole numbers of the same order (both zeros alike, a NaN below everything): comparing and taking the largest is one
+// instruction each, also across lanes.
+constexpr int32_t KEY_NONE = INT32_MIN, KEY_LOWEST = (int32_t)0x807fffff; // nothing; -infinity
+__device__ __forceinline__ int32_t key_of(float v)
+{
+    const int32_t b = __float_as_int(v + 0.0f);
+    return v != v ? KEY_NONE : b ^ ((b >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float value_of(int32_t key) { return __int_as_float(key ^ ((key >> 31) & 0x7fffffff)); }
+
 // Top-k of the rows [t0, t1) of logits: G lanes a row, each with V neighbouring logits in registers, so that the first lane of
-// a ballot holds the lowest index among equal values.  k times the largest is taken out; the statistics of the softmax are
-// held in 32 bits.  In the LDS: `count`, a histogram; `chosen`, the experts of the rows that are being worked on.
+// those that hold the largest holds the lowest index.  k times the largest is taken out; the statistics of the softmax are held in
+// 32 bits.  In the LDS: `count`, a histogram; `chosen`, the experts of the rows that are being worked on.
 template <typename T, int G, int V>
 __device__ void choose(const RouteArgs &p, int32_t t0, int32_t t1, int32_t *count, int32_t *chosen)
 {
     const int lane = kn_thread() & 63, at = lane & (G - 1);
     constexpr int PER_ROUND = ROUTE_THREADS / G;
+    const uint64_t before = ((1ull << lane) - 1) & ~((1ull << (lane & ~(G - 1))) - 1); // the row's lanes before this one
     int32_t *mine = chosen + kn_thread() / G * ROUTE_MAX_K; // (of one wavefront alone)
     for (int32_t base = t0; base < t1; base += PER_ROUND) {
         const int32_t t = base + kn_thread() / G;
         const bool there = t < t1; // (lanes without a row stay: the whole wavefront takes part in the ballots)
         float v[V];
+        int32_t key[V];
         load_logits<T, V>(p, t, there, at, v);
         bool nan = false;
 #pragma unroll
-        for (int i = 0; i < V; ++i) nan |= v[i] != v[i];
+        for (int i = 0; i < V; ++i) {
+            nan |= v[i] != v[i];
+            key[i] = key_of(v[i]);
+        }
         const bool poisoned = group_ballot<G>(nan, lane) != 0;
-        float top = -INFINITY, all = 0.0f, value[2] = {-INFINITY, -INFINITY}; // value: the logits of choices at and at + G
+        float all = 0.0f;
+        int32_t first = KEY_NONE, value[2] = {KEY_NONE, KEY_NONE}; // value: the keys of choices at and at + G
         for (int j = 0; j < p.k; ++j) {
-            float best = v[0];
+            int32_t best = key[0];
 #pragma unroll
-            for (int i = 1; i < V; ++i) best = fmaxf(best, v[i]); // (a NaN is never the larger)
-            const float m = group_max<G>(best);
+            for (int i = 1; i < V; ++i) best = max(best, key[i]);
+            const int32_t m = group_max_i32<G>(best);
             if (j == 0) {
-                top = m;
+                first = m;
                 if (!p.renorm) {
+                    const float top = value_of(m);
                     float s = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) s += v[i] == -INFINITY ? 0.0f : expf(v[i] - top);
+                    for (int i = 0; i < V; ++i) s += key[i] <= KEY_LOWEST ? 0.0f : expf(v[i] - top);
                     all = group_sum<G>(s);
                 }
             }
-            const bool some = m > -INFINITY; // (uniform in the group)
-            const uint64_t holds = group_ballot<G>(some && best == m, lane);
-            if (at == (int)__ffsll((unsigned long long)holds) - 1) {
+            const uint64_t holds = __ballot(best == m);
+            if (best == m && m > KEY_LOWEST && (holds & before) == 0) {
                 int i0 = 0;
 #pragma unroll
-                for (int i = V - 1; i >= 0; --i) i0 = v[i] == m ? i : i0;
+                for (int i = V - 1; i >= 0; --i) i0 = key[i] == m ? i : i0;
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[i] = i == i0 ? -INFINITY : v[i];
+                for (int i = 0; i < V; ++i) key[i] = i == i0 ? KEY_NONE : key[i];
                 mine[j] = at * V + i0;
             }
-            if (at == (j & (G - 1))) value[j / G] = some ? m : -INFINITY;
+            if (at == (j & (G - 1))) value[j / G] = m;
         }
-        const float z[2] = {value[0] > -INFINITY ? expf(value[0] - top) : 0.0f, value[1] > -INFINITY ? expf(value[1] - top) : 0.0f};
+        const float top = value_of(first);
+        const float z[2] = {value[0] > KEY_LOWEST ? expf(value_of(value[0]) - top) : 0.0f, value[1] > KEY_LOWEST ? expf(value_of(value[1]) - top) : 0.0f};
         const float scale = p.renorm ? group_sum<G>(z[0] + z[1]) : all;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (there)
@@ -134,7 +170,7 @@ __device__ void choose(const RouteArgs &p, int32_t t0, int32_t t1, int32_t *coun
             for (int n = 0; n < 2; ++n) {
                 const int j = at + n * G;
                 if (j >= p.k) break;
-                const int32_t e = value[n] > -INFINITY ? mine[j] : -1;
+                const int32_t e = value[n] > KEY_LOWEST ? mine[j] : -1;
                 const int64_t pair = (int64_t)t * p.k + j;
                 p.weights[pair] = poisoned ? NAN : e >= 0 ? z[n] / scale : 0.0f;
                 p.ids[pair] = e;
@@ -256,14 +292,30 @@ __global__ void __launch_bounds__(256) k_route_scan(RouteArgs p, int32_t blocks)
     if (kn_thread() == 0) p.totals[kn_block()] = carry;
 }
 
-__global__ void __launch_bounds__(ROUTE_THREADS) k_route_place(RouteArgs p, int32_t blocks)
+// SCANNED: k_route_scan has been there.  Else every workgroup sums the few histograms by itself, which takes less than a launch.
+constexpr int ROUTE_FEW_BLOCKS = 64;
+template <bool SCANNED> __global__ void __launch_bounds__(ROUTE_THREADS) k_route_place(RouteArgs p, int32_t blocks)
 {
     extern __shared__ int32_t lds[];
     __shared__ int32_t scratch[16];
     const int bins = p.E + 1;
-    int32_t *start = lds, *seen = start + bins;
-    for (int e = kn_thread(); e < bins; e += ROUTE_THREADS) start[e] = p.hist[(int64_t)e * blocks + kn_block()];
-    scan_counts(p, p.totals, start, scratch, kn_block() == 0);
+    int32_t *start = lds, *seen = start + bins, *total = seen; // (the totals are read before `seen` is written)
+    for (int e = kn_thread(); e < bins; e += ROUTE_THREADS) {
+        const int32_t *h = p.hist + (int64_t)e * blocks;
+        if constexpr (SCANNED) {
+            start[e] = h[kn_block()];
+        } else {
+            int32_t before = 0, all = 0;
+            for (int b = 0; b < blocks; ++b) {
+                before += b < kn_block() ? h[b] : 0;
+                all += h[b];
+            }
+            start[e] = before;
+            total[e] = all;
+        }
+    }
+    __syncthreads();
+    scan_counts(p, SCANNED ? p.totals : total, start, scratch, kn_block() == 0);
     __syncthreads();
     const int32_t p0 = kn_block() * ROUTE_TOKENS * p.k;
     place(p, p0, (int32_t)min((int64_t)p.T * p.k, (int64_t)p0 + ROUTE_TOKENS * p.k), start, seen);
@@ -468,9 +520,11 @@ extern "C" int kn_route(void *stream, const void *logits, int32_t dtype, int64_t
         });
     }));
     if (blocks == 1) return KN_OK;
-    hipLaunchKernelGGL(k_route_scan, dim3(E + 1), dim3(256), 0, st, p, blocks);
-    KN_CHECK_LAUNCH();
-    hipLaunchKernelGGL(k_route_place, dim3(blocks), dim3(ROUTE_THREADS), bins + seen, st, p, blocks);
+    if (blocks > ROUTE_FEW_BLOCKS) {
+        hipLaunchKernelGGL(k_route_scan, dim3(E + 1), dim3(256), 0, st, p, blocks);
+        KN_CHECK_LAUNCH();
+    }
+    hipLaunchKernelGGL(blocks > ROUTE_FEW_BLOCKS ? k_route_place<true> : k_route_place<false>, dim3(blocks), dim3(ROUTE_THREADS), bins + seen, st, p, blocks);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }
