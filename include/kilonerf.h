@@ -379,9 +379,12 @@ int kn_grouped_linear(void *stream, const kn_linear_desc *desc, const void *x /*
 int kn_grouped_linear_dx(void *stream, const kn_linear_desc *desc, const void *dy /*dev M*N*/, const void *w, const void *x_relu,
                          const int32_t *offsets, const int32_t *rows, void *dx /*dev M*K*/);
 /* Gradients of its weights and biases: dw[e] = sum over the network's rows of x[r]^T dy[i], in w's layout, and db[e] = sum of
- * dy[i]; zeros for a network without rows. */
+ * dy[i]; zeros for a network without rows.  Workspace (dev, 256-byte aligned; NULL where it is 0 bytes): sums of networks with many
+ * rows, whose parts are added in order. */
+int kn_grouped_linear_dw_workspace_bytes(const kn_linear_desc *desc, int64_t *out_bytes);
 int kn_grouped_linear_dw(void *stream, const kn_linear_desc *desc, const void *x, const void *dy, const int32_t *offsets,
-                         const int32_t *rows, void *dw /*dev E*K*N*/, void *db /*dev E*N, nullable*/);
+                         const int32_t *rows, void *dw /*dev E*K*N*/, void *db /*dev E*N, nullable*/, void *workspace,
+                         int64_t workspace_bytes);
 
 /* The same layer in 8 bits (e4m3).  kb = ceil(K / 128) blocks of inputs, zeros behind the K-th.
  * kn_quantize_f8: rows x (R, K) -> q (dev, R * kb*128 bytes) and scales (dev, R * kb): s = max(amax, 2^-100) * (1/448), in fp32, over a

@@ -24,6 +24,7 @@ EXPORTS = ["kn_error_string", "kn_last_hip_error", "kn_params_per_net", "kn_crea
            "kn_workspace_bytes", "kn_cell_ids", "kn_bucket", "kn_eval_grouped", "kn_eval_grouped_static", "kn_march", "kn_composite",
            "kn_render", "kn_composite_deltas", "kn_march_stratified", "kn_render_stratified", "kn_set_render_params", "kn_profile_enable", "kn_profile_read",
            "kn_route_workspace_bytes", "kn_route", "kn_route_backward", "kn_grouped_linear", "kn_grouped_linear_dx", "kn_grouped_linear_dw",
+           "kn_grouped_linear_dw_workspace_bytes",
            "kn_quantize_f8", "kn_quantize_f8_weights", "kn_grouped_linear_f8", "kn_combine", "kn_combine_backward"]
 
 
@@ -111,7 +112,8 @@ def load_library(build_if_missing: bool = True):
     L.kn_route_backward.argtypes = [vp, vp, i32, i64, i32, i64, i32, i32, vp, vp, vp, vp]
     L.kn_grouped_linear.argtypes = [vp, desc, vp, vp, vp, vp, vp, i32, vp]
     L.kn_grouped_linear_dx.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp]
-    L.kn_grouped_linear_dw.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp]
+    L.kn_grouped_linear_dw_workspace_bytes.argtypes = [desc, C.POINTER(i64)]
+    L.kn_grouped_linear_dw.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp, vp, i64]
     L.kn_quantize_f8.argtypes = [vp, vp, i32, i64, i32, i64, vp, vp]
     L.kn_quantize_f8_weights.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp]
     L.kn_grouped_linear_f8.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp, vp, i32, vp]
@@ -558,8 +560,13 @@ def grouped_linear_dw(dy, x, w, offsets, rows=None, want_bias=True):
     d, M, px, _, pr = _linear_desc(x, w, rows)
     dw = torch.empty_like(w)  # (keeps the layout of dense weights)
     db = x.new_empty((d.experts, d.n_out)) if want_bias else None
+    need, ws = C.c_int64(), None
+    if M > 512:  # (fewer rows need no workspace)
+        _check(L.kn_grouped_linear_dw_workspace_bytes(C.byref(d), C.byref(need)), "kn_grouped_linear_dw_workspace_bytes")
+        ws = torch.empty(need.value, dtype=torch.uint8, device=x.device) if need.value else None
     _check(L.kn_grouped_linear_dw(_stream(), C.byref(d), px, _ptr(dy, x.dtype, shape=(M, d.n_out)), _ptr(offsets, torch.int32, shape=(d.experts + 1,)),
-                                  pr, dw.data_ptr(), None if db is None else db.data_ptr()), "kn_grouped_linear_dw")
+                                  pr, dw.data_ptr(), None if db is None else db.data_ptr(), None if ws is None else ws.data_ptr(), need.value),
+           "kn_grouped_linear_dw")
     return dw, db
 
 

@@ -71,19 +71,6 @@ __device__ __forceinline__ KnPiece kn_find_piece(const int32_t *__restrict__ off
     p.begin = number >= first ? o + (number - first) * len : p.end; // (always, where offsets start at 0 and do not fall)
     return p;
 }
-// The network with the `turn`-th most rows (ties: the lower number first), of up to 64: long ones begin first, short ones fill the end.
-__device__ __forceinline__ int32_t kn_longest(const int32_t *__restrict__ offsets, int32_t E, int32_t M, int32_t turn)
-{
-    const int lane = kn_thread() & (KN_WAVE - 1);
-    const int32_t o = kn_offset(offsets, min(lane, E), M);
-    const int32_t n = lane < E ? max(0, kn_offset(offsets, min(lane + 1, E), M) - o) : -1;
-    int32_t rank = 0;
-    for (int e = 0; e < E; ++e) {
-        const int32_t other = __builtin_amdgcn_readlane(n, e);
-        rank += other > n || (other == n && e < lane) ? 1 : 0;
-    }
-    return __builtin_amdgcn_readfirstlane((int32_t)__ffsll((unsigned long long)__ballot(lane < E && rank == turn)) - 1);
-}
 static inline int64_t kn_pieces(int64_t M, int64_t E, int64_t len) { return M / len + E + 1; }
 
 // 16 x 16 products of fragments of 8 values a lane: lane l holds row (or column) l % 16 and the contraction's 8 (l / 16) .. + 7
@@ -105,11 +92,24 @@ __device__ __forceinline__ kn_f32x4 kn_mfma(kn_f32x4 a, kn_f32x4 b, kn_f32x4 c)
 struct KnProduct {
     const void *a, *b, *bias, *mask; // mask: out(i, j) becomes 0 where mask(row i, j) <= 0 (a ReLU's result)
     void *out, *out_bias;            // out_bias (weight gradient): sum over the rows r of b(r, j)
-    const int32_t *offsets, *rows, *mask_rows; // rows: of a, mask_rows: of the mask, both nullable
+    const int32_t *offsets, *rows, *b_index, *mask_rows; // rows: of a, b_index: of b, mask_rows: of the mask; nullable
     int64_t lda, ldb, ldm;           // row strides in elements: a, b (weight gradient), mask
     int64_t b_group, b_c, b_j;       // strides of b_e: network, contraction, column
     int64_t o_group, o_i, o_j;       // strides of out: network (weight gradient), row, column
     int32_t M, E, I, J, C;           // rows, networks; weight gradient: rows of out_e; columns of out; contraction
     int32_t a_rows, b_rows, m_rows;  // rows that a, b (weight gradient) and the mask have (an index outside is a row of zeros)
     int32_t relu;
+    int32_t wide;                    // 8 columns lie in whole 16-byte pieces, of everything that has columns
 };
+
+// What the grouped products check alike
+static inline int kn_linear_check(const kn_linear_desc *d)
+{
+    if (!d || d->rows < 0 || d->x_rows < 0 || d->experts < 1 || d->n_in < 1 || d->n_out < 1 || !kn_dtype_ok(d->dtype) ||
+        (d->w_layout != KN_W_IN_OUT && d->w_layout != KN_W_OUT_IN) || d->ldx < d->n_in)
+        return KN_E_INVALID_ARG;
+    if (d->rows > KN_MAX_ROWS || d->x_rows > KN_MAX_ROWS || d->experts > KN_MAX_EXPERTS || d->n_in > KN_MAX_WIDTH || d->n_out > KN_MAX_WIDTH)
+        return KN_E_UNSUPPORTED;
+    return KN_OK;
+}
+

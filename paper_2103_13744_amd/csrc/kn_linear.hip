@@ -4,127 +4,27 @@
 
 namespace {
 
-constexpr int ANY_TILE = 64, ANY_STEP = 32;
-
-// Any sizes, strides and alignment: values are fetched one by one, checked one by one, and laid out in the LDS with the
-// contraction contiguous, so that a fragment is 8 neighbours of a row.  A workgroup of four wavefronts makes 64 x 64 results,
-// each wavefront 32 x 32 of them as 2 x 2 products of 16 x 16.  REDUCE: the weight gradient, whose contraction is the group.
-template <typename T, bool REDUCE>
-__global__ void __launch_bounds__(256) k_product_any(KnProduct p)
-{
-    constexpr int W = sizeof(T) == 4 ? 4 : 8;       // values of a fragment
-    constexpr int LD = ANY_STEP + 16 / sizeof(T);   // (a row more by 16 bytes: fragments of 16 rows spread over the banks)
-    typedef T Frag __attribute__((ext_vector_type(W)));
-    __shared__ __align__(16) T as[ANY_TILE * LD];
-    __shared__ __align__(16) T bs[ANY_TILE * LD];
-    const int tid = kn_thread(), lane = tid & 63, wave = tid >> 6;
-    const int ntiles = (p.J + ANY_TILE - 1) / ANY_TILE;
-    const int number = kn_block() / ntiles, j0 = (kn_block() % ntiles) * ANY_TILE;
-    int32_t group, i0, iend, c0, cend;
-    if constexpr (REDUCE) {
-        const int itiles = (p.I + ANY_TILE - 1) / ANY_TILE;
-        group = number / itiles;
-        i0 = (number % itiles) * ANY_TILE;
-        iend = p.I;
-        c0 = kn_offset(p.offsets, group, p.M);
-        cend = max(c0, kn_offset(p.offsets, group + 1, p.M));
-    } else {
-        const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, ANY_TILE, number);
-        group = piece.group;
-        i0 = piece.begin;
-        iend = piece.end;
-        c0 = 0;
-        cend = group < p.E ? p.C : 0; // (rows without a network: zeros)
-        if (i0 >= iend) return;
-    }
-    const T *a = (const T *)p.a, *b = (const T *)p.b;
-    if constexpr (!REDUCE) b += (int64_t)group * p.b_group; // (group E: b is not read)
-    const int wi = (wave >> 1) * 32, wj = (wave & 1) * 32;
-    kn_f32x4 acc[2][2] = {};
-    float colsum = 0.0f; // REDUCE with out_bias: thread j < 64 of a workgroup with i0 = 0 sums its column
-    for (; c0 < cend; c0 += ANY_STEP) {
-        __syncthreads();
-#pragma unroll
-        for (int t = 0; t < ANY_TILE * ANY_STEP / 256; ++t) {
-            const int q = tid + 256 * t;
-            // neighbouring threads take neighbouring values in memory
-            int i, c;
-            if constexpr (REDUCE) { i = q % ANY_TILE; c = q / ANY_TILE; } else { c = q % ANY_STEP; i = q / ANY_STEP; }
-            T v = (T)0.0f;
-            if (i0 + i < iend && c0 + c < cend) {
-                const int32_t r = REDUCE ? c0 + c : i0 + i;
-                const int32_t src = p.rows ? p.rows[r] : r;
-                if ((uint32_t)src < (uint32_t)p.a_rows) v = a[(int64_t)src * p.lda + (REDUCE ? i0 + i : c0 + c)];
-            }
-            as[i * LD + c] = v;
-            int j, d;
-            if (REDUCE || p.b_j == 1) { j = q % ANY_TILE; d = q / ANY_TILE; } else { d = q % ANY_STEP; j = q / ANY_STEP; }
-            T w = (T)0.0f;
-            if (j0 + j < p.J && c0 + d < cend)
-                w = REDUCE ? b[(int64_t)(c0 + d) * p.ldb + j0 + j] : b[(int64_t)(c0 + d) * p.b_c + (int64_t)(j0 + j) * p.b_j];
-            bs[j * LD + d] = w;
-        }
-        __syncthreads();
-        if constexpr (REDUCE)
-            if (p.out_bias && i0 == 0 && tid < ANY_TILE)
-                for (int c = 0; c < ANY_STEP; ++c) colsum += (float)bs[tid * LD + c];
-#pragma unroll
-        for (int c = 0; c < ANY_STEP; c += 4 * W) {
-            Frag fa[2], fb[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                fa[u] = *(const Frag *)(as + (wi + 16 * u + (lane & 15)) * LD + c + (lane >> 4) * W);
-                fb[u] = *(const Frag *)(bs + (wj + 16 * u + (lane & 15)) * LD + c + (lane >> 4) * W);
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int v = 0; v < 2; ++v) acc[u][v] = kn_mfma(fa[u], fb[v], acc[u][v]);
-        }
-    }
-    T *out = (T *)p.out;
-    const T *bias = (const T *)p.bias, *mask = (const T *)p.mask;
-    if constexpr (REDUCE) {
-        out += (int64_t)group * p.o_group;
-        if (p.out_bias && i0 == 0 && tid < ANY_TILE && j0 + tid < p.J) ((T *)p.out_bias)[(int64_t)group * p.J + j0 + tid] = (T)colsum;
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int v = 0; v < 2; ++v)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int32_t i = i0 + wi + 16 * u + (lane >> 4) * 4 + r, j = j0 + wj + 16 * v + (lane & 15);
-                if (i >= iend || j >= p.J) continue;
-                float y = acc[u][v][r];
-                if constexpr (!REDUCE) {
-                    if (group < p.E) {
-                        if (bias) y += (float)bias[(int64_t)group * p.J + j];
-                        if (p.relu) y = y > 0.0f || y != y ? y : 0.0f; // (a NaN stays one)
-                        if (mask) {
-                            const int32_t src = p.mask_rows ? p.mask_rows[i] : i;
-                            if ((uint32_t)src >= (uint32_t)p.m_rows || !((float)mask[(int64_t)src * p.ldm + j] > 0.0f)) y = 0.0f;
-                        }
-                    }
-                }
-                out[(int64_t)i * p.o_i + (int64_t)j * p.o_j] = (T)y;
-            }
-}
-
-// What is added to columns j .. j + 7 of a network's results (j a multiple of 8)
-template <typename T> __device__ __forceinline__ void bias_of(const KnProduct &p, bool some, int64_t group, int32_t j, float add[8])
+// What is added to columns j .. j + 7 of a network's results (j a multiple of 8).  wide: 8 columns lie in whole 16-byte pieces, of
+// everything that has columns.
+template <typename T> __device__ __forceinline__ void bias_of(const KnProduct &p, bool some, int64_t group, int32_t j, bool wide, float add[8])
 {
     typedef T Piece __attribute__((ext_vector_type(8)));
 #pragma unroll
     for (int q = 0; q < 8; ++q) add[q] = 0.0f;
-    if (p.bias && some && j < p.J) {
-        const Piece v = *(const Piece *)((const T *)p.bias + group * p.J + j);
+    if (!p.bias || !some || j >= p.J) return;
+    const T *bias = (const T *)p.bias + group * p.J;
+    if (wide) {
+        const Piece v = *(const Piece *)(bias + j);
 #pragma unroll
         for (int q = 0; q < 8; ++q) add[q] = (float)v[q];
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) add[q] = (float)bias[min(j + q, p.J - 1)];
     }
 }
 // The end of 8 neighbouring results of row i: zeros for a row that x does not have, bias, ReLU, the mask of a ReLU before; one rounding
-template <typename T> __device__ __forceinline__ void finish(const KnProduct &p, bool some, int64_t group, int32_t i, int32_t j, const float add[8], float y[8])
+template <typename T>
+__device__ __forceinline__ void finish(const KnProduct &p, bool some, int32_t i, int32_t j, bool wide, const float add[8], float y[8])
 {
     typedef T Piece __attribute__((ext_vector_type(8)));
     if (p.rows && (uint32_t)p.rows[i] >= (uint32_t)p.a_rows) {
@@ -138,28 +38,40 @@ template <typename T> __device__ __forceinline__ void finish(const KnProduct &p,
     }
     if (p.mask && some) {
         const int32_t src = p.mask_rows ? p.mask_rows[i] : i;
-        const bool there = (uint32_t)src < (uint32_t)p.m_rows;
-        const Piece m = *(const Piece *)((const T *)p.mask + (int64_t)(there ? src : 0) * p.ldm + j);
+        Piece m = {};
+        if ((uint32_t)src < (uint32_t)p.m_rows) {
+            const T *row = (const T *)p.mask + (int64_t)src * p.ldm;
+            if (wide) m = *(const Piece *)(row + j);
+            else
+#pragma unroll
+                for (int q = 0; q < 8; ++q) m[q] = row[min(j + q, p.J - 1)];
+        }
 #pragma unroll
         for (int q = 0; q < 8; ++q)
-            if (!there || !((float)m[q] > 0.0f)) y[q] = 0.0f;
+            if (!((float)m[q] > 0.0f)) y[q] = 0.0f;
     }
+    T *out = (T *)p.out + (int64_t)i * p.o_i + j;
     Piece o;
 #pragma unroll
     for (int q = 0; q < 8; ++q) o[q] = (T)y[q];
-    *(Piece *)((T *)p.out + (int64_t)i * p.o_i + j) = o;
+    if (wide) *(Piece *)out = o;
+    else
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (j + q < p.J) out[q] = o[q];
 }
 
-// Rows of 16-byte pieces throughout: tiles of BM x BN results, WR x WC wavefronts, two stages in the LDS, of which one is
-// fetched while the other is multiplied.  COLS: b's columns are contiguous in memory (else its contraction is).
+// Tiles of BM x BN results, WR x WC wavefronts, NB stages in the LDS, of which one is multiplied while the others are fetched.  COLS:
+// b's columns are contiguous in memory (else its contraction is).  DIRECT: rows of whole 16-byte pieces throughout (KnRowLoader).
 // Fragments of b are the products' first operand, so that a lane holds four neighbouring results of a row; they go through
 // the LDS once more to leave in pieces of 8.
-template <typename T, bool COLS, int BM, int BN, int WR, int WC, int NB>
+template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB>
 __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int32_t blocks)
 {
     constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16, CS = 128 / sizeof(T);
     typedef typename KnFrag<T>::Type Frag;
-    typedef KnRowLoader<T, BM, NW> LoadA;
+    static_assert(DIRECT || NB == 2, "");
+    typedef KnRowLoader<T, BM, NW, DIRECT> LoadA;
     constexpr int BYTES = NB * STAGE > NW * 16 * (BN / WC + 4) * 4 ? NB * STAGE : NW * 16 * (BN / WC + 4) * 4;
     __shared__ __align__(16) char lds_[BYTES];
     KN_LDS char *lds = (KN_LDS char *)lds_;
@@ -178,17 +90,18 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
         const int32_t src = p.rows ? p.rows[i] : i;
         return a + (int64_t)((uint32_t)src < (uint32_t)p.a_rows ? src : 0) * p.lda;
     });
-    KnRowLoader<T, BN, NW> lbr;
-    KnColLoader<T, BN, NW> lbc;
-    if constexpr (COLS) lbc.start(wave, lane, b + j0, p.b_c, (p.J - j0) * (int)sizeof(T) / 16);
+    KnRowLoader<T, BN, NW, DIRECT> lbr;
+    KnColLoader<T, BN, NW, DIRECT> lbc;
+    if constexpr (COLS) lbc.start(wave, lane, b + j0, p.b_c, p.J - j0);
     else lbr.start(wave, lane, [&](int r) { return b + (int64_t)min(j0 + r, p.J - 1) * p.b_j; });
-    const int32_t C = some ? p.C : 0, steps = (C + CS - 1) / CS;
+    const int32_t C = some && p.a_rows > 0 ? p.C : 0, steps = (C + CS - 1) / CS;
     constexpr int LOADS = LoadA::N + (COLS ? lbc.N : lbr.N); // a wavefront's, per stage
+    constexpr int LATER = DIRECT ? (NB - 2) * LOADS : 63; // (loads into registers are waited for where they are put down)
     auto fetch = [&](int s, int at) {
         KN_LDS char *tile = lds + at * STAGE;
-        la.fetch(tile, wave, C - s * CS);
+        la.fetch(tile, wave, lane, C - s * CS);
         if constexpr (COLS) lbc.fetch(tile + BM * 128, wave, lane, C - s * CS);
-        else lbr.fetch(tile + BM * 128, wave, C - s * CS);
+        else lbr.fetch(tile + BM * 128, wave, lane, C - s * CS);
     };
     const int wi = (wave / WC) * (BM / WR), wj = (wave % WC) * (BN / WC);
     kn_f32x4 acc[U][V] = {};
@@ -212,8 +125,11 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
     // Half a stage's fragments are read while the other half's are multiplied; in between, the next stage has to have arrived, and the
     // one behind the NB that lie in the LDS takes the place of the one that everybody has just read.
     if (steps > 0) {
+        la.ask_first(C);
+        if constexpr (COLS) lbc.ask_first(wave, lane, C);
+        else lbr.ask_first(C);
         for (int s = 0; s < NB && s < steps; ++s) fetch(s, s);
-        if (steps >= NB) kn_stage_barrier<(NB - 1) * LOADS>();
+        if (DIRECT && steps >= NB) kn_stage_barrier<(NB - 1) * LOADS>();
         else kn_stage_barrier<0>();
         read(0, 0);
         for (int s = 0, at = 0; s < steps; ++s) {
@@ -221,7 +137,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
             read(at, 1);
             multiply(0);
             kn_interleave<U, V, T, COLS>();
-            if (s + NB <= steps) kn_stage_barrier<(NB - 2) * LOADS>();
+            if (s + NB <= steps) kn_stage_barrier<LATER>();
             else kn_stage_barrier<0>();
             if (s + NB < steps) fetch(s + NB, at);
             read(next, 0); // (behind the last stage: what happens to lie there, unused)
@@ -237,8 +153,9 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
     static_assert(64 % LR == 0, "");
     const int cj = lane % LR * 8;
     const int32_t j = j0 + wj + cj;
+    const bool wide = DIRECT || p.wide;
     float add[8];
-    bias_of<T>(p, some, group, j, add);
+    bias_of<T>(p, some, group, j, wide, add);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -250,7 +167,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
             if (r >= 16 || i >= piece.end || j >= p.J) continue;
             const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj + 4);
             float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            finish<T>(p, some, group, i, j, add, y);
+            finish<T>(p, some, i, j, wide, add, y);
         }
     }
 }
@@ -333,8 +250,8 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p, int
 #pragma unroll
             for (int n = 0; n < 4; ++n) { y[n] += lo[n]; y[n + 4] += hi[n]; }
         }
-        bias_of<T>(p, some, group, j, add);
-        finish<T>(p, some, group, i, j, add, y);
+        bias_of<T>(p, some, group, j, true, add);
+        finish<T>(p, some, i, j, true, add, y);
     }
 }
 
@@ -346,24 +263,7 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p, int
 constexpr int SMALL_ROWS = 64, SMALL_WAVES = 4;
 template <typename T> struct SmallFrag {
     static constexpr int W = 16 / sizeof(T), KS = 4 * W;
-    typedef T Any __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T)))); // a piece wherever it lies
 };
-// values k .. k + W - 1 of a row of C (zeros behind its end; k is a multiple of W)
-template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type small_row(const T *row, int32_t k, int32_t C)
-{
-    constexpr int W = SmallFrag<T>::W;
-    typename KnFrag<T>::Type f;
-    if (k + W <= C) {
-        f = *(const typename SmallFrag<T>::Any *)(row + k);
-    } else {
-#pragma unroll
-        for (int q = 0; q < W; ++q) {
-            const T v = row[min(k + q, C - 1)];
-            f[q] = k + q < C ? v : (T)0.0f;
-        }
-    }
-    return f;
-}
 template <typename T, bool COLS, int KF, int V>
 __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p, int32_t pieces)
 {
@@ -382,7 +282,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
     const int32_t C = p.C;
     Frag fa[SUBS][KF], fb[KF][V];
     bool there[SUBS];
-    if (some) {
+    if (some && p.a_rows > 0) {
         const T *arow[SUBS];
 #pragma unroll
         for (int s = 0; s < SUBS; ++s) {
@@ -403,13 +303,13 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
                         fb[k][v][q] = c + q < C ? w : (T)0.0f;
                     }
                 } else {
-                    fb[k][v] = small_row<T>(b + (int64_t)j * p.b_j, c, C);
+                    fb[k][v] = kn_any_piece<T>(b + (int64_t)j * p.b_j, c, C);
                 }
             }
 #pragma unroll
         for (int s = 0; s < SUBS; ++s)
 #pragma unroll
-            for (int k = 0; k < KF; ++k) fa[s][k] = small_row<T>(arow[s], k * KS + g * W, C);
+            for (int k = 0; k < KF; ++k) fa[s][k] = kn_any_piece<T>(arow[s], k * KS + g * W, C);
     }
     const T *bias = (const T *)p.bias, *mask = (const T *)p.mask;
     const bool fours = p.J % 4 == 0 && (((uintptr_t)p.out | (uintptr_t)bias | (uintptr_t)mask) & (4 * sizeof(T) - 1)) == 0 && (!mask || p.ldm % 4 == 0);
@@ -419,7 +319,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
         if (piece.begin + 16 * s >= piece.end) break;
         kn_f32x4 acc[V] = {};
         const T *mrow = nullptr;
-        if (some) {
+        if (some && p.a_rows > 0) {
 #pragma unroll
             for (int k = 0; k < KF; ++k)
 #pragma unroll
@@ -427,10 +327,10 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
             if (!there[s])
 #pragma unroll
                 for (int v = 0; v < V; ++v) acc[v] = kn_f32x4{0, 0, 0, 0};
-            if (mask) {
-                const int32_t m = min(i, piece.end - 1), src = p.mask_rows ? p.mask_rows[m] : m;
-                mrow = (uint32_t)src < (uint32_t)p.m_rows ? mask + (int64_t)src * p.ldm : nullptr;
-            }
+        }
+        if (some && mask) {
+            const int32_t m = min(i, piece.end - 1), src = p.mask_rows ? p.mask_rows[m] : m;
+            mrow = (uint32_t)src < (uint32_t)p.m_rows ? mask + (int64_t)src * p.ldm : nullptr;
         }
         if (i >= piece.end) continue;
         T *out = (T *)p.out + (int64_t)i * p.o_i;
@@ -468,29 +368,23 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
     }
 }
 
-// Whether every row is made of whole 16-byte pieces that lie on multiples of 16 bytes, as k_product_rows takes them
+// Whether 8 columns lie in whole 16-byte pieces on multiples of 16 bytes, of everything that has columns
+template <typename T> bool wide_columns(const KnProduct &p)
+{
+    return p.J % 8 == 0 && ((uintptr_t)p.bias | (uintptr_t)p.mask | (uintptr_t)p.out) % 16 == 0 && (!p.mask || p.ldm * sizeof(T) % 16 == 0);
+}
+// Whether every row is made of such pieces, as the DIRECT kernels take them
 template <typename T> bool rows_of_pieces(const KnProduct &p)
 {
     constexpr int64_t V = 16 / sizeof(T);
-    const uintptr_t at = (uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)p.bias | (uintptr_t)p.mask | (uintptr_t)p.out;
-    return (at & 15) == 0 && p.C % V == 0 && p.J % 8 == 0 && p.lda % V == 0 && (!p.mask || p.ldm % V == 0) && p.a_rows > 0 && (!p.mask || p.m_rows > 0);
+    return wide_columns<T>(p) && ((uintptr_t)p.a | (uintptr_t)p.b) % 16 == 0 && p.C % V == 0 && p.lda % V == 0 && p.a_rows > 0;
 }
 
-template <typename T, bool COLS, int BM, int BN, int WR, int WC, int NB> int launch_rows(hipStream_t st, const KnProduct &p)
+template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB> int launch_rows(hipStream_t st, const KnProduct &p)
 {
     const int64_t blocks = kn_pieces(p.M, p.E, BM) * kn_div_up(p.J, BN);
     if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_product_rows<T, COLS, BM, BN, WR, WC, NB>), dim3((unsigned)blocks), dim3(WR * WC * 64), 0, st, p, (int32_t)blocks);
-    KN_CHECK_LAUNCH();
-    return KN_OK;
-}
-
-template <typename T, bool REDUCE> int launch_any(hipStream_t st, const KnProduct &p)
-{
-    const int64_t groups = REDUCE ? (int64_t)p.E * kn_div_up(p.I, ANY_TILE) : kn_pieces(p.M, p.E, ANY_TILE);
-    const int64_t blocks = groups * kn_div_up(p.J, ANY_TILE);
-    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_product_any<T, REDUCE>), dim3((unsigned)blocks), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((k_product_rows<T, COLS, DIRECT, BM, BN, WR, WC, NB>), dim3((unsigned)blocks), dim3(WR * WC * 64), 0, st, p, (int32_t)blocks);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }
@@ -508,13 +402,14 @@ template <typename T> int launch_few(hipStream_t st, const KnProduct &p)
 template <typename T, bool COLS> int launch_pieces(hipStream_t st, const KnProduct &p)
 {
     const int64_t each = p.M / p.E;
-    if (each >= 384) return launch_rows<T, COLS, 192, 128, 2, 2, 2>(st, p);
-    if (each >= 64) return launch_rows<T, COLS, 128, 128, 2, 4, 2>(st, p);
+    if (!rows_of_pieces<T>(p)) return each >= 64 ? launch_rows<T, COLS, false, 128, 128, 2, 4, 2>(st, p) : launch_rows<T, COLS, false, 32, 128, 1, 4, 2>(st, p);
+    if (each >= 384) return launch_rows<T, COLS, true, 192, 128, 2, 2, 2>(st, p);
+    if (each >= 64) return launch_rows<T, COLS, true, 128, 128, 2, 4, 2>(st, p);
     if constexpr (COLS) {
         if (p.M <= 32 || p.M < p.E) return launch_few<T>(st, p);
-        return launch_rows<T, COLS, 64, 256 / (sizeof(T) / 2), 1, 8 / (sizeof(T) / 2), 2>(st, p);
+        return launch_rows<T, COLS, true, 64, 256 / (sizeof(T) / 2), 1, 8 / (sizeof(T) / 2), 2>(st, p);
     } else {
-        return launch_rows<T, COLS, 32, 64, 1, 4, 4>(st, p);
+        return launch_rows<T, COLS, true, 32, 64, 1, 4, 4>(st, p);
     }
 }
 
@@ -541,158 +436,12 @@ template <typename T, bool COLS> int launch_small_widths(hipStream_t st, const K
     }
 }
 
-template <typename T> int launch_forward(hipStream_t st, const KnProduct &p)
+template <typename T> int launch_forward(hipStream_t st, KnProduct p)
 {
-    if (p.C <= SMALL_MOST && p.J <= SMALL_MOST) return p.b_j == 1 ? launch_small_widths<T, true>(st, p) : launch_small_widths<T, false>(st, p);
-    if (!rows_of_pieces<T>(p)) return launch_any<T, false>(st, p);
-    return p.b_j == 1 ? launch_pieces<T, true>(st, p) : launch_pieces<T, false>(st, p);
-}
-
-// The weight gradient on tiles: both operands column-wise, the contraction is the network's rows, 128 bytes' worth a stage.  GATHER: 1,
-// 2: a's, b's rows are read through the index.  The columns' sums (gradient of the biases) are products with ones of the
-// fragments that are there anyway, in the workgroups of the first tile: SUM_B the columns of b, SUM_A those of a.
-enum { SUM_NONE, SUM_A, SUM_B };
-template <typename T, int GATHER, int BM, int BN, int WR, int WC>
-__global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, int32_t sum)
-{
-    constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16, CS = 128 / sizeof(T);
-    typedef typename KnFrag<T>::Type Frag;
-    __shared__ __align__(16) char lds_[2 * STAGE];
-    KN_LDS char *lds = (KN_LDS char *)lds_;
-    const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int jtiles = (p.J + BN - 1) / BN, itiles = (p.I + BM - 1) / BM;
-    // (a network's tiles go to all XCDs, neighbours among them to one: networks differ in rows, XCDs should not)
-    const int32_t tiles = itiles * jtiles, turn = kn_block() / tiles, number = kn_xcd_order(kn_block() % tiles, tiles);
-    const int32_t group = p.E <= KN_WAVE ? kn_longest(p.offsets, p.E, p.M, turn) : turn;
-    const int j0 = number % jtiles * BN, i0 = number / jtiles * BM;
-    const int32_t c0 = kn_offset(p.offsets, group, p.M), cend = max(c0, kn_offset(p.offsets, group + 1, p.M));
-    const int32_t steps = (cend - c0 + CS - 1) / CS;
-    const bool sum_a = sum == SUM_A && j0 == 0, sum_b = sum == SUM_B && i0 == 0;
-    KnGroupLoader<T, BM, NW, GATHER == 1> la;
-    KnGroupLoader<T, BN, NW, GATHER == 2> lb;
-    const int wi = (wave / WC) * (BM / WR), wj = (wave % WC) * (BN / WC);
-    kn_f32x4 acc[U][V] = {}, side[U > V ? U : V] = {};
-    Frag ones;
-#pragma unroll
-    for (int q = 0; q < (int)(sizeof(Frag) / sizeof(T)); ++q) ones[q] = (T)1.0f;
-    Frag fa[2][U], fb[2][V];
-    auto fetch = [&](int s) {
-        KN_LDS char *tile = lds + (s & 1) * STAGE;
-        la.fetch(tile, wave, lane, c0 + s * CS);
-        lb.fetch(tile + BM * 128, wave, lane, c0 + s * CS);
-    };
-    auto read = [&](int s, int kk) {
-        const KN_LDS char *ta = lds + (s & 1) * STAGE, *tb = ta + BM * 128;
-#pragma unroll
-        for (int u = 0; u < U; ++u) fa[kk][u] = kn_col_frag<T, BM>(ta, wi + 16 * u, kk, lane);
-#pragma unroll
-        for (int v = 0; v < V; ++v) fb[kk][v] = kn_col_frag<T, BN>(tb, wj + 16 * v, kk, lane);
-    };
-    auto multiply = [&](int kk) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[kk][v], fa[kk][u], acc[u][v]);
-    };
-    auto add_up = [&](int kk) {
-        if (sum_a && wj == 0) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) side[u] = kn_mfma(ones, fa[kk][u], side[u]);
-        }
-        if (sum_b && wi == 0) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) side[v] = kn_mfma(fb[kk][v], ones, side[v]);
-        }
-    };
-    if (steps > 0) {
-        la.start(wave, lane, (const T *)p.a + i0, p.lda, (p.I - i0) * (int)sizeof(T) / 16, p.rows, p.a_rows, c0, cend);
-        lb.start(wave, lane, (const T *)p.b + j0, p.ldb, (p.J - j0) * (int)sizeof(T) / 16, p.rows, p.b_rows, c0, cend);
-        fetch(0);
-        kn_stage_barrier();
-        if (steps > 1) fetch(1);
-        read(0, 0);
-        for (int s = 0; s < steps; ++s) {
-            add_up(0);
-            read(s, 1);
-            multiply(0);
-            kn_interleave<U, V, T, true, true>();
-            kn_stage_barrier();
-            if (s + 2 < steps) fetch(s + 2);
-            add_up(1);
-            read(s + 1, 0); // (behind the last stage: what happens to lie there, unused)
-            multiply(1);
-            kn_interleave<U, V, T, true, true>();
-        }
-    }
-    kn_stage_barrier(); // (the tiles' LDS is used again)
-    if (sum_a && wj == 0 && lane < 16) { // (each column of the product is alike: its 16 rows are the sums of 16 columns of a)
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (i0 + wi + 16 * u + lane < p.I) ((T *)p.out_bias)[(int64_t)group * p.I + i0 + wi + 16 * u + lane] = (T)side[u][0];
-    }
-    if (sum_b && wi == 0 && (lane & 15) == 0) {
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int j = j0 + wj + 16 * v + (lane >> 4) * 4 + r;
-                if (j < p.J) ((T *)p.out_bias)[(int64_t)group * p.J + j] = (T)side[v][r];
-            }
-    }
-    constexpr int WN = BN / WC, LD = WN + 4, LR = WN / 8;
-    KN_LDS float *mine = (KN_LDS float *)(lds + wave * (16 * LD * 4));
-    typedef T Out __attribute__((ext_vector_type(8)));
-    T *out = (T *)p.out + (int64_t)group * p.o_group;
-    const int32_t j = j0 + wj + lane % LR * 8;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) *(KN_LDS kn_f32x4 *)(mine + (lane & 15) * LD + 16 * v + (lane >> 4) * 4) = acc[u][v];
-#pragma unroll
-        for (int h = 0; h < 16 * LR / 64; ++h) {
-            const int r = h * (64 / LR) + lane / LR;
-            const int32_t i = i0 + wi + 16 * u + r;
-            const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + lane % LR * 8), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + lane % LR * 8 + 4);
-            if (i >= p.I || j >= p.J) continue;
-            const Out o = {(T)lo[0], (T)lo[1], (T)lo[2], (T)lo[3], (T)hi[0], (T)hi[1], (T)hi[2], (T)hi[3]};
-            *(Out *)(out + (int64_t)i * p.o_i + j) = o;
-        }
-    }
-}
-
-template <typename T, int GATHER> int launch_reduce(hipStream_t st, const KnProduct &p, int32_t sum)
-{
-    const int64_t blocks = (int64_t)p.E * kn_div_up(p.I, 128) * kn_div_up(p.J, 128);
-    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_product_reduce<T, GATHER, 128, 128, 2, 4>), dim3((unsigned)blocks), dim3(512), 0, st, p, sum);
-    KN_CHECK_LAUNCH();
-    return KN_OK;
-}
-
-// q: the product with out's contiguous index as columns
-template <typename T> int launch_dw(hipStream_t st, const KnProduct &p)
-{
-    constexpr int64_t V = 16 / sizeof(T);
-    const uintptr_t at = (uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)p.out;
-    const bool pieces = (at & 15) == 0 && p.I % 8 == 0 && p.J % 8 == 0 && p.lda % V == 0 && p.ldb % V == 0;
-    if (!pieces) return launch_any<T, true>(st, p);
-    KnProduct q = p;
-    q.b_rows = p.M;
-    if (p.o_j == 1) return p.rows ? launch_reduce<T, 1>(st, q, p.out_bias ? SUM_B : SUM_NONE) : launch_reduce<T, 0>(st, q, p.out_bias ? SUM_B : SUM_NONE);
-    q.a = p.b; q.b = p.a; q.lda = p.ldb; q.ldb = p.lda; q.a_rows = p.M; q.b_rows = p.a_rows;
-    q.I = p.J; q.J = p.I; q.o_i = p.o_j; q.o_j = p.o_i;
-    return p.rows ? launch_reduce<T, 2>(st, q, p.out_bias ? SUM_A : SUM_NONE) : launch_reduce<T, 0>(st, q, p.out_bias ? SUM_A : SUM_NONE);
-}
-
-// What the three calls check alike
-int check(const kn_linear_desc *d)
-{
-    if (!d || d->rows < 0 || d->x_rows < 0 || d->experts < 1 || d->n_in < 1 || d->n_out < 1 || !kn_dtype_ok(d->dtype) ||
-        (d->w_layout != KN_W_IN_OUT && d->w_layout != KN_W_OUT_IN) || d->ldx < d->n_in)
-        return KN_E_INVALID_ARG;
-    if (d->rows > KN_MAX_ROWS || d->x_rows > KN_MAX_ROWS || d->experts > KN_MAX_EXPERTS || d->n_in > KN_MAX_WIDTH || d->n_out > KN_MAX_WIDTH)
-        return KN_E_UNSUPPORTED;
-    return KN_OK;
+    p.wide = wide_columns<T>(p);
+    const bool cols = p.b_j == 1 && p.b_c != 1; // (one column of one input: either)
+    if (p.C <= SMALL_MOST && p.J <= SMALL_MOST) return cols ? launch_small_widths<T, true>(st, p) : launch_small_widths<T, false>(st, p);
+    return cols ? launch_pieces<T, true>(st, p) : launch_pieces<T, false>(st, p);
 }
 
 } // namespace
@@ -700,7 +449,7 @@ int check(const kn_linear_desc *d)
 extern "C" int kn_grouped_linear(void *stream, const kn_linear_desc *d, const void *x, const void *w, const void *bias,
                                  const int32_t *offsets, const int32_t *rows, int32_t relu, void *y)
 {
-    KN_TRY(check(d));
+    KN_TRY(kn_linear_check(d));
     if (d->rows == 0) return KN_OK;
     if (!w || !offsets || !y || (d->x_rows > 0 && !x) || (!rows && d->x_rows < d->rows)) return KN_E_INVALID_ARG;
     KnProduct p = {};
@@ -717,7 +466,7 @@ extern "C" int kn_grouped_linear(void *stream, const kn_linear_desc *d, const vo
 extern "C" int kn_grouped_linear_dx(void *stream, const kn_linear_desc *d, const void *dy, const void *w, const void *x_relu,
                                     const int32_t *offsets, const int32_t *rows, void *dx)
 {
-    KN_TRY(check(d));
+    KN_TRY(kn_linear_check(d));
     if (d->rows == 0) return KN_OK;
     if (!dy || !w || !offsets || !dx || (x_relu && !rows && d->x_rows < d->rows)) return KN_E_INVALID_ARG;
     KnProduct p = {};
@@ -732,17 +481,3 @@ extern "C" int kn_grouped_linear_dx(void *stream, const kn_linear_desc *d, const
     return kn_with_type(d->dtype, [&](auto v) { return launch_forward<decltype(v)>((hipStream_t)stream, p); });
 }
 
-extern "C" int kn_grouped_linear_dw(void *stream, const kn_linear_desc *d, const void *x, const void *dy, const int32_t *offsets,
-                                    const int32_t *rows, void *dw, void *db)
-{
-    KN_TRY(check(d));
-    if (!offsets || !dw || (d->rows > 0 && (!dy || (d->x_rows > 0 && !x))) || (d->rows > 0 && !rows && d->x_rows < d->rows)) return KN_E_INVALID_ARG;
-    KnProduct p = {};
-    const bool io = d->w_layout == KN_W_IN_OUT;
-    p.a = x; p.b = dy; p.out = dw; p.out_bias = db; p.offsets = offsets; p.rows = rows;
-    p.lda = d->ldx; p.ldb = d->n_out;
-    p.o_group = (int64_t)d->n_in * d->n_out; p.o_i = io ? d->n_out : 1; p.o_j = io ? 1 : d->n_in;
-    p.M = (int32_t)d->rows; p.E = d->experts; p.I = d->n_in; p.J = d->n_out;
-    p.a_rows = (int32_t)d->x_rows;
-    return kn_with_type(d->dtype, [&](auto v) { return launch_dw<decltype(v)>((hipStream_t)stream, p); });
-}

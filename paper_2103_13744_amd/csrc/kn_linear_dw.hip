@@ -1,0 +1,250 @@
+// Gradients of the weights and biases of a layer of all networks: kn_grouped_linear_dw.
+#include "kn_tile.h"
+
+namespace {
+
+// A network's rows are cut into parts of at most `len`: a network of one part has its sums written at once, of several, each
+// part's go to the workspace in fp32 and k_reduce_join adds them in order, so that the result does not depend on who was first.  Part c
+// of a network whose rows begin at o has place 2 (o / len) + c: a network of several parts has more than len rows, so these
+// places do not meet, and there are at most 2 (M / len) + 2.
+struct Parts {
+    int32_t len;
+    float *sums, *bias_sums; // (places, I, J) and (places, columns of dy)
+};
+__host__ __device__ inline int64_t part_places(int64_t M, int64_t len) { return 2 * (M / len) + 2; }
+
+// Tiles of BM x BN of a network's out(i, j) = sum over rows r of a(r, i) b(r, j): both operands column-wise, the contraction is the
+// rows, 128 bytes' worth a stage.  The columns' sums (gradient of the biases) are products with ones of the fragments that are
+// there anyway, in the workgroups of the first tile: SUM_B the columns of b, SUM_A those of a.
+enum { SUM_NONE, SUM_A, SUM_B };
+template <typename T, bool DIRECT, int BM, int BN, int WR, int WC>
+__global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, int32_t sum, Parts parts)
+{
+    constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16, CS = 128 / sizeof(T);
+    typedef typename KnFrag<T>::Type Frag;
+    __shared__ __align__(16) char lds_[2 * STAGE];
+    KN_LDS char *lds = (KN_LDS char *)lds_;
+    const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int jtiles = (p.J + BN - 1) / BN, itiles = (p.I + BM - 1) / BM;
+    // (a part's tiles go to all XCDs, neighbours among them to one: networks differ in rows, XCDs should not)
+    const int32_t tiles = itiles * jtiles, number = kn_xcd_order(kn_block() % tiles, tiles);
+    const int32_t part = kn_block() / tiles;
+    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, parts.len, part);
+    const int32_t group = piece.group;
+    if (group >= p.E) return;
+    const int32_t o = kn_offset(p.offsets, group, p.M), c0 = piece.begin, cend = max(c0, min(piece.end, c0 + parts.len));
+    if (c0 >= cend && c0 != o) return; // (the first part of a network without rows writes zeros)
+    const bool several = piece.end - o > parts.len;
+    const int64_t place = 2 * (o / parts.len) + (c0 - o) / parts.len;
+    const int j0 = number % jtiles * BN, i0 = number / jtiles * BM;
+    const int32_t steps = (cend - c0 + CS - 1) / CS;
+    const bool sum_a = sum == SUM_A && j0 == 0, sum_b = sum == SUM_B && i0 == 0;
+    KnGroupLoader<T, BM, NW, DIRECT> la;
+    KnGroupLoader<T, BN, NW, DIRECT> lb;
+    const int wi = (wave / WC) * (BM / WR), wj = (wave % WC) * (BN / WC);
+    kn_f32x4 acc[U][V] = {}, side[U > V ? U : V] = {};
+    Frag ones;
+#pragma unroll
+    for (int q = 0; q < (int)(sizeof(Frag) / sizeof(T)); ++q) ones[q] = (T)1.0f;
+    Frag fa[2][U], fb[2][V];
+    auto fetch = [&](int s) {
+        KN_LDS char *tile = lds + (s & 1) * STAGE;
+        la.fetch(tile, wave, lane, c0 + s * CS);
+        lb.fetch(tile + BM * 128, wave, lane, c0 + s * CS);
+    };
+    auto read = [&](int s, int kk) {
+        const KN_LDS char *ta = lds + (s & 1) * STAGE, *tb = ta + BM * 128;
+#pragma unroll
+        for (int u = 0; u < U; ++u) fa[kk][u] = kn_col_frag<T, BM>(ta, wi + 16 * u, kk, lane);
+#pragma unroll
+        for (int v = 0; v < V; ++v) fb[kk][v] = kn_col_frag<T, BN>(tb, wj + 16 * v, kk, lane);
+    };
+    auto multiply = [&](int kk) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[kk][v], fa[kk][u], acc[u][v]);
+    };
+    auto add_up = [&](int kk) {
+        if (sum_a && wj == 0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) side[u] = kn_mfma(ones, fa[kk][u], side[u]);
+        }
+        if (sum_b && wi == 0) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) side[v] = kn_mfma(fb[kk][v], ones, side[v]);
+        }
+    };
+    if (steps > 0) {
+        la.start(wave, lane, (const T *)p.a + i0, p.lda, p.I - i0, p.rows, p.a_rows, c0, cend);
+        lb.start(wave, lane, (const T *)p.b + j0, p.ldb, p.J - j0, p.b_index, p.b_rows, c0, cend);
+        fetch(0);
+        if (!DIRECT && steps > 1) fetch(1);
+        kn_stage_barrier();
+        if (DIRECT && steps > 1) fetch(1);
+        read(0, 0);
+        for (int s = 0; s < steps; ++s) {
+            add_up(0);
+            read(s, 1);
+            multiply(0);
+            kn_interleave<U, V, T, true, true>();
+            kn_stage_barrier<DIRECT ? 0 : 63>(); // (loads into registers are waited for where they are put down)
+            if (s + 2 < steps) fetch(s + 2);
+            add_up(1);
+            read(s + 1, 0); // (behind the last stage: what happens to lie there, unused)
+            multiply(1);
+            kn_interleave<U, V, T, true, true>();
+        }
+    }
+    kn_stage_barrier(); // (the tiles' LDS is used again)
+    auto put_bias = [&](int j, int n, float v) {
+        if (j >= n) return;
+        if (several) parts.bias_sums[place * n + j] = v;
+        else ((T *)p.out_bias)[(int64_t)group * n + j] = (T)v;
+    };
+    if (sum_a && wj == 0 && lane < 16) { // (each column of the product is alike: its 16 rows are the sums of 16 columns of a)
+#pragma unroll
+        for (int u = 0; u < U; ++u) put_bias(i0 + wi + 16 * u + lane, p.I, side[u][0]);
+    }
+    if (sum_b && wi == 0 && (lane & 15) == 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) put_bias(j0 + wj + 16 * v + (lane >> 4) * 4 + r, p.J, side[v][r]);
+    }
+    constexpr int WN = BN / WC, LD = WN + 4, LR = WN / 8;
+    static_assert(64 % LR == 0, "");
+    KN_LDS float *mine = (KN_LDS float *)(lds + wave * (16 * LD * 4));
+    typedef T Out __attribute__((ext_vector_type(8)));
+    const bool wide = DIRECT || p.wide;
+    const int cj = lane % LR * 8;
+    const int32_t j = j0 + wj + cj;
+    float *sums = parts.sums + place * p.I * p.J;
+    T *out = (T *)p.out + (int64_t)group * p.o_group;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) *(KN_LDS kn_f32x4 *)(mine + (lane & 15) * LD + 16 * v + (lane >> 4) * 4) = acc[u][v];
+#pragma unroll
+        for (int h = 0; h < (16 * LR + 63) / 64; ++h) {
+            const int r = h * (64 / LR) + lane / LR;
+            const int32_t i = i0 + wi + 16 * u + r;
+            if (r >= 16 || i >= p.I || j >= p.J) continue;
+            const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj + 4);
+            const float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if (several) {
+                float *at = sums + (int64_t)i * p.J + j;
+                if (wide) {
+                    *(kn_f32x4 *)at = lo;
+                    *(kn_f32x4 *)(at + 4) = hi;
+                } else
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (j + q < p.J) at[q] = y[q];
+            } else {
+                T *at = out + (int64_t)i * p.o_i + j;
+                Out v;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[q] = (T)y[q];
+                if (wide) *(Out *)at = v;
+                else
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (j + q < p.J) at[q] = v[q];
+            }
+        }
+    }
+}
+
+// The parts' sums of the networks that have several, in the order of the parts; JOIN results per workgroup.
+constexpr int JOIN = 4096;
+template <typename T> __global__ void __launch_bounds__(256) k_reduce_join(KnProduct p, int32_t sum, Parts parts)
+{
+    const int64_t n = (int64_t)p.I * p.J;
+    const int32_t pieces = (int32_t)((n + JOIN - 1) / JOIN), group = kn_block() / pieces;
+    const int32_t o = kn_offset(p.offsets, group, p.M), rows = kn_offset(p.offsets, group + 1, p.M) - o;
+    if (rows <= parts.len) return;
+    const int32_t count = (rows + parts.len - 1) / parts.len;
+    const int64_t place = 2 * (o / parts.len), first = (int64_t)(kn_block() % pieces) * JOIN;
+    T *out = (T *)p.out + (int64_t)group * p.o_group;
+    for (int64_t q = first + kn_thread(); q < min(n, first + JOIN); q += 256) {
+        float y = 0.0f;
+        for (int c = 0; c < count; ++c) y += parts.sums[(place + c) * n + q];
+        out[q / p.J * p.o_i + q % p.J] = (T)y;
+    }
+    if (sum == SUM_NONE || first > 0) return;
+    const int32_t m = sum == SUM_A ? p.I : p.J;
+    for (int32_t j = kn_thread(); j < m; j += 256) {
+        float y = 0.0f;
+        for (int c = 0; c < count; ++c) y += parts.bias_sums[(place + c) * m + j];
+        ((T *)p.out_bias)[(int64_t)group * m + j] = (T)y;
+    }
+}
+
+// Tiles of 64 x 64 for layers no wider than that (four times as many workgroups at a time: such a tile's few rows are latency), of
+// 128 x 128 else.
+bool narrow(const kn_linear_desc *d) { return d->n_in <= 64 && d->n_out <= 64; }
+
+// Rows of a part: enough parts for the chip, none shorter than 512 rows.
+int32_t part_length(const kn_linear_desc *d)
+{
+    const int64_t tile = narrow(d) ? 64 : 128, tiles = kn_div_up(d->n_in, tile) * kn_div_up(d->n_out, tile);
+    const int64_t len = kn_div_up(d->rows, kn_div_up(1024, tiles));
+    return (int32_t)kn_align_up(len < 512 ? 512 : len, 64);
+}
+
+template <typename T, bool DIRECT> int launch_reduce(hipStream_t st, const kn_linear_desc *d, const KnProduct &p, int32_t sum, const Parts &parts)
+{
+    const int tile = narrow(d) ? 64 : 128;
+    const int64_t blocks = kn_pieces(p.M, p.E, parts.len) * kn_div_up(p.I, tile) * kn_div_up(p.J, tile);
+    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
+    if (narrow(d)) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 64, 64, 2, 2>), dim3((unsigned)blocks), dim3(256), 0, st, p, sum, parts);
+    else hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 128, 128, 2, 4>), dim3((unsigned)blocks), dim3(512), 0, st, p, sum, parts);
+    KN_CHECK_LAUNCH();
+    if (p.M <= parts.len) return KN_OK; // (no network has several)
+    const int64_t joins = (int64_t)p.E * kn_div_up((int64_t)p.I * p.J, JOIN);
+    if (joins > 0x7fffffffLL) return KN_E_UNSUPPORTED;
+    hipLaunchKernelGGL((k_reduce_join<T>), dim3((unsigned)joins), dim3(256), 0, st, p, sum, parts);
+    KN_CHECK_LAUNCH();
+    return KN_OK;
+}
+
+} // namespace
+
+extern "C" int kn_grouped_linear_dw_workspace_bytes(const kn_linear_desc *d, int64_t *out_bytes)
+{
+    KN_TRY(kn_linear_check(d));
+    if (!out_bytes) return KN_E_INVALID_ARG;
+    const int32_t len = part_length(d);
+    *out_bytes = d->rows <= len ? 0 : kn_align_up(part_places(d->rows, len) * ((int64_t)d->n_in * d->n_out + d->n_out) * 4, 256);
+    return KN_OK;
+}
+
+extern "C" int kn_grouped_linear_dw(void *stream, const kn_linear_desc *d, const void *x, const void *dy, const int32_t *offsets,
+                                    const int32_t *rows, void *dw, void *db, void *workspace, int64_t workspace_bytes)
+{
+    KN_TRY(kn_linear_check(d));
+    if (!offsets || !dw || (d->rows > 0 && (!dy || (d->x_rows > 0 && !x))) || (d->rows > 0 && !rows && d->x_rows < d->rows)) return KN_E_INVALID_ARG;
+    int64_t need = 0;
+    KN_TRY(kn_grouped_linear_dw_workspace_bytes(d, &need));
+    if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return KN_E_WORKSPACE;
+    Parts parts = {part_length(d), (float *)workspace, nullptr};
+    parts.bias_sums = parts.sums + part_places(d->rows, parts.len) * (int64_t)d->n_in * d->n_out;
+    KnProduct p = {};
+    const bool io = d->w_layout == KN_W_IN_OUT; // (columns are what is contiguous in dw)
+    p.a = io ? x : dy; p.b = io ? dy : x;
+    p.lda = io ? d->ldx : d->n_out; p.ldb = io ? d->n_out : d->ldx;
+    p.rows = io ? rows : nullptr; p.b_index = io ? nullptr : rows;
+    p.M = (int32_t)d->rows; p.E = d->experts; p.I = io ? d->n_in : d->n_out; p.J = io ? d->n_out : d->n_in;
+    p.a_rows = (int32_t)(io ? d->x_rows : d->rows); p.b_rows = (int32_t)(io ? d->rows : d->x_rows);
+    p.out = dw; p.out_bias = db; p.offsets = offsets;
+    p.o_group = (int64_t)d->n_in * d->n_out; p.o_i = p.J; p.o_j = 1;
+    const int32_t sum = !db ? SUM_NONE : io ? SUM_B : SUM_A;
+    return kn_with_type(d->dtype, [&](auto v) -> int {
+        typedef decltype(v) E_;
+        constexpr int64_t V = 16 / sizeof(E_);
+        p.wide = p.J % 8 == 0 && ((uintptr_t)dw & 15) == 0;
+        const bool direct = p.wide && p.I % 8 == 0 && (((uintptr_t)p.a | (uintptr_t)p.b) & 15) == 0 && p.lda % V == 0 && p.ldb % V == 0;
+        return direct ? launch_reduce<E_, true>((hipStream_t)stream, d, p, sum, parts) : launch_reduce<E_, false>((hipStream_t)stream, d, p, sum, parts);
+    });
+}

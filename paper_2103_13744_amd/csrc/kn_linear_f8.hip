@@ -122,8 +122,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
 {
     constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16;
     static_assert(F8_BLOCK % BN == 0, "a tile's columns share a scale");
-    typedef KnRowLoader<uint8_t, BM, NW> LoadA;
-    typedef KnRowLoader<uint8_t, BN, NW> LoadB;
+    typedef KnRowLoader<uint8_t, BM, NW, true> LoadA;
+    typedef KnRowLoader<uint8_t, BN, NW, true> LoadB;
     constexpr int WN = BN / WC, LD = WN + 4, LR = WN / 8;
     constexpr int BYTES = NB * STAGE > NW * 16 * LD * 4 ? NB * STAGE : NW * 16 * LD * 4;
     __shared__ __align__(16) char lds_[BYTES];
@@ -147,8 +147,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
     const int32_t steps = some ? p.kb : 0;
     constexpr int LOADS = LoadA::N + LoadB::N;
     auto fetch = [&](int s, int at) {
-        la.fetch(lds + at * STAGE, wave, F8_BLOCK);
-        lb.fetch(lds + at * STAGE + BM * 128, wave, F8_BLOCK);
+        la.fetch(lds + at * STAGE, wave, lane, F8_BLOCK);
+        lb.fetch(lds + at * STAGE + BM * 128, wave, lane, F8_BLOCK);
     };
     const float *ws = p.ws + (group * ((p.N + F8_BLOCK - 1) / F8_BLOCK) + j0 / F8_BLOCK) * p.kb;
     const int wi = (wave / WC) * (BM / WR), wj = (wave % WC) * WN;

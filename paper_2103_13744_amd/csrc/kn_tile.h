@@ -22,19 +22,21 @@ __device__ __forceinline__ void kn_fetch(const void *src, KN_LDS char *lds)
     __builtin_amdgcn_global_load_lds((const KN_GLOBAL uint32_t *)src, (KN_LDS uint32_t *)lds, 16, 0, 0);
 }
 
-template <typename T> struct KnFrag;
+template <typename T> struct KnFrag; // 16 bytes of values
+template <> struct KnFrag<uint8_t> { typedef kn_u32x4 Type; };
 template <> struct KnFrag<_Float16> { typedef kn_f16x8 Type; };
 template <> struct KnFrag<__bf16> { typedef kn_bf16x8 Type; };
 template <> struct KnFrag<float> { typedef kn_f32x4 Type; };
 
 // byte in a row-wise tile
 __device__ __forceinline__ int kn_row_byte(int r, int piece) { return r * 128 + ((piece ^ (r & 7)) << 4); }
-// exclusive or on the piece's number in row c of a column-wise tile: 16-bit fragments read rows 8 g + 0..3 of two g at a time, 32
-// bytes of each; fp32 fragments rows 4 g of four g, 64 bytes of each
-template <typename T> __device__ __forceinline__ int kn_col_swizzle(int c)
+// exclusive or on the piece's number in row c of a column-wise tile W wide: 16-bit fragments read rows 8 g + 0..3 of two g at a time,
+// 32 bytes of each (rows of 128 bytes lie two to a line of the banks); fp32 fragments rows 4 g of four g, 64 bytes of each
+template <typename T, int W> __device__ __forceinline__ int kn_col_swizzle(int c)
 {
-    if constexpr (sizeof(T) == 2) return ((c & 3) | ((c >> 3 & 1) << 2)) << 1;
-    else return (c >> 2 & 3) << 2;
+    if constexpr (sizeof(T) == 4) return (c >> 2 & 3) << 2;
+    else if constexpr (W == 64) return ((c >> 1 & 1) | (c >> 3 & 1) << 1) << 1;
+    else return ((c & 3) | (c >> 3 & 1) << 2) << 1;
 }
 
 typedef short kn_s16x4 __attribute__((ext_vector_type(4)));
@@ -51,7 +53,7 @@ template <typename T, int W> __device__ __forceinline__ typename KnFrag<T>::Type
     if constexpr (sizeof(T) == 2) {
         const int g = lane >> 4, i = lane & 15, c = kk * 32 + 8 * g + (i >> 2);
         const int piece = (j0 >> 3) + (i >> 1 & 1);
-        const KN_LDS char *at = tile + c * (W * 2) + ((piece ^ kn_col_swizzle<T>(c)) << 4) + (i & 1) * 8;
+        const KN_LDS char *at = tile + c * (W * 2) + ((piece ^ kn_col_swizzle<T, W>(c)) << 4) + (i & 1) * 8;
         union { kn_s16x4 h[2]; typename KnFrag<T>::Type v; } f;
         f.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KN_LDS kn_s16x4 *)at);
         f.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KN_LDS kn_s16x4 *)(at + 4 * W * 2)); // (the same swizzle)
@@ -61,102 +63,184 @@ template <typename T, int W> __device__ __forceinline__ typename KnFrag<T>::Type
         const int c = kk * 16 + 4 * (lane >> 4), j = j0 + (lane & 15);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-            v[q] = *(const KN_LDS float *)(tile + (c + q) * (W * 4) + (((j >> 2) ^ kn_col_swizzle<T>(c + q)) << 4) + (j & 3) * 4);
+            v[q] = *(const KN_LDS float *)(tile + (c + q) * (W * 4) + (((j >> 2) ^ kn_col_swizzle<T, W>(c + q)) << 4) + (j & 3) * 4);
         return v;
     }
 }
 
-// What a wavefront fetches of each stage of a row-wise tile of R rows (NW wavefronts in the workgroup): N times 8 rows.
-// row(r): address of row r's first value (any valid one for a row that does not exist: its results are not used).
-template <typename T, int R, int NW> struct KnRowLoader {
-    static constexpr int N = R / 8 / NW, CS = 128 / sizeof(T);
-    const char *at[N];
+// Values k .. k + W - 1 of a row of C wherever it lies, W = 16 bytes' worth; zeros behind its end.  k is a multiple of W.
+template <typename T> struct KnAny { typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T)))); };
+template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type kn_any_piece(const T *row, int32_t k, int32_t C)
+{
+    constexpr int W = 16 / sizeof(T);
+    typename KnFrag<T>::Type f;
+    if (k + W <= C) {
+        f = *(const typename KnAny<T>::Piece *)(row + k);
+    } else {
+#pragma unroll
+        for (int q = 0; q < W; ++q) {
+            const T v = row[min(k + q, C - 1)];
+            f[q] = k + q < C ? v : (T)0.0f;
+        }
+    }
+    return f;
+}
+
+// What a wavefront brings of each stage of a tile (NW wavefronts in the workgroup).  DIRECT: rows are made of whole 16-byte pieces on
+// multiples of 16 bytes, which go straight from memory to the LDS.  Else pieces that start anywhere and may end inside go through
+// registers: `fetch` puts down the stage that is there and asks for the one after it, so that `ask_first` comes before the first.
+//
+// A row-wise tile of R rows: N times 8 rows.  row(r): where row r begins (a row that does not exist: any valid one, its results
+// are not used).
+template <typename T, int R, int NW, bool DIRECT> struct KnRowLoader {
+    static constexpr int N = R / 8 / NW, CS = 128 / sizeof(T), W = 16 / sizeof(T);
+    const T *at[N];
+    typename KnFrag<T>::Type held[DIRECT ? 1 : N];
     int piece; // this lane's piece of a row
     template <typename F> __device__ __forceinline__ void start(int wave, int lane, F &&row)
     {
         piece = (lane & 7) ^ (lane >> 3);
 #pragma unroll
-        for (int t = 0; t < N; ++t) at[t] = (const char *)row((wave * N + t) * 8 + (lane >> 3)) + (piece << 4);
+        for (int t = 0; t < N; ++t) at[t] = row((wave * N + t) * 8 + (lane >> 3));
     }
-    // left: values of the contraction from this stage on; the stage's pieces behind them are zeros
-    __device__ __forceinline__ void fetch(KN_LDS char *tile, int wave, int32_t left)
+    // left: values of the contraction from the stage on; what lies behind them becomes zeros
+    __device__ __forceinline__ void ask(int32_t left)
     {
-        const bool none = left < CS && piece * 16 >= left * (int)sizeof(T);
 #pragma unroll
         for (int t = 0; t < N; ++t) {
-            kn_fetch(none ? (const char *)&kn_zeros : at[t], tile + (wave * N + t) * 1024);
-            at[t] += 128;
+            held[t] = typename KnFrag<T>::Type{};
+            if (piece * W < left) held[t] = kn_any_piece(at[t], piece * W, left);
+            at[t] += CS;
+        }
+    }
+    __device__ __forceinline__ void ask_first(int32_t left) { if constexpr (!DIRECT) ask(left); }
+    __device__ __forceinline__ void fetch(KN_LDS char *tile, int wave, int lane, int32_t left)
+    {
+        if constexpr (DIRECT) {
+            const bool none = left < CS && piece * W >= left;
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                kn_fetch(none ? (const void *)&kn_zeros : at[t] + piece * W, tile + (wave * N + t) * 1024);
+                at[t] += CS;
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < N; ++t) *(KN_LDS typename KnFrag<T>::Type *)(tile + (wave * N + t) * 1024 + lane * 16) = held[t];
+            if (left > CS) ask(left - CS);
         }
     }
 };
-// The same of a column-wise tile W wide: N times 1024 / (W sizeof(T)) rows of the contraction.  `pieces`: 16-byte pieces of a row
-// that are there (from the tile's first column on); a lane behind them fetches the last one.
-template <typename T, int W, int NW> struct KnColLoader {
-    static constexpr int CS = 128 / sizeof(T), PR = W * sizeof(T) / 16, RP = 64 / PR, N = CS / RP / NW;
-    const char *at[N];
+// A column-wise tile W wide: N times 1024 / (W sizeof(T)) rows of the contraction, `stride` values apart; `columns`: those that are
+// there from the tile's first on.  (DIRECT: a lane behind them fetches the last whole piece.)
+template <typename T, int W, int NW, bool DIRECT> struct KnColLoader {
+    static constexpr int CS = 128 / sizeof(T), PW = 16 / sizeof(T), PR = W / PW, RP = 64 / PR, N = CS / RP / NW;
+    const T *at[N];
+    typename KnFrag<T>::Type held[DIRECT ? 1 : N];
     int64_t step;
+    int32_t columns;
     __device__ __forceinline__ int row(int wave, int lane, int t) const { return (wave * N + t) * RP + lane / PR; }
-    __device__ __forceinline__ int piece(int wave, int lane, int t, int pieces) const
+    __device__ __forceinline__ int first_column(int wave, int lane, int t) const
     {
-        return min((lane % PR) ^ kn_col_swizzle<T>(row(wave, lane, t)), pieces - 1);
+        const int k = ((lane % PR) ^ kn_col_swizzle<T, W>(row(wave, lane, t))) * PW;
+        return DIRECT ? min(k, columns - PW) : k;
     }
-    __device__ __forceinline__ void start(int wave, int lane, const T *first, int64_t stride, int pieces)
+    __device__ __forceinline__ void start(int wave, int lane, const T *first, int64_t stride, int32_t n)
     {
-        step = stride * (int64_t)sizeof(T) * CS;
+        columns = n;
+        step = stride * CS;
 #pragma unroll
-        for (int t = 0; t < N; ++t) at[t] = (const char *)(first + row(wave, lane, t) * stride) + piece(wave, lane, t, pieces) * 16;
+        for (int t = 0; t < N; ++t) at[t] = first + row(wave, lane, t) * stride + (DIRECT ? first_column(wave, lane, t) : 0);
     }
-    __device__ __forceinline__ void fetch(KN_LDS char *tile, int wave, int lane, int32_t left)
+    __device__ __forceinline__ void ask(int wave, int lane, int32_t left)
     {
 #pragma unroll
         for (int t = 0; t < N; ++t) {
-            kn_fetch(row(wave, lane, t) < left ? at[t] : (const char *)&kn_zeros, tile + (wave * N + t) * 1024);
+            const int k = first_column(wave, lane, t);
+            held[t] = typename KnFrag<T>::Type{};
+            if (row(wave, lane, t) < left && k < columns) held[t] = kn_any_piece(at[t], k, columns);
             at[t] += step;
         }
     }
+    __device__ __forceinline__ void ask_first(int wave, int lane, int32_t left) { if constexpr (!DIRECT) ask(wave, lane, left); }
+    __device__ __forceinline__ void fetch(KN_LDS char *tile, int wave, int lane, int32_t left)
+    {
+        if constexpr (DIRECT) {
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                kn_fetch(row(wave, lane, t) < left ? (const void *)at[t] : (const void *)&kn_zeros, tile + (wave * N + t) * 1024);
+                at[t] += step;
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < N; ++t) *(KN_LDS typename KnFrag<T>::Type *)(tile + (wave * N + t) * 1024 + lane * 16) = held[t];
+            if (left > CS) ask(wave, lane, left - CS);
+        }
+    }
 };
-
-// A column-wise tile whose rows are those of one network, through an index or not: the numbers of the next stage's rows are
-// asked for before this stage's values, so that they are there when that stage is fetched.
-template <typename T, int W, int NW, bool INDEX> struct KnGroupLoader {
-    static constexpr int CS = 128 / sizeof(T), PR = W * sizeof(T) / 16, RP = 64 / PR, N = CS / RP / NW;
+// A column-wise tile whose rows are rows c0 .. last of a matrix of `rows`, through an index or (nullptr) not; the numbers of a
+// stage's rows are asked for a stage before its values.
+template <typename T, int W, int NW, bool DIRECT> struct KnGroupLoader {
+    static constexpr int CS = 128 / sizeof(T), PW = 16 / sizeof(T), PR = W / PW, RP = 64 / PR, N = CS / RP / NW;
     int32_t next[N];
-    int at[N]; // bytes of this lane's piece in a row
-    const char *base;
+    typename KnFrag<T>::Type held[DIRECT ? 1 : N];
+    const T *base;
     const int32_t *index;
     int64_t stride;
-    int32_t rows, last; // rows that there are; the network's last
+    int32_t rows, last, columns;
     __device__ __forceinline__ int row(int wave, int lane, int t) const { return (wave * N + t) * RP + lane / PR; }
-    __device__ __forceinline__ void ask(int wave, int lane, int32_t c0)
+    __device__ __forceinline__ int first_column(int wave, int lane, int t) const
+    {
+        const int k = ((lane % PR) ^ kn_col_swizzle<T, W>(row(wave, lane, t))) * PW;
+        return DIRECT ? min(k, columns - PW) : k;
+    }
+    __device__ __forceinline__ void ask_rows(int wave, int lane, int32_t c0)
     {
 #pragma unroll
         for (int t = 0; t < N; ++t) {
             const int32_t c = min(c0 + row(wave, lane, t), last);
-            next[t] = INDEX ? index[c] : c;
+            next[t] = index ? index[c] : c;
         }
     }
-    // first: the tile's first column; c0: the network's first row
-    __device__ __forceinline__ void start(int wave, int lane, const T *first, int64_t ld, int pieces, const int32_t *idx, int32_t n, int32_t c0, int32_t cend)
+    __device__ __forceinline__ void start(int wave, int lane, const T *first, int64_t ld, int32_t n_columns, const int32_t *idx, int32_t n_rows, int32_t c0,
+                                          int32_t cend)
     {
-        base = (const char *)first;
-        stride = ld * (int64_t)sizeof(T);
+        base = first;
+        stride = ld;
         index = idx;
-        rows = n;
+        rows = n_rows;
         last = cend - 1;
-#pragma unroll
-        for (int t = 0; t < N; ++t) at[t] = min((lane % PR) ^ kn_col_swizzle<T>(row(wave, lane, t)), pieces - 1) * 16;
-        ask(wave, lane, c0);
+        columns = n_columns;
+        ask_rows(wave, lane, c0);
+        if constexpr (!DIRECT) ask(wave, lane, c0);
     }
-    __device__ __forceinline__ void fetch(KN_LDS char *tile, int wave, int lane, int32_t c0)
+    __device__ __forceinline__ void ask(int wave, int lane, int32_t c0)
     {
-        int32_t now[N];
-#pragma unroll
-        for (int t = 0; t < N; ++t) now[t] = next[t];
-        ask(wave, lane, c0 + CS);
 #pragma unroll
         for (int t = 0; t < N; ++t) {
-            const bool there = c0 + row(wave, lane, t) <= last && (uint32_t)now[t] < (uint32_t)rows;
-            kn_fetch(there ? base + (int64_t)now[t] * stride + at[t] : (const char *)&kn_zeros, tile + (wave * N + t) * 1024);
+            const int k = first_column(wave, lane, t);
+            const bool there = c0 + row(wave, lane, t) <= last && (uint32_t)next[t] < (uint32_t)rows && k < columns;
+            held[t] = typename KnFrag<T>::Type{};
+            if (there) held[t] = kn_any_piece(base + next[t] * stride, k, columns);
+        }
+        ask_rows(wave, lane, c0 + CS);
+    }
+    // the stage whose first row is c0
+    __device__ __forceinline__ void fetch(KN_LDS char *tile, int wave, int lane, int32_t c0)
+    {
+        if constexpr (DIRECT) {
+            int32_t now[N];
+#pragma unroll
+            for (int t = 0; t < N; ++t) now[t] = next[t];
+            ask_rows(wave, lane, c0 + CS);
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                const bool there = c0 + row(wave, lane, t) <= last && (uint32_t)now[t] < (uint32_t)rows;
+                kn_fetch(there ? (const void *)(base + now[t] * stride + first_column(wave, lane, t)) : (const void *)&kn_zeros, tile + (wave * N + t) * 1024);
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < N; ++t) *(KN_LDS typename KnFrag<T>::Type *)(tile + (wave * N + t) * 1024 + lane * 16) = held[t];
+            if (c0 + CS <= last) ask(wave, lane, c0 + CS);
         }
     }
 };

@@ -81,7 +81,7 @@ def dev(t):
 SIZES = [  # rows, networks, inputs, outputs
     (0, 3, 16, 16), (1, 1, 1, 1), (1, 4, 64, 64), (2, 70, 128, 136), (5, 2, 2, 3), (16, 8, 256, 64), (17, 3, 33, 65), (64, 1, 64, 64),
     (65, 2, 63, 32), (129, 5, 91, 64), (200, 65, 32, 33), (257, 3, 72, 200), (300, 130, 64, 3), (500, 4, 320, 520), (1000, 7, 129, 127),
-    (1100, 3, 512, 256), (3000, 4200, 32, 32), (2100, 2, 136, 264), (300, 20, 200, 328), (1000, 30, 520, 256), (40, 2, 72, 520), (1300, 3, 40, 72),
+    (1100, 3, 512, 256), (3000, 4200, 32, 32), (2100, 2, 136, 264), (300, 20, 200, 328), (1000, 30, 520, 256), (40, 2, 72, 520), (1300, 3, 40, 72), (6000, 3, 40, 72), (5000, 4, 64, 33), (4000, 2, 200, 131),
 ]
 
 
@@ -486,7 +486,8 @@ def test_refusals_of_the_library():
         return C.byref(kn.LinearDesc(*[d[f] for f, _ in kn.LinearDesc._fields_]))
 
     calls = [lambda d: L.kn_grouped_linear(None, d, p, p, None, p, None, 0, p), lambda d: L.kn_grouped_linear_dx(None, d, p, p, None, p, None, p),
-             lambda d: L.kn_grouped_linear_dw(None, d, p, p, p, None, p, None)]
+             lambda d: L.kn_grouped_linear_dw(None, d, p, p, p, None, p, None, None, 0),
+             lambda d: L.kn_grouped_linear_dw_workspace_bytes(d, C.byref(n))]
     for call in calls:
         assert call(None) == -1
         for bad in (dict(dtype=3), dict(w_layout=2), dict(experts=0), dict(n_in=0), dict(n_out=0), dict(rows=-1), dict(x_rows=-1), dict(ldx=7)):
@@ -498,7 +499,12 @@ def test_refusals_of_the_library():
     assert L.kn_grouped_linear(None, desc(rows=0), None, None, None, None, None, 0, None) == 0
     assert L.kn_grouped_linear_dx(None, desc(), None, p, None, p, None, p) == -1
     assert L.kn_grouped_linear_dx(None, desc(rows=0), None, None, None, None, None, None) == 0
-    assert L.kn_grouped_linear_dw(None, desc(), p, p, None, None, p, None) == -1           # offsets are needed even for zeros
+    assert L.kn_grouped_linear_dw(None, desc(), p, p, None, None, p, None, None, 0) == -1  # offsets are needed even for zeros
+    many = desc(rows=100000, x_rows=100000, n_in=256, n_out=256, ldx=256)
+    assert L.kn_grouped_linear_dw_workspace_bytes(many, C.byref(n)) == 0 and n.value >= 2 * 256 * 256 * 4
+    assert L.kn_grouped_linear_dw(None, many, p, p, p, None, p, None, None, 0) == -3
+    assert L.kn_grouped_linear_dw(None, many, p, p, p, None, p, None, p + 16, n.value) == -3
+    assert L.kn_grouped_linear_dw(None, many, p, p, p, None, p, None, p, n.value - 1) == -3
     assert L.kn_grouped_linear_f8(None, desc(), p, p, p + 8, p, None, p, None, 0, p) == -1  # 16-byte rows
     assert L.kn_grouped_linear_f8(None, desc(), p, None, p, p, None, p, None, 0, p) == -1
     assert L.kn_grouped_linear_f8(None, desc(dtype=5), p, p, p, p, None, p, None, 0, p) == -1
