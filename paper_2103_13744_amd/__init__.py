@@ -457,31 +457,37 @@ def composite(sigma, rgb, offsets, step, term_eps=0.0, bg=(0.0, 0.0, 0.0)):
 
 # ---------------------------------------------------------------------------------------------
 # networks chosen per row: router, grouped products, weighted sum
+_dtype_ids = None  # (dtype -> kn_dtype; filled once torch is there)
+
+
 def _dtype_id(dtype) -> int:
-    wd = {torch.float32: KN_F32, torch.float16: KN_F16, torch.bfloat16: KN_BF16}.get(dtype)
+    global _dtype_ids
+    if _dtype_ids is None:
+        _dtype_ids = {torch.float32: KN_F32, torch.float16: KN_F16, torch.bfloat16: KN_BF16}
+    wd = _dtype_ids.get(dtype)
     if wd is None:
         raise KnError("unsupported dtype %s" % dtype)
     return wd
 
 
-def _rows_ptr(t, shape):
+def _rows_ptr(t, width):
     """Pointer and row stride of a matrix whose rows are contiguous but may lie apart (a slice of the columns of a wider one)."""
-    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        raise KnError("expected a device matrix with contiguous rows")
-    if any(w is not None and int(w) != int(h) for w, h in zip(shape, t.shape)):
-        raise KnError("expected shape %s, got %s" % (tuple(shape), tuple(t.shape)))
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if t.is_cuda and t.dim() == 2 and t.shape[1] == width:
+        if t.is_contiguous():
+            return t.data_ptr(), width
+        if (width == 1 or t.stride(1) == 1) and t.stride(0) >= width:
+            return t.data_ptr(), t.stride(0)
+    raise KnError("expected a device matrix with contiguous rows of %d, got %s" % (width, tuple(t.shape)))
 
 
 def _weights_layout(w):
     """kn_w_layout of (E, n_in, n_out) weights: contiguous, or the transpose of contiguous (E, n_out, n_in) ones."""
-    if w.dim() != 3 or not w.is_cuda:
-        raise KnError("weights must be a device tensor (experts, n_in, n_out)")
-    if w.is_contiguous():
-        return 0
-    if w.transpose(1, 2).is_contiguous():
-        return 1
-    raise KnError("weights must be contiguous, or a transpose of contiguous (experts, n_out, n_in) ones")
+    if w.dim() == 3 and w.is_cuda:
+        if w.is_contiguous():
+            return 0
+        if w.transpose(1, 2).is_contiguous():
+            return 1
+    raise KnError("weights must be a device tensor (experts, n_in, n_out), contiguous or a transpose of contiguous (experts, n_out, n_in) ones")
 
 
 def route(logits, k, renormalize=True):
@@ -489,7 +495,7 @@ def route(logits, k, renormalize=True):
     all but the first: what ``grouped_linear`` takes as ``rows`` and ``offsets`` and ``combine`` as ``slots`` and ``weights``."""
     L = load_library()
     T, E = logits.shape
-    ptr, ld = _rows_ptr(logits, (None, None))
+    ptr, ld = _rows_ptr(logits, E)
     dt, k, i32 = _dtype_id(logits.dtype), int(k), torch.int32
     if k < 1 or k > E:
         raise KnError("expected 1 <= k <= %d experts, got %d" % (E, k))
@@ -510,7 +516,7 @@ def route_backward(logits, weights, ids, dweights, renormalize=True):
     L = load_library()
     T, E = logits.shape
     k = ids.shape[1]
-    ptr, ld = _rows_ptr(logits, (None, None))
+    ptr, ld = _rows_ptr(logits, E)
     out = logits.new_empty((T, E))
     f = torch.float32
     _check(L.kn_route_backward(_stream(), ptr, _dtype_id(logits.dtype), T, E, ld, k, 1 if renormalize else 0, _ptr(weights, f, shape=(T, k)),
@@ -523,7 +529,7 @@ def _linear_desc(x, w, rows):
     E, n_in, n_out = w.shape
     if x.dtype is not w.dtype:
         raise KnError("inputs and weights must have one dtype, got %s and %s" % (x.dtype, w.dtype))
-    px, ld = _rows_ptr(x, (None, n_in))
+    px, ld = _rows_ptr(x, n_in)
     M = x.shape[0] if rows is None else rows.shape[0]
     pr = None if rows is None else _ptr(rows, torch.int32, shape=(M,))
     return LinearDesc(_dtype_id(x.dtype), _weights_layout(w), E, n_in, n_out, M, x.shape[0], ld), M, px, w.data_ptr(), pr
@@ -580,7 +586,7 @@ def quantize_f8(x):
     """Rows in 8 bits: (R, K) -> (float8_e4m3fn (R, kb * 128), zeros behind the K-th; float32 scales (R, kb)), kb = ceil(K / 128)."""
     L = load_library()
     R, K = x.shape
-    ptr, ld = _rows_ptr(x, (None, None))
+    ptr, ld = _rows_ptr(x, K)
     kb = -(-K // 128)
     q, s = x.new_empty((R, kb * 128), dtype=torch.float8_e4m3fn), x.new_empty((R, kb), dtype=torch.float32)
     _check(L.kn_quantize_f8(_stream(), ptr, _dtype_id(x.dtype), R, K, ld, q.data_ptr(), s.data_ptr()), "kn_quantize_f8")

@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
 {
     constexpr int W = SmallFrag<T>::W, KS = SmallFrag<T>::KS, SUBS = SMALL_ROWS / 16;
     typedef typename KnFrag<T>::Type Frag;
-    typedef T Four __attribute__((ext_vector_type(4)));
+    typedef T Four __attribute__((ext_vector_type(4), aligned(sizeof(T)))); // wherever they lie
     const int lane = kn_thread() & 63, col = lane & 15, g = lane >> 4;
     const int32_t number = __builtin_amdgcn_readfirstlane(kn_block() * SMALL_WAVES + (kn_thread() >> 6));
     const int ntiles = (p.J + 16 * V - 1) / (16 * V);
@@ -312,7 +312,6 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
             for (int k = 0; k < KF; ++k) fa[s][k] = kn_any_piece<T>(arow[s], k * KS + g * W, C);
     }
     const T *bias = (const T *)p.bias, *mask = (const T *)p.mask;
-    const bool fours = p.J % 4 == 0 && (((uintptr_t)p.out | (uintptr_t)bias | (uintptr_t)mask) & (4 * sizeof(T) - 1)) == 0 && (!mask || p.ldm % 4 == 0);
 #pragma unroll
     for (int s = 0; s < SUBS; ++s) {
         const int32_t i = piece.begin + 16 * s + col;
@@ -339,12 +338,14 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
             const int32_t j = j0 + 16 * v + 4 * g; // this lane's columns j .. j + 3
             if (j >= p.J) continue;
             float y[4] = {acc[v][0], acc[v][1], acc[v][2], acc[v][3]};
+            const bool fours = j + 4 <= p.J;
             Four m = {}, o, add = {};
             if (some && bias) {
-                if (fours) add = *(const Four *)(bias + group * p.J + j);
+                const T *at = bias + group * p.J;
+                if (fours) add = *(const Four *)(at + j);
                 else
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) add[r] = bias[group * p.J + min(j + r, p.J - 1)];
+                    for (int r = 0; r < 4; ++r) add[r] = at[min(j + r, p.J - 1)];
             }
             if (mrow) {
                 if (fours) m = *(const Four *)(mrow + j);

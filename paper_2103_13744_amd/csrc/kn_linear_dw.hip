@@ -156,12 +156,129 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
     }
 }
 
-// The parts' sums of the networks that have several, in the order of the parts; JOIN results per workgroup.
-constexpr int JOIN = 4096;
-template <typename T> __global__ void __launch_bounds__(256) k_reduce_join(KnProduct p, int32_t sum, Parts parts)
+// Layers of the small networks' kind whose rows are not whole pieces: a workgroup of four wavefronts per part and 64 x 16 V results; a
+// wavefront takes every fourth step of rows, straight into fragments, value by value (16 neighbouring lanes, 16 neighbouring values),
+// and the four are summed in the order of their numbers.  Nothing is staged and nothing waits until then: a part of a few
+// hundred rows is one chain of look-up, index, values, and the chains in flight are what counts.
+constexpr int SMALL_WAVES = 4, SMALL_I = 64;
+template <typename T, int V>
+__global__ void __launch_bounds__(SMALL_WAVES * 64) k_reduce_small(KnProduct p, int32_t sum, Parts parts)
 {
+    constexpr int W = 16 / sizeof(T), RS = 4 * W, U = SMALL_I / 16, BN = 16 * V, LD = BN + 4;
+    typedef typename KnFrag<T>::Type Frag;
+    __shared__ __align__(16) float red[SMALL_I * LD];
+    __shared__ float side_a[SMALL_I], side_b[BN];
+    const int tid = kn_thread(), lane = tid & 63, col = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int jtiles = (p.J + BN - 1) / BN, itiles = (p.I + SMALL_I - 1) / SMALL_I, tiles = itiles * jtiles;
+    const int number = kn_block() % tiles;
+    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, parts.len, kn_block() / tiles);
+    const int32_t group = piece.group;
+    if (group >= p.E) return;
+    const int32_t o = kn_offset(p.offsets, group, p.M), c0 = piece.begin, cend = max(c0, min(piece.end, c0 + parts.len));
+    if (c0 >= cend && c0 != o) return; // (the first part of a network without rows writes zeros)
+    const bool several = piece.end - o > parts.len;
+    const int64_t place = 2 * (o / parts.len) + (c0 - o) / parts.len;
+    const int j0 = number % jtiles * BN, i0 = number / jtiles * SMALL_I;
+    const bool sum_a = sum == SUM_A && j0 == 0, sum_b = sum == SUM_B && i0 == 0;
+    int32_t ai[U], bj[V];
+#pragma unroll
+    for (int u = 0; u < U; ++u) ai[u] = min(i0 + 16 * u + col, p.I - 1);
+#pragma unroll
+    for (int v = 0; v < V; ++v) bj[v] = min(j0 + 16 * v + col, p.J - 1);
+    kn_f32x4 acc[U][V] = {}, sa[U] = {}, sb[V] = {};
+    Frag ones;
+#pragma unroll
+    for (int q = 0; q < W; ++q) ones[q] = (T)1.0f;
+    for (int32_t c = c0 + wave * RS; c < cend; c += SMALL_WAVES * RS) {
+        Frag fa[U], fb[V];
+#pragma unroll
+        for (int q = 0; q < W; ++q) { // (rows behind the part, and rows that a matrix does not have: zeros)
+            const int32_t r = min(c + g * W + q, cend - 1), ra = p.rows ? p.rows[r] : r, rb = p.b_index ? p.b_index[r] : r;
+            const bool in = c + g * W + q < cend, in_a = in && (uint32_t)ra < (uint32_t)p.a_rows, in_b = in && (uint32_t)rb < (uint32_t)p.b_rows;
+            const T *a = (const T *)p.a + (int64_t)(in_a ? ra : 0) * p.lda, *b = (const T *)p.b + (int64_t)(in_b ? rb : 0) * p.ldb;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const T x = p.a_rows > 0 ? a[ai[u]] : (T)0.0f;
+                fa[u][q] = in_a ? x : (T)0.0f;
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const T x = p.b_rows > 0 ? b[bj[v]] : (T)0.0f;
+                fb[v][q] = in_b ? x : (T)0.0f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[v], fa[u], acc[u][v]);
+        if (sum_a)
+#pragma unroll
+            for (int u = 0; u < U; ++u) sa[u] = kn_mfma(ones, fa[u], sa[u]);
+        if (sum_b)
+#pragma unroll
+            for (int v = 0; v < V; ++v) sb[v] = kn_mfma(fb[v], ones, sb[v]);
+    }
+    for (int w = 0; w < SMALL_WAVES; ++w) { // (a lane's four results are neighbours in a row)
+        if (wave == w) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    kn_f32x4 *at = (kn_f32x4 *)(red + (16 * u + col) * LD + 16 * v + 4 * g);
+                    *at = w ? *at + acc[u][v] : acc[u][v];
+                }
+                if (sum_a && g == 0) side_a[16 * u + col] = w ? side_a[16 * u + col] + sa[u][0] : sa[u][0];
+            }
+            if (sum_b && col == 0)
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) side_b[16 * v + 4 * g + r] = w ? side_b[16 * v + 4 * g + r] + sb[v][r] : sb[v][r];
+        }
+        __syncthreads();
+    }
+    const int32_t in = min(p.I - i0, SMALL_I), jn = min(p.J - j0, BN);
+    float *sums = parts.sums + place * p.I * p.J;
+    T *out = (T *)p.out + (int64_t)group * p.o_group;
+    for (int q = tid; q < in * jn; q += SMALL_WAVES * 64) {
+        const int i = q / jn, j = q % jn;
+        const int64_t at = (int64_t)(i0 + i) * p.J + j0 + j;
+        if (several) sums[at] = red[i * LD + j];
+        else out[at] = (T)red[i * LD + j];
+    }
+    const int n = sum_a ? in : sum_b ? jn : 0, first = sum_a ? i0 : j0, all = sum_a ? p.I : p.J;
+    if (tid < n) {
+        const float y = sum_a ? side_a[tid] : side_b[tid];
+        if (several) parts.bias_sums[place * all + first + tid] = y;
+        else ((T *)p.out_bias)[(int64_t)group * all + first + tid] = (T)y;
+    }
+}
+
+// The parts' sums of the networks that have several, in the order of the parts; JOIN results per workgroup.  SEARCH: there are at most
+// M / len such networks, and a workgroup looks for its own among all (few networks of many results); else there is one for
+// every network's results, and most find nothing to do.
+constexpr int JOIN = 4096;
+template <typename T, bool SEARCH> __global__ void __launch_bounds__(256) k_reduce_join(KnProduct p, int32_t sum, Parts parts)
+{
+    __shared__ int32_t scratch[4], found;
     const int64_t n = (int64_t)p.I * p.J;
-    const int32_t pieces = (int32_t)((n + JOIN - 1) / JOIN), group = kn_block() / pieces;
+    const int32_t pieces = (int32_t)((n + JOIN - 1) / JOIN), turn = kn_block() / pieces;
+    int32_t group = turn;
+    if constexpr (SEARCH) {
+        int32_t before = 0;
+        if (kn_thread() == 0) found = -1;
+        for (int32_t e0 = 0; e0 < p.E && before <= turn; e0 += 256) {
+            const int32_t e = e0 + kn_thread();
+            const bool several = e < p.E && kn_offset(p.offsets, e + 1, p.M) - kn_offset(p.offsets, e, p.M) > parts.len;
+            int32_t all;
+            const int32_t rank = before + kn_block_exclusive_scan(several ? 1 : 0, scratch, all);
+            if (several && rank == turn) found = e;
+            before += all;
+        }
+        __syncthreads();
+        group = found;
+        if (group < 0) return;
+    }
     const int32_t o = kn_offset(p.offsets, group, p.M), rows = kn_offset(p.offsets, group + 1, p.M) - o;
     if (rows <= parts.len) return;
     const int32_t count = (rows + parts.len - 1) / parts.len;
@@ -170,7 +287,7 @@ template <typename T> __global__ void __launch_bounds__(256) k_reduce_join(KnPro
     for (int64_t q = first + kn_thread(); q < min(n, first + JOIN); q += 256) {
         float y = 0.0f;
         for (int c = 0; c < count; ++c) y += parts.sums[(place + c) * n + q];
-        out[q / p.J * p.o_i + q % p.J] = (T)y;
+        out[q] = (T)y; // (out's rows follow one another)
     }
     if (sum == SUM_NONE || first > 0) return;
     const int32_t m = sum == SUM_A ? p.I : p.J;
@@ -181,30 +298,45 @@ template <typename T> __global__ void __launch_bounds__(256) k_reduce_join(KnPro
     }
 }
 
-// Tiles of 64 x 64 for layers no wider than that (four times as many workgroups at a time: such a tile's few rows are latency), of
-// 128 x 128 else.
-bool narrow(const kn_linear_desc *d) { return d->n_in <= 64 && d->n_out <= 64; }
+// Layers of up to 128 x 128 whose rows are not whole pieces are k_reduce_small's.  Else tiles of 64 x 64 for layers no wider than that
+// (four times as many workgroups at a time: such a tile's few rows are latency), of 128 x 128 for wider ones.
+enum Way { WAY_SMALL, WAY_64, WAY_128 };
+Way way_of(const kn_linear_desc *d, bool direct)
+{
+    if (!direct && d->n_in <= 128 && d->n_out <= 128) return WAY_SMALL;
+    return d->n_in <= 64 && d->n_out <= 64 ? WAY_64 : WAY_128;
+}
+bool narrow(const kn_linear_desc *d) { return d->n_in <= 128 && d->n_out <= 128; }
 
-// Rows of a part: enough parts for the chip, none shorter than 512 rows.
+// Rows of a part: a part more is a tile written and read again in fp32, so that there are only as many as keep the chip busy (wide
+// layers: 32 networks 1024 x 2048, the longest of 32,768 rows 5,741: parts of 1,024 rows 357 us, of 4,096 264, of 8,192 238, none
+// 231; 8 networks 512 x 512, the longest 23,284: 135, 89, 126, 299).
 int32_t part_length(const kn_linear_desc *d)
 {
-    const int64_t tile = narrow(d) ? 64 : 128, tiles = kn_div_up(d->n_in, tile) * kn_div_up(d->n_out, tile);
-    const int64_t len = kn_div_up(d->rows, kn_div_up(1024, tiles));
-    return (int32_t)kn_align_up(len < 512 ? 512 : len, 64);
+    const int64_t tiles = narrow(d) ? 1 : kn_div_up(d->n_in, 128) * kn_div_up(d->n_out, 128);
+    const int64_t len = kn_div_up(d->rows, kn_div_up(narrow(d) ? 1024 : 512, tiles)), least = narrow(d) ? 512 : 2048;
+    return (int32_t)kn_align_up(len < least ? least : len, 64);
 }
 
 template <typename T, bool DIRECT> int launch_reduce(hipStream_t st, const kn_linear_desc *d, const KnProduct &p, int32_t sum, const Parts &parts)
 {
-    const int tile = narrow(d) ? 64 : 128;
-    const int64_t blocks = kn_pieces(p.M, p.E, parts.len) * kn_div_up(p.I, tile) * kn_div_up(p.J, tile);
+    const Way way = way_of(d, DIRECT);
+    const int bn = way == WAY_64 ? 64 : way == WAY_128 ? 128 : p.J <= 16 ? 16 : p.J <= 32 ? 32 : 64, bm = way == WAY_128 ? 128 : 64;
+    const int64_t blocks = kn_pieces(p.M, p.E, parts.len) * kn_div_up(p.I, bm) * kn_div_up(p.J, bn);
     if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    if (narrow(d)) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 64, 64, 2, 2>), dim3((unsigned)blocks), dim3(256), 0, st, p, sum, parts);
-    else hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 128, 128, 2, 4>), dim3((unsigned)blocks), dim3(512), 0, st, p, sum, parts);
+    const dim3 grid((unsigned)blocks);
+    if (way == WAY_128) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 128, 128, 2, 4>), grid, dim3(512), 0, st, p, sum, parts);
+    else if constexpr (DIRECT) hipLaunchKernelGGL((k_product_reduce<T, true, 64, 64, 2, 2>), grid, dim3(256), 0, st, p, sum, parts);
+    else if (bn == 16) hipLaunchKernelGGL((k_reduce_small<T, 1>), grid, dim3(SMALL_WAVES * 64), 0, st, p, sum, parts);
+    else if (bn == 32) hipLaunchKernelGGL((k_reduce_small<T, 2>), grid, dim3(SMALL_WAVES * 64), 0, st, p, sum, parts);
+    else hipLaunchKernelGGL((k_reduce_small<T, 4>), grid, dim3(SMALL_WAVES * 64), 0, st, p, sum, parts);
     KN_CHECK_LAUNCH();
     if (p.M <= parts.len) return KN_OK; // (no network has several)
-    const int64_t joins = (int64_t)p.E * kn_div_up((int64_t)p.I * p.J, JOIN);
+    const int64_t most = p.M / parts.len, pieces = kn_div_up((int64_t)p.I * p.J, JOIN);
+    const bool search = most < p.E && p.E * pieces > 8192;
+    const int64_t joins = (search ? most : p.E) * pieces;
     if (joins > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_reduce_join<T>), dim3((unsigned)joins), dim3(256), 0, st, p, sum, parts);
+    hipLaunchKernelGGL(search ? (k_reduce_join<T, true>) : (k_reduce_join<T, false>), dim3((unsigned)joins), dim3(256), 0, st, p, sum, parts);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }
