@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p, int
 // registers; nothing goes through the LDS and no wavefront waits for another.  Such calls are bound by their bytes, or rather by the
 // latency of one look-up, one fetch and one store per piece: what is under way at a time is what counts, so all of a piece is
 // asked for at once.
-constexpr int SMALL_ROWS = 64, SMALL_WAVES = 4;
+constexpr int SMALL_ROWS = 32, SMALL_WAVES = 4;
 template <typename T> struct SmallFrag {
     static constexpr int W = 16 / sizeof(T), KS = 4 * W;
 };
@@ -270,7 +270,9 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
     constexpr int W = SmallFrag<T>::W, KS = SmallFrag<T>::KS, SUBS = SMALL_ROWS / 16;
     typedef typename KnFrag<T>::Type Frag;
     typedef T Four __attribute__((ext_vector_type(4), aligned(sizeof(T)))); // wherever they lie
+    __shared__ __align__(16) T rows_of[SMALL_WAVES][16 * 16 * V + W]; // 16 rows of results of a wavefront, as they follow one another
     const int lane = kn_thread() & 63, col = lane & 15, g = lane >> 4;
+    T *line = rows_of[kn_thread() >> 6];
     const int32_t number = __builtin_amdgcn_readfirstlane(kn_block() * SMALL_WAVES + (kn_thread() >> 6));
     const int ntiles = (p.J + 16 * V - 1) / (16 * V);
     if (number / ntiles >= pieces) return;
@@ -311,13 +313,37 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
 #pragma unroll
             for (int k = 0; k < KF; ++k) fa[s][k] = kn_any_piece<T>(arow[s], k * KS + g * W, C);
     }
+    const bool together = p.J % 4 != 0 && ntiles == 1; // rows that follow one another without fours of their own: stored as one line
+    // four neighbours j .. j + 3 of a row of J (behind its end: the last one, unused)
+    auto four = [&](const T *row, int32_t j) {
+        Four f;
+        if (j + 4 <= p.J) f = *(const Four *)(row + j);
+        else
+#pragma unroll
+            for (int r = 0; r < 4; ++r) f[r] = row[min(j + r, p.J - 1)];
+        return f;
+    };
     const T *bias = (const T *)p.bias, *mask = (const T *)p.mask;
+    Four add[V], m[SUBS][V]; // (a lane's columns are j0 + 16 v + 4 g .. + 3)
+#pragma unroll
+    for (int v = 0; v < V; ++v) add[v] = some && bias ? four(bias + group * p.J, min(j0 + 16 * v + 4 * g, p.J - 1)) : Four{};
+    if (some && mask) { // (asked for before the first result is stored, not one after the other's)
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) {
+            const int32_t i = min(piece.begin + 16 * s + col, piece.end - 1), src = p.mask_rows ? p.mask_rows[i] : i;
+            const bool in = (uint32_t)src < (uint32_t)p.m_rows;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                m[s][v] = Four{};
+                if (in) m[s][v] = four(mask + (int64_t)src * p.ldm, min(j0 + 16 * v + 4 * g, p.J - 1));
+            }
+        }
+    }
 #pragma unroll
     for (int s = 0; s < SUBS; ++s) {
         const int32_t i = piece.begin + 16 * s + col;
         if (piece.begin + 16 * s >= piece.end) break;
         kn_f32x4 acc[V] = {};
-        const T *mrow = nullptr;
         if (some && p.a_rows > 0) {
 #pragma unroll
             for (int k = 0; k < KF; ++k)
@@ -327,44 +353,40 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
 #pragma unroll
                 for (int v = 0; v < V; ++v) acc[v] = kn_f32x4{0, 0, 0, 0};
         }
-        if (some && mask) {
-            const int32_t m = min(i, piece.end - 1), src = p.mask_rows ? p.mask_rows[m] : m;
-            mrow = (uint32_t)src < (uint32_t)p.m_rows ? mask + (int64_t)src * p.ldm : nullptr;
-        }
-        if (i >= piece.end) continue;
-        T *out = (T *)p.out + (int64_t)i * p.o_i;
+        T *out = (T *)p.out + (int64_t)i * p.o_i, *first = (T *)p.out + (int64_t)(i - col) * p.o_i;
+        const int shift = (int)((uintptr_t)first / sizeof(T) % W); // (of the first result in its 16 bytes)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int32_t j = j0 + 16 * v + 4 * g; // this lane's columns j .. j + 3
-            if (j >= p.J) continue;
-            float y[4] = {acc[v][0], acc[v][1], acc[v][2], acc[v][3]};
-            const bool fours = j + 4 <= p.J;
-            Four m = {}, o, add = {};
-            if (some && bias) {
-                const T *at = bias + group * p.J;
-                if (fours) add = *(const Four *)(at + j);
-                else
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) add[r] = at[min(j + r, p.J - 1)];
-            }
-            if (mrow) {
-                if (fours) m = *(const Four *)(mrow + j);
-                else
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) m[r] = mrow[min(j + r, p.J - 1)];
-            }
+            const int32_t j = j0 + 16 * v + 4 * g;
+            if (j >= p.J || i >= piece.end) continue;
+            Four o;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                if (some && bias) y[r] += (float)add[r];
-                if (p.relu) y[r] = y[r] > 0.0f || y[r] != y[r] ? y[r] : 0.0f; // (a NaN stays one)
-                if (mask && !((float)m[r] > 0.0f)) y[r] = 0.0f;
-                o[r] = (T)y[r];
+                float y = acc[v][r];
+                if (some && bias) y += (float)add[v][r];
+                if (p.relu) y = y > 0.0f || y != y ? y : 0.0f; // (a NaN stays one)
+                if (some && mask && !((float)m[s][v][r] > 0.0f)) y = 0.0f;
+                o[r] = (T)y;
             }
-            if (fours) *(Four *)(out + j) = o;
-            else
+            if (together) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (j + r < p.J) line[shift + col * p.J + j + r] = o[r];
+            } else if (j + 4 <= p.J) {
+                *(Four *)(out + j) = o;
+            } else {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     if (j + r < p.J) out[j + r] = o[r];
+            }
+        }
+        if (together) {
+            const int end = shift + min(16, piece.end - (i - col)) * p.J;
+            for (int q = lane * W; q < end; q += 64 * W) {
+                if (q >= shift && q + W <= end) *(Frag *)(first + q - shift) = *(const Frag *)(line + q);
+                else
+                    for (int r = max(q, shift); r < min(q + W, end); ++r) first[r - shift] = line[r];
+            }
         }
     }
 }

@@ -77,11 +77,13 @@ template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type kn_any
     if (k + W <= C) {
         f = *(const typename KnAny<T>::Piece *)(row + k);
     } else {
+        f = typename KnFrag<T>::Type{};
+        if (k < C)
 #pragma unroll
-        for (int q = 0; q < W; ++q) {
-            const T v = row[min(k + q, C - 1)];
-            f[q] = k + q < C ? v : (T)0.0f;
-        }
+            for (int q = 0; q < W; ++q) {
+                const T v = row[min(k + q, C - 1)];
+                f[q] = k + q < C ? v : (T)0.0f;
+            }
     }
     return f;
 }
