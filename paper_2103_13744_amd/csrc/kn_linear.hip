@@ -77,7 +77,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
     KN_LDS char *lds = (KN_LDS char *)lds_;
     const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ntiles = (p.J + BN - 1) / BN;
-    const int32_t number = kn_xcd_order(kn_block(), blocks);
+    // (where a network has a piece or none, its columns go to all XCDs: only some networks have rows, XCDs should be alike)
+    const int32_t number = p.M < (int64_t)BM * p.E ? kn_block() : kn_xcd_order(kn_block(), blocks);
     const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, BM, number / ntiles);
     const int j0 = number % ntiles * BN;
     if (piece.begin >= piece.end) return;
@@ -180,14 +181,14 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
 // ones by naming.
 constexpr int FEW_WAVES = 8;
 template <typename T>
-__global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p, int32_t blocks)
+__global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p)
 {
     constexpr int R = 16 / sizeof(T), BN = 16 * R, KS = 4 * R, LD = BN + 4;
     typedef typename KnFrag<T>::Type Frag;
     __shared__ __align__(16) float red[FEW_WAVES * 16 * LD];
     const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ntiles = (p.J + BN - 1) / BN;
-    const int32_t number = kn_xcd_order(kn_block(), blocks);
+    const int32_t number = kn_block(); // (a network's columns over all XCDs: there is nothing to share but a few rows)
     const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, 16, number / ntiles);
     const int j0 = number % ntiles * BN;
     if (piece.begin >= piece.end) return;
@@ -416,7 +417,7 @@ template <typename T> int launch_few(hipStream_t st, const KnProduct &p)
 {
     const int64_t blocks = kn_pieces(p.M, p.E, 16) * kn_div_up(p.J, 256 / (int)sizeof(T));
     if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_product_few<T>), dim3((unsigned)blocks), dim3(FEW_WAVES * 64), 0, st, p, (int32_t)blocks);
+    hipLaunchKernelGGL((k_product_few<T>), dim3((unsigned)blocks), dim3(FEW_WAVES * 64), 0, st, p);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }

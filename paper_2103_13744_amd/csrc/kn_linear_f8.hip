@@ -130,7 +130,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
     KN_LDS char *lds = (KN_LDS char *)lds_;
     const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ntiles = (p.N + BN - 1) / BN;
-    const int32_t number = kn_xcd_order(kn_block(), blocks);
+    // (where a network has a piece or none, its columns go to all XCDs: only some networks have rows, XCDs should be alike)
+    const int32_t number = p.M < (int64_t)BM * p.E ? kn_block() : kn_xcd_order(kn_block(), blocks);
     const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, BM, number / ntiles);
     const int j0 = number % ntiles * BN;
     if (piece.begin >= piece.end) return;
