@@ -422,19 +422,31 @@ template <typename T> int launch_few(hipStream_t st, const KnProduct &p)
     return KN_OK;
 }
 
-// Which tile, by the rows that a network has on average.
+// Which kernel.  Large tiles fetch least per product, small ones fill the chip; measured (bf16, us, weights not in a cache):
+//   rows, networks, K, N (columns contiguous)      few   64 x 128   128 x 128   192 x 128
+//   32, 64, 2048, 1024, most networks without         21         31          35          40
+//   256, 8, 1024, 2048                                 9         13          14          18
+//   512, 64, 2048, 1024                               65         59          53          59
+//   8,192, 64, 2048, 1024                            194         85          88          98
+//   16,384, 64, 2048, 1024                                      126         113         127
+//   4,096, 8, 1024, 2048                              77         32          32          29
+//   65,536, 64, 2048, 1024                                      381         328         318
+// and with the contraction contiguous, 32 x 64 in four stages against 64 x 128: 24 to 32, 10 to 13, 61 to 68, 120 to 92.
 template <typename T, bool COLS> int launch_pieces(hipStream_t st, const KnProduct &p)
 {
-    const int64_t each = p.M / p.E;
-    if (!rows_of_pieces<T>(p)) return each >= 64 ? launch_rows<T, COLS, false, 128, 128, 2, 4, 2>(st, p) : launch_rows<T, COLS, false, 32, 128, 1, 4, 2>(st, p);
-    if (each >= 384) return launch_rows<T, COLS, true, 192, 128, 2, 2, 2>(st, p);
-    if (each >= 64) return launch_rows<T, COLS, true, 128, 128, 2, 4, 2>(st, p);
+    const int64_t each = p.M / p.E; // rows of a network, on average
+    auto tiles = [&](int64_t bm) { return (p.M + bm - 1) / bm * ((p.J + 127) / 128); };
+    if (!rows_of_pieces<T>(p))
+        return each >= 64 && tiles(128) >= 256 ? launch_rows<T, COLS, false, 128, 128, 2, 4, 2>(st, p) : launch_rows<T, COLS, false, 32, 128, 1, 4, 2>(st, p);
+    const bool little = (int64_t)p.M * p.J <= 1 << 19;
     if constexpr (COLS) {
-        if (p.M <= 32 || p.M < p.E) return launch_few<T>(st, p);
-        return launch_rows<T, COLS, true, 64, 256 / (sizeof(T) / 2), 1, 8 / (sizeof(T) / 2), 2>(st, p);
+        if (little && (each < 2 || (int64_t)p.E * p.C * p.J <= 1 << 25)) return launch_few<T>(st, p);
     } else {
-        return launch_rows<T, COLS, true, 32, 64, 1, 4, 4>(st, p);
+        if (little || each < 64) return launch_rows<T, COLS, true, 32, 64, 1, 4, 4>(st, p);
     }
+    if (each >= 384 && tiles(192) >= 256) return launch_rows<T, COLS, true, 192, 128, 2, 2, 2>(st, p);
+    if (each >= 192 && tiles(128) >= 512) return launch_rows<T, COLS, true, 128, 128, 2, 4, 2>(st, p);
+    return launch_rows<T, COLS, true, 64, 128, 1, 4, 2>(st, p);
 }
 
 template <typename T, bool COLS, int KF, int V> int launch_small(hipStream_t st, const KnProduct &p)

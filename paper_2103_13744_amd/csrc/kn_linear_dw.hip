@@ -298,13 +298,14 @@ template <typename T, bool SEARCH> __global__ void __launch_bounds__(256) k_redu
     }
 }
 
-// Layers of up to 128 x 128 whose rows are not whole pieces are k_reduce_small's.  Else tiles of 64 x 64 for layers no wider than that
-// (four times as many workgroups at a time: such a tile's few rows are latency), of 128 x 128 for wider ones.
+// Layers of up to 128 x 128 whose rows are not whole pieces are k_reduce_small's.  Else tiles of 64 x 64 where 128 x 128 would be few,
+// or layers are no wider than that (four times as many workgroups at a time: such a tile's few rows are latency).
 enum Way { WAY_SMALL, WAY_64, WAY_128 };
 Way way_of(const kn_linear_desc *d, bool direct)
 {
     if (!direct && d->n_in <= 128 && d->n_out <= 128) return WAY_SMALL;
-    return d->n_in <= 64 && d->n_out <= 64 ? WAY_64 : WAY_128;
+    if (d->n_in <= 64 && d->n_out <= 64) return WAY_64;
+    return d->experts * kn_div_up(d->n_in, 128) * kn_div_up(d->n_out, 128) < 256 && d->rows < 65536 ? WAY_64 : WAY_128;
 }
 bool narrow(const kn_linear_desc *d) { return d->n_in <= 128 && d->n_out <= 128; }
 
@@ -326,7 +327,7 @@ template <typename T, bool DIRECT> int launch_reduce(hipStream_t st, const kn_li
     if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
     const dim3 grid((unsigned)blocks);
     if (way == WAY_128) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 128, 128, 2, 4>), grid, dim3(512), 0, st, p, sum, parts);
-    else if constexpr (DIRECT) hipLaunchKernelGGL((k_product_reduce<T, true, 64, 64, 2, 2>), grid, dim3(256), 0, st, p, sum, parts);
+    else if (way == WAY_64) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 64, 64, 2, 2>), grid, dim3(256), 0, st, p, sum, parts);
     else if (bn == 16) hipLaunchKernelGGL((k_reduce_small<T, 1>), grid, dim3(SMALL_WAVES * 64), 0, st, p, sum, parts);
     else if (bn == 32) hipLaunchKernelGGL((k_reduce_small<T, 2>), grid, dim3(SMALL_WAVES * 64), 0, st, p, sum, parts);
     else hipLaunchKernelGGL((k_reduce_small<T, 4>), grid, dim3(SMALL_WAVES * 64), 0, st, p, sum, parts);
