@@ -99,7 +99,6 @@ struct KnProduct {
     int32_t M, E, I, J, C;           // rows, networks; weight gradient: rows of out_e; columns of out; contraction
     int32_t a_rows, b_rows, m_rows;  // rows that a, b (weight gradient) and the mask have (an index outside is a row of zeros)
     int32_t relu;
-    int32_t wide;                    // 8 columns lie in whole 16-byte pieces, of everything that has columns
 };
 
 // What the grouped products check alike

@@ -4,29 +4,19 @@
 
 namespace {
 
-// What is added to columns j .. j + 7 of a network's results (j a multiple of 8).  wide: 8 columns lie in whole 16-byte pieces, of
-// everything that has columns.
-template <typename T> __device__ __forceinline__ void bias_of(const KnProduct &p, bool some, int64_t group, int32_t j, bool wide, float add[8])
+// What is added to columns j .. j + 7 of a network's results (j a multiple of 8)
+template <typename T> __device__ __forceinline__ void bias_of(const KnProduct &p, bool some, int64_t group, int32_t j, float add[8])
 {
-    typedef T Piece __attribute__((ext_vector_type(8)));
+    const bool any = p.bias && some && j < p.J;
+    typename KnEight<T>::Piece v = {};
+    if (any) v = KnEight<T>::load((const T *)p.bias + group * p.J, j, p.J);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) add[q] = 0.0f;
-    if (!p.bias || !some || j >= p.J) return;
-    const T *bias = (const T *)p.bias + group * p.J;
-    if (wide) {
-        const Piece v = *(const Piece *)(bias + j);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) add[q] = (float)v[q];
-    } else {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) add[q] = (float)bias[min(j + q, p.J - 1)];
-    }
+    for (int q = 0; q < 8; ++q) add[q] = any ? (float)v[q] : 0.0f;
 }
 // The end of 8 neighbouring results of row i: zeros for a row that x does not have, bias, ReLU, the mask of a ReLU before; one rounding
 template <typename T>
-__device__ __forceinline__ void finish(const KnProduct &p, bool some, int32_t i, int32_t j, bool wide, const float add[8], float y[8])
+__device__ __forceinline__ void finish(const KnProduct &p, bool some, int32_t i, int32_t j, const float add[8], float y[8])
 {
-    typedef T Piece __attribute__((ext_vector_type(8)));
     if (p.rows && (uint32_t)p.rows[i] >= (uint32_t)p.a_rows) {
 #pragma unroll
         for (int q = 0; q < 8; ++q) y[q] = 0.0f;
@@ -38,27 +28,16 @@ __device__ __forceinline__ void finish(const KnProduct &p, bool some, int32_t i,
     }
     if (p.mask && some) {
         const int32_t src = p.mask_rows ? p.mask_rows[i] : i;
-        Piece m = {};
-        if ((uint32_t)src < (uint32_t)p.m_rows) {
-            const T *row = (const T *)p.mask + (int64_t)src * p.ldm;
-            if (wide) m = *(const Piece *)(row + j);
-            else
-#pragma unroll
-                for (int q = 0; q < 8; ++q) m[q] = row[min(j + q, p.J - 1)];
-        }
+        typename KnEight<T>::Piece m = {};
+        if ((uint32_t)src < (uint32_t)p.m_rows) m = KnEight<T>::load((const T *)p.mask + (int64_t)src * p.ldm, j, p.J);
 #pragma unroll
         for (int q = 0; q < 8; ++q)
             if (!((float)m[q] > 0.0f)) y[q] = 0.0f;
     }
-    T *out = (T *)p.out + (int64_t)i * p.o_i + j;
-    Piece o;
+    typename KnEight<T>::Piece o;
 #pragma unroll
     for (int q = 0; q < 8; ++q) o[q] = (T)y[q];
-    if (wide) *(Piece *)out = o;
-    else
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (j + q < p.J) out[q] = o[q];
+    KnEight<T>::store((T *)p.out + (int64_t)i * p.o_i, j, p.J, o);
 }
 
 // Tiles of BM x BN results, WR x WC wavefronts, NB stages in the LDS, of which one is multiplied while the others are fetched.  COLS:
@@ -154,9 +133,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
     static_assert(64 % LR == 0, "");
     const int cj = lane % LR * 8;
     const int32_t j = j0 + wj + cj;
-    const bool wide = DIRECT || p.wide;
     float add[8];
-    bias_of<T>(p, some, group, j, wide, add);
+    bias_of<T>(p, some, group, j, add);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -168,7 +146,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
             if (r >= 16 || i >= piece.end || j >= p.J) continue;
             const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj + 4);
             float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            finish<T>(p, some, i, j, wide, add, y);
+            finish<T>(p, some, i, j, add, y);
         }
     }
 }
@@ -251,8 +229,8 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p)
 #pragma unroll
             for (int n = 0; n < 4; ++n) { y[n] += lo[n]; y[n + 4] += hi[n]; }
         }
-        bias_of<T>(p, some, group, j, true, add);
-        finish<T>(p, some, i, j, true, add, y);
+        bias_of<T>(p, some, group, j, add);
+        finish<T>(p, some, i, j, add, y);
     }
 }
 
@@ -392,16 +370,11 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
     }
 }
 
-// Whether 8 columns lie in whole 16-byte pieces on multiples of 16 bytes, of everything that has columns
-template <typename T> bool wide_columns(const KnProduct &p)
-{
-    return p.J % 8 == 0 && ((uintptr_t)p.bias | (uintptr_t)p.mask | (uintptr_t)p.out) % 16 == 0 && (!p.mask || p.ldm * sizeof(T) % 16 == 0);
-}
-// Whether every row is made of such pieces, as the DIRECT kernels take them
-template <typename T> bool rows_of_pieces(const KnProduct &p)
+// Whether the rows of a and of b are made of whole 16-byte pieces on multiples of 16 bytes, as the DIRECT kernels take them
+template <typename T, bool COLS> bool rows_of_pieces(const KnProduct &p)
 {
     constexpr int64_t V = 16 / sizeof(T);
-    return wide_columns<T>(p) && ((uintptr_t)p.a | (uintptr_t)p.b) % 16 == 0 && p.C % V == 0 && p.lda % V == 0 && p.a_rows > 0;
+    return ((uintptr_t)p.a | (uintptr_t)p.b) % 16 == 0 && p.C % V == 0 && p.lda % V == 0 && (!COLS || p.J % V == 0) && p.a_rows > 0;
 }
 
 template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB> int launch_rows(hipStream_t st, const KnProduct &p)
@@ -436,7 +409,7 @@ template <typename T, bool COLS> int launch_pieces(hipStream_t st, const KnProdu
 {
     const int64_t each = p.M / p.E; // rows of a network, on average
     auto tiles = [&](int64_t bm) { return (p.M + bm - 1) / bm * ((p.J + 127) / 128); };
-    if (!rows_of_pieces<T>(p))
+    if (!rows_of_pieces<T, COLS>(p))
         return each >= 64 && tiles(128) >= 256 ? launch_rows<T, COLS, false, 128, 128, 2, 4, 2>(st, p) : launch_rows<T, COLS, false, 32, 128, 1, 4, 2>(st, p);
     const bool little = (int64_t)p.M * p.J <= 1 << 19;
     if constexpr (COLS) {
@@ -472,9 +445,8 @@ template <typename T, bool COLS> int launch_small_widths(hipStream_t st, const K
     }
 }
 
-template <typename T> int launch_forward(hipStream_t st, KnProduct p)
+template <typename T> int launch_forward(hipStream_t st, const KnProduct &p)
 {
-    p.wide = wide_columns<T>(p);
     const bool cols = p.b_j == 1 && p.b_c != 1; // (one column of one input: either)
     if (p.C <= SMALL_MOST && p.J <= SMALL_MOST) return cols ? launch_small_widths<T, true>(st, p) : launch_small_widths<T, false>(st, p);
     return cols ? launch_pieces<T, true>(st, p) : launch_pieces<T, false>(st, p);

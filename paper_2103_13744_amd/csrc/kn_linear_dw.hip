@@ -115,8 +115,6 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
     constexpr int WN = BN / WC, LD = WN + 4, LR = WN / 8;
     static_assert(64 % LR == 0, "");
     KN_LDS float *mine = (KN_LDS float *)(lds + wave * (16 * LD * 4));
-    typedef T Out __attribute__((ext_vector_type(8)));
-    const bool wide = DIRECT || p.wide;
     const int cj = lane % LR * 8;
     const int32_t j = j0 + wj + cj;
     float *sums = parts.sums + place * p.I * p.J;
@@ -131,26 +129,11 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
             const int32_t i = i0 + wi + 16 * u + r;
             if (r >= 16 || i >= p.I || j >= p.J) continue;
             const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj + 4);
-            const float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
             if (several) {
-                float *at = sums + (int64_t)i * p.J + j;
-                if (wide) {
-                    *(kn_f32x4 *)at = lo;
-                    *(kn_f32x4 *)(at + 4) = hi;
-                } else
-#pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        if (j + q < p.J) at[q] = y[q];
+                KnEight<float>::store(sums + (int64_t)i * p.J, j, p.J, typename KnEight<float>::Piece{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
             } else {
-                T *at = out + (int64_t)i * p.o_i + j;
-                Out v;
-#pragma unroll
-                for (int q = 0; q < 8; ++q) v[q] = (T)y[q];
-                if (wide) *(Out *)at = v;
-                else
-#pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        if (j + q < p.J) at[q] = v[q];
+                const typename KnEight<T>::Piece v = {(T)lo[0], (T)lo[1], (T)lo[2], (T)lo[3], (T)hi[0], (T)hi[1], (T)hi[2], (T)hi[3]};
+                KnEight<T>::store(out + (int64_t)i * p.o_i, j, p.J, v);
             }
         }
     }
@@ -376,8 +359,7 @@ extern "C" int kn_grouped_linear_dw(void *stream, const kn_linear_desc *d, const
     return kn_with_type(d->dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
         constexpr int64_t V = 16 / sizeof(E_);
-        p.wide = p.J % 8 == 0 && ((uintptr_t)dw & 15) == 0;
-        const bool direct = p.wide && p.I % 8 == 0 && (((uintptr_t)p.a | (uintptr_t)p.b) & 15) == 0 && p.lda % V == 0 && p.ldb % V == 0;
+        const bool direct = p.I % V == 0 && p.J % V == 0 && (((uintptr_t)p.a | (uintptr_t)p.b) & 15) == 0 && p.lda % V == 0 && p.ldb % V == 0;
         return direct ? launch_reduce<E_, true>((hipStream_t)stream, d, p, sum, parts) : launch_reduce<E_, false>((hipStream_t)stream, d, p, sum, parts);
     });
 }

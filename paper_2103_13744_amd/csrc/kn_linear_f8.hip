@@ -27,7 +27,7 @@ __device__ __forceinline__ float f8_row_max(float v)
 }
 
 // 16 lanes per row and block of 128 inputs, 8 values a lane.  Inputs beyond K are zeros.
-template <typename T, bool WIDE>
+template <typename T>
 __global__ void __launch_bounds__(256) k_quantize_rows(const T *__restrict__ x, int64_t R, int32_t K, int64_t ld, int32_t kb,
                                                        uint8_t *__restrict__ q, float *__restrict__ scales)
 {
@@ -37,18 +37,11 @@ __global__ void __launch_bounds__(256) k_quantize_rows(const T *__restrict__ x, 
     const int64_t row = g / kb;
     const int32_t blk = (int32_t)(g % kb), k0 = blk * F8_BLOCK + at * 8;
     float v[8];
-    const T *src = x + row * ld + k0;
-    if (WIDE && k0 + 8 <= K) {
-        typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T))));
 #pragma unroll
-        for (int i = 0; i < 8; i += 16 / (int)sizeof(T)) {
-            const Piece p = *(const Piece *)(src + i);
+    for (int i = 0; i < 8; i += 16 / (int)sizeof(T)) {
+        const typename KnFrag<T>::Type p = kn_any_piece(x + row * ld, k0 + i, K);
 #pragma unroll
-            for (int j = 0; j < 16 / (int)sizeof(T); ++j) v[i + j] = (float)p[j];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = k0 + i < K ? (float)src[i] : 0.0f;
+        for (int j = 0; j < 16 / (int)sizeof(T); ++j) v[i + j] = (float)p[j];
     }
     float amax = 0.0f;
 #pragma unroll
@@ -211,11 +204,9 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
     const T *bias = (const T *)p.bias;
     const int cj = lane % LR * 8;
     const int32_t j = j0 + wj + cj;
-    const bool wide = p.N % 8 == 0 && ((uintptr_t)y & 15) == 0;
-    typedef T Out __attribute__((ext_vector_type(8)));
     float add[8];
 #pragma unroll
-    for (int q = 0; q < 8; ++q) add[q] = bias && some && j + q < p.N ? (float)bias[group * p.N + j + q] : 0.0f;
+    for (int q = 0; q < 8; ++q) add[q] = bias && some && j < p.N ? (float)bias[group * p.N + min(j + q, p.N - 1)] : 0.0f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -227,18 +218,14 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
             if (r >= 16 || i >= piece.end || j >= p.N) continue;
             const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj + 4);
             const float s[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            Out o;
+            typename KnEight<T>::Piece o;
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 float t = s[q] + add[q];
                 if (p.relu) t = t > 0.0f || t != t ? t : 0.0f; // (a NaN stays one)
                 o[q] = (T)t;
             }
-            if (wide) *(Out *)(y + (int64_t)i * p.N + j) = o;
-            else
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    if (j + q < p.N) y[(int64_t)i * p.N + j + q] = o[q];
+            KnEight<T>::store(y + (int64_t)i * p.N, j, p.N, o);
         }
     }
 }
@@ -262,11 +249,9 @@ extern "C" int kn_quantize_f8(void *stream, const void *x, int32_t dtype, int64_
     const int32_t kb = (int32_t)kn_div_up(K, F8_BLOCK);
     const int64_t blocks = kn_div_up(R * kb, 16);
     if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    const bool wide = ((uintptr_t)x & 15) == 0 && ld * kn_item(dtype) % 16 == 0;
     return kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
-        auto kernel = wide ? k_quantize_rows<E_, true> : k_quantize_rows<E_, false>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, (const E_ *)x, R, K, ld, kb, (uint8_t *)q, scales);
+        hipLaunchKernelGGL((k_quantize_rows<E_>), dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, (const E_ *)x, R, K, ld, kb, (uint8_t *)q, scales);
         KN_CHECK_LAUNCH();
         return KN_OK;
     });

@@ -88,6 +88,28 @@ template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type kn_any
     return f;
 }
 
+// Eight neighbouring values of a row of J from j on, wherever they lie (behind its end: the last one / nothing)
+template <typename T> struct KnEight {
+    typedef T Piece __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    static __device__ __forceinline__ Piece load(const T *row, int32_t j, int32_t J)
+    {
+        Piece f;
+        if (j + 8 <= J) f = *(const Piece *)(row + j);
+        else
+#pragma unroll
+            for (int q = 0; q < 8; ++q) f[q] = row[min(j + q, J - 1)];
+        return f;
+    }
+    static __device__ __forceinline__ void store(T *row, int32_t j, int32_t J, Piece f)
+    {
+        if (j + 8 <= J) *(Piece *)(row + j) = f;
+        else
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (j + q < J) row[j + q] = f[q];
+    }
+};
+
 // What a wavefront brings of each stage of a tile (NW wavefronts in the workgroup).  DIRECT: rows are made of whole 16-byte pieces on
 // multiples of 16 bytes, which go straight from memory to the LDS.  Else pieces that start anywhere and may end inside go through
 // registers: `fetch` puts down the stage that is there and asks for the one after it, so that `ask_first` comes before the first.
