@@ -185,6 +185,49 @@ def test_linear_not_finite_values_stay_where_they_are():
 
 
 @pytest.mark.gpu
+def test_linear_many_networks():
+    """As many networks as there may be, most without a row: the look-up of a row's network takes three steps, every gradient is written."""
+    e, m, k, n = 65535, 700, 16, 24
+    ids = np.sort(np.random.default_rng(1).choice(e, m // 2).repeat(2))
+    off = torch.from_numpy(np.searchsorted(ids, np.arange(e + 1)).astype(np.int32))
+    x, w, dy = rand(1, m, k).bfloat16(), rand(2, e, k, n).bfloat16(), rand(3, m, n).bfloat16()
+    y = kn.grouped_linear(dev(x), dev(w), dev(off))
+    wx, dx64 = w.double()[ids], dy.double()
+    close(y, (x.double()[:, None] @ wx)[:, 0], (x.double().abs()[:, None] @ wx.abs())[:, 0], k, "bf16")
+    dx, dw, db = kn.grouped_linear_backward(dev(dy), dev(x), dev(w), dev(off))
+    close(dx, (dx64[:, None] @ wx.transpose(1, 2))[:, 0], (dx64.abs()[:, None] @ wx.abs().transpose(1, 2))[:, 0], n, "bf16")
+    want, mag = torch.zeros(e, k, n, dtype=torch.float64), torch.zeros(e, k, n, dtype=torch.float64)
+    outer = x.double()[:, :, None] * dx64[:, None, :]
+    want.index_add_(0, torch.from_numpy(ids), outer)
+    mag.index_add_(0, torch.from_numpy(ids), outer.abs())
+    close(dw, want, mag, int(np.bincount(ids).max()), "bf16")
+    wdb = torch.zeros(e, n, dtype=torch.float64).index_add_(0, torch.from_numpy(ids), dx64)
+    close(db, wdb, torch.zeros(e, n, dtype=torch.float64).index_add_(0, torch.from_numpy(ids), dx64.abs()), int(np.bincount(ids).max()), "bf16")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("k", [4096, 4095], ids=["pieces", "anywhere"])
+def test_linear_rows_beyond_32_bits(k):
+    """Rows of x whose bytes lie 4 GiB and more behind its first."""
+    x_rows, m, e, n = (1 << 19) + 777, 200, 2, 136
+    rows = torch.cat([torch.arange(x_rows - 100, x_rows), torch.arange(100) * 5000]).to(torch.int32)
+    off = torch.tensor([0, 90, 200], dtype=torch.int32)
+    some, w, dy = rand(1, m, k).bfloat16(), rand(2, e, k, n).bfloat16(), rand(3, m, n).bfloat16()
+    x = torch.empty(x_rows, k, dtype=torch.bfloat16, device="cuda")
+    assert x.numel() * 2 > 1 << 32
+    x[rows.long().cuda()] = dev(some)
+    want, mag = ref_linear(some, w, off, None, None, False)
+    close(kn.grouped_linear(x, dev(w), dev(off), rows=dev(rows)), want, mag, k, "bf16")
+    dw, _ = kn.grouped_linear_dw(dev(dy), x, dev(w), dev(off), rows=dev(rows), want_bias=False)
+    for g in range(e):
+        a, b = int(off[g]), int(off[g + 1])
+        xs, d = some[a:b].double(), dy[a:b].double()
+        close(dw[g], xs.T @ d, xs.abs().T @ d.abs(), b - a, "bf16")
+    q, s = kn.quantize_f8(x[-300:])
+    assert torch.equal(q[200:].view(torch.uint8), kn.quantize_f8(x[-100:])[0].view(torch.uint8))
+
+
+@pytest.mark.gpu
 def test_linear_gradient_against_differences():
     """The layer is linear in each input alone: (f(w + d) - f(w - d)) / 2 = <dw, d> up to rounding, and alike for x and bias."""
     m, e, k, n = 120, 4, 24, 40
@@ -520,6 +563,22 @@ def test_refusals_of_the_library():
 
 
 @pytest.mark.gpu
+def test_8_bit_sums_of_any_bits():
+    """Values over the whole range of e4m3, at random: the matrix instruction's own sum of a block keeps them within 2^-12 of the sum of
+    the products' magnitudes (it is narrower than fp32), the rest is fp32."""
+    g = torch.Generator().manual_seed(1)
+    m, k, n = 64, 256, 128
+    bits = lambda *s: torch.randint(0, 256, s, generator=g, dtype=torch.int32).to(torch.uint8)  # noqa: E731
+    finite = lambda b: torch.where((b & 127) == 127, b ^ 1, b).view(torch.float8_e4m3fn)  # noqa: E731
+    xq, wq = finite(bits(m, k)), finite(bits(1, n, k))
+    xs, ws = torch.exp(rand(2, m, k // 128)), torch.exp(rand(3, 1, 1, k // 128))
+    y = kn.grouped_linear_f8(xq.cuda(), xs.cuda(), wq.cuda(), ws.cuda(), torch.tensor([0, m], dtype=torch.int32).cuda(), dtype=torch.float32)
+    vx = xq.double() * xs.double().repeat_interleave(128, 1)
+    vw = wq[0].double() * ws[0].double().repeat_interleave(128, 1)
+    assert ((y.double().cpu() - vx @ vw.T).abs() <= 2.0 ** -12 * (vx.abs() @ vw.abs().T)).all()
+
+
+@pytest.mark.gpu
 def test_refusals_of_the_binding():
     x, w, off = torch.zeros(8, 4).cuda(), torch.zeros(2, 4, 6).cuda(), torch.zeros(3, dtype=torch.int32).cuda()
     for bad in (lambda: kn.grouped_linear(x.double(), w.double(), off), lambda: kn.grouped_linear(x.half(), w, off), lambda: kn.grouped_linear(x[:, :3], w, off),
@@ -532,3 +591,17 @@ def test_refusals_of_the_binding():
                 lambda: kn.grouped_linear_f8(x, x, w, w, off)):
         with pytest.raises(kn.KnError):
             bad()
+
+
+@pytest.mark.gpu
+def test_the_example_learns_and_serves_in_8_bits():
+    """Two hundred steps bring the loss to a small part of what it was; weights and inputs of 3 significant bits add about
+    (2^-4)^2 of the results' square per layer at most, far below what the field had to learn."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "routed_field.py")
+    spec = importlib.util.spec_from_file_location("routed_field", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    first, full, eight = module.main(steps=200, say=lambda *_: None)
+    assert full < first / 5 and eight < full + first / 20
