@@ -2,6 +2,8 @@
 // kn_grouped_linear_dw.
 #include "kn_tile.h"
 
+#include <type_traits>
+
 namespace {
 
 // What is added to columns j .. j + 7 of a network's results (j a multiple of 8)
@@ -96,14 +98,33 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
             else fb[kk][v] = kn_row_frag<T>(tb, wj + 16 * v, kk, lane);
         }
     };
-    auto multiply = [&](int kk) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[kk][v], fa[kk][u], acc[u][v]);
-    };
     // Half a stage's fragments are read while the other half's are multiplied; in between, the next stage has to have arrived, and the
-    // one behind the NB that lie in the LDS takes the place of the one that everybody has just read.
+    // one behind the NB that lie in the LDS takes the place of the one that everybody has just read.  A wavefront without rows (the
+    // end of a network's) only fetches: what its products would cost is power, which the others are short of.
+    auto march = [&](auto rows_there) {
+        constexpr bool ROWS = decltype(rows_there)::value;
+        auto multiply = [&](int kk) {
+            if constexpr (ROWS) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[kk][v], fa[kk][u], acc[u][v]);
+                kn_interleave<U, V, T, COLS>();
+            }
+        };
+        if constexpr (ROWS) read(0, 0);
+        for (int s = 0, at = 0; s < steps; ++s) {
+            const int next = at + 1 == NB ? 0 : at + 1;
+            if constexpr (ROWS) read(at, 1);
+            multiply(0);
+            if (s + NB <= steps) kn_stage_barrier<LATER>();
+            else kn_stage_barrier<0>();
+            if (s + NB < steps) fetch(s + NB, at);
+            if constexpr (ROWS) read(next, 0); // (behind the last stage: what happens to lie there, unused)
+            multiply(1);
+            at = next;
+        }
+    };
     if (steps > 0) {
         la.ask_first(C);
         if constexpr (COLS) lbc.ask_first(wave, lane, C);
@@ -111,20 +132,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
         for (int s = 0; s < NB && s < steps; ++s) fetch(s, s);
         if (DIRECT && steps >= NB) kn_stage_barrier<(NB - 1) * LOADS>();
         else kn_stage_barrier<0>();
-        read(0, 0);
-        for (int s = 0, at = 0; s < steps; ++s) {
-            const int next = at + 1 == NB ? 0 : at + 1;
-            read(at, 1);
-            multiply(0);
-            kn_interleave<U, V, T, COLS>();
-            if (s + NB <= steps) kn_stage_barrier<LATER>();
-            else kn_stage_barrier<0>();
-            if (s + NB < steps) fetch(s + NB, at);
-            read(next, 0); // (behind the last stage: what happens to lie there, unused)
-            multiply(1);
-            kn_interleave<U, V, T, COLS>();
-            at = next;
-        }
+        if (WR == 1 || piece.begin + wi < piece.end) march(std::true_type());
+        else march(std::false_type());
     }
     kn_stage_barrier(); // (the tiles' LDS is used again)
     // 16 rows of the wavefront's results at a time, in LDS of its own
