@@ -125,7 +125,7 @@ template <typename T, int R, int NW, bool DIRECT> struct KnRowLoader {
     {
         piece = (lane & 7) ^ (lane >> 3);
 #pragma unroll
-        for (int t = 0; t < N; ++t) at[t] = row((wave * N + t) * 8 + (lane >> 3));
+        for (int t = 0; t < N; ++t) at[t] = row((wave * N + t) * 8 + (lane >> 3)) + (DIRECT ? piece * W : 0);
     }
     // left: values of the contraction from the stage on; what lies behind them becomes zeros
     __device__ __forceinline__ void ask(int32_t left)
@@ -144,7 +144,7 @@ template <typename T, int R, int NW, bool DIRECT> struct KnRowLoader {
             const bool none = left < CS && piece * W >= left;
 #pragma unroll
             for (int t = 0; t < N; ++t) {
-                kn_fetch(none ? (const void *)&kn_zeros : at[t] + piece * W, tile + (wave * N + t) * 1024);
+                kn_fetch(none ? (const void *)&kn_zeros : at[t], tile + (wave * N + t) * 1024);
                 at[t] += CS;
             }
         } else {
