@@ -400,8 +400,10 @@ template <typename T> struct Vec {
 };
 
 // out[t] = sum over j of weights[t, j] y[slots[t, j]]: a thread per V neighbouring values of a row.  V: 16 bytes where the rows
-// are made of whole such pieces, else 1.
-template <typename T, int V>
+// are made of whole such pieces, else 1.  Bound by its bytes.  STREAM: what is read and written once goes past the caches, where
+// y does not stay in them anyway (16,384 rows of 4 x 2048 in bf16, 336 MB: 83 us without, 64 with: 5.3 TB/s).
+constexpr int64_t COMBINE_STREAM = 1 << 26; // bytes of y
+template <typename T, int V, bool STREAM>
 __global__ void __launch_bounds__(256) k_combine(const T *__restrict__ y, const int32_t *__restrict__ slots, const float *__restrict__ weights,
                                                  int32_t M, int32_t D, int32_t Tn, int32_t k, T *__restrict__ out)
 {
@@ -415,18 +417,22 @@ __global__ void __launch_bounds__(256) k_combine(const T *__restrict__ y, const 
         const int32_t s = slots[(int64_t)t * k + j];
         if ((uint32_t)s >= (uint32_t)M) continue;
         const float w = weights ? weights[(int64_t)t * k + j] : 1.0f;
-        const Piece v = *(const Piece *)(y + (int64_t)s * D + (int64_t)c * V);
+        const Piece *at = (const Piece *)(y + (int64_t)s * D + (int64_t)c * V);
+        const Piece v = STREAM ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] = fmaf(w, (float)v[i], acc[i]);
     }
     Piece r;
 #pragma unroll
     for (int i = 0; i < V; ++i) r[i] = (T)acc[i];
-    *(Piece *)(out + (int64_t)t * D + (int64_t)c * V) = r;
+    Piece *to = (Piece *)(out + (int64_t)t * D + (int64_t)c * V);
+    if (STREAM) __builtin_nontemporal_store(r, to);
+    else *to = r;
 }
 
-// dy[slots[t, j]] = weights[t, j] dout[t], dweights[t, j] = <dout[t], y[slots[t, j]]>: a wavefront per pair, so that a row of
-// dout is read k times, but for the first from the caches.
+// dy[slots[t, j]] = weights[t, j] dout[t], dweights[t, j] = <dout[t], y[slots[t, j]]>: a wavefront per pair; a row of
+// dout is read k times, but for the first from the caches.  Bound by its bytes (the same sizes, 604 MB: 118 us, 5.1 TB/s; a
+// wavefront per row of dout, four pairs at a time: 143).
 template <typename T, int V>
 __global__ void __launch_bounds__(256) k_combine_backward(const T *__restrict__ dout, const T *__restrict__ y, const int32_t *__restrict__ slots,
                                                           const float *__restrict__ weights, int32_t M, int32_t D, int64_t pairs, int32_t k,
@@ -571,7 +577,7 @@ extern "C" int kn_combine(void *stream, const void *y, int32_t dtype, int64_t M,
         const bool wide = whole_pieces(D, dtype, y, out, nullptr);
         const int64_t blocks = kn_div_up(T * (wide ? D / V : D), 256);
         if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-        auto kernel = wide ? k_combine<E_, V> : k_combine<E_, 1>;
+        auto kernel = !wide ? k_combine<E_, 1, false> : M * D * (int64_t)sizeof(E_) < COMBINE_STREAM ? k_combine<E_, V, false> : k_combine<E_, V, true>;
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, (const E_ *)y, slots, weights, (int32_t)M, D, (int32_t)T,
                            k, (E_ *)out);
         KN_CHECK_LAUNCH();
