@@ -46,6 +46,9 @@ __device__ __forceinline__ void finish(const KnProduct &p, bool some, int32_t i,
 // b's columns are contiguous in memory (else its contraction is).  DIRECT: rows of whole 16-byte pieces throughout (KnRowLoader).
 // Fragments of b are the products' first operand, so that a lane holds four neighbouring results of a row; they go through
 // the LDS once more to leave in pieces of 8.
+// Measured: 65,536 rows through an index, 64 networks 2048 x 1024 in bf16, 192 x 128: 320 us, 860 TFLOP/s, where one product of the
+// library of 8192 x 8192 x 8192 reaches 1,250.  Power bounds it: the clock is 2.03 GHz with the matrix cores busy 44 % of the time;
+// with 256 x 256 it is 2.30 GHz and 39 %, and the time is the same.  With every fetch a hit in the L2 it would be 250 us.
 template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB>
 __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int32_t blocks)
 {
@@ -165,7 +168,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
 // summed at the end, in the order of their numbers.  Columns contiguous in memory: lane l takes R = 16 / sizeof(T) columns from
 // R (l % 16) on, of the R rows of the contraction from R (l / 16) on: an R x R square, whose transpose is, per column j of it, one
 // product's fragment: column j of every lane's square.  16-bit squares are turned by byte permutations of register pairs, fp32
-// ones by naming.
+// ones by naming.  Bound by the weights' bytes: 32 rows in about 25 of 64 networks 2048 x 1024, bf16: 24 us, 4.4 TB/s.
 constexpr int FEW_WAVES = 8;
 template <typename T>
 __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p)
@@ -247,7 +250,9 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p)
 // sizes, strides and alignment: a wavefront takes SMALL_ROWS rows of one network by itself, with the network's fragments in its
 // registers; nothing goes through the LDS and no wavefront waits for another.  Such calls are bound by their bytes, or rather by the
 // latency of one look-up, one fetch and one store per piece: what is under way at a time is what counts, so all of a piece is
-// asked for at once.
+// asked for at once.  Measured: 262,145 rows through an index, 4,096 networks 63 x 32 in fp32: 44 us, 3.0 TB/s (rows of 252 bytes touch
+// a third more lines than they fill); 524,291 rows, 64 x 64 in fp16, input gradient with a ReLU's mask: 68 us, 3.5 TB/s.  Pieces of 64
+// rows: 49 and 69, of 128: 70 and 90.
 constexpr int SMALL_ROWS = 32, SMALL_WAVES = 4;
 template <typename T> struct SmallFrag {
     static constexpr int W = 16 / sizeof(T), KS = 4 * W;

@@ -16,6 +16,10 @@ __host__ __device__ inline int64_t part_places(int64_t M, int64_t len) { return 
 // Tiles of BM x BN of a network's out(i, j) = sum over rows r of a(r, i) b(r, j): both operands column-wise, the contraction is the
 // rows, 128 bytes' worth a stage.  The columns' sums (gradient of the biases) are products with ones of the fragments that are
 // there anyway, in the workgroups of the first tile: SUM_B the columns of b, SUM_A those of a.
+// Measured: 32,768 rows through an index, 32 networks 1024 x 2048 in bf16: 231 us, 595 TFLOP/s.  The transposing read brings 8 bytes a
+// lane, so that fragments cost twice the reads of the forward product's, and the LDS bounds it (128 x 128 by four wavefronts of 64 x
+// 64: 230 against 219 on even networks; 256 x 128: 230; 128 x 256: 246).  64 x 64 tiles: 524,291 rows, 4,096 networks 64 x 64 in fp16: 34
+// us, 4.9 TB/s (47 with 128 x 128).
 enum { SUM_NONE, SUM_A, SUM_B };
 template <typename T, bool DIRECT, int BM, int BN, int WR, int WC>
 __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, int32_t sum, Parts parts)
@@ -142,7 +146,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
 // Layers of the small networks' kind whose rows are not whole pieces: a workgroup of four wavefronts per part and 64 x 16 V results; a
 // wavefront takes every fourth step of rows, straight into fragments, value by value (16 neighbouring lanes, 16 neighbouring values),
 // and the four are summed in the order of their numbers.  Nothing is staged and nothing waits until then: a part of a few
-// hundred rows is one chain of look-up, index, values, and the chains in flight are what counts.
+// hundred rows is one chain of look-up, index, values, and the chains in flight are what counts.  Measured: 684,936 rows of 126 bytes
+// through an index, 4,096 networks 63 x 3 in bf16: 75 us (103 with tiles staged in the LDS).
 constexpr int SMALL_WAVES = 4, SMALL_I = 64;
 template <typename T, int V>
 __global__ void __launch_bounds__(SMALL_WAVES * 64) k_reduce_small(KnProduct p, int32_t sum, Parts parts)
