@@ -418,6 +418,8 @@ template <typename T> int launch_few(hipStream_t st, const KnProduct &p)
 //   16,384, 64, 2048, 1024                                      126         113         127
 //   4,096, 8, 1024, 2048                              77         32          32          29
 //   65,536, 64, 2048, 1024                                      381         328         318
+//   20,306, 23, 64, 1472                                         29          26          31
+//   65,536, 64, 256, 1024                                       112          98         100
 // and with the contraction contiguous, 32 x 64 in four stages against 64 x 128: 24 to 32, 10 to 13, 61 to 68, 120 to 92.
 template <typename T, bool COLS> int launch_pieces(hipStream_t st, const KnProduct &p)
 {
@@ -431,7 +433,7 @@ template <typename T, bool COLS> int launch_pieces(hipStream_t st, const KnProdu
     } else {
         if (little || each < 64) return launch_rows<T, COLS, true, 32, 64, 1, 4, 4>(st, p);
     }
-    if (each >= 384 && tiles(192) >= 256) return launch_rows<T, COLS, true, 192, 128, 2, 2, 2>(st, p);
+    if (each >= 384 && tiles(192) >= 256 && p.C * (int64_t)sizeof(T) >= 1024) return launch_rows<T, COLS, true, 192, 128, 2, 2, 2>(st, p);
     if (each >= 192 && tiles(128) >= 512) return launch_rows<T, COLS, true, 128, 128, 2, 4, 2>(st, p);
     return launch_rows<T, COLS, true, 64, 128, 1, 4, 2>(st, p);
 }
