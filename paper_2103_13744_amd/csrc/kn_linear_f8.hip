@@ -292,12 +292,15 @@ extern "C" int kn_grouped_linear_f8(void *stream, const kn_linear_desc *d, const
         return KN_E_INVALID_ARG;
     F8Args p = {(const uint8_t *)xq, (const uint8_t *)wq, xs, ws, bias, y, offsets, rows, (int32_t)d->rows, d->experts, d->n_out,
                 (int32_t)kn_div_up(d->n_in, F8_BLOCK), (int32_t)d->x_rows, relu != 0};
+    // Which tile (us): 7,794 rows, 7 networks 2048 x 64: 32 x 128 12, 64 x 128 15, 192 x 128 29; 2,048 rows, 32 networks 2560 x 2048: 53, 53, 69;
+    // 8,192 rows, 16 networks 2048 x 2048: 88, 69, 69; 32,768 of them: 304, 237, 200.
     const int64_t each = p.M / p.E; // rows of a network, on average
+    auto tiles = [&](int64_t bm) { return kn_div_up(p.M, bm) * kn_div_up(p.N, 128); };
     return kn_with_type(d->dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
         hipStream_t st = (hipStream_t)stream;
-        if (each >= 512) return launch_f8<E_, 192, 128, 2, 2, 2>(st, p);
-        if (each >= 32) return launch_f8<E_, 64, 128, 1, 4, 2>(st, p);
+        if (each >= 512 && tiles(192) >= 256) return launch_f8<E_, 192, 128, 2, 2, 2>(st, p);
+        if (each >= 32 && tiles(64) >= 128) return launch_f8<E_, 64, 128, 1, 4, 2>(st, p);
         return launch_f8<E_, 32, 128, 1, 4, 2>(st, p);
     });
 }
