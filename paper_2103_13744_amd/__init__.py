@@ -567,7 +567,7 @@ def grouped_linear_dw(dy, x, w, offsets, rows=None, want_bias=True):
     dw = torch.empty_like(w)  # (keeps the layout of dense weights)
     db = x.new_empty((d.experts, d.n_out)) if want_bias else None
     need, ws = C.c_int64(), None
-    if M > 512:  # (fewer rows need no workspace)
+    if M > 128:  # (fewer rows need no workspace)
         _check(L.kn_grouped_linear_dw_workspace_bytes(C.byref(d), C.byref(need)), "kn_grouped_linear_dw_workspace_bytes")
         ws = torch.empty(need.value, dtype=torch.uint8, device=x.device) if need.value else None
     _check(L.kn_grouped_linear_dw(_stream(), C.byref(d), px, _ptr(dy, x.dtype, shape=(M, d.n_out)), _ptr(offsets, torch.int32, shape=(d.experts + 1,)),

@@ -143,21 +143,21 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
     }
 }
 
-// Layers of the small networks' kind whose rows are not whole pieces: a workgroup of four wavefronts per part and 64 x 16 V results; a
+// Layers of the small networks' kind whose rows are not whole pieces: a workgroup of four wavefronts per part and 16 U x 16 V results; a
 // wavefront takes every fourth step of rows, straight into fragments, value by value (16 neighbouring lanes, 16 neighbouring values),
 // and the four are summed in the order of their numbers.  Nothing is staged and nothing waits until then: a part of a few
 // hundred rows is one chain of look-up, index, values, and the chains in flight are what counts.  Measured: 684,936 rows of 126 bytes
 // through an index, 4,096 networks 63 x 3 in bf16: 75 us (103 with tiles staged in the LDS).
-constexpr int SMALL_WAVES = 4, SMALL_I = 64;
-template <typename T, int V>
+constexpr int SMALL_WAVES = 4;
+template <typename T, int U, int V>
 __global__ void __launch_bounds__(SMALL_WAVES * 64) k_reduce_small(KnProduct p, int32_t sum, Parts parts)
 {
-    constexpr int W = 16 / sizeof(T), RS = 4 * W, U = SMALL_I / 16, BN = 16 * V, LD = BN + 4;
+    constexpr int W = 16 / sizeof(T), RS = 4 * W, BM = 16 * U, BN = 16 * V, LD = BN + 4;
     typedef typename KnFrag<T>::Type Frag;
-    __shared__ __align__(16) float red[SMALL_I * LD];
-    __shared__ float side_a[SMALL_I], side_b[BN];
+    __shared__ __align__(16) float red[BM * LD];
+    __shared__ float side_a[BM], side_b[BN];
     const int tid = kn_thread(), lane = tid & 63, col = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int jtiles = (p.J + BN - 1) / BN, itiles = (p.I + SMALL_I - 1) / SMALL_I, tiles = itiles * jtiles;
+    const int jtiles = (p.J + BN - 1) / BN, itiles = (p.I + BM - 1) / BM, tiles = itiles * jtiles;
     const int number = kn_block() % tiles;
     const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, parts.len, kn_block() / tiles);
     const int32_t group = piece.group;
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_reduce_small(KnProduct p, 
     if (c0 >= cend && c0 != o) return; // (the first part of a network without rows writes zeros)
     const bool several = piece.end - o > parts.len;
     const int64_t place = 2 * (o / parts.len) + (c0 - o) / parts.len;
-    const int j0 = number % jtiles * BN, i0 = number / jtiles * SMALL_I;
+    const int j0 = number % jtiles * BN, i0 = number / jtiles * BM;
     const bool sum_a = sum == SUM_A && j0 == 0, sum_b = sum == SUM_B && i0 == 0;
     int32_t ai[U], bj[V];
 #pragma unroll
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_reduce_small(KnProduct p, 
         }
         __syncthreads();
     }
-    const int32_t in = min(p.I - i0, SMALL_I), jn = min(p.J - j0, BN);
+    const int32_t in = min(p.I - i0, BM), jn = min(p.J - j0, BN);
     float *sums = parts.sums + place * p.I * p.J;
     T *out = (T *)p.out + (int64_t)group * p.o_group;
     for (int q = tid; q < in * jn; q += SMALL_WAVES * 64) {
@@ -242,15 +242,14 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_reduce_small(KnProduct p, 
     }
 }
 
-// The parts' sums of the networks that have several, in the order of the parts; JOIN results per workgroup.  SEARCH: there are at most
+// The parts' sums of the networks that have several, in the order of the parts; `chunk` results per workgroup.  SEARCH: there are at most
 // M / len such networks, and a workgroup looks for its own among all (few networks of many results); else there is one for
 // every network's results, and most find nothing to do.
-constexpr int JOIN = 4096;
-template <typename T, bool SEARCH> __global__ void __launch_bounds__(256) k_reduce_join(KnProduct p, int32_t sum, Parts parts)
+template <typename T, bool SEARCH> __global__ void __launch_bounds__(256) k_reduce_join(KnProduct p, int32_t sum, Parts parts, int32_t chunk)
 {
     __shared__ int32_t scratch[4], found;
     const int64_t n = (int64_t)p.I * p.J;
-    const int32_t pieces = (int32_t)((n + JOIN - 1) / JOIN), turn = kn_block() / pieces;
+    const int32_t pieces = (int32_t)((n + chunk - 1) / chunk), turn = kn_block() / pieces;
     int32_t group = turn;
     if constexpr (SEARCH) {
         int32_t before = 0;
@@ -270,10 +269,11 @@ template <typename T, bool SEARCH> __global__ void __launch_bounds__(256) k_redu
     const int32_t o = kn_offset(p.offsets, group, p.M), rows = kn_offset(p.offsets, group + 1, p.M) - o;
     if (rows <= parts.len) return;
     const int32_t count = (rows + parts.len - 1) / parts.len;
-    const int64_t place = 2 * (o / parts.len), first = (int64_t)(kn_block() % pieces) * JOIN;
+    const int64_t place = 2 * (o / parts.len), first = (int64_t)(kn_block() % pieces) * chunk;
     T *out = (T *)p.out + (int64_t)group * p.o_group;
-    for (int64_t q = first + kn_thread(); q < min(n, first + JOIN); q += 256) {
+    for (int64_t q = first + kn_thread(); q < min(n, first + chunk); q += 256) {
         float y = 0.0f;
+#pragma unroll 4
         for (int c = 0; c < count; ++c) y += parts.sums[(place + c) * n + q];
         out[q] = (T)y; // (out's rows follow one another)
     }
@@ -299,33 +299,49 @@ bool narrow(const kn_linear_desc *d) { return d->n_in <= 128 && d->n_out <= 128;
 
 // Rows of a part: a part more is a tile written and read again in fp32, so that there are only as many as keep the chip busy (wide
 // layers: 32 networks 1024 x 2048, the longest of 32,768 rows 5,741: parts of 1,024 rows 357 us, of 4,096 264, of 8,192 238, none
-// 231; 8 networks 512 x 512, the longest 23,284: 135, 89, 126, 299).
+// 231; 8 networks 512 x 512, the longest 23,284: 135, 89, 126, 299).  Narrow layers' parts are small, and more of them are chains that
+// run at the same time.
 int32_t part_length(const kn_linear_desc *d)
 {
     const int64_t tiles = narrow(d) ? 1 : kn_div_up(d->n_in, 128) * kn_div_up(d->n_out, 128);
-    const int64_t len = kn_div_up(d->rows, kn_div_up(narrow(d) ? 1024 : 512, tiles)), least = narrow(d) ? 512 : 2048;
+    const int64_t len = kn_div_up(d->rows, kn_div_up(narrow(d) ? 1024 : 512, tiles)), least = narrow(d) ? 128 : 2048;
     return (int32_t)kn_align_up(len < least ? least : len, 64);
 }
 
 template <typename T, bool DIRECT> int launch_reduce(hipStream_t st, const kn_linear_desc *d, const KnProduct &p, int32_t sum, const Parts &parts)
 {
     const Way way = way_of(d, DIRECT);
-    const int bn = way == WAY_64 ? 64 : way == WAY_128 ? 128 : p.J <= 16 ? 16 : p.J <= 32 ? 32 : 64, bm = way == WAY_128 ? 128 : 64;
+    const int bm = way == WAY_128 ? 128 : way == WAY_SMALL && p.I <= 32 ? 32 : 64;
+    const int bn = way == WAY_128 ? 128 : way == WAY_64 || p.J > 48 ? 64 : p.J > 32 ? 48 : p.J > 16 ? 32 : 16;
     const int64_t blocks = kn_pieces(p.M, p.E, parts.len) * kn_div_up(p.I, bm) * kn_div_up(p.J, bn);
     if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
     const dim3 grid((unsigned)blocks);
     if (way == WAY_128) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 128, 128, 2, 4>), grid, dim3(512), 0, st, p, sum, parts);
     else if (way == WAY_64) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 64, 64, 2, 2>), grid, dim3(256), 0, st, p, sum, parts);
-    else if (bn == 16) hipLaunchKernelGGL((k_reduce_small<T, 1>), grid, dim3(SMALL_WAVES * 64), 0, st, p, sum, parts);
-    else if (bn == 32) hipLaunchKernelGGL((k_reduce_small<T, 2>), grid, dim3(SMALL_WAVES * 64), 0, st, p, sum, parts);
-    else hipLaunchKernelGGL((k_reduce_small<T, 4>), grid, dim3(SMALL_WAVES * 64), 0, st, p, sum, parts);
+    else if constexpr (!DIRECT) {
+#define KN_SMALL(U, V) hipLaunchKernelGGL((k_reduce_small<T, U, V>), grid, dim3(SMALL_WAVES * 64), 0, st, p, sum, parts)
+        if (bm == 32) {
+            if (bn == 16) KN_SMALL(2, 1);
+            else if (bn == 32) KN_SMALL(2, 2);
+            else if (bn == 48) KN_SMALL(2, 3);
+            else KN_SMALL(2, 4);
+        } else {
+            if (bn == 16) KN_SMALL(4, 1);
+            else if (bn == 32) KN_SMALL(4, 2);
+            else if (bn == 48) KN_SMALL(4, 3);
+            else KN_SMALL(4, 4);
+        }
+#undef KN_SMALL
+    }
     KN_CHECK_LAUNCH();
     if (p.M <= parts.len) return KN_OK; // (no network has several)
-    const int64_t most = p.M / parts.len, pieces = kn_div_up((int64_t)p.I * p.J, JOIN);
+    const int64_t most = p.M / parts.len, results = (int64_t)p.I * p.J;
+    const int32_t chunk = results * (most < p.E ? most : p.E) <= 1 << 20 ? 1024 : 4096; // (few results: more workgroups)
+    const int64_t pieces = kn_div_up(results, chunk);
     const bool search = most < p.E && p.E * pieces > 8192;
     const int64_t joins = (search ? most : p.E) * pieces;
     if (joins > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL(search ? (k_reduce_join<T, true>) : (k_reduce_join<T, false>), dim3((unsigned)joins), dim3(256), 0, st, p, sum, parts);
+    hipLaunchKernelGGL(search ? (k_reduce_join<T, true>) : (k_reduce_join<T, false>), dim3((unsigned)joins), dim3(256), 0, st, p, sum, parts, chunk);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }
