@@ -77,11 +77,15 @@ static inline int64_t kn_pieces(int64_t M, int64_t E, int64_t len) { return M / 
 // of 32; results: column l % 16, rows 4 (l / 16) .. + 3.
 __device__ __forceinline__ kn_f32x4 kn_mfma(kn_f16x8 a, kn_f16x8 b, kn_f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ kn_f32x4 kn_mfma(kn_bf16x8 a, kn_bf16x8 b, kn_f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-// the same for 4 values a lane of fp32: four products over 4 each, contraction 4 (l / 16) + j in the order j = 0 .. 3
+// the same for 4 values a lane of fp32: four products over 4 each, contraction 4 (l / 16) + j in the order j = 0 .. 3.  The 16 terms
+// are summed by themselves and then added: a long sum rounds at its own size once per 16 terms.
 __device__ __forceinline__ kn_f32x4 kn_mfma(kn_f32x4 a, kn_f32x4 b, kn_f32x4 c)
 {
+    kn_f32x4 sum = {0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+    for (int j = 0; j < 4; ++j) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], sum, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] += sum[j];
     return c;
 }
 
