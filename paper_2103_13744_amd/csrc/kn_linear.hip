@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
     }
 }
 
-// A row or none per network: the weights are read once, straight into the registers they are multiplied from, 16 bytes a lane and load.
+// A row or none per network, or few rows of fp32: the weights are read once, straight into the registers they are multiplied from, 16 bytes a lane and load.
 // A workgroup makes 16 rows of FEW_COLS results; its FEW_WAVES wavefronts take every FEW_WAVES-th step of the contraction and are
 // summed at the end, in the order of their numbers.  Columns contiguous in memory: lane l takes R = 16 / sizeof(T) columns from
 // R (l % 16) on, of the R rows of the contraction from R (l / 16) on: an R x R square, whose transpose is, per column j of it, one
@@ -421,21 +421,42 @@ template <typename T> int launch_few(hipStream_t st, const KnProduct &p)
 //   20,306, 23, 64, 1472                                         29          26          31
 //   65,536, 64, 256, 1024                                       112          98         100
 // and with the contraction contiguous, 32 x 64 in four stages against 64 x 128: 24 to 32, 10 to 13, 61 to 68, 120 to 92.
+// fp32 is bound by the matrix cores, a sixteenth as fast: rows that a tile does not have cost more than what it fetches twice.
+//   rows, networks, K, N                           few    32 x 64    32 x 128    64 x 128   128 x 128
+//   266, 37, 1584, 1280, columns contiguous         66                  71         117         120
+//   1,024, 8, 1024, 1024                            30                  45          47          78
+//   2,048, 64, 512, 512                             26                  34          43          44
+//   8,192, 64, 512, 512                                                 60          65          78
+//   32,768, 8, 512, 1024                                               339         306         317
+//   2,048, 64, 512, 512, contraction contiguous                22       33          41          42
+//   8,192, 16, 1024, 1024                                     180      167         177         209
 template <typename T, bool COLS> int launch_pieces(hipStream_t st, const KnProduct &p)
 {
     const int64_t each = p.M / p.E; // rows of a network, on average
     auto tiles = [&](int64_t bm) { return (p.M + bm - 1) / bm * ((p.J + 127) / 128); };
-    if (!rows_of_pieces<T, COLS>(p))
-        return each >= 64 && tiles(128) >= 256 ? launch_rows<T, COLS, false, 128, 128, 2, 4, 2>(st, p) : launch_rows<T, COLS, false, 32, 128, 1, 4, 2>(st, p);
-    const bool little = (int64_t)p.M * p.J <= 1 << 19;
-    if constexpr (COLS) {
-        if (little && (each < 2 || (int64_t)p.E * p.C * p.J <= 1 << 25)) return launch_few<T>(st, p);
+    if constexpr (sizeof(T) == 4) {
+        const bool narrow = (int64_t)p.M * p.J <= 1 << 20; // (too few tiles of 32 x 128 for the chip)
+        if (!rows_of_pieces<T, COLS>(p))
+            return each < 512 ? launch_rows<T, COLS, false, 32, 128, 1, 4, 2>(st, p) : launch_rows<T, COLS, false, 64, 128, 1, 4, 2>(st, p);
+        if constexpr (COLS) {
+            if (narrow) return launch_few<T>(st, p);
+            return each < 512 ? launch_rows<T, COLS, true, 32, 128, 1, 4, 2>(st, p) : launch_rows<T, COLS, true, 64, 128, 1, 4, 2>(st, p);
+        } else {
+            return narrow ? launch_rows<T, COLS, true, 32, 64, 1, 4, 4>(st, p) : launch_rows<T, COLS, true, 32, 128, 1, 4, 2>(st, p);
+        }
     } else {
-        if (little || each < 64) return launch_rows<T, COLS, true, 32, 64, 1, 4, 4>(st, p);
+        if (!rows_of_pieces<T, COLS>(p))
+            return each >= 64 && tiles(128) >= 256 ? launch_rows<T, COLS, false, 128, 128, 2, 4, 2>(st, p) : launch_rows<T, COLS, false, 32, 128, 1, 4, 2>(st, p);
+        const bool little = (int64_t)p.M * p.J <= 1 << 19;
+        if constexpr (COLS) {
+            if (little && (each < 2 || (int64_t)p.E * p.C * p.J <= 1 << 25)) return launch_few<T>(st, p);
+        } else {
+            if (little || each < 64) return launch_rows<T, COLS, true, 32, 64, 1, 4, 4>(st, p);
+        }
+        if (each >= 384 && tiles(192) >= 256 && p.C * (int64_t)sizeof(T) >= 1024) return launch_rows<T, COLS, true, 192, 128, 2, 2, 2>(st, p);
+        if (each >= 192 && tiles(128) >= 512) return launch_rows<T, COLS, true, 128, 128, 2, 4, 2>(st, p);
+        return launch_rows<T, COLS, true, 64, 128, 1, 4, 2>(st, p);
     }
-    if (each >= 384 && tiles(192) >= 256 && p.C * (int64_t)sizeof(T) >= 1024) return launch_rows<T, COLS, true, 192, 128, 2, 2, 2>(st, p);
-    if (each >= 192 && tiles(128) >= 512) return launch_rows<T, COLS, true, 128, 128, 2, 4, 2>(st, p);
-    return launch_rows<T, COLS, true, 64, 128, 1, 4, 2>(st, p);
 }
 
 template <typename T, bool COLS, int KF, int V> int launch_small(hipStream_t st, const KnProduct &p)
