@@ -287,24 +287,29 @@ template <typename T, bool SEARCH> __global__ void __launch_bounds__(256) k_redu
 }
 
 // Layers of up to 128 x 128 whose rows are not whole pieces are k_reduce_small's.  Else tiles of 64 x 64 where 128 x 128 would be few,
-// or layers are no wider than that (four times as many workgroups at a time: such a tile's few rows are latency).
+// or layers are no wider than that (four times as many workgroups at a time: such a tile's few rows are latency), and in fp32, which the
+// matrix cores bound: what a tile fetches is no matter, how evenly tiles fill the chip is (8,192 rows, 16 networks 1024 x 1024, the
+// longest 2,892: 64 x 64 189 us, 128 x 128 226; 128 networks 512 x 512, the longest 568: 88, 99).
 enum Way { WAY_SMALL, WAY_64, WAY_128 };
 Way way_of(const kn_linear_desc *d, bool direct)
 {
     if (!direct && d->n_in <= 128 && d->n_out <= 128) return WAY_SMALL;
-    if (d->n_in <= 64 && d->n_out <= 64) return WAY_64;
+    if (d->dtype == KN_F32 || (d->n_in <= 64 && d->n_out <= 64)) return WAY_64;
     return d->experts * kn_div_up(d->n_in, 128) * kn_div_up(d->n_out, 128) < 256 && d->rows < 65536 ? WAY_64 : WAY_128;
 }
 bool narrow(const kn_linear_desc *d) { return d->n_in <= 128 && d->n_out <= 128; }
 
-// Rows of a part: a part more is a tile written and read again in fp32, so that there are only as many as keep the chip busy (wide
+// Rows of a part: a part more is a tile written and read again in fp32, so that there are only as many as keep the chip busy.  Wide
 // layers: 32 networks 1024 x 2048, the longest of 32,768 rows 5,741: parts of 1,024 rows 357 us, of 4,096 264, of 8,192 238, none
-// 231; 8 networks 512 x 512, the longest 23,284: 135, 89, 126, 299).  Narrow layers' parts are small, and more of them are chains that
-// run at the same time.
+// 231; 8 networks 512 x 512, the longest 23,284: of 1,024 97, of 2,048 80, none 261; 4 networks 256 x 256, the longest of 16,384
+// 11,740: of 256 31, of 1,024 23, of 2,048 33.  In fp32, where a tile takes longest and its sums are the less: of 512 51, of 2,048 71.
+// Narrow layers' parts are small, and more of them are chains that run at the same time.
 int32_t part_length(const kn_linear_desc *d)
 {
+    const bool whole = d->dtype == KN_F32;
     const int64_t tiles = narrow(d) ? 1 : kn_div_up(d->n_in, 128) * kn_div_up(d->n_out, 128);
-    const int64_t len = kn_div_up(d->rows, kn_div_up(narrow(d) ? 1024 : 512, tiles)), least = narrow(d) ? 128 : 2048;
+    const int64_t len = kn_div_up(d->rows, kn_div_up(narrow(d) ? 1024 : whole ? 256 : 512, tiles));
+    const int64_t least = narrow(d) ? 128 : whole ? 512 : tiles <= 8 ? 1024 : 2048;
     return (int32_t)kn_align_up(len < least ? least : len, 64);
 }
 
