@@ -299,8 +299,8 @@ Way way_of(const kn_linear_desc *d, bool direct)
 }
 bool narrow(const kn_linear_desc *d) { return d->n_in <= 128 && d->n_out <= 128; }
 
-// Rows of a part: a part more is a tile written and read again in fp32, so that there are only as many as keep the chip busy.  Wide
-// layers: 32 networks 1024 x 2048, the longest of 32,768 rows 5,741: parts of 1,024 rows 357 us, of 4,096 264, of 8,192 238, none
+// Rows of a part: a part more is a tile written and read again in fp32, so that there are only as many as keep the chip busy, and
+// up to 1,024 rows of a wide layer are one (the join is a launch more, 4 us).  Wide layers: 32 networks 1024 x 2048, the longest of 32,768 rows 5,741: parts of 1,024 rows 357 us, of 4,096 264, of 8,192 238, none
 // 231; 8 networks 512 x 512, the longest 23,284: of 1,024 97, of 2,048 80, none 261; 4 networks 256 x 256, the longest of 16,384
 // 11,740: of 256 31, of 1,024 23, of 2,048 33.  In fp32, where a tile takes longest and its sums are the less: of 512 51, of 2,048 71.
 // Narrow layers' parts are small, and more of them are chains that run at the same time.
@@ -309,7 +309,7 @@ int32_t part_length(const kn_linear_desc *d)
     const bool whole = d->dtype == KN_F32;
     const int64_t tiles = narrow(d) ? 1 : kn_div_up(d->n_in, 128) * kn_div_up(d->n_out, 128);
     const int64_t len = kn_div_up(d->rows, kn_div_up(narrow(d) ? 1024 : whole ? 256 : 512, tiles));
-    const int64_t least = narrow(d) ? 128 : whole ? 512 : tiles <= 8 ? 1024 : 2048;
+    const int64_t least = narrow(d) ? 128 : whole && d->rows > 1024 ? 512 : tiles <= 8 ? 1024 : 2048;
     return (int32_t)kn_align_up(len < least ? least : len, 64);
 }
 
