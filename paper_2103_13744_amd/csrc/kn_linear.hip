@@ -437,7 +437,7 @@ template <typename T, bool COLS> int launch_pieces(hipStream_t st, const KnProdu
     if constexpr (sizeof(T) == 4) {
         const bool narrow = (int64_t)p.M * p.J <= 1 << 20; // (too few tiles of 32 x 128 for the chip)
         if (!rows_of_pieces<T, COLS>(p))
-            return each < 512 ? launch_rows<T, COLS, false, 32, 128, 1, 4, 2>(st, p) : launch_rows<T, COLS, false, 64, 128, 1, 4, 2>(st, p);
+            return narrow ? launch_rows<T, COLS, false, 32, 64, 1, 4, 2>(st, p) : each < 512 ? launch_rows<T, COLS, false, 32, 128, 1, 4, 2>(st, p) : launch_rows<T, COLS, false, 64, 128, 1, 4, 2>(st, p);
         if constexpr (COLS) {
             if (narrow) return launch_few<T>(st, p);
             return each < 512 ? launch_rows<T, COLS, true, 32, 128, 1, 4, 2>(st, p) : launch_rows<T, COLS, true, 64, 128, 1, 4, 2>(st, p);

@@ -289,12 +289,14 @@ template <typename T, bool SEARCH> __global__ void __launch_bounds__(256) k_redu
 // Layers of up to 128 x 128 whose rows are not whole pieces are k_reduce_small's.  Else tiles of 64 x 64 where 128 x 128 would be few,
 // or layers are no wider than that (four times as many workgroups at a time: such a tile's few rows are latency), and in fp32, which the
 // matrix cores bound: what a tile fetches is no matter, how evenly tiles fill the chip is (8,192 rows, 16 networks 1024 x 1024, the
-// longest 2,892: 64 x 64 189 us, 128 x 128 226; 128 networks 512 x 512, the longest 568: 88, 99).
-enum Way { WAY_SMALL, WAY_64, WAY_128 };
+// longest 2,892: 64 x 64 189 us, 128 x 128 226; 128 networks 512 x 512, the longest 568: 88, 99);
+// and 32 x 32 where 64 x 64 would be few (1,001 rows, 5 networks 259 x 131: 9.6 us, 64 x 64 14.6).
+enum Way { WAY_SMALL, WAY_32, WAY_64, WAY_128 };
 Way way_of(const kn_linear_desc *d, bool direct)
 {
     if (!direct && d->n_in <= 128 && d->n_out <= 128) return WAY_SMALL;
-    if (d->dtype == KN_F32 || (d->n_in <= 64 && d->n_out <= 64)) return WAY_64;
+    if (d->dtype == KN_F32) return (d->experts + d->rows / 512) * kn_div_up(d->n_in, 64) * kn_div_up(d->n_out, 64) < 256 ? WAY_32 : WAY_64;
+    if (d->n_in <= 64 && d->n_out <= 64) return WAY_64;
     return d->experts * kn_div_up(d->n_in, 128) * kn_div_up(d->n_out, 128) < 256 && d->rows < 65536 ? WAY_64 : WAY_128;
 }
 bool narrow(const kn_linear_desc *d) { return d->n_in <= 128 && d->n_out <= 128; }
@@ -316,14 +318,17 @@ int32_t part_length(const kn_linear_desc *d)
 template <typename T, bool DIRECT> int launch_reduce(hipStream_t st, const kn_linear_desc *d, const KnProduct &p, int32_t sum, const Parts &parts)
 {
     const Way way = way_of(d, DIRECT);
-    const int bm = way == WAY_128 ? 128 : way == WAY_SMALL && p.I <= 32 ? 32 : 64;
-    const int bn = way == WAY_128 ? 128 : way == WAY_64 || p.J > 48 ? 64 : p.J > 32 ? 48 : p.J > 16 ? 32 : 16;
+    const int bm = way == WAY_128 ? 128 : way == WAY_32 || (way == WAY_SMALL && p.I <= 32) ? 32 : 64;
+    const int bn = way == WAY_128 ? 128 : way == WAY_32 ? 32 : way == WAY_64 || p.J > 48 ? 64 : p.J > 32 ? 48 : p.J > 16 ? 32 : 16;
     const int64_t blocks = kn_pieces(p.M, p.E, parts.len) * kn_div_up(p.I, bm) * kn_div_up(p.J, bn);
     if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
     const dim3 grid((unsigned)blocks);
-    if (way == WAY_128) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 128, 128, 2, 4>), grid, dim3(512), 0, st, p, sum, parts);
-    else if (way == WAY_64) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 64, 64, 2, 2>), grid, dim3(256), 0, st, p, sum, parts);
-    else if constexpr (!DIRECT) {
+    if (way == WAY_128) {
+        if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 128, 128, 2, 4>), grid, dim3(512), 0, st, p, sum, parts);
+    } else if (way == WAY_64) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 64, 64, 2, 2>), grid, dim3(256), 0, st, p, sum, parts);
+    else if (way == WAY_32) {
+        if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 32, 32, 2, 2>), grid, dim3(256), 0, st, p, sum, parts);
+    } else if constexpr (!DIRECT) {
 #define KN_SMALL(U, V) hipLaunchKernelGGL((k_reduce_small<T, U, V>), grid, dim3(SMALL_WAVES * 64), 0, st, p, sum, parts)
         if (bm == 32) {
             if (bn == 16) KN_SMALL(2, 1);

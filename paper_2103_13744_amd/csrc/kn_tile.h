@@ -34,7 +34,7 @@ __device__ __forceinline__ int kn_row_byte(int r, int piece) { return r * 128 + 
 // 32 bytes of each (rows of 128 bytes lie two to a line of the banks); fp32 fragments rows 4 g of four g, 64 bytes of each
 template <typename T, int W> __device__ __forceinline__ int kn_col_swizzle(int c)
 {
-    if constexpr (sizeof(T) == 4) return (c >> 2 & 3) << 2;
+    if constexpr (sizeof(T) == 4) return (c >> 2 & (W == 32 ? 1 : 3)) << 2;
     else if constexpr (W == 64) return ((c >> 1 & 1) | (c >> 3 & 1) << 1) << 1;
     else return ((c & 3) | (c >> 3 & 1) << 2) << 1;
 }
