@@ -251,8 +251,8 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p)
 // registers; nothing goes through the LDS and no wavefront waits for another.  Such calls are bound by their bytes, or rather by the
 // latency of one look-up, one fetch and one store per piece: what is under way at a time is what counts, so all of a piece is
 // asked for at once.  Measured: 262,145 rows through an index, 4,096 networks 63 x 32 in fp32: 44 us, 3.0 TB/s (rows of 252 bytes touch
-// a third more lines than they fill); 524,291 rows, 64 x 64 in fp16, input gradient with a ReLU's mask: 68 us, 3.5 TB/s.  Pieces of 64
-// rows: 49 and 69, of 128: 70 and 90.
+// a third more lines than they fill); 524,291 rows, 64 x 64 in fp16, input gradient with a ReLU's mask: 59 us, 4.0 TB/s (68 where a
+// lane stores and masks 8 bytes at a time).  Pieces of 64 rows: 49 and 69, of 128: 70 and 90, of 16: 52 and 85.
 constexpr int SMALL_ROWS = 32, SMALL_WAVES = 4;
 template <typename T> struct SmallFrag {
     static constexpr int W = 16 / sizeof(T), KS = 4 * W;
@@ -261,8 +261,10 @@ template <typename T, bool COLS, int KF, int V>
 __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p, int32_t pieces)
 {
     constexpr int W = SmallFrag<T>::W, KS = SmallFrag<T>::KS, SUBS = SMALL_ROWS / 16;
+    // A lane's four results of W / 4 products are neighbours, W of them: the products' columns are dealt out in fours
+    constexpr int PAIR = W / 4, RUNS = V / PAIR;
     typedef typename KnFrag<T>::Type Frag;
-    typedef T Four __attribute__((ext_vector_type(4), aligned(sizeof(T)))); // wherever they lie
+    typedef T Run __attribute__((ext_vector_type(W), aligned(sizeof(T)))); // wherever they lie
     __shared__ __align__(16) T rows_of[SMALL_WAVES][16 * 16 * V + W]; // 16 rows of results of a wavefront, as they follow one another
     const int lane = kn_thread() & 63, col = lane & 15, g = lane >> 4;
     T *line = rows_of[kn_thread() >> 6];
@@ -290,7 +292,8 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
         for (int k = 0; k < KF; ++k)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int32_t c = k * KS + g * W, j = min(j0 + 16 * v + col, p.J - 1);
+                const int32_t c = k * KS + g * W;
+                const int32_t j = min(j0 + v / PAIR * (16 * PAIR) + (col >> 2) * W + v % PAIR * 4 + (col & 3), p.J - 1);
                 if constexpr (COLS) {
 #pragma unroll
                     for (int q = 0; q < W; ++q) {
@@ -306,29 +309,29 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
 #pragma unroll
             for (int k = 0; k < KF; ++k) fa[s][k] = kn_any_piece<T>(arow[s], k * KS + g * W, C);
     }
-    const bool together = p.J % 4 != 0 && ntiles == 1; // rows that follow one another without fours of their own: stored as one line
-    // four neighbours j .. j + 3 of a row of J (behind its end: the last one, unused)
-    auto four = [&](const T *row, int32_t j) {
-        Four f;
-        if (j + 4 <= p.J) f = *(const Four *)(row + j);
+    const bool together = p.J % W != 0 && ntiles == 1; // rows that follow one another without whole pieces of their own: stored as one line
+    // W neighbours j .. of a row of J (behind its end: the last one, unused)
+    auto run = [&](const T *row, int32_t j) {
+        Run f;
+        if (j + W <= p.J) f = *(const Run *)(row + j);
         else
 #pragma unroll
-            for (int r = 0; r < 4; ++r) f[r] = row[min(j + r, p.J - 1)];
+            for (int r = 0; r < W; ++r) f[r] = row[min(j + r, p.J - 1)];
         return f;
     };
     const T *bias = (const T *)p.bias, *mask = (const T *)p.mask;
-    Four add[V], m[SUBS][V]; // (a lane's columns are j0 + 16 v + 4 g .. + 3)
+    Run add[RUNS], m[SUBS][RUNS]; // (a lane's columns are j0 + 4 W n + W g .. + W - 1)
 #pragma unroll
-    for (int v = 0; v < V; ++v) add[v] = some && bias ? four(bias + group * p.J, min(j0 + 16 * v + 4 * g, p.J - 1)) : Four{};
+    for (int n = 0; n < RUNS; ++n) add[n] = some && bias ? run(bias + group * p.J, min(j0 + 4 * W * n + W * g, p.J - 1)) : Run{};
     if (some && mask) { // (asked for before the first result is stored, not one after the other's)
 #pragma unroll
         for (int s = 0; s < SUBS; ++s) {
             const int32_t i = min(piece.begin + 16 * s + col, piece.end - 1), src = p.mask_rows ? p.mask_rows[i] : i;
             const bool in = (uint32_t)src < (uint32_t)p.m_rows;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                m[s][v] = Four{};
-                if (in) m[s][v] = four(mask + (int64_t)src * p.ldm, min(j0 + 16 * v + 4 * g, p.J - 1));
+            for (int n = 0; n < RUNS; ++n) {
+                m[s][n] = Run{};
+                if (in) m[s][n] = run(mask + (int64_t)src * p.ldm, min(j0 + 4 * W * n + W * g, p.J - 1));
             }
         }
     }
@@ -349,27 +352,27 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
         T *out = (T *)p.out + (int64_t)i * p.o_i, *first = (T *)p.out + (int64_t)(i - col) * p.o_i;
         const int shift = (int)((uintptr_t)first / sizeof(T) % W); // (of the first result in its 16 bytes)
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int32_t j = j0 + 16 * v + 4 * g;
+        for (int n = 0; n < RUNS; ++n) {
+            const int32_t j = j0 + 4 * W * n + W * g;
             if (j >= p.J || i >= piece.end) continue;
-            Four o;
+            Run o;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float y = acc[v][r];
-                if (some && bias) y += (float)add[v][r];
+            for (int r = 0; r < W; ++r) {
+                float y = acc[n * PAIR + r / 4][r % 4];
+                if (some && bias) y += (float)add[n][r];
                 if (p.relu) y = y > 0.0f || y != y ? y : 0.0f; // (a NaN stays one)
-                if (some && mask && !((float)m[s][v][r] > 0.0f)) y = 0.0f;
+                if (some && mask && !((float)m[s][n][r] > 0.0f)) y = 0.0f;
                 o[r] = (T)y;
             }
             if (together) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+                for (int r = 0; r < W; ++r)
                     if (j + r < p.J) line[shift + col * p.J + j + r] = o[r];
-            } else if (j + 4 <= p.J) {
-                *(Four *)(out + j) = o;
+            } else if (j + W <= p.J) {
+                *(Run *)(out + j) = o;
             } else {
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+                for (int r = 0; r < W; ++r)
                     if (j + r < p.J) out[j + r] = o[r];
             }
         }
