@@ -443,8 +443,10 @@ template <typename T, bool COLS> int launch_pieces(hipStream_t st, const KnProdu
             return narrow ? launch_rows<T, COLS, false, 32, 64, 1, 4, 2>(st, p) : each < 512 ? launch_rows<T, COLS, false, 32, 128, 1, 4, 2>(st, p) : launch_rows<T, COLS, false, 64, 128, 1, 4, 2>(st, p);
         if constexpr (COLS) {
             if (narrow) return launch_few<T>(st, p);
+            if (p.J <= 64) return launch_rows<T, COLS, true, 32, 64, 1, 4, 2>(st, p);
             return each < 512 ? launch_rows<T, COLS, true, 32, 128, 1, 4, 2>(st, p) : launch_rows<T, COLS, true, 64, 128, 1, 4, 2>(st, p);
         } else {
+            if (p.J <= 64 && !narrow) return launch_rows<T, COLS, true, 32, 64, 1, 4, 2>(st, p); // (two stages: more workgroups at a time)
             return narrow ? launch_rows<T, COLS, true, 32, 64, 1, 4, 4>(st, p) : launch_rows<T, COLS, true, 32, 128, 1, 4, 2>(st, p);
         }
     } else {
@@ -488,7 +490,10 @@ template <typename T, bool COLS> int launch_small_widths(hipStream_t st, const K
 template <typename T> int launch_forward(hipStream_t st, const KnProduct &p)
 {
     const bool cols = p.b_j == 1 && p.b_c != 1; // (one column of one input: either)
-    if (p.C <= SMALL_MOST && p.J <= SMALL_MOST) return cols ? launch_small_widths<T, true>(st, p) : launch_small_widths<T, false>(st, p);
+    // (us, small against tiles: 524,291 rows, 4,096 networks 64 x 64: 48 and 57 in bf16, 117 and 107 in fp32; 262,145 rows, 1,600 networks
+    // 128 x 128: 79 and 50, 206 and 129; 91 x 64, whose rows are not whole pieces: 43 and 71, 103 and 123)
+    const bool tiles = (cols ? rows_of_pieces<T, true>(p) : rows_of_pieces<T, false>(p)) && p.C * p.J > (sizeof(T) == 4 ? 4095 : 4096);
+    if (p.C <= SMALL_MOST && p.J <= SMALL_MOST && !tiles) return cols ? launch_small_widths<T, true>(st, p) : launch_small_widths<T, false>(st, p);
     return cols ? launch_pieces<T, true>(st, p) : launch_pieces<T, false>(st, p);
 }
 

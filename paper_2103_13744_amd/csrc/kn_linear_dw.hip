@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
     }
 }
 
-// Layers of the small networks' kind whose rows are not whole pieces: a workgroup of four wavefronts per part and 16 U x 16 V results; a
+// Layers of the small networks' kind whose rows are not whole pieces: a workgroup of four wavefronts per part, 16 U x 16 V results at most; a
 // wavefront takes every fourth step of rows, straight into fragments, value by value (16 neighbouring lanes, 16 neighbouring values),
 // and the four are summed in the order of their numbers.  Nothing is staged and nothing waits until then: a part of a few
 // hundred rows is one chain of look-up, index, values, and the chains in flight are what counts.  Measured: 684,936 rows of 126 bytes
@@ -157,22 +157,19 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_reduce_small(KnProduct p, 
     __shared__ __align__(16) float red[BM * LD];
     __shared__ float side_a[BM], side_b[BN];
     const int tid = kn_thread(), lane = tid & 63, col = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int jtiles = (p.J + BN - 1) / BN, itiles = (p.I + BM - 1) / BM, tiles = itiles * jtiles;
-    const int number = kn_block() % tiles;
-    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, parts.len, kn_block() / tiles);
+    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, parts.len, kn_block());
     const int32_t group = piece.group;
     if (group >= p.E) return;
     const int32_t o = kn_offset(p.offsets, group, p.M), c0 = piece.begin, cend = max(c0, min(piece.end, c0 + parts.len));
     if (c0 >= cend && c0 != o) return; // (the first part of a network without rows writes zeros)
     const bool several = piece.end - o > parts.len;
     const int64_t place = 2 * (o / parts.len) + (c0 - o) / parts.len;
-    const int j0 = number % jtiles * BN, i0 = number / jtiles * BM;
-    const bool sum_a = sum == SUM_A && j0 == 0, sum_b = sum == SUM_B && i0 == 0;
+    const bool sum_a = sum == SUM_A, sum_b = sum == SUM_B;
     int32_t ai[U], bj[V];
 #pragma unroll
-    for (int u = 0; u < U; ++u) ai[u] = min(i0 + 16 * u + col, p.I - 1);
+    for (int u = 0; u < U; ++u) ai[u] = min(16 * u + col, p.I - 1);
 #pragma unroll
-    for (int v = 0; v < V; ++v) bj[v] = min(j0 + 16 * v + col, p.J - 1);
+    for (int v = 0; v < V; ++v) bj[v] = min(16 * v + col, p.J - 1);
     kn_f32x4 acc[U][V] = {}, sa[U] = {}, sb[V] = {};
     Frag ones;
 #pragma unroll
@@ -225,20 +222,18 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_reduce_small(KnProduct p, 
         }
         __syncthreads();
     }
-    const int32_t in = min(p.I - i0, BM), jn = min(p.J - j0, BN);
     float *sums = parts.sums + place * p.I * p.J;
-    T *out = (T *)p.out + (int64_t)group * p.o_group;
-    for (int q = tid; q < in * jn; q += SMALL_WAVES * 64) {
-        const int i = q / jn, j = q % jn;
-        const int64_t at = (int64_t)(i0 + i) * p.J + j0 + j;
-        if (several) sums[at] = red[i * LD + j];
-        else out[at] = (T)red[i * LD + j];
+    T *out = (T *)p.out + (int64_t)group * p.o_group; // (its rows follow one another)
+    for (int q = tid; q < p.I * p.J; q += SMALL_WAVES * 64) {
+        const float y = red[q / p.J * LD + q % p.J];
+        if (several) sums[q] = y;
+        else out[q] = (T)y;
     }
-    const int n = sum_a ? in : sum_b ? jn : 0, first = sum_a ? i0 : j0, all = sum_a ? p.I : p.J;
+    const int n = sum_a ? p.I : sum_b ? p.J : 0;
     if (tid < n) {
         const float y = sum_a ? side_a[tid] : side_b[tid];
-        if (several) parts.bias_sums[place * all + first + tid] = y;
-        else ((T *)p.out_bias)[(int64_t)group * all + first + tid] = (T)y;
+        if (several) parts.bias_sums[place * n + tid] = y;
+        else ((T *)p.out_bias)[(int64_t)group * n + tid] = (T)y;
     }
 }
 
@@ -286,7 +281,8 @@ template <typename T, bool SEARCH> __global__ void __launch_bounds__(256) k_redu
     }
 }
 
-// Layers of up to 128 x 128 whose rows are not whole pieces are k_reduce_small's.  Else tiles of 64 x 64 where 128 x 128 would be few,
+// Layers of up to 64 x 64 whose rows are not whole pieces are k_reduce_small's (us, against 64 x 64 staged in the LDS: 524,291 rows, 4,096
+// networks 63 x 32: 57 and 63 in bf16, 91 and 123 in fp32; 262,145 rows, 1,600 networks 91 x 64: 109 and 75, 151 and 102).  Else tiles of 64 x 64 where 128 x 128 would be few,
 // or layers are no wider than that (four times as many workgroups at a time: such a tile's few rows are latency), and in fp32, which the
 // matrix cores bound: what a tile fetches is no matter, how evenly tiles fill the chip is (8,192 rows, 16 networks 1024 x 1024, the
 // longest 2,892: 64 x 64 189 us, 128 x 128 226; 128 networks 512 x 512, the longest 568: 88, 99);
@@ -294,7 +290,7 @@ template <typename T, bool SEARCH> __global__ void __launch_bounds__(256) k_redu
 enum Way { WAY_SMALL, WAY_32, WAY_64, WAY_128 };
 Way way_of(const kn_linear_desc *d, bool direct)
 {
-    if (!direct && d->n_in <= 128 && d->n_out <= 128) return WAY_SMALL;
+    if (!direct && d->n_in <= 64 && d->n_out <= 64) return WAY_SMALL;
     if (d->dtype == KN_F32) return (d->experts + d->rows / 512) * kn_div_up(d->n_in, 64) * kn_div_up(d->n_out, 64) < 256 ? WAY_32 : WAY_64;
     if (d->n_in <= 64 && d->n_out <= 64) return WAY_64;
     return d->experts * kn_div_up(d->n_in, 128) * kn_div_up(d->n_out, 128) < 256 && d->rows < 65536 ? WAY_64 : WAY_128;
