@@ -250,13 +250,33 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p)
 // sizes, strides and alignment: a wavefront takes SMALL_ROWS rows of one network by itself, with the network's fragments in its
 // registers; nothing goes through the LDS and no wavefront waits for another.  Such calls are bound by their bytes, or rather by the
 // latency of one look-up, one fetch and one store per piece: what is under way at a time is what counts, so all of a piece is
-// asked for at once.  Measured: 262,145 rows through an index, 4,096 networks 63 x 32 in fp32: 44 us, 3.0 TB/s (rows of 252 bytes touch
-// a third more lines than they fill); 524,291 rows, 64 x 64 in fp16, input gradient with a ReLU's mask: 59 us, 4.0 TB/s (68 where a
+// asked for at once.  Measured: 262,145 rows through an index, 4,096 networks 63 x 32 in fp32: 39 us, 3.4 TB/s (rows of 252 bytes touch
+// a third more lines than they fill; 44 us where each odd end is waited for); 524,291 rows, 64 x 64 in fp16, input gradient with a ReLU's mask: 59 us, 4.0 TB/s (68 where a
 // lane stores and masks 8 bytes at a time).  Pieces of 64 rows: 49 and 69, of 128: 70 and 90, of 16: 52 and 85.
 constexpr int SMALL_ROWS = 32, SMALL_WAVES = 4;
 template <typename T> struct SmallFrag {
     static constexpr int W = 16 / sizeof(T), KS = 4 * W;
 };
+// kn_any_piece in two parts, so that nothing waits for a fetch before all are under way: a piece that ends behind the row is fetched from
+// its last 16 bytes, and shifted to its place at the end.
+template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type small_ask(const T *row, int32_t k, int32_t C)
+{
+    constexpr int W = SmallFrag<T>::W;
+    if (C < W) return kn_any_piece<T>(row, k, C);
+    typename KnFrag<T>::Type f = {};
+    if (k < C) f = *(const typename KnAny<T>::Piece *)(row + min(k, C - W));
+    return f;
+}
+template <typename T> __device__ __forceinline__ void small_place(typename KnFrag<T>::Type &f, int32_t k, int32_t C)
+{
+    constexpr int W = SmallFrag<T>::W;
+    const int bytes = (W - C % W) % W * (int)sizeof(T); // alike for all lanes
+    kn_u32x4 d = __builtin_bit_cast(kn_u32x4, f);
+    if (bytes & 2) d = kn_u32x4{d[0] >> 16 | d[1] << 16, d[1] >> 16 | d[2] << 16, d[2] >> 16 | d[3] << 16, d[3] >> 16};
+    if (bytes & 4) d = kn_u32x4{d[1], d[2], d[3], 0};
+    if (bytes & 8) d = kn_u32x4{d[2], d[3], 0, 0};
+    if (k < C && k + W > C) f = __builtin_bit_cast(typename KnFrag<T>::Type, d);
+}
 template <typename T, bool COLS, int KF, int V>
 __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p, int32_t pieces)
 {
@@ -301,13 +321,13 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
                         fb[k][v][q] = c + q < C ? w : (T)0.0f;
                     }
                 } else {
-                    fb[k][v] = kn_any_piece<T>(b + (int64_t)j * p.b_j, c, C);
+                    fb[k][v] = small_ask<T>(b + (int64_t)j * p.b_j, c, C);
                 }
             }
 #pragma unroll
         for (int s = 0; s < SUBS; ++s)
 #pragma unroll
-            for (int k = 0; k < KF; ++k) fa[s][k] = kn_any_piece<T>(arow[s], k * KS + g * W, C);
+            for (int k = 0; k < KF; ++k) fa[s][k] = small_ask<T>(arow[s], k * KS + g * W, C);
     }
     const bool together = p.J % W != 0 && ntiles == 1; // rows that follow one another without whole pieces of their own: stored as one line
     // W neighbours j .. of a row of J (behind its end: the last one, unused)
@@ -333,6 +353,17 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
                 m[s][n] = Run{};
                 if (in) m[s][n] = run(mask + (int64_t)src * p.ldm, min(j0 + 4 * W * n + W * g, p.J - 1));
             }
+        }
+    }
+    if (C % W && C > W) {
+#pragma unroll
+        for (int k = 0; k < KF; ++k) {
+            if ((k + 1) * KS <= C) continue;
+#pragma unroll
+            for (int s = 0; s < SUBS; ++s) small_place<T>(fa[s][k], k * KS + g * W, C);
+            if constexpr (!COLS)
+#pragma unroll
+                for (int v = 0; v < V; ++v) small_place<T>(fb[k][v], k * KS + g * W, C);
         }
     }
 #pragma unroll
