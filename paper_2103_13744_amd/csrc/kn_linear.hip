@@ -258,26 +258,45 @@ template <typename T> struct SmallFrag {
     static constexpr int W = 16 / sizeof(T), KS = 4 * W;
 };
 // kn_any_piece in two parts, so that nothing waits for a fetch before all are under way: a piece that ends behind the row is fetched from
-// its last 16 bytes, and shifted to its place at the end.
-template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type small_ask(const T *row, int32_t k, int32_t C)
+// its last 16 bytes, and shifted to its place at the end.  `odd`: 16-bit rows may begin between two words, where a fetch of 16 bytes is
+// several times as slow: the words that the piece lies in are fetched (five; each holds a value of the piece) and joined at the end
+// (524,291 rows, 4,096 networks 63 x 32 in bf16: 50 -> 40 us, with weights whose rows are 63 values 60 -> 35).
+template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type small_ask(const T *row, int32_t k, int32_t C, bool odd, uint32_t &fifth)
 {
     constexpr int W = SmallFrag<T>::W;
     if (C < W) return kn_any_piece<T>(row, k, C);
     typename KnFrag<T>::Type f = {};
-    if (k < C) f = *(const typename KnAny<T>::Piece *)(row + min(k, C - W));
+    fifth = 0;
+    if (k < C) {
+        const T *at = row + min(k, C - W);
+        if (sizeof(T) == 2 && odd) {
+            const uintptr_t word = ~(uintptr_t)3;
+            f = *(const typename KnAny<T>::Words *)((uintptr_t)at & word);
+            fifth = *(const uint32_t *)(((uintptr_t)at + 14) & word);
+        } else {
+            f = *(const typename KnAny<T>::Piece *)at;
+        }
+    }
     return f;
 }
-template <typename T> __device__ __forceinline__ void small_place(typename KnFrag<T>::Type &f, int32_t k, int32_t C)
+template <typename T>
+__device__ __forceinline__ void small_place(typename KnFrag<T>::Type &f, const T *row, int32_t k, int32_t C, bool odd, uint32_t fifth)
 {
     constexpr int W = SmallFrag<T>::W;
-    const int bytes = (W - C % W) % W * (int)sizeof(T); // alike for all lanes
     kn_u32x4 d = __builtin_bit_cast(kn_u32x4, f);
+    if (sizeof(T) == 2 && odd) {
+        const uint32_t low = (uint32_t)(uintptr_t)(row + min(k, C - W)) & 2;
+        d = kn_u32x4{__builtin_amdgcn_alignbyte(d[1], d[0], low), __builtin_amdgcn_alignbyte(d[2], d[1], low), __builtin_amdgcn_alignbyte(d[3], d[2], low),
+                     __builtin_amdgcn_alignbyte(fifth, d[3], low)};
+    }
+    const kn_u32x4 whole = d;
+    const int bytes = (W - C % W) % W * (int)sizeof(T); // alike for all lanes
     if (bytes & 2) d = kn_u32x4{d[0] >> 16 | d[1] << 16, d[1] >> 16 | d[2] << 16, d[2] >> 16 | d[3] << 16, d[3] >> 16};
     if (bytes & 4) d = kn_u32x4{d[1], d[2], d[3], 0};
     if (bytes & 8) d = kn_u32x4{d[2], d[3], 0, 0};
-    if (k < C && k + W > C) f = __builtin_bit_cast(typename KnFrag<T>::Type, d);
+    f = __builtin_bit_cast(typename KnFrag<T>::Type, k < C && k + W > C ? d : whole);
 }
-template <typename T, bool COLS, int KF, int V>
+template <typename T, bool COLS, int KF, int V, bool ODD>
 __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p, int32_t pieces)
 {
     constexpr int W = SmallFrag<T>::W, KS = SmallFrag<T>::KS, SUBS = SMALL_ROWS / 16;
@@ -300,7 +319,9 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
     Frag fa[SUBS][KF], fb[KF][V];
     bool there[SUBS];
     if (some && p.a_rows > 0) {
-        const T *arow[SUBS];
+        const T *arow[SUBS], *brow[V];
+        uint32_t fifth_a[SUBS][KF], fifth_b[KF][V];
+        const bool odd_a = ODD && (((uintptr_t)p.a / sizeof(T) | p.lda) & 1), odd_b = ODD && (((uintptr_t)p.b / sizeof(T) | p.b_j) & 1);
 #pragma unroll
         for (int s = 0; s < SUBS; ++s) {
             const int32_t i = min(piece.begin + 16 * s + col, piece.end - 1), src = p.rows ? p.rows[i] : i;
@@ -321,13 +342,25 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
                         fb[k][v][q] = c + q < C ? w : (T)0.0f;
                     }
                 } else {
-                    fb[k][v] = small_ask<T>(b + (int64_t)j * p.b_j, c, C);
+                    brow[v] = b + (int64_t)j * p.b_j;
+                    fb[k][v] = small_ask<T>(brow[v], c, C, odd_b, fifth_b[k][v]);
                 }
             }
 #pragma unroll
         for (int s = 0; s < SUBS; ++s)
 #pragma unroll
-            for (int k = 0; k < KF; ++k) fa[s][k] = small_ask<T>(arow[s], k * KS + g * W, C);
+            for (int k = 0; k < KF; ++k) fa[s][k] = small_ask<T>(arow[s], k * KS + g * W, C, odd_a, fifth_a[s][k]);
+        if (C >= W && (ODD || C % W)) {
+#pragma unroll
+            for (int k = 0; k < KF; ++k) {
+                if (!ODD && (k + 1) * KS <= C) continue;
+#pragma unroll
+                for (int s = 0; s < SUBS; ++s) small_place<T>(fa[s][k], arow[s], k * KS + g * W, C, odd_a, fifth_a[s][k]);
+                if constexpr (!COLS)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) small_place<T>(fb[k][v], brow[v], k * KS + g * W, C, odd_b, fifth_b[k][v]);
+            }
+        }
     }
     const bool together = p.J % W != 0 && ntiles == 1; // rows that follow one another without whole pieces of their own: stored as one line
     // W neighbours j .. of a row of J (behind its end: the last one, unused)
@@ -353,17 +386,6 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
                 m[s][n] = Run{};
                 if (in) m[s][n] = run(mask + (int64_t)src * p.ldm, min(j0 + 4 * W * n + W * g, p.J - 1));
             }
-        }
-    }
-    if (C % W && C > W) {
-#pragma unroll
-        for (int k = 0; k < KF; ++k) {
-            if ((k + 1) * KS <= C) continue;
-#pragma unroll
-            for (int s = 0; s < SUBS; ++s) small_place<T>(fa[s][k], k * KS + g * W, C);
-            if constexpr (!COLS)
-#pragma unroll
-                for (int v = 0; v < V; ++v) small_place<T>(fb[k][v], k * KS + g * W, C);
         }
     }
 #pragma unroll
@@ -495,13 +517,20 @@ template <typename T, bool COLS> int launch_pieces(hipStream_t st, const KnProdu
     }
 }
 
-template <typename T, bool COLS, int KF, int V> int launch_small(hipStream_t st, const KnProduct &p)
+template <typename T, bool COLS, int KF, int V, bool ODD> int launch_small_of(hipStream_t st, const KnProduct &p)
 {
     const int64_t pieces = kn_pieces(p.M, p.E, SMALL_ROWS), waves = pieces * kn_div_up(p.J, 16 * V);
     if (waves > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_product_small<T, COLS, KF, V>), dim3((unsigned)kn_div_up(waves, SMALL_WAVES)), dim3(SMALL_WAVES * 64), 0, st, p, (int32_t)pieces);
+    hipLaunchKernelGGL((k_product_small<T, COLS, KF, V, ODD>), dim3((unsigned)kn_div_up(waves, SMALL_WAVES)), dim3(SMALL_WAVES * 64), 0, st, p, (int32_t)pieces);
     KN_CHECK_LAUNCH();
     return KN_OK;
+}
+template <typename T, bool COLS, int KF, int V> int launch_small(hipStream_t st, const KnProduct &p)
+{
+    if constexpr (sizeof(T) == 2) { // rows that begin between two words
+        if (((uintptr_t)p.a / 2 | p.lda | (COLS ? 0 : (uintptr_t)p.b / 2 | p.b_j)) & 1) return launch_small_of<T, COLS, KF, V, true>(st, p);
+    }
+    return launch_small_of<T, COLS, KF, V, false>(st, p);
 }
 constexpr int SMALL_MOST = 128; // widest contraction and most columns that k_product_small takes
 template <typename T, bool COLS> int launch_small_widths(hipStream_t st, const KnProduct &p)

@@ -69,7 +69,10 @@ template <typename T, int W> __device__ __forceinline__ typename KnFrag<T>::Type
 }
 
 // Values k .. k + W - 1 of a row of C wherever it lies, W = 16 bytes' worth; zeros behind its end.  k is a multiple of W.
-template <typename T> struct KnAny { typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T)))); };
+template <typename T> struct KnAny {
+    typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+    typedef T Words __attribute__((ext_vector_type(16 / sizeof(T)), aligned(4)));
+};
 template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type kn_any_piece(const T *row, int32_t k, int32_t C)
 {
     constexpr int W = 16 / sizeof(T);

@@ -157,6 +157,58 @@ def test_linear_rows_lie_apart_and_start_anywhere(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("k", [1, 7, 8, 9, 31, 40, 63, 65, 91, 127, 131])
+def test_linear_of_rows_between_others(k, dtype):
+    """Rows and weights of any width at addresses of every alignment: nothing of what lies beside them (NaN) comes into the results."""
+    dt, m, e, n = DT[dtype], 70, 3, 35
+    off = split(m, e, "tail", 5)
+    for lead, more, nk in ((0, 1, False), (1, 0, True), (1, 1, False), (2, 1, True), (3, 2, True), (1, 7 + 8 * k - k, False)):
+        wide = torch.full((m, lead + k + more), math.nan, dtype=dt)
+        wide[:, lead:lead + k] = rand(7, m, k).to(dt)
+        line = torch.full((lead + e * k * n + 9,), math.nan, dtype=dt)
+        line[lead:lead + e * k * n] = rand(8, e * k * n).to(dt)
+
+        def weights(flat):
+            flat = flat[lead:lead + e * k * n]
+            return flat.view(e, n, k).transpose(1, 2) if nk else flat.view(e, k, n)
+
+        y = kn.grouped_linear(dev(wide)[:, lead:lead + k], weights(dev(line)), dev(off))
+        want, mag = ref_linear(wide[:, lead:lead + k], weights(line), off, None, None, False)
+        close(y, want, mag, k, dtype)
+        dy = rand(9, m, n).to(dt)
+        dx, dw, _ = kn.grouped_linear_backward(dev(dy), dev(wide)[:, lead:lead + k], weights(dev(line)), dev(off), want_bias=False)
+        wdx, mdx = ref_linear(dy, weights(line).transpose(1, 2), off, None, None, False)
+        close(dx, wdx, mdx, n, dtype)
+        for g in range(e):
+            a, b = int(off[g]), int(off[g + 1])
+            xs, d = wide[a:b, lead:lead + k].double(), dy[a:b].double()
+            close(dw[g], xs.T @ d, xs.abs().T @ d.abs(), b - a, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [(266, 37, 200, 328), (3000, 3, 264, 512), (5000, 5, 192, 64), (4000, 3, 131, 259), (2300, 2, 72, 136), (70, 2, 260, 1028)], ids=str)
+def test_linear_in_full_precision_of_other_sizes(size):
+    """The ways that fp32 goes by itself: few rows for the chip, narrow results, layers of few tiles, many rows of odd sizes."""
+    m, e, k, n = size
+    for i, (how, gather, nk) in enumerate([("skew", True, True), ("one", False, False), ("tail", True, False)]):
+        x, w, off, rows = make(m, e, k, n, "f32", how, gather, nk, 100 * m + i)
+        y = kn.grouped_linear(dev(x), dev(w), dev(off), rows=dev(rows))
+        want, mag = ref_linear(x, w, off, rows, None, False)
+        close(y, want, mag, k, "f32")
+        dy = rand(9 + i, m, n)
+        dx, dw, db = kn.grouped_linear_backward(dev(dy), dev(x), dev(w), dev(off), rows=dev(rows))
+        wdx, mdx = ref_linear(dy, w.transpose(1, 2), off, None, None, False)
+        close(dx, wdx, mdx, n, "f32")
+        xs = (x if rows is None else x[rows.long()]).double()
+        for g in range(e):
+            a, b = int(off[g]), int(off[g + 1])
+            d = dy[a:b].double()
+            close(dw[g], xs[a:b].T @ d, xs[a:b].abs().T @ d.abs(), b - a, "f32")
+            close(db[g], d.sum(0), d.abs().sum(0), b - a, "f32")
+
+
+@pytest.mark.gpu
 def test_linear_not_finite_values_stay_where_they_are():
     """A NaN or an infinity in a row reaches that row's results only, one in a network's weights that network's only."""
     for dtype, k, n in (("bf16", 128, 128), ("f16", 96, 40), ("f32", 64, 64)):
