@@ -143,14 +143,14 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
     }
 }
 
-// Layers of the small networks' kind whose rows are not whole pieces: a workgroup of four wavefronts per part, 16 U x 16 V results at most; a
-// wavefront takes every fourth step of rows, straight into fragments, value by value (16 neighbouring lanes, 16 neighbouring values),
-// and the four are summed in the order of their numbers.  Nothing is staged and nothing waits until then: a part of a few
+// Layers of the small networks' kind whose rows are not whole pieces: a workgroup of WAVES wavefronts per part, 16 U x 16 V results at
+// most; a wavefront takes every WAVES-th step of rows, straight into fragments, value by value (16 neighbouring lanes, 16 neighbouring
+// values), and they are summed in the order of their numbers.  Nothing is staged and nothing waits until then: a part of a few
 // hundred rows is one chain of look-up, index, values, and the chains in flight are what counts.  Measured: 684,936 rows of 126 bytes
-// through an index, 4,096 networks 63 x 3 in bf16: 75 us (103 with tiles staged in the LDS).
-constexpr int SMALL_WAVES = 4;
-template <typename T, int U, int V>
-__global__ void __launch_bounds__(SMALL_WAVES * 64) k_reduce_small(KnProduct p, int32_t sum, Parts parts)
+// through an index, 4,096 networks 63 x 3 in bf16: 75 us (103 with tiles staged in the LDS).  Where networks have fewer rows than a step
+// or two on average, WAVES is 1: 27,000 rows of 4,096 networks 63 x 33 in fp16: 25 us, with four wavefronts 43.
+template <typename T, int U, int V, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) k_reduce_small(KnProduct p, int32_t sum, Parts parts)
 {
     constexpr int W = 16 / sizeof(T), RS = 4 * W, BM = 16 * U, BN = 16 * V, LD = BN + 4;
     typedef typename KnFrag<T>::Type Frag;
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_reduce_small(KnProduct p, 
     Frag ones;
 #pragma unroll
     for (int q = 0; q < W; ++q) ones[q] = (T)1.0f;
-    for (int32_t c = c0 + wave * RS; c < cend; c += SMALL_WAVES * RS) {
+    for (int32_t c = c0 + wave * RS; c < cend; c += WAVES * RS) {
         Frag fa[U], fb[V];
 #pragma unroll
         for (int q = 0; q < W; ++q) { // (rows behind the part, and rows that a matrix does not have: zeros)
@@ -203,7 +203,8 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_reduce_small(KnProduct p, 
 #pragma unroll
             for (int v = 0; v < V; ++v) sb[v] = kn_mfma(fb[v], ones, sb[v]);
     }
-    for (int w = 0; w < SMALL_WAVES; ++w) { // (a lane's four results are neighbours in a row)
+    const int busy = max(1, min(WAVES, (cend - c0 + RS - 1) / RS));
+    for (int w = 0; w < busy; ++w) { // (a lane's four results are neighbours in a row)
         if (wave == w) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -224,7 +225,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_reduce_small(KnProduct p, 
     }
     float *sums = parts.sums + place * p.I * p.J;
     T *out = (T *)p.out + (int64_t)group * p.o_group; // (its rows follow one another)
-    for (int q = tid; q < p.I * p.J; q += SMALL_WAVES * 64) {
+    for (int q = tid; q < p.I * p.J; q += WAVES * 64) {
         const float y = red[q / p.J * LD + q % p.J];
         if (several) sums[q] = y;
         else out[q] = (T)y;
@@ -325,24 +326,26 @@ template <typename T, bool DIRECT> int launch_reduce(hipStream_t st, const kn_li
     else if (way == WAY_32) {
         if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 32, 32, 2, 2>), grid, dim3(256), 0, st, p, sum, parts);
     } else if constexpr (!DIRECT) {
-#define KN_SMALL(U, V) hipLaunchKernelGGL((k_reduce_small<T, U, V>), grid, dim3(SMALL_WAVES * 64), 0, st, p, sum, parts)
-        if (bm == 32) {
-            if (bn == 16) KN_SMALL(2, 1);
-            else if (bn == 32) KN_SMALL(2, 2);
-            else if (bn == 48) KN_SMALL(2, 3);
-            else KN_SMALL(2, 4);
-        } else {
-            if (bn == 16) KN_SMALL(4, 1);
-            else if (bn == 32) KN_SMALL(4, 2);
-            else if (bn == 48) KN_SMALL(4, 3);
-            else KN_SMALL(4, 4);
+#define KN_SMALL(U, V)                                                                                                                      \
+    if (d->rows / d->experts < 32) hipLaunchKernelGGL((k_reduce_small<T, U, V, 1>), grid, dim3(64), 0, st, p, sum, parts);                  \
+    else hipLaunchKernelGGL((k_reduce_small<T, U, V, 4>), grid, dim3(256), 0, st, p, sum, parts)
+        switch (bm + bn / 16) {
+        case 33: KN_SMALL(2, 1); break;
+        case 34: KN_SMALL(2, 2); break;
+        case 35: KN_SMALL(2, 3); break;
+        case 36: KN_SMALL(2, 4); break;
+        case 65: KN_SMALL(4, 1); break;
+        case 66: KN_SMALL(4, 2); break;
+        case 67: KN_SMALL(4, 3); break;
+        default: KN_SMALL(4, 4);
         }
 #undef KN_SMALL
     }
     KN_CHECK_LAUNCH();
     if (p.M <= parts.len) return KN_OK; // (no network has several)
     const int64_t most = p.M / parts.len, results = (int64_t)p.I * p.J;
-    const int32_t chunk = results * (most < p.E ? most : p.E) <= 1 << 20 ? 1024 : 4096; // (few results: more workgroups)
+    const bool few = results * (most < p.E ? most : p.E) <= 1 << 20 && p.E * kn_div_up(results, 1024) <= 8192;
+    const int32_t chunk = few ? 1024 : 4096; // (few results: more workgroups)
     const int64_t pieces = kn_div_up(results, chunk);
     const bool search = most < p.E && p.E * pieces > 8192;
     const int64_t joins = (search ? most : p.E) * pieces;
