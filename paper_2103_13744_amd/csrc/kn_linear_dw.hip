@@ -148,7 +148,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
 // values), and they are summed in the order of their numbers.  Nothing is staged and nothing waits until then: a part of a few
 // hundred rows is one chain of look-up, index, values, and the chains in flight are what counts.  Measured: 684,936 rows of 126 bytes
 // through an index, 4,096 networks 63 x 3 in bf16: 75 us (103 with tiles staged in the LDS).  Where networks have fewer rows than a step
-// or two on average, WAVES is 1: 27,000 rows of 4,096 networks 63 x 33 in fp16: 25 us, with four wavefronts 43.
+// on average, or a few steps' and are enough to fill the chip, WAVES is 1: 27,000 rows of 4,096 networks 63 x 33 in fp16: 25 us, with
+// four wavefronts 43; 262,145 rows of 32 x 33 in bf16 (with the join) 30 and 41, 524,291 rows of 63 x 32: 57 and 57.
 template <typename T, int U, int V, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64) k_reduce_small(KnProduct p, int32_t sum, Parts parts)
 {
@@ -326,8 +327,10 @@ template <typename T, bool DIRECT> int launch_reduce(hipStream_t st, const kn_li
     else if (way == WAY_32) {
         if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 32, 32, 2, 2>), grid, dim3(256), 0, st, p, sum, parts);
     } else if constexpr (!DIRECT) {
+        const int64_t each = d->rows / d->experts;
+        const bool alone = each < 32 || (each < 256 && d->experts >= 1024);
 #define KN_SMALL(U, V)                                                                                                                      \
-    if (d->rows / d->experts < 32) hipLaunchKernelGGL((k_reduce_small<T, U, V, 1>), grid, dim3(64), 0, st, p, sum, parts);                  \
+    if (alone) hipLaunchKernelGGL((k_reduce_small<T, U, V, 1>), grid, dim3(64), 0, st, p, sum, parts);                                      \
     else hipLaunchKernelGGL((k_reduce_small<T, U, V, 4>), grid, dim3(256), 0, st, p, sum, parts)
         switch (bm + bn / 16) {
         case 33: KN_SMALL(2, 1); break;
