@@ -113,7 +113,7 @@ struct F8Args {
 // in the LDS they took the place of a workgroup.
 // Measured: 32,822 rows through an index, 16 networks 2048 x 2048: 195 to 220 us, 1,250 to 1,400 TFLOP/s (one product of the library of
 // 8192 x 8192 x 8192 with one scale: 2,660); reading half of a stage ahead, as the 16-bit kernel does, takes 64 registers and a
-// workgroup's place: 300 us.  32 rows in about 27 of 32 networks 2560 x 2048: 24 us, 5.9 TB/s.
+// workgroup's place: 300 us.  32 rows in about 20 of 32 networks 2560 x 2048: 24 us, 4.5 TB/s.
 template <typename T, int BM, int BN, int WR, int WC, int NB>
 __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t blocks)
 {
