@@ -15,18 +15,18 @@ template <typename T> __device__ __forceinline__ float to_float(T v) { return (f
 __device__ __forceinline__ float row_max(float v)
 {
     constexpr int ROW_ROR = 0x120; // dpp_ctrl encoding
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 8, 0xf, 0xf, false)));
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 4, 0xf, 0xf, false)));
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 2, 0xf, 0xf, false)));
-    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 1, 0xf, 0xf, false)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 8, 0xf, 0xf, true)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 4, 0xf, 0xf, true)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 2, 0xf, 0xf, true)));
+    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 1, 0xf, 0xf, true)));
 }
 __device__ __forceinline__ float row_sum(float v)
 {
     constexpr int ROW_ROR = 0x120;
-    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 8, 0xf, 0xf, false));
-    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 4, 0xf, 0xf, false));
-    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 2, 0xf, 0xf, false));
-    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 1, 0xf, 0xf, false));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 8, 0xf, 0xf, true));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 4, 0xf, 0xf, true));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 2, 0xf, 0xf, true));
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 1, 0xf, 0xf, true));
 }
 // G = 16: a row of the wavefront works on a row of logits; 64: the whole wavefront
 template <int G> __device__ __forceinline__ float group_max(float v)
@@ -57,10 +57,10 @@ template <int G> __device__ __forceinline__ uint64_t group_ballot(bool v, int la
 __device__ __forceinline__ int32_t row_max_i32(int32_t v)
 {
     constexpr int ROW_ROR = 0x120;
-    v = max(v, __builtin_amdgcn_update_dpp(v, v, ROW_ROR + 8, 0xf, 0xf, false));
-    v = max(v, __builtin_amdgcn_update_dpp(v, v, ROW_ROR + 4, 0xf, 0xf, false));
-    v = max(v, __builtin_amdgcn_update_dpp(v, v, ROW_ROR + 2, 0xf, 0xf, false));
-    return max(v, __builtin_amdgcn_update_dpp(v, v, ROW_ROR + 1, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, ROW_ROR + 8, 0xf, 0xf, true));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, ROW_ROR + 4, 0xf, 0xf, true));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, ROW_ROR + 2, 0xf, 0xf, true));
+    return max(v, __builtin_amdgcn_update_dpp(0, v, ROW_ROR + 1, 0xf, 0xf, true));
 }
 template <int G> __device__ __forceinline__ int32_t group_max_i32(int32_t v)
 {
@@ -113,7 +113,7 @@ __device__ __forceinline__ float value_of(int32_t key) { return __int_as_float(k
 // Top-k of the rows [t0, t1) of logits: G lanes a row, each with V neighbouring logits in registers, so that the first lane of
 // those that hold the largest holds the lowest index.  k times the largest is taken out; the statistics of the softmax are held in
 // 32 bits.  In the LDS: `count`, a histogram; `chosen`, the experts of the rows that are being worked on.
-// Measured: 32,768 rows of 128 logits in fp32, k = 8: 13 us, bound by vector instructions (some 30 per choice and 4 rows); their
+// Measured: 32,768 rows of 128 logits in fp32, k = 8: 12.5 us, bound by vector instructions (some 80 per choice of 4 rows); their
 // order takes 4 + 6 us more, in launches of latency.  16 rows of 64, k = 4, order included: 3.8 us, one launch.
 template <typename T, int G, int V>
 __device__ void choose(const RouteArgs &p, int32_t t0, int32_t t1, int32_t *count, int32_t *chosen)
