@@ -209,6 +209,27 @@ def test_linear_in_full_precision_of_other_sizes(size):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("k, n", [(63, 63), (31, 31), (31, 17), (63, 17), (9, 63), (47, 33)])
+def test_linear_gradient_of_narrow_layers(k, n, dtype):
+    """Networks with a few rows, with several parts, and very many networks with some: every width of a narrow layer's tiles."""
+    dt = DT[dtype]
+    for m, e, how, nk in ((40, 5, "even", False), (700, 3, "skew", True), (40, 2, "tail", True), (900, 2, "one", False), (9000, 1100, "skew", False)):
+        x, w, off, _ = make(m, e, k, n, dtype, how, False, nk, 10 * m + k)
+        dy = rand(m + n, m, n).to(dt)
+        dw, db = kn.grouped_linear_dw(dev(dy), dev(x), dev(w), dev(off))
+        want, mag, wdb, mdb = (torch.zeros(s, dtype=torch.float64) for s in ((e, k, n), (e, k, n), (e, n), (e, n)))
+        most = 0
+        for g in range(e):
+            a, b = int(off[g]), int(off[g + 1])
+            most = max(most, b - a)
+            xs, d = x[a:b].double(), dy[a:b].double()
+            want[g], mag[g], wdb[g], mdb[g] = xs.T @ d, xs.abs().T @ d.abs(), d.sum(0), d.abs().sum(0)
+        close(dw, want, mag, most, dtype)
+        close(db, wdb, mdb, most, dtype)
+
+
+@pytest.mark.gpu
 def test_linear_not_finite_values_stay_where_they_are():
     """A NaN or an infinity in a row reaches that row's results only, one in a network's weights that network's only."""
     for dtype, k, n in (("bf16", 128, 128), ("f16", 96, 40), ("f32", 64, 64)):
