@@ -241,10 +241,12 @@ __global__ void __launch_bounds__(WAVES * 64) k_reduce_small(KnProduct p, int32_
 
 // The parts' sums of the networks that have several, in the order of the parts; `chunk` results per workgroup.  SEARCH: there are at most
 // M / len such networks, and a workgroup looks for its own among all (few networks of many results); else there is one for
-// every network's results, and most find nothing to do.
-template <typename T, bool SEARCH> __global__ void __launch_bounds__(256) k_reduce_join(KnProduct p, int32_t sum, Parts parts, int32_t chunk)
+// every network's results, and most find nothing to do.  SPLIT: each wavefront sums a quarter of a network's parts, and the quarters are added
+// in order (50,560 rows of 25 networks 64 x 112, the longest of some 160 parts: 51 -> 17 us).
+template <typename T, bool SEARCH, bool SPLIT> __global__ void __launch_bounds__(256) k_reduce_join(KnProduct p, int32_t sum, Parts parts, int32_t chunk)
 {
     __shared__ int32_t scratch[4], found;
+    __shared__ float quarter[4][64];
     const int64_t n = (int64_t)p.I * p.J;
     const int32_t pieces = (int32_t)((n + chunk - 1) / chunk), turn = kn_block() / pieces;
     int32_t group = turn;
@@ -268,7 +270,20 @@ template <typename T, bool SEARCH> __global__ void __launch_bounds__(256) k_redu
     const int32_t count = (rows + parts.len - 1) / parts.len;
     const int64_t place = 2 * (o / parts.len), first = (int64_t)(kn_block() % pieces) * chunk;
     T *out = (T *)p.out + (int64_t)group * p.o_group;
-    for (int64_t q = first + kn_thread(); q < min(n, first + chunk); q += 256) {
+    if constexpr (SPLIT) {
+        const int lane = kn_thread() & 63, wave = kn_thread() >> 6;
+        const int c0 = count * wave / 4, c1 = count * (wave + 1) / 4;
+        for (int64_t q = first + lane; q - lane < min(n, first + chunk); q += 64) {
+            float y = 0.0f;
+            if (q < n)
+#pragma unroll 8
+                for (int c = c0; c < c1; ++c) y += parts.sums[(place + c) * n + q];
+            quarter[wave][lane] = y;
+            __syncthreads();
+            if (wave == 0 && q < n) out[q] = (T)(((quarter[0][lane] + quarter[1][lane]) + quarter[2][lane]) + quarter[3][lane]);
+            __syncthreads();
+        }
+    } else for (int64_t q = first + kn_thread(); q < min(n, first + chunk); q += 256) {
         float y = 0.0f;
 #pragma unroll 4
         for (int c = 0; c < count; ++c) y += parts.sums[(place + c) * n + q];
@@ -278,6 +293,7 @@ template <typename T, bool SEARCH> __global__ void __launch_bounds__(256) k_redu
     const int32_t m = sum == SUM_A ? p.I : p.J;
     for (int32_t j = kn_thread(); j < m; j += 256) {
         float y = 0.0f;
+#pragma unroll 16
         for (int c = 0; c < count; ++c) y += parts.bias_sums[(place + c) * m + j];
         ((T *)p.out_bias)[(int64_t)group * m + j] = (T)y;
     }
@@ -347,13 +363,14 @@ template <typename T, bool DIRECT> int launch_reduce(hipStream_t st, const kn_li
     KN_CHECK_LAUNCH();
     if (p.M <= parts.len) return KN_OK; // (no network has several)
     const int64_t most = p.M / parts.len, results = (int64_t)p.I * p.J;
-    const bool few = results * (most < p.E ? most : p.E) <= 1 << 20 && p.E * kn_div_up(results, 1024) <= 8192;
-    const int32_t chunk = few ? 1024 : 4096; // (few results: more workgroups)
+    const bool few = results * (most < p.E ? most : p.E) <= 1 << 20 && p.E * kn_div_up(results, 256) <= 8192;
+    const int32_t chunk = few ? 256 : 4096; // (few results: more workgroups, whose wavefronts take a quarter of the parts each)
     const int64_t pieces = kn_div_up(results, chunk);
     const bool search = most < p.E && p.E * pieces > 8192;
     const int64_t joins = (search ? most : p.E) * pieces;
     if (joins > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL(search ? (k_reduce_join<T, true>) : (k_reduce_join<T, false>), dim3((unsigned)joins), dim3(256), 0, st, p, sum, parts, chunk);
+    auto join = few ? (k_reduce_join<T, false, true>) : search ? (k_reduce_join<T, true, false>) : (k_reduce_join<T, false, false>); // (few: no more than 8,192 workgroups)
+    hipLaunchKernelGGL(join, dim3((unsigned)joins), dim3(256), 0, st, p, sum, parts, chunk);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }
