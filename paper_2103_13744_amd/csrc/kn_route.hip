@@ -402,25 +402,31 @@ template <typename T> struct Vec {
     typedef T Type __attribute__((ext_vector_type(16 / sizeof(T))));
 };
 
-// out[t] = sum over j of weights[t, j] y[slots[t, j]]: a thread per V neighbouring values of a row.  V: 16 bytes where the rows
-// are made of whole such pieces, else 1.  Bound by its bytes.  STREAM: what is read and written once goes past the caches, where
+// V neighbouring values of a row.  WHOLE: rows are made of such pieces, each on a multiple of its size; else they lie anywhere, and a row's
+// last piece is its last V values, some of which the piece before has too (narrower rows: V = 1).  Rows of 2,468 values, 25,295 of 2 in bf16: pieces
+// anywhere 213 us for the sums and their gradients, single values 582.
+template <typename T, int V, bool WHOLE> struct RowPiece {
+    typedef T Type __attribute__((ext_vector_type(V), aligned((WHOLE ? V : 1) * sizeof(T))));
+};
+
+// out[t] = sum over j of weights[t, j] y[slots[t, j]]: a thread per piece of a row, 16 bytes or one value.  Bound by its bytes.  STREAM: what is read and written once goes past the caches, where
 // y does not stay in them anyway (16,384 rows of 4 x 2048 in bf16, 336 MB: 83 us without, 64 with: 5.3 TB/s).
 constexpr int64_t COMBINE_STREAM = 1 << 26; // bytes of y
-template <typename T, int V, bool STREAM>
+template <typename T, int V, bool WHOLE, bool STREAM>
 __global__ void __launch_bounds__(256) k_combine(const T *__restrict__ y, const int32_t *__restrict__ slots, const float *__restrict__ weights,
                                                  int32_t M, int32_t D, int32_t Tn, int32_t k, T *__restrict__ out)
 {
-    typedef T Piece __attribute__((ext_vector_type(V)));
-    const int32_t pieces = D / V;
+    typedef typename RowPiece<T, V, WHOLE>::Type Piece;
+    const int32_t pieces = (D + V - 1) / V;
     const int64_t q = (int64_t)kn_block() * 256 + kn_thread();
     if (q >= (int64_t)Tn * pieces) return;
-    const int32_t t = (int32_t)(q / pieces), c = (int32_t)(q % pieces);
+    const int32_t t = (int32_t)(q / pieces), c = WHOLE ? (int32_t)(q % pieces) * V : min((int32_t)(q % pieces) * V, D - V);
     float acc[V] = {};
     for (int j = 0; j < k; ++j) {
         const int32_t s = slots[(int64_t)t * k + j];
         if ((uint32_t)s >= (uint32_t)M) continue;
         const float w = weights ? weights[(int64_t)t * k + j] : 1.0f;
-        const Piece *at = (const Piece *)(y + (int64_t)s * D + (int64_t)c * V);
+        const Piece *at = (const Piece *)(y + (int64_t)s * D + c);
         const Piece v = STREAM ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] = fmaf(w, (float)v[i], acc[i]);
@@ -428,7 +434,7 @@ __global__ void __launch_bounds__(256) k_combine(const T *__restrict__ y, const 
     Piece r;
 #pragma unroll
     for (int i = 0; i < V; ++i) r[i] = (T)acc[i];
-    Piece *to = (Piece *)(out + (int64_t)t * D + (int64_t)c * V);
+    Piece *to = (Piece *)(out + (int64_t)t * D + c);
     if (STREAM) __builtin_nontemporal_store(r, to);
     else *to = r;
 }
@@ -436,12 +442,12 @@ __global__ void __launch_bounds__(256) k_combine(const T *__restrict__ y, const 
 // dy[slots[t, j]] = weights[t, j] dout[t], dweights[t, j] = <dout[t], y[slots[t, j]]>: a wavefront per pair; a row of
 // dout is read k times, but for the first from the caches.  Bound by its bytes (the same sizes, 604 MB: 118 us, 5.1 TB/s; a
 // wavefront per row of dout, four pairs at a time: 143).
-template <typename T, int V>
+template <typename T, int V, bool WHOLE>
 __global__ void __launch_bounds__(256) k_combine_backward(const T *__restrict__ dout, const T *__restrict__ y, const int32_t *__restrict__ slots,
                                                           const float *__restrict__ weights, int32_t M, int32_t D, int64_t pairs, int32_t k,
                                                           T *__restrict__ dy, float *__restrict__ dweights)
 {
-    typedef T Piece __attribute__((ext_vector_type(V)));
+    typedef typename RowPiece<T, V, WHOLE>::Type Piece;
     const int lane = kn_thread() & 63;
     const int64_t q = (int64_t)kn_block() * 4 + (kn_thread() >> 6);
     if (q >= pairs) return;
@@ -451,13 +457,15 @@ __global__ void __launch_bounds__(256) k_combine_backward(const T *__restrict__ 
     const float w = weights ? weights[q] : 1.0f;
     float dot = 0.0f;
     if (there)
-        for (int32_t c = lane * V; c < D; c += 64 * V) {
+        for (int32_t own = lane * V; own < D; own += 64 * V) {
+            const int32_t c = WHOLE ? own : min(own, D - V);
             const Piece a = *(const Piece *)(g + c);
             Piece r;
             if (dweights) {
                 const Piece b = *(const Piece *)(y + (int64_t)s * D + c);
 #pragma unroll
-                for (int i = 0; i < V; ++i) dot = fmaf((float)a[i], (float)b[i], dot);
+                for (int i = 0; i < V; ++i)
+                    if (WHOLE || c + i >= own) dot = fmaf((float)a[i], (float)b[i], dot); // (each value once)
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) r[i] = (T)(w * (float)a[i]);
@@ -578,9 +586,10 @@ extern "C" int kn_combine(void *stream, const void *y, int32_t dtype, int64_t M,
         typedef decltype(v) E_;
         constexpr int V = 16 / sizeof(E_);
         const bool wide = whole_pieces(D, dtype, y, out, nullptr);
-        const int64_t blocks = kn_div_up(T * (wide ? D / V : D), 256);
+        const int64_t blocks = kn_div_up(T * (D < V ? D : kn_div_up(D, V)), 256);
         if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-        auto kernel = !wide ? k_combine<E_, 1, false> : M * D * (int64_t)sizeof(E_) < COMBINE_STREAM ? k_combine<E_, V, false> : k_combine<E_, V, true>;
+        auto kernel = D < V ? k_combine<E_, 1, true, false> : !wide ? k_combine<E_, V, false, false>
+                    : M * D * (int64_t)sizeof(E_) < COMBINE_STREAM ? k_combine<E_, V, true, false> : k_combine<E_, V, true, true>;
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, (const E_ *)y, slots, weights, (int32_t)M, D, (int32_t)T,
                            k, (E_ *)out);
         KN_CHECK_LAUNCH();
@@ -597,7 +606,8 @@ extern "C" int kn_combine_backward(void *stream, const void *dout, const void *y
     return kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
         constexpr int V = 16 / sizeof(E_);
-        auto kernel = whole_pieces(D, dtype, dout, dweights ? y : nullptr, dy) ? k_combine_backward<E_, V> : k_combine_backward<E_, 1>;
+        auto kernel = D < V ? k_combine_backward<E_, 1, true>
+                    : whole_pieces(D, dtype, dout, dweights ? y : nullptr, dy) ? k_combine_backward<E_, V, true> : k_combine_backward<E_, V, false>;
         hipLaunchKernelGGL(kernel, dim3((unsigned)kn_div_up(T * k, 4)), dim3(256), 0, (hipStream_t)stream, (const E_ *)dout, (const E_ *)y, slots,
                            weights, (int32_t)M, D, T * k, k, (E_ *)dy, dweights);
         KN_CHECK_LAUNCH();
