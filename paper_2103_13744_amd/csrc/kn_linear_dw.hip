@@ -300,26 +300,29 @@ template <typename T, bool SEARCH, bool SPLIT> __global__ void __launch_bounds__
 }
 
 // Layers of up to 64 x 64 whose rows are not whole pieces are k_reduce_small's (us, against 64 x 64 staged in the LDS: 524,291 rows, 4,096
-// networks 63 x 32: 57 and 63 in bf16, 91 and 123 in fp32; 262,145 rows, 1,600 networks 91 x 64: 109 and 75, 151 and 102).  Else tiles of 64 x 64 where 128 x 128 would be few,
-// or layers are no wider than that (four times as many workgroups at a time: such a tile's few rows are latency), and in fp32, which the
-// matrix cores bound: what a tile fetches is no matter, how evenly tiles fill the chip is (8,192 rows, 16 networks 1024 x 1024, the
-// longest 2,892: 64 x 64 189 us, 128 x 128 226; 128 networks 512 x 512, the longest 568: 88, 99);
-// and 32 x 32 where 64 x 64 would be few (1,001 rows, 5 networks 259 x 131: 9.6 us, 64 x 64 14.6).
+// networks 63 x 32: 57 and 63 in bf16, 91 and 123 in fp32; 262,145 rows, 1,600 networks 91 x 64: 109 and 52, 151 and 102).  Else tiles
+// of 64 x 64 where 128 x 128 would be few, or a side is no wider than that and the other no wider than 128, or rows are few (more
+// workgroups at a time: such a tile's few rows are latency; 262,145 rows, 1,600 networks 91 x 64 in bf16: 52 us, 128 x 128 75; 20,000
+// rows, 300 networks 512 x 64: 20, 22; but 200,000 rows, 16 networks 1024 x 64: 128, 108), and in fp32, which the matrix cores bound:
+// what a tile fetches is no matter, how evenly tiles fill the chip is (8,192 rows, 16 networks 1024 x 1024, the longest 2,892:
+// 64 x 64 189 us, 128 x 128 226; 128 networks 512 x 512, the longest 568: 88, 99); and 32 x 32 where 64 x 64 would be few (1,001 rows,
+// 5 networks 259 x 131: 9.6 us, 64 x 64 14.6).
+bool narrow(const kn_linear_desc *d) { return d->n_in <= 128 && d->n_out <= 128; }
 enum Way { WAY_SMALL, WAY_32, WAY_64, WAY_128 };
 Way way_of(const kn_linear_desc *d, bool direct)
 {
     if (!direct && d->n_in <= 64 && d->n_out <= 64) return WAY_SMALL;
     if (d->dtype == KN_F32) return (d->experts + d->rows / 512) * kn_div_up(d->n_in, 64) * kn_div_up(d->n_out, 64) < 256 ? WAY_32 : WAY_64;
-    if (d->n_in <= 64 && d->n_out <= 64) return WAY_64;
+    if ((d->n_in <= 64 || d->n_out <= 64) && (narrow(d) || d->rows / d->experts < 256)) return WAY_64;
     return d->experts * kn_div_up(d->n_in, 128) * kn_div_up(d->n_out, 128) < 256 && d->rows < 65536 ? WAY_64 : WAY_128;
 }
-bool narrow(const kn_linear_desc *d) { return d->n_in <= 128 && d->n_out <= 128; }
 
-// Rows of a part: a part more is a tile written and read again in fp32, so that there are only as many as keep the chip busy, and
-// up to 1,024 rows of a wide layer are one (the join is a launch more, 4 us).  Wide layers: 32 networks 1024 x 2048, the longest of 32,768 rows 5,741: parts of 1,024 rows 357 us, of 4,096 264, of 8,192 238, none
-// 231; 8 networks 512 x 512, the longest 23,284: of 1,024 97, of 2,048 80, none 261; 4 networks 256 x 256, the longest of 16,384
-// 11,740: of 256 31, of 1,024 23, of 2,048 33.  In fp32, where a tile takes longest and its sums are the less: of 512 51, of 2,048 71.
-// Narrow layers' parts are small, and more of them are chains that run at the same time.
+// Rows of a part: a part more is a tile written and read again in fp32, so that there are only as many as keep the chip busy, and up to
+// 1,024 rows of a wide layer are one (the join is a launch more, 4 us).  Wide layers: 32 networks 1024 x 2048, the longest of 32,768
+// rows 5,741: parts of 1,024 rows 357 us, of 4,096 264, of 8,192 238, none 231; 8 networks 512 x 512, the longest 23,284: of 1,024 97,
+// of 2,048 80, none 261; 4 networks 256 x 256, the longest of 16,384 11,740: of 256 31, of 1,024 23, of 2,048 33.  In fp32, where a
+// tile takes longest and its sums are the less: of 512 51, of 2,048 71.  Narrow layers' parts are small, and more of them are chains
+// that run at the same time.
 int32_t part_length(const kn_linear_desc *d)
 {
     const bool whole = d->dtype == KN_F32;
