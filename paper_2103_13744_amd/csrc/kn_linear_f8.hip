@@ -106,14 +106,36 @@ struct F8Args {
     int32_t M, E, N, kb, x_rows, relu;
 };
 
-// Tiles of BM x BN results, WR x WC wavefronts, NB stages in the LDS, fetched ahead.  A stage is a block of 128 inputs, which is one
-// instruction's contraction, so that every product starts from zero and is scaled, in fp32, as it is added.  Fragments of the
+// 32 values of 8 bits as 4 fragments of 8 in fp16, which holds every e4m3 value (448 down to 2^-9, NaN) exactly
+struct F8Wide {
+    kn_f16x8 part[4];
+};
+__device__ __forceinline__ F8Wide f8_widen(kn_u32x4 lo, kn_u32x4 hi)
+{
+    typedef _Float16 Pair __attribute__((ext_vector_type(2)));
+    F8Wide w;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        const uint32_t v = q < 4 ? lo[q] : hi[q - 4];
+        const Pair a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.0f, true);
+        w.part[q / 2][q % 2 * 4] = a[0];
+        w.part[q / 2][q % 2 * 4 + 1] = a[1];
+        w.part[q / 2][q % 2 * 4 + 2] = b[0];
+        w.part[q / 2][q % 2 * 4 + 3] = b[1];
+    }
+    return w;
+}
+
+// Tiles of BM x BN results, WR x WC wavefronts, NB stages in the LDS, fetched ahead.  A stage is a block of 128 inputs, whose sum
+// starts from zero and is scaled, in fp32, as it is added.  The 8-bit matrix instructions do not hold it in 32 bits: each 8 neighbouring
+// products are brought to the largest one's exponent and cut off 13 bits below it, so that of 8 products, one of them 2^14 times the others,
+// one is left.  Values are widened to fp16 on their way from the LDS instead (their products are exact in fp32), and the
+// 16-bit instruction's sums are fp32's.  Fragments of the
 // weights are the first operand: a lane's four results are neighbours in a row, and one factor, the product of the row's
 // scale and the weights', serves all of them.  The four lanes of a row hold the factors of four blocks and hand them to each other:
 // in the LDS they took the place of a workgroup.
-// Measured: 32,822 rows through an index, 16 networks 2048 x 2048: 195 to 220 us, 1,250 to 1,400 TFLOP/s (one product of the library of
-// 8192 x 8192 x 8192 with one scale: 2,660); reading half of a stage ahead, as the 16-bit kernel does, takes 64 registers and a
-// workgroup's place: 300 us.  32 rows in about 20 of 32 networks 2560 x 2048: 24 us, 4.5 TB/s.
+// Measured: 32,822 rows through an index, 16 networks 2048 x 2048: 290 us, 950 TFLOP/s (the 8-bit instructions: 205).  32 rows in about 20
+// of 32 networks 2560 x 2048: 27 us, 4.0 TB/s.
 template <typename T, int BM, int BN, int WR, int WC, int NB>
 __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t blocks)
 {
@@ -179,26 +201,27 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
                 if (s + 4 < steps) ask(s + 4);
             }
             const KN_LDS char *ta = lds + at * STAGE, *tb = ta + BM * 128;
-            union Frag { kn_u32x4 h[2]; kn_i32x8 v; } fa[U], fb[V];
-            float f[U];
+            auto frag = [&](const KN_LDS char *tile, int r0) { // (which 8 inputs of the 128 a lane has in which part is the same in a and b)
+                const int r = r0 + (lane & 15);
+                return f8_widen(*(const KN_LDS kn_u32x4 *)(tile + kn_row_byte(r, lane >> 4)), *(const KN_LDS kn_u32x4 *)(tile + kn_row_byte(r, 4 + (lane >> 4))));
+            };
+            F8Wide fb[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) fb[v].h[h] = *(const KN_LDS kn_u32x4 *)(tb + kn_row_byte(wj + 16 * v + (lane & 15), h * 4 + (lane >> 4)));
+            for (int v = 0; v < V; ++v) fb[v] = frag(tb, wj + 16 * v);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                const F8Wide fa = frag(ta, wi + 16 * u);
+                const float f = __shfl(factor[u], (lane & 15) + 16 * (s & 3));
+                kn_f32x4 r[V] = {};
 #pragma unroll
-                for (int h = 0; h < 2; ++h) fa[u].h[h] = *(const KN_LDS kn_u32x4 *)(ta + kn_row_byte(wi + 16 * u + (lane & 15), h * 4 + (lane >> 4)));
-                f[u] = __shfl(factor[u], (lane & 15) + 16 * (s & 3));
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) r[v] = kn_mfma(fb[v].part[q], fa.part[q], r[v]);
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[u][v][i] = fmaf(r[v][i], f, acc[u][v][i]);
             }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const kn_f32x4 r = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[v].v, fa[u].v, kn_f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[u][v][i] = fmaf(r[i], f[u], acc[u][v][i]);
-                }
             at = at + 1 == NB ? 0 : at + 1;
         }
     }
@@ -292,15 +315,16 @@ extern "C" int kn_grouped_linear_f8(void *stream, const kn_linear_desc *d, const
         return KN_E_INVALID_ARG;
     F8Args p = {(const uint8_t *)xq, (const uint8_t *)wq, xs, ws, bias, y, offsets, rows, (int32_t)d->rows, d->experts, d->n_out,
                 (int32_t)kn_div_up(d->n_in, F8_BLOCK), (int32_t)d->x_rows, relu != 0};
-    // Which tile (us): 7,794 rows, 7 networks 2048 x 64: 32 x 128 12, 64 x 128 15, 192 x 128 29; 2,048 rows, 32 networks 2560 x 2048: 53, 53, 69;
-    // 8,192 rows, 16 networks 2048 x 2048: 88, 69, 69; 32,768 of them: 304, 237, 200.
+    // Which tile (us; 32, 64 and 192 rows x 128): 7,791 rows, 7 networks 2048 x 64: 16, 22, 37; 2,048 rows, 32 networks 2560 x 2048: 61, 65, 89;
+    // 12,000 rows, 64 networks 512 x 512: 19, 19, 21; 8,728 rows, 5 networks 576 x 2048: 43, 39, 41; 8,192 rows, 16 networks 2048 x 2048:
+    // 110, 101, 98; 32,768 of them: 399, 343, 294.
     const int64_t each = p.M / p.E; // rows of a network, on average
     auto tiles = [&](int64_t bm) { return kn_div_up(p.M, bm) * kn_div_up(p.N, 128); };
     return kn_with_type(d->dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
         hipStream_t st = (hipStream_t)stream;
         if (each >= 512 && tiles(192) >= 256) return launch_f8<E_, 192, 128, 2, 2, 2>(st, p);
-        if (each >= 32 && tiles(64) >= 128) return launch_f8<E_, 64, 128, 1, 4, 2>(st, p);
+        if (each >= 128 && tiles(64) >= 128) return launch_f8<E_, 64, 128, 1, 4, 2>(st, p);
         return launch_f8<E_, 32, 128, 1, 4, 2>(st, p);
     });
 }

@@ -1,0 +1,54 @@
+"""Networks chosen per row: inputs at the edge of what the calls take, against plain implementations in 64 bits.  Bounds as in
+test_experts.py."""
+import math
+
+import pytest
+import torch
+
+import paper_2103_13744_amd as kn
+
+from .test_experts import DT, U, rand, split
+
+
+def close(got, want, mags, terms, dtype):
+    """test_experts.close, where everything is on the device."""
+    assert got.shape == want.shape and got.dtype == DT[dtype]
+    bound = U[dtype] * want.abs() + (terms + 8) * 2.0 ** -23 * mags + 2.0 ** -24
+    off = (got.double() - want).abs()
+    high = want.abs() + bound >= float(torch.finfo(DT[dtype]).max)  # (beyond the type's range: infinity)
+    bad = ~((off <= bound) | (high & (got.double() == want.sign() * math.inf)))
+    assert not bad.any(), (int(bad.sum()), float(off[bad].max()), bad.nonzero()[:4].tolist())
+
+
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("size", [(64, 1, 384, 128), (1100, 20, 256, 1024), (2700, 20, 256, 1024), (6200, 8, 256, 1024)], ids=str)  # (tiles of 32, 64 and 192 rows)
+def test_8_bit_sums_are_held_in_32_bits(size, dtype):
+    """Any finite 8-bit values: products that lie up to 2^35 apart."""
+    m, e, k, n = size
+    g = torch.Generator().manual_seed(m)
+    bits = lambda *s: torch.randint(0, 256, s, generator=g, dtype=torch.int32).to(torch.uint8)  # noqa: E731
+    finite = lambda b: torch.where((b & 127) == 127, b ^ 1, b).view(torch.float8_e4m3fn).cuda()  # noqa: E731
+    xq, wq, off = finite(bits(m, k)), finite(bits(e, n, k)), split(m, e, "even", 1)
+    xs, ws = torch.exp(rand(2, m, k // 128)).cuda() / 32, torch.exp(rand(3, e, n // 128, k // 128)).cuda() / 32
+    y = kn.grouped_linear_f8(xq, xs, wq, ws, off.cuda(), dtype=DT[dtype])
+    vx = xq.double() * xs.double().repeat_interleave(128, 1)
+    vw = wq.double() * ws.double().repeat_interleave(128, 1).repeat_interleave(128, 2)
+    want, mag = torch.zeros(m, n, dtype=torch.float64, device="cuda"), torch.zeros(m, n, dtype=torch.float64, device="cuda")
+    for i, (a, b) in enumerate(zip(off[:-1].tolist(), off[1:].tolist())):
+        wt = vw[i].t().contiguous()
+        want[a:b], mag[a:b] = vx[a:b] @ wt, vx[a:b].abs() @ wt.abs()
+    close(y, want, mag, k + 8, dtype)
+
+
+@pytest.mark.gpu
+def test_8_bit_sums_keep_what_is_small_beside_what_cancels():
+    """Of each eight neighbouring products one is 2^16 or -2^16 and seven are 4: 448 is left, which sums in fp32 miss by 34 at most."""
+    x, w = torch.full((3, 128), 2.0), torch.full((128, 128), 2.0)
+    x[:, ::16], x[:, 8::16], w[:, ::8] = 256.0, -256.0, 256.0
+    one = torch.ones(3, 1).cuda()
+    y = kn.grouped_linear_f8(x.to(torch.float8_e4m3fn).cuda(), one, w.to(torch.float8_e4m3fn).cuda()[None], one[:1].reshape(1, 1, 1),
+                             torch.tensor([0, 3], dtype=torch.int32).cuda(), dtype=torch.float32)
+    mag = torch.full((3, 128), 16 * 2.0 ** 16 + 112 * 4.0, dtype=torch.float64, device="cuda")
+    close(y, torch.full_like(mag, 448.0), mag, 128, "f32")
