@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
         return p.x + ((uint32_t)src < (uint32_t)p.x_rows ? src : 0) * kp;
     });
     lb.start(wave, lane, [&](int r) { return p.w + (group * p.N + min(j0 + r, p.N - 1)) * kp; });
-    const int32_t steps = some ? p.kb : 0;
+    const int32_t steps = some && p.x_rows > 0 ? p.kb : 0; // (an x without rows is not looked at)
     constexpr int LOADS = LoadA::N + LoadB::N;
     auto fetch = [&](int s, int at) {
         la.fetch(lds + at * STAGE, wave, lane, F8_BLOCK);

@@ -52,3 +52,26 @@ def test_8_bit_sums_keep_what_is_small_beside_what_cancels():
                              torch.tensor([0, 3], dtype=torch.int32).cuda(), dtype=torch.float32)
     mag = torch.full((3, 128), 16 * 2.0 ** 16 + 112 * 4.0, dtype=torch.float64, device="cuda")
     close(y, torch.full_like(mag, 448.0), mag, 128, "f32")
+
+
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("size", [(9, 3, 40, 20), (300, 4, 264, 136), (2700, 20, 256, 1024), (6200, 8, 512, 1024)], ids=str)
+def test_an_x_without_rows_counts_as_zeros(size, dtype):
+    """Every row comes through an index into nothing: the biases are left, and zeros for rows of no network."""
+    m, e, k, n = size
+    off, rows = split(m, e, "tail", 1).cuda(), torch.arange(m, dtype=torch.int32).cuda() - m // 2
+    x, b = torch.empty(0, k, dtype=DT[dtype], device="cuda"), rand(2, e, n).to(DT[dtype]).cuda()
+    w, dy = rand(3, e, k, n).to(DT[dtype]).cuda(), rand(4, m, n).to(DT[dtype]).cuda()
+    want, wdb, mag = torch.zeros(m, n, dtype=DT[dtype], device="cuda"), torch.zeros(e, n, dtype=torch.float64, device="cuda"), torch.zeros(e, n, dtype=torch.float64, device="cuda")
+    for i, (p, q) in enumerate(zip(off[:-1].tolist(), off[1:].tolist())):
+        want[p:q], wdb[i], mag[i] = b[i], dy[p:q].double().sum(0), dy[p:q].double().abs().sum(0)
+    for relu in (False, True):
+        y = kn.grouped_linear(x, w, off, rows=rows, bias=b, relu=relu)
+        assert torch.equal(y, want.relu() if relu else want)
+        y = kn.grouped_linear_f8(*kn.quantize_f8(x), *kn.quantize_f8_weights(w), off, rows=rows, bias=b, relu=relu, dtype=DT[dtype])
+        assert torch.equal(y, want.relu() if relu else want)
+    dw, db = kn.grouped_linear_dw(dy, x, w, off, rows=rows)
+    assert not dw.any()
+    close(db, wdb, mag, m, dtype)
