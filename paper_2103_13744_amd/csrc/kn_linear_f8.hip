@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
     const float *ws = p.ws + (group * ((p.N + F8_BLOCK - 1) / F8_BLOCK) + j0 / F8_BLOCK) * p.kb;
     const int wi = (wave / WC) * (BM / WR), wj = (wave % WC) * WN;
     const float *xs[U]; // this lane's row's scales, from its own of four on
-    bool there[U];      // (rows that x does not have count as zeros)
+    bool there[U];      // (a row that x does not have goes through with row 0's values, and is zeros in the end: a product with zero would keep a NaN)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int32_t i = min(piece.begin + wi + 16 * u + (lane & 15), piece.end - 1), src = p.rows ? p.rows[i] : i;
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
             if (s + NB - 1 < steps) fetch(s + NB - 1, at == 0 ? NB - 1 : at - 1);
             if (s % 4 == 0) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) factor[u] = there[u] ? asked[u] * asked_w : 0.0f;
+                for (int u = 0; u < U; ++u) factor[u] = asked[u] * asked_w;
                 if (s + 4 < steps) ask(s + 4);
             }
             const KN_LDS char *ta = lds + at * STAGE, *tb = ta + BM * 128;
@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) *(KN_LDS kn_f32x4 *)(mine + (lane & 15) * LD + 16 * v + (lane >> 4) * 4) = acc[u][v];
+        for (int v = 0; v < V; ++v) *(KN_LDS kn_f32x4 *)(mine + (lane & 15) * LD + 16 * v + (lane >> 4) * 4) = there[u] ? acc[u][v] : kn_f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int h = 0; h < (16 * LR + 63) / 64; ++h) {
             const int r = h * (64 / LR) + lane / LR;

@@ -75,3 +75,27 @@ def test_an_x_without_rows_counts_as_zeros(size, dtype):
     dw, db = kn.grouped_linear_dw(dy, x, w, off, rows=rows)
     assert not dw.any()
     close(db, wdb, mag, m, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("size", [(9, 3, 40, 20), (300, 4, 264, 136), (2700, 20, 256, 1024), (6200, 8, 512, 1024)], ids=str)
+def test_rows_out_of_range_take_nothing_from_row_0(size, dtype):
+    """Row 0 of x holds NaN and infinities (which become NaN in 8 bits); an entry that x does not have is a row of zeros all the same, and
+    row 0's own results are NaN."""
+    m, e, k, n = size
+    off, x_rows = split(m, e, "tail", 1).cuda(), 50
+    rows = torch.randint(-4, x_rows + 4, (m,), generator=torch.Generator().manual_seed(5), dtype=torch.int32).cuda()
+    x, w, b = rand(2, x_rows, k).to(DT[dtype]).cuda(), rand(3, e, k, n).to(DT[dtype]).cuda(), rand(4, e, n).to(DT[dtype]).cuda()
+    x[0] = math.inf
+    x[0, 1::2] = math.nan
+    inside = torch.arange(m, device="cuda") < off[-1]
+    out, first = (inside & ((rows < 0) | (rows >= x_rows))).nonzero()[:, 0], (inside & (rows == 0)).nonzero()[:, 0]
+    net = torch.searchsorted(off, torch.arange(m, dtype=torch.int32, device="cuda"), right=True) - 1
+    assert len(out) > 0 and (len(first) > 0 or m < 50)
+    for y in (kn.grouped_linear(x, w, off, rows=rows, bias=b),
+              kn.grouped_linear_f8(*kn.quantize_f8(x), *kn.quantize_f8_weights(w), off, rows=rows, bias=b, dtype=DT[dtype])):
+        assert torch.equal(y[out], b[net[out]]) and torch.isnan(y[first]).all() and not y[~inside].any()
+        assert torch.isfinite(y[inside & (rows != 0)]).all()
+    dw, db = kn.grouped_linear_dw(rand(6, m, n).to(DT[dtype]).cuda(), x, w, off, rows=torch.where(rows == 0, -1, rows).contiguous())
+    assert torch.isfinite(dw).all() and torch.isfinite(db).all()
