@@ -392,7 +392,8 @@ int kn_grouped_linear_dw(void *stream, const kn_linear_desc *desc, const void *x
  * kn_quantize_f8_weights: w -> q (dev, E * N * kb*128 bytes, input innermost) and scales (dev, E * ceil(N/128) * kb), one per
  * 128 outputs x 128 inputs.  To be done once per weights.  q 16-byte aligned.
  * kn_grouped_linear_f8: y[i] = act(sum over blocks of s_x s_w (q_x q_w) + b_e); y of desc's dtype.  The products of 8-bit
- * values are exact, a block's are summed in fp32, and so are the blocks. */
+ * values are exact, a block's are summed in fp32, and so are the blocks.  desc's w_layout and ldx are not looked at: xq and wq lie as
+ * the quantisers leave them. */
 int kn_quantize_f8(void *stream, const void *x, int32_t dtype, int64_t R, int32_t K, int64_t ld, void *q, float *scales);
 int kn_quantize_f8_weights(void *stream, const void *w, int32_t dtype, int32_t w_layout, int32_t experts, int32_t n_in,
                            int32_t n_out, void *q, float *scales);

@@ -608,6 +608,8 @@ def quantize_f8_weights(w):
 def grouped_linear_f8(xq, xs, wq, ws, offsets, rows=None, bias=None, relu=False, dtype=None, out=None):
     """``grouped_linear`` on what ``quantize_f8`` and ``quantize_f8_weights`` gave; the result is of ``dtype`` (bfloat16)."""
     L = load_library()
+    if wq.dim() != 3 or wq.shape[2] % 128:
+        raise KnError("expected weights (experts, n_out, whole blocks of 128 inputs) as quantize_f8_weights gives them, got %s" % (tuple(wq.shape),))
     E, N, kp = wq.shape
     X, kb, f8, f = xq.shape[0], kp // 128, torch.float8_e4m3fn, torch.float32
     dtype = (torch.bfloat16 if dtype is None else dtype) if out is None else out.dtype

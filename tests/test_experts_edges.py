@@ -99,3 +99,13 @@ def test_rows_out_of_range_take_nothing_from_row_0(size, dtype):
         assert torch.isfinite(y[inside & (rows != 0)]).all()
     dw, db = kn.grouped_linear_dw(rand(6, m, n).to(DT[dtype]).cuda(), x, w, off, rows=torch.where(rows == 0, -1, rows).contiguous())
     assert torch.isfinite(dw).all() and torch.isfinite(db).all()
+
+
+def test_8_bit_weights_of_no_whole_blocks_are_refused():
+    """The library would count a block more than the shapes that are checked have.  (Looked at before any address: no device needed.)"""
+    for shape in ((2, 8, 200), (2, 8, 127), (2, 8, 1), (8, 256)):
+        wq = torch.zeros(shape).to(torch.float8_e4m3fn)
+        kb = shape[-1] // 128
+        xq, xs, ws = torch.zeros(4, kb * 128).to(torch.float8_e4m3fn), torch.ones(4, kb), torch.ones(2, 1, kb)
+        with pytest.raises(kn.KnError, match="whole blocks of 128"):
+            kn.grouped_linear_f8(xq, xs, wq, ws, torch.zeros(3, dtype=torch.int32))
