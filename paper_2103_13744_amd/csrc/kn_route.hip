@@ -477,7 +477,7 @@ __global__ void __launch_bounds__(256) k_combine_backward(const T *__restrict__ 
     }
 }
 
-bool route_supported(int64_t T, int32_t E, int32_t k) { return E <= ROUTE_MAX_EXPERTS && k <= ROUTE_MAX_K && T * k <= KN_MAX_ROWS; }
+bool route_supported(int64_t T, int32_t E, int32_t k) { return E <= ROUTE_MAX_EXPERTS && k <= ROUTE_MAX_K && T <= KN_MAX_ROWS && T * k <= KN_MAX_ROWS; }
 bool route_valid(int64_t T, int32_t E, int32_t k) { return T >= 0 && E >= 1 && k >= 1 && k <= E; }
 
 // Calls f with the lanes that take a row of E logits and the logits that each of them holds.
@@ -568,7 +568,7 @@ extern "C" int kn_route_backward(void *stream, const void *logits, int32_t dtype
 static int combine_check(int32_t dtype, int64_t M, int64_t D, int64_t T, int32_t k)
 {
     if (M < 0 || D < 1 || T < 0 || k < 1 || !kn_dtype_ok(dtype)) return KN_E_INVALID_ARG;
-    if (M > KN_MAX_ROWS || D > KN_MAX_WIDTH || T * k > KN_MAX_ROWS) return KN_E_UNSUPPORTED;
+    if (M > KN_MAX_ROWS || D > KN_MAX_WIDTH || T > KN_MAX_ROWS || T * k > KN_MAX_ROWS) return KN_E_UNSUPPORTED;
     return KN_OK;
 }
 static bool whole_pieces(int64_t D, int32_t dtype, const void *a, const void *b, const void *c)

@@ -1,5 +1,6 @@
 """Networks chosen per row: inputs at the edge of what the calls take, against plain implementations in 64 bits.  Bounds as in
 test_experts.py."""
+import ctypes as C
 import math
 
 import pytest
@@ -109,3 +110,15 @@ def test_8_bit_weights_of_no_whole_blocks_are_refused():
         xq, xs, ws = torch.zeros(4, kb * 128).to(torch.float8_e4m3fn), torch.ones(4, kb), torch.ones(2, 1, kb)
         with pytest.raises(kn.KnError, match="whole blocks of 128"):
             kn.grouped_linear_f8(xq, xs, wq, ws, torch.zeros(3, dtype=torch.int32))
+
+
+def test_products_of_counts_beyond_64_bits_are_refused():
+    """rows x choices is a multiple of 2^64 here: too many all the same.  (No device needed.)"""
+    L, n, p = kn.load_library(), C.c_int64(), 4096  # (an address that is never dereferenced)
+    for t, k in ((1 << 59, 32), (1 << 60, 16), ((1 << 59) + (1 << 58), 32)):
+        assert L.kn_route_workspace_bytes(t, 100, k, C.byref(n)) == -2
+        assert L.kn_route(None, p, 0, t, 100, 100, k, 1, p, p, p, p, p, p, 1 << 40) == -2
+        assert L.kn_route_backward(None, p, 0, t, 100, 100, k, 1, p, p, p, p) == -2
+    for t, k in ((1 << 40, 1 << 30), (1 << 33, 1 << 30), (1 << 59, 32)):
+        assert L.kn_combine(None, p, 0, 4, 8, p, p, t, k, p) == -2
+        assert L.kn_combine_backward(None, p, p, 0, 4, 8, p, p, t, k, p, p) == -2
