@@ -31,6 +31,19 @@ template <typename F> static inline int kn_with_type(int32_t dtype, F &&f)
     return f((__bf16)0.0f);
 }
 
+// Calls f(workgroups, number of the first) for so many workgroups.  A launch holds less than 2^32 threads: the runtime takes more without a
+// word and runs what is left of them modulo 2^32.  (Launches begin at a multiple of eight: a workgroup's XCD goes by its number.)
+template <typename F> static inline int kn_launch(int64_t blocks, int threads, F &&f)
+{
+    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
+    const int64_t most = (0xffffffffLL / threads) & ~7LL;
+    for (int64_t first = 0; first < blocks; first += most) {
+        f(dim3((unsigned)(blocks - first < most ? blocks - first : most)), (int32_t)first);
+        KN_CHECK_LAUNCH();
+    }
+    return KN_OK;
+}
+
 // Rows of one network among the sorted rows: where a workgroup's piece lies.
 struct KnPiece {
     int32_t group;   // the network, or E: rows of no network
@@ -103,6 +116,7 @@ struct KnProduct {
     int32_t M, E, I, J, C;           // rows, networks; weight gradient: rows of out_e; columns of out; contraction
     int32_t a_rows, b_rows, m_rows;  // rows that a, b (weight gradient) and the mask have (an index outside is a row of zeros)
     int32_t relu;
+    int32_t first;                   // number of the launch's first workgroup
 };
 
 // What the grouped products check alike

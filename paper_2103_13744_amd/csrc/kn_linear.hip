@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
     const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ntiles = (p.J + BN - 1) / BN;
     // (where a network has a piece or none, its columns go to all XCDs: only some networks have rows, XCDs should be alike)
-    const int32_t number = p.M < (int64_t)BM * p.E ? kn_block() : kn_xcd_order(kn_block(), blocks);
+    const int32_t number = p.M < (int64_t)BM * p.E ? p.first + kn_block() : kn_xcd_order(p.first + kn_block(), blocks);
     const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, BM, number / ntiles);
     const int j0 = number % ntiles * BN;
     if (piece.begin >= piece.end) return;
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p)
     __shared__ __align__(16) float red[FEW_WAVES * 16 * LD];
     const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ntiles = (p.J + BN - 1) / BN;
-    const int32_t number = kn_block(); // (a network's columns over all XCDs: there is nothing to share but a few rows)
+    const int32_t number = p.first + kn_block(); // (a network's columns over all XCDs: there is nothing to share but a few rows)
     const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, 16, number / ntiles);
     const int j0 = number % ntiles * BN;
     if (piece.begin >= piece.end) return;
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
     __shared__ __align__(16) T rows_of[SMALL_WAVES][16 * 16 * V + W]; // 16 rows of results of a wavefront, as they follow one another
     const int lane = kn_thread() & 63, col = lane & 15, g = lane >> 4;
     T *line = rows_of[kn_thread() >> 6];
-    const int32_t number = __builtin_amdgcn_readfirstlane(kn_block() * SMALL_WAVES + (kn_thread() >> 6));
+    const int32_t number = __builtin_amdgcn_readfirstlane((p.first + kn_block()) * SMALL_WAVES + (kn_thread() >> 6));
     const int ntiles = (p.J + 16 * V - 1) / (16 * V);
     if (number / ntiles >= pieces) return;
     const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, SMALL_ROWS, number / ntiles);
@@ -450,19 +450,21 @@ template <typename T, bool COLS> bool rows_of_pieces(const KnProduct &p)
 template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB> int launch_rows(hipStream_t st, const KnProduct &p)
 {
     const int64_t blocks = kn_pieces(p.M, p.E, BM) * kn_div_up(p.J, BN);
-    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_product_rows<T, COLS, DIRECT, BM, BN, WR, WC, NB>), dim3((unsigned)blocks), dim3(WR * WC * 64), 0, st, p, (int32_t)blocks);
-    KN_CHECK_LAUNCH();
-    return KN_OK;
+    return kn_launch(blocks, WR * WC * 64, [&](dim3 grid, int32_t first) {
+        KnProduct q = p;
+        q.first = first;
+        hipLaunchKernelGGL((k_product_rows<T, COLS, DIRECT, BM, BN, WR, WC, NB>), grid, dim3(WR * WC * 64), 0, st, q, (int32_t)blocks);
+    });
 }
 
 template <typename T> int launch_few(hipStream_t st, const KnProduct &p)
 {
     const int64_t blocks = kn_pieces(p.M, p.E, 16) * kn_div_up(p.J, 256 / (int)sizeof(T));
-    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_product_few<T>), dim3((unsigned)blocks), dim3(FEW_WAVES * 64), 0, st, p);
-    KN_CHECK_LAUNCH();
-    return KN_OK;
+    return kn_launch(blocks, FEW_WAVES * 64, [&](dim3 grid, int32_t first) {
+        KnProduct q = p;
+        q.first = first;
+        hipLaunchKernelGGL((k_product_few<T>), grid, dim3(FEW_WAVES * 64), 0, st, q);
+    });
 }
 
 // Which kernel.  Large tiles fetch least per product, small ones fill the chip; measured (bf16, us, weights not in a cache):
@@ -521,9 +523,11 @@ template <typename T, bool COLS, int KF, int V, bool ODD> int launch_small_of(hi
 {
     const int64_t pieces = kn_pieces(p.M, p.E, SMALL_ROWS), waves = pieces * kn_div_up(p.J, 16 * V);
     if (waves > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_product_small<T, COLS, KF, V, ODD>), dim3((unsigned)kn_div_up(waves, SMALL_WAVES)), dim3(SMALL_WAVES * 64), 0, st, p, (int32_t)pieces);
-    KN_CHECK_LAUNCH();
-    return KN_OK;
+    return kn_launch(kn_div_up(waves, SMALL_WAVES), SMALL_WAVES * 64, [&](dim3 grid, int32_t first) {
+        KnProduct q = p;
+        q.first = first;
+        hipLaunchKernelGGL((k_product_small<T, COLS, KF, V, ODD>), grid, dim3(SMALL_WAVES * 64), 0, st, q, (int32_t)pieces);
+    });
 }
 template <typename T, bool COLS, int KF, int V> int launch_small(hipStream_t st, const KnProduct &p)
 {

@@ -31,8 +31,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
     const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int jtiles = (p.J + BN - 1) / BN, itiles = (p.I + BM - 1) / BM;
     // (a part's tiles go to all XCDs, neighbours among them to one: networks differ in rows, XCDs should not)
-    const int32_t tiles = itiles * jtiles, number = kn_xcd_order(kn_block() % tiles, tiles);
-    const int32_t part = kn_block() / tiles;
+    const int32_t tiles = itiles * jtiles, block = p.first + kn_block(), number = kn_xcd_order(block % tiles, tiles);
+    const int32_t part = block / tiles;
     const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, parts.len, part);
     const int32_t group = piece.group;
     if (group >= p.E) return;
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(WAVES * 64) k_reduce_small(KnProduct p, int32_
     __shared__ __align__(16) float red[BM * LD];
     __shared__ float side_a[BM], side_b[BN];
     const int tid = kn_thread(), lane = tid & 63, col = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, parts.len, kn_block());
+    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, parts.len, p.first + kn_block());
     const int32_t group = piece.group;
     if (group >= p.E) return;
     const int32_t o = kn_offset(p.offsets, group, p.M), c0 = piece.begin, cend = max(c0, min(piece.end, c0 + parts.len));
@@ -248,7 +248,7 @@ template <typename T, bool SEARCH, bool SPLIT> __global__ void __launch_bounds__
     __shared__ int32_t scratch[4], found;
     __shared__ float quarter[4][64];
     const int64_t n = (int64_t)p.I * p.J;
-    const int32_t pieces = (int32_t)((n + chunk - 1) / chunk), turn = kn_block() / pieces;
+    const int32_t pieces = (int32_t)((n + chunk - 1) / chunk), block = p.first + kn_block(), turn = block / pieces;
     int32_t group = turn;
     if constexpr (SEARCH) {
         int32_t before = 0;
@@ -268,7 +268,7 @@ template <typename T, bool SEARCH, bool SPLIT> __global__ void __launch_bounds__
     const int32_t o = kn_offset(p.offsets, group, p.M), rows = kn_offset(p.offsets, group + 1, p.M) - o;
     if (rows <= parts.len) return;
     const int32_t count = (rows + parts.len - 1) / parts.len;
-    const int64_t place = 2 * (o / parts.len), first = (int64_t)(kn_block() % pieces) * chunk;
+    const int64_t place = 2 * (o / parts.len), first = (int64_t)(block % pieces) * chunk;
     T *out = (T *)p.out + (int64_t)group * p.o_group;
     if constexpr (SPLIT) {
         const int lane = kn_thread() & 63, wave = kn_thread() >> 6;
@@ -338,32 +338,34 @@ template <typename T, bool DIRECT> int launch_reduce(hipStream_t st, const kn_li
     const int bm = way == WAY_128 ? 128 : way == WAY_32 || (way == WAY_SMALL && p.I <= 32) ? 32 : 64;
     const int bn = way == WAY_128 ? 128 : way == WAY_32 ? 32 : way == WAY_64 || p.J > 48 ? 64 : p.J > 32 ? 48 : p.J > 16 ? 32 : 16;
     const int64_t blocks = kn_pieces(p.M, p.E, parts.len) * kn_div_up(p.I, bm) * kn_div_up(p.J, bn);
-    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    const dim3 grid((unsigned)blocks);
-    if (way == WAY_128) {
-        if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 128, 128, 2, 4>), grid, dim3(512), 0, st, p, sum, parts);
-    } else if (way == WAY_64) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 64, 64, 2, 2>), grid, dim3(256), 0, st, p, sum, parts);
-    else if (way == WAY_32) {
-        if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 32, 32, 2, 2>), grid, dim3(256), 0, st, p, sum, parts);
-    } else if constexpr (!DIRECT) {
-        const int64_t each = d->rows / d->experts;
-        const bool alone = each < 32 || (each < 256 && d->experts >= 1024);
+    const int64_t each = d->rows / d->experts;
+    const bool alone = way == WAY_SMALL && (each < 32 || (each < 256 && d->experts >= 1024));
+    const int status = kn_launch(blocks, way == WAY_128 ? 512 : alone ? 64 : 256, [&](dim3 grid, int32_t first) {
+        KnProduct q = p;
+        q.first = first;
+        if (way == WAY_128) {
+            if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 128, 128, 2, 4>), grid, dim3(512), 0, st, q, sum, parts);
+        } else if (way == WAY_64) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 64, 64, 2, 2>), grid, dim3(256), 0, st, q, sum, parts);
+        else if (way == WAY_32) {
+            if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 32, 32, 2, 2>), grid, dim3(256), 0, st, q, sum, parts);
+        } else if constexpr (!DIRECT) {
 #define KN_SMALL(U, V)                                                                                                                      \
-    if (alone) hipLaunchKernelGGL((k_reduce_small<T, U, V, 1>), grid, dim3(64), 0, st, p, sum, parts);                                      \
-    else hipLaunchKernelGGL((k_reduce_small<T, U, V, 4>), grid, dim3(256), 0, st, p, sum, parts)
-        switch (bm + bn / 16) {
-        case 33: KN_SMALL(2, 1); break;
-        case 34: KN_SMALL(2, 2); break;
-        case 35: KN_SMALL(2, 3); break;
-        case 36: KN_SMALL(2, 4); break;
-        case 65: KN_SMALL(4, 1); break;
-        case 66: KN_SMALL(4, 2); break;
-        case 67: KN_SMALL(4, 3); break;
-        default: KN_SMALL(4, 4);
-        }
+    if (alone) hipLaunchKernelGGL((k_reduce_small<T, U, V, 1>), grid, dim3(64), 0, st, q, sum, parts);                                      \
+    else hipLaunchKernelGGL((k_reduce_small<T, U, V, 4>), grid, dim3(256), 0, st, q, sum, parts)
+            switch (bm + bn / 16) {
+            case 33: KN_SMALL(2, 1); break;
+            case 34: KN_SMALL(2, 2); break;
+            case 35: KN_SMALL(2, 3); break;
+            case 36: KN_SMALL(2, 4); break;
+            case 65: KN_SMALL(4, 1); break;
+            case 66: KN_SMALL(4, 2); break;
+            case 67: KN_SMALL(4, 3); break;
+            default: KN_SMALL(4, 4);
+            }
 #undef KN_SMALL
-    }
-    KN_CHECK_LAUNCH();
+        }
+    });
+    KN_TRY(status);
     if (p.M <= parts.len) return KN_OK; // (no network has several)
     const int64_t most = p.M / parts.len, results = (int64_t)p.I * p.J;
     const bool few = results * (most < p.E ? most : p.E) <= 1 << 20 && p.E * kn_div_up(results, 256) <= 8192;
@@ -371,11 +373,12 @@ template <typename T, bool DIRECT> int launch_reduce(hipStream_t st, const kn_li
     const int64_t pieces = kn_div_up(results, chunk);
     const bool search = most < p.E && p.E * pieces > 8192;
     const int64_t joins = (search ? most : p.E) * pieces;
-    if (joins > 0x7fffffffLL) return KN_E_UNSUPPORTED;
     auto join = few ? (k_reduce_join<T, false, true>) : search ? (k_reduce_join<T, true, false>) : (k_reduce_join<T, false, false>); // (few: no more than 8,192 workgroups)
-    hipLaunchKernelGGL(join, dim3((unsigned)joins), dim3(256), 0, st, p, sum, parts, chunk);
-    KN_CHECK_LAUNCH();
-    return KN_OK;
+    return kn_launch(joins, 256, [&](dim3 grid, int32_t first) {
+        KnProduct q = p;
+        q.first = first;
+        hipLaunchKernelGGL(join, grid, dim3(256), 0, st, q, sum, parts, chunk);
+    });
 }
 
 } // namespace

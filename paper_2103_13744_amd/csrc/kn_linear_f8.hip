@@ -30,9 +30,9 @@ __device__ __forceinline__ float f8_row_max(float v)
 // 4.1 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(256) k_quantize_rows(const T *__restrict__ x, int64_t R, int32_t K, int64_t ld, int32_t kb,
-                                                       uint8_t *__restrict__ q, float *__restrict__ scales)
+                                                       uint8_t *__restrict__ q, float *__restrict__ scales, int32_t first)
 {
-    const int64_t g = ((int64_t)kn_block() * 256 + kn_thread()) >> 4;
+    const int64_t g = (((int64_t)first + kn_block()) * 256 + kn_thread()) >> 4;
     if (g >= R * kb) return;
     const int at = kn_thread() & 15;
     const int64_t row = g / kb;
@@ -59,12 +59,12 @@ __global__ void __launch_bounds__(256) k_quantize_rows(const T *__restrict__ x, 
 // which).  Outputs beyond N are not stored, inputs beyond K are zeros.  Done once per weights, and not tuned.
 template <typename T>
 __global__ void __launch_bounds__(256) k_quantize_weights(const T *__restrict__ w, int32_t N, int32_t K, int64_t s_n, int64_t s_k, int32_t nb,
-                                                          int32_t kb, uint8_t *__restrict__ q, float *__restrict__ scales)
+                                                          int32_t kb, uint8_t *__restrict__ q, float *__restrict__ scales, int32_t first)
 {
     constexpr int LD = F8_BLOCK + 1;
     __shared__ float t[F8_BLOCK / 2 * LD]; // half a block at a time
     __shared__ float part[4];
-    const int64_t blk = kn_block();
+    const int64_t blk = first + kn_block();
     const int32_t bk = (int32_t)(blk % kb), bn = (int32_t)(blk / kb % nb);
     const int64_t e = blk / kb / nb;
     const T *src = w + e * N * K;
@@ -104,6 +104,7 @@ struct F8Args {
     void *y;
     const int32_t *offsets, *rows;
     int32_t M, E, N, kb, x_rows, relu;
+    int32_t first; // number of the launch's first workgroup
 };
 
 // 32 values of 8 bits as 4 fragments of 8 in fp16, which holds every e4m3 value (448 down to 2^-9, NaN) exactly
@@ -150,7 +151,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
     const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ntiles = (p.N + BN - 1) / BN;
     // (where a network has a piece or none, its columns go to all XCDs: only some networks have rows, XCDs should be alike)
-    const int32_t number = p.M < (int64_t)BM * p.E ? kn_block() : kn_xcd_order(kn_block(), blocks);
+    const int32_t number = p.M < (int64_t)BM * p.E ? p.first + kn_block() : kn_xcd_order(p.first + kn_block(), blocks);
     const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, BM, number / ntiles);
     const int j0 = number % ntiles * BN;
     if (piece.begin >= piece.end) return;
@@ -260,10 +261,11 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
 template <typename T, int BM, int BN, int WR, int WC, int NB> int launch_f8(hipStream_t st, const F8Args &p)
 {
     const int64_t blocks = kn_pieces(p.M, p.E, BM) * kn_div_up(p.N, BN);
-    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    hipLaunchKernelGGL((k_linear_f8<T, BM, BN, WR, WC, NB>), dim3((unsigned)blocks), dim3(WR * WC * 64), 0, st, p, (int32_t)blocks);
-    KN_CHECK_LAUNCH();
-    return KN_OK;
+    return kn_launch(blocks, WR * WC * 64, [&](dim3 grid, int32_t first) {
+        F8Args q = p;
+        q.first = first;
+        hipLaunchKernelGGL((k_linear_f8<T, BM, BN, WR, WC, NB>), grid, dim3(WR * WC * 64), 0, st, q, (int32_t)blocks);
+    });
 }
 
 } // namespace
@@ -275,12 +277,11 @@ extern "C" int kn_quantize_f8(void *stream, const void *x, int32_t dtype, int64_
     if (R == 0) return KN_OK;
     const int32_t kb = (int32_t)kn_div_up(K, F8_BLOCK);
     const int64_t blocks = kn_div_up(R * kb, 16);
-    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
     return kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
-        hipLaunchKernelGGL((k_quantize_rows<E_>), dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, (const E_ *)x, R, K, ld, kb, (uint8_t *)q, scales);
-        KN_CHECK_LAUNCH();
-        return KN_OK;
+        return kn_launch(blocks, 256, [&](dim3 grid, int32_t first) {
+            hipLaunchKernelGGL((k_quantize_rows<E_>), grid, dim3(256), 0, (hipStream_t)stream, (const E_ *)x, R, K, ld, kb, (uint8_t *)q, scales, first);
+        });
     });
 }
 
@@ -293,14 +294,13 @@ extern "C" int kn_quantize_f8_weights(void *stream, const void *w, int32_t dtype
     if (experts > KN_MAX_EXPERTS || n_in > KN_MAX_WIDTH || n_out > KN_MAX_WIDTH) return KN_E_UNSUPPORTED;
     const int32_t nb = (int32_t)kn_div_up(n_out, F8_BLOCK), kb = (int32_t)kn_div_up(n_in, F8_BLOCK);
     const int64_t blocks = (int64_t)experts * nb * kb;
-    if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
     const bool io = w_layout == KN_W_IN_OUT;
     return kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
-        hipLaunchKernelGGL((k_quantize_weights<E_>), dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, (const E_ *)w, n_out, n_in,
-                           (int64_t)(io ? 1 : n_in), (int64_t)(io ? n_out : 1), nb, kb, (uint8_t *)q, scales);
-        KN_CHECK_LAUNCH();
-        return KN_OK;
+        return kn_launch(blocks, 256, [&](dim3 grid, int32_t first) {
+            hipLaunchKernelGGL((k_quantize_weights<E_>), grid, dim3(256), 0, (hipStream_t)stream, (const E_ *)w, n_out, n_in,
+                               (int64_t)(io ? 1 : n_in), (int64_t)(io ? n_out : 1), nb, kb, (uint8_t *)q, scales, first);
+        });
     });
 }
 

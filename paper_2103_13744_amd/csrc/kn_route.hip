@@ -81,6 +81,7 @@ struct RouteArgs {
     int32_t *hist;   // (E + 1, workgroups): pairs of each expert in each workgroup, then those before it
     int32_t *totals; // E + 1
     int32_t wide;    // a lane's logits are one aligned piece
+    int32_t blocks, first; // workgroups in all, number of the launch's first one
 };
 
 // The V logits of row t that lane `at` holds: neighbours, -infinity behind the end
@@ -263,7 +264,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route_choose(RouteArgs p)
     int32_t *count = lds, *start = count + bins, *seen = start + bins; // (start, seen: ONE only)
     for (int e = kn_thread(); e < bins; e += ROUTE_THREADS) count[e] = 0;
     __syncthreads();
-    const int32_t t0 = kn_block() * ROUTE_TOKENS, t1 = min(p.T, t0 + ROUTE_TOKENS);
+    const int32_t block = p.first + kn_block(), t0 = block * ROUTE_TOKENS, t1 = min(p.T, t0 + ROUTE_TOKENS);
     choose<T, G, V>(p, t0, t1, count, chosen);
     __syncthreads();
     if constexpr (ONE) {
@@ -274,14 +275,15 @@ __global__ void __launch_bounds__(ROUTE_THREADS) k_route_choose(RouteArgs p)
         __syncthreads();
         place(p, 0, p.T * p.k, start, seen);
     } else {
-        for (int e = kn_thread(); e < bins; e += ROUTE_THREADS) p.hist[(int64_t)e * gridDim.x + kn_block()] = count[e];
+        for (int e = kn_thread(); e < bins; e += ROUTE_THREADS) p.hist[(int64_t)e * p.blocks + block] = count[e];
     }
 }
 
 // One workgroup per expert: its pairs before each workgroup, and in all
-__global__ void __launch_bounds__(256) k_route_scan(RouteArgs p, int32_t blocks)
+__global__ void __launch_bounds__(256) k_route_scan(RouteArgs p)
 {
     __shared__ int32_t scratch[16];
+    const int32_t blocks = p.blocks;
     int32_t *h = p.hist + (int64_t)kn_block() * blocks;
     int32_t carry = 0;
     for (int32_t b0 = 0; b0 < blocks; b0 += 256) {
@@ -296,20 +298,20 @@ __global__ void __launch_bounds__(256) k_route_scan(RouteArgs p, int32_t blocks)
 
 // SCANNED: k_route_scan has been there.  Else every workgroup sums the few histograms by itself, which takes less than a launch.
 constexpr int ROUTE_FEW_BLOCKS = 64;
-template <bool SCANNED> __global__ void __launch_bounds__(ROUTE_THREADS) k_route_place(RouteArgs p, int32_t blocks)
+template <bool SCANNED> __global__ void __launch_bounds__(ROUTE_THREADS) k_route_place(RouteArgs p)
 {
     extern __shared__ int32_t lds[];
     __shared__ int32_t scratch[16];
-    const int bins = p.E + 1;
+    const int32_t bins = p.E + 1, blocks = p.blocks, block = p.first + kn_block();
     int32_t *start = lds, *seen = start + bins, *total = seen; // (the totals are read before `seen` is written)
     for (int e = kn_thread(); e < bins; e += ROUTE_THREADS) {
         const int32_t *h = p.hist + (int64_t)e * blocks;
         if constexpr (SCANNED) {
-            start[e] = h[kn_block()];
+            start[e] = h[block];
         } else {
             int32_t before = 0, all = 0;
             for (int b = 0; b < blocks; ++b) {
-                before += b < kn_block() ? h[b] : 0;
+                before += b < block ? h[b] : 0;
                 all += h[b];
             }
             start[e] = before;
@@ -317,9 +319,9 @@ template <bool SCANNED> __global__ void __launch_bounds__(ROUTE_THREADS) k_route
         }
     }
     __syncthreads();
-    scan_counts(p, SCANNED ? p.totals : total, start, scratch, kn_block() == 0);
+    scan_counts(p, SCANNED ? p.totals : total, start, scratch, block == 0);
     __syncthreads();
-    const int32_t p0 = kn_block() * ROUTE_TOKENS * p.k;
+    const int32_t p0 = block * ROUTE_TOKENS * p.k;
     place(p, p0, (int32_t)min((int64_t)p.T * p.k, (int64_t)p0 + ROUTE_TOKENS * p.k), start, seen);
 }
 
@@ -338,7 +340,7 @@ __global__ void __launch_bounds__(256) k_route_backward(RouteArgs p, const float
     __shared__ float lds[256 * V];
     const int lane = kn_thread() & 63, at = lane & (G - 1);
     float *row = lds + (kn_thread() & ~(G - 1)) * V; // (of one wavefront alone)
-    const int32_t t = kn_block() * (256 / G) + kn_thread() / G;
+    const int32_t t = (p.first + kn_block()) * (256 / G) + kn_thread() / G;
     const bool there = t < p.T;
     const float other = __int_as_float(0x7fc00001); // marks an expert that was not chosen (no product here has these bits)
 #pragma unroll
@@ -414,11 +416,11 @@ template <typename T, int V, bool WHOLE> struct RowPiece {
 constexpr int64_t COMBINE_STREAM = 1 << 26; // bytes of y
 template <typename T, int V, bool WHOLE, bool STREAM>
 __global__ void __launch_bounds__(256) k_combine(const T *__restrict__ y, const int32_t *__restrict__ slots, const float *__restrict__ weights,
-                                                 int32_t M, int32_t D, int32_t Tn, int32_t k, T *__restrict__ out)
+                                                 int32_t M, int32_t D, int32_t Tn, int32_t k, T *__restrict__ out, int32_t first)
 {
     typedef typename RowPiece<T, V, WHOLE>::Type Piece;
     const int32_t pieces = (D + V - 1) / V;
-    const int64_t q = (int64_t)kn_block() * 256 + kn_thread();
+    const int64_t q = ((int64_t)first + kn_block()) * 256 + kn_thread();
     if (q >= (int64_t)Tn * pieces) return;
     const int32_t t = (int32_t)(q / pieces), c = WHOLE ? (int32_t)(q % pieces) * V : min((int32_t)(q % pieces) * V, D - V);
     float acc[V] = {};
@@ -445,11 +447,11 @@ __global__ void __launch_bounds__(256) k_combine(const T *__restrict__ y, const 
 template <typename T, int V, bool WHOLE>
 __global__ void __launch_bounds__(256) k_combine_backward(const T *__restrict__ dout, const T *__restrict__ y, const int32_t *__restrict__ slots,
                                                           const float *__restrict__ weights, int32_t M, int32_t D, int64_t pairs, int32_t k,
-                                                          T *__restrict__ dy, float *__restrict__ dweights)
+                                                          T *__restrict__ dy, float *__restrict__ dweights, int32_t first)
 {
     typedef typename RowPiece<T, V, WHOLE>::Type Piece;
     const int lane = kn_thread() & 63;
-    const int64_t q = (int64_t)kn_block() * 4 + (kn_thread() >> 6);
+    const int64_t q = ((int64_t)first + kn_block()) * 4 + (kn_thread() >> 6);
     if (q >= pairs) return;
     const int32_t s = slots[q];
     const bool there = (uint32_t)s < (uint32_t)M;
@@ -523,27 +525,29 @@ extern "C" int kn_route(void *stream, const void *logits, int32_t dtype, int64_t
     KN_TRY(kn_route_workspace_bytes(T, E, k, &need));
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return KN_E_WORKSPACE;
     const int32_t blocks = (int32_t)kn_div_up(T, ROUTE_TOKENS);
-    RouteArgs p = {logits, ld, (int32_t)T, E, k, renormalize != 0, weights, ids, slots, rows, offsets, (int32_t *)workspace, (int32_t *)workspace + (int64_t)blocks * (E + 1), 0};
+    RouteArgs p = {logits, ld, (int32_t)T, E, k, renormalize != 0, weights, ids, slots, rows, offsets, (int32_t *)workspace, (int32_t *)workspace + (int64_t)blocks * (E + 1), 0, blocks, 0};
     const size_t seen = (size_t)(ROUTE_THREADS / 64) * (E + 1) * 4, bins = (size_t)(E + 1) * 4;
     KN_TRY(kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
         return route_shape(E, [&](auto g, auto n) -> int {
             constexpr int G = decltype(g)::n, V = decltype(n)::n;
             p.wide = route_wide(logits, ld, E, V, sizeof(E_));
-            if (blocks == 1) hipLaunchKernelGGL((k_route_choose<E_, G, V, true>), dim3(1), dim3(ROUTE_THREADS), 2 * bins + seen, st, p);
-            else hipLaunchKernelGGL((k_route_choose<E_, G, V, false>), dim3(blocks), dim3(ROUTE_THREADS), bins, st, p);
-            KN_CHECK_LAUNCH();
-            return KN_OK;
+            return kn_launch(blocks, ROUTE_THREADS, [&](dim3 grid, int32_t first) {
+                p.first = first;
+                if (blocks == 1) hipLaunchKernelGGL((k_route_choose<E_, G, V, true>), grid, dim3(ROUTE_THREADS), 2 * bins + seen, st, p);
+                else hipLaunchKernelGGL((k_route_choose<E_, G, V, false>), grid, dim3(ROUTE_THREADS), bins, st, p);
+            });
         });
     }));
     if (blocks == 1) return KN_OK;
     if (blocks > ROUTE_FEW_BLOCKS) {
-        hipLaunchKernelGGL(k_route_scan, dim3(E + 1), dim3(256), 0, st, p, blocks);
+        hipLaunchKernelGGL(k_route_scan, dim3(E + 1), dim3(256), 0, st, p);
         KN_CHECK_LAUNCH();
     }
-    hipLaunchKernelGGL(blocks > ROUTE_FEW_BLOCKS ? k_route_place<true> : k_route_place<false>, dim3(blocks), dim3(ROUTE_THREADS), bins + seen, st, p, blocks);
-    KN_CHECK_LAUNCH();
-    return KN_OK;
+    return kn_launch(blocks, ROUTE_THREADS, [&](dim3 grid, int32_t first) {
+        p.first = first;
+        hipLaunchKernelGGL(blocks > ROUTE_FEW_BLOCKS ? k_route_place<true> : k_route_place<false>, grid, dim3(ROUTE_THREADS), bins + seen, st, p);
+    });
 }
 
 extern "C" int kn_route_backward(void *stream, const void *logits, int32_t dtype, int64_t T, int32_t E, int64_t ld, int32_t k, int32_t renormalize,
@@ -552,15 +556,16 @@ extern "C" int kn_route_backward(void *stream, const void *logits, int32_t dtype
     if (!route_valid(T, E, k) || !kn_dtype_ok(dtype) || ld < E || (T > 0 && (!logits || !weights || !ids || !dweights || !dlogits))) return KN_E_INVALID_ARG;
     if (!route_supported(T, E, k)) return KN_E_UNSUPPORTED;
     if (T == 0) return KN_OK;
-    RouteArgs p = {logits, ld, (int32_t)T, E, k, renormalize != 0, const_cast<float *>(weights), const_cast<int32_t *>(ids), nullptr, nullptr, nullptr, nullptr, nullptr, 0};
+    RouteArgs p = {logits, ld, (int32_t)T, E, k, renormalize != 0, const_cast<float *>(weights), const_cast<int32_t *>(ids), nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0, 0};
     return kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
         return route_shape(E, [&](auto g, auto n) -> int {
             constexpr int G = decltype(g)::n, V = decltype(n)::n;
             p.wide = route_wide(logits, ld, E, V, sizeof(E_)) && route_wide(dlogits, E, E, V, sizeof(E_));
-            hipLaunchKernelGGL((k_route_backward<E_, G, V>), dim3((unsigned)kn_div_up(T, 256 / G)), dim3(256), 0, (hipStream_t)stream, p, dweights, (E_ *)dlogits);
-            KN_CHECK_LAUNCH();
-            return KN_OK;
+            return kn_launch(kn_div_up(T, 256 / G), 256, [&](dim3 grid, int32_t first) {
+                p.first = first;
+                hipLaunchKernelGGL((k_route_backward<E_, G, V>), grid, dim3(256), 0, (hipStream_t)stream, p, dweights, (E_ *)dlogits);
+            });
         });
     });
 }
@@ -587,13 +592,11 @@ extern "C" int kn_combine(void *stream, const void *y, int32_t dtype, int64_t M,
         constexpr int V = 16 / sizeof(E_);
         const bool wide = whole_pieces(D, dtype, y, out, nullptr);
         const int64_t blocks = kn_div_up(T * (D < V ? D : kn_div_up(D, V)), 256);
-        if (blocks > 0x7fffffffLL) return KN_E_UNSUPPORTED;
         auto kernel = D < V ? k_combine<E_, 1, true, false> : !wide ? k_combine<E_, V, false, false>
                     : M * D * (int64_t)sizeof(E_) < COMBINE_STREAM ? k_combine<E_, V, true, false> : k_combine<E_, V, true, true>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, (const E_ *)y, slots, weights, (int32_t)M, D, (int32_t)T,
-                           k, (E_ *)out);
-        KN_CHECK_LAUNCH();
-        return KN_OK;
+        return kn_launch(blocks, 256, [&](dim3 grid, int32_t first) {
+            hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, (const E_ *)y, slots, weights, (int32_t)M, D, (int32_t)T, k, (E_ *)out, first);
+        });
     });
 }
 
@@ -608,9 +611,9 @@ extern "C" int kn_combine_backward(void *stream, const void *dout, const void *y
         constexpr int V = 16 / sizeof(E_);
         auto kernel = D < V ? k_combine_backward<E_, 1, true>
                     : whole_pieces(D, dtype, dout, dweights ? y : nullptr, dy) ? k_combine_backward<E_, V, true> : k_combine_backward<E_, V, false>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)kn_div_up(T * k, 4)), dim3(256), 0, (hipStream_t)stream, (const E_ *)dout, (const E_ *)y, slots,
-                           weights, (int32_t)M, D, T * k, k, (E_ *)dy, dweights);
-        KN_CHECK_LAUNCH();
-        return KN_OK;
+        return kn_launch(kn_div_up(T * k, 4), 256, [&](dim3 grid, int32_t first) {
+            hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, (const E_ *)dout, (const E_ *)y, slots, weights, (int32_t)M, D, T * k, k,
+                               (E_ *)dy, dweights, first);
+        });
     });
 }

@@ -122,3 +122,82 @@ def test_products_of_counts_beyond_64_bits_are_refused():
     for t, k in ((1 << 40, 1 << 30), (1 << 33, 1 << 30), (1 << 59, 32)):
         assert L.kn_combine(None, p, 0, 4, 8, p, p, t, k, p) == -2
         assert L.kn_combine_backward(None, p, p, 0, 4, 8, p, p, t, k, p, p) == -2
+
+
+# ---------------------------------------------------------------------------------------------
+# Calls of 2^32 threads and more: a launch's threads are counted in 32 bits
+@pytest.mark.gpu
+def test_weighted_sum_of_more_pairs_than_a_launch_has():
+    t = (1 << 25) + 3
+    y = (torch.arange(2 * t, device="cuda") % 251).bfloat16().reshape(-1, 1)
+    slots = (2 * t - 1 - torch.arange(2 * t, dtype=torch.int32, device="cuda")).reshape(t, 2)
+    dout = (torch.arange(t, device="cuda") % 127).bfloat16().reshape(-1, 1)
+    dy, dw = kn.combine_backward(dout, y, slots)
+    assert torch.equal(dw, dout.float() * y.float().flip(0).reshape(t, 2))
+    assert torch.equal(dy.flip(0).reshape(t, 2), dout.expand(t, 2))
+    del dy, dw, slots, dout
+    t, d = (1 << 32) // 7 + 1000, 7
+    y = torch.arange(1000 * d, device="cuda").remainder(251).bfloat16().reshape(1000, d)
+    slots = (torch.arange(t, device="cuda") % 1000).to(torch.int32).reshape(t, 1)
+    out = kn.combine(y, slots)
+    n = t // 1000
+    assert torch.equal(out[:n * 1000].reshape(n, 1000, d), y.expand(n, 1000, d)) and torch.equal(out[n * 1000:], y[:t - n * 1000])
+
+
+@pytest.mark.gpu
+def test_router_of_more_rows_than_a_launch_has():
+    t = (1 << 29) + 70
+    logits = torch.zeros(t, 2, dtype=torch.bfloat16, device="cuda")
+    logits[::3, 1] = 1.0  # every third row goes to expert 1
+    weights, ids, slots, rows, offsets = kn.route(logits, 1, renormalize=False)
+    one = -(-t // 3)
+    assert offsets.tolist() == [0, t - one, t] and int(ids.sum()) == one and not ids[1::3].any() and bool(ids[::3].all())
+    assert torch.equal(rows[t - one:], torch.arange(0, t, 3, dtype=torch.int32, device="cuda"))
+    assert torch.equal(rows[:t - one:2], torch.arange(1, t, 3, dtype=torch.int32, device="cuda"))
+    assert torch.equal(slots[::3, 0], torch.arange(t - one, t, dtype=torch.int32, device="cuda"))
+    assert torch.equal(slots[1::3, 0], torch.arange(0, t - one, 2, dtype=torch.int32, device="cuda"))
+    del slots, rows
+    hi = math.e / (1.0 + math.e)
+    assert ((weights[::3] - hi).abs() < 1e-6).all() and ((weights[1::3] - 0.5).abs() < 1e-6).all()
+    dl = kn.route_backward(logits, weights, ids, torch.ones_like(weights), renormalize=False)
+    for at, e, p in ((0, 1, hi), (1, 0, 0.5), (2, 0, 0.5)):
+        want = torch.tensor([p * (1.0 - p) if i == e else -p * (1.0 - p) for i in (0, 1)]).bfloat16().cuda()
+        assert ((dl[at::3].float() - want.float()).abs() <= 2.0 ** -8 * 0.25).all()
+
+
+@pytest.mark.gpu
+def test_8_bit_rows_of_more_blocks_than_a_launch_has():
+    r = (1 << 28) + 100
+    x = (torch.arange(r, device="cuda") % 97).bfloat16().reshape(r, 1)
+    q, s = kn.quantize_f8(x)
+    v = q[:, 0].float() * s[:, 0]
+    assert ((v - x[:, 0].float()).abs() <= 1e-6 * x[:, 0].float()).all() and (q[-1000:, 1:].float() == 0.0).all()
+
+
+@pytest.mark.gpu
+def test_linear_of_more_tiles_than_a_launch_has():
+    """The last of very many networks that are wide one way, and very many rows of few results."""
+    e, k, n = 65535, 8, 16448
+    off = torch.zeros(e + 1, dtype=torch.int32)
+    off[1:e], off[e] = 10, 32
+    w = torch.empty((e, k, n), dtype=torch.bfloat16, device="cuda")
+    w[0], w[e - 1] = rand(1, k, n).bfloat16().cuda(), rand(2, k, n).bfloat16().cuda()
+    x, dy = rand(3, 32, k).bfloat16().cuda(), rand(4, 32, n).bfloat16().cuda()
+    y = kn.grouped_linear(x, w, off.cuda())
+    dw, db = kn.grouped_linear_dw(dy, x, w, off.cuda())
+    for g, a, b in ((0, 0, 10), (e - 1, 10, 32)):
+        xg, wg, d = x[a:b].double(), w[g].double(), dy[a:b].double()
+        close(y[a:b], xg @ wg, xg.abs() @ wg.abs(), k, "bf16")
+        xt = xg.t().contiguous()
+        close(dw[g], xt @ d, xt.abs() @ d.abs(), b - a, "bf16")
+        close(db[g], d.sum(0), d.abs().sum(0), b - a, "bf16")
+    del w
+    assert not dw[1:e - 1].any() and not db[1:e - 1].any()
+    del dw, db
+    m, k, n = (1 << 29) + 100, 256, 2
+    x, w = rand(5, 64, k).bfloat16().cuda(), rand(6, 1, k, n).bfloat16().cuda()
+    rows, off = (torch.arange(m, device="cuda") % 64).to(torch.int32), torch.tensor([0, m - 50], dtype=torch.int32).cuda()
+    y = kn.grouped_linear_f8(*kn.quantize_f8(x), *kn.quantize_f8_weights(w), off, rows=rows)
+    whole = (m - 50) // 64 * 64
+    assert torch.equal(y[:whole].reshape(-1, 64, n), y[:64].expand(whole // 64, 64, n)) and torch.isfinite(y[:64]).all() and y[:64].any(dim=1).all()
+    assert torch.equal(y[whole:m - 50], y[:m - 50 - whole]) and not y[m - 50:].any()
