@@ -375,7 +375,8 @@ int kn_grouped_linear(void *stream, const kn_linear_desc *desc, const void *x /*
                       const void *bias /*dev E*N, nullable*/, const int32_t *offsets, const int32_t *rows /*dev M, nullable*/,
                       int32_t relu, void *y /*dev M*N*/);
 /* Gradient of its inputs, a row per row of y: dx[i] = dy[i] W_e^T (with `rows`: sum them with kn_combine).  x_relu (nullable):
- * the layer's x where that is a ReLU's result; dx is then 0 where x[r] is not above 0, which is the gradient before that ReLU. */
+ * the layer's x where that is a ReLU's result; dx is then 0 where x[r] is not above 0, which is the gradient before that ReLU (x_rows
+ * 0: any address but NULL, every row is zeros). */
 int kn_grouped_linear_dx(void *stream, const kn_linear_desc *desc, const void *dy /*dev M*N*/, const void *w, const void *x_relu,
                          const int32_t *offsets, const int32_t *rows, void *dx /*dev M*K*/);
 /* Gradients of its weights and biases: dw[e] = sum over the network's rows of x[r]^T dy[i], in w's layout, and db[e] = sum of

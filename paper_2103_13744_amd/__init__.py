@@ -554,8 +554,8 @@ def grouped_linear_dx(dy, x, w, offsets, rows=None, relu_in=False):
     of x several times).  ``relu_in``: x is a ReLU's result, and the gradient is that before the ReLU."""
     L = load_library()
     d, M, px, pw, pr = _linear_desc(x, w, rows)
-    dx = x.new_empty((M, d.n_in))
-    _check(L.kn_grouped_linear_dx(_stream(), C.byref(d), _ptr(dy, x.dtype, shape=(M, d.n_out)), pw, px if relu_in else None,
+    dx = x.new_empty((M, d.n_in))  # (an x without rows has no address, which is how the library tells a mask: any other will do)
+    _check(L.kn_grouped_linear_dx(_stream(), C.byref(d), _ptr(dy, x.dtype, shape=(M, d.n_out)), pw, (px or pw) if relu_in else None,
                                   _ptr(offsets, torch.int32, shape=(d.experts + 1,)), pr if relu_in else None, dx.data_ptr()), "kn_grouped_linear_dx")
     return dx
 

@@ -80,6 +80,17 @@ def test_an_x_without_rows_counts_as_zeros(size, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("size", [(9, 3, 40, 20), (300, 4, 264, 136), (6200, 8, 512, 1024)], ids=str)
+def test_gradient_before_a_relu_without_rows_is_zero(size, dtype):
+    m, e, k, n = size
+    off, rows = split(m, e, "tail", 1).cuda(), torch.arange(m, dtype=torch.int32).cuda() - m // 2
+    x, w, dy = torch.empty(0, k, dtype=DT[dtype], device="cuda"), rand(3, e, k, n).to(DT[dtype]).cuda(), rand(4, m, n).to(DT[dtype]).cuda()
+    assert not kn.grouped_linear_dx(dy, x, w, off, rows=rows, relu_in=True).any()
+    assert kn.grouped_linear_dx(dy, x, w, off, rows=rows).any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("size", [(9, 3, 40, 20), (300, 4, 264, 136), (2700, 20, 256, 1024), (6200, 8, 512, 1024)], ids=str)
 def test_rows_out_of_range_take_nothing_from_row_0(size, dtype):
     """Row 0 of x holds NaN and infinities (which become NaN in 8 bits); an entry that x does not have is a row of zeros all the same, and
