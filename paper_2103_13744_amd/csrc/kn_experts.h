@@ -44,6 +44,10 @@ template <typename F> static inline int kn_launch(int64_t blocks, int threads, F
     return KN_OK;
 }
 
+// Between what a wavefront's lanes write to the LDS and what others of its lanes read there, and before that place is written again.  The
+// hardware keeps a wavefront's accesses in order; this holds the compiler to it.  No instruction comes of it.
+__device__ __forceinline__ void kn_lanes_meet() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
 // Rows of one network among the sorted rows: where a workgroup's piece lies.
 struct KnPiece {
     int32_t group;   // the network, or E: rows of no network

@@ -151,6 +151,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
     for (int u = 0; u < U; ++u) {
 #pragma unroll
         for (int v = 0; v < V; ++v) *(KN_LDS kn_f32x4 *)(mine + (lane & 15) * LD + 16 * v + (lane >> 4) * 4) = acc[u][v];
+        kn_lanes_meet();
 #pragma unroll
         for (int h = 0; h < (16 * LR + 63) / 64; ++h) {
             const int r = h * (64 / LR) + lane / LR;
@@ -160,6 +161,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
             float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
             finish<T>(p, some, i, j, add, y);
         }
+        kn_lanes_meet();
     }
 }
 
@@ -430,12 +432,14 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
             }
         }
         if (together) {
+            kn_lanes_meet();
             const int end = shift + min(16, piece.end - (i - col)) * p.J;
             for (int q = lane * W; q < end; q += 64 * W) {
                 if (q >= shift && q + W <= end) *(Frag *)(first + q - shift) = *(const Frag *)(line + q);
                 else
                     for (int r = max(q, shift); r < min(q + W, end); ++r) first[r - shift] = line[r];
             }
+            kn_lanes_meet();
         }
     }
 }

@@ -127,6 +127,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
     for (int u = 0; u < U; ++u) {
 #pragma unroll
         for (int v = 0; v < V; ++v) *(KN_LDS kn_f32x4 *)(mine + (lane & 15) * LD + 16 * v + (lane >> 4) * 4) = acc[u][v];
+        kn_lanes_meet();
 #pragma unroll
         for (int h = 0; h < (16 * LR + 63) / 64; ++h) {
             const int r = h * (64 / LR) + lane / LR;
@@ -140,6 +141,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
                 KnEight<T>::store(out + (int64_t)i * p.o_i, j, p.J, v);
             }
         }
+        kn_lanes_meet();
     }
 }
 

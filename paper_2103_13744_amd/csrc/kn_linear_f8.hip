@@ -239,6 +239,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
     for (int u = 0; u < U; ++u) {
 #pragma unroll
         for (int v = 0; v < V; ++v) *(KN_LDS kn_f32x4 *)(mine + (lane & 15) * LD + 16 * v + (lane >> 4) * 4) = there[u] ? acc[u][v] : kn_f32x4{0, 0, 0, 0};
+        kn_lanes_meet();
 #pragma unroll
         for (int h = 0; h < (16 * LR + 63) / 64; ++h) {
             const int r = h * (64 / LR) + lane / LR;
@@ -255,6 +256,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_linear_f8(F8Args p, int32_t bl
             }
             KnEight<T>::store(y + (int64_t)i * p.N, j, p.N, o);
         }
+        kn_lanes_meet();
     }
 }
 
