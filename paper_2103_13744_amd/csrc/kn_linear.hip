@@ -560,7 +560,7 @@ template <typename T> int launch_forward(hipStream_t st, const KnProduct &p)
     const bool cols = p.b_j == 1 && p.b_c != 1; // (one column of one input: either)
     // (us, small against tiles: 524,291 rows, 4,096 networks 64 x 64: 48 and 57 in bf16, 117 and 107 in fp32; 262,145 rows, 1,600 networks
     // 128 x 128: 79 and 50, 206 and 129; 91 x 64, whose rows are not whole pieces: 43 and 71, 103 and 123)
-    const bool tiles = (cols ? rows_of_pieces<T, true>(p) : rows_of_pieces<T, false>(p)) && p.C * p.J > (sizeof(T) == 4 ? 4095 : 4096);
+    const bool tiles = (cols ? rows_of_pieces<T, true>(p) : rows_of_pieces<T, false>(p)) && (int64_t)p.C * p.J > (sizeof(T) == 4 ? 4095 : 4096);
     if (p.C <= SMALL_MOST && p.J <= SMALL_MOST && !tiles) return cols ? launch_small_widths<T, true>(st, p) : launch_small_widths<T, false>(st, p);
     return cols ? launch_pieces<T, true>(st, p) : launch_pieces<T, false>(st, p);
 }
