@@ -7,18 +7,11 @@
 typedef float kn_f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 kn_f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 kn_bf16x8 __attribute__((ext_vector_type(8)));
-typedef int kn_i32x4 __attribute__((ext_vector_type(4)));
-typedef int kn_i32x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t kn_u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int32_t KN_MAX_EXPERTS = 65535;
 constexpr int32_t KN_MAX_WIDTH = 1 << 20;
 constexpr int64_t KN_MAX_ROWS = 1ll << 30;
-
-template <typename T> struct KnType;
-template <> struct KnType<float> { static constexpr int id = KN_F32; };
-template <> struct KnType<_Float16> { static constexpr int id = KN_F16; };
-template <> struct KnType<__bf16> { static constexpr int id = KN_BF16; };
 
 static inline int kn_item(int32_t dtype) { return dtype == KN_F32 ? 4 : 2; }
 static inline bool kn_dtype_ok(int32_t dtype) { return dtype == KN_F32 || dtype == KN_F16 || dtype == KN_BF16; }
@@ -42,6 +35,16 @@ template <typename F> static inline int kn_launch(int64_t blocks, int threads, F
         KN_CHECK_LAUNCH();
     }
     return KN_OK;
+}
+
+// Largest value among the 16 lanes of a row of the wavefront, in all of them: rotations inside the row.
+__device__ __forceinline__ float kn_row_max(float v)
+{
+    constexpr int ROW_ROR = 0x120; // dpp_ctrl encoding
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 8, 0xf, 0xf, true)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 4, 0xf, 0xf, true)));
+    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 2, 0xf, 0xf, true)));
+    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 1, 0xf, 0xf, true)));
 }
 
 // Between what a wavefront's lanes write to the LDS and what others of its lanes read there, and before that place is written again.  The
@@ -116,7 +119,7 @@ struct KnProduct {
     const int32_t *offsets, *rows, *b_index, *mask_rows; // rows: of a, b_index: of b, mask_rows: of the mask; nullable
     int64_t lda, ldb, ldm;           // row strides in elements: a, b (weight gradient), mask
     int64_t b_group, b_c, b_j;       // strides of b_e: network, contraction, column
-    int64_t o_group, o_i, o_j;       // strides of out: network (weight gradient), row, column
+    int64_t o_group, o_i;            // strides of out: network (weight gradient), row (columns are neighbours)
     int32_t M, E, I, J, C;           // rows, networks; weight gradient: rows of out_e; columns of out; contraction
     int32_t a_rows, b_rows, m_rows;  // rows that a, b (weight gradient) and the mask have (an index outside is a row of zeros)
     int32_t relu;

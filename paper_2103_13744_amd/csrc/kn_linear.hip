@@ -1,5 +1,4 @@
-// Products grouped by network with ragged sizes, and their gradients: kn_grouped_linear, kn_grouped_linear_dx,
-// kn_grouped_linear_dw.
+// Products grouped by network with ragged sizes, and the gradient of their inputs: kn_grouped_linear, kn_grouped_linear_dx.
 #include "kn_tile.h"
 
 #include <type_traits>
@@ -578,7 +577,7 @@ extern "C" int kn_grouped_linear(void *stream, const kn_linear_desc *d, const vo
     p.a = x; p.b = w; p.bias = bias; p.out = y; p.offsets = offsets; p.rows = rows;
     p.lda = d->ldx;
     p.b_group = (int64_t)d->n_in * d->n_out; p.b_c = io ? d->n_out : 1; p.b_j = io ? 1 : d->n_in;
-    p.o_i = d->n_out; p.o_j = 1;
+    p.o_i = d->n_out;
     p.M = (int32_t)d->rows; p.E = d->experts; p.J = d->n_out; p.C = d->n_in;
     p.a_rows = (int32_t)d->x_rows; p.relu = relu != 0;
     return kn_with_type(d->dtype, [&](auto v) { return launch_forward<decltype(v)>((hipStream_t)stream, p); });
@@ -595,7 +594,7 @@ extern "C" int kn_grouped_linear_dx(void *stream, const kn_linear_desc *d, const
     p.a = dy; p.b = w; p.mask = x_relu; p.out = dx; p.offsets = offsets; p.rows = nullptr;
     p.lda = d->n_out; p.ldm = d->ldx;
     p.b_group = (int64_t)d->n_in * d->n_out; p.b_c = io ? 1 : d->n_in; p.b_j = io ? d->n_out : 1;
-    p.o_i = d->n_in; p.o_j = 1;
+    p.o_i = d->n_in;
     p.M = (int32_t)d->rows; p.E = d->experts; p.J = d->n_in; p.C = d->n_out;
     p.a_rows = p.M; p.m_rows = (int32_t)d->x_rows;
     p.mask_rows = x_relu ? rows : nullptr;

@@ -412,7 +412,7 @@ extern "C" int kn_grouped_linear_dw(void *stream, const kn_linear_desc *d, const
     p.M = (int32_t)d->rows; p.E = d->experts; p.I = io ? d->n_in : d->n_out; p.J = io ? d->n_out : d->n_in;
     p.a_rows = (int32_t)(io ? d->x_rows : d->rows); p.b_rows = (int32_t)(io ? d->rows : d->x_rows);
     p.out = dw; p.out_bias = db; p.offsets = offsets;
-    p.o_group = (int64_t)d->n_in * d->n_out; p.o_i = p.J; p.o_j = 1;
+    p.o_group = (int64_t)d->n_in * d->n_out; p.o_i = p.J;
     const int32_t sum = !db ? SUM_NONE : io ? SUM_B : SUM_A;
     return kn_with_type(d->dtype, [&](auto v) -> int {
         typedef decltype(v) E_;

@@ -17,15 +17,6 @@ __device__ __forceinline__ uint32_t f8_pack(float a, float b, float c, float d, 
     int v = __builtin_amdgcn_cvt_pk_fp8_f32(a / s, b / s, 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c / s, d / s, v, true);
 }
-__device__ __forceinline__ float f8_row_max(float v)
-{
-    constexpr int ROW_ROR = 0x120; // dpp_ctrl encoding: rotation inside 16 lanes
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 8, 0xf, 0xf, false)));
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 4, 0xf, 0xf, false)));
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 2, 0xf, 0xf, false)));
-    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 1, 0xf, 0xf, false)));
-}
-
 // 16 lanes per row and block of 128 inputs, 8 values a lane.  Inputs beyond K are zeros.  Bound by its bytes: 16,411 x 2048 in bf16, 25 us,
 // 4.1 TB/s.
 template <typename T>
@@ -47,7 +38,7 @@ __global__ void __launch_bounds__(256) k_quantize_rows(const T *__restrict__ x, 
     float amax = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(v[i]));
-    const float s = f8_scale(f8_row_max(amax));
+    const float s = f8_scale(kn_row_max(amax));
     uint2 out;
     out.x = f8_pack(v[0], v[1], v[2], v[3], s);
     out.y = f8_pack(v[4], v[5], v[6], v[7], s);
@@ -73,7 +64,7 @@ __global__ void __launch_bounds__(256) k_quantize_weights(const T *__restrict__ 
         const int32_t n = bn * F8_BLOCK + (s_n == 1 ? i % F8_BLOCK : i / F8_BLOCK), k = bk * F8_BLOCK + (s_n == 1 ? i / F8_BLOCK : i % F8_BLOCK);
         if (n < N && k < K) amax = fmaxf(amax, fabsf((float)src[n * s_n + k * s_k]));
     }
-    amax = f8_row_max(amax);
+    amax = kn_row_max(amax);
     amax = fmaxf(amax, __shfl_xor(amax, 16));
     amax = fmaxf(amax, __shfl_xor(amax, 32));
     if ((kn_thread() & 63) == 0) part[kn_thread() >> 6] = amax;

@@ -11,18 +11,10 @@ constexpr int ROUTE_PAIRS = ROUTE_TOKENS * ROUTE_MAX_K;   // pairs (row, choice)
 
 template <typename T> __device__ __forceinline__ float to_float(T v) { return (float)v; }
 
-// Largest value among the 16 lanes of a row of the wavefront, in all of them: rotations inside the row.
-__device__ __forceinline__ float row_max(float v)
-{
-    constexpr int ROW_ROR = 0x120; // dpp_ctrl encoding
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 8, 0xf, 0xf, true)));
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 4, 0xf, 0xf, true)));
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 2, 0xf, 0xf, true)));
-    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 1, 0xf, 0xf, true)));
-}
+// Sum over the 16 lanes of a row of the wavefront, in all of them: rotations inside the row
 __device__ __forceinline__ float row_sum(float v)
 {
-    constexpr int ROW_ROR = 0x120;
+    constexpr int ROW_ROR = 0x120; // dpp_ctrl encoding
     v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 8, 0xf, 0xf, true));
     v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 4, 0xf, 0xf, true));
     v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ROW_ROR + 2, 0xf, 0xf, true));
@@ -31,7 +23,7 @@ __device__ __forceinline__ float row_sum(float v)
 // G = 16: a row of the wavefront works on a row of logits; 64: the whole wavefront
 template <int G> __device__ __forceinline__ float group_max(float v)
 {
-    v = row_max(v);
+    v = kn_row_max(v);
     if constexpr (G == 64) {
         v = fmaxf(v, __shfl_xor(v, 16));
         v = fmaxf(v, __shfl_xor(v, 32));
@@ -397,12 +389,6 @@ __global__ void __launch_bounds__(256) k_route_backward(RouteArgs p, const float
             if (at * V + i < p.E) out[i] = (T)d[i];
     }
 }
-
-// 16 bytes of values
-template <typename T> struct Vec {
-    static constexpr int N = 16 / sizeof(T);
-    typedef T Type __attribute__((ext_vector_type(16 / sizeof(T))));
-};
 
 // V neighbouring values of a row.  WHOLE: rows are made of such pieces, each on a multiple of its size; else they lie anywhere, and a row's
 // last piece is its last V values, some of which the piece before has too (narrower rows: V = 1).  Rows of 2,468 values, 25,295 of 2 in bf16: pieces
