@@ -397,9 +397,11 @@ template <typename T, int V, bool WHOLE> struct RowPiece {
     typedef T Type __attribute__((ext_vector_type(V), aligned((WHOLE ? V : 1) * sizeof(T))));
 };
 
-// out[t] = sum over j of weights[t, j] y[slots[t, j]]: a thread per piece of a row, 16 bytes or one value.  Bound by its bytes.  STREAM: what is read and written once goes past the caches, where
-// y does not stay in them anyway (16,384 rows of 4 x 2048 in bf16, 336 MB: 83 us without, 64 with: 5.3 TB/s).
-constexpr int64_t COMBINE_STREAM = 1 << 26; // bytes of y
+// out[t] = sum over j of weights[t, j] y[slots[t, j]]: a thread per piece of a row, 16 bytes or one value.  Bound by its bytes.  STREAM: what
+// is read and written once goes past the caches, where y does not stay in them anyway (us; kept in them, past them; rows of 4 x 2048 in
+// bf16 but where said; y of the call before or another one): 32 MiB: 8 and 9; 64: 14 and 17; 128: 26 or 33, 30 or 32; 128 (2 each): 31 or 36, 36 or
+// 37; 188 (fp32): 35 or 45, 42 or 44; 256: 68, 61 (5.5 TB/s); 256 (fp32): 66, 58; 256 (8 x 512): 65, 55; 1,024 (8 each): 242, 217.
+constexpr int64_t COMBINE_STREAM = 3 << 26; // bytes of y
 template <typename T, int V, bool WHOLE, bool STREAM>
 __global__ void __launch_bounds__(256) k_combine(const T *__restrict__ y, const int32_t *__restrict__ slots, const float *__restrict__ weights,
                                                  int32_t M, int32_t D, int32_t Tn, int32_t k, T *__restrict__ out, int32_t first)

@@ -181,12 +181,13 @@ def test_route_of_many_rows(size):
         assert ((w.double() - want).abs() <= (e + 16) * 2.0 ** -23 * want).all()
 
 
+@pytest.mark.parametrize("t", [16200, 49200])
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
-def test_combine_past_the_caches(dtype):
-    """More than 64 MiB of rows: those go past the caches."""
-    t, k, d = 16200, 4, 520 if dtype != "f32" else 264
+def test_combine_past_the_caches(dtype, t):
+    """64 MiB of rows and more, and 192 and more: those go past the caches."""
+    k, d = 4, 520 if dtype != "f32" else 264
     y, dout, w = rand(1, t * k, d).to(DT[dtype]).cuda(), rand(2, t, d).to(DT[dtype]).cuda(), rand(3, t, k).cuda()
-    assert y.numel() * y.element_size() > 1 << 26
+    assert y.numel() * y.element_size() > (1 << 26 if t < 40000 else 3 << 26)
     slots = torch.randperm(t * k, generator=torch.Generator().manual_seed(4)).to(torch.int32).reshape(t, k)
     slots[::7, 1] = -1
     slots = slots.cuda()
