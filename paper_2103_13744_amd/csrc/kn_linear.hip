@@ -554,13 +554,41 @@ template <typename T, bool COLS> int launch_small_widths(hipStream_t st, const K
     }
 }
 
+// Layers of up to SMALL_MOST by SMALL_MOST whose rows are whole pieces: by tiles or a wavefront per 32 rows (small).  Tiles share a
+// network's weights among more rows, small starts sooner and takes wide layers of few rows per network without empty rows of tiles.
+// Measured (us, small / tiles), by rows per network of 2,000, and as rows, networks:
+//                               4        16        64       128       256     20,000, 4,096    65,536, 200
+//   fp32   48 x 64            12/15     19/14     32/26     51/42     94/93        21/22          19/14
+//          64 x 64            12/16     20/14     36/27     57/52    102/100       23/22          20/14
+//          96 x 64            18/18     27/18     54/32     96/64    174/122       34/27          27/17
+//          128 x 32           12/19     20/27     33/36     57/66    100/115       21/37          20/18
+//          32 x 128           11/27     18/17     34/32     53/52    122/131       20/26          19/17
+//   fp16, columns contiguous
+//          64 x 128           10/12     14/14     24/24     37/33     76/68        17/24          14/12
+//          72 x 64            10/19     13/15     21/25     33/35     61/62        17/26          13/12
+//          128 x 32           10/19     11/15     20/25     31/34     60/62        15/25          12/12
+//          72 x 72            15/13     20/15     37/26     59/36    109/66        28/26          18/12
+//   fp16, contraction contiguous
+//          64 x 128           10/17     14/21     25/23     39/32     76/66        18/35          15/11
+//          72 x 72             9/19     12/23     23/25     36/34     67/65        18/39          12/12
+//          96 x 64             7/11      9/13     18/25     26/33     46/64        15/22          10/12
+//          128 x 64           10/11     11/14     22/24     35/35     62/66        18/23          14/12
+//          128 x 128          18/20     20/24     38/27     65/46    120/83        29/40          22/13
+// 16 bits and up to 64 x 64, 32 x 128: small throughout (64 x 64: 524,288 rows, 4,096 networks 45/71, 300,000 of 16 21/25).
+template <typename T> bool small_by_tiles(const KnProduct &p, bool cols)
+{
+    const int64_t each = p.M / p.E;
+    if constexpr (sizeof(T) == 4) return p.C > 32 && p.J > 32 ? each >= 16 || p.C + p.J >= 128 : p.C * p.J >= 4096 && each >= 256;
+    if (p.J <= 64) return p.C > 64 && p.J > 32 && (cols ? each >= 96 : p.C > 96 && each >= 256);
+    return p.C > 64 ? cols || each >= 64 : p.C > 32 && each >= 96;
+}
 template <typename T> int launch_forward(hipStream_t st, const KnProduct &p)
 {
     const bool cols = p.b_j == 1 && p.b_c != 1; // (one column of one input: either)
-    // (us, small against tiles: 524,291 rows, 4,096 networks 64 x 64: 48 and 57 in bf16, 117 and 107 in fp32; 262,145 rows, 1,600 networks
-    // 128 x 128: 79 and 50, 206 and 129; 91 x 64, whose rows are not whole pieces: 43 and 71, 103 and 123)
-    const bool tiles = (cols ? rows_of_pieces<T, true>(p) : rows_of_pieces<T, false>(p)) && (int64_t)p.C * p.J > (sizeof(T) == 4 ? 4095 : 4096);
-    if (p.C <= SMALL_MOST && p.J <= SMALL_MOST && !tiles) return cols ? launch_small_widths<T, true>(st, p) : launch_small_widths<T, false>(st, p);
+    // (91 x 64, whose rows are not whole pieces, by staged tiles: 262,145 rows, 1,600 networks 43 and 71 us in bf16, 103 and 123 in fp32)
+    const bool pieces = cols ? rows_of_pieces<T, true>(p) : rows_of_pieces<T, false>(p);
+    if (p.C <= SMALL_MOST && p.J <= SMALL_MOST && !(pieces && small_by_tiles<T>(p, cols)))
+        return cols ? launch_small_widths<T, true>(st, p) : launch_small_widths<T, false>(st, p);
     return cols ? launch_pieces<T, true>(st, p) : launch_pieces<T, false>(st, p);
 }
 

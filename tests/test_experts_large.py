@@ -84,6 +84,18 @@ def test_forward_of_large_calls(size, dtype):
         close(y, *ref_linear(x, w, off, rows, b, relu), k + 1, dtype)
 
 
+# Layers of up to 128 x 128 whose rows are whole pieces, on both sides of what rows per network and widths decide
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("each", [3, 40, 70, 130, 300])
+@pytest.mark.parametrize("k, n", [(32, 128), (40, 40), (64, 64), (64, 128), (72, 64), (72, 72), (128, 32), (128, 64), (128, 128)])
+def test_layers_between_small_and_tiles(k, n, each, dtype):
+    e = 12
+    for i, (how, nk) in enumerate([("even", False), ("tail", True)]):
+        x, w, off, rows = make(e * each, e, k, n, dtype, how, False, nk, each + i)
+        b = rand(7 + i, e, n).to(DT[dtype]).cuda()
+        close(kn.grouped_linear(x, w, off.cuda(), bias=b, relu=True), *ref_linear(x, w, off, None, b, True), k + 1, dtype)
+
+
 @pytest.mark.parametrize("size, dtype", LAYERS, ids=str)
 def test_backward_of_large_calls(size, dtype):
     m, e, k, n = size
