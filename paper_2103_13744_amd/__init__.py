@@ -456,7 +456,8 @@ def composite(sigma, rgb, offsets, step, term_eps=0.0, bg=(0.0, 0.0, 0.0)):
 
 
 # ---------------------------------------------------------------------------------------------
-# networks chosen per row: router, grouped products, weighted sum
+# networks chosen per row: router, grouped products, weighted sum.  Like the rest of this module these calls take no part in
+# automatic differentiation: results carry no graph, gradients are calls of their own.
 _dtype_ids = None  # (dtype -> kn_dtype; filled once torch is there)
 
 
@@ -538,7 +539,8 @@ def _linear_desc(x, w, rows):
 def grouped_linear(x, w, offsets, rows=None, bias=None, relu=False, out=None):
     """One layer of all networks: row i of the result, of network e with offsets[e] <= i < offsets[e + 1], is
     x[rows[i]] @ w[e] + bias[e], then a ReLU where asked for; rows from offsets[E] on are zeros.  ``w``: (E, n_in, n_out),
-    contiguous or the transpose of contiguous (E, n_out, n_in) weights."""
+    contiguous or the transpose of contiguous (E, n_out, n_in) weights.  (The offsets of ``Scene.bucket`` have one entry more:
+    offsets[:-1].contiguous().)"""
     L = load_library()
     d, M, px, pw, pr = _linear_desc(x, w, rows)
     if out is None:
@@ -578,7 +580,7 @@ def grouped_linear_dw(dy, x, w, offsets, rows=None, want_bias=True):
 
 def grouped_linear_backward(dy, x, w, offsets, rows=None, relu_in=False, want_bias=True):
     """(dx, dw, db) of ``grouped_linear``: see ``grouped_linear_dx`` and ``grouped_linear_dw``.  dy is the gradient before the layer's
-    own ReLU, if it has one (the next layer's ``relu_in``)."""
+    own ReLU, if it has one: the next layer's ``relu_in`` gives that, and behind a last layer with a ReLU, dy * (y > 0)."""
     return (grouped_linear_dx(dy, x, w, offsets, rows, relu_in), *grouped_linear_dw(dy, x, w, offsets, rows, want_bias))
 
 

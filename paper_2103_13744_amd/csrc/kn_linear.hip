@@ -46,8 +46,9 @@ __device__ __forceinline__ void finish(const KnProduct &p, bool some, int32_t i,
 // Fragments of b are the products' first operand, so that a lane holds four neighbouring results of a row; they go through
 // the LDS once more to leave in pieces of 8.
 // Measured: 65,536 rows through an index, 64 networks 2048 x 1024 in bf16, 192 x 128: 320 us, 860 TFLOP/s, where one product of the
-// library of 8192 x 8192 x 8192 reaches 1,250.  Power bounds it: the clock is 2.03 GHz with the matrix cores busy 44 % of the time;
-// with 256 x 256 it is 2.30 GHz and 39 %, and the time is the same.  With every fetch a hit in the L2 it would be 250 us.
+// library of 8192 x 8192 x 8192 reaches 1,250.  The clock is 2.03 GHz with the matrix cores busy 44 % of the time (256 x 256: 2.30 GHz, 39 %, the
+// same time); with every fetch a hit in the L2 it would be 250 us, so that more than half of what is above the floor is the wait for what
+// the L2 does not have.
 template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB>
 __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int32_t blocks)
 {
@@ -260,7 +261,8 @@ template <typename T> struct SmallFrag {
 };
 // kn_any_piece in two parts, so that nothing waits for a fetch before all are under way: a piece that ends behind the row is fetched from
 // its last 16 bytes, and shifted to its place at the end.  `odd`: 16-bit rows may begin between two words, where a fetch of 16 bytes is
-// several times as slow: the words that the piece lies in are fetched (five; each holds a value of the piece) and joined at the end
+// several times as slow: the words that the piece lies in are fetched (five; each holds a value of the piece, so that no more than the other
+// half of a word of the row's is read beside it, and shifted out) and joined at the end
 // (524,291 rows, 4,096 networks 63 x 32 in bf16: 50 -> 40 us, with weights whose rows are 63 values 60 -> 35).
 template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type small_ask(const T *row, int32_t k, int32_t C, bool odd, uint32_t &fifth)
 {
