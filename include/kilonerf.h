@@ -369,6 +369,20 @@ int kn_route(void *stream, const void *logits /*dev T rows*/, int32_t dtype, int
 int kn_route_backward(void *stream, const void *logits, int32_t dtype, int64_t T, int32_t experts, int64_t ld, int32_t k,
                       int32_t renormalize, const float *weights, const int32_t *ids, const float *dweights, void *dlogits);
 
+/* What keeps a router even.  p: softmax over all E logits of a row, Z: logarithm of the sum of its exponentials, n: rows that count, those with
+ * a logit above -infinity (a padding token's are all -infinity), counts[e] = offsets[e+1] - offsets[e] (kn_route's):
+ * losses[0] = E / (k n^2) sum over e of counts[e] probs[e], probs[e] = sum over rows of p_e (1 where all is even);
+ * losses[1] = mean over rows of Z^2.  Zeros where n is 0; a NaN or +infinity among a row's logits makes losses and probs NaN.
+ * counts has a last entry n.  Several processes may add up their counts before the backward call (and their probs), which then is that of all their rows.
+ * Workspace: kn_route_balance_workspace_bytes (0 for up to 64 rows: then NULL will do), dev, 256-byte aligned. */
+int kn_route_balance_workspace_bytes(int64_t T, int32_t experts, int64_t *out_bytes);
+int kn_route_balance(void *stream, const void *logits, int32_t dtype, int64_t T, int32_t experts, int64_t ld, int32_t k, const int32_t *offsets /*dev E+1*/,
+                     float *losses /*dev 2*/, int32_t *counts /*dev E+1*/, float *probs /*dev E*/, void *workspace, int64_t workspace_bytes);
+/* Its gradient by the logits, counts held fixed: dlogits (dev, T*E, contiguous, of the logits' type) = add + dlosses[0] d losses[0] + dlosses[1] d losses[1],
+ * rounded once.  add (nullable): T*E, contiguous, of the same type (kn_route_backward's result); dlogits may be add. */
+int kn_route_balance_backward(void *stream, const void *logits, int32_t dtype, int64_t T, int32_t experts, int64_t ld, int32_t k, const int32_t *counts /*dev E+1*/,
+                              const float *dlosses /*dev 2*/, const void *add, void *dlogits);
+
 /* One layer of all networks: y[i] = act(x[r] W_e + b_e) for the rows i of network e, r = rows[i] (i itself where rows is
  * NULL); act is a ReLU or nothing.  Rows of no network: zeros. */
 int kn_grouped_linear(void *stream, const kn_linear_desc *desc, const void *x /*dev*/, const void *w /*dev E*K*N*/,

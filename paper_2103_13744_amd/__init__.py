@@ -23,7 +23,7 @@ EXPORTS = ["kn_error_string", "kn_last_hip_error", "kn_params_per_net", "kn_crea
            "kn_extract_workspace_bytes", "kn_extract_occupancy", "kn_layered_workspace_bytes", "kn_eval_grouped_layered",
            "kn_workspace_bytes", "kn_cell_ids", "kn_bucket", "kn_eval_grouped", "kn_eval_grouped_static", "kn_march", "kn_composite",
            "kn_render", "kn_composite_deltas", "kn_march_stratified", "kn_render_stratified", "kn_set_render_params", "kn_profile_enable", "kn_profile_read",
-           "kn_route_workspace_bytes", "kn_route", "kn_route_backward", "kn_grouped_linear", "kn_grouped_linear_dx", "kn_grouped_linear_dw",
+           "kn_route_workspace_bytes", "kn_route", "kn_route_backward", "kn_route_balance_workspace_bytes", "kn_route_balance", "kn_route_balance_backward", "kn_grouped_linear", "kn_grouped_linear_dx", "kn_grouped_linear_dw",
            "kn_grouped_linear_dw_workspace_bytes",
            "kn_quantize_f8", "kn_quantize_f8_weights", "kn_grouped_linear_f8", "kn_combine", "kn_combine_backward"]
 
@@ -110,6 +110,9 @@ def load_library(build_if_missing: bool = True):
     L.kn_route_workspace_bytes.argtypes = [i64, i32, i32, C.POINTER(i64)]
     L.kn_route.argtypes = [vp, vp, i32, i64, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, i64]
     L.kn_route_backward.argtypes = [vp, vp, i32, i64, i32, i64, i32, i32, vp, vp, vp, vp]
+    L.kn_route_balance_workspace_bytes.argtypes = [i64, i32, C.POINTER(i64)]
+    L.kn_route_balance.argtypes = [vp, vp, i32, i64, i32, i64, i32, vp, vp, vp, vp, vp, i64]
+    L.kn_route_balance_backward.argtypes = [vp, vp, i32, i64, i32, i64, i32, vp, vp, vp, vp]
     L.kn_grouped_linear.argtypes = [vp, desc, vp, vp, vp, vp, vp, i32, vp]
     L.kn_grouped_linear_dx.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp]
     L.kn_grouped_linear_dw_workspace_bytes.argtypes = [desc, C.POINTER(i64)]
@@ -522,6 +525,39 @@ def route_backward(logits, weights, ids, dweights, renormalize=True):
     f = torch.float32
     _check(L.kn_route_backward(_stream(), ptr, _dtype_id(logits.dtype), T, E, ld, k, 1 if renormalize else 0, _ptr(weights, f, shape=(T, k)),
                                _ptr(ids, torch.int32, shape=(T, k)), _ptr(dweights, f, shape=(T, k)), out.data_ptr()), "kn_route_backward")
+    return out
+
+
+def route_balance(logits, k, offsets):
+    """What keeps a router even, on ``route``'s (T, E) logits, k and offsets: (losses (2,), counts (E + 1,) int32, probs (E,)), float32 but for the
+    counts.  losses[0]: E / (k n^2) * sum of counts * probs, which is 1 where all is even; losses[1]: the mean square of a row's log-sum-exp; counts: each
+    network's pairs, then the n rows that have a logit above -inf; probs: the sums of their softmax over all logits."""
+    L = load_library()
+    T, E = logits.shape
+    ptr, ld = _rows_ptr(logits, E)
+    dt, k, f = _dtype_id(logits.dtype), int(k), torch.float32
+    if k < 1 or k > E:
+        raise KnError("expected 1 <= k <= %d experts, got %d" % (E, k))
+    losses, probs, counts = logits.new_empty(2, dtype=f), logits.new_empty(E, dtype=f), logits.new_empty(E + 1, dtype=torch.int32)
+    need, ws = C.c_int64(), None
+    if T > 64:  # (fewer need no workspace)
+        _check(L.kn_route_balance_workspace_bytes(T, E, C.byref(need)), "kn_route_balance_workspace_bytes")
+        ws = torch.empty(need.value, dtype=torch.uint8, device=logits.device)
+    _check(L.kn_route_balance(_stream(), ptr, dt, T, E, ld, k, _ptr(offsets, torch.int32, shape=(E + 1,)), losses.data_ptr(), counts.data_ptr(), probs.data_ptr(),
+                              None if ws is None else ws.data_ptr(), need.value), "kn_route_balance")
+    return losses, counts, probs
+
+
+def route_balance_backward(logits, k, counts, dlosses, add=None):
+    """Gradient of ``route_balance``'s losses by its logits, the counts held fixed: (T, E) of the logits' type.  ``dlosses``: (2,) float32 on the device;
+    ``add``: a gradient that this one is added to before it is rounded (``route_backward``'s)."""
+    L = load_library()
+    T, E = logits.shape
+    ptr, ld = _rows_ptr(logits, E)
+    out = logits.new_empty((T, E))
+    _check(L.kn_route_balance_backward(_stream(), ptr, _dtype_id(logits.dtype), T, E, ld, int(k), _ptr(counts, torch.int32, shape=(E + 1,)),
+                                       _ptr(dlosses, torch.float32, shape=(2,)), _ptr(add, logits.dtype, allow_none=True, shape=(T, E)), out.data_ptr()),
+           "kn_route_balance_backward")
     return out
 
 

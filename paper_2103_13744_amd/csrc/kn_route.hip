@@ -1,5 +1,5 @@
-// The choice of networks per row by a learned router (kn_route: top-k of a softmax, and the rows' order by network), the weighted
-// sum of the networks' results (kn_combine), and their gradients.
+// The choice of networks per row by a learned router (kn_route: top-k of a softmax, and the rows' order by network), the losses that keep
+// it even (kn_route_balance), the weighted sum of the networks' results (kn_combine), and their gradients.
 #include "kn_experts.h"
 
 namespace {
@@ -390,6 +390,223 @@ __global__ void __launch_bounds__(256) k_route_backward(RouteArgs p, const float
     }
 }
 
+// A router's losses.  With p the softmax over a row's logits, Z the logarithm of its sum, n the rows that have a logit above -infinity (or a NaN), c the
+// pairs of each network: E / (k n^2) sum over e of c_e (sum over t of p_te), and the mean of Z^2.
+struct BalanceArgs {
+    RouteArgs route;     // logits, ld, T, E, k, wide; offsets
+    int32_t per;         // rows of a workgroup
+    float *probs, *losses;
+    int32_t *counts;
+    float *sums;         // (workgroups, E): sums of p
+    double *tail;        // (workgroups, 2): sum of Z^2, rows counted; behind them a part of the first loss per workgroup of the join
+    int32_t *ticket;     // workgroups of the join that are done
+};
+constexpr int BALANCE_JOIN = 64; // columns of a workgroup of the join
+
+// Softmax of the row that G lanes hold: p in v, Z returned; whether the row counts.  (A NaN, or +infinity, makes both NaN.)
+template <int G, int V> __device__ __forceinline__ bool softmax_row(float v[V], float &lse, int lane)
+{
+    float best = -INFINITY, s = 0.0f;
+    bool some = false;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        best = fmaxf(best, v[i]);
+        some |= v[i] != -INFINITY;
+    }
+    const float top = group_max<G>(best);
+    const bool counts = group_ballot<G>(some, lane) != 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        v[i] = expf(v[i] - top);
+        s += v[i];
+    }
+    const float all = group_sum<G>(s), inverse = 1.0f / all;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = counts ? v[i] * inverse : 0.0f;
+    lse = counts ? top + logf(all) : 0.0f;
+    return counts;
+}
+
+// Sums over the rows [block * per, + per): G lanes a row, whose columns' sums stay in registers from row to row and meet in the LDS at the end, in
+// the order of the groups.  ONE: these are all rows, and the results are written too; else they are left for k_balance_join.
+// Bound by its bytes where there are many rows, by latency where there are few.
+template <typename T, int G, int V, bool ONE>
+__global__ void __launch_bounds__(256) k_balance(BalanceArgs a)
+{
+    constexpr int GROUPS = 256 / G;
+    __shared__ float parts[GROUPS][G * V];
+    __shared__ float squares[GROUPS], terms[4];
+    __shared__ int32_t rows[GROUPS];
+    const RouteArgs &p = a.route;
+    const int tid = kn_thread(), lane = tid & 63, at = lane & (G - 1), group = tid / G;
+    const int32_t block = p.first + kn_block();
+    const int32_t t0 = block * a.per, t1 = (int32_t)min((int64_t)p.T, (int64_t)t0 + a.per);
+    float sum[V] = {}, square = 0.0f;
+    int32_t n = 0;
+    for (int32_t base = t0; base < t1; base += GROUPS) {
+        const int32_t t = base + group;
+        float v[V], lse;
+        load_logits<T, V>(p, t, t < t1, at, v); // (a row that is not there is one of -infinity)
+        n += softmax_row<G, V>(v, lse, lane) ? 1 : 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[i] += v[i];
+        square = fmaf(lse, lse, square);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) parts[group][at * V + i] = sum[i];
+    if (at == 0) {
+        squares[group] = square;
+        rows[group] = n;
+    }
+    if (!ONE && block == 0 && tid == 0) *a.ticket = 0;
+    __syncthreads();
+    float all_squares = 0.0f, term = 0.0f;
+    int32_t all_rows = 0;
+    for (int g = 0; g < GROUPS; ++g) {
+        all_squares += squares[g];
+        all_rows += rows[g];
+    }
+    for (int32_t e = tid; e < p.E; e += 256) {
+        float y = 0.0f;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) y += parts[g][e];
+        if constexpr (ONE) {
+            const int32_t c = p.offsets[e + 1] - p.offsets[e];
+            a.probs[e] = y;
+            a.counts[e] = c;
+            term = fmaf((float)c, y, term);
+        } else {
+            a.sums[(int64_t)block * p.E + e] = y;
+        }
+    }
+    if constexpr (ONE) {
+        term = group_sum<64>(term);
+        if (lane == 0) terms[tid >> 6] = term;
+        __syncthreads();
+        if (tid == 0) {
+            const float inverse = all_rows > 0 ? 1.0f / (float)all_rows : 0.0f;
+            a.counts[p.E] = all_rows;
+            a.losses[0] = (terms[0] + terms[1] + terms[2] + terms[3]) * inverse * inverse * ((float)p.E / (float)p.k);
+            a.losses[1] = all_squares * inverse;
+        }
+    } else if (tid == 0) {
+        a.tail[2 * (int64_t)block] = all_squares;
+        a.tail[2 * (int64_t)block + 1] = all_rows;
+    }
+}
+
+// The workgroups' sums, BALANCE_JOIN columns a workgroup, 16 threads a column, in 64 bits; the workgroup that is done last sums the parts of the first loss, in
+// their order.
+__global__ void __launch_bounds__(1024) k_balance_join(BalanceArgs a)
+{
+    __shared__ double parts[1024];
+    __shared__ int32_t done;
+    const int32_t E = a.route.E, blocks = a.route.blocks, join = kn_block(), joins = (E + BALANCE_JOIN - 1) / BALANCE_JOIN;
+    const int tid = kn_thread(), col = tid & (BALANCE_JOIN - 1), turn = tid / BALANCE_JOIN;
+    const int32_t e = join * BALANCE_JOIN + col;
+    double *first = a.tail + 2 * (int64_t)blocks;
+    double y = 0.0;
+    if (e < E)
+#pragma unroll 8
+        for (int32_t b = turn; b < blocks; b += 16) y += a.sums[(int64_t)b * E + e];
+    parts[tid] = y;
+    __syncthreads();
+    if (tid < BALANCE_JOIN) {
+        for (int q = 1; q < 16; ++q) y += parts[q * BALANCE_JOIN + tid];
+        double term = 0.0;
+        if (e < E) {
+            const int32_t c = a.route.offsets[e + 1] - a.route.offsets[e];
+            a.probs[e] = (float)y;
+            a.counts[e] = c;
+            term = c * y;
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) term += __shfl_xor(term, d);
+        if (tid == 0) {
+            __hip_atomic_store(&first[join], term, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            done = __hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1;
+        }
+    }
+    __syncthreads();
+    if (done != joins) return;
+    double squares = 0.0, rows = 0.0;
+    for (int32_t b = tid; b < blocks; b += 1024) {
+        squares += a.tail[2 * (int64_t)b];
+        rows += a.tail[2 * (int64_t)b + 1];
+    }
+    auto total = [&](double v) { // (in one order)
+        __syncthreads();
+        parts[tid] = v;
+        __syncthreads();
+        for (int d = 512; d > 0; d >>= 1) {
+            if (tid < d) parts[tid] += parts[tid + d];
+            __syncthreads();
+        }
+        return parts[0];
+    };
+    const double n = total(rows), z = total(squares);
+    if (tid == 0) {
+        double sum = 0.0;
+        for (int32_t j = 0; j < joins; ++j) sum += __hip_atomic_load(&first[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        a.counts[E] = (int32_t)n;
+        a.losses[0] = n > 0.0 ? (float)(sum * E / (a.route.k * n * n)) : 0.0f;
+        a.losses[1] = n > 0.0 ? (float)(z / n) : 0.0f;
+    }
+}
+
+// dl_te = p_te (g_0 (s_e - sum over i of p_ti s_i) + g_1 (2 / n) Z_t), s_e = E c_e / (k n^2), and what it is added to.  Bound by its bytes.
+template <typename T, int G, int V>
+__global__ void __launch_bounds__(256) k_balance_backward(RouteArgs p, const int32_t *__restrict__ counts, const float *__restrict__ dlosses,
+                                                          const T *add, T *dlogits)
+{
+    const int lane = kn_thread() & 63, at = lane & (G - 1);
+    const int32_t t = (p.first + kn_block()) * (256 / G) + kn_thread() / G;
+    const bool there = t < p.T;
+    float v[V], share[V], lse;
+    load_logits<T, V>(p, t, there, at, v);
+    typedef T Piece __attribute__((ext_vector_type(V)));
+    const int64_t place = (int64_t)t * p.E + at * V;
+    T more[V];
+    if (add) { // (asked for before the row is worked on)
+        if (p.wide) {
+            Piece x = {};
+            if (there && at * V < p.E) x = *(const Piece *)(add + place);
+#pragma unroll
+            for (int i = 0; i < V; ++i) more[i] = x[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) more[i] = there && at * V + i < p.E ? add[place + i] : (T)0.0f;
+        }
+    }
+    const int32_t n = counts[p.E];
+    const float inverse = n > 0 ? 1.0f / (float)n : 0.0f, unit = (float)p.E / (float)p.k * inverse * inverse;
+#pragma unroll
+    for (int i = 0; i < V; ++i) share[i] = at * V + i < p.E ? unit * (float)counts[at * V + i] : 0.0f;
+    softmax_row<G, V>(v, lse, lane);
+    float part = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) part = fmaf(v[i], share[i], part);
+    const float mean = group_sum<G>(part), g0 = dlosses[0], shift = dlosses[1] * (2.0f * inverse) * lse;
+    if (!there) return;
+    float d[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        d[i] = v[i] * fmaf(g0, share[i] - mean, shift);
+        if (add) d[i] += (float)more[i];
+    }
+    T *out = dlogits + place;
+    if (p.wide) {
+        Piece x;
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = (T)d[i];
+        if (at * V < p.E) *(Piece *)out = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (at * V + i < p.E) out[i] = (T)d[i];
+    }
+}
+
 // V neighbouring values of a row.  WHOLE: rows are made of such pieces, each on a multiple of its size; else they lie anywhere, and a row's
 // last piece is its last V values, some of which the piece before has too (narrower rows: V = 1).  Rows of 2,468 values, 25,295 of 2 in bf16: pieces
 // anywhere 213 us for the sums and their gradients, single values 582.
@@ -553,6 +770,78 @@ extern "C" int kn_route_backward(void *stream, const void *logits, int32_t dtype
             return kn_launch(kn_div_up(T, 256 / G), 256, [&](dim3 grid, int32_t first) {
                 p.first = first;
                 hipLaunchKernelGGL((k_route_backward<E_, G, V>), grid, dim3(256), 0, (hipStream_t)stream, p, dweights, (E_ *)dlogits);
+            });
+        });
+    });
+}
+
+// Rows of a workgroup's sums: workgroups for the whole chip, and no sum of more than 2,048 rows in 32 bits
+static int32_t balance_rows(int64_t T, int32_t E)
+{
+    const int64_t set = E <= 256 ? 16 : 4, per = kn_align_up(kn_div_up(T, 512), set);
+    return (int32_t)(per < 2048 ? per : 2048);
+}
+
+extern "C" int kn_route_balance_workspace_bytes(int64_t T, int32_t E, int64_t *out_bytes)
+{
+    if (!out_bytes || T < 0 || E < 1) return KN_E_INVALID_ARG;
+    if (!route_supported(T, E, 1)) return KN_E_UNSUPPORTED;
+    const int64_t blocks = T <= ROUTE_TOKENS ? 0 : kn_div_up(T, balance_rows(T, E));
+    *out_bytes = blocks == 0 ? 0 : kn_align_up((2 * blocks + kn_div_up(E, BALANCE_JOIN)) * 8 + blocks * E * 4 + 4, 256);
+    return KN_OK;
+}
+
+extern "C" int kn_route_balance(void *stream, const void *logits, int32_t dtype, int64_t T, int32_t E, int64_t ld, int32_t k, const int32_t *offsets,
+                                float *losses, int32_t *counts, float *probs, void *workspace, int64_t workspace_bytes)
+{
+    if (!route_valid(T, E, k) || !kn_dtype_ok(dtype) || ld < E || !offsets || !losses || !counts || !probs || (T > 0 && !logits)) return KN_E_INVALID_ARG;
+    if (!route_supported(T, E, k)) return KN_E_UNSUPPORTED;
+    int64_t need = 0;
+    KN_TRY(kn_route_balance_workspace_bytes(T, E, &need));
+    if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return KN_E_WORKSPACE;
+    const bool one = need == 0;
+    BalanceArgs a = {};
+    a.per = one ? ROUTE_TOKENS : balance_rows(T, E);
+    const int32_t blocks = one ? 1 : (int32_t)kn_div_up(T, a.per);
+    a.route = {logits, ld, (int32_t)T, E, k, 0, nullptr, nullptr, nullptr, nullptr, const_cast<int32_t *>(offsets), nullptr, nullptr, 0, blocks, 0};
+    a.probs = probs; a.losses = losses; a.counts = counts;
+    a.tail = (double *)workspace;
+    a.sums = (float *)(a.tail + 2 * (int64_t)blocks + kn_div_up(E, BALANCE_JOIN));
+    a.ticket = (int32_t *)(a.sums + (int64_t)blocks * E);
+    hipStream_t st = (hipStream_t)stream;
+    KN_TRY(kn_with_type(dtype, [&](auto v) -> int {
+        typedef decltype(v) E_;
+        return route_shape(E, [&](auto g, auto n) -> int {
+            constexpr int G = decltype(g)::n, V = decltype(n)::n;
+            a.route.wide = route_wide(logits, ld, E, V, sizeof(E_));
+            return kn_launch(blocks, 256, [&](dim3 grid, int32_t first) {
+                a.route.first = first;
+                if (one) hipLaunchKernelGGL((k_balance<E_, G, V, true>), grid, dim3(256), 0, st, a);
+                else hipLaunchKernelGGL((k_balance<E_, G, V, false>), grid, dim3(256), 0, st, a);
+            });
+        });
+    }));
+    if (one) return KN_OK;
+    hipLaunchKernelGGL(k_balance_join, dim3((unsigned)kn_div_up(E, BALANCE_JOIN)), dim3(1024), 0, st, a);
+    KN_CHECK_LAUNCH();
+    return KN_OK;
+}
+
+extern "C" int kn_route_balance_backward(void *stream, const void *logits, int32_t dtype, int64_t T, int32_t E, int64_t ld, int32_t k, const int32_t *counts,
+                                         const float *dlosses, const void *add, void *dlogits)
+{
+    if (!route_valid(T, E, k) || !kn_dtype_ok(dtype) || ld < E || (T > 0 && (!logits || !counts || !dlosses || !dlogits))) return KN_E_INVALID_ARG;
+    if (!route_supported(T, E, k)) return KN_E_UNSUPPORTED;
+    if (T == 0) return KN_OK;
+    RouteArgs p = {logits, ld, (int32_t)T, E, k, 0, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0, 0};
+    return kn_with_type(dtype, [&](auto v) -> int {
+        typedef decltype(v) E_;
+        return route_shape(E, [&](auto g, auto n) -> int {
+            constexpr int G = decltype(g)::n, V = decltype(n)::n;
+            p.wide = route_wide(logits, ld, E, V, sizeof(E_)) && route_wide(dlogits, E, E, V, sizeof(E_)) && (!add || route_wide(add, E, E, V, sizeof(E_)));
+            return kn_launch(kn_div_up(T, 256 / G), 256, [&](dim3 grid, int32_t first) {
+                p.first = first;
+                hipLaunchKernelGGL((k_balance_backward<E_, G, V>), grid, dim3(256), 0, (hipStream_t)stream, p, counts, dlosses, (const E_ *)add, (E_ *)dlogits);
             });
         });
     });
