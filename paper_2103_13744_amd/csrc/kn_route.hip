@@ -393,17 +393,57 @@ __global__ void __launch_bounds__(256) k_route_backward(RouteArgs p, const float
 // A router's losses.  With p the softmax over a row's logits, Z the logarithm of its sum, n the rows that have a logit above -infinity (or a NaN), c the
 // pairs of each network: E / (k n^2) sum over e of c_e (sum over t of p_te), and the mean of Z^2.
 struct BalanceArgs {
-    RouteArgs route;     // logits, ld, T, E, k, wide; offsets
-    int32_t per;         // rows of a workgroup
-    float *probs, *losses;
+    const void *logits, *add;
+    void *dlogits;
+    int64_t ld;
+    int32_t T, E, k;
+    int32_t per, blocks, first; // rows of a workgroup, workgroups in all, number of the launch's first one
+    const int32_t *offsets;
     int32_t *counts;
-    float *sums;         // (workgroups, E): sums of p
-    double *tail;        // (workgroups, 2): sum of Z^2, rows counted; behind them a part of the first loss per workgroup of the join
-    int32_t *ticket;     // workgroups of the join that are done
+    const float *dlosses;
+    float *probs, *losses;
+    float *sums;     // (workgroups, E): sums of p
+    double *tail;    // (workgroups, 2): sum of Z^2, rows counted; behind them (workgroups of the join, 2): their parts of the results
+    int32_t *ticket; // workgroups of the join that are done
 };
-constexpr int BALANCE_JOIN = 64; // columns of a workgroup of the join
+constexpr int JOIN_COLUMNS = 32, JOIN_TURNS = 32; // columns of a workgroup of the join, threads that share one
+static_assert(ROUTE_MAX_EXPERTS <= 63 * JOIN_COLUMNS, "a wavefront adds up the join's parts");
 
-// Softmax of the row that G lanes hold: p in v, Z returned; whether the row counts.  (A NaN, or +infinity, makes both NaN.)
+// How G lanes hold a row: pieces of 16 bytes (or V values), the lanes' next to each other, wherever the row begins.  The piece that would pass the row's end is its
+// last CH values (E >= CH), of which those count that no piece before has; so there is no branch around a fetch, and what is asked for ahead is not waited for.
+template <typename T, int G, int V> struct RowOf {
+    static constexpr int CH = V * (int)sizeof(T) < 16 ? V : 16 / (int)sizeof(T), N = V / CH;
+    typedef T Piece __attribute__((ext_vector_type(CH), aligned(sizeof(T))));
+    Piece x[N];
+    static __device__ __forceinline__ int start(int at, int n) { return (n * G + at) * CH; }
+    static __device__ __forceinline__ int column(int at, int i, int32_t E) { return min(start(at, i / CH), E - CH) + i % CH; }
+    static __device__ __forceinline__ bool counts(int at, int i, int32_t E) { return column(at, i, E) >= start(at, i / CH); }
+    __device__ __forceinline__ void ask(const T *row, int32_t E, int at)
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) x[n] = *(const Piece *)(row + min(start(at, n), E - CH));
+    }
+    __device__ __forceinline__ float value(int i) const { return to_float((T)x[i / CH][i % CH]); }
+    static __device__ __forceinline__ void store(T *row, int32_t E, int at, const float v[V])
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int c = start(at, n);
+            Piece x;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) x[i] = (T)v[n * CH + i];
+            if (c + CH <= E) *(Piece *)(row + c) = x;
+            else
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+                    if (counts(at, n * CH + i, E)) row[E - CH + i] = x[i];
+        }
+    }
+};
+
+// Softmax of the row that G lanes hold: p in v, Z returned; whether the row counts.  (A NaN, or +infinity, makes both NaN.)  An exponential is
+// the hardware's of base 2, whose argument is rounded once: a p that is e^-x of the largest is off by x 2^-24 of itself more than expf's, which would be two thirds of
+// all instructions (16,385 rows of 1,000 in bf16: 18 and 23 us with it, forward and backward).
 template <int G, int V> __device__ __forceinline__ bool softmax_row(float v[V], float &lse, int lane)
 {
     float best = -INFINITY, s = 0.0f;
@@ -417,7 +457,7 @@ template <int G, int V> __device__ __forceinline__ bool softmax_row(float v[V], 
     const bool counts = group_ballot<G>(some, lane) != 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        v[i] = expf(v[i] - top);
+        v[i] = __builtin_amdgcn_exp2f((v[i] - top) * 1.4426950408889634f);
         s += v[i];
     }
     const float all = group_sum<G>(s), inverse = 1.0f / all;
@@ -428,182 +468,191 @@ template <int G, int V> __device__ __forceinline__ bool softmax_row(float v[V], 
 }
 
 // Sums over the rows [block * per, + per): G lanes a row, whose columns' sums stay in registers from row to row and meet in the LDS at the end, in
-// the order of the groups.  ONE: these are all rows, and the results are written too; else they are left for k_balance_join.
-// Bound by its bytes where there are many rows, by latency where there are few.
+// the order of the groups.  A row is asked for while the one before is worked on.  ONE: these are all rows, and the results are written too; else they are
+// left for k_balance_join.
 template <typename T, int G, int V, bool ONE>
 __global__ void __launch_bounds__(256) k_balance(BalanceArgs a)
 {
     constexpr int GROUPS = 256 / G;
+    typedef RowOf<T, G, V> Row;
     __shared__ float parts[GROUPS][G * V];
     __shared__ float squares[GROUPS], terms[4];
     __shared__ int32_t rows[GROUPS];
-    const RouteArgs &p = a.route;
     const int tid = kn_thread(), lane = tid & 63, at = lane & (G - 1), group = tid / G;
-    const int32_t block = p.first + kn_block();
-    const int32_t t0 = block * a.per, t1 = (int32_t)min((int64_t)p.T, (int64_t)t0 + a.per);
+    const int32_t block = a.first + kn_block();
+    const int32_t t0 = block * a.per, t1 = (int32_t)min((int64_t)a.T, (int64_t)t0 + a.per);
+    const T *logits = (const T *)a.logits;
     float sum[V] = {}, square = 0.0f;
     int32_t n = 0;
+    Row next;
+    auto ask = [&](int32_t t) { next.ask(logits + (int64_t)min(t, a.T - 1) * a.ld, a.E, at); };
+    if (t0 < t1) ask(t0 + group);
     for (int32_t base = t0; base < t1; base += GROUPS) {
-        const int32_t t = base + group;
         float v[V], lse;
-        load_logits<T, V>(p, t, t < t1, at, v); // (a row that is not there is one of -infinity)
+        const int32_t t = base + group; // (a row that is not there is one of -infinity)
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = t < t1 && Row::counts(at, i, a.E) ? next.value(i) : -INFINITY;
+        ask(t + GROUPS);
         n += softmax_row<G, V>(v, lse, lane) ? 1 : 0;
 #pragma unroll
         for (int i = 0; i < V; ++i) sum[i] += v[i];
         square = fmaf(lse, lse, square);
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) parts[group][at * V + i] = sum[i];
+    for (int i = 0; i < V; ++i)
+        if (Row::counts(at, i, a.E)) parts[group][Row::column(at, i, a.E)] = sum[i];
     if (at == 0) {
         squares[group] = square;
         rows[group] = n;
     }
     if (!ONE && block == 0 && tid == 0) *a.ticket = 0;
     __syncthreads();
-    float all_squares = 0.0f, term = 0.0f;
-    int32_t all_rows = 0;
-    for (int g = 0; g < GROUPS; ++g) {
-        all_squares += squares[g];
-        all_rows += rows[g];
-    }
-    for (int32_t e = tid; e < p.E; e += 256) {
+    float term = 0.0f;
+    for (int32_t e = tid; e < a.E; e += 256) {
         float y = 0.0f;
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) y += parts[g][e];
         if constexpr (ONE) {
-            const int32_t c = p.offsets[e + 1] - p.offsets[e];
+            const int32_t c = a.offsets[e + 1] - a.offsets[e];
             a.probs[e] = y;
             a.counts[e] = c;
             term = fmaf((float)c, y, term);
         } else {
-            a.sums[(int64_t)block * p.E + e] = y;
+            a.sums[(int64_t)block * a.E + e] = y;
         }
     }
     if constexpr (ONE) {
         term = group_sum<64>(term);
         if (lane == 0) terms[tid >> 6] = term;
         __syncthreads();
-        if (tid == 0) {
-            const float inverse = all_rows > 0 ? 1.0f / (float)all_rows : 0.0f;
-            a.counts[p.E] = all_rows;
-            a.losses[0] = (terms[0] + terms[1] + terms[2] + terms[3]) * inverse * inverse * ((float)p.E / (float)p.k);
-            a.losses[1] = all_squares * inverse;
-        }
-    } else if (tid == 0) {
+    }
+    if (tid > 0) return;
+    float all_squares = 0.0f;
+    int32_t all_rows = 0;
+    for (int g = 0; g < GROUPS; ++g) {
+        all_squares += squares[g];
+        all_rows += rows[g];
+    }
+    if constexpr (ONE) {
+        const float inverse = all_rows > 0 ? 1.0f / (float)all_rows : 0.0f;
+        a.counts[a.E] = all_rows;
+        a.losses[0] = (terms[0] + terms[1] + terms[2] + terms[3]) * inverse * inverse * ((float)a.E / (float)a.k);
+        a.losses[1] = all_squares * inverse;
+    } else {
         a.tail[2 * (int64_t)block] = all_squares;
         a.tail[2 * (int64_t)block + 1] = all_rows;
     }
 }
 
-// The workgroups' sums, BALANCE_JOIN columns a workgroup, 16 threads a column, in 64 bits; the workgroup that is done last sums the parts of the first loss, in
-// their order.
-__global__ void __launch_bounds__(1024) k_balance_join(BalanceArgs a)
+// The workgroups' sums, in 64 bits and one order: JOIN_COLUMNS columns a workgroup, and one more workgroup for the sums of Z^2 and the rows.  Each leaves its part
+// of the losses where all XCDs see it, and the one that is done last adds the parts up, in their order.
+__global__ void __launch_bounds__(JOIN_COLUMNS * JOIN_TURNS) k_balance_join(BalanceArgs a)
 {
-    __shared__ double parts[1024];
-    __shared__ int32_t done;
-    const int32_t E = a.route.E, blocks = a.route.blocks, join = kn_block(), joins = (E + BALANCE_JOIN - 1) / BALANCE_JOIN;
-    const int tid = kn_thread(), col = tid & (BALANCE_JOIN - 1), turn = tid / BALANCE_JOIN;
-    const int32_t e = join * BALANCE_JOIN + col;
-    double *first = a.tail + 2 * (int64_t)blocks;
-    double y = 0.0;
-    if (e < E)
-#pragma unroll 8
-        for (int32_t b = turn; b < blocks; b += 16) y += a.sums[(int64_t)b * E + e];
-    parts[tid] = y;
-    __syncthreads();
-    if (tid < BALANCE_JOIN) {
-        for (int q = 1; q < 16; ++q) y += parts[q * BALANCE_JOIN + tid];
-        double term = 0.0;
-        if (e < E) {
-            const int32_t c = a.route.offsets[e + 1] - a.route.offsets[e];
+    constexpr int AHEAD = 16;
+    __shared__ double parts[JOIN_TURNS][JOIN_COLUMNS];
+    const int32_t E = a.E, blocks = a.blocks, join = kn_block(), joins = (E + JOIN_COLUMNS - 1) / JOIN_COLUMNS;
+    const int tid = kn_thread();
+    double *part = a.tail + 2 * (int64_t)blocks, first = 0.0, second = 0.0; // (the second: of the tail only)
+    auto total = [](double v) {
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+        return v;
+    };
+    if (join == joins) {
+        for (int32_t b = tid; b < blocks; b += JOIN_COLUMNS * JOIN_TURNS) {
+            first += a.tail[2 * (int64_t)b];
+            second += a.tail[2 * (int64_t)b + 1];
+        }
+        first = total(first);
+        second = total(second);
+        if ((tid & 63) == 0) {
+            parts[0][tid >> 6] = first;
+            parts[1][tid >> 6] = second;
+        }
+        __syncthreads();
+        if (tid >= 64) return;
+        first = total(tid < JOIN_COLUMNS * JOIN_TURNS / 64 ? parts[0][tid] : 0.0);
+        second = total(tid < JOIN_COLUMNS * JOIN_TURNS / 64 ? parts[1][tid] : 0.0);
+    } else {
+        const int col = tid % JOIN_COLUMNS, turn = tid / JOIN_COLUMNS;
+        const int32_t e = join * JOIN_COLUMNS + col;
+        const float *sums = a.sums + min(e, E - 1);
+        double y = 0.0;
+        for (int32_t b0 = turn; b0 < blocks; b0 += AHEAD * JOIN_TURNS) {
+            float x[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) x[u] = sums[(int64_t)min(b0 + u * JOIN_TURNS, blocks - 1) * E];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) y += b0 + u * JOIN_TURNS < blocks ? (double)x[u] : 0.0;
+        }
+        parts[turn][col] = y;
+        __syncthreads();
+        if (tid >= 64) return;
+        if (tid < JOIN_COLUMNS && e < E) {
+#pragma unroll
+            for (int q = 1; q < JOIN_TURNS; ++q) y += parts[q][tid];
+            const int32_t c = a.offsets[e + 1] - a.offsets[e];
             a.probs[e] = (float)y;
             a.counts[e] = c;
-            term = c * y;
+            first = c * y;
         }
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) term += __shfl_xor(term, d);
-        if (tid == 0) {
-            __hip_atomic_store(&first[join], term, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            done = __hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1;
-        }
+        first = total(first);
     }
-    __syncthreads();
-    if (done != joins) return;
-    double squares = 0.0, rows = 0.0;
-    for (int32_t b = tid; b < blocks; b += 1024) {
-        squares += a.tail[2 * (int64_t)b];
-        rows += a.tail[2 * (int64_t)b + 1];
-    }
-    auto total = [&](double v) { // (in one order)
-        __syncthreads();
-        parts[tid] = v;
-        __syncthreads();
-        for (int d = 512; d > 0; d >>= 1) {
-            if (tid < d) parts[tid] += parts[tid + d];
-            __syncthreads();
-        }
-        return parts[0];
-    };
-    const double n = total(rows), z = total(squares);
+    int32_t done = 0;
     if (tid == 0) {
-        double sum = 0.0;
-        for (int32_t j = 0; j < joins; ++j) sum += __hip_atomic_load(&first[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(&part[2 * join], first, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(&part[2 * join + 1], second, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        done = __hip_atomic_fetch_add(a.ticket, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (__builtin_amdgcn_readfirstlane(done) != joins) return;
+    const double sum = total(tid < joins ? __hip_atomic_load(&part[2 * tid], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0);
+    if (tid == 0) {
+        const double z = __hip_atomic_load(&part[2 * joins], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), n = __hip_atomic_load(&part[2 * joins + 1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         a.counts[E] = (int32_t)n;
-        a.losses[0] = n > 0.0 ? (float)(sum * E / (a.route.k * n * n)) : 0.0f;
+        a.losses[0] = n > 0.0 ? (float)(sum * E / (a.k * n * n)) : 0.0f;
         a.losses[1] = n > 0.0 ? (float)(z / n) : 0.0f;
     }
 }
 
-// dl_te = p_te (g_0 (s_e - sum over i of p_ti s_i) + g_1 (2 / n) Z_t), s_e = E c_e / (k n^2), and what it is added to.  Bound by its bytes.
-template <typename T, int G, int V>
-__global__ void __launch_bounds__(256) k_balance_backward(RouteArgs p, const int32_t *__restrict__ counts, const float *__restrict__ dlosses,
-                                                          const T *add, T *dlogits)
+// dl_te = p_te (g_0 (s_e - sum over i of p_ti s_i) + g_1 (2 / n) Z_t), s_e = E c_e / (k n^2), and (ADD) what it is added to.  Rows as in k_balance.
+template <typename T, int G, int V, bool ADD>
+__global__ void __launch_bounds__(256) k_balance_backward(BalanceArgs a)
 {
-    const int lane = kn_thread() & 63, at = lane & (G - 1);
-    const int32_t t = (p.first + kn_block()) * (256 / G) + kn_thread() / G;
-    const bool there = t < p.T;
-    float v[V], share[V], lse;
-    load_logits<T, V>(p, t, there, at, v);
-    typedef T Piece __attribute__((ext_vector_type(V)));
-    const int64_t place = (int64_t)t * p.E + at * V;
-    T more[V];
-    if (add) { // (asked for before the row is worked on)
-        if (p.wide) {
-            Piece x = {};
-            if (there && at * V < p.E) x = *(const Piece *)(add + place);
+    constexpr int GROUPS = 256 / G;
+    typedef RowOf<T, G, V> Row;
+    const int lane = kn_thread() & 63, at = lane & (G - 1), group = kn_thread() / G;
+    const int32_t t0 = (a.first + kn_block()) * a.per, t1 = (int32_t)min((int64_t)a.T, (int64_t)t0 + a.per);
+    const T *logits = (const T *)a.logits, *add = (const T *)a.add;
+    T *out = (T *)a.dlogits;
+    Row next, more;
+    auto ask = [&](int32_t t) {
+        const int64_t row = min(t, t1 - 1); // (within this workgroup's own rows: `add` may be what is written)
+        next.ask(logits + row * a.ld, a.E, at);
+        if constexpr (ADD) more.ask(add + row * a.E, a.E, at);
+    };
+    ask(t0 + group);
+    const int32_t n = a.counts[a.E];
+    const float inverse = n > 0 ? 1.0f / (float)n : 0.0f, unit = (float)a.E / (float)a.k * inverse * inverse;
+    const float g0 = a.dlosses[0], g1 = a.dlosses[1] * (2.0f * inverse);
+    float share[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) more[i] = x[i];
-        } else {
+    for (int i = 0; i < V; ++i) share[i] = unit * (float)a.counts[Row::column(at, i, a.E)];
+    for (int32_t base = t0; base < t1; base += GROUPS) {
+        const int32_t t = base + group;
+        float v[V], d[V], lse, part = 0.0f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) more[i] = there && at * V + i < p.E ? add[place + i] : (T)0.0f;
+        for (int i = 0; i < V; ++i) {
+            v[i] = t < t1 && Row::counts(at, i, a.E) ? next.value(i) : -INFINITY;
+            d[i] = ADD ? more.value(i) : 0.0f;
         }
-    }
-    const int32_t n = counts[p.E];
-    const float inverse = n > 0 ? 1.0f / (float)n : 0.0f, unit = (float)p.E / (float)p.k * inverse * inverse;
+        ask(t + GROUPS);
+        softmax_row<G, V>(v, lse, lane);
 #pragma unroll
-    for (int i = 0; i < V; ++i) share[i] = at * V + i < p.E ? unit * (float)counts[at * V + i] : 0.0f;
-    softmax_row<G, V>(v, lse, lane);
-    float part = 0.0f;
+        for (int i = 0; i < V; ++i) part = fmaf(v[i], share[i], part);
+        const float mean = group_sum<G>(part), shift = g1 * lse;
 #pragma unroll
-    for (int i = 0; i < V; ++i) part = fmaf(v[i], share[i], part);
-    const float mean = group_sum<G>(part), g0 = dlosses[0], shift = dlosses[1] * (2.0f * inverse) * lse;
-    if (!there) return;
-    float d[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        d[i] = v[i] * fmaf(g0, share[i] - mean, shift);
-        if (add) d[i] += (float)more[i];
-    }
-    T *out = dlogits + place;
-    if (p.wide) {
-        Piece x;
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = (T)d[i];
-        if (at * V < p.E) *(Piece *)out = x;
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (at * V + i < p.E) out[i] = (T)d[i];
+        for (int i = 0; i < V; ++i) d[i] = v[i] * fmaf(g0, share[i] - mean, shift) + d[i];
+        if (t < t1) Row::store(out + (int64_t)t * a.E, a.E, at, d);
     }
 }
 
@@ -775,10 +824,10 @@ extern "C" int kn_route_backward(void *stream, const void *logits, int32_t dtype
     });
 }
 
-// Rows of a workgroup's sums: workgroups for the whole chip, and no sum of more than 2,048 rows in 32 bits
+// Rows of a workgroup: enough workgroups for the whole chip, and no sum of more than 2,048 rows in 32 bits
 static int32_t balance_rows(int64_t T, int32_t E)
 {
-    const int64_t set = E <= 256 ? 16 : 4, per = kn_align_up(kn_div_up(T, 512), set);
+    const int64_t set = E <= 256 ? 16 : 4, per = kn_align_up(kn_div_up(T, 1024), set);
     return (int32_t)(per < 2048 ? per : 2048);
 }
 
@@ -787,7 +836,7 @@ extern "C" int kn_route_balance_workspace_bytes(int64_t T, int32_t E, int64_t *o
     if (!out_bytes || T < 0 || E < 1) return KN_E_INVALID_ARG;
     if (!route_supported(T, E, 1)) return KN_E_UNSUPPORTED;
     const int64_t blocks = T <= ROUTE_TOKENS ? 0 : kn_div_up(T, balance_rows(T, E));
-    *out_bytes = blocks == 0 ? 0 : kn_align_up((2 * blocks + kn_div_up(E, BALANCE_JOIN)) * 8 + blocks * E * 4 + 4, 256);
+    *out_bytes = blocks == 0 ? 0 : kn_align_up((blocks + kn_div_up(E, JOIN_COLUMNS) + 1) * 16 + blocks * E * 4 + 4, 256);
     return KN_OK;
 }
 
@@ -800,29 +849,29 @@ extern "C" int kn_route_balance(void *stream, const void *logits, int32_t dtype,
     KN_TRY(kn_route_balance_workspace_bytes(T, E, &need));
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return KN_E_WORKSPACE;
     const bool one = need == 0;
+    const int64_t joins = kn_div_up(E, JOIN_COLUMNS);
     BalanceArgs a = {};
+    a.logits = logits; a.ld = ld; a.T = (int32_t)T; a.E = E; a.k = k;
     a.per = one ? ROUTE_TOKENS : balance_rows(T, E);
-    const int32_t blocks = one ? 1 : (int32_t)kn_div_up(T, a.per);
-    a.route = {logits, ld, (int32_t)T, E, k, 0, nullptr, nullptr, nullptr, nullptr, const_cast<int32_t *>(offsets), nullptr, nullptr, 0, blocks, 0};
-    a.probs = probs; a.losses = losses; a.counts = counts;
+    a.blocks = one ? 1 : (int32_t)kn_div_up(T, a.per);
+    a.offsets = offsets; a.counts = counts; a.probs = probs; a.losses = losses;
     a.tail = (double *)workspace;
-    a.sums = (float *)(a.tail + 2 * (int64_t)blocks + kn_div_up(E, BALANCE_JOIN));
-    a.ticket = (int32_t *)(a.sums + (int64_t)blocks * E);
+    a.sums = (float *)(a.tail + 2 * (a.blocks + joins + 1));
+    a.ticket = (int32_t *)(a.sums + (int64_t)a.blocks * E);
     hipStream_t st = (hipStream_t)stream;
     KN_TRY(kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
         return route_shape(E, [&](auto g, auto n) -> int {
             constexpr int G = decltype(g)::n, V = decltype(n)::n;
-            a.route.wide = route_wide(logits, ld, E, V, sizeof(E_));
-            return kn_launch(blocks, 256, [&](dim3 grid, int32_t first) {
-                a.route.first = first;
+            return kn_launch(a.blocks, 256, [&](dim3 grid, int32_t first) {
+                a.first = first;
                 if (one) hipLaunchKernelGGL((k_balance<E_, G, V, true>), grid, dim3(256), 0, st, a);
                 else hipLaunchKernelGGL((k_balance<E_, G, V, false>), grid, dim3(256), 0, st, a);
             });
         });
     }));
     if (one) return KN_OK;
-    hipLaunchKernelGGL(k_balance_join, dim3((unsigned)kn_div_up(E, BALANCE_JOIN)), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL(k_balance_join, dim3((unsigned)joins + 1), dim3(JOIN_COLUMNS * JOIN_TURNS), 0, st, a);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }
@@ -833,15 +882,18 @@ extern "C" int kn_route_balance_backward(void *stream, const void *logits, int32
     if (!route_valid(T, E, k) || !kn_dtype_ok(dtype) || ld < E || (T > 0 && (!logits || !counts || !dlosses || !dlogits))) return KN_E_INVALID_ARG;
     if (!route_supported(T, E, k)) return KN_E_UNSUPPORTED;
     if (T == 0) return KN_OK;
-    RouteArgs p = {logits, ld, (int32_t)T, E, k, 0, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0, 0};
+    BalanceArgs a = {};
+    a.logits = logits; a.add = add; a.dlogits = dlogits; a.ld = ld; a.T = (int32_t)T; a.E = E; a.k = k;
+    a.per = balance_rows(T, E);
+    a.counts = const_cast<int32_t *>(counts); a.dlosses = dlosses;
     return kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
         return route_shape(E, [&](auto g, auto n) -> int {
             constexpr int G = decltype(g)::n, V = decltype(n)::n;
-            p.wide = route_wide(logits, ld, E, V, sizeof(E_)) && route_wide(dlogits, E, E, V, sizeof(E_)) && (!add || route_wide(add, E, E, V, sizeof(E_)));
-            return kn_launch(kn_div_up(T, 256 / G), 256, [&](dim3 grid, int32_t first) {
-                p.first = first;
-                hipLaunchKernelGGL((k_balance_backward<E_, G, V>), grid, dim3(256), 0, (hipStream_t)stream, p, counts, dlosses, (const E_ *)add, (E_ *)dlogits);
+            return kn_launch(kn_div_up(T, a.per), 256, [&](dim3 grid, int32_t first) {
+                a.first = first;
+                if (add) hipLaunchKernelGGL((k_balance_backward<E_, G, V, true>), grid, dim3(256), 0, (hipStream_t)stream, a);
+                else hipLaunchKernelGGL((k_balance_backward<E_, G, V, false>), grid, dim3(256), 0, (hipStream_t)stream, a);
             });
         });
     });
