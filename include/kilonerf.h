@@ -401,6 +401,26 @@ int kn_grouped_linear_dw(void *stream, const kn_linear_desc *desc, const void *x
                          const int32_t *rows, void *dw /*dev E*K*N*/, void *db /*dev E*N, nullable*/, void *workspace,
                          int64_t workspace_bytes);
 
+/* Networks that share a layer and differ by a low-rank product (adapters of many requests beside one projection):
+ * h[i] = scales[e] x[r] A_e, y[i] = act(x[r] W + h[i] B_e + bias) for the rows i of network e, r = rows[i] (i itself where rows is NULL).  Rows of no
+ * network: act(x[r] W + bias); an entry of `rows` that x does not have: act(bias).  One rank for all networks (fewer: zeros); desc's n_in, n_out are
+ * W's, w_layout is that of all three: W (K, N), A (E, K, rank), B (E, rank, N), or W (N, K), A (E, rank, K), B (E, N, rank).
+ * scales: dev, E, nullable (ones); bias: dev, N.  h (dev, nullable, 16-byte aligned): M rows of `rank` values and zeros up to the next 16 bytes, in desc's
+ * dtype, to which the first product is rounded (16-bit matrix products take it in 16 bits); the backward call reads it.
+ * Workspace: dev, 256-byte aligned. */
+int kn_adapted_linear_workspace_bytes(const kn_linear_desc *desc, int32_t rank, int64_t *out_bytes);
+int kn_adapted_linear(void *stream, const kn_linear_desc *desc, int32_t rank, const void *x, const void *w, const void *a, const void *b,
+                      const float *scales, const void *bias, const int32_t *offsets, const int32_t *rows, int32_t relu, void *y /*dev M*N*/, void *h,
+                      void *workspace, int64_t workspace_bytes);
+/* Its gradients: dx[i] = dy[i] W^T + g[i] A_e^T with g[i] = scales[e] dy[i] B_e^T (a row per row of y; relu_in: 0 where x[r] is not above 0, which is the
+ * gradient before the ReLU that x is the result of), da[e] = sum of x[r]^T g[i], db[e] = sum of h[i]^T dy[i], laid out as a and b; zeros for a network
+ * without rows.  g is rounded as h is.  dy is the gradient before the layer's own ReLU.  Where W and bias are trained too, their gradients are
+ * kn_grouped_linear_dw's of one network whose rows are all M. */
+int kn_adapted_linear_backward_workspace_bytes(const kn_linear_desc *desc, int32_t rank, int64_t *out_bytes);
+int kn_adapted_linear_backward(void *stream, const kn_linear_desc *desc, int32_t rank, const void *dy, const void *x, const void *h, const void *w,
+                               const void *a, const void *b, const float *scales, const int32_t *offsets, const int32_t *rows, int32_t relu_in,
+                               void *dx /*dev M*K*/, void *da, void *db, void *workspace, int64_t workspace_bytes);
+
 /* The same layer in 8 bits (e4m3).  kb = ceil(K / 128) blocks of inputs, zeros behind the K-th.
  * kn_quantize_f8: rows x (R, K) -> q (dev, R * kb*128 bytes) and scales (dev, R * kb): s = max(amax, 2^-100) * (1/448), in fp32, over a
  * row's block, q the e4m3 nearest to the fp32 x / s.  A NaN stays one; an infinity makes its block zeros and NaN.

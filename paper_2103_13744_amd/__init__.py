@@ -25,6 +25,7 @@ EXPORTS = ["kn_error_string", "kn_last_hip_error", "kn_params_per_net", "kn_crea
            "kn_render", "kn_composite_deltas", "kn_march_stratified", "kn_render_stratified", "kn_set_render_params", "kn_profile_enable", "kn_profile_read",
            "kn_route_workspace_bytes", "kn_route", "kn_route_backward", "kn_route_balance_workspace_bytes", "kn_route_balance", "kn_route_balance_backward", "kn_grouped_linear", "kn_grouped_linear_dx", "kn_grouped_linear_dw",
            "kn_grouped_linear_dw_workspace_bytes",
+           "kn_adapted_linear_workspace_bytes", "kn_adapted_linear", "kn_adapted_linear_backward_workspace_bytes", "kn_adapted_linear_backward",
            "kn_quantize_f8", "kn_quantize_f8_weights", "kn_grouped_linear_f8", "kn_combine", "kn_combine_backward"]
 
 
@@ -117,6 +118,10 @@ def load_library(build_if_missing: bool = True):
     L.kn_grouped_linear_dx.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp]
     L.kn_grouped_linear_dw_workspace_bytes.argtypes = [desc, C.POINTER(i64)]
     L.kn_grouped_linear_dw.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp, vp, i64]
+    L.kn_adapted_linear_workspace_bytes.argtypes = [desc, i32, C.POINTER(i64)]
+    L.kn_adapted_linear.argtypes = [vp, desc, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, i64]
+    L.kn_adapted_linear_backward_workspace_bytes.argtypes = [desc, i32, C.POINTER(i64)]
+    L.kn_adapted_linear_backward.argtypes = [vp, desc, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, i64]
     L.kn_quantize_f8.argtypes = [vp, vp, i32, i64, i32, i64, vp, vp]
     L.kn_quantize_f8_weights.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp]
     L.kn_grouped_linear_f8.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp, vp, i32, vp]
@@ -618,6 +623,62 @@ def grouped_linear_backward(dy, x, w, offsets, rows=None, relu_in=False, want_bi
     """(dx, dw, db) of ``grouped_linear``: see ``grouped_linear_dx`` and ``grouped_linear_dw``.  dy is the gradient before the layer's
     own ReLU, if it has one: the next layer's ``relu_in`` gives that, and behind a last layer with a ReLU, dy * (y > 0)."""
     return (grouped_linear_dx(dy, x, w, offsets, rows, relu_in), *grouped_linear_dw(dy, x, w, offsets, rows, want_bias))
+
+
+def _adapted_args(x, w, a, b, offsets, rows, scales):
+    """(desc, M, rank, pointers of x, w, a, b, scales, offsets, rows): weights that are all contiguous, or all transposes of contiguous ones."""
+    if w.dim() != 2 or a.dim() != 3 or b.dim() != 3:
+        raise KnError("expected weights (n_in, n_out), (networks, n_in, rank) and (networks, rank, n_out), got %s, %s, %s" % (tuple(w.shape), tuple(a.shape), tuple(b.shape)))
+    K, N = w.shape
+    E, _, rank = a.shape
+    if a.shape != (E, K, rank) or b.shape != (E, rank, N) or not x.dtype is w.dtype is a.dtype is b.dtype:
+        raise KnError("expected weights (%d, %d), (%d, %d, %d) and (%d, %d, %d) of one dtype with x" % (K, N, E, K, rank, E, rank, N))
+    if not (w.is_cuda and a.is_cuda and b.is_cuda):
+        raise KnError("weights must be device tensors")
+    if w.is_contiguous() and a.is_contiguous() and b.is_contiguous():
+        layout = 0
+    elif w.t().is_contiguous() and a.transpose(1, 2).is_contiguous() and b.transpose(1, 2).is_contiguous():
+        layout = 1
+    else:
+        raise KnError("the shared weights and the adapters must all be contiguous, or all be transposes of contiguous weights")
+    px, ld = _rows_ptr(x, K)
+    M = x.shape[0] if rows is None else rows.shape[0]
+    d = LinearDesc(_dtype_id(x.dtype), layout, E, K, N, M, x.shape[0], ld)
+    return (d, M, rank, px, w.data_ptr(), a.data_ptr(), b.data_ptr(), _ptr(scales, torch.float32, allow_none=True, shape=(E,)),
+            _ptr(offsets, torch.int32, shape=(E + 1,)), None if rows is None else _ptr(rows, torch.int32, shape=(M,)))
+
+
+def adapted_linear(x, w, a, b, offsets, rows=None, scales=None, bias=None, relu=False, want_h=False, out=None):
+    """A layer that all networks share, with a low-rank product of each one's own: row i of the result, of network e with offsets[e] <= i < offsets[e + 1], is
+    x[rows[i]] @ w + h[i] @ b[e] + bias with h[i] = scales[e] * (x[rows[i]] @ a[e]), then a ReLU where asked for; rows from offsets[E] on have no
+    such product.  ``w``: (n_in, n_out), ``a``: (E, n_in, rank), ``b``: (E, rank, n_out), all contiguous, or all transposes of contiguous weights;
+    ``scales``: (E,) float32 or None (ones).  ``want_h``: (result, h) for ``adapted_linear_backward``, h in rows of whole 16 bytes."""
+    L = load_library()
+    d, M, rank, px, pw, pa, pb, ps, po, pr = _adapted_args(x, w, a, b, offsets, rows, scales)
+    if out is None:
+        out = x.new_empty((M, d.n_out))
+    unit = 4 if d.dtype == KN_F32 else 8
+    h, need = x.new_empty((M, -(-rank // unit) * unit)) if want_h else None, C.c_int64()
+    _check(L.kn_adapted_linear_workspace_bytes(C.byref(d), rank, C.byref(need)), "kn_adapted_linear_workspace_bytes")
+    ws = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+    _check(L.kn_adapted_linear(_stream(), C.byref(d), rank, px, pw, pa, pb, ps, _ptr(bias, x.dtype, allow_none=True, shape=(d.n_out,)), po, pr, 1 if relu else 0,
+                               _ptr(out, x.dtype, shape=(M, d.n_out)), None if h is None else h.data_ptr(), ws.data_ptr(), need.value), "kn_adapted_linear")
+    return (out, h) if want_h else out
+
+
+def adapted_linear_backward(dy, x, h, w, a, b, offsets, rows=None, scales=None, relu_in=False):
+    """(dx, da, db) of ``adapted_linear`` with its h: dx (M, n_in) has a row per row of dy, da and db are laid out as a and b.  ``relu_in`` and dy as in
+    ``grouped_linear_backward``.  The gradients of w and bias, where those are trained: ``grouped_linear_dw`` with w[None] and offsets [0, M]."""
+    L = load_library()
+    d, M, rank, px, pw, pa, pb, ps, po, pr = _adapted_args(x, w, a, b, offsets, rows, scales)
+    unit = 4 if d.dtype == KN_F32 else 8
+    dx, da, db, need = x.new_empty((M, d.n_in)), torch.empty_like(a), torch.empty_like(b), C.c_int64()
+    _check(L.kn_adapted_linear_backward_workspace_bytes(C.byref(d), rank, C.byref(need)), "kn_adapted_linear_backward_workspace_bytes")
+    ws = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+    _check(L.kn_adapted_linear_backward(_stream(), C.byref(d), rank, _ptr(dy, x.dtype, shape=(M, d.n_out)), px, _ptr(h, x.dtype, shape=(M, -(-rank // unit) * unit)),
+                                        pw, pa, pb, ps, po, pr, 1 if relu_in else 0, dx.data_ptr(), da.data_ptr(), db.data_ptr(), ws.data_ptr(), need.value),
+           "kn_adapted_linear_backward")
+    return dx, da, db
 
 
 def quantize_f8(x):

@@ -1,0 +1,493 @@
+// A layer that all networks share, with a low-rank product of each network's own beside it (kn_adapted_linear), and its gradients.
+//
+// y_i = x_i W + h_i B_e, h_i = s_e x_i A_e.  The second part is the first's contraction, made longer: a tile of rows meets n networks, and their B one
+// under the other are a matrix of n times the rank rows, before which a row's h stands in the columns of its own network, between zeros.  So
+// rows of all networks share tiles of W, whatever their order costs is the contraction of a few more steps, and y is written once.
+#include "kn_tile.h"
+
+#include <type_traits>
+
+namespace {
+
+// h(i, j) = scale_e sum over c of a(i, c) b_e(c, j), rows of `rp` values with zeros behind the rank; net(i): the row's network, or -1
+struct Down {
+    const void *a, *b;
+    const float *scales;
+    void *h;
+    int32_t *net;
+    const int32_t *offsets, *rows;
+    int64_t lda, b_group, b_c, b_j;
+    int32_t M, E, C, rank, rp, a_rows;
+    int32_t first; // number of the launch's first workgroup
+};
+// What the shared product takes beside its own operands
+struct Beside {
+    const void *h, *b;
+    const int32_t *net;
+    int64_t b_group, b_c, b_j;
+    int32_t E, rank, rp;
+};
+
+// Values k .. k + W - 1 of a contraction of C in steps of `step`
+template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type strided_piece(const T *at, int64_t step, int32_t k, int32_t C)
+{
+    typename KnFrag<T>::Type f;
+#pragma unroll
+    for (int q = 0; q < 16 / (int)sizeof(T); ++q) {
+        const T v = at[min(k + q, C - 1) * step];
+        f[q] = k + q < C ? v : (T)0.0f;
+    }
+    return f;
+}
+
+// 16 U rows of one network by 16 columns: a workgroup's WAVES wavefronts take every WAVES-th step of the contraction, straight into registers, and are summed in
+// the order of their numbers.  COLS: b's columns are contiguous (else its contraction is).
+template <typename T, bool COLS, int U, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) k_adapt_down(Down p)
+{
+    constexpr int W = 16 / sizeof(T), KS = 4 * W, LD = 20;
+    typedef typename KnFrag<T>::Type Frag;
+    __shared__ __align__(16) float red[WAVES * 16 * U * LD];
+    const int tid = kn_thread(), lane = tid & 63, col = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ntiles = (p.rp + 15) / 16;
+    const int32_t number = p.first + kn_block();
+    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, 16 * U, number / ntiles);
+    const int j0 = number % ntiles * 16;
+    if (piece.begin >= piece.end) return;
+    const bool some = piece.group < p.E;
+    const int64_t group = some ? piece.group : 0;
+    const T *arow[U], *b = (const T *)p.b + group * p.b_group + (int64_t)min(j0 + col, p.rank - 1) * p.b_j;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int32_t i = min(piece.begin + 16 * u + col, piece.end - 1), src = p.rows ? p.rows[i] : i;
+        arow[u] = (const T *)p.a + (int64_t)((uint32_t)src < (uint32_t)p.a_rows ? src : 0) * p.lda;
+    }
+    const int32_t steps = some && p.a_rows > 0 ? (p.C + KS - 1) / KS : 0;
+    kn_f32x4 acc[U] = {};
+    for (int32_t s = wave; s < steps; s += WAVES) {
+        const int32_t k = s * KS + W * g;
+        const Frag fb = COLS ? strided_piece<T>(b, p.b_c, k, p.C) : kn_any_piece<T>(b, k, p.C);
+#pragma unroll
+        for (int u = 0; u < U; ++u) acc[u] = kn_mfma(fb, kn_any_piece<T>(arow[u], k, p.C), acc[u]);
+    }
+    // (a lane's four results are neighbours in a row)
+#pragma unroll
+    for (int u = 0; u < U; ++u) *(kn_f32x4 *)(red + ((wave * U + u) * 16 + col) * LD + 4 * g) = acc[u];
+    __syncthreads();
+    const float scale = p.scales && some ? p.scales[group] : 1.0f;
+    for (int q = tid; q < 16 * U * 4; q += WAVES * 64) {
+        const int r = q >> 2, j = j0 + (q & 3) * 4;
+        const int32_t i = piece.begin + r;
+        if (i >= piece.end) continue;
+        if (j == 0) p.net[i] = some ? piece.group : -1;
+        if (j >= p.rp) continue;
+        kn_f32x4 y = {0, 0, 0, 0};
+        if (!p.rows || (uint32_t)p.rows[i] < (uint32_t)p.a_rows)
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) y += *(const kn_f32x4 *)(red + (w * 16 * U + r) * LD + (q & 3) * 4);
+        typedef T Four __attribute__((ext_vector_type(4)));
+        Four o;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) o[n] = j + n < p.rank ? (T)(scale * y[n]) : (T)0.0f; // (16 bits: what the matrix cores take)
+        *(Four *)((T *)p.h + (int64_t)i * p.rp + j) = o;
+    }
+}
+
+// A stage of the rows' h, row-wise: row r's stand at columns slot_r * rp of the longer contraction
+template <typename T, int R, int NW, bool DIRECT> struct LoadH {
+    static constexpr int N = R / 8 / NW, CS = 128 / sizeof(T), W = 16 / sizeof(T);
+    const T *at[N];
+    int32_t first[N]; // column of the row's first value (negative: none)
+    typename KnFrag<T>::Type held[DIRECT ? 1 : N];
+    int32_t piece, rp;
+    __device__ __forceinline__ void start(int wave, int lane, const T *h, int32_t width, int32_t begin, int32_t end, const int32_t *slots)
+    {
+        piece = (lane & 7) ^ (lane >> 3);
+        rp = width;
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const int r = (wave * N + t) * 8 + (lane >> 3);
+            const int32_t slot = slots[r];
+            first[t] = slot < 0 ? -1 : slot * rp;
+            at[t] = h + (int64_t)min(begin + r, end - 1) * rp;
+        }
+    }
+    __device__ __forceinline__ const T *from(int t, int s) const // (nullptr: zeros)
+    {
+        const int32_t q = s * CS + piece * W - first[t];
+        return first[t] >= 0 && q >= 0 && q < rp ? at[t] + q : nullptr;
+    }
+    __device__ __forceinline__ void ask(int s)
+    {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const T *v = from(t, s);
+            held[t] = typename KnFrag<T>::Type{};
+            if (v) held[t] = *(const typename KnFrag<T>::Type *)v;
+        }
+    }
+    __device__ __forceinline__ void fetch(KN_LDS char *tile, int wave, int lane, int s)
+    {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            if constexpr (DIRECT) {
+                const T *v = from(t, s);
+                kn_fetch(v ? (const void *)v : (const void *)&kn_zeros, tile + (wave * N + t) * 1024);
+            } else {
+                *(KN_LDS typename KnFrag<T>::Type *)(tile + (wave * N + t) * 1024 + lane * 16) = held[t];
+            }
+        }
+    }
+};
+// A stage of the networks' B one under the other, column-wise (COLS) or row-wise, R columns of it
+template <typename T, int R, int NW, bool COLS, bool DIRECT> struct LoadB {
+    static constexpr int CS = 128 / sizeof(T), W = 16 / sizeof(T), PR = R / W, RP = 64 / PR, N = COLS ? CS / RP / NW : R / 8 / NW;
+    typename KnFrag<T>::Type held[DIRECT ? 1 : N];
+    const T *b;
+    const int32_t *nets;
+    int64_t group, along, across;
+    int32_t j0, J, count, rp, rank;
+    __device__ __forceinline__ void start(const Beside &p, int32_t first, int32_t columns, const int32_t *of, int32_t n)
+    {
+        b = (const T *)p.b;
+        nets = of;
+        group = p.b_group; along = p.b_c; across = p.b_j;
+        j0 = first; J = columns; count = n; rp = p.rp; rank = p.rank;
+    }
+    // where the lane's piece t of stage s begins (nullptr: zeros), and how many of its values are there
+    __device__ __forceinline__ const T *from(int wave, int lane, int t, int s, int32_t &left) const
+    {
+        int32_t c, k;
+        if constexpr (COLS) {
+            const int r = (wave * N + t) * RP + lane / PR;
+            c = s * CS + r;
+            k = ((lane % PR) ^ kn_col_swizzle<T, COLS ? R : 64>(r)) * W;
+            if (DIRECT) k = min(k, J - j0 - W);
+            left = J - j0 - k;
+        } else {
+            k = min((wave * N + t) * 8 + (lane >> 3), J - 1 - j0);
+            c = s * CS + ((lane & 7) ^ (lane >> 3)) * W;
+        }
+        const int32_t slot = (uint32_t)c / (uint32_t)rp, q = c - slot * rp;
+        if constexpr (!COLS) left = rank - q;
+        if (slot >= count || q >= rank || left <= 0) return nullptr;
+        return b + nets[slot] * group + q * along + (j0 + k) * across;
+    }
+    __device__ __forceinline__ void ask(int wave, int lane, int s)
+    {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            int32_t left;
+            const T *v = from(wave, lane, t, s, left);
+            held[t] = typename KnFrag<T>::Type{};
+            if (v) held[t] = kn_any_piece<T>(v, 0, left);
+        }
+    }
+    __device__ __forceinline__ void fetch(KN_LDS char *tile, int wave, int lane, int s)
+    {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            if constexpr (DIRECT) {
+                int32_t left;
+                const T *v = from(wave, lane, t, s, left);
+                kn_fetch(v ? (const void *)v : (const void *)&kn_zeros, tile + (wave * N + t) * 1024);
+            } else {
+                *(KN_LDS typename KnFrag<T>::Type *)(tile + (wave * N + t) * 1024 + lane * 16) = held[t];
+            }
+        }
+    }
+};
+
+// Tiles of BM x BN results, WR x WC wavefronts, NB stages in the LDS, of which one is multiplied while the others are fetched, as in the grouped products; behind the
+// stages of the shared contraction come those of the tile's networks.  COLS: the columns of w and b are contiguous (else the contraction is).  DIRECT: rows
+// of whole 16-byte pieces throughout.
+template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB>
+__global__ void __launch_bounds__(WR * WC * 64) k_adapt_up(KnProduct p, Beside beside, int32_t blocks)
+{
+    constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16, CS = 128 / sizeof(T);
+    typedef typename KnFrag<T>::Type Frag;
+    static_assert(DIRECT || NB == 2, "");
+    static_assert(BM <= NW * 64, "a thread looks at a row");
+    typedef KnRowLoader<T, BM, NW, DIRECT> LoadA;
+    constexpr int BYTES = NB * STAGE > NW * 16 * (BN / WC + 4) * 4 ? NB * STAGE : NW * 16 * (BN / WC + 4) * 4;
+    __shared__ __align__(16) char lds_[BYTES];
+    __shared__ int32_t slots[BM], nets[BM], met[NW]; // a row's place among the tile's networks (-1: none), the networks, how many begin in a wavefront's rows
+    KN_LDS char *lds = (KN_LDS char *)lds_;
+    const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ntiles = (p.J + BN - 1) / BN;
+    const int32_t number = kn_xcd_order(p.first + kn_block(), blocks);
+    const int32_t begin = number / ntiles * BM, end = min(p.M, begin + BM);
+    const int j0 = number % ntiles * BN;
+    int32_t count = 0;
+    {
+        const int32_t i = begin + tid;
+        const bool in = tid < BM && i < end;
+        const int32_t net = in ? beside.net[i] : -1, before = in && tid > 0 ? beside.net[i - 1] : -1;
+        const bool some = (uint32_t)net < (uint32_t)beside.E, begins = some && net != before;
+        const uint64_t all = __ballot(begins);
+        if (lane == 0) met[wave] = __popcll(all);
+        __syncthreads();
+        int32_t rank = __popcll(all & ((2ull << lane) - 1)) - 1;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            if (w < wave) rank += met[w];
+            count += met[w];
+        }
+        if (tid < BM) slots[tid] = some ? rank : -1;
+        if (begins) nets[rank] = net;
+        __syncthreads();
+    }
+    const T *a = (const T *)p.a, *b = (const T *)p.b;
+    LoadA la;
+    la.start(wave, lane, [&](int r) {
+        const int32_t i = min(begin + r, end - 1);
+        const int32_t src = p.rows ? p.rows[i] : i;
+        return a + (int64_t)((uint32_t)src < (uint32_t)p.a_rows ? src : 0) * p.lda;
+    });
+    KnRowLoader<T, BN, NW, DIRECT> lbr;
+    KnColLoader<T, BN, NW, DIRECT> lbc;
+    if constexpr (COLS) lbc.start(wave, lane, b + j0, p.b_c, p.J - j0);
+    else lbr.start(wave, lane, [&](int r) { return b + (int64_t)min(j0 + r, p.J - 1) * p.b_j; });
+    LoadH<T, BM, NW, DIRECT> lh;
+    LoadB<T, BN, NW, COLS, DIRECT> lo;
+    lh.start(wave, lane, (const T *)beside.h, beside.rp, begin, end, slots);
+    lo.start(beside, j0, p.J, nets, count);
+    const int32_t C = p.a_rows > 0 ? p.C : 0, shared = (C + CS - 1) / CS, steps = C > 0 ? shared + (count * beside.rp + CS - 1) / CS : 0;
+    constexpr int LOADS = LoadA::N + (COLS ? lbc.N : lbr.N); // a wavefront's, per stage
+    static_assert(LOADS == lh.N + lo.N, "");
+    constexpr int LATER = DIRECT ? (NB - 2) * LOADS : 63; // (loads into registers are waited for where they are put down)
+    auto fetch = [&](int s, int at) {
+        KN_LDS char *tile = lds + at * STAGE;
+        if (s < shared) {
+            la.fetch(tile, wave, lane, C - s * CS);
+            if constexpr (COLS) lbc.fetch(tile + BM * 128, wave, lane, C - s * CS);
+            else lbr.fetch(tile + BM * 128, wave, lane, C - s * CS);
+        } else {
+            lh.fetch(tile, wave, lane, s - shared);
+            lo.fetch(tile + BM * 128, wave, lane, s - shared);
+        }
+        if (!DIRECT && s + 1 >= shared && s + 1 < steps) {
+            lh.ask(s + 1 - shared);
+            lo.ask(wave, lane, s + 1 - shared);
+        }
+    };
+    const int wi = (wave / WC) * (BM / WR), wj = (wave % WC) * (BN / WC);
+    kn_f32x4 acc[U][V] = {};
+    Frag fa[2][U], fb[2][V];
+    auto read = [&](int at, int kk) {
+        const KN_LDS char *ta = lds + at * STAGE, *tb = ta + BM * 128;
+#pragma unroll
+        for (int u = 0; u < U; ++u) fa[kk][u] = kn_row_frag<T>(ta, wi + 16 * u, kk, lane);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if constexpr (COLS) fb[kk][v] = kn_col_frag<T, BN>(tb, wj + 16 * v, kk, lane);
+            else fb[kk][v] = kn_row_frag<T>(tb, wj + 16 * v, kk, lane);
+        }
+    };
+    auto march = [&](auto rows_there) {
+        constexpr bool ROWS = decltype(rows_there)::value;
+        auto multiply = [&](int kk) {
+            if constexpr (ROWS) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(fb[kk][v], fa[kk][u], acc[u][v]);
+                kn_interleave<U, V, T, COLS>();
+            }
+        };
+        if constexpr (ROWS) read(0, 0);
+        for (int s = 0, at = 0; s < steps; ++s) {
+            const int next = at + 1 == NB ? 0 : at + 1;
+            if constexpr (ROWS) read(at, 1);
+            multiply(0);
+            if (s + NB <= steps) kn_stage_barrier<LATER>();
+            else kn_stage_barrier<0>();
+            if (s + NB < steps) fetch(s + NB, at);
+            if constexpr (ROWS) read(next, 0); // (behind the last stage: what happens to lie there, unused)
+            multiply(1);
+            at = next;
+        }
+    };
+    if (steps > 0) {
+        la.ask_first(C);
+        if constexpr (COLS) lbc.ask_first(wave, lane, C);
+        else lbr.ask_first(C);
+        for (int s = 0; s < NB && s < steps; ++s) fetch(s, s);
+        if (DIRECT && steps >= NB) kn_stage_barrier<(NB - 1) * LOADS>();
+        else kn_stage_barrier<0>();
+        if (WR == 1 || begin + wi < end) march(std::true_type());
+        else march(std::false_type());
+    }
+    kn_stage_barrier(); // (the tiles' LDS is used again)
+    // 16 rows of the wavefront's results at a time, in LDS of its own
+    constexpr int WN = BN / WC, LD = WN + 4, LR = WN / 8; // LR lanes take a row
+    KN_LDS float *mine = (KN_LDS float *)(lds + wave * (16 * LD * 4));
+    static_assert(64 % LR == 0, "");
+    const int cj = lane % LR * 8;
+    const int32_t j = j0 + wj + cj;
+    float add[8];
+    kn_bias_of<T>(p, true, 0, j, add);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) *(KN_LDS kn_f32x4 *)(mine + (lane & 15) * LD + 16 * v + (lane >> 4) * 4) = acc[u][v];
+        kn_lanes_meet();
+#pragma unroll
+        for (int h = 0; h < (16 * LR + 63) / 64; ++h) {
+            const int r = h * (64 / LR) + lane / LR;
+            const int32_t i = begin + wi + 16 * u + r;
+            if (r >= 16 || i >= end || j >= p.J) continue;
+            const kn_f32x4 lo4 = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj), hi4 = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj + 4);
+            float y[8] = {lo4[0], lo4[1], lo4[2], lo4[3], hi4[0], hi4[1], hi4[2], hi4[3]};
+            kn_finish<T>(p, true, i, j, add, y);
+        }
+        kn_lanes_meet();
+    }
+}
+
+template <typename T, bool COLS> int launch_down(hipStream_t st, const Down &p)
+{
+    const int ntiles = (p.rp + 15) / 16;
+    const bool narrow = p.C * (int64_t)sizeof(T) <= 512;
+    return kn_launch(kn_pieces(p.M, p.E, 32) * ntiles, narrow ? 64 : 512, [&](dim3 grid, int32_t first) {
+        Down q = p;
+        q.first = first;
+        if (narrow) hipLaunchKernelGGL((k_adapt_down<T, COLS, 2, 1>), grid, dim3(64), 0, st, q);
+        else hipLaunchKernelGGL((k_adapt_down<T, COLS, 2, 8>), grid, dim3(512), 0, st, q);
+    });
+}
+
+template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB> int launch_tiles(hipStream_t st, const KnProduct &p, const Beside &beside)
+{
+    const int64_t blocks = kn_div_up(p.M, BM) * kn_div_up(p.J, BN);
+    return kn_launch(blocks, WR * WC * 64, [&](dim3 grid, int32_t first) {
+        KnProduct q = p;
+        q.first = first;
+        hipLaunchKernelGGL((k_adapt_up<T, COLS, DIRECT, BM, BN, WR, WC, NB>), grid, dim3(WR * WC * 64), 0, st, q, beside, (int32_t)blocks);
+    });
+}
+
+template <typename T, bool COLS> int launch_up(hipStream_t st, const KnProduct &p, const Beside &beside)
+{
+    constexpr int64_t W = 16 / sizeof(T);
+    auto tiles = [&](int64_t bm) { return (p.M + bm - 1) / bm * ((p.J + 127) / 128); };
+    const bool direct = (((uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)beside.b) & 15) == 0 && p.C % W == 0 && p.lda % W == 0 && (COLS ? p.J % W == 0 : beside.rank % W == 0);
+    const bool narrow = p.J <= 64 || tiles(64) < 256;
+    if constexpr (sizeof(T) == 4) {
+        if (!direct) return narrow ? launch_tiles<T, COLS, false, 32, 64, 1, 4, 2>(st, p, beside) : launch_tiles<T, COLS, false, 64, 128, 1, 4, 2>(st, p, beside);
+        return narrow ? launch_tiles<T, COLS, true, 32, 64, 1, 4, 4>(st, p, beside) : launch_tiles<T, COLS, true, 64, 128, 1, 4, 2>(st, p, beside);
+    } else {
+        if (!direct) return narrow ? launch_tiles<T, COLS, false, 32, 64, 1, 4, 2>(st, p, beside) : launch_tiles<T, COLS, false, 128, 128, 2, 4, 2>(st, p, beside);
+        if (narrow) return launch_tiles<T, COLS, true, 32, 64, 1, 4, 4>(st, p, beside);
+        if (tiles(192) >= 256) return launch_tiles<T, COLS, true, 192, 128, 2, 2, 2>(st, p, beside);
+        return launch_tiles<T, COLS, true, 64, 128, 1, 4, 2>(st, p, beside);
+    }
+}
+
+// Both products of a call on `a` (rows through `rows`): h = scale a b_e, out = a w + h c_e.  cols: those of b are contiguous, and not those of w and c
+int run(hipStream_t st, int32_t dtype, bool b_cols, const Down &down, const KnProduct &up, const Beside &beside)
+{
+    return kn_with_type(dtype, [&](auto v) -> int {
+        typedef decltype(v) E_;
+        KN_TRY(b_cols ? (launch_down<E_, true>(st, down)) : (launch_down<E_, false>(st, down)));
+        return up.b_j == 1 && up.b_c != 1 ? launch_up<E_, true>(st, up, beside) : launch_up<E_, false>(st, up, beside);
+    });
+}
+
+int32_t padded_rank(int32_t dtype, int32_t rank) { return (int32_t)kn_align_up(rank, 16 / kn_item(dtype)); }
+int check(const kn_linear_desc *d, int32_t rank)
+{
+    KN_TRY(kn_linear_check(d));
+    if (rank < 1) return KN_E_INVALID_ARG;
+    return rank > KN_MAX_WIDTH ? KN_E_UNSUPPORTED : KN_OK;
+}
+int64_t net_bytes(const kn_linear_desc *d) { return kn_align_up(d->rows * 4, 256); }
+int64_t h_bytes(const kn_linear_desc *d, int32_t rank) { return kn_align_up(d->rows * (int64_t)padded_rank(d->dtype, rank) * kn_item(d->dtype), 256); }
+// The gradients of A and B as those of a grouped layer
+kn_linear_desc layer_of(const kn_linear_desc *d, int32_t n_in, int32_t n_out, int64_t x_rows, int64_t ldx)
+{
+    kn_linear_desc l = *d;
+    l.n_in = n_in; l.n_out = n_out; l.x_rows = x_rows; l.ldx = ldx;
+    return l;
+}
+int dw_bytes(const kn_linear_desc *d, int32_t rank, int64_t *out)
+{
+    const kn_linear_desc a = layer_of(d, d->n_in, rank, d->x_rows, d->ldx), b = layer_of(d, rank, d->n_out, d->rows, padded_rank(d->dtype, rank));
+    int64_t na = 0, nb = 0;
+    KN_TRY(kn_grouped_linear_dw_workspace_bytes(&a, &na));
+    KN_TRY(kn_grouped_linear_dw_workspace_bytes(&b, &nb));
+    *out = na > nb ? na : nb;
+    return KN_OK;
+}
+bool bad_workspace(const void *ws, int64_t have, int64_t need) { return need > 0 && (!ws || ((uintptr_t)ws & 255) || have < need); }
+
+} // namespace
+
+extern "C" int kn_adapted_linear_workspace_bytes(const kn_linear_desc *d, int32_t rank, int64_t *out_bytes)
+{
+    KN_TRY(check(d, rank));
+    if (!out_bytes) return KN_E_INVALID_ARG;
+    *out_bytes = net_bytes(d) + h_bytes(d, rank);
+    return KN_OK;
+}
+
+extern "C" int kn_adapted_linear(void *stream, const kn_linear_desc *d, int32_t rank, const void *x, const void *w, const void *a, const void *b,
+                                 const float *scales, const void *bias, const int32_t *offsets, const int32_t *rows, int32_t relu, void *y, void *h,
+                                 void *workspace, int64_t workspace_bytes)
+{
+    KN_TRY(check(d, rank));
+    if (d->rows == 0) return KN_OK;
+    if (!w || !a || !b || !offsets || !y || (d->x_rows > 0 && !x) || (!rows && d->x_rows < d->rows) || ((uintptr_t)h & 15)) return KN_E_INVALID_ARG;
+    if (bad_workspace(workspace, workspace_bytes, net_bytes(d) + h_bytes(d, rank))) return KN_E_WORKSPACE;
+    const bool io = d->w_layout == KN_W_IN_OUT;
+    const int64_t K = d->n_in, N = d->n_out, R = rank;
+    Down down = {x, a, scales, h ? h : (char *)workspace + net_bytes(d), (int32_t *)workspace, offsets, rows, d->ldx, K * R, io ? R : 1, io ? 1 : K,
+                 (int32_t)d->rows, d->experts, d->n_in, rank, padded_rank(d->dtype, rank), (int32_t)d->x_rows, 0};
+    Beside beside = {down.h, b, down.net, R * N, io ? N : 1, io ? 1 : R, d->experts, rank, down.rp};
+    KnProduct p = {};
+    p.a = x; p.b = w; p.bias = bias; p.out = y; p.rows = rows;
+    p.lda = d->ldx; p.b_c = io ? N : 1; p.b_j = io ? 1 : K; p.o_i = N;
+    p.M = down.M; p.J = d->n_out; p.C = d->n_in; p.a_rows = down.a_rows; p.relu = relu != 0;
+    return run((hipStream_t)stream, d->dtype, io, down, p, beside);
+}
+
+extern "C" int kn_adapted_linear_backward_workspace_bytes(const kn_linear_desc *d, int32_t rank, int64_t *out_bytes)
+{
+    KN_TRY(check(d, rank));
+    if (!out_bytes) return KN_E_INVALID_ARG;
+    int64_t dw = 0;
+    KN_TRY(dw_bytes(d, rank, &dw));
+    *out_bytes = net_bytes(d) + h_bytes(d, rank) + dw;
+    return KN_OK;
+}
+
+extern "C" int kn_adapted_linear_backward(void *stream, const kn_linear_desc *d, int32_t rank, const void *dy, const void *x, const void *h, const void *w,
+                                          const void *a, const void *b, const float *scales, const int32_t *offsets, const int32_t *rows, int32_t relu_in,
+                                          void *dx, void *da, void *db, void *workspace, int64_t workspace_bytes)
+{
+    KN_TRY(check(d, rank));
+    if (!offsets || !da || !db ||
+        (d->rows > 0 && (!dy || !h || !w || !a || !b || !dx || (d->x_rows > 0 && !x) || (!rows && d->x_rows < d->rows) || ((uintptr_t)h & 15))))
+        return KN_E_INVALID_ARG;
+    int64_t dw = 0;
+    KN_TRY(dw_bytes(d, rank, &dw));
+    if (bad_workspace(workspace, workspace_bytes, net_bytes(d) + h_bytes(d, rank) + dw)) return KN_E_WORKSPACE;
+    const bool io = d->w_layout == KN_W_IN_OUT;
+    const int64_t K = d->n_in, N = d->n_out, R = rank;
+    char *g = (char *)workspace + net_bytes(d), *sums = g + h_bytes(d, rank);
+    const int32_t rp = padded_rank(d->dtype, rank);
+    if (d->rows > 0) {
+        Down down = {dy, b, scales, g, (int32_t *)workspace, offsets, nullptr, N, R * N, io ? 1 : R, io ? N : 1,
+                     (int32_t)d->rows, d->experts, d->n_out, rank, rp, (int32_t)d->rows, 0};
+        Beside beside = {g, a, down.net, K * R, io ? 1 : K, io ? R : 1, d->experts, rank, rp};
+        KnProduct p = {};
+        p.a = dy; p.b = w; p.mask = relu_in ? (x ? x : w) : nullptr; p.out = dx; // (an x without rows may have no address)
+        p.lda = N; p.ldm = d->ldx; p.b_c = io ? 1 : K; p.b_j = io ? N : 1; p.o_i = K;
+        p.M = down.M; p.J = d->n_in; p.C = d->n_out; p.a_rows = p.M; p.m_rows = (int32_t)d->x_rows;
+        p.mask_rows = relu_in ? rows : nullptr;
+        KN_TRY(run((hipStream_t)stream, d->dtype, !io, down, p, beside));
+    }
+    const kn_linear_desc la = layer_of(d, d->n_in, rank, d->x_rows, d->ldx), lb = layer_of(d, rank, d->n_out, d->rows, rp);
+    KN_TRY(kn_linear_dw_run(stream, &la, x, g, rp, offsets, rows, da, nullptr, sums, dw));
+    return kn_linear_dw_run(stream, &lb, h, dy, N, offsets, nullptr, db, nullptr, sums, dw);
+}

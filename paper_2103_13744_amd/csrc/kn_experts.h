@@ -126,6 +126,10 @@ struct KnProduct {
     int32_t first;                   // number of the launch's first workgroup
 };
 
+// kn_grouped_linear_dw, with rows of dy that may lie apart
+int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const void *dy, int64_t lddy, const int32_t *offsets, const int32_t *rows,
+                     void *dw, void *db, void *workspace, int64_t workspace_bytes);
+
 // What the grouped products check alike
 static inline int kn_linear_check(const kn_linear_desc *d)
 {

@@ -5,42 +5,6 @@
 
 namespace {
 
-// What is added to columns j .. j + 7 of a network's results (j a multiple of 8)
-template <typename T> __device__ __forceinline__ void bias_of(const KnProduct &p, bool some, int64_t group, int32_t j, float add[8])
-{
-    const bool any = p.bias && some && j < p.J;
-    typename KnEight<T>::Piece v = {};
-    if (any) v = KnEight<T>::load((const T *)p.bias + group * p.J, j, p.J);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) add[q] = any ? (float)v[q] : 0.0f;
-}
-// The end of 8 neighbouring results of row i: zeros for a row that x does not have, bias, ReLU, the mask of a ReLU before; one rounding
-template <typename T>
-__device__ __forceinline__ void finish(const KnProduct &p, bool some, int32_t i, int32_t j, const float add[8], float y[8])
-{
-    if (p.rows && (uint32_t)p.rows[i] >= (uint32_t)p.a_rows) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) y[q] = 0.0f;
-    }
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        y[q] += add[q];
-        if (p.relu) y[q] = y[q] > 0.0f || y[q] != y[q] ? y[q] : 0.0f; // (a NaN stays one)
-    }
-    if (p.mask && some) {
-        const int32_t src = p.mask_rows ? p.mask_rows[i] : i;
-        typename KnEight<T>::Piece m = {};
-        if ((uint32_t)src < (uint32_t)p.m_rows) m = KnEight<T>::load((const T *)p.mask + (int64_t)src * p.ldm, j, p.J);
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (!((float)m[q] > 0.0f)) y[q] = 0.0f;
-    }
-    typename KnEight<T>::Piece o;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) o[q] = (T)y[q];
-    KnEight<T>::store((T *)p.out + (int64_t)i * p.o_i, j, p.J, o);
-}
-
 // Tiles of BM x BN results, WR x WC wavefronts, NB stages in the LDS, of which one is multiplied while the others are fetched.  COLS:
 // b's columns are contiguous in memory (else its contraction is).  DIRECT: rows of whole 16-byte pieces throughout (KnRowLoader).
 // Fragments of b are the products' first operand, so that a lane holds four neighbouring results of a row; they go through
@@ -146,7 +110,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
     const int cj = lane % LR * 8;
     const int32_t j = j0 + wj + cj;
     float add[8];
-    bias_of<T>(p, some, group, j, add);
+    kn_bias_of<T>(p, some, group, j, add);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -159,7 +123,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
             if (r >= 16 || i >= piece.end || j >= p.J) continue;
             const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj + 4);
             float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            finish<T>(p, some, i, j, add, y);
+            kn_finish<T>(p, some, i, j, add, y);
         }
         kn_lanes_meet();
     }
@@ -243,8 +207,8 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p)
 #pragma unroll
             for (int n = 0; n < 4; ++n) { y[n] += lo[n]; y[n + 4] += hi[n]; }
         }
-        bias_of<T>(p, some, group, j, add);
-        finish<T>(p, some, i, j, add, y);
+        kn_bias_of<T>(p, some, group, j, add);
+        kn_finish<T>(p, some, i, j, add, y);
     }
 }
 

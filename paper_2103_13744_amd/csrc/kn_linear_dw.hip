@@ -397,6 +397,12 @@ extern "C" int kn_grouped_linear_dw_workspace_bytes(const kn_linear_desc *d, int
 extern "C" int kn_grouped_linear_dw(void *stream, const kn_linear_desc *d, const void *x, const void *dy, const int32_t *offsets,
                                     const int32_t *rows, void *dw, void *db, void *workspace, int64_t workspace_bytes)
 {
+    return kn_linear_dw_run(stream, d, x, dy, d ? d->n_out : 0, offsets, rows, dw, db, workspace, workspace_bytes);
+}
+
+int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const void *dy, int64_t lddy, const int32_t *offsets, const int32_t *rows,
+                     void *dw, void *db, void *workspace, int64_t workspace_bytes)
+{
     KN_TRY(kn_linear_check(d));
     if (!offsets || !dw || (d->rows > 0 && (!dy || (d->x_rows > 0 && !x))) || (d->rows > 0 && !rows && d->x_rows < d->rows)) return KN_E_INVALID_ARG;
     int64_t need = 0;
@@ -407,7 +413,7 @@ extern "C" int kn_grouped_linear_dw(void *stream, const kn_linear_desc *d, const
     KnProduct p = {};
     const bool io = d->w_layout == KN_W_IN_OUT; // (columns are what is contiguous in dw)
     p.a = io ? x : dy; p.b = io ? dy : x;
-    p.lda = io ? d->ldx : d->n_out; p.ldb = io ? d->n_out : d->ldx;
+    p.lda = io ? d->ldx : lddy; p.ldb = io ? lddy : d->ldx;
     p.rows = io ? rows : nullptr; p.b_index = io ? nullptr : rows;
     p.M = (int32_t)d->rows; p.E = d->experts; p.I = io ? d->n_in : d->n_out; p.J = io ? d->n_out : d->n_in;
     p.a_rows = (int32_t)(io ? d->x_rows : d->rows); p.b_rows = (int32_t)(io ? d->rows : d->x_rows);

@@ -113,6 +113,42 @@ template <typename T> struct KnEight {
     }
 };
 
+// What is added to columns j .. j + 7 of a network's results (j a multiple of 8)
+template <typename T> __device__ __forceinline__ void kn_bias_of(const KnProduct &p, bool some, int64_t group, int32_t j, float add[8])
+{
+    const bool any = p.bias && some && j < p.J;
+    typename KnEight<T>::Piece v = {};
+    if (any) v = KnEight<T>::load((const T *)p.bias + group * p.J, j, p.J);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) add[q] = any ? (float)v[q] : 0.0f;
+}
+// The end of 8 neighbouring results of row i: zeros for a row that x does not have, bias, ReLU, the mask of a ReLU before; one rounding
+template <typename T>
+__device__ __forceinline__ void kn_finish(const KnProduct &p, bool some, int32_t i, int32_t j, const float add[8], float y[8])
+{
+    if (p.rows && (uint32_t)p.rows[i] >= (uint32_t)p.a_rows) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) y[q] = 0.0f;
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        y[q] += add[q];
+        if (p.relu) y[q] = y[q] > 0.0f || y[q] != y[q] ? y[q] : 0.0f; // (a NaN stays one)
+    }
+    if (p.mask && some) {
+        const int32_t src = p.mask_rows ? p.mask_rows[i] : i;
+        typename KnEight<T>::Piece m = {};
+        if ((uint32_t)src < (uint32_t)p.m_rows) m = KnEight<T>::load((const T *)p.mask + (int64_t)src * p.ldm, j, p.J);
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (!((float)m[q] > 0.0f)) y[q] = 0.0f;
+    }
+    typename KnEight<T>::Piece o;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) o[q] = (T)y[q];
+    KnEight<T>::store((T *)p.out + (int64_t)i * p.o_i, j, p.J, o);
+}
+
 // What a wavefront brings of each stage of a tile (NW wavefronts in the workgroup).  DIRECT: rows are made of whole 16-byte pieces on
 // multiples of 16 bytes, which go straight from memory to the LDS.  Else pieces that start anywhere and may end inside go through
 // registers: `fetch` puts down the stage that is there and asks for the one after it, so that `ask_first` comes before the first.

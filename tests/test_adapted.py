@@ -1,0 +1,105 @@
+"""A shared layer with low-rank adapters per network, forward and backward, against plain implementations in 64 bits on the CPU.
+
+Bounds.  h and g are rounded to the type T before they are multiplied on, so the reference is taken in two steps: h against its own exact value (one rounding of the
+scaled sum: u_T of it, and (C + 8) 2^-23 of the sum of magnitudes, test_experts.py), and what is made of h against the exact value of the h that was
+returned.  g is not returned: what it enters is bounded by its error's largest effect, u_T |g| + (N + 9) 2^-23 (magnitudes of g) through |A|.
+"""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+import paper_2103_13744_amd as kn
+
+from .test_experts import DT, U, dev, rand, split
+
+
+def make(m, e, k, n, r, dtype, how, gather, nk, seed):
+    dt, off = DT[dtype], split(m, e, how, seed)
+    rows, xr = None, m
+    if gather:
+        xr = max(1, m // 3)
+        rows = torch.randint(0, xr, (m,), generator=torch.Generator().manual_seed(seed + 1), dtype=torch.int32)
+    lay = lambda s, *shape: (rand(s, *shape[:-2], shape[-1], shape[-2]).transpose(-1, -2) if nk else rand(s, *shape)) / math.sqrt(shape[-2])  # noqa: E731
+    return (rand(seed + 2, xr, k).to(dt), lay(seed + 3, k, n).to(dt), lay(seed + 4, e, k, r).to(dt), lay(seed + 5, e, r, n).to(dt), off, rows,
+            0.5 + torch.rand(e, generator=torch.Generator().manual_seed(seed + 6)))
+
+
+def groups(off):
+    return [(g, a, b) for g, (a, b) in enumerate(zip(off[:-1].tolist(), off[1:].tolist())) if b > a]
+
+
+def within(got, want, bound, dtype):
+    assert tuple(got.shape) == tuple(want.shape) and got.dtype == DT[dtype]
+    bad = ~((got.double().cpu() - want).abs() <= U[dtype] * want.abs() + bound + 2.0 ** -24)
+    assert not bad.any(), (int(bad.sum()), float((got.double().cpu() - want).abs()[bad].max()), bad.nonzero()[:4].tolist())
+
+
+def check_forward(x, w, a, b, off, rows, s, bias, relu, y, h, dtype):
+    m, r, (k, n) = y.shape[0], a.shape[2], w.shape
+    xs = (x if rows is None else x[rows.long()]).double()
+    wh, mh = torch.zeros(m, r, dtype=torch.float64), torch.zeros(m, r, dtype=torch.float64)
+    for g, i, j in groups(off):
+        sc = 1.0 if s is None else float(s[g])
+        wh[i:j], mh[i:j] = sc * (xs[i:j] @ a[g].double()), sc * (xs[i:j].abs() @ a[g].double().abs())
+    tail = int(off[-1])
+    assert h.shape[1] % (4 if dtype == "f32" else 8) == 0 and not h[:, r:].any() and not h[tail:].any()
+    within(h[:, :r], wh, (k + 10) * 2.0 ** -23 * mh, dtype)
+    hd = h.double().cpu()[:, :r]
+    want, mag = xs @ w.double(), xs.abs() @ w.double().abs()
+    for g, i, j in groups(off):
+        want[i:j] += hd[i:j] @ b[g].double()
+        mag[i:j] += hd[i:j].abs() @ b[g].double().abs()
+    if bias is not None:
+        want, mag = want + bias.double(), mag + bias.double().abs()
+    within(y, want.clamp(min=0.0) if relu else want, (k + r + 16) * 2.0 ** -23 * mag, dtype)
+
+
+def check_backward(dy, x, w, a, b, off, rows, s, relu, h, got, dtype):
+    dx, da, db = got
+    m, (e, k, r), n = dy.shape[0], a.shape, w.shape[1]
+    xs, d, u = (x if rows is None else x[rows.long()]).double(), dy.double(), U[dtype]
+    wdx, mdx = d @ w.double().T, (n + 8) * 2.0 ** -23 * (d.abs() @ w.double().abs().T)
+    wda, mda, wdb, mdb = (torch.zeros(t, dtype=torch.float64) for t in ((e, k, r), (e, k, r), (e, r, n), (e, r, n)))
+    for q, i, j in groups(off):
+        sc = 1.0 if s is None else float(s[q])
+        g, mg = sc * (d[i:j] @ b[q].double().T), sc * (d[i:j].abs() @ b[q].double().abs().T)
+        off_g = u * g.abs() + (n + 10) * 2.0 ** -23 * mg + 2.0 ** -24  # how far the rounded g may be from g
+        am, xm = a[q].double().abs(), xs[i:j].abs()
+        wdx[i:j] += g @ a[q].double().T
+        mdx[i:j] += off_g @ am.T + (r + 16) * 2.0 ** -23 * (g.abs() @ am.T)
+        wda[q], mda[q] = xs[i:j].T @ g, xm.T @ off_g + (j - i + 8) * 2.0 ** -23 * (xm.T @ g.abs())
+        hd = h.double().cpu()[i:j, :r]
+        wdb[q], mdb[q] = hd.T @ d[i:j], (j - i + 8) * 2.0 ** -23 * (hd.abs().T @ d[i:j].abs())
+    if relu:
+        wdx, mdx = wdx * (xs > 0), mdx * (xs > 0)
+    within(dx, wdx, 1.01 * mdx, dtype)
+    within(da, wda, 1.01 * mda, dtype)
+    within(db, wdb, 1.01 * mdb, dtype)
+    assert da.stride() == dev(a).stride() and db.stride() == dev(b).stride()
+
+
+SIZES = [  # rows, networks, inputs, outputs, rank
+    (1, 1, 1, 1, 1), (1, 3, 64, 64, 4), (2, 70, 128, 136, 8), (5, 2, 2, 3, 2), (16, 8, 256, 64, 16), (17, 3, 33, 65, 5), (33, 33, 64, 72, 8), (48, 20, 512, 264, 16),
+    (64, 1, 64, 64, 64), (65, 2, 63, 32, 4), (100, 100, 96, 40, 24), (129, 5, 91, 64, 7), (200, 65, 32, 33, 1), (257, 3, 72, 200, 80), (300, 130, 64, 3, 2), (500, 4, 320, 520, 16),
+    (1000, 7, 129, 127, 9), (1100, 3, 512, 256, 32), (3000, 4200, 32, 32, 4), (2100, 2, 136, 264, 13), (1300, 3, 40, 72, 130), (5000, 4, 64, 33, 3), (700, 9, 2000, 48, 8),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_adapted(size, dtype):
+    m, e, k, n, r = size
+    for i, (how, gather, nk, bias, relu, scaled) in enumerate([("even", False, False, True, True, True), ("skew", True, True, False, False, True),
+                                                               ("tail", True, False, True, False, False), ("one", False, True, True, True, True)]):
+        x, w, a, b, off, rows, s = make(m, e, k, n, r, dtype, how, gather, nk, 100 * m + i)
+        x, s, bv = x.relu() if relu else x, s if scaled else None, rand(7 + i, n).to(DT[dtype]) if bias else None
+        args = (dev(x), dev(w), dev(a), dev(b), dev(off))
+        y, h = kn.adapted_linear(*args, rows=dev(rows), scales=dev(s), bias=dev(bv), relu=relu, want_h=True)
+        check_forward(x, w, a, b, off, rows, s, bv, relu, y, h, dtype)
+        assert torch.equal(kn.adapted_linear(*args, rows=dev(rows), scales=dev(s), bias=dev(bv), relu=relu), y)
+        dy = rand(9 + i, m, n).to(DT[dtype])
+        got = kn.adapted_linear_backward(dev(dy), dev(x), h, *args[1:], rows=dev(rows), scales=dev(s), relu_in=relu)
+        check_backward(dy, x, w, a, b, off, rows, s, relu, h, got, dtype)
