@@ -435,6 +435,23 @@ int kn_quantize_f8_weights(void *stream, const void *w, int32_t dtype, int32_t w
 int kn_grouped_linear_f8(void *stream, const kn_linear_desc *desc, const void *xq, const float *x_scales, const void *wq,
                          const float *w_scales, const void *bias, const int32_t *offsets, const int32_t *rows, int32_t relu, void *y);
 
+/* Rows kept in 8 bits (e4m3) until a backward pass, a quarter or half of what they take, and the gradients from what was kept.
+ * kn_save_f8: rows x (R, K) -> q (dev, 16-byte aligned, R rows of K bytes rounded up to 16, zeros behind the K-th) and exponents (dev, R * ceil(K/128) bytes): a
+ * block of 128 values of a row stands for q 2^(exponent - 127), with the least power of two from 2^-100 on that brings its largest finite magnitude to 448 or
+ * less, and q the e4m3 nearest to the exact quotient (ties to even), but 2^-9 where x is above zero and q would be zero,
+ * and 240 where the value would pass the largest of x's type.  So q is above zero exactly where x is,
+ * which is what a ReLU's gradient asks; not finite values become NaN, that of +infinity without the sign bit, others with it, and do not touch their block.
+ * kn_restore_f8: the values again, of any dtype (exact in x's own).
+ * kn_grouped_linear_dx_saved, kn_grouped_linear_dw_saved: kn_grouped_linear_dx with the mask, and kn_grouped_linear_dw, of an x that was saved; dy, w and the
+ * results are of desc's dtype, desc's ldx is not looked at.  The values are exact in the products (in fp16: where they were saved from fp16), whose sums and
+ * workspace are kn_grouped_linear_dw's. */
+int kn_save_f8(void *stream, const void *x, int32_t dtype, int64_t R, int32_t K, int64_t ld, void *q, uint8_t *exponents);
+int kn_restore_f8(void *stream, const void *q, const uint8_t *exponents, int64_t R, int32_t K, int32_t dtype, void *x /*dev R*K*/);
+int kn_grouped_linear_dx_saved(void *stream, const kn_linear_desc *desc, const void *dy /*dev M*N*/, const void *w, const void *q, const int32_t *offsets,
+                               const int32_t *rows, void *dx /*dev M*K*/);
+int kn_grouped_linear_dw_saved(void *stream, const kn_linear_desc *desc, const void *q, const uint8_t *exponents, const void *dy, const int32_t *offsets,
+                               const int32_t *rows, void *dw, void *db, void *workspace, int64_t workspace_bytes);
+
 /* The networks' results brought back to their rows: out[t] = sum over j < k of weights[t*k + j] y[slots[t*k + j]] (weights NULL:
  * ones, which is the gradient of reading x through `rows`).  y (dev, M rows of `width`), out (dev, T rows). */
 int kn_combine(void *stream, const void *y, int32_t dtype, int64_t M, int32_t width, const int32_t *slots /*dev T*k*/,

@@ -26,6 +26,7 @@ EXPORTS = ["kn_error_string", "kn_last_hip_error", "kn_params_per_net", "kn_crea
            "kn_route_workspace_bytes", "kn_route", "kn_route_backward", "kn_route_balance_workspace_bytes", "kn_route_balance", "kn_route_balance_backward", "kn_grouped_linear", "kn_grouped_linear_dx", "kn_grouped_linear_dw",
            "kn_grouped_linear_dw_workspace_bytes",
            "kn_adapted_linear_workspace_bytes", "kn_adapted_linear", "kn_adapted_linear_backward_workspace_bytes", "kn_adapted_linear_backward",
+           "kn_save_f8", "kn_restore_f8", "kn_grouped_linear_dx_saved", "kn_grouped_linear_dw_saved",
            "kn_quantize_f8", "kn_quantize_f8_weights", "kn_grouped_linear_f8", "kn_combine", "kn_combine_backward"]
 
 
@@ -122,6 +123,10 @@ def load_library(build_if_missing: bool = True):
     L.kn_adapted_linear.argtypes = [vp, desc, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, i64]
     L.kn_adapted_linear_backward_workspace_bytes.argtypes = [desc, i32, C.POINTER(i64)]
     L.kn_adapted_linear_backward.argtypes = [vp, desc, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, i64]
+    L.kn_save_f8.argtypes = [vp, vp, i32, i64, i32, i64, vp, vp]
+    L.kn_restore_f8.argtypes = [vp, vp, vp, i64, i32, i32, vp]
+    L.kn_grouped_linear_dx_saved.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp]
+    L.kn_grouped_linear_dw_saved.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp, vp, vp, i64]
     L.kn_quantize_f8.argtypes = [vp, vp, i32, i64, i32, i64, vp, vp]
     L.kn_quantize_f8_weights.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp]
     L.kn_grouped_linear_f8.argtypes = [vp, desc, vp, vp, vp, vp, vp, vp, vp, i32, vp]
@@ -721,6 +726,80 @@ def grouped_linear_f8(xq, xs, wq, ws, offsets, rows=None, bias=None, relu=False,
                                   _ptr(offsets, torch.int32, shape=(E + 1,)), None if rows is None else _ptr(rows, torch.int32, shape=(M,)),
                                   1 if relu else 0, _ptr(out, dtype, shape=(M, N))), "kn_grouped_linear_f8")
     return out
+
+
+def save_f8(x):
+    """Rows kept in 8 bits until a backward pass: (R, K) -> (float8_e4m3fn (R, K rounded up to 16), zeros behind the K-th; float8_e8m0fnu (R, ceil(K / 128)), a power of
+    two per block).  q is above zero exactly where x is; what is not finite becomes NaN."""
+    L = load_library()
+    R, K = x.shape
+    ptr, ld = _rows_ptr(x, K)
+    q, e = x.new_empty((R, -(-K // 16) * 16), dtype=torch.float8_e4m3fn), x.new_empty((R, -(-K // 128)), dtype=torch.float8_e8m0fnu)
+    _check(L.kn_save_f8(_stream(), ptr, _dtype_id(x.dtype), R, K, ld, q.data_ptr(), e.data_ptr()), "kn_save_f8")
+    return q, e
+
+
+def _saved_ptrs(q, e, K):
+    """Pointers of what save_f8 gave for rows of K values."""
+    R = q.shape[0]
+    return _ptr(q, torch.float8_e4m3fn, shape=(R, -(-K // 16) * 16)), _ptr(e, torch.float8_e8m0fnu, shape=(R, -(-K // 128)))
+
+
+def restore_f8(q, e, width, dtype):
+    """The rows that ``save_f8`` kept, (R, width) of ``dtype``: exact where that is the type that they were saved from."""
+    L = load_library()
+    pq, pe = _saved_ptrs(q, e, int(width))
+    out = q.new_empty((q.shape[0], int(width)), dtype=dtype)
+    _check(L.kn_restore_f8(_stream(), pq, pe, q.shape[0], int(width), _dtype_id(dtype), out.data_ptr()), "kn_restore_f8")
+    return out
+
+
+def _saved_desc(q, e, w, rows):
+    """(desc, M, pointers of q, e, w, rows): x as save_f8 left it, w (E, n_in, n_out), rows (M,) int32 or None."""
+    E, n_in, n_out = w.shape
+    pq, pe = _saved_ptrs(q, e, n_in)
+    M = q.shape[0] if rows is None else rows.shape[0]
+    pr = None if rows is None else _ptr(rows, torch.int32, shape=(M,))
+    return LinearDesc(_dtype_id(w.dtype), _weights_layout(w), E, n_in, n_out, M, q.shape[0], n_in), M, pq, pe, w.data_ptr(), pr
+
+
+def grouped_linear_dx_saved(dy, q, e, w, offsets, rows=None):
+    """``grouped_linear_dx`` with ``relu_in``, of an x that ``save_f8`` kept: the mask is exact."""
+    L = load_library()
+    d, M, pq, _, pw, pr = _saved_desc(q, e, w, rows)
+    dx = dy.new_empty((M, d.n_in))  # (rows that are not there have no address: any other will do)
+    _check(L.kn_grouped_linear_dx_saved(_stream(), C.byref(d), _ptr(dy, w.dtype, shape=(M, d.n_out)), pw, pq or 256, _ptr(offsets, torch.int32, shape=(d.experts + 1,)),
+                                        pr, dx.data_ptr()), "kn_grouped_linear_dx_saved")
+    return dx
+
+
+def grouped_linear_dw_saved(dy, q, e, w, offsets, rows=None, want_bias=True):
+    """``grouped_linear_dw`` of an x that ``save_f8`` kept: w gives the gradient's shape, type and layout."""
+    L = load_library()
+    d, M, pq, pe, _, pr = _saved_desc(q, e, w, rows)
+    dw = torch.empty_like(w)  # (keeps the layout of dense weights)
+    db = dy.new_empty((d.experts, d.n_out)) if want_bias else None
+    need, ws = C.c_int64(), None
+    if M > 128:  # (fewer rows need no workspace)
+        _check(L.kn_grouped_linear_dw_workspace_bytes(C.byref(d), C.byref(need)), "kn_grouped_linear_dw_workspace_bytes")
+        ws = torch.empty(need.value, dtype=torch.uint8, device=dy.device) if need.value else None
+    _check(L.kn_grouped_linear_dw_saved(_stream(), C.byref(d), pq, pe, _ptr(dy, w.dtype, shape=(M, d.n_out)), _ptr(offsets, torch.int32, shape=(d.experts + 1,)),
+                                        pr, dw.data_ptr(), None if db is None else db.data_ptr(), None if ws is None else ws.data_ptr(), need.value),
+           "kn_grouped_linear_dw_saved")
+    return dw, db
+
+
+def grouped_linear_backward_saved(dy, q, e, w, offsets, rows=None, relu_in=False, want_bias=True):
+    """(dx, dw, db) of ``grouped_linear`` as ``grouped_linear_backward`` gives them, from the x that ``save_f8`` kept."""
+    if relu_in:
+        dx = grouped_linear_dx_saved(dy, q, e, w, offsets, rows)
+    else:
+        L = load_library()
+        d, M, _, _, pw, _ = _saved_desc(q, e, w, rows)
+        dx = dy.new_empty((M, d.n_in))
+        _check(L.kn_grouped_linear_dx(_stream(), C.byref(d), _ptr(dy, w.dtype, shape=(M, d.n_out)), pw, None, _ptr(offsets, torch.int32, shape=(d.experts + 1,)), None,
+                                      dx.data_ptr()), "kn_grouped_linear_dx")
+    return (dx, *grouped_linear_dw_saved(dy, q, e, w, offsets, rows, want_bias))
 
 
 def combine(y, slots, weights=None):

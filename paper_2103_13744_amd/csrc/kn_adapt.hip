@@ -488,6 +488,6 @@ extern "C" int kn_adapted_linear_backward(void *stream, const kn_linear_desc *d,
         KN_TRY(run((hipStream_t)stream, d->dtype, !io, down, p, beside));
     }
     const kn_linear_desc la = layer_of(d, d->n_in, rank, d->x_rows, d->ldx), lb = layer_of(d, rank, d->n_out, d->rows, rp);
-    KN_TRY(kn_linear_dw_run(stream, &la, x, g, rp, offsets, rows, da, nullptr, sums, dw));
-    return kn_linear_dw_run(stream, &lb, h, dy, N, offsets, nullptr, db, nullptr, sums, dw);
+    KN_TRY(kn_linear_dw_run(stream, &la, x, nullptr, g, rp, offsets, rows, da, nullptr, sums, dw));
+    return kn_linear_dw_run(stream, &lb, h, nullptr, dy, N, offsets, nullptr, db, nullptr, sums, dw);
 }

@@ -116,6 +116,7 @@ __device__ __forceinline__ kn_f32x4 kn_mfma(kn_f32x4 a, kn_f32x4 b, kn_f32x4 c)
 struct KnProduct {
     const void *a, *b, *bias, *mask; // mask: out(i, j) becomes 0 where mask(row i, j) <= 0 (a ReLU's result)
     void *out, *out_bias;            // out_bias (weight gradient): sum over the rows r of b(r, j)
+    const int8_t *mask_saved;        // the same mask from what kn_save_f8 left: a positive byte is a positive value (rows of ldm bytes)
     const int32_t *offsets, *rows, *b_index, *mask_rows; // rows: of a, b_index: of b, mask_rows: of the mask; nullable
     int64_t lda, ldb, ldm;           // row strides in elements: a, b (weight gradient), mask
     int64_t b_group, b_c, b_j;       // strides of b_e: network, contraction, column
@@ -126,8 +127,12 @@ struct KnProduct {
     int32_t first;                   // number of the launch's first workgroup
 };
 
-// kn_grouped_linear_dw, with rows of dy that may lie apart
-int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const void *dy, int64_t lddy, const int32_t *offsets, const int32_t *rows,
+// What kn_save_f8 leaves of K values of a row
+constexpr int KN_SAVED_BLOCK = 128;
+static inline int64_t kn_saved_bytes(int64_t K) { return kn_align_up(K, 16); }
+
+// kn_grouped_linear_dw, with rows of dy that may lie apart; exponents: x is what kn_save_f8 left
+int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const uint8_t *exponents, const void *dy, int64_t lddy, const int32_t *offsets, const int32_t *rows,
                      void *dw, void *db, void *workspace, int64_t workspace_bytes);
 
 // What the grouped products check alike
@@ -139,5 +144,13 @@ static inline int kn_linear_check(const kn_linear_desc *d)
     if (d->rows > KN_MAX_ROWS || d->x_rows > KN_MAX_ROWS || d->experts > KN_MAX_EXPERTS || d->n_in > KN_MAX_WIDTH || d->n_out > KN_MAX_WIDTH)
         return KN_E_UNSUPPORTED;
     return KN_OK;
+}
+// ldx is not looked at where x is what kn_save_f8 left
+static inline int kn_saved_check(const kn_linear_desc *d)
+{
+    if (!d) return KN_E_INVALID_ARG;
+    kn_linear_desc whole = *d;
+    whole.ldx = d->n_in;
+    return kn_linear_check(&whole);
 }
 

@@ -343,6 +343,23 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
     Run add[RUNS], m[SUBS][RUNS]; // (a lane's columns are j0 + 4 W n + W g .. + W - 1)
 #pragma unroll
     for (int n = 0; n < RUNS; ++n) add[n] = some && bias ? run(bias + group * p.J, min(j0 + 4 * W * n + W * g, p.J - 1)) : Run{};
+    if (some && p.mask_saved) { // (a lane's W columns lie in a saved row's whole 16 bytes)
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) {
+            const int32_t i = min(piece.begin + 16 * s + col, piece.end - 1), src = p.mask_rows ? p.mask_rows[i] : i;
+            const bool in = (uint32_t)src < (uint32_t)p.m_rows;
+#pragma unroll
+            for (int n = 0; n < RUNS; ++n) {
+                typedef int8_t Bytes __attribute__((ext_vector_type(W)));
+                const int32_t j = j0 + 4 * W * n + W * g;
+                Bytes b = {};
+                if (in && j < p.J) b = *(const Bytes *)(p.mask_saved + (int64_t)src * p.ldm + j);
+#pragma unroll
+                for (int r = 0; r < W; ++r) m[s][n][r] = (T)(b[r] > 0 ? 1.0f : 0.0f);
+            }
+        }
+    }
+    const bool masked = some && (mask || p.mask_saved);
     if (some && mask) { // (asked for before the first result is stored, not one after the other's)
 #pragma unroll
         for (int s = 0; s < SUBS; ++s) {
@@ -381,7 +398,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
                 float y = acc[n * PAIR + r / 4][r % 4];
                 if (some && bias) y += (float)add[n][r];
                 if (p.relu) y = y > 0.0f || y != y ? y : 0.0f; // (a NaN stays one)
-                if (some && mask && !((float)m[s][n][r] > 0.0f)) y = 0.0f;
+                if (masked && !((float)m[s][n][r] > 0.0f)) y = 0.0f;
                 o[r] = (T)y;
             }
             if (together) {
@@ -577,21 +594,38 @@ extern "C" int kn_grouped_linear(void *stream, const kn_linear_desc *d, const vo
     return kn_with_type(d->dtype, [&](auto v) { return launch_forward<decltype(v)>((hipStream_t)stream, p); });
 }
 
-extern "C" int kn_grouped_linear_dx(void *stream, const kn_linear_desc *d, const void *dy, const void *w, const void *x_relu,
-                                    const int32_t *offsets, const int32_t *rows, void *dx)
+namespace {
+// The gradient of a layer's inputs; x_relu or saved: the mask of a ReLU before it
+int linear_dx(void *stream, const kn_linear_desc *d, const void *dy, const void *w, const void *x_relu, const void *saved, const int32_t *offsets,
+              const int32_t *rows, void *dx)
 {
-    KN_TRY(kn_linear_check(d));
-    if (d->rows == 0) return KN_OK;
-    if (!dy || !w || !offsets || !dx || (x_relu && !rows && d->x_rows < d->rows)) return KN_E_INVALID_ARG;
+    const bool masked = x_relu || saved;
+    if (!dy || !w || !offsets || !dx || (masked && !rows && d->x_rows < d->rows)) return KN_E_INVALID_ARG;
     KnProduct p = {};
     const bool io = d->w_layout == KN_W_IN_OUT;
-    p.a = dy; p.b = w; p.mask = x_relu; p.out = dx; p.offsets = offsets; p.rows = nullptr;
-    p.lda = d->n_out; p.ldm = d->ldx;
+    p.a = dy; p.b = w; p.mask = x_relu; p.mask_saved = (const int8_t *)saved; p.out = dx; p.offsets = offsets; p.rows = nullptr;
+    p.lda = d->n_out; p.ldm = saved ? kn_saved_bytes(d->n_in) : d->ldx;
     p.b_group = (int64_t)d->n_in * d->n_out; p.b_c = io ? 1 : d->n_in; p.b_j = io ? d->n_out : 1;
     p.o_i = d->n_in;
     p.M = (int32_t)d->rows; p.E = d->experts; p.J = d->n_in; p.C = d->n_out;
     p.a_rows = p.M; p.m_rows = (int32_t)d->x_rows;
-    p.mask_rows = x_relu ? rows : nullptr;
+    p.mask_rows = masked ? rows : nullptr;
     return kn_with_type(d->dtype, [&](auto v) { return launch_forward<decltype(v)>((hipStream_t)stream, p); });
 }
+} // namespace
 
+extern "C" int kn_grouped_linear_dx(void *stream, const kn_linear_desc *d, const void *dy, const void *w, const void *x_relu,
+                                    const int32_t *offsets, const int32_t *rows, void *dx)
+{
+    KN_TRY(kn_linear_check(d));
+    return d->rows == 0 ? KN_OK : linear_dx(stream, d, dy, w, x_relu, nullptr, offsets, rows, dx);
+}
+
+extern "C" int kn_grouped_linear_dx_saved(void *stream, const kn_linear_desc *d, const void *dy, const void *w, const void *q, const int32_t *offsets,
+                                          const int32_t *rows, void *dx)
+{
+    KN_TRY(kn_saved_check(d));
+    if (d->rows == 0) return KN_OK;
+    if (!q || ((uintptr_t)q & 15)) return KN_E_INVALID_ARG;
+    return linear_dx(stream, d, dy, w, nullptr, q, offsets, rows, dx);
+}

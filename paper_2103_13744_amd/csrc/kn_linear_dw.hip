@@ -20,9 +20,11 @@ __host__ __device__ inline int64_t part_places(int64_t M, int64_t len) { return 
 // lane, so that fragments cost twice the reads of the forward product's, and the LDS bounds it (128 x 128 by four wavefronts of 64 x
 // 64: 230 against 219 on even networks; 256 x 128: 230; 128 x 256: 246).  64 x 64 tiles: 524,291 rows, 4,096 networks 64 x 64 in fp16: 34
 // us, 4.9 TB/s (47 with 128 x 128).
+// SAVED: a, or b, is what kn_save_f8 left of x (its exponents beside it), and goes through registers.
 enum { SUM_NONE, SUM_A, SUM_B };
-template <typename T, bool DIRECT, int BM, int BN, int WR, int WC>
-__global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, int32_t sum, Parts parts)
+enum { SAVED_NONE, SAVED_A, SAVED_B };
+template <typename T, bool DIRECT, int BM, int BN, int WR, int WC, int SAVED = SAVED_NONE>
+__global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, int32_t sum, Parts parts, const uint8_t *exponents)
 {
     constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16, CS = 128 / sizeof(T);
     typedef typename KnFrag<T>::Type Frag;
@@ -43,8 +45,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
     const int j0 = number % jtiles * BN, i0 = number / jtiles * BM;
     const int32_t steps = (cend - c0 + CS - 1) / CS;
     const bool sum_a = sum == SUM_A && j0 == 0, sum_b = sum == SUM_B && i0 == 0;
-    KnGroupLoader<T, BM, NW, DIRECT> la;
-    KnGroupLoader<T, BN, NW, DIRECT> lb;
+    typename std::conditional<SAVED == SAVED_A, KnSavedLoader<T, BM, NW>, KnGroupLoader<T, BM, NW, DIRECT>>::type la;
+    typename std::conditional<SAVED == SAVED_B, KnSavedLoader<T, BN, NW>, KnGroupLoader<T, BN, NW, DIRECT>>::type lb;
     const int wi = (wave / WC) * (BM / WR), wj = (wave % WC) * (BN / WC);
     kn_f32x4 acc[U][V] = {}, side[U > V ? U : V] = {};
     Frag ones;
@@ -80,8 +82,10 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_reduce(KnProduct p, in
         }
     };
     if (steps > 0) {
-        la.start(wave, lane, (const T *)p.a + i0, p.lda, p.I - i0, p.rows, p.a_rows, c0, cend);
-        lb.start(wave, lane, (const T *)p.b + j0, p.ldb, p.J - j0, p.b_index, p.b_rows, c0, cend);
+        if constexpr (SAVED == SAVED_A) la.start(wave, lane, (const uint8_t *)p.a, exponents, i0, p.I, p.rows, p.a_rows, c0, cend);
+        else la.start(wave, lane, (const T *)p.a + i0, p.lda, p.I - i0, p.rows, p.a_rows, c0, cend);
+        if constexpr (SAVED == SAVED_B) lb.start(wave, lane, (const uint8_t *)p.b, exponents, j0, p.J, p.b_index, p.b_rows, c0, cend);
+        else lb.start(wave, lane, (const T *)p.b + j0, p.ldb, p.J - j0, p.b_index, p.b_rows, c0, cend);
         fetch(0);
         if (!DIRECT && steps > 1) fetch(1);
         kn_stage_barrier();
@@ -334,9 +338,10 @@ int32_t part_length(const kn_linear_desc *d)
     return (int32_t)kn_align_up(len < least ? least : len, 64);
 }
 
-template <typename T, bool DIRECT> int launch_reduce(hipStream_t st, const kn_linear_desc *d, const KnProduct &p, int32_t sum, const Parts &parts)
+template <typename T, bool DIRECT, int SAVED>
+int launch_reduce(hipStream_t st, const kn_linear_desc *d, const KnProduct &p, int32_t sum, const Parts &parts, const uint8_t *exponents)
 {
-    const Way way = way_of(d, DIRECT);
+    const Way way = way_of(d, DIRECT || SAVED != SAVED_NONE);
     const int bm = way == WAY_128 ? 128 : way == WAY_32 || (way == WAY_SMALL && p.I <= 32) ? 32 : 64;
     const int bn = way == WAY_128 ? 128 : way == WAY_32 ? 32 : way == WAY_64 || p.J > 48 ? 64 : p.J > 32 ? 48 : p.J > 16 ? 32 : 16;
     const int64_t blocks = kn_pieces(p.M, p.E, parts.len) * kn_div_up(p.I, bm) * kn_div_up(p.J, bn);
@@ -346,11 +351,11 @@ template <typename T, bool DIRECT> int launch_reduce(hipStream_t st, const kn_li
         KnProduct q = p;
         q.first = first;
         if (way == WAY_128) {
-            if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 128, 128, 2, 4>), grid, dim3(512), 0, st, q, sum, parts);
-        } else if (way == WAY_64) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 64, 64, 2, 2>), grid, dim3(256), 0, st, q, sum, parts);
+            if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 128, 128, 2, 4, SAVED>), grid, dim3(512), 0, st, q, sum, parts, exponents);
+        } else if (way == WAY_64) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 64, 64, 2, 2, SAVED>), grid, dim3(256), 0, st, q, sum, parts, exponents);
         else if (way == WAY_32) {
-            if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 32, 32, 2, 2>), grid, dim3(256), 0, st, q, sum, parts);
-        } else if constexpr (!DIRECT) {
+            if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((k_product_reduce<T, DIRECT, 32, 32, 2, 2, SAVED>), grid, dim3(256), 0, st, q, sum, parts, exponents);
+        } else if constexpr (!DIRECT && SAVED == SAVED_NONE) {
 #define KN_SMALL(U, V)                                                                                                                      \
     if (alone) hipLaunchKernelGGL((k_reduce_small<T, U, V, 1>), grid, dim3(64), 0, st, q, sum, parts);                                      \
     else hipLaunchKernelGGL((k_reduce_small<T, U, V, 4>), grid, dim3(256), 0, st, q, sum, parts)
@@ -397,13 +402,24 @@ extern "C" int kn_grouped_linear_dw_workspace_bytes(const kn_linear_desc *d, int
 extern "C" int kn_grouped_linear_dw(void *stream, const kn_linear_desc *d, const void *x, const void *dy, const int32_t *offsets,
                                     const int32_t *rows, void *dw, void *db, void *workspace, int64_t workspace_bytes)
 {
-    return kn_linear_dw_run(stream, d, x, dy, d ? d->n_out : 0, offsets, rows, dw, db, workspace, workspace_bytes);
+    KN_TRY(kn_linear_check(d));
+    return kn_linear_dw_run(stream, d, x, nullptr, dy, d->n_out, offsets, rows, dw, db, workspace, workspace_bytes);
 }
 
-int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const void *dy, int64_t lddy, const int32_t *offsets, const int32_t *rows,
-                     void *dw, void *db, void *workspace, int64_t workspace_bytes)
+extern "C" int kn_grouped_linear_dw_saved(void *stream, const kn_linear_desc *d, const void *q, const uint8_t *exponents, const void *dy, const int32_t *offsets,
+                                          const int32_t *rows, void *dw, void *db, void *workspace, int64_t workspace_bytes)
 {
-    KN_TRY(kn_linear_check(d));
+    KN_TRY(kn_saved_check(d));
+    if (((uintptr_t)q & 15) || (d->rows > 0 && d->x_rows > 0 && !exponents)) return KN_E_INVALID_ARG;
+    kn_linear_desc whole = *d;
+    whole.ldx = d->n_in;
+    static const uint8_t none = 0; // (no row is read: any address but NULL)
+    return kn_linear_dw_run(stream, &whole, q, exponents ? exponents : &none, dy, d->n_out, offsets, rows, dw, db, workspace, workspace_bytes);
+}
+
+int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const uint8_t *exponents, const void *dy, int64_t lddy, const int32_t *offsets,
+                     const int32_t *rows, void *dw, void *db, void *workspace, int64_t workspace_bytes)
+{
     if (!offsets || !dw || (d->rows > 0 && (!dy || (d->x_rows > 0 && !x))) || (d->rows > 0 && !rows && d->x_rows < d->rows)) return KN_E_INVALID_ARG;
     int64_t need = 0;
     KN_TRY(kn_grouped_linear_dw_workspace_bytes(d, &need));
@@ -423,7 +439,13 @@ int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const
     return kn_with_type(d->dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
         constexpr int64_t V = 16 / sizeof(E_);
+        hipStream_t st = (hipStream_t)stream;
+        if (exponents) {
+            const bool direct = d->n_out % V == 0 && ((uintptr_t)dy & 15) == 0 && lddy % V == 0;
+            if (io) return direct ? launch_reduce<E_, true, SAVED_A>(st, d, p, sum, parts, exponents) : launch_reduce<E_, false, SAVED_A>(st, d, p, sum, parts, exponents);
+            return direct ? launch_reduce<E_, true, SAVED_B>(st, d, p, sum, parts, exponents) : launch_reduce<E_, false, SAVED_B>(st, d, p, sum, parts, exponents);
+        }
         const bool direct = p.I % V == 0 && p.J % V == 0 && (((uintptr_t)p.a | (uintptr_t)p.b) & 15) == 0 && p.lda % V == 0 && p.ldb % V == 0;
-        return direct ? launch_reduce<E_, true>((hipStream_t)stream, d, p, sum, parts) : launch_reduce<E_, false>((hipStream_t)stream, d, p, sum, parts);
+        return direct ? launch_reduce<E_, true, SAVED_NONE>(st, d, p, sum, parts, nullptr) : launch_reduce<E_, false, SAVED_NONE>(st, d, p, sum, parts, nullptr);
     });
 }

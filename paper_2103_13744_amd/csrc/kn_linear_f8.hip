@@ -1,5 +1,5 @@
 // Products grouped by network in 8-bit floating point (e4m3) with fp32 scales: kn_quantize_f8 (a scale per row and 128 inputs),
-// kn_quantize_f8_weights (a scale per 128 x 128), kn_grouped_linear_f8.
+// kn_quantize_f8_weights (a scale per 128 x 128), kn_grouped_linear_f8; and rows kept in 8 bits for a backward pass: kn_save_f8, kn_restore_f8.
 #include "kn_tile.h"
 
 namespace {
@@ -44,6 +44,91 @@ __global__ void __launch_bounds__(256) k_quantize_rows(const T *__restrict__ x, 
     out.y = f8_pack(v[4], v[5], v[6], v[7], s);
     *(uint2 *)(q + row * kb * F8_BLOCK + k0) = out;
     if (at == 0) scales[g] = s;
+}
+
+// The power of two of a block of saved values: the least n >= -100 with amax <= 448 2^n (448 = 1.75 2^8), so that a value's quotient is exact and its 8 bits
+// are rounded once; the value that they stand for is exact in the 16-bit types.
+constexpr int SAVED_LEAST = -100;
+// Of the largest values of a type some would round to a power of two that it does not have (65504 to 2^16): they are kept as 240 2^n instead.
+template <typename T> constexpr int saved_most() { return std::is_same<T, _Float16>::value ? 8 : 120; }
+__device__ __forceinline__ int saved_exponent(float amax)
+{
+    const int b = __float_as_int(amax);
+    return max((b >> 23) - 127 - 8 + ((b & 0x7fffff) > 0x600000 ? 1 : 0), SAVED_LEAST);
+}
+// 16 lanes per row and block of 128 values, as above.  A value above zero keeps its sign: what would round to zero becomes the smallest
+// value, 2^-9.  What is not finite has no part in the scale: +infinity becomes the NaN without, NaN and -infinity the one with the sign bit.
+template <typename T>
+__global__ void __launch_bounds__(256) k_save_rows(const T *__restrict__ x, int64_t R, int32_t K, int64_t ld, int32_t kb, uint8_t *__restrict__ q,
+                                                   uint8_t *__restrict__ exponents, int32_t first)
+{
+    const int64_t g = (((int64_t)first + kn_block()) * 256 + kn_thread()) >> 4;
+    if (g >= R * kb) return;
+    const int at = kn_thread() & 15;
+    const int64_t row = g / kb;
+    const int32_t blk = (int32_t)(g % kb), k0 = blk * KN_SAVED_BLOCK + at * 8, bytes = (K + 15) & ~15;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; i += 16 / (int)sizeof(T)) {
+        const typename KnFrag<T>::Type p = kn_any_piece(x + row * ld, k0 + i, K);
+#pragma unroll
+        for (int j = 0; j < 16 / (int)sizeof(T); ++j) v[i + j] = (float)p[j];
+    }
+    float amax = 0.0f;
+    bool finite = true;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float m = fabsf(v[i]);
+        const bool good = m < INFINITY;
+        finite &= good;
+        amax = good ? fmaxf(amax, m) : amax;
+    }
+    const int n = saved_exponent(kn_row_max(amax));
+    const float inverse = __int_as_float((127 - n) << 23);
+    const float cap = n == saved_most<T>() ? 240.0f : 448.0f;
+    float t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        t[i] = fminf(fmaxf(v[i] * inverse, -cap), cap); // (what is not finite is looked at below)
+        t[i] = v[i] > 0.0f ? fmaxf(t[i], 0x1p-9f) : t[i];
+    }
+    uint32_t out[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int w = __builtin_amdgcn_cvt_pk_fp8_f32(t[4 * h], t[4 * h + 1], 0, false);
+        out[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[4 * h + 2], t[4 * h + 3], w, true);
+    }
+    if (!finite) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (!(fabsf(v[i]) < INFINITY)) {
+                const int shift = 8 * (i & 3);
+                out[i / 4] = (out[i / 4] & ~(0xffu << shift)) | (v[i] > 0.0f ? 0x7fu : 0xffu) << shift;
+            }
+    }
+    if (k0 < bytes) *(uint2 *)(q + row * bytes + k0) = make_uint2(out[0], out[1]);
+    if (at == 0) exponents[g] = (uint8_t)(n + 127);
+}
+
+// The values that saved rows stand for: a thread per 8 of them
+template <typename T>
+__global__ void __launch_bounds__(256) k_restore_rows(const uint8_t *__restrict__ q, const uint8_t *__restrict__ exponents, int64_t R, int32_t K, int32_t kb,
+                                                      T *__restrict__ x, int32_t first)
+{
+    const int32_t eights = (K + 7) / 8, bytes = (K + 15) & ~15;
+    const int64_t at = ((int64_t)first + kn_block()) * 256 + kn_thread();
+    if (at >= R * eights) return;
+    const int64_t row = at / eights;
+    const int32_t k = (int32_t)(at % eights) * 8;
+    const uint2 v = *(const uint2 *)(q + row * bytes + k);
+    const float power = kn_power(exponents[row * kb + k / KN_SAVED_BLOCK]);
+    T wide[8];
+    kn_widen_saved<T>(v.x, power, wide);
+    kn_widen_saved<T>(v.y, power, wide + 4);
+    typename KnEight<T>::Piece o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = wide[i];
+    KnEight<T>::store(x + row * K, k, K, o);
 }
 
 // One workgroup per 128 x 128 block of a network's weights, through the LDS (the two layouts differ in which index is next to
@@ -274,6 +359,34 @@ extern "C" int kn_quantize_f8(void *stream, const void *x, int32_t dtype, int64_
         typedef decltype(v) E_;
         return kn_launch(blocks, 256, [&](dim3 grid, int32_t first) {
             hipLaunchKernelGGL((k_quantize_rows<E_>), grid, dim3(256), 0, (hipStream_t)stream, (const E_ *)x, R, K, ld, kb, (uint8_t *)q, scales, first);
+        });
+    });
+}
+
+extern "C" int kn_save_f8(void *stream, const void *x, int32_t dtype, int64_t R, int32_t K, int64_t ld, void *q, uint8_t *exponents)
+{
+    if (R < 0 || K < 1 || ld < K || !kn_dtype_ok(dtype) || (R > 0 && (!x || !q || !exponents)) || ((uintptr_t)q & 15)) return KN_E_INVALID_ARG;
+    if (R > KN_MAX_ROWS || K > KN_MAX_WIDTH) return KN_E_UNSUPPORTED;
+    if (R == 0) return KN_OK;
+    const int32_t kb = (int32_t)kn_div_up(K, KN_SAVED_BLOCK);
+    return kn_with_type(dtype, [&](auto v) -> int {
+        typedef decltype(v) E_;
+        return kn_launch(kn_div_up(R * kb, 16), 256, [&](dim3 grid, int32_t first) {
+            hipLaunchKernelGGL((k_save_rows<E_>), grid, dim3(256), 0, (hipStream_t)stream, (const E_ *)x, R, K, ld, kb, (uint8_t *)q, exponents, first);
+        });
+    });
+}
+
+extern "C" int kn_restore_f8(void *stream, const void *q, const uint8_t *exponents, int64_t R, int32_t K, int32_t dtype, void *x)
+{
+    if (R < 0 || K < 1 || !kn_dtype_ok(dtype) || (R > 0 && (!x || !q || !exponents)) || ((uintptr_t)q & 15)) return KN_E_INVALID_ARG;
+    if (R > KN_MAX_ROWS || K > KN_MAX_WIDTH) return KN_E_UNSUPPORTED;
+    if (R == 0) return KN_OK;
+    const int32_t kb = (int32_t)kn_div_up(K, KN_SAVED_BLOCK);
+    return kn_with_type(dtype, [&](auto v) -> int {
+        typedef decltype(v) E_;
+        return kn_launch(kn_div_up(R * kn_div_up(K, 8), 256), 256, [&](dim3 grid, int32_t first) {
+            hipLaunchKernelGGL((k_restore_rows<E_>), grid, dim3(256), 0, (hipStream_t)stream, (const uint8_t *)q, exponents, R, K, kb, (E_ *)x, first);
         });
     });
 }

@@ -10,6 +10,8 @@
 
 #include "kn_experts.h"
 
+#include <type_traits>
+
 #define KN_LDS __attribute__((address_space(3)))
 #define KN_GLOBAL __attribute__((address_space(1)))
 
@@ -142,6 +144,15 @@ __device__ __forceinline__ void kn_finish(const KnProduct &p, bool some, int32_t
 #pragma unroll
         for (int q = 0; q < 8; ++q)
             if (!((float)m[q] > 0.0f)) y[q] = 0.0f;
+    }
+    if (p.mask_saved && some) { // (j is a multiple of eight, and saved rows are of whole 16 bytes)
+        typedef int8_t Eight __attribute__((ext_vector_type(8)));
+        const int32_t src = p.mask_rows ? p.mask_rows[i] : i;
+        Eight m = {};
+        if ((uint32_t)src < (uint32_t)p.m_rows) m = *(const Eight *)(p.mask_saved + (int64_t)src * p.ldm + j);
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (m[q] <= 0) y[q] = 0.0f;
     }
     typename KnEight<T>::Piece o;
 #pragma unroll
@@ -305,6 +316,90 @@ template <typename T, int W, int NW, bool DIRECT> struct KnGroupLoader {
             for (int t = 0; t < N; ++t) *(KN_LDS typename KnFrag<T>::Type *)(tile + (wave * N + t) * 1024 + lane * 16) = held[t];
             if (c0 + CS <= last) ask(wave, lane, c0 + CS);
         }
+    }
+};
+
+// Four values of 8 bits times a power of two, in T: exact in bf16 and fp32, and in fp16 where the values came from there
+template <typename T> __device__ __forceinline__ void kn_widen_saved(uint32_t v, float power, T to[4])
+{
+    if constexpr (std::is_same<T, __bf16>::value) {
+        const auto a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, power, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, power, true);
+        to[0] = a[0]; to[1] = a[1]; to[2] = b[0]; to[3] = b[1];
+    } else if constexpr (std::is_same<T, _Float16>::value) {
+        const auto a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, power, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, power, true);
+        to[0] = a[0]; to[1] = a[1]; to[2] = b[0]; to[3] = b[1];
+    } else {
+        const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v, power, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v, power, true);
+        to[0] = a[0]; to[1] = a[1]; to[2] = b[0]; to[3] = b[1];
+    }
+}
+__device__ __forceinline__ float kn_power(uint8_t exponent) { return __int_as_float((int)exponent << 23); }
+
+// KnGroupLoader for rows that kn_save_f8 left, widened on their way through the registers.  Values and exponents of a stage are asked for a stage before they
+// are put down, the numbers of its rows two.
+template <typename T, int W, int NW> struct KnSavedLoader {
+    static constexpr int CS = 128 / sizeof(T), PW = 16 / sizeof(T), PR = W / PW, RP = 64 / PR, N = CS / RP / NW;
+    int32_t next[N];
+    uint32_t held[N][PW / 4];
+    uint8_t power[N];
+    const uint8_t *base, *exponents;
+    const int32_t *index;
+    int64_t stride;
+    int32_t rows, last, columns, blocks;
+    __device__ __forceinline__ int row(int wave, int lane, int t) const { return (wave * N + t) * RP + lane / PR; }
+    __device__ __forceinline__ int first_column(int wave, int lane, int t) const { return ((lane % PR) ^ kn_col_swizzle<T, W>(row(wave, lane, t))) * PW; }
+    __device__ __forceinline__ void ask_rows(int wave, int lane, int32_t c0)
+    {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const int32_t c = min(c0 + row(wave, lane, t), last);
+            next[t] = index ? index[c] : c;
+        }
+    }
+    // first: column of the tile's first value, of `width` in a row
+    __device__ __forceinline__ void start(int wave, int lane, const uint8_t *q, const uint8_t *exps, int32_t first, int32_t width, const int32_t *idx, int32_t n_rows,
+                                          int32_t c0, int32_t cend)
+    {
+        stride = (width + 15) & ~15;
+        blocks = (width + KN_SAVED_BLOCK - 1) / KN_SAVED_BLOCK;
+        base = q + first;
+        exponents = exps + first / KN_SAVED_BLOCK; // (a tile is no wider than a block, and lies in one)
+        columns = (int32_t)stride - first;
+        index = idx;
+        rows = n_rows;
+        last = cend - 1;
+        ask_rows(wave, lane, c0);
+        ask(wave, lane, c0);
+    }
+    __device__ __forceinline__ void ask(int wave, int lane, int32_t c0)
+    {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const int k = first_column(wave, lane, t);
+            const bool there = c0 + row(wave, lane, t) <= last && (uint32_t)next[t] < (uint32_t)rows && k < columns;
+#pragma unroll
+            for (int q = 0; q < PW / 4; ++q) held[t][q] = 0;
+            power[t] = 0;
+            if (there) {
+                const uint32_t *v = (const uint32_t *)(base + next[t] * stride + k);
+#pragma unroll
+                for (int q = 0; q < PW / 4; ++q) held[t][q] = v[q];
+                power[t] = exponents[(int64_t)next[t] * blocks];
+            }
+        }
+        ask_rows(wave, lane, c0 + CS);
+    }
+    // the stage whose first row is c0
+    __device__ __forceinline__ void fetch(KN_LDS char *tile, int wave, int lane, int32_t c0)
+    {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            union { T v[PW]; typename KnFrag<T>::Type f; } wide;
+#pragma unroll
+            for (int q = 0; q < PW / 4; ++q) kn_widen_saved<T>(held[t][q], kn_power(power[t]), wide.v + 4 * q);
+            *(KN_LDS typename KnFrag<T>::Type *)(tile + (wave * N + t) * 1024 + lane * 16) = wide.f;
+        }
+        if (c0 + CS <= last) ask(wave, lane, c0 + CS);
     }
 };
 
