@@ -100,7 +100,7 @@ template <typename T, int R, int NW, bool DIRECT> struct LoadH {
     int32_t first[N]; // column of the row's first value (negative: none)
     typename KnFrag<T>::Type held[DIRECT ? 1 : N];
     int32_t piece, rp;
-    __device__ __forceinline__ void start(int wave, int lane, const T *h, int32_t width, int32_t begin, int32_t end, const int32_t *slots)
+    __device__ __forceinline__ void start(int wave, int lane, const T *h, int32_t width, int32_t begin, int32_t end, const KN_LDS int32_t *slots)
     {
         piece = (lane & 7) ^ (lane >> 3);
         rp = width;
@@ -140,17 +140,18 @@ template <typename T, int R, int NW, bool DIRECT> struct LoadH {
     }
 };
 // A stage of the networks' B one under the other, column-wise (COLS) or row-wise, R columns of it
-template <typename T, int R, int NW, bool COLS, bool DIRECT> struct LoadB {
+template <typename T, int R, int NW, int LIST, bool COLS, bool DIRECT> struct LoadB {
     static constexpr int CS = 128 / sizeof(T), W = 16 / sizeof(T), PR = R / W, RP = 64 / PR, N = COLS ? CS / RP / NW : R / 8 / NW;
     typename KnFrag<T>::Type held[DIRECT ? 1 : N];
     const T *b;
-    const int32_t *nets;
+    int32_t nets[LIST]; // lane l's: of networks l, 64 + l, ..
     int64_t group, along, across;
     int32_t j0, J, count, rp, rank;
-    __device__ __forceinline__ void start(const Beside &p, int32_t first, int32_t columns, const int32_t *of, int32_t n)
+    __device__ __forceinline__ void start(const Beside &p, int32_t first, int32_t columns, const KN_LDS int32_t *of, int32_t n, int lane)
     {
         b = (const T *)p.b;
-        nets = of;
+#pragma unroll
+        for (int c = 0; c < LIST; ++c) nets[c] = of[64 * c + lane];
         group = p.b_group; along = p.b_c; across = p.b_j;
         j0 = first; J = columns; count = n; rp = p.rp; rank = p.rank;
     }
@@ -170,8 +171,14 @@ template <typename T, int R, int NW, bool COLS, bool DIRECT> struct LoadB {
         }
         const int32_t slot = (uint32_t)c / (uint32_t)rp, q = c - slot * rp;
         if constexpr (!COLS) left = rank - q;
+        int32_t net = __shfl(nets[0], slot & 63);
+#pragma unroll
+        for (int c = 1; c < LIST; ++c) {
+            const int32_t more = __shfl(nets[c], slot & 63);
+            net = slot >> 6 == c ? more : net;
+        }
         if (slot >= count || q >= rank || left <= 0) return nullptr;
-        return b + nets[slot] * group + q * along + (j0 + k) * across;
+        return b + net * group + q * along + (j0 + k) * across;
     }
     __device__ __forceinline__ void ask(int wave, int lane, int s)
     {
@@ -204,23 +211,25 @@ template <typename T, int R, int NW, bool COLS, bool DIRECT> struct LoadB {
 template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB>
 __global__ void __launch_bounds__(WR * WC * 64) k_adapt_up(KnProduct p, Beside beside, int32_t blocks)
 {
-    constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16, CS = 128 / sizeof(T);
+    constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16, CS = 128 / sizeof(T), LIST = (BM + 63) / 64;
     typedef typename KnFrag<T>::Type Frag;
     static_assert(DIRECT || NB == 2, "");
     static_assert(BM <= NW * 64, "a thread looks at a row");
     typedef KnRowLoader<T, BM, NW, DIRECT> LoadA;
     constexpr int BYTES = NB * STAGE > NW * 16 * (BN / WC + 4) * 4 ? NB * STAGE : NW * 16 * (BN / WC + 4) * 4;
     __shared__ __align__(16) char lds_[BYTES];
-    __shared__ int32_t slots[BM], nets[BM], met[NW]; // a row's place among the tile's networks (-1: none), the networks, how many begin in a wavefront's rows
     KN_LDS char *lds = (KN_LDS char *)lds_;
     const int tid = kn_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ntiles = (p.J + BN - 1) / BN;
     const int32_t number = kn_xcd_order(p.first + kn_block(), blocks);
     const int32_t begin = number / ntiles * BM, end = min(p.M, begin + BM);
     const int j0 = number % ntiles * BN;
+    LoadH<T, BM, NW, DIRECT> lh;
+    LoadB<T, BN, NW, LIST, COLS, DIRECT> lo;
     int32_t count = 0;
-    {
-        const int32_t i = begin + tid;
+    { // (in the stages' LDS, before they are there: with more of it there would be one workgroup at a time)
+        KN_LDS int32_t *slots = (KN_LDS int32_t *)lds, *nets = slots + BM, *met = nets + 64 * LIST; // a row's place among the tile's networks (-1: none), the
+        const int32_t i = begin + tid;                                                         // networks, how many begin in a wavefront's rows
         const bool in = tid < BM && i < end;
         const int32_t net = in ? beside.net[i] : -1, before = in && tid > 0 ? beside.net[i - 1] : -1;
         const bool some = (uint32_t)net < (uint32_t)beside.E, begins = some && net != before;
@@ -236,6 +245,9 @@ __global__ void __launch_bounds__(WR * WC * 64) k_adapt_up(KnProduct p, Beside b
         if (tid < BM) slots[tid] = some ? rank : -1;
         if (begins) nets[rank] = net;
         __syncthreads();
+        lh.start(wave, lane, (const T *)beside.h, beside.rp, begin, end, slots);
+        lo.start(beside, j0, p.J, nets, count, lane);
+        __syncthreads();
     }
     const T *a = (const T *)p.a, *b = (const T *)p.b;
     LoadA la;
@@ -248,10 +260,6 @@ __global__ void __launch_bounds__(WR * WC * 64) k_adapt_up(KnProduct p, Beside b
     KnColLoader<T, BN, NW, DIRECT> lbc;
     if constexpr (COLS) lbc.start(wave, lane, b + j0, p.b_c, p.J - j0);
     else lbr.start(wave, lane, [&](int r) { return b + (int64_t)min(j0 + r, p.J - 1) * p.b_j; });
-    LoadH<T, BM, NW, DIRECT> lh;
-    LoadB<T, BN, NW, COLS, DIRECT> lo;
-    lh.start(wave, lane, (const T *)beside.h, beside.rp, begin, end, slots);
-    lo.start(beside, j0, p.J, nets, count);
     const int32_t C = p.a_rows > 0 ? p.C : 0, shared = (C + CS - 1) / CS, steps = C > 0 ? shared + (count * beside.rp + CS - 1) / CS : 0;
     constexpr int LOADS = LoadA::N + (COLS ? lbc.N : lbr.N); // a wavefront's, per stage
     static_assert(LOADS == lh.N + lo.N, "");
