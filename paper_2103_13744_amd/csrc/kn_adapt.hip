@@ -40,43 +40,118 @@ template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type stride
     return f;
 }
 
-// 16 U rows of one network by 16 columns: a workgroup's WAVES wavefronts take every WAVES-th step of the contraction, straight into registers, and are summed in
-// the order of their numbers.  COLS: b's columns are contiguous (else its contraction is).
-template <typename T, bool COLS, int U, int WAVES>
+// Values k .. k + W - 1 of a row of C >= W, in two parts, so that nothing waits for a fetch before all are under way: a piece that ends behind the row is fetched from
+// the row's last 16 bytes, and shifted to its place at the end.
+template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type row_ask(const T *row, int32_t k, int32_t C)
+{
+    return __builtin_bit_cast(typename KnFrag<T>::Type, *(const typename KnAny<T>::Piece *)(row + min(k, C - 16 / (int)sizeof(T))));
+}
+template <typename T> __device__ __forceinline__ void row_place(typename KnFrag<T>::Type &f, int32_t k, int32_t C)
+{
+    constexpr int W = 16 / sizeof(T);
+    kn_u32x4 d = __builtin_bit_cast(kn_u32x4, f);
+    const kn_u32x4 whole = d, none = {0, 0, 0, 0};
+    const int bytes = (W - C % W) % W * (int)sizeof(T); // alike for all lanes
+    if (bytes & 2) d = kn_u32x4{d[0] >> 16 | d[1] << 16, d[1] >> 16 | d[2] << 16, d[2] >> 16 | d[3] << 16, d[3] >> 16};
+    if (bytes & 4) d = kn_u32x4{d[1], d[2], d[3], 0};
+    if (bytes & 8) d = kn_u32x4{d[2], d[3], 0, 0};
+    f = __builtin_bit_cast(typename KnFrag<T>::Type, k + W <= C ? whole : k < C ? d : none);
+}
+
+// 16 U rows of one network by 16 V columns: a workgroup's WAVES wavefronts take every WAVES-th step of the contraction, straight into registers, AHEAD steps
+// asked for while as many are multiplied, and are summed in the order of their numbers.  COLS: b's columns are contiguous (else its contraction is).
+template <typename T, bool COLS, int U, int V, int WAVES, int AHEAD>
 __global__ void __launch_bounds__(WAVES * 64) k_adapt_down(Down p)
 {
-    constexpr int W = 16 / sizeof(T), KS = 4 * W, LD = 20;
+    constexpr int W = 16 / sizeof(T), KS = 4 * W, LD = 16 * V + 4;
     typedef typename KnFrag<T>::Type Frag;
     __shared__ __align__(16) float red[WAVES * 16 * U * LD];
     const int tid = kn_thread(), lane = tid & 63, col = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int ntiles = (p.rp + 15) / 16;
+    const int ntiles = (p.rp + 16 * V - 1) / (16 * V);
     const int32_t number = p.first + kn_block();
     const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, 16 * U, number / ntiles);
-    const int j0 = number % ntiles * 16;
+    const int j0 = number % ntiles * 16 * V;
     if (piece.begin >= piece.end) return;
     const bool some = piece.group < p.E;
     const int64_t group = some ? piece.group : 0;
-    const T *arow[U], *b = (const T *)p.b + group * p.b_group + (int64_t)min(j0 + col, p.rank - 1) * p.b_j;
+    const int32_t C = p.C;
+    const T *arow[U], *brow[V];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int32_t i = min(piece.begin + 16 * u + col, piece.end - 1), src = p.rows ? p.rows[i] : i;
         arow[u] = (const T *)p.a + (int64_t)((uint32_t)src < (uint32_t)p.a_rows ? src : 0) * p.lda;
     }
-    const int32_t steps = some && p.a_rows > 0 ? (p.C + KS - 1) / KS : 0;
-    kn_f32x4 acc[U] = {};
-    for (int32_t s = wave; s < steps; s += WAVES) {
-        const int32_t k = s * KS + W * g;
-        const Frag fb = COLS ? strided_piece<T>(b, p.b_c, k, p.C) : kn_any_piece<T>(b, k, p.C);
 #pragma unroll
-        for (int u = 0; u < U; ++u) acc[u] = kn_mfma(fb, kn_any_piece<T>(arow[u], k, p.C), acc[u]);
+    for (int v = 0; v < V; ++v) brow[v] = (const T *)p.b + group * p.b_group + (int64_t)min(j0 + 16 * v + col, p.rank - 1) * p.b_j;
+    const int32_t steps = some && p.a_rows > 0 ? (C + KS - 1) / KS : 0;
+    kn_f32x4 acc[U][V] = {};
+    struct Steps { Frag a[AHEAD][U], b[AHEAD][V]; };
+    auto load = [&](Steps &x, int32_t s) { // (behind the last step: the row's end, unused)
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) {
+            const int32_t k = (s + n * WAVES) * KS + W * g;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if constexpr (COLS)
+#pragma unroll
+                    for (int q = 0; q < W; ++q) x.b[n][v][q] = brow[v][min(k + q, C - 1) * p.b_c];
+                else x.b[n][v] = row_ask<T>(brow[v], k, C);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) x.a[n][u] = row_ask<T>(arow[u], k, C);
+        }
+    };
+    auto multiply = [&](Steps &x, int32_t s) {
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) {
+            const int32_t at = s + n * WAVES, k = at * KS + W * g;
+            if (at >= steps) return;
+            if ((at + 1) * KS > C) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    if constexpr (COLS)
+#pragma unroll
+                        for (int q = 0; q < W; ++q) x.b[n][v][q] = k + q < C ? x.b[n][v][q] : (T)0.0f;
+                    else row_place<T>(x.b[n][v], k, C);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) row_place<T>(x.a[n][u], k, C);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(x.b[n][v], x.a[n][u], acc[u][v]);
+        }
+    };
+    if (C < W) { // (rows of less than a piece: one step)
+        if (wave < steps) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const Frag fb = COLS ? strided_piece<T>(brow[v], p.b_c, W * g, C) : kn_any_piece<T>(brow[v], W * g, C);
+#pragma unroll
+                for (int u = 0; u < U; ++u) acc[u][v] = kn_mfma(fb, kn_any_piece<T>(arow[u], W * g, C), acc[u][v]);
+            }
+        }
+    } else if (wave < steps) {
+        constexpr int TURN = AHEAD * WAVES;
+        Steps even, odd;
+        load(even, wave);
+        for (int32_t s = wave; s < steps; s += 2 * TURN) {
+            load(odd, s + TURN);
+            multiply(even, s);
+            load(even, s + 2 * TURN);
+            multiply(odd, s + TURN);
+        }
     }
     // (a lane's four results are neighbours in a row)
 #pragma unroll
-    for (int u = 0; u < U; ++u) *(kn_f32x4 *)(red + ((wave * U + u) * 16 + col) * LD + 4 * g) = acc[u];
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int v = 0; v < V; ++v) *(kn_f32x4 *)(red + ((wave * U + u) * 16 + col) * LD + 16 * v + 4 * g) = acc[u][v];
     __syncthreads();
     const float scale = p.scales && some ? p.scales[group] : 1.0f;
-    for (int q = tid; q < 16 * U * 4; q += WAVES * 64) {
-        const int r = q >> 2, j = j0 + (q & 3) * 4;
+    for (int q = tid; q < 16 * U * 4 * V; q += WAVES * 64) {
+        const int r = q / (4 * V), cj = q % (4 * V) * 4, j = j0 + cj;
         const int32_t i = piece.begin + r;
         if (i >= piece.end) continue;
         if (j == 0) p.net[i] = some ? piece.group : -1;
@@ -84,7 +159,7 @@ __global__ void __launch_bounds__(WAVES * 64) k_adapt_down(Down p)
         kn_f32x4 y = {0, 0, 0, 0};
         if (!p.rows || (uint32_t)p.rows[i] < (uint32_t)p.a_rows)
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) y += *(const kn_f32x4 *)(red + (w * 16 * U + r) * LD + (q & 3) * 4);
+            for (int w = 0; w < WAVES; ++w) y += *(const kn_f32x4 *)(red + (w * 16 * U + r) * LD + cj);
         typedef T Four __attribute__((ext_vector_type(4)));
         Four o;
 #pragma unroll
@@ -353,16 +428,24 @@ __global__ void __launch_bounds__(WR * WC * 64) k_adapt_up(KnProduct p, Beside b
     }
 }
 
-template <typename T, bool COLS> int launch_down(hipStream_t st, const Down &p)
+template <typename T, bool COLS, int U, int V, int WAVES, int AHEAD> int launch_down_of(hipStream_t st, const Down &p)
 {
-    const int ntiles = (p.rp + 15) / 16;
-    const bool narrow = p.C * (int64_t)sizeof(T) <= 512;
-    return kn_launch(kn_pieces(p.M, p.E, 32) * ntiles, narrow ? 64 : 512, [&](dim3 grid, int32_t first) {
+    return kn_launch(kn_pieces(p.M, p.E, 16 * U) * kn_div_up(p.rp, 16 * V), WAVES * 64, [&](dim3 grid, int32_t first) {
         Down q = p;
         q.first = first;
-        if (narrow) hipLaunchKernelGGL((k_adapt_down<T, COLS, 2, 1>), grid, dim3(64), 0, st, q);
-        else hipLaunchKernelGGL((k_adapt_down<T, COLS, 2, 8>), grid, dim3(512), 0, st, q);
+        hipLaunchKernelGGL((k_adapt_down<T, COLS, U, V, WAVES, AHEAD>), grid, dim3(WAVES * 64), 0, st, q);
     });
+}
+template <typename T, bool COLS, int V> int launch_down_columns(hipStream_t st, const Down &p)
+{
+    if (p.C * (int64_t)sizeof(T) <= 512) return launch_down_of<T, COLS, 2, V, 1, 2>(st, p);
+    if (p.M / p.E >= 32) return launch_down_of<T, COLS, 4, V, 8, 1>(st, p);
+    return launch_down_of<T, COLS, 1, V, 8, 2>(st, p);
+}
+template <typename T, bool COLS> int launch_down(hipStream_t st, const Down &p)
+{
+    if (p.rp <= 16) return launch_down_columns<T, COLS, 1>(st, p);
+    return p.rp <= 32 ? launch_down_columns<T, COLS, 2>(st, p) : launch_down_columns<T, COLS, 4>(st, p);
 }
 
 template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB> int launch_tiles(hipStream_t st, const KnProduct &p, const Beside &beside)
@@ -387,7 +470,7 @@ template <typename T, bool COLS> int launch_up(hipStream_t st, const KnProduct &
     } else {
         if (!direct) return narrow ? launch_tiles<T, COLS, false, 32, 64, 1, 4, 2>(st, p, beside) : launch_tiles<T, COLS, false, 128, 128, 2, 4, 2>(st, p, beside);
         if (narrow) return launch_tiles<T, COLS, true, 32, 64, 1, 4, 4>(st, p, beside);
-        if (tiles(192) >= 256) return launch_tiles<T, COLS, true, 192, 128, 2, 2, 2>(st, p, beside);
+        if (tiles(128) >= 256) return launch_tiles<T, COLS, true, 128, 128, 2, 4, 2>(st, p, beside);
         return launch_tiles<T, COLS, true, 64, 128, 1, 4, 2>(st, p, beside);
     }
 }
