@@ -58,97 +58,143 @@ template <typename T> __device__ __forceinline__ void row_place(typename KnFrag<
     f = __builtin_bit_cast(typename KnFrag<T>::Type, k + W <= C ? whole : k < C ? d : none);
 }
 
-// 16 U rows of one network by 16 V columns: a workgroup's WAVES wavefronts take every WAVES-th step of the contraction, straight into registers, AHEAD steps
-// asked for while as many are multiplied, and are summed in the order of their numbers.  COLS: b's columns are contiguous (else its contraction is).
-template <typename T, bool COLS, int U, int V, int WAVES, int AHEAD>
-__global__ void __launch_bounds__(WAVES * 64) k_adapt_down(Down p)
+// 16 U rows of one network by 16 V columns: a workgroup's WAVES wavefronts take turns of AHEAD steps of the contraction, straight into registers, one asked
+// for while another is multiplied, and are summed in the order of their numbers.  Where b's columns are contiguous (not its contraction) and in whole 16-byte
+// pieces, 16-bit values are turned by the transposing read of an LDS that each wavefront has for itself; else they are fetched one by one, eight for a fragment.
+enum { B_ROWS, B_COLS, B_PIECES };
+// Where row r of a step's 32 rows of 16 V columns, and its piece, lie: the 4 x 4 rows of a transposing read are spread over all banks
+template <int V> __device__ __forceinline__ int turned_byte(int r, int piece)
 {
-    constexpr int W = 16 / sizeof(T), KS = 4 * W, LD = 16 * V + 4;
-    typedef typename KnFrag<T>::Type Frag;
-    __shared__ __align__(16) float red[WAVES * 16 * U * LD];
-    const int tid = kn_thread(), lane = tid & 63, col = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if constexpr (V == 1) return (r ^ (r >> 3 & 1) << 2) * 32 + piece * 16;
+    else if constexpr (V == 2) return r * 64 + (piece ^ (r >> 3 & 1) << 1) * 16;
+    else return r * 128 + (piece ^ ((r >> 1 & 1) | (r >> 3 & 1) << 1) << 1) * 16;
+}
+template <typename T, int B, int U, int V, int WAVES, int AHEAD> struct Sums {
+    static constexpr int W = 16 / sizeof(T), KS = 4 * W, LD = 16 * V + 4, WORDS = WAVES * 16 * U * LD;
+    static constexpr bool COLS = B == B_COLS, TURN_B = B == B_PIECES;
+    static_assert(!TURN_B || 16 * U * LD * 4 >= V * 1024, "");
+    // Leaves each wavefront's sums over its turns among the steps [first, last) in `red`: row r and column j of wavefront w at (w 16 U + r) LD + j.  arow: the lane's rows
+    // (column l % 16 of each 16), b: the first value of column j0, whose columns are b_j apart and whose contraction b_c.
+    static __device__ __forceinline__ void run(const T *const arow[U], const T *b, int64_t b_c, int64_t b_j, int32_t columns, int32_t C, int32_t first, int32_t last, float *red)
+    {
+        typedef typename KnFrag<T>::Type Frag;
+        const int tid = kn_thread(), lane = tid & 63, col = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        KN_LDS char *turn = (KN_LDS char *)red + wave * (16 * U * LD * 4);
+        const T *brow[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) // (TURN_B: of the lane's v-th piece)
+            brow[v] = b + (TURN_B ? min((lane + 64 * v) % (2 * V) * W, columns - W) : min(16 * v + col, columns - 1)) * b_j;
+        kn_f32x4 acc[U][V] = {};
+        struct Steps { Frag a[AHEAD][U], b[AHEAD][V]; };
+        auto load = [&](Steps &x, int32_t s) { // (behind the last step: the row's end, unused)
+#pragma unroll
+            for (int n = 0; n < AHEAD; ++n) {
+                const int32_t k = (s + n) * KS + W * g;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    if constexpr (TURN_B) x.b[n][v] = *(const Frag *)(brow[v] + min((s + n) * KS + (lane + 64 * v) / (2 * V), C - 1) * b_c);
+                    else if constexpr (COLS)
+#pragma unroll
+                        for (int q = 0; q < W; ++q) x.b[n][v][q] = brow[v][min(k + q, C - 1) * b_c];
+                    else x.b[n][v] = row_ask<T>(brow[v], k, C);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) x.a[n][u] = row_ask<T>(arow[u], k, C);
+            }
+        };
+        auto multiply = [&](Steps &x, int32_t s) {
+#pragma unroll
+            for (int n = 0; n < AHEAD; ++n) {
+                const int32_t at = s + n, k = at * KS + W * g;
+                if (at >= last) return;
+                if ((at + 1) * KS > C) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        if constexpr (TURN_B) {
+                            if (at * KS + (lane + 64 * v) / (2 * V) >= C) x.b[n][v] = Frag{};
+                        } else if constexpr (COLS)
+#pragma unroll
+                            for (int q = 0; q < W; ++q) x.b[n][v][q] = k + q < C ? x.b[n][v][q] : (T)0.0f;
+                        else row_place<T>(x.b[n][v], k, C);
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u) row_place<T>(x.a[n][u], k, C);
+                }
+                if constexpr (TURN_B) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) *(KN_LDS Frag *)(turn + turned_byte<V>((lane + 64 * v) / (2 * V), (lane + 64 * v) % (2 * V))) = x.b[n][v];
+                    kn_lanes_meet();
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        union { kn_s16x4 h[2]; Frag f; } t;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            t.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KN_LDS kn_s16x4 *)(turn + turned_byte<V>(8 * g + 4 * h + (col >> 2), 2 * v + (col >> 1 & 1)) + (col & 1) * 8));
+                        x.b[n][v] = t.f;
+                    }
+                    kn_lanes_meet();
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(x.b[n][v], x.a[n][u], acc[u][v]);
+            }
+        };
+        if (!TURN_B && C < W) { // (rows of less than a piece: one step)
+            if (first + wave < last) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const Frag fb = COLS ? strided_piece<T>(brow[v], b_c, W * g, C) : kn_any_piece<T>(brow[v], W * g, C);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) acc[u][v] = kn_mfma(fb, kn_any_piece<T>(arow[u], W * g, C), acc[u][v]);
+                }
+            }
+        } else if (first + wave * AHEAD < last) {
+            constexpr int TURN = AHEAD * WAVES;
+            Steps even, odd;
+            load(even, first + wave * AHEAD);
+            for (int32_t s = first + wave * AHEAD; s < last; s += 2 * TURN) {
+                load(odd, s + TURN);
+                multiply(even, s);
+                load(even, s + 2 * TURN);
+                multiply(odd, s + TURN);
+            }
+        }
+        // (a lane's four results are neighbours in a row; a wavefront's part of `red` is what it turned b in)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int v = 0; v < V; ++v) *(kn_f32x4 *)(red + ((wave * U + u) * 16 + col) * LD + 16 * v + 4 * g) = acc[u][v];
+        __syncthreads();
+    }
+    static __device__ __forceinline__ kn_f32x4 of(const float *red, int r, int j)
+    {
+        kn_f32x4 y = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) y += *(const kn_f32x4 *)(red + (w * 16 * U + r) * LD + j);
+        return y;
+    }
+};
+
+// The h of 16 U rows of one network, 16 V values
+template <typename T, int B, int U, int V, int WAVES, int AHEAD> __device__ __forceinline__ void down_piece(const Down &p, int32_t number, float *red)
+{
+    typedef Sums<T, B, U, V, WAVES, AHEAD> Core;
+    const int tid = kn_thread(), col = tid & 15;
     const int ntiles = (p.rp + 16 * V - 1) / (16 * V);
-    const int32_t number = p.first + kn_block();
     const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, 16 * U, number / ntiles);
     const int j0 = number % ntiles * 16 * V;
     if (piece.begin >= piece.end) return;
     const bool some = piece.group < p.E;
     const int64_t group = some ? piece.group : 0;
-    const int32_t C = p.C;
-    const T *arow[U], *brow[V];
+    const T *arow[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int32_t i = min(piece.begin + 16 * u + col, piece.end - 1), src = p.rows ? p.rows[i] : i;
         arow[u] = (const T *)p.a + (int64_t)((uint32_t)src < (uint32_t)p.a_rows ? src : 0) * p.lda;
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) brow[v] = (const T *)p.b + group * p.b_group + (int64_t)min(j0 + 16 * v + col, p.rank - 1) * p.b_j;
-    const int32_t steps = some && p.a_rows > 0 ? (C + KS - 1) / KS : 0;
-    kn_f32x4 acc[U][V] = {};
-    struct Steps { Frag a[AHEAD][U], b[AHEAD][V]; };
-    auto load = [&](Steps &x, int32_t s) { // (behind the last step: the row's end, unused)
-#pragma unroll
-        for (int n = 0; n < AHEAD; ++n) {
-            const int32_t k = (s + n * WAVES) * KS + W * g;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if constexpr (COLS)
-#pragma unroll
-                    for (int q = 0; q < W; ++q) x.b[n][v][q] = brow[v][min(k + q, C - 1) * p.b_c];
-                else x.b[n][v] = row_ask<T>(brow[v], k, C);
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) x.a[n][u] = row_ask<T>(arow[u], k, C);
-        }
-    };
-    auto multiply = [&](Steps &x, int32_t s) {
-#pragma unroll
-        for (int n = 0; n < AHEAD; ++n) {
-            const int32_t at = s + n * WAVES, k = at * KS + W * g;
-            if (at >= steps) return;
-            if ((at + 1) * KS > C) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    if constexpr (COLS)
-#pragma unroll
-                        for (int q = 0; q < W; ++q) x.b[n][v][q] = k + q < C ? x.b[n][v][q] : (T)0.0f;
-                    else row_place<T>(x.b[n][v], k, C);
-                }
-#pragma unroll
-                for (int u = 0; u < U; ++u) row_place<T>(x.a[n][u], k, C);
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int v = 0; v < V; ++v) acc[u][v] = kn_mfma(x.b[n][v], x.a[n][u], acc[u][v]);
-        }
-    };
-    if (C < W) { // (rows of less than a piece: one step)
-        if (wave < steps) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const Frag fb = COLS ? strided_piece<T>(brow[v], p.b_c, W * g, C) : kn_any_piece<T>(brow[v], W * g, C);
-#pragma unroll
-                for (int u = 0; u < U; ++u) acc[u][v] = kn_mfma(fb, kn_any_piece<T>(arow[u], W * g, C), acc[u][v]);
-            }
-        }
-    } else if (wave < steps) {
-        constexpr int TURN = AHEAD * WAVES;
-        Steps even, odd;
-        load(even, wave);
-        for (int32_t s = wave; s < steps; s += 2 * TURN) {
-            load(odd, s + TURN);
-            multiply(even, s);
-            load(even, s + 2 * TURN);
-            multiply(odd, s + TURN);
-        }
-    }
-    // (a lane's four results are neighbours in a row)
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int v = 0; v < V; ++v) *(kn_f32x4 *)(red + ((wave * U + u) * 16 + col) * LD + 16 * v + 4 * g) = acc[u][v];
-    __syncthreads();
+    Core::run(arow, (const T *)p.b + group * p.b_group + j0 * p.b_j, p.b_c, p.b_j, p.rank - j0, p.C, 0,
+              some && p.a_rows > 0 ? (p.C + Core::KS - 1) / Core::KS : 0, red);
     const float scale = p.scales && some ? p.scales[group] : 1.0f;
     for (int q = tid; q < 16 * U * 4 * V; q += WAVES * 64) {
         const int r = q / (4 * V), cj = q % (4 * V) * 4, j = j0 + cj;
@@ -157,15 +203,131 @@ __global__ void __launch_bounds__(WAVES * 64) k_adapt_down(Down p)
         if (j == 0) p.net[i] = some ? piece.group : -1;
         if (j >= p.rp) continue;
         kn_f32x4 y = {0, 0, 0, 0};
-        if (!p.rows || (uint32_t)p.rows[i] < (uint32_t)p.a_rows)
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) y += *(const kn_f32x4 *)(red + (w * 16 * U + r) * LD + cj);
+        if (!p.rows || (uint32_t)p.rows[i] < (uint32_t)p.a_rows) y = Core::of(red, r, cj);
         typedef T Four __attribute__((ext_vector_type(4)));
         Four o;
 #pragma unroll
         for (int n = 0; n < 4; ++n) o[n] = j + n < p.rank ? (T)(scale * y[n]) : (T)0.0f; // (16 bits: what the matrix cores take)
         *(Four *)((T *)p.h + (int64_t)i * p.rp + j) = o;
     }
+}
+template <typename T, int B, int U, int V, int WAVES, int AHEAD> __global__ void __launch_bounds__(WAVES * 64) k_adapt_down(Down p)
+{
+    __shared__ __align__(16) float red[Sums<T, B, U, V, WAVES, AHEAD>::WORDS];
+    down_piece<T, B, U, V, WAVES, AHEAD>(p, p.first + kn_block(), red);
+}
+
+// Few rows (16 U at most): one launch leaves h and the shared product's sums, cut into parts of the contraction so that all of w is on its way at once; the
+// second adds the parts up and what h has to add.
+struct Few {
+    float *sums;       // (parts, M, J)
+    int32_t parts, each; // of so many steps
+    int32_t products;  // workgroups of the shared product
+};
+constexpr int FEW_ROWS = 64;
+template <typename T, int B, int U, int V, int DOWN_V> __global__ void __launch_bounds__(512) k_adapt_few(KnProduct p, Down down, Few few)
+{
+    typedef Sums<T, B, U, V, 8, 1> Core;
+    typedef Sums<T, B, 1, DOWN_V, 8, 2> Low;
+    __shared__ __align__(16) float red[Core::WORDS > Low::WORDS ? Core::WORDS : Low::WORDS];
+    const int32_t block = kn_block();
+    if (block >= few.products) {
+        down_piece<T, B, 1, DOWN_V, 8, 2>(down, block - few.products, red);
+        return;
+    }
+    const int tid = kn_thread(), col = tid & 15;
+    const int ntiles = (p.J + 16 * V - 1) / (16 * V), number = kn_xcd_order(block, few.products);
+    const int part = number / ntiles, j0 = number % ntiles * 16 * V;
+    const T *arow[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int32_t i = min(16 * u + col, p.M - 1), src = p.rows ? p.rows[i] : i;
+        arow[u] = (const T *)p.a + (int64_t)((uint32_t)src < (uint32_t)p.a_rows ? src : 0) * p.lda;
+    }
+    const int32_t steps = p.a_rows > 0 ? (p.C + Core::KS - 1) / Core::KS : 0;
+    Core::run(arow, (const T *)p.b + j0 * p.b_j, p.b_c, p.b_j, p.J - j0, p.C, min(part * few.each, steps), min((part + 1) * few.each, steps), red);
+    for (int q = tid; q < 16 * U * 4 * V; q += 512) {
+        const int i = q / (4 * V), cj = q % (4 * V) * 4, j = j0 + cj;
+        if (i >= p.M || j >= p.J) continue;
+        const kn_f32x4 y = Core::of(red, i, cj);
+        float *to = few.sums + ((int64_t)part * p.M + i) * p.J + j;
+        if (p.J % 4 == 0) *(kn_f32x4 *)to = y;
+        else
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+                if (j + n < p.J) to[n] = y[n];
+    }
+}
+// Four results of a row per thread
+template <typename T> __global__ void __launch_bounds__(128) k_adapt_few_join(KnProduct p, Beside beside, Few few)
+{
+    typedef T Four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    typedef float Sum __attribute__((ext_vector_type(4), aligned(4)));
+    const int32_t fours = (p.J + 3) / 4, q = kn_block() * 128 + kn_thread();
+    const int32_t i = q / fours, j = q % fours * 4;
+    if (i >= p.M) return;
+    const bool whole = j + 4 <= p.J;
+    const int32_t net = beside.net[i];
+    float y[4] = {};
+    for (int part = 0; part < few.parts; ++part) {
+        const float *from = few.sums + ((int64_t)part * p.M + i) * p.J + j;
+        Sum v = {};
+        if (whole) v = *(const Sum *)from;
+        else
+#pragma unroll
+            for (int n = 0; n < 4; ++n) v[n] = from[min(n, p.J - 1 - j)];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) y[n] += v[n];
+    }
+    if ((uint32_t)net < (uint32_t)beside.E && p.a_rows > 0) {
+        const T *h = (const T *)beside.h + (int64_t)i * beside.rp, *b = (const T *)beside.b + net * beside.b_group + j * beside.b_j;
+        float low[4] = {};
+        if (beside.b_j == 1 && beside.b_c != 1) {
+#pragma unroll 8
+            for (int32_t c = 0; c < beside.rank; ++c) {
+                Four v;
+                if (whole) v = *(const Four *)(b + c * beside.b_c);
+                else
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) v[n] = b[c * beside.b_c + min(n, p.J - 1 - j)];
+                const float a = (float)h[c];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) low[n] = fmaf(a, (float)v[n], low[n]);
+            }
+        } else {
+            constexpr int W = 16 / sizeof(T);
+            for (int32_t c = 0; c < beside.rank; c += W) { // (h has zeros behind the rank)
+                const typename KnFrag<T>::Type a = *(const typename KnFrag<T>::Type *)(h + c);
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const typename KnFrag<T>::Type v = kn_any_piece<T>(b + min(n, p.J - 1 - j) * beside.b_j, c, beside.rank);
+#pragma unroll
+                    for (int w = 0; w < W; ++w) low[n] = fmaf((float)a[w], (float)v[w], low[n]);
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < 4; ++n) y[n] += low[n];
+    }
+    const bool out_of_x = p.rows && (uint32_t)p.rows[i] >= (uint32_t)p.a_rows;
+    const int32_t src = p.mask_rows ? p.mask_rows[i] : i;
+    const T *mask = p.mask && (uint32_t)src < (uint32_t)p.m_rows ? (const T *)p.mask + (int64_t)src * p.ldm + j : nullptr;
+    Four o;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const int at = min(n, p.J - 1 - j);
+        float v = out_of_x ? 0.0f : y[n];
+        if (p.bias) v += (float)((const T *)p.bias)[j + at];
+        if (p.relu) v = v > 0.0f || v != v ? v : 0.0f; // (a NaN stays one)
+        if (p.mask && !(mask && (float)mask[at] > 0.0f)) v = 0.0f;
+        o[n] = (T)v;
+    }
+    T *out = (T *)p.out + (int64_t)i * p.o_i + j;
+    if (whole) *(Four *)out = o;
+    else
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+            if (j + n < p.J) out[n] = o[n];
 }
 
 // A stage of the rows' h, row-wise: row r's stand at columns slot_r * rp of the longer contraction
@@ -428,24 +590,32 @@ __global__ void __launch_bounds__(WR * WC * 64) k_adapt_up(KnProduct p, Beside b
     }
 }
 
-template <typename T, bool COLS, int U, int V, int WAVES, int AHEAD> int launch_down_of(hipStream_t st, const Down &p)
+template <typename T, int B, int U, int V, int WAVES, int AHEAD> int launch_down_of(hipStream_t st, const Down &p)
 {
     return kn_launch(kn_pieces(p.M, p.E, 16 * U) * kn_div_up(p.rp, 16 * V), WAVES * 64, [&](dim3 grid, int32_t first) {
         Down q = p;
         q.first = first;
-        hipLaunchKernelGGL((k_adapt_down<T, COLS, U, V, WAVES, AHEAD>), grid, dim3(WAVES * 64), 0, st, q);
+        hipLaunchKernelGGL((k_adapt_down<T, B, U, V, WAVES, AHEAD>), grid, dim3(WAVES * 64), 0, st, q);
     });
 }
-template <typename T, bool COLS, int V> int launch_down_columns(hipStream_t st, const Down &p)
+template <typename T, int B, int V> int launch_down_columns(hipStream_t st, const Down &p)
 {
-    if (p.C * (int64_t)sizeof(T) <= 512) return launch_down_of<T, COLS, 2, V, 1, 2>(st, p);
-    if (p.M / p.E >= 32) return launch_down_of<T, COLS, 4, V, 8, 1>(st, p);
-    return launch_down_of<T, COLS, 1, V, 8, 2>(st, p);
+    if (p.C * (int64_t)sizeof(T) <= 512) return launch_down_of<T, B, 2, V, 1, 2>(st, p);
+    if (p.M / p.E >= 32) return launch_down_of<T, B, 2, V, 4, 2>(st, p);
+    return launch_down_of<T, B, 1, V, 8, 2>(st, p);
 }
-template <typename T, bool COLS> int launch_down(hipStream_t st, const Down &p)
+template <typename T, int B> int launch_down_of_b(hipStream_t st, const Down &p)
 {
-    if (p.rp <= 16) return launch_down_columns<T, COLS, 1>(st, p);
-    return p.rp <= 32 ? launch_down_columns<T, COLS, 2>(st, p) : launch_down_columns<T, COLS, 4>(st, p);
+    if (p.rp <= 16) return launch_down_columns<T, B, 1>(st, p);
+    return p.rp <= 32 ? launch_down_columns<T, B, 2>(st, p) : launch_down_columns<T, B, 4>(st, p);
+}
+template <typename T> int launch_down(hipStream_t st, const Down &p, bool cols)
+{
+    if (!cols) return launch_down_of_b<T, B_ROWS>(st, p);
+    if constexpr (sizeof(T) == 2) {
+        if (p.rank % 8 == 0 && p.C >= 8 && ((uintptr_t)p.b & 15) == 0) return launch_down_of_b<T, B_PIECES>(st, p);
+    }
+    return launch_down_of_b<T, B_COLS>(st, p);
 }
 
 template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB> int launch_tiles(hipStream_t st, const KnProduct &p, const Beside &beside)
@@ -475,13 +645,65 @@ template <typename T, bool COLS> int launch_up(hipStream_t st, const KnProduct &
     }
 }
 
-// Both products of a call on `a` (rows through `rows`): h = scale a b_e, out = a w + h c_e.  cols: those of b are contiguous, and not those of w and c
-int run(hipStream_t st, int32_t dtype, bool b_cols, const Down &down, const KnProduct &up, const Beside &beside)
+// How few rows' product is cut: columns of a workgroup, parts of the contraction until there are workgroups for the chip, no part of less than a step per wavefront
+Few few_of(int64_t M, int32_t J, int32_t C, int item, int columns)
+{
+    Few f = {};
+    const int64_t tiles = kn_div_up(J, columns), steps = kn_div_up(C, 64 / item);
+    int64_t parts = kn_div_up(256, tiles);
+    if (parts > kn_div_up(steps, 8)) parts = kn_div_up(steps, 8);
+    f.each = (int32_t)kn_div_up(steps, parts);
+    f.parts = (int32_t)kn_div_up(steps, f.each);
+    f.products = (int32_t)(tiles * f.parts);
+    return f;
+}
+constexpr int FEW_V = 2;
+int64_t few_bytes(int64_t M, int32_t J, int32_t C, int item) { return M > FEW_ROWS ? 0 : kn_align_up(few_of(M, J, C, item, 16 * FEW_V).parts * M * J * 4, 256); }
+
+template <typename T, int B, int U, int DOWN_V> int launch_few_of(hipStream_t st, const Down &down, const KnProduct &p, const Few &few)
+{
+    const int64_t blocks = few.products + kn_pieces(down.M, down.E, 16) * kn_div_up(down.rp, 16 * DOWN_V);
+    hipLaunchKernelGGL((k_adapt_few<T, B, U, FEW_V, DOWN_V>), dim3((unsigned)blocks), dim3(512), 0, st, p, down, few);
+    KN_CHECK_LAUNCH();
+    return KN_OK;
+}
+template <typename T, int B, int U> int launch_few_rank(hipStream_t st, const Down &down, const KnProduct &p, const Few &few)
+{
+    return down.rp <= 16 ? launch_few_of<T, B, U, 1>(st, down, p, few) : launch_few_of<T, B, U, 2>(st, down, p, few);
+}
+template <typename T, int B> int launch_few_rows(hipStream_t st, const Down &down, const KnProduct &p, const Few &few)
+{
+    if (p.M <= 16) return launch_few_rank<T, B, 1>(st, down, p, few);
+    return p.M <= 32 ? launch_few_rank<T, B, 2>(st, down, p, few) : launch_few_rank<T, B, 4>(st, down, p, few);
+}
+template <typename T> int launch_few_b(hipStream_t st, const Down &down, const KnProduct &p, const Few &few, bool cols)
+{
+    if (!cols) return launch_few_rows<T, B_ROWS>(st, down, p, few);
+    if constexpr (sizeof(T) == 2) {
+        if (p.J % 8 == 0 && down.rank % 8 == 0 && p.C >= 8 && (((uintptr_t)p.b | (uintptr_t)down.b) & 15) == 0) return launch_few_rows<T, B_PIECES>(st, down, p, few);
+    }
+    return launch_few_rows<T, B_COLS>(st, down, p, few);
+}
+template <typename T> int launch_few(hipStream_t st, const Down &down, const KnProduct &p, const Beside &beside, bool cols, float *sums)
+{
+    Few few = few_of(p.M, p.J, p.C, sizeof(T), 16 * FEW_V);
+    few.sums = sums;
+    KN_TRY(launch_few_b<T>(st, down, p, few, cols));
+    hipLaunchKernelGGL((k_adapt_few_join<T>), dim3((unsigned)kn_div_up((int64_t)p.M * kn_div_up(p.J, 4), 128)), dim3(128), 0, st, p, beside, few);
+    KN_CHECK_LAUNCH();
+    return KN_OK;
+}
+
+// Both products of a call on `a` (rows through `rows`): h = scale a b_e, out = a w + h c_e.  cols: the columns of b and w are contiguous, and c's; else their contractions
+// are.  sums: room for few rows' parts.
+int run(hipStream_t st, int32_t dtype, bool cols, const Down &down, const KnProduct &up, const Beside &beside, float *sums)
 {
     return kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
-        KN_TRY(b_cols ? (launch_down<E_, true>(st, down)) : (launch_down<E_, false>(st, down)));
-        return up.b_j == 1 && up.b_c != 1 ? launch_up<E_, true>(st, up, beside) : launch_up<E_, false>(st, up, beside);
+        // (very many networks of a very large rank: the other way's launches are cut)
+        if (up.M <= FEW_ROWS && down.E * (int64_t)down.rp <= 1 << 24) return launch_few<E_>(st, down, up, beside, cols, sums);
+        KN_TRY(launch_down<E_>(st, down, cols));
+        return cols && up.b_c != 1 ? launch_up<E_, true>(st, up, beside) : launch_up<E_, false>(st, up, beside);
     });
 }
 
@@ -507,7 +729,9 @@ int dw_bytes(const kn_linear_desc *d, int32_t rank, int64_t *out)
     int64_t na = 0, nb = 0;
     KN_TRY(kn_grouped_linear_dw_workspace_bytes(&a, &na));
     KN_TRY(kn_grouped_linear_dw_workspace_bytes(&b, &nb));
+    const int64_t few = few_bytes(d->rows, d->n_in, d->n_out, kn_item(d->dtype)); // (done with before the others begin)
     *out = na > nb ? na : nb;
+    *out = few > *out ? few : *out;
     return KN_OK;
 }
 bool bad_workspace(const void *ws, int64_t have, int64_t need) { return need > 0 && (!ws || ((uintptr_t)ws & 255) || have < need); }
@@ -518,7 +742,7 @@ extern "C" int kn_adapted_linear_workspace_bytes(const kn_linear_desc *d, int32_
 {
     KN_TRY(check(d, rank));
     if (!out_bytes) return KN_E_INVALID_ARG;
-    *out_bytes = net_bytes(d) + h_bytes(d, rank);
+    *out_bytes = net_bytes(d) + h_bytes(d, rank) + few_bytes(d->rows, d->n_out, d->n_in, kn_item(d->dtype));
     return KN_OK;
 }
 
@@ -529,7 +753,9 @@ extern "C" int kn_adapted_linear(void *stream, const kn_linear_desc *d, int32_t 
     KN_TRY(check(d, rank));
     if (d->rows == 0) return KN_OK;
     if (!w || !a || !b || !offsets || !y || (d->x_rows > 0 && !x) || (!rows && d->x_rows < d->rows) || ((uintptr_t)h & 15)) return KN_E_INVALID_ARG;
-    if (bad_workspace(workspace, workspace_bytes, net_bytes(d) + h_bytes(d, rank))) return KN_E_WORKSPACE;
+    int64_t need = 0;
+    KN_TRY(kn_adapted_linear_workspace_bytes(d, rank, &need));
+    if (bad_workspace(workspace, workspace_bytes, need)) return KN_E_WORKSPACE;
     const bool io = d->w_layout == KN_W_IN_OUT;
     const int64_t K = d->n_in, N = d->n_out, R = rank;
     Down down = {x, a, scales, h ? h : (char *)workspace + net_bytes(d), (int32_t *)workspace, offsets, rows, d->ldx, K * R, io ? R : 1, io ? 1 : K,
@@ -539,7 +765,7 @@ extern "C" int kn_adapted_linear(void *stream, const kn_linear_desc *d, int32_t 
     p.a = x; p.b = w; p.bias = bias; p.out = y; p.rows = rows;
     p.lda = d->ldx; p.b_c = io ? N : 1; p.b_j = io ? 1 : K; p.o_i = N;
     p.M = down.M; p.J = d->n_out; p.C = d->n_in; p.a_rows = down.a_rows; p.relu = relu != 0;
-    return run((hipStream_t)stream, d->dtype, io, down, p, beside);
+    return run((hipStream_t)stream, d->dtype, io, down, p, beside, (float *)((char *)workspace + net_bytes(d) + h_bytes(d, rank)));
 }
 
 extern "C" int kn_adapted_linear_backward_workspace_bytes(const kn_linear_desc *d, int32_t rank, int64_t *out_bytes)
@@ -576,7 +802,7 @@ extern "C" int kn_adapted_linear_backward(void *stream, const kn_linear_desc *d,
         p.lda = N; p.ldm = d->ldx; p.b_c = io ? 1 : K; p.b_j = io ? N : 1; p.o_i = K;
         p.M = down.M; p.J = d->n_in; p.C = d->n_out; p.a_rows = p.M; p.m_rows = (int32_t)d->x_rows;
         p.mask_rows = relu_in ? rows : nullptr;
-        KN_TRY(run((hipStream_t)stream, d->dtype, !io, down, p, beside));
+        KN_TRY(run((hipStream_t)stream, d->dtype, !io, down, p, beside, (float *)sums));
     }
     const kn_linear_desc la = layer_of(d, d->n_in, rank, d->x_rows, d->ldx), lb = layer_of(d, rank, d->n_out, d->rows, rp);
     KN_TRY(kn_linear_dw_run(stream, &la, x, nullptr, g, rp, offsets, rows, da, nullptr, sums, dw));
