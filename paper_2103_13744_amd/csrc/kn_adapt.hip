@@ -40,24 +40,6 @@ template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type stride
     return f;
 }
 
-// Values k .. k + W - 1 of a row of C >= W, in two parts, so that nothing waits for a fetch before all are under way: a piece that ends behind the row is fetched from
-// the row's last 16 bytes, and shifted to its place at the end.
-template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type row_ask(const T *row, int32_t k, int32_t C)
-{
-    return __builtin_bit_cast(typename KnFrag<T>::Type, *(const typename KnAny<T>::Piece *)(row + min(k, C - 16 / (int)sizeof(T))));
-}
-template <typename T> __device__ __forceinline__ void row_place(typename KnFrag<T>::Type &f, int32_t k, int32_t C)
-{
-    constexpr int W = 16 / sizeof(T);
-    kn_u32x4 d = __builtin_bit_cast(kn_u32x4, f);
-    const kn_u32x4 whole = d, none = {0, 0, 0, 0};
-    const int bytes = (W - C % W) % W * (int)sizeof(T); // alike for all lanes
-    if (bytes & 2) d = kn_u32x4{d[0] >> 16 | d[1] << 16, d[1] >> 16 | d[2] << 16, d[2] >> 16 | d[3] << 16, d[3] >> 16};
-    if (bytes & 4) d = kn_u32x4{d[1], d[2], d[3], 0};
-    if (bytes & 8) d = kn_u32x4{d[2], d[3], 0, 0};
-    f = __builtin_bit_cast(typename KnFrag<T>::Type, k + W <= C ? whole : k < C ? d : none);
-}
-
 // 16 U rows of one network by 16 V columns: a workgroup's WAVES wavefronts take turns of AHEAD steps of the contraction, straight into registers, one asked
 // for while another is multiplied, and are summed in the order of their numbers.  Where b's columns are contiguous (not its contraction) and in whole 16-byte
 // pieces, 16-bit values are turned by the transposing read of an LDS that each wavefront has for itself; else they are fetched one by one, eight for a fragment.
@@ -86,6 +68,7 @@ template <typename T, int B, int U, int V, int WAVES, int AHEAD> struct Sums {
             brow[v] = b + (TURN_B ? min((lane + 64 * v) % (2 * V) * W, columns - W) : min(16 * v + col, columns - 1)) * b_j;
         kn_f32x4 acc[U][V] = {};
         struct Steps { Frag a[AHEAD][U], b[AHEAD][V]; };
+        uint32_t none; // (rows are fetched as they lie)
         auto load = [&](Steps &x, int32_t s) { // (behind the last step: the row's end, unused)
 #pragma unroll
             for (int n = 0; n < AHEAD; ++n) {
@@ -96,10 +79,10 @@ template <typename T, int B, int U, int V, int WAVES, int AHEAD> struct Sums {
                     else if constexpr (COLS)
 #pragma unroll
                         for (int q = 0; q < W; ++q) x.b[n][v][q] = brow[v][min(k + q, C - 1) * b_c];
-                    else x.b[n][v] = row_ask<T>(brow[v], k, C);
+                    else x.b[n][v] = kn_row_ask<T>(brow[v], k, C, false, none);
                 }
 #pragma unroll
-                for (int u = 0; u < U; ++u) x.a[n][u] = row_ask<T>(arow[u], k, C);
+                for (int u = 0; u < U; ++u) x.a[n][u] = kn_row_ask<T>(arow[u], k, C, false, none);
             }
         };
         auto multiply = [&](Steps &x, int32_t s) {
@@ -115,10 +98,10 @@ template <typename T, int B, int U, int V, int WAVES, int AHEAD> struct Sums {
                         } else if constexpr (COLS)
 #pragma unroll
                             for (int q = 0; q < W; ++q) x.b[n][v][q] = k + q < C ? x.b[n][v][q] : (T)0.0f;
-                        else row_place<T>(x.b[n][v], k, C);
+                        else kn_row_place<T>(x.b[n][v], brow[v], k, C, false, 0);
                     }
 #pragma unroll
-                    for (int u = 0; u < U; ++u) row_place<T>(x.a[n][u], k, C);
+                    for (int u = 0; u < U; ++u) kn_row_place<T>(x.a[n][u], arow[u], k, C, false, 0);
                 }
                 if constexpr (TURN_B) {
 #pragma unroll
@@ -590,6 +573,226 @@ __global__ void __launch_bounds__(WR * WC * 64) k_adapt_up(KnProduct p, Beside b
     }
 }
 
+// Layers of the small networks' kind (contraction up to KF fragments, columns up to V of 16, or a few such tiles; a rank of up to 16), of any sizes, strides and
+// alignment: a wavefront takes SMALL_ROWS rows of one network by itself, the shared weights and the network's own in its registers, and makes h
+// and y at once: rows are read once, and nothing goes through memory between the two products.  Lanes hand each other h where they hold four of a row's values
+// as results and take eight as an operand (16 bits; in fp32 both are the same four).
+constexpr int SMALL_ROWS = 32, SMALL_WAVES = 4, SMALL_MOST = 128; // (the last: the widest)
+template <typename T, bool COLS, int KF, int V, bool ODD>
+__global__ void __launch_bounds__(SMALL_WAVES * 64) k_adapt_small(KnProduct p, Down down, Beside beside, int32_t pieces)
+{
+    constexpr int W = KnSmallFrag<T>::W, KS = KnSmallFrag<T>::KS, SUBS = SMALL_ROWS / 16, PAIR = W / 4, RUNS = V / PAIR;
+    typedef typename KnFrag<T>::Type Frag;
+    typedef T Run __attribute__((ext_vector_type(W), aligned(sizeof(T)))); // wherever they lie
+    typedef T Four __attribute__((ext_vector_type(4)));
+    __shared__ __align__(16) T rows_of[SMALL_WAVES][16 * 16 * V + W]; // 16 rows of results of a wavefront, as they follow one another
+    const int lane = kn_thread() & 63, col = lane & 15, g = lane >> 4;
+    T *line = rows_of[kn_thread() >> 6];
+    const int32_t number = __builtin_amdgcn_readfirstlane((p.first + kn_block()) * SMALL_WAVES + (kn_thread() >> 6));
+    const int ntiles = (p.J + 16 * V - 1) / (16 * V);
+    if (number / ntiles >= pieces) return;
+    const KnPiece piece = kn_find_piece(down.offsets, down.E, p.M, SMALL_ROWS, number / ntiles);
+    const int32_t j0 = number % ntiles * 16 * V;
+    if (piece.begin >= piece.end) return;
+    const bool some = piece.group < down.E;
+    const int64_t group = some ? piece.group : 0;
+    const int32_t C = p.C;
+    Frag fa[SUBS][KF], fb[KF][V], la[KF], lb[V];
+    bool there[SUBS];
+    const bool any = p.a_rows > 0;
+    // A lane's four results of W / 4 products are neighbours, W of them: the products' columns are dealt out in fours
+    auto column = [&](int v) { return min(j0 + v / PAIR * (16 * PAIR) + (col >> 2) * W + v % PAIR * 4 + (col & 3), p.J - 1); };
+    if (any) {
+        const T *arow[SUBS], *brow[V], *lrow = (const T *)down.b + group * down.b_group + min(col, down.rank - 1) * down.b_j;
+        uint32_t fifth_a[SUBS][KF], fifth_b[KF][V], fifth_l[KF];
+        const bool odd_a = ODD && (((uintptr_t)p.a / sizeof(T) | p.lda) & 1), odd_b = ODD && (((uintptr_t)p.b / sizeof(T) | p.b_j) & 1),
+                   odd_l = ODD && (((uintptr_t)down.b / sizeof(T) | down.b_j) & 1);
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) {
+            const int32_t i = min(piece.begin + 16 * s + col, piece.end - 1), src = p.rows ? p.rows[i] : i;
+            there[s] = (uint32_t)src < (uint32_t)p.a_rows;
+            arow[s] = (const T *)p.a + (int64_t)(there[s] ? src : 0) * p.lda;
+        }
+#pragma unroll
+        for (int k = 0; k < KF; ++k) {
+            const int32_t c = k * KS + g * W;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int32_t j = column(v);
+                if constexpr (COLS) {
+#pragma unroll
+                    for (int q = 0; q < W; ++q) {
+                        const T w = ((const T *)p.b)[min(c + q, C - 1) * p.b_c + j];
+                        fb[k][v][q] = c + q < C ? w : (T)0.0f;
+                    }
+                } else {
+                    brow[v] = (const T *)p.b + j * p.b_j;
+                    fb[k][v] = kn_row_ask<T>(brow[v], c, C, odd_b, fifth_b[k][v]);
+                }
+            }
+            if constexpr (COLS) la[k] = strided_piece<T>(lrow, down.b_c, c, C);
+            else la[k] = kn_row_ask<T>(lrow, c, C, odd_l, fifth_l[k]);
+        }
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s)
+#pragma unroll
+            for (int k = 0; k < KF; ++k) fa[s][k] = kn_row_ask<T>(arow[s], k * KS + g * W, C, odd_a, fifth_a[s][k]);
+        const T *b = (const T *)beside.b + group * beside.b_group;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int32_t j = column(v);
+            if constexpr (COLS) lb[v] = strided_piece<T>(b + j, beside.b_c, g * W, beside.rank);
+            else lb[v] = kn_any_piece<T>(b + j * beside.b_j, g * W, beside.rank);
+        }
+        if (C >= W && (ODD || C % W)) {
+#pragma unroll
+            for (int k = 0; k < KF; ++k) {
+                if (!ODD && (k + 1) * KS <= C) continue;
+                const int32_t c = k * KS + g * W;
+#pragma unroll
+                for (int s = 0; s < SUBS; ++s) kn_row_place<T>(fa[s][k], arow[s], c, C, odd_a, fifth_a[s][k]);
+                if constexpr (!COLS) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) kn_row_place<T>(fb[k][v], brow[v], c, C, odd_b, fifth_b[k][v]);
+                    kn_row_place<T>(la[k], lrow, c, C, odd_l, fifth_l[k]);
+                }
+            }
+        }
+    }
+    const float scale = some && down.scales ? down.scales[group] : 1.0f;
+    const bool together = p.J % W != 0 && ntiles == 1; // rows that follow one another without whole pieces of their own: stored as one line
+    // W neighbours j .. of a row of J (behind its end: the last one, unused)
+    auto run = [&](const T *row, int32_t j) {
+        Run f;
+        if (j + W <= p.J) f = *(const Run *)(row + j);
+        else
+#pragma unroll
+            for (int r = 0; r < W; ++r) f[r] = row[min(j + r, p.J - 1)];
+        return f;
+    };
+    const T *bias = (const T *)p.bias, *mask = (const T *)p.mask;
+    Run add[RUNS], m[SUBS][RUNS]; // (a lane's columns are j0 + 4 W n + W g .. + W - 1)
+#pragma unroll
+    for (int n = 0; n < RUNS; ++n) add[n] = bias ? run(bias, min(j0 + 4 * W * n + W * g, p.J - 1)) : Run{};
+    if (mask) { // (asked for before the first result is stored, not one after the other's)
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) {
+            const int32_t i = min(piece.begin + 16 * s + col, piece.end - 1), src = p.mask_rows ? p.mask_rows[i] : i;
+            const bool in = (uint32_t)src < (uint32_t)p.m_rows;
+#pragma unroll
+            for (int n = 0; n < RUNS; ++n) {
+                m[s][n] = Run{};
+                if (in) m[s][n] = run(mask + (int64_t)src * p.ldm, min(j0 + 4 * W * n + W * g, p.J - 1));
+            }
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
+        const int32_t i = piece.begin + 16 * s + col;
+        if (piece.begin + 16 * s >= piece.end) break;
+        kn_f32x4 acc[V] = {}, low = {0, 0, 0, 0};
+        if (any) {
+#pragma unroll
+            for (int k = 0; k < KF; ++k) {
+                low = kn_mfma(la[k], fa[s][k], low);
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[v] = kn_mfma(fb[k][v], fa[s][k], acc[v]);
+            }
+        }
+        Four h; // of row `col`: values 4 g .. + 3
+#pragma unroll
+        for (int r = 0; r < 4; ++r) h[r] = some && any && there[s] && 4 * g + r < down.rank ? (T)(scale * low[r]) : (T)0.0f;
+        if (j0 == 0 && i < piece.end && 4 * g < down.rp) *(Four *)((T *)down.h + (int64_t)i * down.rp + 4 * g) = h;
+        if (any) {
+            Frag hf;
+            if constexpr (sizeof(T) == 4) {
+                hf = h;
+            } else { // values 8 g .. + 7: those of lanes 2 g and 2 g + 1 of the row's four (behind the 16th: zeros, as B's are)
+                union { Four v; uint32_t u[2]; } mine;
+                union { Frag v; uint32_t u[4]; } all;
+                mine.v = h;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t v = __shfl(mine.u[q & 1], (2 * (g & 1) + (q >> 1)) * 16 + col);
+                    all.u[q] = g < 2 ? v : 0;
+                }
+                hf = all.v;
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) acc[v] = kn_mfma(lb[v], hf, acc[v]);
+            if (!there[s])
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[v] = kn_f32x4{0, 0, 0, 0};
+        }
+        T *out = (T *)p.out + (int64_t)i * p.o_i, *first = (T *)p.out + (int64_t)(i - col) * p.o_i;
+        const int shift = (int)((uintptr_t)first / sizeof(T) % W); // (of the first result in its 16 bytes)
+#pragma unroll
+        for (int n = 0; n < RUNS; ++n) {
+            const int32_t j = j0 + 4 * W * n + W * g;
+            if (j >= p.J || i >= piece.end) continue;
+            Run o;
+#pragma unroll
+            for (int r = 0; r < W; ++r) {
+                float y = acc[n * PAIR + r / 4][r % 4];
+                if (bias) y += (float)add[n][r];
+                if (p.relu) y = y > 0.0f || y != y ? y : 0.0f; // (a NaN stays one)
+                if (mask && !((float)m[s][n][r] > 0.0f)) y = 0.0f;
+                o[r] = (T)y;
+            }
+            if (together) {
+#pragma unroll
+                for (int r = 0; r < W; ++r)
+                    if (j + r < p.J) line[shift + col * p.J + j + r] = o[r];
+            } else if (j + W <= p.J) {
+                *(Run *)(out + j) = o;
+            } else {
+#pragma unroll
+                for (int r = 0; r < W; ++r)
+                    if (j + r < p.J) out[j + r] = o[r];
+            }
+        }
+        if (together) {
+            kn_lanes_meet();
+            const int end = shift + min(16, piece.end - (i - col)) * p.J;
+            for (int q = lane * W; q < end; q += 64 * W) {
+                if (q >= shift && q + W <= end) *(Frag *)(first + q - shift) = *(const Frag *)(line + q);
+                else
+                    for (int r = max(q, shift); r < min(q + W, end); ++r) first[r - shift] = line[r];
+            }
+            kn_lanes_meet();
+        }
+    }
+}
+
+template <typename T, bool COLS, int KF, int V, bool ODD> int launch_small_of(hipStream_t st, const Down &down, const KnProduct &p, const Beside &beside)
+{
+    const int64_t pieces = kn_pieces(p.M, down.E, SMALL_ROWS), waves = pieces * kn_div_up(p.J, 16 * V);
+    if (waves > 0x7fffffffLL) return KN_E_UNSUPPORTED;
+    return kn_launch(kn_div_up(waves, SMALL_WAVES), SMALL_WAVES * 64, [&](dim3 grid, int32_t first) {
+        KnProduct q = p;
+        q.first = first;
+        hipLaunchKernelGGL((k_adapt_small<T, COLS, KF, V, ODD>), grid, dim3(SMALL_WAVES * 64), 0, st, q, down, beside, (int32_t)pieces);
+    });
+}
+template <typename T, bool COLS, int KF, int V> int launch_small_v(hipStream_t st, const Down &down, const KnProduct &p, const Beside &beside)
+{
+    if constexpr (sizeof(T) == 2) { // rows that begin between two words
+        if (((uintptr_t)p.a / 2 | p.lda | (COLS ? 0 : (uintptr_t)p.b / 2 | p.b_j | (uintptr_t)down.b / 2 | down.b_j)) & 1) return launch_small_of<T, COLS, KF, V, true>(st, down, p, beside);
+    }
+    return launch_small_of<T, COLS, KF, V, false>(st, down, p, beside);
+}
+template <typename T, bool COLS> int launch_small(hipStream_t st, const Down &down, const KnProduct &p, const Beside &beside)
+{
+    const int kf = (p.C + KnSmallFrag<T>::KS - 1) / KnSmallFrag<T>::KS;
+    if constexpr (sizeof(T) == 4) {
+        if (kf > 4) return launch_small_v<T, COLS, 8, 2>(st, down, p, beside);
+        return p.J <= 32 ? launch_small_v<T, COLS, 4, 2>(st, down, p, beside) : launch_small_v<T, COLS, 4, 4>(st, down, p, beside);
+    } else {
+        if (kf > 2) return launch_small_v<T, COLS, 4, 4>(st, down, p, beside);
+        return p.J <= 32 ? launch_small_v<T, COLS, 2, 2>(st, down, p, beside) : launch_small_v<T, COLS, 2, 4>(st, down, p, beside);
+    }
+}
+
 template <typename T, int B, int U, int V, int WAVES, int AHEAD> int launch_down_of(hipStream_t st, const Down &p)
 {
     return kn_launch(kn_pieces(p.M, p.E, 16 * U) * kn_div_up(p.rp, 16 * V), WAVES * 64, [&](dim3 grid, int32_t first) {
@@ -639,31 +842,34 @@ template <typename T, bool COLS> int launch_up(hipStream_t st, const KnProduct &
         return narrow ? launch_tiles<T, COLS, true, 32, 64, 1, 4, 4>(st, p, beside) : launch_tiles<T, COLS, true, 64, 128, 1, 4, 2>(st, p, beside);
     } else {
         if (!direct) return narrow ? launch_tiles<T, COLS, false, 32, 64, 1, 4, 2>(st, p, beside) : launch_tiles<T, COLS, false, 128, 128, 2, 4, 2>(st, p, beside);
-        if (narrow) return launch_tiles<T, COLS, true, 32, 64, 1, 4, 4>(st, p, beside);
-        if (tiles(128) >= 256) return launch_tiles<T, COLS, true, 128, 128, 2, 4, 2>(st, p, beside);
-        return launch_tiles<T, COLS, true, 64, 128, 1, 4, 2>(st, p, beside);
+        if (p.J > 64 && tiles(128) >= 384) return launch_tiles<T, COLS, true, 128, 128, 2, 4, 2>(st, p, beside);
+        if (p.J > 64 && tiles(64) >= 256) return launch_tiles<T, COLS, true, 64, 128, 1, 4, 3>(st, p, beside);
+        if (kn_div_up(p.M, 64) * kn_div_up(p.J, 64) >= 256) return launch_tiles<T, COLS, true, 64, 64, 2, 2, 4>(st, p, beside);
+        return launch_tiles<T, COLS, true, 32, 64, 1, 4, 4>(st, p, beside);
     }
 }
 
-// How few rows' product is cut: columns of a workgroup, parts of the contraction until there are workgroups for the chip, no part of less than a step per wavefront
-Few few_of(int64_t M, int32_t J, int32_t C, int item, int columns)
+// How few rows' product is cut: up to 16 rows by 16 columns, more by 32, and the contraction until there are 128 workgroups, in no part of less than a step per
+// wavefront.  Measured (us; one row 2048 x 2048, 48 rows 2048 x 2560 with 32 networks, bf16, both launches): 16 columns, 128 workgroups 9.1, 16.2; 32
+// columns, 128 10.0, 14.2; 32, 256 12.4, 15.9; 32, 512 15.1, 20.5; 64, 128 11.2, 14.8.
+int few_columns(int64_t M) { return M <= 16 ? 16 : 32; }
+Few few_of(int64_t M, int32_t J, int32_t C, int item)
 {
     Few f = {};
-    const int64_t tiles = kn_div_up(J, columns), steps = kn_div_up(C, 64 / item);
-    int64_t parts = kn_div_up(256, tiles);
+    const int64_t tiles = kn_div_up(J, few_columns(M)), steps = kn_div_up(C, 64 / item);
+    int64_t parts = kn_div_up(128, tiles);
     if (parts > kn_div_up(steps, 8)) parts = kn_div_up(steps, 8);
     f.each = (int32_t)kn_div_up(steps, parts);
     f.parts = (int32_t)kn_div_up(steps, f.each);
     f.products = (int32_t)(tiles * f.parts);
     return f;
 }
-constexpr int FEW_V = 2;
-int64_t few_bytes(int64_t M, int32_t J, int32_t C, int item) { return M > FEW_ROWS ? 0 : kn_align_up(few_of(M, J, C, item, 16 * FEW_V).parts * M * J * 4, 256); }
+int64_t few_bytes(int64_t M, int32_t J, int32_t C, int item) { return M > FEW_ROWS ? 0 : kn_align_up(few_of(M, J, C, item).parts * M * J * 4, 256); }
 
 template <typename T, int B, int U, int DOWN_V> int launch_few_of(hipStream_t st, const Down &down, const KnProduct &p, const Few &few)
 {
     const int64_t blocks = few.products + kn_pieces(down.M, down.E, 16) * kn_div_up(down.rp, 16 * DOWN_V);
-    hipLaunchKernelGGL((k_adapt_few<T, B, U, FEW_V, DOWN_V>), dim3((unsigned)blocks), dim3(512), 0, st, p, down, few);
+    hipLaunchKernelGGL((k_adapt_few<T, B, U, U == 1 ? 1 : 2, DOWN_V>), dim3((unsigned)blocks), dim3(512), 0, st, p, down, few);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }
@@ -686,7 +892,7 @@ template <typename T> int launch_few_b(hipStream_t st, const Down &down, const K
 }
 template <typename T> int launch_few(hipStream_t st, const Down &down, const KnProduct &p, const Beside &beside, bool cols, float *sums)
 {
-    Few few = few_of(p.M, p.J, p.C, sizeof(T), 16 * FEW_V);
+    Few few = few_of(p.M, p.J, p.C, sizeof(T));
     few.sums = sums;
     KN_TRY(launch_few_b<T>(st, down, p, few, cols));
     hipLaunchKernelGGL((k_adapt_few_join<T>), dim3((unsigned)kn_div_up((int64_t)p.M * kn_div_up(p.J, 4), 128)), dim3(128), 0, st, p, beside, few);
@@ -702,6 +908,8 @@ int run(hipStream_t st, int32_t dtype, bool cols, const Down &down, const KnProd
         typedef decltype(v) E_;
         // (very many networks of a very large rank: the other way's launches are cut)
         if (up.M <= FEW_ROWS && down.E * (int64_t)down.rp <= 1 << 24) return launch_few<E_>(st, down, up, beside, cols, sums);
+        if (up.C <= SMALL_MOST && up.J <= SMALL_MOST && down.rp <= 16)
+            return cols ? launch_small<E_, true>(st, down, up, beside) : launch_small<E_, false>(st, down, up, beside);
         KN_TRY(launch_down<E_>(st, down, cols));
         return cols && up.b_c != 1 ? launch_up<E_, true>(st, up, beside) : launch_up<E_, false>(st, up, beside);
     });

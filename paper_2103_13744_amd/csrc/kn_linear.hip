@@ -220,53 +220,10 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p)
 // a third more lines than they fill; 44 us where each odd end is waited for); 524,291 rows, 64 x 64 in fp16, input gradient with a ReLU's mask: 59 us, 4.0 TB/s (68 where a
 // lane stores and masks 8 bytes at a time).  Pieces of 64 rows: 49 and 69, of 128: 70 and 90, of 16: 52 and 85.
 constexpr int SMALL_ROWS = 32, SMALL_WAVES = 4;
-template <typename T> struct SmallFrag {
-    static constexpr int W = 16 / sizeof(T), KS = 4 * W;
-};
-// kn_any_piece in two parts, so that nothing waits for a fetch before all are under way: a piece that ends behind the row is fetched from
-// its last 16 bytes, and shifted to its place at the end.  `odd`: 16-bit rows may begin between two words, where a fetch of 16 bytes is
-// several times as slow: the words that the piece lies in are fetched (five; each holds a value of the piece, so that no more than the other
-// half of a word of the row's is read beside it, and shifted out) and joined at the end
-// (524,291 rows, 4,096 networks 63 x 32 in bf16: 50 -> 40 us, with weights whose rows are 63 values 60 -> 35).
-template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type small_ask(const T *row, int32_t k, int32_t C, bool odd, uint32_t &fifth)
-{
-    constexpr int W = SmallFrag<T>::W;
-    if (C < W) return kn_any_piece<T>(row, k, C);
-    typename KnFrag<T>::Type f = {};
-    fifth = 0;
-    if (k < C) {
-        const T *at = row + min(k, C - W);
-        if (sizeof(T) == 2 && odd) {
-            const uintptr_t word = ~(uintptr_t)3;
-            f = *(const typename KnAny<T>::Words *)((uintptr_t)at & word);
-            fifth = *(const uint32_t *)(((uintptr_t)at + 14) & word);
-        } else {
-            f = *(const typename KnAny<T>::Piece *)at;
-        }
-    }
-    return f;
-}
-template <typename T>
-__device__ __forceinline__ void small_place(typename KnFrag<T>::Type &f, const T *row, int32_t k, int32_t C, bool odd, uint32_t fifth)
-{
-    constexpr int W = SmallFrag<T>::W;
-    kn_u32x4 d = __builtin_bit_cast(kn_u32x4, f);
-    if (sizeof(T) == 2 && odd) {
-        const uint32_t low = (uint32_t)(uintptr_t)(row + min(k, C - W)) & 2;
-        d = kn_u32x4{__builtin_amdgcn_alignbyte(d[1], d[0], low), __builtin_amdgcn_alignbyte(d[2], d[1], low), __builtin_amdgcn_alignbyte(d[3], d[2], low),
-                     __builtin_amdgcn_alignbyte(fifth, d[3], low)};
-    }
-    const kn_u32x4 whole = d;
-    const int bytes = (W - C % W) % W * (int)sizeof(T); // alike for all lanes
-    if (bytes & 2) d = kn_u32x4{d[0] >> 16 | d[1] << 16, d[1] >> 16 | d[2] << 16, d[2] >> 16 | d[3] << 16, d[3] >> 16};
-    if (bytes & 4) d = kn_u32x4{d[1], d[2], d[3], 0};
-    if (bytes & 8) d = kn_u32x4{d[2], d[3], 0, 0};
-    f = __builtin_bit_cast(typename KnFrag<T>::Type, k < C && k + W > C ? d : whole);
-}
 template <typename T, bool COLS, int KF, int V, bool ODD>
 __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p, int32_t pieces)
 {
-    constexpr int W = SmallFrag<T>::W, KS = SmallFrag<T>::KS, SUBS = SMALL_ROWS / 16;
+    constexpr int W = KnSmallFrag<T>::W, KS = KnSmallFrag<T>::KS, SUBS = SMALL_ROWS / 16;
     // A lane's four results of W / 4 products are neighbours, W of them: the products' columns are dealt out in fours
     constexpr int PAIR = W / 4, RUNS = V / PAIR;
     typedef typename KnFrag<T>::Type Frag;
@@ -310,22 +267,22 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
                     }
                 } else {
                     brow[v] = b + (int64_t)j * p.b_j;
-                    fb[k][v] = small_ask<T>(brow[v], c, C, odd_b, fifth_b[k][v]);
+                    fb[k][v] = kn_row_ask<T>(brow[v], c, C, odd_b, fifth_b[k][v]);
                 }
             }
 #pragma unroll
         for (int s = 0; s < SUBS; ++s)
 #pragma unroll
-            for (int k = 0; k < KF; ++k) fa[s][k] = small_ask<T>(arow[s], k * KS + g * W, C, odd_a, fifth_a[s][k]);
+            for (int k = 0; k < KF; ++k) fa[s][k] = kn_row_ask<T>(arow[s], k * KS + g * W, C, odd_a, fifth_a[s][k]);
         if (C >= W && (ODD || C % W)) {
 #pragma unroll
             for (int k = 0; k < KF; ++k) {
                 if (!ODD && (k + 1) * KS <= C) continue;
 #pragma unroll
-                for (int s = 0; s < SUBS; ++s) small_place<T>(fa[s][k], arow[s], k * KS + g * W, C, odd_a, fifth_a[s][k]);
+                for (int s = 0; s < SUBS; ++s) kn_row_place<T>(fa[s][k], arow[s], k * KS + g * W, C, odd_a, fifth_a[s][k]);
                 if constexpr (!COLS)
 #pragma unroll
-                    for (int v = 0; v < V; ++v) small_place<T>(fb[k][v], brow[v], k * KS + g * W, C, odd_b, fifth_b[k][v]);
+                    for (int v = 0; v < V; ++v) kn_row_place<T>(fb[k][v], brow[v], k * KS + g * W, C, odd_b, fifth_b[k][v]);
             }
         }
     }
@@ -525,7 +482,7 @@ template <typename T, bool COLS, int KF, int V> int launch_small(hipStream_t st,
 constexpr int SMALL_MOST = 128; // widest contraction and most columns that k_product_small takes
 template <typename T, bool COLS> int launch_small_widths(hipStream_t st, const KnProduct &p)
 {
-    const int kf = (p.C + SmallFrag<T>::KS - 1) / SmallFrag<T>::KS;
+    const int kf = (p.C + KnSmallFrag<T>::KS - 1) / KnSmallFrag<T>::KS;
     if constexpr (sizeof(T) == 4) {
         if (kf > 4) return launch_small<T, COLS, 8, 2>(st, p);
         if (kf > 2) return p.J <= 32 ? launch_small<T, COLS, 4, 2>(st, p) : launch_small<T, COLS, 4, 4>(st, p);

@@ -115,6 +115,49 @@ template <typename T> struct KnEight {
     }
 };
 
+template <typename T> struct KnSmallFrag {
+    static constexpr int W = 16 / sizeof(T), KS = 4 * W;
+};
+// kn_any_piece in two parts, so that nothing waits for a fetch before all are under way: a piece that ends behind the row is fetched from
+// its last 16 bytes, and shifted to its place at the end.  `odd`: 16-bit rows may begin between two words, where a fetch of 16 bytes is
+// several times as slow: the words that the piece lies in are fetched (five; each holds a value of the piece, so that no more than the other
+// half of a word of the row's is read beside it, and shifted out) and joined at the end
+// (524,291 rows, 4,096 networks 63 x 32 in bf16: 50 -> 40 us, with weights whose rows are 63 values 60 -> 35).
+template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type kn_row_ask(const T *row, int32_t k, int32_t C, bool odd, uint32_t &fifth)
+{
+    constexpr int W = KnSmallFrag<T>::W;
+    if (C < W) return kn_any_piece<T>(row, k, C);
+    typename KnFrag<T>::Type f = {};
+    fifth = 0;
+    if (k < C) {
+        const T *at = row + min(k, C - W);
+        if (sizeof(T) == 2 && odd) {
+            const uintptr_t word = ~(uintptr_t)3;
+            f = *(const typename KnAny<T>::Words *)((uintptr_t)at & word);
+            fifth = *(const uint32_t *)(((uintptr_t)at + 14) & word);
+        } else {
+            f = *(const typename KnAny<T>::Piece *)at;
+        }
+    }
+    return f;
+}
+template <typename T>
+__device__ __forceinline__ void kn_row_place(typename KnFrag<T>::Type &f, const T *row, int32_t k, int32_t C, bool odd, uint32_t fifth)
+{
+    constexpr int W = KnSmallFrag<T>::W;
+    kn_u32x4 d = __builtin_bit_cast(kn_u32x4, f);
+    if (sizeof(T) == 2 && odd) {
+        const uint32_t low = (uint32_t)(uintptr_t)(row + min(k, C - W)) & 2;
+        d = kn_u32x4{__builtin_amdgcn_alignbyte(d[1], d[0], low), __builtin_amdgcn_alignbyte(d[2], d[1], low), __builtin_amdgcn_alignbyte(d[3], d[2], low),
+                     __builtin_amdgcn_alignbyte(fifth, d[3], low)};
+    }
+    const kn_u32x4 whole = d;
+    const int bytes = (W - C % W) % W * (int)sizeof(T); // alike for all lanes
+    if (bytes & 2) d = kn_u32x4{d[0] >> 16 | d[1] << 16, d[1] >> 16 | d[2] << 16, d[2] >> 16 | d[3] << 16, d[3] >> 16};
+    if (bytes & 4) d = kn_u32x4{d[1], d[2], d[3], 0};
+    if (bytes & 8) d = kn_u32x4{d[2], d[3], 0, 0};
+    f = __builtin_bit_cast(typename KnFrag<T>::Type, k < C && k + W > C ? d : whole);
+}
 // What is added to columns j .. j + 7 of a network's results (j a multiple of 8)
 template <typename T> __device__ __forceinline__ void kn_bias_of(const KnProduct &p, bool some, int64_t group, int32_t j, float add[8])
 {
