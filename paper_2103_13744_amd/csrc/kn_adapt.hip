@@ -574,8 +574,8 @@ __global__ void __launch_bounds__(WR * WC * 64) k_adapt_up(KnProduct p, Beside b
 }
 
 // Layers of the small networks' kind (contraction up to KF fragments, columns up to V of 16, or a few such tiles; a rank of up to 16), of any sizes, strides and
-// alignment: a wavefront takes SMALL_ROWS rows of one network by itself, the shared weights and the network's own in its registers, and makes h
-// and y at once: rows are read once, and nothing goes through memory between the two products.  Lanes hand each other h where they hold four of a row's values
+// alignment: a wavefront takes SMALL_ROWS rows of one network by itself, the shared weights in the LDS, as fragments, and the network's own in its registers, and
+// makes h and y at once: rows are read once, and nothing goes through memory between the two products.  Lanes hand each other h where they hold four of a row's values
 // as results and take eight as an operand (16 bits; in fp32 both are the same four).
 constexpr int SMALL_ROWS = 32, SMALL_WAVES = 4, SMALL_MOST = 128; // (the last: the widest)
 template <typename T, bool COLS, int KF, int V, bool ODD>
@@ -587,26 +587,40 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_adapt_small(KnProduct p, D
     typedef T Four __attribute__((ext_vector_type(4)));
     __shared__ __align__(16) T rows_of[SMALL_WAVES][16 * 16 * V + W]; // 16 rows of results of a wavefront, as they follow one another
     const int lane = kn_thread() & 63, col = lane & 15, g = lane >> 4;
-    T *line = rows_of[kn_thread() >> 6];
-    const int32_t number = __builtin_amdgcn_readfirstlane((p.first + kn_block()) * SMALL_WAVES + (kn_thread() >> 6));
-    const int ntiles = (p.J + 16 * V - 1) / (16 * V);
-    if (number / ntiles >= pieces) return;
-    const KnPiece piece = kn_find_piece(down.offsets, down.E, p.M, SMALL_ROWS, number / ntiles);
-    const int32_t j0 = number % ntiles * 16 * V;
-    if (piece.begin >= piece.end) return;
-    const bool some = piece.group < down.E;
-    const int64_t group = some ? piece.group : 0;
-    const int32_t C = p.C;
-    Frag fa[SUBS][KF], fb[KF][V], la[KF], lb[V];
-    bool there[SUBS];
+    __shared__ __align__(16) Frag shared[KF][V][64];
+    const int wave = __builtin_amdgcn_readfirstlane(kn_thread() >> 6);
+    T *line = rows_of[wave];
+    const int ntiles = (p.J + 16 * V - 1) / (16 * V), block = p.first + kn_block();
+    const int32_t number = block / ntiles * SMALL_WAVES + wave, j0 = block % ntiles * 16 * V, C = p.C;
     const bool any = p.a_rows > 0;
     // A lane's four results of W / 4 products are neighbours, W of them: the products' columns are dealt out in fours
     auto column = [&](int v) { return min(j0 + v / PAIR * (16 * PAIR) + (col >> 2) * W + v % PAIR * 4 + (col & 3), p.J - 1); };
+#pragma unroll
+    for (int f = 0; f < KF * V / SMALL_WAVES; ++f) {
+        const int n = f * SMALL_WAVES + wave, k = n / V, v = n % V;
+        const int32_t c = k * KS + g * W, j = column(v);
+        Frag w;
+        if constexpr (COLS) {
+            w = strided_piece<T>((const T *)p.b + j, p.b_c, c, C);
+        } else {
+            uint32_t fifth = 0;
+            const bool odd = ODD && (((uintptr_t)p.b / sizeof(T) | p.b_j) & 1);
+            w = kn_row_ask<T>((const T *)p.b + j * p.b_j, c, C, odd, fifth);
+            if (C >= W) kn_row_place<T>(w, (const T *)p.b + j * p.b_j, c, C, odd, fifth);
+        }
+        shared[k][v][lane] = w;
+    }
+    const KnPiece piece = number < pieces ? kn_find_piece(down.offsets, down.E, p.M, SMALL_ROWS, number) : KnPiece{0, 0, 0};
+    __syncthreads();
+    if (piece.begin >= piece.end) return;
+    const bool some = piece.group < down.E;
+    const int64_t group = some ? piece.group : 0;
+    Frag fa[SUBS][KF], la[KF], lb[V];
+    bool there[SUBS];
     if (any) {
-        const T *arow[SUBS], *brow[V], *lrow = (const T *)down.b + group * down.b_group + min(col, down.rank - 1) * down.b_j;
-        uint32_t fifth_a[SUBS][KF], fifth_b[KF][V], fifth_l[KF];
-        const bool odd_a = ODD && (((uintptr_t)p.a / sizeof(T) | p.lda) & 1), odd_b = ODD && (((uintptr_t)p.b / sizeof(T) | p.b_j) & 1),
-                   odd_l = ODD && (((uintptr_t)down.b / sizeof(T) | down.b_j) & 1);
+        const T *arow[SUBS], *lrow = (const T *)down.b + group * down.b_group + min(col, down.rank - 1) * down.b_j;
+        uint32_t fifth_a[SUBS][KF], fifth_l[KF];
+        const bool odd_a = ODD && (((uintptr_t)p.a / sizeof(T) | p.lda) & 1), odd_l = ODD && (((uintptr_t)down.b / sizeof(T) | down.b_j) & 1);
 #pragma unroll
         for (int s = 0; s < SUBS; ++s) {
             const int32_t i = min(piece.begin + 16 * s + col, piece.end - 1), src = p.rows ? p.rows[i] : i;
@@ -616,20 +630,6 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_adapt_small(KnProduct p, D
 #pragma unroll
         for (int k = 0; k < KF; ++k) {
             const int32_t c = k * KS + g * W;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int32_t j = column(v);
-                if constexpr (COLS) {
-#pragma unroll
-                    for (int q = 0; q < W; ++q) {
-                        const T w = ((const T *)p.b)[min(c + q, C - 1) * p.b_c + j];
-                        fb[k][v][q] = c + q < C ? w : (T)0.0f;
-                    }
-                } else {
-                    brow[v] = (const T *)p.b + j * p.b_j;
-                    fb[k][v] = kn_row_ask<T>(brow[v], c, C, odd_b, fifth_b[k][v]);
-                }
-            }
             if constexpr (COLS) la[k] = strided_piece<T>(lrow, down.b_c, c, C);
             else la[k] = kn_row_ask<T>(lrow, c, C, odd_l, fifth_l[k]);
         }
@@ -651,11 +651,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_adapt_small(KnProduct p, D
                 const int32_t c = k * KS + g * W;
 #pragma unroll
                 for (int s = 0; s < SUBS; ++s) kn_row_place<T>(fa[s][k], arow[s], c, C, odd_a, fifth_a[s][k]);
-                if constexpr (!COLS) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) kn_row_place<T>(fb[k][v], brow[v], c, C, odd_b, fifth_b[k][v]);
-                    kn_row_place<T>(la[k], lrow, c, C, odd_l, fifth_l[k]);
-                }
+                if constexpr (!COLS) kn_row_place<T>(la[k], lrow, c, C, odd_l, fifth_l[k]);
             }
         }
     }
@@ -686,19 +682,26 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_adapt_small(KnProduct p, D
             }
         }
     }
+    kn_f32x4 sums[SUBS][V] = {}, lows[SUBS] = {};
+    if (any) {
+#pragma unroll
+        for (int k = 0; k < KF; ++k) {
+#pragma unroll
+            for (int s = 0; s < SUBS; ++s) lows[s] = kn_mfma(la[k], fa[s][k], lows[s]);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const Frag w = shared[k][v][lane];
+#pragma unroll
+                for (int s = 0; s < SUBS; ++s) sums[s][v] = kn_mfma(w, fa[s][k], sums[s][v]);
+            }
+        }
+    }
 #pragma unroll
     for (int s = 0; s < SUBS; ++s) {
         const int32_t i = piece.begin + 16 * s + col;
         if (piece.begin + 16 * s >= piece.end) break;
-        kn_f32x4 acc[V] = {}, low = {0, 0, 0, 0};
-        if (any) {
-#pragma unroll
-            for (int k = 0; k < KF; ++k) {
-                low = kn_mfma(la[k], fa[s][k], low);
-#pragma unroll
-                for (int v = 0; v < V; ++v) acc[v] = kn_mfma(fb[k][v], fa[s][k], acc[v]);
-            }
-        }
+        kn_f32x4 *acc = sums[s];
+        const kn_f32x4 low = lows[s];
         Four h; // of row `col`: values 4 g .. + 3
 #pragma unroll
         for (int r = 0; r < 4; ++r) h[r] = some && any && there[s] && 4 * g + r < down.rank ? (T)(scale * low[r]) : (T)0.0f;
@@ -766,9 +769,8 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_adapt_small(KnProduct p, D
 
 template <typename T, bool COLS, int KF, int V, bool ODD> int launch_small_of(hipStream_t st, const Down &down, const KnProduct &p, const Beside &beside)
 {
-    const int64_t pieces = kn_pieces(p.M, down.E, SMALL_ROWS), waves = pieces * kn_div_up(p.J, 16 * V);
-    if (waves > 0x7fffffffLL) return KN_E_UNSUPPORTED;
-    return kn_launch(kn_div_up(waves, SMALL_WAVES), SMALL_WAVES * 64, [&](dim3 grid, int32_t first) {
+    const int64_t pieces = kn_pieces(p.M, down.E, SMALL_ROWS);
+    return kn_launch(kn_div_up(pieces, SMALL_WAVES) * kn_div_up(p.J, 16 * V), SMALL_WAVES * 64, [&](dim3 grid, int32_t first) {
         KnProduct q = p;
         q.first = first;
         hipLaunchKernelGGL((k_adapt_small<T, COLS, KF, V, ODD>), grid, dim3(SMALL_WAVES * 64), 0, st, q, down, beside, (int32_t)pieces);
