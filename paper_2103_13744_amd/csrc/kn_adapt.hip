@@ -573,6 +573,21 @@ __global__ void __launch_bounds__(WR * WC * 64) k_adapt_up(KnProduct p, Beside b
     }
 }
 
+// strided_piece of a small matrix (less than 4 GiB) at an address that all lanes share: offsets of 32 bits, one addition for a value.  `at`: of the lane's first
+// value; `step`: bytes from one to the next
+template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type strided_near(const T *base, uint32_t at, uint32_t step, int32_t k, int32_t C, bool tail)
+{
+    typename KnFrag<T>::Type f;
+    uint32_t off = at + (uint32_t)k * step;
+    const uint32_t last = at + (uint32_t)(C - 1) * step;
+#pragma unroll
+    for (int q = 0; q < 16 / (int)sizeof(T); ++q, off += step) f[q] = *(const T *)((const char *)base + min(off, last));
+    if (tail)
+#pragma unroll
+        for (int q = 0; q < 16 / (int)sizeof(T); ++q) f[q] = k + q < C ? f[q] : (T)0.0f;
+    return f;
+}
+
 // Layers of the small networks' kind (contraction up to KF fragments, columns up to V of 16, or a few such tiles; a rank of up to 16), of any sizes, strides and
 // alignment: a wavefront takes SMALL_ROWS rows of one network by itself, the shared weights in the LDS, as fragments, and the network's own in its registers, and
 // makes h and y at once: rows are read once, and nothing goes through memory between the two products.  Lanes hand each other h where they hold four of a row's values
@@ -601,7 +616,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_adapt_small(KnProduct p, D
         const int32_t c = k * KS + g * W, j = column(v);
         Frag w;
         if constexpr (COLS) {
-            w = strided_piece<T>((const T *)p.b + j, p.b_c, c, C);
+            w = strided_near<T>((const T *)p.b, j * sizeof(T), (uint32_t)p.b_c * sizeof(T), c, C, (k + 1) * KS > C);
         } else {
             uint32_t fifth = 0;
             const bool odd = ODD && (((uintptr_t)p.b / sizeof(T) | p.b_j) & 1);
@@ -630,7 +645,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_adapt_small(KnProduct p, D
 #pragma unroll
         for (int k = 0; k < KF; ++k) {
             const int32_t c = k * KS + g * W;
-            if constexpr (COLS) la[k] = strided_piece<T>(lrow, down.b_c, c, C);
+            if constexpr (COLS) la[k] = strided_near<T>((const T *)down.b + group * down.b_group, min(col, down.rank - 1) * sizeof(T), (uint32_t)down.b_c * sizeof(T), c, C, (k + 1) * KS > C);
             else la[k] = kn_row_ask<T>(lrow, c, C, odd_l, fifth_l[k]);
         }
 #pragma unroll
@@ -641,7 +656,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_adapt_small(KnProduct p, D
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int32_t j = column(v);
-            if constexpr (COLS) lb[v] = strided_piece<T>(b + j, beside.b_c, g * W, beside.rank);
+            if constexpr (COLS) lb[v] = strided_near<T>(b, j * sizeof(T), (uint32_t)beside.b_c * sizeof(T), g * W, beside.rank, true);
             else lb[v] = kn_any_piece<T>(b + j * beside.b_j, g * W, beside.rank);
         }
         if (C >= W && (ODD || C % W)) {
