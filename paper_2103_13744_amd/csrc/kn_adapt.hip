@@ -44,13 +44,6 @@ template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type stride
 // for while another is multiplied, and are summed in the order of their numbers.  Where b's columns are contiguous (not its contraction) and in whole 16-byte
 // pieces, 16-bit values are turned by the transposing read of an LDS that each wavefront has for itself; else they are fetched one by one, eight for a fragment.
 enum { B_ROWS, B_COLS, B_PIECES };
-// Where row r of a step's 32 rows of 16 V columns, and its piece, lie: the 4 x 4 rows of a transposing read are spread over all banks
-template <int V> __device__ __forceinline__ int turned_byte(int r, int piece)
-{
-    if constexpr (V == 1) return (r ^ (r >> 3 & 1) << 2) * 32 + piece * 16;
-    else if constexpr (V == 2) return r * 64 + (piece ^ (r >> 3 & 1) << 1) * 16;
-    else return r * 128 + (piece ^ ((r >> 1 & 1) | (r >> 3 & 1) << 1) << 1) * 16;
-}
 template <typename T, int B, int U, int V, int WAVES, int AHEAD> struct Sums {
     static constexpr int W = 16 / sizeof(T), KS = 4 * W, LD = 16 * V + 4, WORDS = WAVES * 16 * U * LD;
     static constexpr bool COLS = B == B_COLS, TURN_B = B == B_PIECES;
@@ -105,16 +98,10 @@ template <typename T, int B, int U, int V, int WAVES, int AHEAD> struct Sums {
                 }
                 if constexpr (TURN_B) {
 #pragma unroll
-                    for (int v = 0; v < V; ++v) *(KN_LDS Frag *)(turn + turned_byte<V>((lane + 64 * v) / (2 * V), (lane + 64 * v) % (2 * V))) = x.b[n][v];
+                    for (int v = 0; v < V; ++v) *(KN_LDS Frag *)(turn + kn_turned_byte<V>((lane + 64 * v) / (2 * V), (lane + 64 * v) % (2 * V))) = x.b[n][v];
                     kn_lanes_meet();
 #pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        union { kn_s16x4 h[2]; Frag f; } t;
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            t.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KN_LDS kn_s16x4 *)(turn + turned_byte<V>(8 * g + 4 * h + (col >> 2), 2 * v + (col >> 1 & 1)) + (col & 1) * 8));
-                        x.b[n][v] = t.f;
-                    }
+                    for (int v = 0; v < V; ++v) x.b[n][v] = __builtin_bit_cast(Frag, kn_turned_frag<V>(turn, v, lane));
                     kn_lanes_meet();
                 }
 #pragma unroll
@@ -848,11 +835,35 @@ template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, in
     });
 }
 
-template <typename T, bool COLS> int launch_up(hipStream_t st, const KnProduct &p, const Beside &beside)
+// Whether the rows of all operands are made of whole 16-byte pieces
+template <typename T, bool COLS> bool rows_of_pieces(const KnProduct &p, const Beside &beside)
 {
     constexpr int64_t W = 16 / sizeof(T);
+    return (((uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)beside.b) & 15) == 0 && p.C % W == 0 && p.lda % W == 0 && (COLS ? p.J % W == 0 : beside.rank % W == 0);
+}
+// Layers of up to 128 x 128 and a rank of up to 16: by a wavefront per 32 rows (small), or the two kernels (us, small / tiles; rank 8, columns contiguous):
+//   rows, networks         262,144, 4,096   262,144, 64   20,000, 4,096   2,000, 500
+//   fp32   64 x 64               84/96          64/83          31/21          9/11
+//          128 x 64             133/130        101/122         49/27         13/13
+//          64 x 128             157/116        117/108         52/34         12/11
+//          128 x 128            238/167        187/153         86/43         18/13
+//   fp16   64 x 64               30/50          25/47          13/14          6/9
+//          128 x 64              47/62          35/56          18/16          7/9
+//          64 x 128              53/48          40/44          19/17          6/9
+//          128 x 128             93/65          63/56          29/18          7/9
+// and 262,145 rows of 1,600 networks 91 x 64 in bf16, which are not whole pieces, 41/78.
+template <typename T> bool small_layer(const KnProduct &p, const Down &down, bool pieces)
+{
+    if (p.C > SMALL_MOST || p.J > SMALL_MOST || down.rp > 16) return false;
+    if (!pieces) return true;
+    if (p.M <= 8192) return sizeof(T) == 2 || p.J <= 64;
+    return p.J <= 64 && p.M / down.E >= 16 && (sizeof(T) == 2 || p.C <= 64);
+}
+
+template <typename T, bool COLS> int launch_up(hipStream_t st, const KnProduct &p, const Beside &beside)
+{
     auto tiles = [&](int64_t bm) { return (p.M + bm - 1) / bm * ((p.J + 127) / 128); };
-    const bool direct = (((uintptr_t)p.a | (uintptr_t)p.b | (uintptr_t)beside.b) & 15) == 0 && p.C % W == 0 && p.lda % W == 0 && (COLS ? p.J % W == 0 : beside.rank % W == 0);
+    const bool direct = rows_of_pieces<T, COLS>(p, beside);
     const bool narrow = p.J <= 64 || tiles(64) < 256;
     if constexpr (sizeof(T) == 4) {
         if (!direct) return narrow ? launch_tiles<T, COLS, false, 32, 64, 1, 4, 2>(st, p, beside) : launch_tiles<T, COLS, false, 64, 128, 1, 4, 2>(st, p, beside);
@@ -925,7 +936,7 @@ int run(hipStream_t st, int32_t dtype, bool cols, const Down &down, const KnProd
         typedef decltype(v) E_;
         // (very many networks of a very large rank: the other way's launches are cut)
         if (up.M <= FEW_ROWS && down.E * (int64_t)down.rp <= 1 << 24) return launch_few<E_>(st, down, up, beside, cols, sums);
-        if (up.C <= SMALL_MOST && up.J <= SMALL_MOST && down.rp <= 16)
+        if (small_layer<E_>(up, down, cols ? rows_of_pieces<E_, true>(up, beside) : rows_of_pieces<E_, false>(up, beside)))
             return cols ? launch_small<E_, true>(st, down, up, beside) : launch_small<E_, false>(st, down, up, beside);
         KN_TRY(launch_down<E_>(st, down, cols));
         return cols && up.b_c != 1 ? launch_up<E_, true>(st, up, beside) : launch_up<E_, false>(st, up, beside);
@@ -952,8 +963,8 @@ int dw_bytes(const kn_linear_desc *d, int32_t rank, int64_t *out)
 {
     const kn_linear_desc a = layer_of(d, d->n_in, rank, d->x_rows, d->ldx), b = layer_of(d, rank, d->n_out, d->rows, padded_rank(d->dtype, rank));
     int64_t na = 0, nb = 0;
-    KN_TRY(kn_grouped_linear_dw_workspace_bytes(&a, &na));
-    KN_TRY(kn_grouped_linear_dw_workspace_bytes(&b, &nb));
+    KN_TRY(kn_linear_dw_bytes(&a, true, &na));
+    KN_TRY(kn_linear_dw_bytes(&b, true, &nb));
     const int64_t few = few_bytes(d->rows, d->n_in, d->n_out, kn_item(d->dtype)); // (done with before the others begin)
     *out = na > nb ? na : nb;
     *out = few > *out ? few : *out;
@@ -1030,6 +1041,6 @@ extern "C" int kn_adapted_linear_backward(void *stream, const kn_linear_desc *d,
         KN_TRY(run((hipStream_t)stream, d->dtype, !io, down, p, beside, (float *)sums));
     }
     const kn_linear_desc la = layer_of(d, d->n_in, rank, d->x_rows, d->ldx), lb = layer_of(d, rank, d->n_out, d->rows, rp);
-    KN_TRY(kn_linear_dw_run(stream, &la, x, nullptr, g, rp, offsets, rows, da, nullptr, sums, dw));
-    return kn_linear_dw_run(stream, &lb, h, nullptr, dy, N, offsets, nullptr, db, nullptr, sums, dw);
+    KN_TRY(kn_linear_dw_run(stream, &la, x, nullptr, g, rp, offsets, rows, da, nullptr, sums, dw, true));
+    return kn_linear_dw_run(stream, &lb, h, nullptr, dy, N, offsets, nullptr, db, nullptr, sums, dw, true);
 }

@@ -245,6 +245,115 @@ __global__ void __launch_bounds__(WAVES * 64) k_reduce_small(KnProduct p, int32_
     }
 }
 
+// One side of up to 64 values (a low-rank product's), the other long: a workgroup of THIN_WAVES wavefronts per part and tile of 16 FI x 16 FJ results; a wavefront
+// takes every THIN_WAVES-th step of rows by itself, asked for while another is multiplied, and they are summed in the order of their numbers.  TURN: 16-bit rows
+// of whole pieces, which an LDS of the wavefront's own turns into columns; else value by value, 16 neighbouring lanes, 16 neighbouring values.  Bound by
+// the long side's bytes.
+constexpr int THIN_WAVES = 4;
+template <typename T, int FI, int FJ, bool TURN>
+__global__ void __launch_bounds__(THIN_WAVES * 64) k_reduce_thin(KnProduct p, Parts parts)
+{
+    constexpr int W = 16 / sizeof(T), RS = 4 * W, LD = 16 * FJ + 4, OWN = 16 * FI * LD * 4 > (FI + FJ) * 1024 ? 16 * FI * LD * 4 : (FI + FJ) * 1024;
+    typedef typename KnFrag<T>::Type Frag;
+    __shared__ __align__(16) char lds_[THIN_WAVES * OWN];
+    const int tid = kn_thread(), lane = tid & 63, col = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    KN_LDS char *own = (KN_LDS char *)lds_ + wave * OWN;
+    const int jtiles = (p.J + 16 * FJ - 1) / (16 * FJ), itiles = (p.I + 16 * FI - 1) / (16 * FI), tiles = itiles * jtiles;
+    const int32_t block = p.first + kn_block(), number = block % tiles;
+    const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, parts.len, block / tiles);
+    const int32_t group = piece.group;
+    if (group >= p.E) return;
+    const int32_t o = kn_offset(p.offsets, group, p.M), c0 = piece.begin, cend = max(c0, min(piece.end, c0 + parts.len));
+    if (c0 >= cend && c0 != o) return; // (the first part of a network without rows writes zeros)
+    const bool several = piece.end - o > parts.len;
+    const int64_t place = 2 * (o / parts.len) + (c0 - o) / parts.len;
+    const int j0 = number % jtiles * 16 * FJ, i0 = number / jtiles * 16 * FI;
+    kn_f32x4 acc[FI][FJ] = {};
+    // F fragments' worth of a step's rows of one side
+    auto ask = [&](auto count, const T *at, int64_t ld, const int32_t *index, int32_t rows, int32_t width, int32_t c, Frag *to, uint32_t &none) {
+        constexpr int F = decltype(count)::value;
+        none = 0; // a bit for each fragment (TURN) or value of a fragment: rows that are not there
+#pragma unroll
+        for (int f = 0; f < (TURN ? F : W); ++f) {
+            const int32_t r = c + (TURN ? (lane + 64 * f) / (2 * F) : g * W + f);
+            const int32_t src = index ? index[min(r, cend - 1)] : min(r, cend - 1);
+            const bool there = r < cend && (uint32_t)src < (uint32_t)rows;
+            none |= there ? 0u : 1u << f;
+            const T *row = at + (int64_t)(there ? src : 0) * ld;
+            if constexpr (TURN) to[f] = *(const Frag *)(row + min((lane + 64 * f) % (2 * F) * W, width - W));
+            else
+#pragma unroll
+                for (int v = 0; v < F; ++v) to[v][f] = row[min(16 * v + col, width - 1)];
+        }
+    };
+    auto turn = [&](auto count, Frag *to, uint32_t none, KN_LDS char *lds) {
+        constexpr int F = decltype(count)::value;
+        if constexpr (TURN) {
+#pragma unroll
+            for (int f = 0; f < F; ++f) *(KN_LDS Frag *)(lds + kn_turned_byte<F>((lane + 64 * f) / (2 * F), (lane + 64 * f) % (2 * F))) = none >> f & 1 ? Frag{} : to[f];
+        } else {
+#pragma unroll
+            for (int v = 0; v < F; ++v)
+#pragma unroll
+                for (int f = 0; f < W; ++f) to[v][f] = none >> f & 1 ? (T)0.0f : to[v][f];
+        }
+    };
+    struct Step { Frag a[FI], b[FJ]; uint32_t none_a, none_b; };
+    std::integral_constant<int, FI> fi;
+    std::integral_constant<int, FJ> fj;
+    auto load = [&](Step &x, int32_t c) {
+        ask(fi, (const T *)p.a + i0, p.lda, p.rows, p.a_rows, p.I - i0, c, x.a, x.none_a);
+        ask(fj, (const T *)p.b + j0, p.ldb, p.b_index, p.b_rows, p.J - j0, c, x.b, x.none_b);
+    };
+    auto multiply = [&](Step &x, int32_t c) {
+        if (c >= cend) return;
+        turn(fi, x.a, x.none_a, own);
+        turn(fj, x.b, x.none_b, own + FI * 1024);
+        if constexpr (TURN) {
+            kn_lanes_meet();
+#pragma unroll
+            for (int u = 0; u < FI; ++u) x.a[u] = __builtin_bit_cast(Frag, kn_turned_frag<FI>(own, u, lane));
+#pragma unroll
+            for (int v = 0; v < FJ; ++v) x.b[v] = __builtin_bit_cast(Frag, kn_turned_frag<FJ>(own + FI * 1024, v, lane));
+            kn_lanes_meet();
+        }
+#pragma unroll
+        for (int u = 0; u < FI; ++u)
+#pragma unroll
+            for (int v = 0; v < FJ; ++v) acc[u][v] = kn_mfma(x.b[v], x.a[u], acc[u][v]);
+    };
+    if (p.a_rows > 0 && p.b_rows > 0 && c0 + wave * RS < cend) {
+        constexpr int TURNS = THIN_WAVES * RS;
+        Step even, odd;
+        load(even, c0 + wave * RS);
+        for (int32_t c = c0 + wave * RS; c < cend; c += 2 * TURNS) { // (behind the part's end: its last row, unused)
+            load(odd, c + TURNS);
+            multiply(even, c);
+            load(even, c + 2 * TURNS);
+            multiply(odd, c + TURNS);
+        }
+    }
+    kn_lanes_meet();
+    KN_LDS float *red = (KN_LDS float *)own;
+#pragma unroll
+    for (int u = 0; u < FI; ++u)
+#pragma unroll
+        for (int v = 0; v < FJ; ++v) *(KN_LDS kn_f32x4 *)(red + (16 * u + col) * LD + 16 * v + 4 * g) = acc[u][v];
+    __syncthreads();
+    float *sums = parts.sums + place * p.I * p.J;
+    T *out = (T *)p.out + (int64_t)group * p.o_group; // (its rows follow one another)
+    for (int q = tid; q < 16 * FI * 16 * FJ; q += THIN_WAVES * 64) {
+        const int r = q / (16 * FJ), c = q % (16 * FJ);
+        if (i0 + r >= p.I || j0 + c >= p.J) continue;
+        float y = 0.0f;
+#pragma unroll
+        for (int w = 0; w < THIN_WAVES; ++w) y += *(const KN_LDS float *)((KN_LDS char *)lds_ + w * OWN + (r * LD + c) * 4);
+        const int64_t at = (int64_t)(i0 + r) * p.J + j0 + c;
+        if (several) sums[at] = y;
+        else out[at] = (T)y;
+    }
+}
+
 // The parts' sums of the networks that have several, in the order of the parts; `chunk` results per workgroup.  SEARCH: there are at most
 // M / len such networks, and a workgroup looks for its own among all (few networks of many results); else there is one for
 // every network's results, and most find nothing to do.  SPLIT: each wavefront sums a quarter of a network's parts, and the quarters are added
@@ -329,13 +438,38 @@ Way way_of(const kn_linear_desc *d, bool direct)
 // of 2,048 80, none 261; 4 networks 256 x 256, the longest of 16,384 11,740: of 256 31, of 1,024 23, of 2,048 33.  In fp32, where a
 // tile takes longest and its sums are the less: of 512 51, of 2,048 71.  Narrow layers' parts are small, and more of them are chains
 // that run at the same time.
-int32_t part_length(const kn_linear_desc *d)
+int32_t part_length(const kn_linear_desc *d, bool thin)
 {
+    if (thin) return (int32_t)kn_align_up(d->rows > 512 * 256 ? kn_div_up(d->rows, 256) : 512, 64); // (no more than a few hundred parts)
     const bool whole = d->dtype == KN_F32;
     const int64_t tiles = narrow(d) ? 1 : kn_div_up(d->n_in, 128) * kn_div_up(d->n_out, 128);
     const int64_t len = kn_div_up(d->rows, kn_div_up(narrow(d) ? 1024 : whole ? 256 : 512, tiles));
     const int64_t least = narrow(d) ? 128 : whole && d->rows > 1024 ? 512 : tiles <= 8 ? 1024 : 2048;
     return (int32_t)kn_align_up(len < least ? least : len, 64);
+}
+
+// A low-rank product's gradients, whose other side is longer than what the narrow layers' kernels take
+bool is_thin(const kn_linear_desc *d) { return (d->n_in <= 64) != (d->n_out <= 64); }
+
+template <typename T> int launch_join(hipStream_t st, const KnProduct &p, int32_t sum, const Parts &parts);
+
+template <typename T, bool TURN> int launch_thin(hipStream_t st, const KnProduct &p, const Parts &parts)
+{
+    auto launch = [&](auto fi, auto fj) -> int {
+        constexpr int FI = decltype(fi)::value, FJ = decltype(fj)::value;
+        const int64_t blocks = kn_pieces(p.M, p.E, parts.len) * kn_div_up(p.I, 16 * FI) * kn_div_up(p.J, 16 * FJ);
+        return kn_launch(blocks, THIN_WAVES * 64, [&](dim3 grid, int32_t first) {
+            KnProduct q = p;
+            q.first = first;
+            hipLaunchKernelGGL((k_reduce_thin<T, FI, FJ, TURN>), grid, dim3(THIN_WAVES * 64), 0, st, q, parts);
+        });
+    };
+    std::integral_constant<int, 1> one;
+    std::integral_constant<int, 2> two;
+    std::integral_constant<int, 4> four;
+    if (p.I <= p.J) KN_TRY(p.I <= 16 ? launch(one, four) : p.I <= 32 ? launch(two, four) : launch(four, four));
+    else KN_TRY(p.J <= 16 ? launch(four, one) : p.J <= 32 ? launch(four, two) : launch(four, four));
+    return launch_join<T>(st, p, SUM_NONE, parts);
 }
 
 template <typename T, bool DIRECT, int SAVED>
@@ -373,6 +507,11 @@ int launch_reduce(hipStream_t st, const kn_linear_desc *d, const KnProduct &p, i
         }
     });
     KN_TRY(status);
+    return launch_join<T>(st, p, sum, parts);
+}
+
+template <typename T> int launch_join(hipStream_t st, const KnProduct &p, int32_t sum, const Parts &parts)
+{
     if (p.M <= parts.len) return KN_OK; // (no network has several)
     const int64_t most = p.M / parts.len, results = (int64_t)p.I * p.J;
     const bool few = results * (most < p.E ? most : p.E) <= 1 << 20 && p.E * kn_div_up(results, 256) <= 8192;
@@ -393,8 +532,12 @@ int launch_reduce(hipStream_t st, const kn_linear_desc *d, const KnProduct &p, i
 extern "C" int kn_grouped_linear_dw_workspace_bytes(const kn_linear_desc *d, int64_t *out_bytes)
 {
     KN_TRY(kn_linear_check(d));
-    if (!out_bytes) return KN_E_INVALID_ARG;
-    const int32_t len = part_length(d);
+    return out_bytes ? kn_linear_dw_bytes(d, false, out_bytes) : KN_E_INVALID_ARG;
+}
+
+int kn_linear_dw_bytes(const kn_linear_desc *d, bool thin, int64_t *out_bytes)
+{
+    const int32_t len = part_length(d, thin && is_thin(d));
     *out_bytes = d->rows <= len ? 0 : kn_align_up(part_places(d->rows, len) * ((int64_t)d->n_in * d->n_out + d->n_out) * 4, 256);
     return KN_OK;
 }
@@ -418,13 +561,14 @@ extern "C" int kn_grouped_linear_dw_saved(void *stream, const kn_linear_desc *d,
 }
 
 int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const uint8_t *exponents, const void *dy, int64_t lddy, const int32_t *offsets,
-                     const int32_t *rows, void *dw, void *db, void *workspace, int64_t workspace_bytes)
+                     const int32_t *rows, void *dw, void *db, void *workspace, int64_t workspace_bytes, bool thin)
 {
+    thin = thin && is_thin(d);
     if (!offsets || !dw || (d->rows > 0 && (!dy || (d->x_rows > 0 && !x))) || (d->rows > 0 && !rows && d->x_rows < d->rows)) return KN_E_INVALID_ARG;
     int64_t need = 0;
-    KN_TRY(kn_grouped_linear_dw_workspace_bytes(d, &need));
+    KN_TRY(kn_linear_dw_bytes(d, thin, &need));
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return KN_E_WORKSPACE;
-    Parts parts = {part_length(d), (float *)workspace, nullptr};
+    Parts parts = {part_length(d, thin), (float *)workspace, nullptr};
     parts.bias_sums = parts.sums + part_places(d->rows, parts.len) * (int64_t)d->n_in * d->n_out;
     KnProduct p = {};
     const bool io = d->w_layout == KN_W_IN_OUT; // (columns are what is contiguous in dw)
@@ -446,6 +590,12 @@ int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const
             return direct ? launch_reduce<E_, true, SAVED_B>(st, d, p, sum, parts, exponents) : launch_reduce<E_, false, SAVED_B>(st, d, p, sum, parts, exponents);
         }
         const bool direct = p.I % V == 0 && p.J % V == 0 && (((uintptr_t)p.a | (uintptr_t)p.b) & 15) == 0 && p.lda % V == 0 && p.ldb % V == 0;
+        if (thin) {
+            if constexpr (sizeof(E_) == 2) {
+                if (direct) return launch_thin<E_, true>(st, p, parts);
+            }
+            return launch_thin<E_, false>(st, p, parts);
+        }
         return direct ? launch_reduce<E_, true, SAVED_NONE>(st, d, p, sum, parts, nullptr) : launch_reduce<E_, false, SAVED_NONE>(st, d, p, sum, parts, nullptr);
     });
 }

@@ -158,6 +158,25 @@ __device__ __forceinline__ void kn_row_place(typename KnFrag<T>::Type &f, const 
     if (bytes & 8) d = kn_u32x4{d[2], d[3], 0, 0};
     f = __builtin_bit_cast(typename KnFrag<T>::Type, k < C && k + W > C ? d : whole);
 }
+// 32 rows of 16 V values of 16 bits in an LDS that one wavefront has for itself, to be read column by column: where row r and its piece lie, so that the 4 x 4 rows
+// of a transposing read are spread over all banks.
+template <int V> __device__ __forceinline__ int kn_turned_byte(int r, int piece)
+{
+    if constexpr (V == 1) return (r ^ (r >> 3 & 1) << 2) * 32 + piece * 16;
+    else if constexpr (V == 2) return r * 64 + (piece ^ (r >> 3 & 1) << 1) * 16;
+    else return r * 128 + (piece ^ ((r >> 1 & 1) | (r >> 3 & 1) << 1) << 1) * 16;
+}
+// Column 16 v + l % 16 of rows 8 (l / 16) .. + 7
+template <int V> __device__ __forceinline__ kn_f16x8 kn_turned_frag(KN_LDS char *turn, int v, int lane)
+{
+    const int g = lane >> 4, i = lane & 15;
+    union { kn_s16x4 h[2]; kn_f16x8 f; } t;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        t.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((KN_LDS kn_s16x4 *)(turn + kn_turned_byte<V>(8 * g + 4 * h + (i >> 2), 2 * v + (i >> 1 & 1)) + (i & 1) * 8));
+    return t.f;
+}
+
 // What is added to columns j .. j + 7 of a network's results (j a multiple of 8)
 template <typename T> __device__ __forceinline__ void kn_bias_of(const KnProduct &p, bool some, int64_t group, int32_t j, float add[8])
 {
