@@ -245,17 +245,16 @@ __global__ void __launch_bounds__(WAVES * 64) k_reduce_small(KnProduct p, int32_
     }
 }
 
-// One side of up to 64 values (a low-rank product's), the other long: a workgroup of THIN_WAVES wavefronts per part and tile of 16 FI x 16 FJ results; a wavefront
-// takes every THIN_WAVES-th step of rows by itself, asked for while another is multiplied, and they are summed in the order of their numbers.  TURN: 16-bit rows
+// One side of up to 64 values (a low-rank product's), the other long: a workgroup of WAVES wavefronts per part and tile of 16 FI x 16 FJ results; a wavefront
+// takes every WAVES-th step of rows by itself, asked for while another is multiplied, and they are summed in the order of their numbers.  TURN: 16-bit rows
 // of whole pieces, which an LDS of the wavefront's own turns into columns; else value by value, 16 neighbouring lanes, 16 neighbouring values.  Bound by
 // the long side's bytes.
-constexpr int THIN_WAVES = 4;
-template <typename T, int FI, int FJ, bool TURN>
-__global__ void __launch_bounds__(THIN_WAVES * 64) k_reduce_thin(KnProduct p, Parts parts)
+template <typename T, int FI, int FJ, bool TURN, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) k_reduce_thin(KnProduct p, Parts parts)
 {
     constexpr int W = 16 / sizeof(T), RS = 4 * W, LD = 16 * FJ + 4, OWN = 16 * FI * LD * 4 > (FI + FJ) * 1024 ? 16 * FI * LD * 4 : (FI + FJ) * 1024;
     typedef typename KnFrag<T>::Type Frag;
-    __shared__ __align__(16) char lds_[THIN_WAVES * OWN];
+    __shared__ __align__(16) char lds_[WAVES * OWN];
     const int tid = kn_thread(), lane = tid & 63, col = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     KN_LDS char *own = (KN_LDS char *)lds_ + wave * OWN;
     const int jtiles = (p.J + 16 * FJ - 1) / (16 * FJ), itiles = (p.I + 16 * FI - 1) / (16 * FI), tiles = itiles * jtiles;
@@ -323,7 +322,7 @@ __global__ void __launch_bounds__(THIN_WAVES * 64) k_reduce_thin(KnProduct p, Pa
             for (int v = 0; v < FJ; ++v) acc[u][v] = kn_mfma(x.b[v], x.a[u], acc[u][v]);
     };
     if (p.a_rows > 0 && p.b_rows > 0 && c0 + wave * RS < cend) {
-        constexpr int TURNS = THIN_WAVES * RS;
+        constexpr int TURNS = WAVES * RS;
         Step even, odd;
         load(even, c0 + wave * RS);
         for (int32_t c = c0 + wave * RS; c < cend; c += 2 * TURNS) { // (behind the part's end: its last row, unused)
@@ -342,12 +341,12 @@ __global__ void __launch_bounds__(THIN_WAVES * 64) k_reduce_thin(KnProduct p, Pa
     __syncthreads();
     float *sums = parts.sums + place * p.I * p.J;
     T *out = (T *)p.out + (int64_t)group * p.o_group; // (its rows follow one another)
-    for (int q = tid; q < 16 * FI * 16 * FJ; q += THIN_WAVES * 64) {
+    for (int q = tid; q < 16 * FI * 16 * FJ; q += WAVES * 64) {
         const int r = q / (16 * FJ), c = q % (16 * FJ);
         if (i0 + r >= p.I || j0 + c >= p.J) continue;
         float y = 0.0f;
 #pragma unroll
-        for (int w = 0; w < THIN_WAVES; ++w) y += *(const KN_LDS float *)((KN_LDS char *)lds_ + w * OWN + (r * LD + c) * 4);
+        for (int w = 0; w < WAVES; ++w) y += *(const KN_LDS float *)((KN_LDS char *)lds_ + w * OWN + (r * LD + c) * 4);
         const int64_t at = (int64_t)(i0 + r) * p.J + j0 + c;
         if (several) sums[at] = y;
         else out[at] = (T)y;
@@ -438,9 +437,16 @@ Way way_of(const kn_linear_desc *d, bool direct)
 // of 2,048 80, none 261; 4 networks 256 x 256, the longest of 16,384 11,740: of 256 31, of 1,024 23, of 2,048 33.  In fp32, where a
 // tile takes longest and its sums are the less: of 512 51, of 2,048 71.  Narrow layers' parts are small, and more of them are chains
 // that run at the same time.
+// k_reduce_thin: four wavefronts and parts of 512 rows, or eight and 1,024 (us, whole forward and backward calls): 8,192 rows of 16 networks 1024 x 2048, rank 16, 143 and
+// 138, of even networks 138 and 130; 16,384 of 4 412 and 410; 16,384 of one 1024 x 1024 141 and 147; but 4,096 of 64 107 and 132, 20,000 of 100 515 x
+// 300 149 and 165, 262,145 of 1,600 91 x 64 181 and 235.
+bool many_rows(int64_t rows, int64_t networks) { return rows / networks >= 256; }
 int32_t part_length(const kn_linear_desc *d, bool thin)
 {
-    if (thin) return (int32_t)kn_align_up(d->rows > 512 * 256 ? kn_div_up(d->rows, 256) : 512, 64); // (no more than a few hundred parts)
+    if (thin) { // (no more than a few hundred parts)
+        const int64_t least = many_rows(d->rows, d->experts) ? 1024 : 512, len = kn_div_up(d->rows, 256);
+        return (int32_t)kn_align_up(len < least ? least : len, 64);
+    }
     const bool whole = d->dtype == KN_F32;
     const int64_t tiles = narrow(d) ? 1 : kn_div_up(d->n_in, 128) * kn_div_up(d->n_out, 128);
     const int64_t len = kn_div_up(d->rows, kn_div_up(narrow(d) ? 1024 : whole ? 256 : 512, tiles));
@@ -458,10 +464,12 @@ template <typename T, bool TURN> int launch_thin(hipStream_t st, const KnProduct
     auto launch = [&](auto fi, auto fj) -> int {
         constexpr int FI = decltype(fi)::value, FJ = decltype(fj)::value;
         const int64_t blocks = kn_pieces(p.M, p.E, parts.len) * kn_div_up(p.I, 16 * FI) * kn_div_up(p.J, 16 * FJ);
-        return kn_launch(blocks, THIN_WAVES * 64, [&](dim3 grid, int32_t first) {
+        const bool many = many_rows(p.M, p.E);
+        return kn_launch(blocks, many ? 512 : 256, [&](dim3 grid, int32_t first) {
             KnProduct q = p;
             q.first = first;
-            hipLaunchKernelGGL((k_reduce_thin<T, FI, FJ, TURN>), grid, dim3(THIN_WAVES * 64), 0, st, q, parts);
+            if (many) hipLaunchKernelGGL((k_reduce_thin<T, FI, FJ, TURN, 8>), grid, dim3(512), 0, st, q, parts);
+            else hipLaunchKernelGGL((k_reduce_thin<T, FI, FJ, TURN, 4>), grid, dim3(256), 0, st, q, parts);
         });
     };
     std::integral_constant<int, 1> one;
