@@ -642,7 +642,8 @@ def _adapted_args(x, w, a, b, offsets, rows, scales):
         raise KnError("weights must be device tensors")
     if w.is_contiguous() and a.is_contiguous() and b.is_contiguous():
         layout = 0
-    elif w.t().is_contiguous() and a.transpose(1, 2).is_contiguous() and b.transpose(1, 2).is_contiguous():
+    elif (w.stride() == (1, K) and a.stride() == (K * rank, 1, K) and b.stride() == (rank * N, 1, rank)) or (
+            w.t().is_contiguous() and a.transpose(1, 2).is_contiguous() and b.transpose(1, 2).is_contiguous()):  # (axes of one value have any stride)
         layout = 1
     else:
         raise KnError("the shared weights and the adapters must all be contiguous, or all be transposes of contiguous weights")

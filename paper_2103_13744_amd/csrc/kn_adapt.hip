@@ -19,11 +19,15 @@ struct Down {
     int64_t lda, b_group, b_c, b_j;
     int32_t M, E, C, rank, rp, a_rows;
     int32_t first; // number of the launch's first workgroup
+    // what the networks' second products are made with, `values` of each: whether a network's are all finite is left in apart[network] (nullptr: not asked)
+    const void *next;
+    int64_t values;
+    int32_t *apart;
 };
 // What the shared product takes beside its own operands
 struct Beside {
     const void *h, *b;
-    const int32_t *net;
+    const int32_t *net, *apart; // apart: a network's b has infinities or NaN
     int64_t b_group, b_c, b_j;
     int32_t E, rank, rp;
 };
@@ -146,6 +150,11 @@ template <typename T, int B, int U, int V, int WAVES, int AHEAD> struct Sums {
     }
 };
 
+// Whether a value is an infinity or a NaN
+__device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ bool not_finite(_Float16 v) { return (__builtin_bit_cast(uint16_t, v) & 0x7c00u) == 0x7c00u; }
+__device__ __forceinline__ bool not_finite(__bf16 v) { return (__builtin_bit_cast(uint16_t, v) & 0x7f80u) == 0x7f80u; }
+
 // The h of 16 U rows of one network, 16 V values
 template <typename T, int B, int U, int V, int WAVES, int AHEAD> __device__ __forceinline__ void down_piece(const Down &p, int32_t number, float *red)
 {
@@ -179,6 +188,30 @@ template <typename T, int B, int U, int V, int WAVES, int AHEAD> __device__ __fo
 #pragma unroll
         for (int n = 0; n < 4; ++n) o[n] = j + n < p.rank ? (T)(scale * y[n]) : (T)0.0f; // (16 bits: what the matrix cores take)
         *(Four *)((T *)p.h + (int64_t)i * p.rp + j) = o;
+    }
+    if (!p.apart || !some || j0 > 0 || piece.begin != kn_offset(p.offsets, piece.group, p.M)) return;
+    // (the network's first rows)
+    constexpr int W = Core::W;
+    const T *values = (const T *)p.next + group * p.values;
+    bool any = false;
+    for (int64_t at = (int64_t)tid * W; at < p.values; at += WAVES * 64 * W) {
+        if (at + W <= p.values) {
+            const typename KnAny<T>::Piece v = *(const typename KnAny<T>::Piece *)(values + at);
+#pragma unroll
+            for (int q = 0; q < W; ++q) any |= not_finite((T)v[q]);
+        } else {
+            for (int64_t q = at; q < p.values; ++q) any |= not_finite(values[q]);
+        }
+    }
+    __syncthreads();
+    int32_t *found = (int32_t *)red;
+    const bool of_wave = __ballot(any) != 0;
+    if ((tid & 63) == 0) found[tid >> 6] = of_wave;
+    __syncthreads();
+    if (tid == 0) {
+        int32_t all = 0;
+        for (int w = 0; w < WAVES; ++w) all |= found[w];
+        p.apart[piece.group] = all;
     }
 }
 template <typename T, int B, int U, int V, int WAVES, int AHEAD> __global__ void __launch_bounds__(WAVES * 64) k_adapt_down(Down p)
@@ -384,7 +417,7 @@ template <typename T, int R, int NW, int LIST, bool COLS, bool DIRECT> struct Lo
             const int32_t more = __shfl(nets[c], slot & 63);
             net = slot >> 6 == c ? more : net;
         }
-        if (slot >= count || q >= rank || left <= 0) return nullptr;
+        if (slot >= count || net < 0 || q >= rank || left <= 0) return nullptr;
         return b + net * group + q * along + (j0 + k) * across;
     }
     __device__ __forceinline__ void ask(int wave, int lane, int s)
@@ -413,10 +446,12 @@ template <typename T, int R, int NW, int LIST, bool COLS, bool DIRECT> struct Lo
 };
 
 // Tiles of BM x BN results, WR x WC wavefronts, NB stages in the LDS, of which one is multiplied while the others are fetched, as in the grouped products; behind the
-// stages of the shared contraction come those of the tile's networks.  COLS: the columns of w and b are contiguous (else the contraction is).  DIRECT: rows
+// stages of the shared contraction come those of the tile's networks.  There a row meets other networks' values with zeros, and a zero times what is not finite is a
+// NaN: networks with such values are left out, and their rows get their part at the end, value by value.  COLS: the columns of w and b are contiguous (else the contraction is).  DIRECT: rows
 // of whole 16-byte pieces throughout.
+// (128 x 128: registers for two workgroups at a time)
 template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB>
-__global__ void __launch_bounds__(WR * WC * 64) k_adapt_up(KnProduct p, Beside beside, int32_t blocks)
+__global__ void __launch_bounds__(WR * WC * 64, DIRECT && BM == 128 ? 4 : 1) k_adapt_up(KnProduct p, Beside beside, int32_t blocks)
 {
     constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16, CS = 128 / sizeof(T), LIST = (BM + 63) / 64;
     typedef typename KnFrag<T>::Type Frag;
@@ -434,23 +469,28 @@ __global__ void __launch_bounds__(WR * WC * 64) k_adapt_up(KnProduct p, Beside b
     LoadH<T, BM, NW, DIRECT> lh;
     LoadB<T, BN, NW, LIST, COLS, DIRECT> lo;
     int32_t count = 0;
+    bool apart = false; // networks that are left out
     { // (in the stages' LDS, before they are there: with more of it there would be one workgroup at a time)
         KN_LDS int32_t *slots = (KN_LDS int32_t *)lds, *nets = slots + BM, *met = nets + 64 * LIST; // a row's place among the tile's networks (-1: none), the
         const int32_t i = begin + tid;                                                         // networks, how many begin in a wavefront's rows
         const bool in = tid < BM && i < end;
         const int32_t net = in ? beside.net[i] : -1, before = in && tid > 0 ? beside.net[i - 1] : -1;
-        const bool some = (uint32_t)net < (uint32_t)beside.E, begins = some && net != before;
-        const uint64_t all = __ballot(begins);
-        if (lane == 0) met[wave] = __popcll(all);
+        const bool known = (uint32_t)net < (uint32_t)beside.E, left_out = known && beside.apart[net] != 0, begins = known && net != before;
+        const uint64_t all = __ballot(begins), out = __ballot(left_out);
+        if (lane == 0) {
+            met[wave] = __popcll(all);
+            met[NW + wave] = out != 0;
+        }
         __syncthreads();
         int32_t rank = __popcll(all & ((2ull << lane) - 1)) - 1;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             if (w < wave) rank += met[w];
             count += met[w];
+            apart |= met[NW + w] != 0;
         }
-        if (tid < BM) slots[tid] = some ? rank : -1;
-        if (begins) nets[rank] = net;
+        if (tid < BM) slots[tid] = known && !left_out ? rank : -1;
+        if (begins) nets[rank] = left_out ? -1 : net; // (it keeps its place: the others' sums are as they were)
         __syncthreads();
         lh.start(wave, lane, (const T *)beside.h, beside.rp, begin, end, slots);
         lo.start(beside, j0, p.J, nets, count, lane);
@@ -554,6 +594,21 @@ __global__ void __launch_bounds__(WR * WC * 64) k_adapt_up(KnProduct p, Beside b
             if (r >= 16 || i >= end || j >= p.J) continue;
             const kn_f32x4 lo4 = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj), hi4 = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj + 4);
             float y[8] = {lo4[0], lo4[1], lo4[2], lo4[3], hi4[0], hi4[1], hi4[2], hi4[3]};
+            if (apart && C > 0) {
+                const int32_t net = beside.net[i];
+                if ((uint32_t)net < (uint32_t)beside.E && beside.apart[net]) {
+                    const T *h = (const T *)beside.h + (int64_t)i * beside.rp, *v = (const T *)beside.b + net * beside.b_group;
+#pragma unroll 1
+                    for (int q = 0; q < 8; ++q) {
+                        const T *column = v + min(j + q, p.J - 1) * beside.b_j;
+                        float low = 0.0f;
+#pragma unroll 1
+                        for (int32_t c = 0; c < beside.rank; ++c) low = fmaf((float)h[c], (float)column[c * beside.b_c], low);
+#pragma unroll
+                        for (int n = 0; n < 8; ++n) y[n] += n == q ? low : 0.0f;
+                    }
+                }
+            }
             kn_finish<T>(p, true, i, j, add, y);
         }
         kn_lanes_meet();
@@ -922,7 +977,9 @@ template <typename T> int launch_few(hipStream_t st, const Down &down, const KnP
 {
     Few few = few_of(p.M, p.J, p.C, sizeof(T));
     few.sums = sums;
-    KN_TRY(launch_few_b<T>(st, down, p, few, cols));
+    Down alone = down;
+    alone.apart = nullptr; // (rows are added up one by one)
+    KN_TRY(launch_few_b<T>(st, alone, p, few, cols));
     hipLaunchKernelGGL((k_adapt_few_join<T>), dim3((unsigned)kn_div_up((int64_t)p.M * kn_div_up(p.J, 4), 128)), dim3(128), 0, st, p, beside, few);
     KN_CHECK_LAUNCH();
     return KN_OK;
@@ -950,7 +1007,9 @@ int check(const kn_linear_desc *d, int32_t rank)
     if (rank < 1) return KN_E_INVALID_ARG;
     return rank > KN_MAX_WIDTH ? KN_E_UNSUPPORTED : KN_OK;
 }
-int64_t net_bytes(const kn_linear_desc *d) { return kn_align_up(d->rows * 4, 256); }
+// networks of the rows, and which networks are left out
+int64_t net_bytes(const kn_linear_desc *d) { return kn_align_up(d->rows * 4, 256) + kn_align_up(d->experts * 4, 256); }
+int32_t *apart_of(const kn_linear_desc *d, void *workspace) { return (int32_t *)((char *)workspace + kn_align_up(d->rows * 4, 256)); }
 int64_t h_bytes(const kn_linear_desc *d, int32_t rank) { return kn_align_up(d->rows * (int64_t)padded_rank(d->dtype, rank) * kn_item(d->dtype), 256); }
 // The gradients of A and B as those of a grouped layer
 kn_linear_desc layer_of(const kn_linear_desc *d, int32_t n_in, int32_t n_out, int64_t x_rows, int64_t ldx)
@@ -995,8 +1054,8 @@ extern "C" int kn_adapted_linear(void *stream, const kn_linear_desc *d, int32_t 
     const bool io = d->w_layout == KN_W_IN_OUT;
     const int64_t K = d->n_in, N = d->n_out, R = rank;
     Down down = {x, a, scales, h ? h : (char *)workspace + net_bytes(d), (int32_t *)workspace, offsets, rows, d->ldx, K * R, io ? R : 1, io ? 1 : K,
-                 (int32_t)d->rows, d->experts, d->n_in, rank, padded_rank(d->dtype, rank), (int32_t)d->x_rows, 0};
-    Beside beside = {down.h, b, down.net, R * N, io ? N : 1, io ? 1 : R, d->experts, rank, down.rp};
+                 (int32_t)d->rows, d->experts, d->n_in, rank, padded_rank(d->dtype, rank), (int32_t)d->x_rows, 0, b, R * N, apart_of(d, workspace)};
+    Beside beside = {down.h, b, down.net, down.apart, R * N, io ? N : 1, io ? 1 : R, d->experts, rank, down.rp};
     KnProduct p = {};
     p.a = x; p.b = w; p.bias = bias; p.out = y; p.rows = rows;
     p.lda = d->ldx; p.b_c = io ? N : 1; p.b_j = io ? 1 : K; p.o_i = N;
@@ -1031,8 +1090,8 @@ extern "C" int kn_adapted_linear_backward(void *stream, const kn_linear_desc *d,
     const int32_t rp = padded_rank(d->dtype, rank);
     if (d->rows > 0) {
         Down down = {dy, b, scales, g, (int32_t *)workspace, offsets, nullptr, N, R * N, io ? 1 : R, io ? N : 1,
-                     (int32_t)d->rows, d->experts, d->n_out, rank, rp, (int32_t)d->rows, 0};
-        Beside beside = {g, a, down.net, K * R, io ? 1 : K, io ? R : 1, d->experts, rank, rp};
+                     (int32_t)d->rows, d->experts, d->n_out, rank, rp, (int32_t)d->rows, 0, a, K * R, apart_of(d, workspace)};
+        Beside beside = {g, a, down.net, down.apart, K * R, io ? 1 : K, io ? R : 1, d->experts, rank, rp};
         KnProduct p = {};
         p.a = dy; p.b = w; p.mask = relu_in ? (x ? x : w) : nullptr; p.out = dx; // (an x without rows may have no address)
         p.lda = N; p.ldm = d->ldx; p.b_c = io ? 1 : K; p.b_j = io ? N : 1; p.o_i = K;

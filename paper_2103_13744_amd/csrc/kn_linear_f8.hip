@@ -56,15 +56,15 @@ __device__ __forceinline__ int saved_exponent(float amax)
     const int b = __float_as_int(amax);
     return max((b >> 23) - 127 - 8 + ((b & 0x7fffff) > 0x600000 ? 1 : 0), SAVED_LEAST);
 }
-// 16 lanes per row and block of 128 values, as above.  A value above zero keeps its sign: what would round to zero becomes the smallest
+// LANES per row and block of 128 values (16, or as many as a shorter row fills), 8 values a lane.  A value above zero keeps its sign: what would round to zero becomes the smallest
 // value, 2^-9.  What is not finite has no part in the scale: +infinity becomes the NaN without, NaN and -infinity the one with the sign bit.
-template <typename T>
+template <typename T, int LANES>
 __global__ void __launch_bounds__(256) k_save_rows(const T *__restrict__ x, int64_t R, int32_t K, int64_t ld, int32_t kb, uint8_t *__restrict__ q,
                                                    uint8_t *__restrict__ exponents, int32_t first)
 {
-    const int64_t g = (((int64_t)first + kn_block()) * 256 + kn_thread()) >> 4;
+    const int64_t g = (((int64_t)first + kn_block()) * 256 + kn_thread()) / LANES;
     if (g >= R * kb) return;
-    const int at = kn_thread() & 15;
+    const int at = kn_thread() & (LANES - 1);
     const int64_t row = g / kb;
     const int32_t blk = (int32_t)(g % kb), k0 = blk * KN_SAVED_BLOCK + at * 8, bytes = (K + 15) & ~15;
     float v[8];
@@ -83,7 +83,11 @@ __global__ void __launch_bounds__(256) k_save_rows(const T *__restrict__ x, int6
         finite &= good;
         amax = good ? fmaxf(amax, m) : amax;
     }
-    const int n = saved_exponent(kn_row_max(amax));
+    if constexpr (LANES == 16) amax = kn_row_max(amax);
+    else
+#pragma unroll
+        for (int d = LANES / 2; d > 0; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d));
+    const int n = saved_exponent(amax);
     const float inverse = __int_as_float((127 - n) << 23);
     const float cap = n == saved_most<T>() ? 240.0f : 448.0f;
     float t[8];
@@ -371,8 +375,10 @@ extern "C" int kn_save_f8(void *stream, const void *x, int32_t dtype, int64_t R,
     const int32_t kb = (int32_t)kn_div_up(K, KN_SAVED_BLOCK);
     return kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
-        return kn_launch(kn_div_up(R * kb, 16), 256, [&](dim3 grid, int32_t first) {
-            hipLaunchKernelGGL((k_save_rows<E_>), grid, dim3(256), 0, (hipStream_t)stream, (const E_ *)x, R, K, ld, kb, (uint8_t *)q, exponents, first);
+        const int lanes = K <= 32 ? 4 : K <= 64 ? 8 : 16;
+        auto kernel = K <= 32 ? k_save_rows<E_, 4> : K <= 64 ? k_save_rows<E_, 8> : k_save_rows<E_, 16>;
+        return kn_launch(kn_div_up(R * kb * lanes, 256), 256, [&](dim3 grid, int32_t first) {
+            hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, (const E_ *)x, R, K, ld, kb, (uint8_t *)q, exponents, first);
         });
     });
 }

@@ -104,3 +104,49 @@ def test_adapted(size, dtype):
         dy = rand(9 + i, m, n).to(DT[dtype])
         got = kn.adapted_linear_backward(dev(dy), dev(x), h, *args[1:], rows=dev(rows), scales=dev(s), relu_in=relu)
         check_backward(dy, x, w, a, b, off, rows, s, relu, h, got, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nk", [False, True])
+@pytest.mark.parametrize("size", [(40, 20, 256, 200, 16), (300, 60, 256, 200, 16), (300, 60, 256, 200, 12), (3000, 100, 256, 520, 16), (3000, 100, 64, 64, 8), (3000, 40, 255, 129, 8), (20000, 90, 512, 1024, 24)],
+                         ids=str)
+def test_adapted_not_finite_values_stay_with_their_network(size, nk):
+    """Rows of several networks share tiles: what is not finite in one network's adapter, or in a row, does not reach another's rows."""
+    m, e, k, n, r = size
+    for dtype in ("bf16", "f16", "f32"):
+        x, w, a, b, off, rows, s = make(m, e, k, n, r, dtype, "tail", False, nk, m)
+        dy = rand(8, m, n).to(DT[dtype])
+        args = lambda a, b: (dev(w), dev(a), dev(b), dev(off))  # noqa: E731
+        y, h = kn.adapted_linear(dev(x), *args(a, b), scales=dev(s), want_h=True)
+        dx, da, db = kn.adapted_linear_backward(dev(dy), dev(x), h, *args(a, b), scales=dev(s))
+        where = torch.searchsorted(off, torch.arange(m, dtype=torch.int32), right=True) - 1
+        some = torch.unique(where[where < e])
+        bad = {int(some[1]): math.nan, int(some[len(some) // 2]): math.inf, int(some[-1]): -math.inf}
+        a2, b2 = a.clone(), b.clone()
+        for i, v in bad.items():
+            b2[i, r // 2, n // 3] = v
+        y2, h2 = kn.adapted_linear(dev(x), *args(a, b2), scales=dev(s), want_h=True)
+        hit = torch.isin(where, torch.tensor(list(bad)))
+        assert torch.equal(h2, h) and not torch.isfinite(y2[hit.cuda(), n // 3]).any()
+        # other networks' rows keep their bits; the network's own other columns may be summed in another order: both results are within
+        # (k + r + 16) 2^-23 of the sum of magnitudes of the same sum, and rounded once each
+        assert torch.equal(y2[~hit.cuda()], y[~hit.cuda()])
+        others = torch.arange(n) != n // 3
+        mag = x[hit].double().abs() @ w.double().abs()
+        for row, i in enumerate(hit.nonzero()[:, 0].tolist()):
+            mag[row] += h[i, :r].double().cpu().abs() @ b[where[i]].double().abs()
+        y1 = y[hit.cuda()].double().cpu()
+        within(y2[hit.cuda()][:, others.cuda()], y1[:, others], (2 * (k + r + 16) * 2.0 ** -23 * mag + U[dtype] * y1.abs())[:, others], dtype)
+        for i, v in bad.items():
+            a2[i, k // 2, r - 1] = v
+        dx2, da2, db2 = kn.adapted_linear_backward(dev(dy), dev(x), h, *args(a2, b), scales=dev(s))
+        assert not torch.isfinite(dx2[hit.cuda(), k // 2]).any()
+        assert torch.equal(dx2[~hit.cuda()], dx[~hit.cuda()]) and torch.equal(da2, da) and torch.equal(db2, db)
+        assert torch.isfinite(dx2[hit.cuda()][:, (torch.arange(k) != k // 2).cuda()]).all()
+        x2 = x.clone()
+        x2[5, 3], x2[m // 2, 0], x2[m - 1, 1] = math.nan, math.inf, math.nan
+        y2, h2 = kn.adapted_linear(dev(x2), *args(a, b), scales=dev(s), want_h=True)
+        keep = torch.ones(m, dtype=torch.bool)
+        keep[[5, m // 2, m - 1]] = False
+        assert torch.equal(y2[keep.cuda()], y[keep.cuda()]) and torch.equal(h2[keep.cuda()], h[keep.cuda()]) and not torch.isfinite(y2[~keep.cuda()]).any()
+        assert (h2[m - 1] == 0).all()  # (a row of no network)
