@@ -19,7 +19,7 @@ struct Down {
     int64_t lda, b_group, b_c, b_j;
     int32_t M, E, C, rank, rp, a_rows;
     int32_t first; // number of the launch's first workgroup
-    // what the networks' second products are made with, `values` of each: whether a network's are all finite is left in apart[network] (nullptr: not asked)
+    // what the networks' second products are made with, `values` of each: whether a network's are not all finite is left in apart[network] (k_adapt_down)
     const void *next;
     int64_t values;
     int32_t *apart;
@@ -189,21 +189,32 @@ template <typename T, int B, int U, int V, int WAVES, int AHEAD> __device__ __fo
         for (int n = 0; n < 4; ++n) o[n] = j + n < p.rank ? (T)(scale * y[n]) : (T)0.0f; // (16 bits: what the matrix cores take)
         *(Four *)((T *)p.h + (int64_t)i * p.rp + j) = o;
     }
-    if (!p.apart || !some || j0 > 0 || piece.begin != kn_offset(p.offsets, piece.group, p.M)) return;
-    // (the network's first rows)
-    constexpr int W = Core::W;
+}
+// Whether the values that network `group` makes its second product with are all finite, if it has rows: a workgroup of its own, so that they are looked at while the
+// first product is made
+template <typename T, int WAVES> __device__ __forceinline__ void look_at(const Down &p, int32_t group, float *red)
+{
+    constexpr int W = 16 / sizeof(T), AHEAD = 8, STEP = WAVES * 64 * W;
+    if (kn_offset(p.offsets, group, p.M) >= kn_offset(p.offsets, group + 1, p.M)) return;
+    const int tid = kn_thread();
     const T *values = (const T *)p.next + group * p.values;
     bool any = false;
-    for (int64_t at = (int64_t)tid * W; at < p.values; at += WAVES * 64 * W) {
-        if (at + W <= p.values) {
-            const typename KnAny<T>::Piece v = *(const typename KnAny<T>::Piece *)(values + at);
+    if (p.values < W) {
+        any = not_finite(values[min((int64_t)tid, p.values - 1)]);
+    } else {
+        for (int64_t at = (int64_t)tid * W; at < p.values; at += AHEAD * STEP) {
+            typename KnAny<T>::Piece v[AHEAD];
 #pragma unroll
-            for (int q = 0; q < W; ++q) any |= not_finite((T)v[q]);
-        } else {
-            for (int64_t q = at; q < p.values; ++q) any |= not_finite(values[q]);
+            for (int n = 0; n < AHEAD; ++n) { // (behind the end: the last ones again)
+                const int64_t from = at + n * STEP, last = p.values - W;
+                v[n] = *(const typename KnAny<T>::Piece *)(values + (from < last ? from : last));
+            }
+#pragma unroll
+            for (int n = 0; n < AHEAD; ++n)
+#pragma unroll
+                for (int q = 0; q < W; ++q) any |= not_finite((T)v[n][q]);
         }
     }
-    __syncthreads();
     int32_t *found = (int32_t *)red;
     const bool of_wave = __ballot(any) != 0;
     if ((tid & 63) == 0) found[tid >> 6] = of_wave;
@@ -211,13 +222,15 @@ template <typename T, int B, int U, int V, int WAVES, int AHEAD> __device__ __fo
     if (tid == 0) {
         int32_t all = 0;
         for (int w = 0; w < WAVES; ++w) all |= found[w];
-        p.apart[piece.group] = all;
+        p.apart[group] = all;
     }
 }
 template <typename T, int B, int U, int V, int WAVES, int AHEAD> __global__ void __launch_bounds__(WAVES * 64) k_adapt_down(Down p)
 {
     __shared__ __align__(16) float red[Sums<T, B, U, V, WAVES, AHEAD>::WORDS];
-    down_piece<T, B, U, V, WAVES, AHEAD>(p, p.first + kn_block(), red);
+    const int32_t block = p.first + kn_block();
+    if (block < p.E) look_at<T, WAVES>(p, block, red);
+    else down_piece<T, B, U, V, WAVES, AHEAD>(p, block - p.E, red);
 }
 
 // Few rows (16 U at most): one launch leaves h and the shared product's sums, cut into parts of the contraction so that all of w is on its way at once; the
@@ -854,7 +867,7 @@ template <typename T, bool COLS> int launch_small(hipStream_t st, const Down &do
 
 template <typename T, int B, int U, int V, int WAVES, int AHEAD> int launch_down_of(hipStream_t st, const Down &p)
 {
-    return kn_launch(kn_pieces(p.M, p.E, 16 * U) * kn_div_up(p.rp, 16 * V), WAVES * 64, [&](dim3 grid, int32_t first) {
+    return kn_launch(p.E + kn_pieces(p.M, p.E, 16 * U) * kn_div_up(p.rp, 16 * V), WAVES * 64, [&](dim3 grid, int32_t first) {
         Down q = p;
         q.first = first;
         hipLaunchKernelGGL((k_adapt_down<T, B, U, V, WAVES, AHEAD>), grid, dim3(WAVES * 64), 0, st, q);
@@ -977,9 +990,7 @@ template <typename T> int launch_few(hipStream_t st, const Down &down, const KnP
 {
     Few few = few_of(p.M, p.J, p.C, sizeof(T));
     few.sums = sums;
-    Down alone = down;
-    alone.apart = nullptr; // (rows are added up one by one)
-    KN_TRY(launch_few_b<T>(st, alone, p, few, cols));
+    KN_TRY(launch_few_b<T>(st, down, p, few, cols));
     hipLaunchKernelGGL((k_adapt_few_join<T>), dim3((unsigned)kn_div_up((int64_t)p.M * kn_div_up(p.J, 4), 128)), dim3(128), 0, st, p, beside, few);
     KN_CHECK_LAUNCH();
     return KN_OK;
