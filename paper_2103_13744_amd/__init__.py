@@ -168,6 +168,15 @@ def _stream():
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+def _stream_on(*tensors):
+    """``_stream()``, of a call on these tensors: what lies on another device than the current one is refused (None: no tensor)."""
+    device = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise KnError("a tensor is on device %d, and the current device is %d" % (t.get_device(), device))
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def params_per_net(hidden: int, L_pos: int = 10, L_dir: int = 4) -> int:
     return int(load_library().kn_params_per_net(hidden, L_pos, L_dir))
 
@@ -553,7 +562,7 @@ def route_balance(logits, k, offsets):
     if T > 64:  # (fewer need no workspace)
         _check(L.kn_route_balance_workspace_bytes(T, E, C.byref(need)), "kn_route_balance_workspace_bytes")
         ws = torch.empty(need.value, dtype=torch.uint8, device=logits.device)
-    _check(L.kn_route_balance(_stream(), ptr, dt, T, E, ld, k, _ptr(offsets, torch.int32, shape=(E + 1,)), losses.data_ptr(), counts.data_ptr(), probs.data_ptr(),
+    _check(L.kn_route_balance(_stream_on(logits, offsets), ptr, dt, T, E, ld, k, _ptr(offsets, torch.int32, shape=(E + 1,)), losses.data_ptr(), counts.data_ptr(), probs.data_ptr(),
                               None if ws is None else ws.data_ptr(), need.value), "kn_route_balance")
     return losses, counts, probs
 
@@ -565,7 +574,7 @@ def route_balance_backward(logits, k, counts, dlosses, add=None):
     T, E = logits.shape
     ptr, ld = _rows_ptr(logits, E)
     out = logits.new_empty((T, E))
-    _check(L.kn_route_balance_backward(_stream(), ptr, _dtype_id(logits.dtype), T, E, ld, int(k), _ptr(counts, torch.int32, shape=(E + 1,)),
+    _check(L.kn_route_balance_backward(_stream_on(logits, counts, dlosses, add), ptr, _dtype_id(logits.dtype), T, E, ld, int(k), _ptr(counts, torch.int32, shape=(E + 1,)),
                                        _ptr(dlosses, torch.float32, shape=(2,)), _ptr(add, logits.dtype, allow_none=True, shape=(T, E)), out.data_ptr()),
            "kn_route_balance_backward")
     return out
@@ -667,7 +676,7 @@ def adapted_linear(x, w, a, b, offsets, rows=None, scales=None, bias=None, relu=
     h, need = x.new_empty((M, -(-rank // unit) * unit)) if want_h else None, C.c_int64()
     _check(L.kn_adapted_linear_workspace_bytes(C.byref(d), rank, C.byref(need)), "kn_adapted_linear_workspace_bytes")
     ws = torch.empty(need.value, dtype=torch.uint8, device=x.device)
-    _check(L.kn_adapted_linear(_stream(), C.byref(d), rank, px, pw, pa, pb, ps, _ptr(bias, x.dtype, allow_none=True, shape=(d.n_out,)), po, pr, 1 if relu else 0,
+    _check(L.kn_adapted_linear(_stream_on(x, w, a, b, offsets, rows, scales, bias, out), C.byref(d), rank, px, pw, pa, pb, ps, _ptr(bias, x.dtype, allow_none=True, shape=(d.n_out,)), po, pr, 1 if relu else 0,
                                _ptr(out, x.dtype, shape=(M, d.n_out)), None if h is None else h.data_ptr(), ws.data_ptr(), need.value), "kn_adapted_linear")
     return (out, h) if want_h else out
 
@@ -681,7 +690,7 @@ def adapted_linear_backward(dy, x, h, w, a, b, offsets, rows=None, scales=None, 
     dx, da, db, need = x.new_empty((M, d.n_in)), torch.empty_like(a), torch.empty_like(b), C.c_int64()
     _check(L.kn_adapted_linear_backward_workspace_bytes(C.byref(d), rank, C.byref(need)), "kn_adapted_linear_backward_workspace_bytes")
     ws = torch.empty(need.value, dtype=torch.uint8, device=x.device)
-    _check(L.kn_adapted_linear_backward(_stream(), C.byref(d), rank, _ptr(dy, x.dtype, shape=(M, d.n_out)), px, _ptr(h, x.dtype, shape=(M, -(-rank // unit) * unit)),
+    _check(L.kn_adapted_linear_backward(_stream_on(dy, x, h, w, a, b, offsets, rows, scales), C.byref(d), rank, _ptr(dy, x.dtype, shape=(M, d.n_out)), px, _ptr(h, x.dtype, shape=(M, -(-rank // unit) * unit)),
                                         pw, pa, pb, ps, po, pr, 1 if relu_in else 0, dx.data_ptr(), da.data_ptr(), db.data_ptr(), ws.data_ptr(), need.value),
            "kn_adapted_linear_backward")
     return dx, da, db
@@ -736,7 +745,7 @@ def save_f8(x):
     R, K = x.shape
     ptr, ld = _rows_ptr(x, K)
     q, e = x.new_empty((R, -(-K // 16) * 16), dtype=torch.float8_e4m3fn), x.new_empty((R, -(-K // 128)), dtype=torch.float8_e8m0fnu)
-    _check(L.kn_save_f8(_stream(), ptr, _dtype_id(x.dtype), R, K, ld, q.data_ptr(), e.data_ptr()), "kn_save_f8")
+    _check(L.kn_save_f8(_stream_on(x), ptr, _dtype_id(x.dtype), R, K, ld, q.data_ptr(), e.data_ptr()), "kn_save_f8")
     return q, e
 
 
@@ -751,7 +760,7 @@ def restore_f8(q, e, width, dtype):
     L = load_library()
     pq, pe = _saved_ptrs(q, e, int(width))
     out = q.new_empty((q.shape[0], int(width)), dtype=dtype)
-    _check(L.kn_restore_f8(_stream(), pq, pe, q.shape[0], int(width), _dtype_id(dtype), out.data_ptr()), "kn_restore_f8")
+    _check(L.kn_restore_f8(_stream_on(q, e), pq, pe, q.shape[0], int(width), _dtype_id(dtype), out.data_ptr()), "kn_restore_f8")
     return out
 
 
@@ -769,7 +778,7 @@ def grouped_linear_dx_saved(dy, q, e, w, offsets, rows=None):
     L = load_library()
     d, M, pq, _, pw, pr = _saved_desc(q, e, w, rows)
     dx = dy.new_empty((M, d.n_in))  # (rows that are not there have no address: any other will do)
-    _check(L.kn_grouped_linear_dx_saved(_stream(), C.byref(d), _ptr(dy, w.dtype, shape=(M, d.n_out)), pw, pq or 256, _ptr(offsets, torch.int32, shape=(d.experts + 1,)),
+    _check(L.kn_grouped_linear_dx_saved(_stream_on(dy, q, w, offsets, rows), C.byref(d), _ptr(dy, w.dtype, shape=(M, d.n_out)), pw, pq or 256, _ptr(offsets, torch.int32, shape=(d.experts + 1,)),
                                         pr, dx.data_ptr()), "kn_grouped_linear_dx_saved")
     return dx
 
@@ -784,7 +793,7 @@ def grouped_linear_dw_saved(dy, q, e, w, offsets, rows=None, want_bias=True):
     if M > 128:  # (fewer rows need no workspace)
         _check(L.kn_grouped_linear_dw_workspace_bytes(C.byref(d), C.byref(need)), "kn_grouped_linear_dw_workspace_bytes")
         ws = torch.empty(need.value, dtype=torch.uint8, device=dy.device) if need.value else None
-    _check(L.kn_grouped_linear_dw_saved(_stream(), C.byref(d), pq, pe, _ptr(dy, w.dtype, shape=(M, d.n_out)), _ptr(offsets, torch.int32, shape=(d.experts + 1,)),
+    _check(L.kn_grouped_linear_dw_saved(_stream_on(dy, q, e, w, offsets, rows), C.byref(d), pq, pe, _ptr(dy, w.dtype, shape=(M, d.n_out)), _ptr(offsets, torch.int32, shape=(d.experts + 1,)),
                                         pr, dw.data_ptr(), None if db is None else db.data_ptr(), None if ws is None else ws.data_ptr(), need.value),
            "kn_grouped_linear_dw_saved")
     return dw, db
@@ -798,7 +807,7 @@ def grouped_linear_backward_saved(dy, q, e, w, offsets, rows=None, relu_in=False
         L = load_library()
         d, M, _, _, pw, _ = _saved_desc(q, e, w, rows)
         dx = dy.new_empty((M, d.n_in))
-        _check(L.kn_grouped_linear_dx(_stream(), C.byref(d), _ptr(dy, w.dtype, shape=(M, d.n_out)), pw, None, _ptr(offsets, torch.int32, shape=(d.experts + 1,)), None,
+        _check(L.kn_grouped_linear_dx(_stream_on(dy, q, w, offsets), C.byref(d), _ptr(dy, w.dtype, shape=(M, d.n_out)), pw, None, _ptr(offsets, torch.int32, shape=(d.experts + 1,)), None,
                                       dx.data_ptr()), "kn_grouped_linear_dx")
     return (dx, *grouped_linear_dw_saved(dy, q, e, w, offsets, rows, want_bias))
 

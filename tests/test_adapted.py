@@ -150,3 +150,164 @@ def test_adapted_not_finite_values_stay_with_their_network(size, nk):
         keep[[5, m // 2, m - 1]] = False
         assert torch.equal(y2[keep.cuda()], y[keep.cuda()]) and torch.equal(h2[keep.cuda()], h[keep.cuda()]) and not torch.isfinite(y2[~keep.cuda()]).any()
         assert (h2[m - 1] == 0).all()  # (a row of no network)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_adapted_rows_lie_apart_start_anywhere_and_out_of_range(dtype):
+    """x as columns of a wider matrix at any address, rows through an index of which some are not there: those take nothing from row 0, which is NaN."""
+    for m, e, k, n, r, nk in ((50, 4, 64, 96, 8, False), (50, 4, 63, 31, 5, True), (400, 4, 64, 48, 8, True), (700, 6, 200, 264, 12, False), (700, 6, 136, 264, 16, True)):
+        x, w, a, b, off, _, s = make(m, e, k, n, r, dtype, "tail", False, nk, m)
+        rows = torch.randint(-4, m + 4, (m,), generator=torch.Generator().manual_seed(5), dtype=torch.int32)
+        rows[rows == 0] = 1
+        rows[3], rows[m - 1] = -1, m
+        bias = rand(6, n).to(DT[dtype])
+        x[0] = math.nan
+        gone = (rows < 0) | (rows >= m)
+        want = torch.where(gone[:, None], 0.0, x[rows.clamp(0, m - 1).long()].float()).to(DT[dtype])
+        ones = (want, w, a, b, off, None, s)
+        for lead, more in ((0, 0), (1, 2), (8, 8)):
+            wide = torch.full((m, lead + k + more), math.nan, dtype=DT[dtype]).cuda()
+            wide[:, lead:lead + k] = dev(x)
+            xs = wide[:, lead:lead + k]
+            y, h = kn.adapted_linear(xs, dev(w), dev(a), dev(b), dev(off), rows=dev(rows), scales=dev(s), bias=dev(bias), want_h=True)
+            check_forward(*ones, bias, False, y, h, dtype)
+            assert torch.equal(y[gone.cuda()], dev(bias).expand(m, n)[gone.cuda()])
+            dy = rand(9, m, n).to(DT[dtype])
+            got = kn.adapted_linear_backward(dev(dy), xs, h, dev(w), dev(a), dev(b), dev(off), rows=dev(rows), scales=dev(s), relu_in=True)
+            check_backward(dy, *ones, True, h, got, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [(9, 3, 40, 20, 4), (300, 4, 264, 136, 8), (300, 4, 64, 32, 8), (2700, 20, 256, 1024, 16)], ids=str)
+def test_adapted_without_rows(size):
+    """An x without rows counts as zeros; a call without rows does nothing, and its weight gradients are zeros."""
+    m, e, k, n, r = size
+    _, w, a, b, off, _, _ = make(m, e, k, n, r, "bf16", "even", False, False, 1)
+    x, rows, bias = torch.empty(0, k, dtype=torch.bfloat16).cuda(), torch.arange(m, dtype=torch.int32).cuda() - m // 2, rand(2, n).bfloat16().cuda()
+    y, h = kn.adapted_linear(x, dev(w), dev(a), dev(b), dev(off), rows=rows, bias=bias, want_h=True)
+    assert torch.equal(y, bias.expand(m, n)) and not h.any()
+    dx, da, db = kn.adapted_linear_backward(torch.ones_like(y), x, h, dev(w), dev(a), dev(b), dev(off), rows=rows, relu_in=True)
+    assert not dx.any() and not da.any() and not db.any()
+    y, h = kn.adapted_linear(x, dev(w), dev(a), dev(b), dev(off) * 0, want_h=True)
+    assert y.shape == (0, n) and h.shape[0] == 0
+    dx, da, db = kn.adapted_linear_backward(y, x, h, dev(w), dev(a), dev(b), dev(off) * 0)
+    assert dx.shape == (0, k) and not da.any() and not db.any()
+
+
+@pytest.mark.gpu
+def test_adapted_rows_beyond_32_bits():
+    k, x_rows, m, e, n, r = 4096, (1 << 19) + 777, 200, 2, 136, 8
+    rows = torch.cat([torch.arange(x_rows - 100, x_rows), torch.arange(100) * 5000]).to(torch.int32)
+    off = torch.tensor([0, 90, 200], dtype=torch.int32)
+    some, w, a, b = rand(1, m, k).bfloat16(), rand(2, k, n).bfloat16(), (rand(3, e, k, r) / 64).bfloat16(), rand(4, e, r, n).bfloat16()
+    x = torch.empty(x_rows, k, dtype=torch.bfloat16, device="cuda")
+    assert x.numel() * 2 > 1 << 32
+    x[rows.long().cuda()] = dev(some)
+    for count in (200, 50):
+        o = off.clamp(max=count)
+        y, h = kn.adapted_linear(x, dev(w), dev(a), dev(b), dev(o), rows=dev(rows[:count]), want_h=True)
+        check_forward(some[:count], w, a, b, o, None, None, None, False, y, h, "bf16")
+        dy = rand(5, count, n).bfloat16()
+        got = kn.adapted_linear_backward(dev(dy), x, h, dev(w), dev(a), dev(b), dev(o), rows=dev(rows[:count]))
+        check_backward(dy, some[:count], w, a, b, o, None, None, False, h, got, "bf16")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [(40, 4, 24, 40, 4), (300, 4, 24, 40, 4), (300, 4, 200, 140, 20)], ids=str)
+def test_adapted_gradient_against_differences(size):
+    """The result is linear in x, in a and in b alone: (f(a + d) - f(a - d)) / 2 = <da, d> up to the rounding of sums of m n results of magnitude 60 at most."""
+    m, e, k, n, r = size
+    x, w, a, b, off, rows, s = make(m, e, k, n, r, "f32", "tail", True, False, 3)
+    g = rand(2, m, n)
+    f = lambda x, a, b: (kn.adapted_linear(dev(x), dev(w), dev(a), dev(b), dev(off), rows=dev(rows), scales=dev(s)).double().cpu() * g.double()).sum()  # noqa: E731
+    _, h = kn.adapted_linear(dev(x), dev(w), dev(a), dev(b), dev(off), rows=dev(rows), scales=dev(s), want_h=True)
+    dx, da, db = kn.adapted_linear_backward(dev(g), dev(x), h, dev(w), dev(a), dev(b), dev(off), rows=dev(rows), scales=dev(s))
+    grad_x = torch.zeros(x.shape, dtype=torch.float64).index_add_(0, rows.long(), dx.double().cpu())
+    for what, grad in (("x", grad_x), ("a", da.double().cpu()), ("b", db.double().cpu())):
+        d = rand(11, *grad.shape)
+        plus = f(x + d if what == "x" else x, a + d if what == "a" else a, b + d if what == "b" else b)
+        minus = f(x - d if what == "x" else x, a - d if what == "a" else a, b - d if what == "b" else b)
+        assert abs(float((plus - minus) / 2 - (grad * d.double()).sum())) <= 2.0 ** -22 * m * n * 60 * 2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [(1, 1, 256, 200, 8), (48, 20, 256, 512, 16), (500, 7, 64, 32, 8), (900, 30, 256, 1024, 16), (9000, 30, 256, 1024, 16)], ids=str)
+def test_adapted_on_another_stream_and_in_a_graph(size):
+    m, e, k, n, r = size
+    x, w, a, b, off, _, s = [dev(t) for t in make(m, e, k, n, r, "bf16", "skew", False, True, 4)]
+    dy = dev(rand(5, m, n).bfloat16())
+
+    def step():
+        y, h = kn.adapted_linear(x, w, a, b, off, scales=s, want_h=True)
+        return [y, h, *kn.adapted_linear_backward(dy, x, h, w, a, b, off, scales=s)]
+
+    want = [v.clone() for v in step()]
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        got = step()
+    torch.cuda.current_stream().wait_stream(other)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for i in range(4):
+        for v in got:
+            v.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, want)), i
+        assert all(torch.equal(p, q) for p, q in zip(step(), want))
+
+
+def test_adapted_refusals_of_the_library():
+    L, n, p = kn.load_library(), C.c_int64(), 4096  # (an address that is never dereferenced)
+
+    def desc(**kw):
+        d = dict(dtype=2, w_layout=0, experts=4, n_in=8, n_out=8, rows=16, x_rows=16, ldx=8)
+        d.update(kw)
+        return C.byref(kn.LinearDesc(*[d[f] for f, _ in kn.LinearDesc._fields_]))
+
+    forward = lambda d=desc(), rank=4, x=p, w=p, a=p, b=p, off=p, rows=None, y=p, h=None, ws=p, size=1 << 30: L.kn_adapted_linear(  # noqa: E731
+        None, d, rank, x, w, a, b, None, None, off, rows, 0, y, h, ws, size)
+    backward = lambda d=desc(), rank=4, dy=p, x=p, h=p, w=p, a=p, b=p, off=p, rows=None, dx=p, da=p, db=p, ws=p, size=1 << 30: L.kn_adapted_linear_backward(  # noqa: E731
+        None, d, rank, dy, x, h, w, a, b, None, off, rows, 0, dx, da, db, ws, size)
+    bytes_ = [lambda d=desc(), rank=4, f=f: f(d, rank, C.byref(n)) for f in (L.kn_adapted_linear_workspace_bytes, L.kn_adapted_linear_backward_workspace_bytes)]
+    for call in (forward, backward, *bytes_):
+        assert call(d=None) == -1 and call(rank=0) == -1 and call(rank=(1 << 20) + 1) == -2
+        for bad in (dict(dtype=3), dict(w_layout=2), dict(experts=0), dict(n_in=0), dict(n_out=0), dict(rows=-1), dict(x_rows=-1), dict(ldx=7)):
+            assert call(d=desc(**bad)) == -1, bad
+        for much in (dict(experts=65536), dict(n_in=(1 << 20) + 1, ldx=1 << 21), dict(n_out=(1 << 20) + 1), dict(rows=(1 << 30) + 1, x_rows=1 << 30)):
+            assert call(d=desc(**much)) == -2, much
+    for bad in (dict(x=None), dict(w=None), dict(a=None), dict(b=None), dict(off=None), dict(y=None), dict(h=p + 8), dict(d=desc(x_rows=8))):
+        assert forward(**bad) == -1, bad
+    for bad in (dict(dy=None), dict(x=None), dict(h=None), dict(h=p + 8), dict(w=None), dict(a=None), dict(b=None), dict(off=None), dict(dx=None), dict(da=None), dict(db=None),
+                dict(d=desc(x_rows=8))):
+        assert backward(**bad) == -1, bad
+    for call, size in ((forward, bytes_[0]), (backward, bytes_[1])):
+        assert size() == 0 and n.value > 0 and n.value % 256 == 0
+        assert call(ws=None) == -3 and call(ws=p + 8) == -3 and call(size=n.value - 1) == -3
+    assert L.kn_adapted_linear_workspace_bytes(desc(), 4, None) == -1 and L.kn_adapted_linear_backward_workspace_bytes(desc(), 4, None) == -1
+    assert forward(d=desc(rows=0), x=None, w=None, a=None, b=None, off=None, y=None, ws=None, size=0) == 0
+
+
+@pytest.mark.gpu
+def test_adapted_refusals_of_the_binding(monkeypatch):
+    x, w, a, b = torch.zeros(8, 4).cuda(), torch.zeros(4, 6).cuda(), torch.zeros(2, 4, 3).cuda(), torch.zeros(2, 3, 6).cuda()
+    off, h, dy = torch.zeros(3, dtype=torch.int32).cuda(), torch.zeros(8, 4).cuda(), torch.zeros(8, 6).cuda()
+    f, g = kn.adapted_linear, kn.adapted_linear_backward
+    for bad in (lambda: f(x.half(), w, a, b, off), lambda: f(x, w, a.half(), b, off), lambda: f(x[:, :3], w, a, b, off), lambda: f(x, w, a, b[:, :2], off),
+                lambda: f(x, w, a[:1], b, off), lambda: f(x, w[None], a, b, off), lambda: f(x, w, a, b, off[:2]), lambda: f(x, w, a, b, off.long()),
+                lambda: f(x, w, a.transpose(1, 2).contiguous().transpose(1, 2), b, off), lambda: f(x.cpu(), w, a, b, off), lambda: f(x, w.cpu(), a, b, off),
+                lambda: f(x, w, a, b, off, scales=torch.ones(3).cuda()), lambda: f(x, w, a, b, off, scales=torch.ones(2).half().cuda()),
+                lambda: f(x, w, a, b, off, bias=torch.ones(2, 6).cuda()), lambda: f(x, w, a, b, off, rows=torch.zeros(8).cuda()), lambda: f(x, w, a, b, off, out=dy[:7]),
+                lambda: f(x.double(), w.double(), a.double(), b.double(), off), lambda: g(dy[:7], x, h, w, a, b, off), lambda: g(dy, x, h[:, :3], w, a, b, off),
+                lambda: g(dy, x, h.half(), w, a, b, off)):
+        with pytest.raises(kn.KnError):
+            bad()
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)  # (as if another device were the current one)
+    for call in (lambda: f(x, w, a, b, off), lambda: g(dy, x, h, w, a, b, off), lambda: kn.save_f8(x), lambda: kn.route_balance(x, 2, torch.zeros(5, dtype=torch.int32).cuda())):
+        with pytest.raises(kn.KnError, match="device"):
+            call()

@@ -242,3 +242,25 @@ def test_balance_refusals_of_the_binding():
                 lambda: kn.route_balance_backward(l, 2, counts, g, add=l.half()), lambda: kn.route_balance_backward(l, 2, counts, g, add=l[:7])):
         with pytest.raises(kn.KnError):
             bad()
+
+
+@pytest.mark.gpu
+def test_balance_rows_beyond_32_bits():
+    """Logits of 4 GiB and more: the sums are those of a distribution that repeats, the last rows' gradient that of a short call with the same counts."""
+    t, e, k = (1 << 21) + 640, 1024, 2
+    part, _ = make(640, e, k, "bf16", True, 4)
+    part = dev(part)
+    l = torch.empty(t, e, dtype=torch.bfloat16, device="cuda")
+    assert l.numel() * 2 > 1 << 32
+    l[:1 << 21] = part[:512].repeat(1 << 12, 1)
+    l[1 << 21:] = part
+    off = torch.arange(e + 1, dtype=torch.int32).cuda() * (t * k // e)
+    losses, counts, probs = kn.route_balance(l, k, off)
+    there = (part > -math.inf).any(1)
+    p = torch.where(there[:, None], torch.softmax(part.double(), 1), 0.0)
+    want = p[:512].sum(0) * (1 << 12) + p.sum(0)
+    assert int(counts[-1]) == int(there[:512].sum()) * (1 << 12) + int(there.sum())
+    assert ((probs.double() - want).abs() <= ((e + 256) * 2.0 ** -23 + 160 * 2.0 ** -24) * want).all()
+    g = torch.tensor([float(t), 0.01 * t]).cuda()
+    d = kn.route_balance_backward(l, k, counts, g)
+    assert torch.equal(d[-640:], kn.route_balance_backward(part, k, counts, g))
