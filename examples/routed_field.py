@@ -5,7 +5,11 @@ for a point's encoding, the best ``k`` evaluate it, and their results are summed
 is ``route``, two ``grouped_linear`` layers, ``combine`` and the gradients of all of them; serving runs the same layers through
 ``quantize_f8`` / ``grouped_linear_f8`` on weights that were brought to 8 bits once.
 
-    python examples/routed_field.py [--steps N]
+Lean training keeps the layers' inputs in 8 bits until the backward pass (``save_f8``, ``grouped_linear_backward_saved``), and adds the
+router's balance losses to what is learned (``route_balance``).  An ``Adapter`` fits a trained field's last layer to a
+variant of what it learned by a low-rank product per network, beside that layer's mean weights (``adapted_linear``).
+
+    python examples/routed_field.py [--steps N] [--lean]
 """
 import argparse
 import math
@@ -17,7 +21,8 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2103_13744_amd as kn  # noqa: E402
 
-EXPERTS, K, HIDDEN, OUT, FREQUENCIES = 16, 2, 128, 8, 6
+EXPERTS, K, HIDDEN, OUT, FREQUENCIES, RANK = 16, 2, 128, 8, 6, 8
+SCALE = 1024.0  # of losses before their gradients are taken
 INPUTS = 3 + 6 * FREQUENCIES
 DTYPE = torch.bfloat16  # of the networks' layers; the router and the master weights are float32
 
@@ -37,15 +42,30 @@ def target(points):
     return torch.stack([a, b, a * b, side, y * z, torch.sin(6.0 * x), a - b, b * side], dim=1)
 
 
+class Adam:
+    """First and second moments of parameters that are float32."""
+
+    def __init__(self, params):
+        self.params, self.moments, self.step_no = params, {n: (torch.zeros_like(p), torch.zeros_like(p)) for n, p in params.items()}, 0
+
+    def step(self, grads, rate):
+        self.step_no += 1
+        for name, param in self.params.items():
+            g, (m, v) = grads[name], self.moments[name]
+            m.mul_(0.9).add_(g, alpha=0.1)
+            v.mul_(0.99).addcmul_(g, g, value=0.01)
+            param.addcdiv_(m / (1.0 - 0.9 ** self.step_no), (v / (1.0 - 0.99 ** self.step_no)).sqrt_().add_(1e-12), value=-rate)
+
+
 class RoutedField:
-    def __init__(self, seed=0):
+    def __init__(self, seed=0, lean=False):
         g = torch.Generator(device="cuda").manual_seed(seed)
         randn = lambda *shape: torch.randn(shape, generator=g, device="cuda")  # noqa: E731
         self.params = {"router": 0.1 * randn(INPUTS, EXPERTS), "w1": randn(EXPERTS, INPUTS, HIDDEN) * math.sqrt(2.0 / INPUTS),
                        "b1": torch.zeros(EXPERTS, HIDDEN, device="cuda"), "w2": randn(EXPERTS, HIDDEN, OUT) / math.sqrt(HIDDEN),
                        "b2": torch.zeros(EXPERTS, OUT, device="cuda")}
-        self.moments = {n: (torch.zeros_like(p), torch.zeros_like(p)) for n, p in self.params.items()}
-        self.step_no = 0
+        self.adam = Adam(self.params)
+        self.lean, self.losses = lean, torch.tensor([1e-2, 1e-3], device="cuda") * SCALE  # (weights of the router's losses)
         self.eight = None
 
     def forward(self, enc):
@@ -57,24 +77,32 @@ class RoutedField:
         y = kn.grouped_linear(hidden, p["w2"], offsets, bias=p["b2"])
         return kn.combine(y, slots, weights), (p, x, logits, weights, ids, slots, rows, offsets, hidden, y)
 
-    def train_step(self, enc, want, rate=3e-3):
-        """One step of Adam on the mean squared error; the loss before it."""
+    def gradients(self, enc, want):
+        """The mean squared error, and its gradients (lean: with the router's losses, from inputs that were kept in 8 bits)."""
         out, (p, x, logits, weights, ids, slots, rows, offsets, hidden, y) = self.forward(enc)
+        if self.lean:  # the layers' inputs are not needed any more
+            x, hidden = kn.save_f8(x), kn.save_f8(hidden)
         diff = out.float() - want
-        dout = (2.0 / diff.numel() * 1024.0 * diff).to(DTYPE)  # (scaled: gradients of a mean are small in 16 bits)
+        dout = (2.0 / diff.numel() * SCALE * diff).to(DTYPE)  # (scaled: gradients of a mean are small in 16 bits)
         dy, dweights = kn.combine_backward(dout, y, slots, weights)
-        dhidden, dw2, db2 = kn.grouped_linear_backward(dy, hidden, p["w2"], offsets, relu_in=True)
-        dw1, db1 = kn.grouped_linear_dw(dhidden, x, p["w1"], offsets, rows=rows)
         dlogits = kn.route_backward(logits, weights, ids, dweights)
+        if self.lean:
+            dhidden, dw2, db2 = kn.grouped_linear_backward_saved(dy, *hidden, p["w2"], offsets, relu_in=True)
+            dw1, db1 = kn.grouped_linear_dw_saved(dhidden, *x, p["w1"], offsets, rows=rows)
+            _, counts, _ = kn.route_balance(logits, K, offsets)
+            dlogits = kn.route_balance_backward(logits, K, counts, self.losses, add=dlogits)
+        else:
+            dhidden, dw2, db2 = kn.grouped_linear_backward(dy, hidden, p["w2"], offsets, relu_in=True)
+            dw1, db1 = kn.grouped_linear_dw(dhidden, x, p["w1"], offsets, rows=rows)
         grads = {"router": enc.t() @ dlogits, "w1": dw1, "b1": db1, "w2": dw2, "b2": db2}
-        self.step_no += 1
-        for name, param in self.params.items():
-            g, (m, v) = grads[name].float() / 1024.0, self.moments[name]
-            m.mul_(0.9).add_(g, alpha=0.1)
-            v.mul_(0.99).addcmul_(g, g, value=0.01)
-            param.addcdiv_(m / (1.0 - 0.9 ** self.step_no), (v / (1.0 - 0.99 ** self.step_no)).sqrt_().add_(1e-12), value=-rate)
+        return diff.square().mean(), {n: g.float() / SCALE for n, g in grads.items()}
+
+    def train_step(self, enc, want, rate=3e-3):
+        """One step of Adam; the mean squared error before it."""
+        loss, grads = self.gradients(enc, want)
+        self.adam.step(grads, rate)
         self.eight = None
-        return diff.square().mean()
+        return loss
 
     def serve(self, enc):
         """The same field from weights in 8 bits, which are made once."""
@@ -88,11 +116,40 @@ class RoutedField:
         return kn.combine(y, slots, weights)
 
 
-def main(steps=400, batch=8192, say=print):
+class Adapter:
+    """A variant of a trained field: its last layer is the mean of the networks' with a low-rank product of each one's own, which alone is trained."""
+
+    def __init__(self, field, rank=RANK, seed=0):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.field, self.w, self.bias = field, field.params["w2"].mean(0).to(DTYPE), field.params["b2"].mean(0).to(DTYPE)
+        self.scales = torch.full((EXPERTS,), 2.0, device="cuda")
+        self.params = {"a": torch.randn((EXPERTS, HIDDEN, rank), generator=g, device="cuda") / math.sqrt(HIDDEN), "b": torch.zeros(EXPERTS, rank, OUT, device="cuda")}
+        self.adam = Adam(self.params)
+
+    def forward(self, enc):
+        _, (_, _, _, weights, _, slots, _, offsets, hidden, _) = self.field.forward(enc)
+        layer = (self.w, self.params["a"].to(DTYPE), self.params["b"].to(DTYPE), offsets)
+        y, h = kn.adapted_linear(hidden, *layer, scales=self.scales, bias=self.bias, want_h=True)
+        return kn.combine(y, slots, weights), (hidden, h, layer, weights, slots, y)
+
+    def gradients(self, enc, want):
+        out, (hidden, h, layer, weights, slots, y) = self.forward(enc)
+        diff = out.float() - want
+        dy, _ = kn.combine_backward((2.0 / diff.numel() * SCALE * diff).to(DTYPE), y, slots, weights)
+        _, da, db = kn.adapted_linear_backward(dy, hidden, h, *layer, scales=self.scales)
+        return diff.square().mean(), {"a": da.float() / SCALE, "b": db.float() / SCALE}
+
+    def train_step(self, enc, want, rate=1e-2):
+        loss, grads = self.gradients(enc, want)
+        self.adam.step(grads, rate)
+        return loss
+
+
+def main(steps=400, batch=8192, say=print, lean=False):
     """Trains for so many steps; (loss at the start, at the end, of the field served in 8 bits)."""
     kn.load_library()
     g = torch.Generator(device="cuda").manual_seed(1)
-    field, losses = RoutedField(), []
+    field, losses = RoutedField(lean=lean), []
     for i in range(steps):
         points = torch.rand((batch, 3), generator=g, device="cuda")
         losses.append(field.train_step(encode(points), target(points)))
@@ -102,10 +159,18 @@ def main(steps=400, batch=8192, say=print):
     full = float((field.forward(encode(points))[0].float() - target(points)).square().mean())
     eight = float((field.serve(encode(points)).float() - target(points)).square().mean())
     say("new points: loss %.5f in bfloat16, %.5f served in 8 bits" % (full, eight))
+    adapter = Adapter(field)
+    for i in range(steps // 2):
+        points = torch.rand((batch, 3), generator=g, device="cuda")
+        loss = adapter.train_step(encode(points), target(points.flip(1)))  # (the same field, seen from another side)
+        if i % max(1, steps // 8) == 0:
+            say("adapters, step %4d  loss %.5f" % (i, float(loss)))
     return float(losses[0]), full, eight
 
 
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--steps", type=int, default=400)
-    main(ap.parse_args().steps)
+    ap.add_argument("--lean", action="store_true", help="keep the layers' inputs in 8 bits, add the router's losses")
+    args = ap.parse_args()
+    main(args.steps, lean=args.lean)

@@ -110,3 +110,65 @@ def test_a_training_step_in_a_graph():
         assert all(torch.equal(got[n], want[n]) for n in want), i
         again, _ = step(v)
         assert all(torch.equal(again[n], want[n]) for n in want)
+
+
+def example():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "routed_field.py")
+    spec = importlib.util.spec_from_file_location("routed_field", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+@pytest.mark.gpu
+def test_the_example_runs_lean_and_with_adapters():
+    m = example()
+    said = []
+    first, full, eight = m.main(steps=8, batch=500, say=said.append, lean=True)
+    assert all(math.isfinite(v) for v in (first, full, eight)) and any("adapters" in line for line in said)
+
+
+@pytest.mark.gpu
+def test_the_examples_lean_gradients():
+    """A kept value is within 2^-4 of the input (or, for the smallest, 2^-9 of a two-hundred-and-fortieth of its block's largest), and has its sign: the biases' gradients
+    are the same bits, and each of the weights' within that share of the sum of its terms' magnitudes, and two roundings to bfloat16 and the sums'."""
+    m = example()
+    points = torch.rand((700, 3), generator=torch.Generator().manual_seed(1)).cuda()
+    enc, want = m.encode(points), m.target(points)
+    plain, lean = m.RoutedField(seed=3), m.RoutedField(seed=3, lean=True)
+    lean.losses.zero_()
+    (l1, g1), (l2, g2) = plain.gradients(enc, want), lean.gradients(enc, want)
+    assert torch.equal(l1, l2) and torch.equal(g1["b1"], g2["b1"]) and torch.equal(g1["b2"], g2["b2"])
+    assert ((g1["router"] - g2["router"]).abs() <= 2.0 ** -20 * g1["router"].abs().max()).all()
+    out, (p, x, logits, weights, ids, slots, rows, off, hidden, y) = plain.forward(enc)
+    diff = out.float() - want
+    dy, _ = kn.combine_backward((2.0 / diff.numel() * m.SCALE * diff).to(m.DTYPE), y, slots, weights)
+    dh = kn.grouped_linear_dx(dy, hidden, p["w2"], off, relu_in=True)
+    for name, xs, d in (("w1", x[rows.long()], dh), ("w2", hidden, dy)):
+        for e, (i, j) in enumerate(zip(off[:-1].tolist(), off[1:].tolist())):
+            a, b = xs[i:j].double(), d[i:j].double().abs()
+            far = torch.maximum(a.abs() * 2.0 ** -4, a.abs().amax(1, keepdim=True) * 2.0 ** -9 / 224.0)
+            bound = (far.t() @ b + (j - i + 8) * 2.0 ** -22 * (a.abs().t() @ b)) / m.SCALE
+            assert ((g1[name][e] - g2[name][e]).double().abs() <= 1.01 * bound + 2.0 ** -8 * (g1[name][e].abs() + g2[name][e].abs())).all()
+
+
+@pytest.mark.gpu
+def test_the_examples_adapter_gradients_against_differences():
+    """The error along a direction, by central differences of 1 % of b: its gradient is smooth (the error is quadratic in b), and the rest is bfloat16's rounding of the results:
+    2^-8 of each, half of them at random signs over 500 points of 8, so that a fiftieth of the gradient's own size is more than it can be off."""
+    m = example()
+    field = m.RoutedField(seed=2)
+    adapter = m.Adapter(field)
+    points = torch.rand((500, 3), generator=torch.Generator().manual_seed(1)).cuda()
+    enc, want = m.encode(points), m.target(points.flip(1))
+    adapter.params["b"].copy_(0.3 * rand(4, *adapter.params["b"].shape).cuda())
+    _, grads = adapter.gradients(enc, want)
+    way, b = grads["b"] / grads["b"].norm(), adapter.params["b"].clone()
+    step, at = 0.5, []
+    for sign in (1.0, -1.0):
+        adapter.params["b"].copy_(b + sign * step * way)
+        at.append(float((adapter.forward(enc)[0].float() - want).double().square().mean()))
+    slope, said = (at[0] - at[1]) / (2 * step), float((grads["b"].double() * way.double()).sum())
+    assert abs(slope - said) <= 0.02 * abs(said), (slope, said)
