@@ -169,11 +169,11 @@ def _stream():
 
 
 def _stream_on(*tensors):
-    """``_stream()``, of a call on these tensors: what lies on another device than the current one is refused (None: no tensor)."""
+    """``_stream()``, of a call on these tensors: what lies on the host or on another device than the current one is refused (None: no tensor)."""
     device = torch._C._cuda_getDevice()
     for t in tensors:
         if t is not None and t.get_device() != device:
-            raise KnError("a tensor is on device %d, and the current device is %d" % (t.get_device(), device))
+            raise KnError("a tensor is on device %d (-1: the host), and the current device is %d" % (t.get_device(), device))
     return torch._C._cuda_getCurrentRawStream(device)
 
 
@@ -641,14 +641,13 @@ def grouped_linear_backward(dy, x, w, offsets, rows=None, relu_in=False, want_bi
 
 def _adapted_args(x, w, a, b, offsets, rows, scales):
     """(desc, M, rank, pointers of x, w, a, b, scales, offsets, rows): weights that are all contiguous, or all transposes of contiguous ones."""
-    if w.dim() != 2 or a.dim() != 3 or b.dim() != 3:
-        raise KnError("expected weights (n_in, n_out), (networks, n_in, rank) and (networks, rank, n_out), got %s, %s, %s" % (tuple(w.shape), tuple(a.shape), tuple(b.shape)))
+    sa, sb, dtype = a.shape, b.shape, x.dtype
+    if w.dim() != 2 or len(sa) != 3 or len(sb) != 3:
+        raise KnError("expected weights (n_in, n_out), (networks, n_in, rank) and (networks, rank, n_out), got %s, %s, %s" % (tuple(w.shape), tuple(sa), tuple(sb)))
     K, N = w.shape
-    E, _, rank = a.shape
-    if a.shape != (E, K, rank) or b.shape != (E, rank, N) or not x.dtype is w.dtype is a.dtype is b.dtype:
+    E, ka, rank = sa
+    if ka != K or sb[0] != E or sb[1] != rank or sb[2] != N or w.dtype is not dtype or a.dtype is not dtype or b.dtype is not dtype:
         raise KnError("expected weights (%d, %d), (%d, %d, %d) and (%d, %d, %d) of one dtype with x" % (K, N, E, K, rank, E, rank, N))
-    if not (w.is_cuda and a.is_cuda and b.is_cuda):
-        raise KnError("weights must be device tensors")
     if w.is_contiguous() and a.is_contiguous() and b.is_contiguous():
         layout = 0
     elif (w.stride() == (1, K) and a.stride() == (K * rank, 1, K) and b.stride() == (rank * N, 1, rank)) or (

@@ -1036,7 +1036,7 @@ int dw_bytes(const kn_linear_desc *d, int32_t rank, int64_t *out)
     KN_TRY(kn_linear_dw_bytes(&a, true, &na));
     KN_TRY(kn_linear_dw_bytes(&b, true, &nb));
     const int64_t few = few_bytes(d->rows, d->n_in, d->n_out, kn_item(d->dtype)); // (done with before the others begin)
-    *out = na > nb ? na : nb;
+    *out = na + nb;
     *out = few > *out ? few : *out;
     return KN_OK;
 }
@@ -1111,6 +1111,5 @@ extern "C" int kn_adapted_linear_backward(void *stream, const kn_linear_desc *d,
         KN_TRY(run((hipStream_t)stream, d->dtype, !io, down, p, beside, (float *)sums));
     }
     const kn_linear_desc la = layer_of(d, d->n_in, rank, d->x_rows, d->ldx), lb = layer_of(d, rank, d->n_out, d->rows, rp);
-    KN_TRY(kn_linear_dw_run(stream, &la, x, nullptr, g, rp, offsets, rows, da, nullptr, sums, dw, true));
-    return kn_linear_dw_run(stream, &lb, h, nullptr, dy, N, offsets, nullptr, db, nullptr, sums, dw, true);
+    return kn_linear_dw_low_rank(stream, &la, x, g, rp, rows, da, &lb, h, dy, N, db, offsets, sums, dw);
 }

@@ -131,11 +131,14 @@ struct KnProduct {
 constexpr int KN_SAVED_BLOCK = 128;
 static inline int64_t kn_saved_bytes(int64_t K) { return kn_align_up(K, 16); }
 
-// kn_grouped_linear_dw, with rows of dy that may lie apart; exponents: x is what kn_save_f8 left; thin: the narrower of x and dy is a low-rank product's, rows of whole
-// 16 bytes
-int kn_linear_dw_bytes(const kn_linear_desc *d, bool thin, int64_t *out_bytes);
+// kn_grouped_linear_dw, with rows of dy that may lie apart; exponents: x is what kn_save_f8 left
 int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const uint8_t *exponents, const void *dy, int64_t lddy, const int32_t *offsets, const int32_t *rows,
-                     void *dw, void *db, void *workspace, int64_t workspace_bytes, bool thin = false);
+                     void *dw, void *db, void *workspace, int64_t workspace_bytes);
+// Workspace of one of the two below (low_rank: whatever kernel it is)
+int kn_linear_dw_bytes(const kn_linear_desc *d, bool low_rank, int64_t *out_bytes);
+// The gradients of a low-rank product's factors, as layers of their own: a (n_in, rank) from x and g, b (rank, n_out) from h and dy
+int kn_linear_dw_low_rank(void *stream, const kn_linear_desc *da, const void *x, const void *g, int64_t ldg, const int32_t *rows, void *out_a, const kn_linear_desc *db,
+                          const void *h, const void *dy, int64_t lddy, void *out_b, const int32_t *offsets, void *workspace, int64_t workspace_bytes);
 
 // What the grouped products check alike
 static inline int kn_linear_check(const kn_linear_desc *d)

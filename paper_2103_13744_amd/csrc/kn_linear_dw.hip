@@ -249,16 +249,16 @@ __global__ void __launch_bounds__(WAVES * 64) k_reduce_small(KnProduct p, int32_
 // takes every WAVES-th step of rows by itself, asked for while another is multiplied, and they are summed in the order of their numbers.  TURN: 16-bit rows
 // of whole pieces, which an LDS of the wavefront's own turns into columns; else value by value, 16 neighbouring lanes, 16 neighbouring values.  Bound by
 // the long side's bytes.
+constexpr int thin_bytes(int fi, int fj) { return 16 * fi * (16 * fj + 4) * 4 > (fi + fj) * 1024 ? 16 * fi * (16 * fj + 4) * 4 : (fi + fj) * 1024; } // of a wavefront
 template <typename T, int FI, int FJ, bool TURN, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64) k_reduce_thin(KnProduct p, Parts parts)
+__device__ __forceinline__ void reduce_thin(const KnProduct &p, const Parts &parts, int32_t block, char *lds_)
 {
-    constexpr int W = 16 / sizeof(T), RS = 4 * W, LD = 16 * FJ + 4, OWN = 16 * FI * LD * 4 > (FI + FJ) * 1024 ? 16 * FI * LD * 4 : (FI + FJ) * 1024;
+    constexpr int W = 16 / sizeof(T), RS = 4 * W, LD = 16 * FJ + 4, OWN = thin_bytes(FI, FJ);
     typedef typename KnFrag<T>::Type Frag;
-    __shared__ __align__(16) char lds_[WAVES * OWN];
     const int tid = kn_thread(), lane = tid & 63, col = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     KN_LDS char *own = (KN_LDS char *)lds_ + wave * OWN;
     const int jtiles = (p.J + 16 * FJ - 1) / (16 * FJ), itiles = (p.I + 16 * FI - 1) / (16 * FI), tiles = itiles * jtiles;
-    const int32_t block = p.first + kn_block(), number = block % tiles;
+    const int32_t number = block % tiles;
     const KnPiece piece = kn_find_piece(p.offsets, p.E, p.M, parts.len, block / tiles);
     const int32_t group = piece.group;
     if (group >= p.E) return;
@@ -352,17 +352,33 @@ __global__ void __launch_bounds__(WAVES * 64) k_reduce_thin(KnProduct p, Parts p
         else out[at] = (T)y;
     }
 }
+// One such gradient, or two of one call side by side: a low-rank product's factors, the long side of one the first index and of the other the second
+struct Thin {
+    KnProduct p;
+    Parts parts;
+};
+template <typename T, int FI, int FJ, bool TURN, int WAVES> __global__ void __launch_bounds__(WAVES * 64) k_reduce_thin(Thin a)
+{
+    __shared__ __align__(16) char lds[WAVES * thin_bytes(FI, FJ)];
+    reduce_thin<T, FI, FJ, TURN, WAVES>(a.p, a.parts, a.p.first + kn_block(), lds);
+}
+template <typename T, int F, bool TURN, int WAVES> __global__ void __launch_bounds__(WAVES * 64) k_reduce_thin_pair(Thin tall, Thin wide, int32_t blocks)
+{
+    __shared__ __align__(16) char lds[WAVES * (thin_bytes(4, F) > thin_bytes(F, 4) ? thin_bytes(4, F) : thin_bytes(F, 4))];
+    const int32_t block = tall.p.first + kn_block();
+    if (block < blocks) reduce_thin<T, 4, F, TURN, WAVES>(tall.p, tall.parts, block, lds);
+    else reduce_thin<T, F, 4, TURN, WAVES>(wide.p, wide.parts, block - blocks, lds);
+}
 
 // The parts' sums of the networks that have several, in the order of the parts; `chunk` results per workgroup.  SEARCH: there are at most
 // M / len such networks, and a workgroup looks for its own among all (few networks of many results); else there is one for
 // every network's results, and most find nothing to do.  SPLIT: each wavefront sums a quarter of a network's parts, and the quarters are added
 // in order (50,560 rows of 25 networks 64 x 112, the longest of some 160 parts: 51 -> 17 us).
-template <typename T, bool SEARCH, bool SPLIT> __global__ void __launch_bounds__(256) k_reduce_join(KnProduct p, int32_t sum, Parts parts, int32_t chunk)
+template <typename T, bool SEARCH, bool SPLIT>
+__device__ __forceinline__ void reduce_join(const KnProduct &p, int32_t sum, const Parts &parts, int32_t chunk, int32_t block, int32_t *scratch, int32_t &found, float (*quarter)[64])
 {
-    __shared__ int32_t scratch[4], found;
-    __shared__ float quarter[4][64];
     const int64_t n = (int64_t)p.I * p.J;
-    const int32_t pieces = (int32_t)((n + chunk - 1) / chunk), block = p.first + kn_block(), turn = block / pieces;
+    const int32_t pieces = (int32_t)((n + chunk - 1) / chunk), turn = block / pieces;
     int32_t group = turn;
     if constexpr (SEARCH) {
         int32_t before = 0;
@@ -412,6 +428,22 @@ template <typename T, bool SEARCH, bool SPLIT> __global__ void __launch_bounds__
         ((T *)p.out_bias)[(int64_t)group * m + j] = (T)y;
     }
 }
+template <typename T, bool SEARCH, bool SPLIT> __global__ void __launch_bounds__(256) k_reduce_join(KnProduct p, int32_t sum, Parts parts, int32_t chunk)
+{
+    __shared__ int32_t scratch[4], found;
+    __shared__ float quarter[4][64];
+    reduce_join<T, SEARCH, SPLIT>(p, sum, parts, chunk, p.first + kn_block(), scratch, found, quarter);
+}
+// of two gradients of few results
+constexpr int32_t FEW_CHUNK = 256;
+template <typename T> __global__ void __launch_bounds__(256) k_reduce_join_pair(Thin a, Thin b, int32_t blocks)
+{
+    __shared__ int32_t scratch[4], found;
+    __shared__ float quarter[4][64];
+    const int32_t block = a.p.first + kn_block();
+    if (block < blocks) reduce_join<T, false, true>(a.p, SUM_NONE, a.parts, FEW_CHUNK, block, scratch, found, quarter);
+    else reduce_join<T, false, true>(b.p, SUM_NONE, b.parts, FEW_CHUNK, block - blocks, scratch, found, quarter);
+}
 
 // Layers of up to 64 x 64 whose rows are not whole pieces are k_reduce_small's (us, against 64 x 64 staged in the LDS: 524,291 rows, 4,096
 // networks 63 x 32: 57 and 63 in bf16, 91 and 123 in fp32; 262,145 rows, 1,600 networks 91 x 64: 109 and 52, 151 and 102).  Else tiles
@@ -457,27 +489,62 @@ int32_t part_length(const kn_linear_desc *d, bool thin)
 // A low-rank product's gradients, whose other side is longer than what the narrow layers' kernels take
 bool is_thin(const kn_linear_desc *d) { return (d->n_in <= 64) != (d->n_out <= 64); }
 
+// Few results, whose parts' sums are joined by more workgroups, a quarter of the parts for a wavefront
+bool few_results(const KnProduct &p, const Parts &parts)
+{
+    const int64_t most = p.M / parts.len, results = (int64_t)p.I * p.J;
+    return results * (most < p.E ? most : p.E) <= 1 << 20 && p.E * kn_div_up(results, FEW_CHUNK) <= 8192;
+}
 template <typename T> int launch_join(hipStream_t st, const KnProduct &p, int32_t sum, const Parts &parts);
 
-template <typename T, bool TURN> int launch_thin(hipStream_t st, const KnProduct &p, const Parts &parts)
+template <typename T, int FI, int FJ, bool TURN> int launch_thin_of(hipStream_t st, const Thin &a)
 {
-    auto launch = [&](auto fi, auto fj) -> int {
-        constexpr int FI = decltype(fi)::value, FJ = decltype(fj)::value;
-        const int64_t blocks = kn_pieces(p.M, p.E, parts.len) * kn_div_up(p.I, 16 * FI) * kn_div_up(p.J, 16 * FJ);
-        const bool many = many_rows(p.M, p.E);
-        return kn_launch(blocks, many ? 512 : 256, [&](dim3 grid, int32_t first) {
-            KnProduct q = p;
-            q.first = first;
-            if (many) hipLaunchKernelGGL((k_reduce_thin<T, FI, FJ, TURN, 8>), grid, dim3(512), 0, st, q, parts);
-            else hipLaunchKernelGGL((k_reduce_thin<T, FI, FJ, TURN, 4>), grid, dim3(256), 0, st, q, parts);
-        });
-    };
-    std::integral_constant<int, 1> one;
-    std::integral_constant<int, 2> two;
-    std::integral_constant<int, 4> four;
-    if (p.I <= p.J) KN_TRY(p.I <= 16 ? launch(one, four) : p.I <= 32 ? launch(two, four) : launch(four, four));
-    else KN_TRY(p.J <= 16 ? launch(four, one) : p.J <= 32 ? launch(four, two) : launch(four, four));
-    return launch_join<T>(st, p, SUM_NONE, parts);
+    const int64_t blocks = kn_pieces(a.p.M, a.p.E, a.parts.len) * kn_div_up(a.p.I, 16 * FI) * kn_div_up(a.p.J, 16 * FJ);
+    const bool many = many_rows(a.p.M, a.p.E);
+    return kn_launch(blocks, many ? 512 : 256, [&](dim3 grid, int32_t first) {
+        Thin q = a;
+        q.p.first = first;
+        if (many) hipLaunchKernelGGL((k_reduce_thin<T, FI, FJ, TURN, 8>), grid, dim3(512), 0, st, q);
+        else hipLaunchKernelGGL((k_reduce_thin<T, FI, FJ, TURN, 4>), grid, dim3(256), 0, st, q);
+    });
+}
+template <typename T, bool TURN> int launch_thin(hipStream_t st, const Thin &a)
+{
+    const int32_t I = a.p.I, J = a.p.J;
+    KN_TRY((I <= J ? I <= 16 ? launch_thin_of<T, 1, 4, TURN>(st, a) : I <= 32 ? launch_thin_of<T, 2, 4, TURN>(st, a) : launch_thin_of<T, 4, 4, TURN>(st, a)
+                   : J <= 16 ? launch_thin_of<T, 4, 1, TURN>(st, a) : J <= 32 ? launch_thin_of<T, 4, 2, TURN>(st, a) : launch_thin_of<T, 4, 4, TURN>(st, a)));
+    return launch_join<T>(st, a.p, SUM_NONE, a.parts);
+}
+template <typename T, int F, bool TURN> int launch_pair_of(hipStream_t st, const Thin &tall, const Thin &wide)
+{
+    const int64_t pieces = kn_pieces(tall.p.M, tall.p.E, tall.parts.len), blocks = pieces * kn_div_up(tall.p.I, 64) * kn_div_up(tall.p.J, 16 * F);
+    const int64_t all = blocks + pieces * kn_div_up(wide.p.I, 16 * F) * kn_div_up(wide.p.J, 64);
+    const bool many = many_rows(tall.p.M, tall.p.E);
+    if (all > 0x7fffffffLL) return KN_E_UNSUPPORTED;
+    return kn_launch(all, many ? 512 : 256, [&](dim3 grid, int32_t first) {
+        Thin q = tall;
+        q.p.first = first;
+        if (many) hipLaunchKernelGGL((k_reduce_thin_pair<T, F, TURN, 8>), grid, dim3(512), 0, st, q, wide, (int32_t)blocks);
+        else hipLaunchKernelGGL((k_reduce_thin_pair<T, F, TURN, 4>), grid, dim3(256), 0, st, q, wide, (int32_t)blocks);
+    });
+}
+// Two at once: a launch less, and one's last workgroups run beside the other's (8,192 rows of 16 networks 1024 x 2048, rank 16 in bf16, with the joins 34 -> 21 us)
+template <typename T, bool TURN> int launch_pair(hipStream_t st, const Thin &a, const Thin &b)
+{
+    const Thin &tall = a.p.I > a.p.J ? a : b, &wide = a.p.I > a.p.J ? b : a;
+    const int32_t rank = tall.p.J;
+    KN_TRY((rank <= 16 ? launch_pair_of<T, 1, TURN>(st, tall, wide) : rank <= 32 ? launch_pair_of<T, 2, TURN>(st, tall, wide) : launch_pair_of<T, 4, TURN>(st, tall, wide)));
+    if (tall.p.M <= tall.parts.len) return KN_OK;
+    if (!few_results(tall.p, tall.parts) || !few_results(wide.p, wide.parts)) {
+        KN_TRY(launch_join<T>(st, tall.p, SUM_NONE, tall.parts));
+        return launch_join<T>(st, wide.p, SUM_NONE, wide.parts);
+    }
+    const int64_t blocks = tall.p.E * kn_div_up((int64_t)tall.p.I * tall.p.J, FEW_CHUNK), all = blocks + wide.p.E * kn_div_up((int64_t)wide.p.I * wide.p.J, FEW_CHUNK);
+    return kn_launch(all, 256, [&](dim3 grid, int32_t first) {
+        Thin q = tall;
+        q.p.first = first;
+        hipLaunchKernelGGL((k_reduce_join_pair<T>), grid, dim3(256), 0, st, q, wide, (int32_t)blocks);
+    });
 }
 
 template <typename T, bool DIRECT, int SAVED>
@@ -522,8 +589,8 @@ template <typename T> int launch_join(hipStream_t st, const KnProduct &p, int32_
 {
     if (p.M <= parts.len) return KN_OK; // (no network has several)
     const int64_t most = p.M / parts.len, results = (int64_t)p.I * p.J;
-    const bool few = results * (most < p.E ? most : p.E) <= 1 << 20 && p.E * kn_div_up(results, 256) <= 8192;
-    const int32_t chunk = few ? 256 : 4096; // (few results: more workgroups, whose wavefronts take a quarter of the parts each)
+    const bool few = few_results(p, parts);
+    const int32_t chunk = few ? FEW_CHUNK : 4096;
     const int64_t pieces = kn_div_up(results, chunk);
     const bool search = most < p.E && p.E * pieces > 8192;
     const int64_t joins = (search ? most : p.E) * pieces;
@@ -568,15 +635,11 @@ extern "C" int kn_grouped_linear_dw_saved(void *stream, const kn_linear_desc *d,
     return kn_linear_dw_run(stream, &whole, q, exponents ? exponents : &none, dy, d->n_out, offsets, rows, dw, db, workspace, workspace_bytes);
 }
 
-int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const uint8_t *exponents, const void *dy, int64_t lddy, const int32_t *offsets,
-                     const int32_t *rows, void *dw, void *db, void *workspace, int64_t workspace_bytes, bool thin)
+// Both operands and the result of a gradient (thin: a low-rank factor's)
+namespace {
+Thin product_of(const kn_linear_desc *d, const void *x, const void *dy, int64_t lddy, const int32_t *offsets, const int32_t *rows, void *dw, void *db, void *workspace, bool thin)
 {
-    thin = thin && is_thin(d);
-    if (!offsets || !dw || (d->rows > 0 && (!dy || (d->x_rows > 0 && !x))) || (d->rows > 0 && !rows && d->x_rows < d->rows)) return KN_E_INVALID_ARG;
-    int64_t need = 0;
-    KN_TRY(kn_linear_dw_bytes(d, thin, &need));
-    if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return KN_E_WORKSPACE;
-    Parts parts = {part_length(d, thin), (float *)workspace, nullptr};
+    Parts parts = {part_length(d, thin && is_thin(d)), (float *)workspace, nullptr};
     parts.bias_sums = parts.sums + part_places(d->rows, parts.len) * (int64_t)d->n_in * d->n_out;
     KnProduct p = {};
     const bool io = d->w_layout == KN_W_IN_OUT; // (columns are what is contiguous in dw)
@@ -587,6 +650,25 @@ int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const
     p.a_rows = (int32_t)(io ? d->x_rows : d->rows); p.b_rows = (int32_t)(io ? d->rows : d->x_rows);
     p.out = dw; p.out_bias = db; p.offsets = offsets;
     p.o_group = (int64_t)d->n_in * d->n_out; p.o_i = p.J;
+    return {p, parts};
+}
+bool whole_rows(const KnProduct &p, int64_t V)
+{
+    return p.I % V == 0 && p.J % V == 0 && (((uintptr_t)p.a | (uintptr_t)p.b) & 15) == 0 && p.lda % V == 0 && p.ldb % V == 0;
+}
+} // namespace
+
+int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const uint8_t *exponents, const void *dy, int64_t lddy, const int32_t *offsets,
+                     const int32_t *rows, void *dw, void *db, void *workspace, int64_t workspace_bytes)
+{
+    if (!offsets || !dw || (d->rows > 0 && (!dy || (d->x_rows > 0 && !x))) || (d->rows > 0 && !rows && d->x_rows < d->rows)) return KN_E_INVALID_ARG;
+    int64_t need = 0;
+    KN_TRY(kn_grouped_linear_dw_workspace_bytes(d, &need));
+    if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return KN_E_WORKSPACE;
+    const bool io = d->w_layout == KN_W_IN_OUT;
+    const Thin t = product_of(d, x, dy, lddy, offsets, rows, dw, db, workspace, false);
+    const KnProduct &p = t.p;
+    const Parts &parts = t.parts;
     const int32_t sum = !db ? SUM_NONE : io ? SUM_B : SUM_A;
     return kn_with_type(d->dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
@@ -597,13 +679,31 @@ int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const
             if (io) return direct ? launch_reduce<E_, true, SAVED_A>(st, d, p, sum, parts, exponents) : launch_reduce<E_, false, SAVED_A>(st, d, p, sum, parts, exponents);
             return direct ? launch_reduce<E_, true, SAVED_B>(st, d, p, sum, parts, exponents) : launch_reduce<E_, false, SAVED_B>(st, d, p, sum, parts, exponents);
         }
-        const bool direct = p.I % V == 0 && p.J % V == 0 && (((uintptr_t)p.a | (uintptr_t)p.b) & 15) == 0 && p.lda % V == 0 && p.ldb % V == 0;
-        if (thin) {
-            if constexpr (sizeof(E_) == 2) {
-                if (direct) return launch_thin<E_, true>(st, p, parts);
-            }
-            return launch_thin<E_, false>(st, p, parts);
-        }
+        const bool direct = whole_rows(p, V);
         return direct ? launch_reduce<E_, true, SAVED_NONE>(st, d, p, sum, parts, nullptr) : launch_reduce<E_, false, SAVED_NONE>(st, d, p, sum, parts, nullptr);
+    });
+}
+
+int kn_linear_dw_low_rank(void *stream, const kn_linear_desc *da, const void *x, const void *g, int64_t ldg, const int32_t *rows, void *out_a, const kn_linear_desc *db,
+                          const void *h, const void *dy, int64_t lddy, void *out_b, const int32_t *offsets, void *workspace, int64_t workspace_bytes)
+{
+    int64_t na = 0, nb = 0;
+    KN_TRY(kn_linear_dw_bytes(da, true, &na));
+    KN_TRY(kn_linear_dw_bytes(db, true, &nb));
+    if (na + nb > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < na + nb)) return KN_E_WORKSPACE;
+    char *ws_b = (char *)workspace + na;
+    const Thin a = product_of(da, x, g, ldg, offsets, rows, out_a, nullptr, workspace, true), b = product_of(db, h, dy, lddy, offsets, nullptr, out_b, nullptr, ws_b, true);
+    const bool thin_a = is_thin(da), thin_b = is_thin(db);
+    hipStream_t st = (hipStream_t)stream;
+    return kn_with_type(da->dtype, [&](auto v) -> int {
+        typedef decltype(v) E_;
+        constexpr int64_t V = 16 / sizeof(E_);
+        constexpr bool TURNS = sizeof(E_) == 2;
+        const bool turn_a = TURNS && whole_rows(a.p, V), turn_b = TURNS && whole_rows(b.p, V);
+        if (thin_a && thin_b && turn_a == turn_b) return turn_a ? launch_pair<E_, TURNS>(st, a, b) : launch_pair<E_, false>(st, a, b);
+        if (thin_a) KN_TRY((turn_a ? launch_thin<E_, TURNS>(st, a) : launch_thin<E_, false>(st, a)));
+        else KN_TRY(kn_linear_dw_run(stream, da, x, nullptr, g, ldg, offsets, rows, out_a, nullptr, workspace, na));
+        if (thin_b) return turn_b ? launch_thin<E_, TURNS>(st, b) : launch_thin<E_, false>(st, b);
+        return kn_linear_dw_run(stream, db, h, nullptr, dy, lddy, offsets, nullptr, out_b, nullptr, ws_b, nb);
     });
 }
