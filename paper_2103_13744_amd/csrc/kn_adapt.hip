@@ -47,6 +47,8 @@ template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type stride
 // 16 U rows of one network by 16 V columns: a workgroup's WAVES wavefronts take turns of AHEAD steps of the contraction, straight into registers, one asked
 // for while another is multiplied, and are summed in the order of their numbers.  Where b's columns are contiguous (not its contraction) and in whole 16-byte
 // pieces, 16-bit values are turned by the transposing read of an LDS that each wavefront has for itself; else they are fetched one by one, eight for a fragment.
+// Bound by the rows' bytes: 16,384 rows of 12 networks, 2048 values, rank 32 in bf16: 24 us, 2.8 TB/s; 32,768 rows of 1024, rank 16: 18, 3.7 TB/s.  Two
+// fragments of rows and four wavefronts; one to four, two to eight, two or four steps under way: 23 to 33.
 enum { B_ROWS, B_COLS, B_PIECES };
 template <typename T, int B, int U, int V, int WAVES, int AHEAD> struct Sums {
     static constexpr int W = 16 / sizeof(T), KS = 4 * W, LD = 16 * V + 4, WORDS = WAVES * 16 * U * LD;
@@ -234,7 +236,8 @@ template <typename T, int B, int U, int V, int WAVES, int AHEAD> __global__ void
 }
 
 // Few rows (16 U at most): one launch leaves h and the shared product's sums, cut into parts of the contraction so that all of w is on its way at once; the
-// second adds the parts up and what h has to add.
+// second adds the parts up and what h has to add.  One row 2048 x 2048: 5.2 and 3.4 us; 48 rows of 32 networks 2048 x 2560, rank 16: 9.2 and 4.3 (as tiles, with
+// k_adapt_down before them, 17 and 20).
 struct Few {
     float *sums;       // (parts, M, J)
     int32_t parts, each; // of so many steps
@@ -462,6 +465,8 @@ template <typename T, int R, int NW, int LIST, bool COLS, bool DIRECT> struct Lo
 // stages of the shared contraction come those of the tile's networks.  There a row meets other networks' values with zeros, and a zero times what is not finite is a
 // NaN: networks with such values are left out, and their rows get their part at the end, value by value.  COLS: the columns of w and b are contiguous (else the contraction is).  DIRECT: rows
 // of whole 16-byte pieces throughout.
+// Measured: 16,384 rows of 12 networks 2048 x 2048, rank 32 in bf16: 154 us, 906 TFLOP/s, where one product of the library of 8192 x 8192 x 8192 reaches 1,221.  Tiles of
+// 192 x 128 (too few registers for two workgroups at a time): 222.
 // (128 x 128: registers for two workgroups at a time)
 template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB>
 __global__ void __launch_bounds__(WR * WC * 64, DIRECT && BM == 128 ? 4 : 1) k_adapt_up(KnProduct p, Beside beside, int32_t blocks)
@@ -646,7 +651,8 @@ template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type stride
 // Layers of the small networks' kind (contraction up to KF fragments, columns up to V of 16, or a few such tiles; a rank of up to 16), of any sizes, strides and
 // alignment: a wavefront takes SMALL_ROWS rows of one network by itself, the shared weights in the LDS, as fragments, and the network's own in its registers, and
 // makes h and y at once: rows are read once, and nothing goes through memory between the two products.  Lanes hand each other h where they hold four of a row's values
-// as results and take eight as an operand (16 bits; in fp32 both are the same four).
+// as results and take eight as an operand (16 bits; in fp32 both are the same four).  262,145 rows of 4,096 networks 63 x 32, rank 4: 45 us in fp32 (2.4 TB/s; the
+// matrix cores are busy a third of the time), 25 in bf16; with the shared weights in registers and by 64-bit addresses 49 and 29.
 constexpr int SMALL_ROWS = 32, SMALL_WAVES = 4, SMALL_MOST = 128; // (the last: the widest)
 template <typename T, bool COLS, int KF, int V, bool ODD>
 __global__ void __launch_bounds__(SMALL_WAVES * 64) k_adapt_small(KnProduct p, Down down, Beside beside, int32_t pieces)
@@ -928,6 +934,14 @@ template <typename T> bool small_layer(const KnProduct &p, const Down &down, boo
     return p.J <= 64 && p.M / down.E >= 16 && (sizeof(T) == 2 || p.C <= 64);
 }
 
+// Which tiles: the largest of which there are enough for the chip.  Measured (us, both kernels; 16 networks, rank 16, 2048 x 2048, columns contiguous, bf16):
+//   rows                          100    256    512    1,024   2,048   4,096
+//   32 x 64, four stages         19.7   20.5   26.0    41.1    71.9     144
+//   64 x 64, four stages         21.6   22.1   24.4    28.6    48.0      86
+//   64 x 128, three stages       25.7   25.9   27.2    28.1    35.0      57
+//   128 x 128, two               33.6   33.6   35.0    34.8    36.3      48
+// rows that are not whole pieces (1023 x 1025, 256, 1,024 and 4,096 rows): 32 x 64 29, 38, 67; 128 x 128 39, 38, 59.  fp32 (1024 x 1024): 32 x 64 28, 38, 107; 64 x 64 38,
+// 40, 98; 64 x 128 61, 60, 92; 128 x 128 98, 93, 97.
 template <typename T, bool COLS> int launch_up(hipStream_t st, const KnProduct &p, const Beside &beside)
 {
     auto tiles = [&](int64_t bm) { return (p.M + bm - 1) / bm * ((p.J + 127) / 128); };
