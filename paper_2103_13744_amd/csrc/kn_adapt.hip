@@ -509,6 +509,8 @@ __global__ void __launch_bounds__(WR * WC * 64, DIRECT && BM == 128 ? 4 : 1) k_a
         }
         if (tid < BM) slots[tid] = known && !left_out ? rank : -1;
         if (begins) nets[rank] = left_out ? -1 : net; // (it keeps its place: the others' sums are as they were)
+        count = __builtin_amdgcn_readfirstlane(count); // (alike for all lanes)
+        apart = __builtin_amdgcn_readfirstlane(apart);
         __syncthreads();
         lh.start(wave, lane, (const T *)beside.h, beside.rp, begin, end, slots);
         lo.start(beside, j0, p.J, nets, count, lane);
