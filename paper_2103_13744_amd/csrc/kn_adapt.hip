@@ -635,6 +635,21 @@ __global__ void __launch_bounds__(WR * WC * 64, DIRECT && BM == 128 ? 4 : 1) k_a
     }
 }
 
+// Rows of `rank` values in rows of whole 16-byte pieces, zeros behind them, of the networks that have rows: a thread per piece.  Else one factor's short rows would send the
+// whole shared product through registers (16,384 rows of 12 networks 2048 x 2048 of rank 4, contraction contiguous, in bf16: 249 us, 172 with this).
+template <typename T> __global__ void __launch_bounds__(256) k_adapt_pad(const T *__restrict__ b, T *__restrict__ to, const int32_t *__restrict__ offsets, int32_t M, int32_t rows,
+                                                                        int32_t rank, int32_t rp, int32_t blocks, int32_t first)
+{
+    constexpr int W = 16 / sizeof(T);
+    const int32_t block = first + kn_block(), net = block / blocks, pieces = rp / W;
+    if (kn_offset(offsets, net, M) >= kn_offset(offsets, net + 1, M)) return;
+    const int64_t q = (int64_t)(block % blocks) * 256 + kn_thread();
+    if (q >= (int64_t)rows * pieces) return;
+    const int64_t row = (int64_t)net * rows + q / pieces;
+    const int32_t k = (int32_t)(q % pieces) * W;
+    *(typename KnFrag<T>::Type *)(to + row * rp + k) = kn_any_piece<T>(b + row * rank, k, rank);
+}
+
 // strided_piece of a small matrix (less than 4 GiB) at an address that all lanes share: offsets of 32 bits, one addition for a value.  `at`: of the lane's first
 // value; `step`: bytes from one to the next
 template <typename T> __device__ __forceinline__ typename KnFrag<T>::Type strided_near(const T *base, uint32_t at, uint32_t step, int32_t k, int32_t C, bool tail)
@@ -1014,7 +1029,8 @@ template <typename T> int launch_few(hipStream_t st, const Down &down, const KnP
 
 // Both products of a call on `a` (rows through `rows`): h = scale a b_e, out = a w + h c_e.  cols: the columns of b and w are contiguous, and c's; else their contractions
 // are.  sums: room for few rows' parts.
-int run(hipStream_t st, int32_t dtype, bool cols, const Down &down, const KnProduct &up, const Beside &beside, float *sums)
+// padded: room for the factor c in rows of whole pieces (padded_bytes), or nullptr
+int run(hipStream_t st, int32_t dtype, bool cols, const Down &down, const KnProduct &up, const Beside &beside, float *sums, void *padded)
 {
     return kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
@@ -1023,6 +1039,19 @@ int run(hipStream_t st, int32_t dtype, bool cols, const Down &down, const KnProd
         if (small_layer<E_>(up, down, cols ? rows_of_pieces<E_, true>(up, beside) : rows_of_pieces<E_, false>(up, beside)))
             return cols ? launch_small<E_, true>(st, down, up, beside) : launch_small<E_, false>(st, down, up, beside);
         KN_TRY(launch_down<E_>(st, down, cols));
+        if (padded && !cols) {
+            Beside whole = beside;
+            whole.b = padded;
+            whole.rank = whole.b_j = beside.rp;
+            whole.b_group = (int64_t)up.J * beside.rp;
+            if (rows_of_pieces<E_, false>(up, whole)) {
+                const int64_t blocks = kn_div_up((int64_t)up.J * beside.rp * (int64_t)sizeof(E_), 256 * 16);
+                KN_TRY(kn_launch(blocks * down.E, 256, [&](dim3 grid, int32_t first) {
+                    hipLaunchKernelGGL((k_adapt_pad<E_>), grid, dim3(256), 0, st, (const E_ *)beside.b, (E_ *)padded, down.offsets, up.M, up.J, beside.rank, beside.rp, (int32_t)blocks, first);
+                }));
+                return launch_up<E_, false>(st, up, whole);
+            }
+        }
         return cols && up.b_c != 1 ? launch_up<E_, true>(st, up, beside) : launch_up<E_, false>(st, up, beside);
     });
 }
@@ -1038,6 +1067,13 @@ int check(const kn_linear_desc *d, int32_t rank)
 int64_t net_bytes(const kn_linear_desc *d) { return kn_align_up(d->rows * 4, 256) + kn_align_up(d->experts * 4, 256); }
 int32_t *apart_of(const kn_linear_desc *d, void *workspace) { return (int32_t *)((char *)workspace + kn_align_up(d->rows * 4, 256)); }
 int64_t h_bytes(const kn_linear_desc *d, int32_t rank) { return kn_align_up(d->rows * (int64_t)padded_rank(d->dtype, rank) * kn_item(d->dtype), 256); }
+// Room for a factor of J rows of `rank` in rows of whole pieces, where its rows are contiguous and not that already (not beyond 256 MiB: then as they are)
+int64_t padded_bytes(const kn_linear_desc *d, int32_t rank, bool cols, int32_t J)
+{
+    const int32_t rp = padded_rank(d->dtype, rank);
+    const int64_t bytes = kn_align_up((int64_t)d->experts * J * rp * kn_item(d->dtype), 256);
+    return cols || rp == rank || d->rows <= FEW_ROWS || bytes > 1 << 28 ? 0 : bytes;
+}
 // The gradients of A and B as those of a grouped layer
 kn_linear_desc layer_of(const kn_linear_desc *d, int32_t n_in, int32_t n_out, int64_t x_rows, int64_t ldx)
 {
@@ -1054,6 +1090,8 @@ int dw_bytes(const kn_linear_desc *d, int32_t rank, int64_t *out)
     const int64_t few = few_bytes(d->rows, d->n_in, d->n_out, kn_item(d->dtype)); // (done with before the others begin)
     *out = na + nb;
     *out = few > *out ? few : *out;
+    const int64_t padded = padded_bytes(d, rank, d->w_layout == KN_W_OUT_IN, d->n_in);
+    *out = padded > *out ? padded : *out;
     return KN_OK;
 }
 bool bad_workspace(const void *ws, int64_t have, int64_t need) { return need > 0 && (!ws || ((uintptr_t)ws & 255) || have < need); }
@@ -1064,7 +1102,7 @@ extern "C" int kn_adapted_linear_workspace_bytes(const kn_linear_desc *d, int32_
 {
     KN_TRY(check(d, rank));
     if (!out_bytes) return KN_E_INVALID_ARG;
-    *out_bytes = net_bytes(d) + h_bytes(d, rank) + few_bytes(d->rows, d->n_out, d->n_in, kn_item(d->dtype));
+    *out_bytes = net_bytes(d) + h_bytes(d, rank) + few_bytes(d->rows, d->n_out, d->n_in, kn_item(d->dtype)) + padded_bytes(d, rank, d->w_layout == KN_W_IN_OUT, d->n_out);
     return KN_OK;
 }
 
@@ -1087,7 +1125,8 @@ extern "C" int kn_adapted_linear(void *stream, const kn_linear_desc *d, int32_t 
     p.a = x; p.b = w; p.bias = bias; p.out = y; p.rows = rows;
     p.lda = d->ldx; p.b_c = io ? N : 1; p.b_j = io ? 1 : K; p.o_i = N;
     p.M = down.M; p.J = d->n_out; p.C = d->n_in; p.a_rows = down.a_rows; p.relu = relu != 0;
-    return run((hipStream_t)stream, d->dtype, io, down, p, beside, (float *)((char *)workspace + net_bytes(d) + h_bytes(d, rank)));
+    char *more = (char *)workspace + net_bytes(d) + h_bytes(d, rank); // (few rows' sums, or a padded factor)
+    return run((hipStream_t)stream, d->dtype, io, down, p, beside, (float *)more, padded_bytes(d, rank, io, d->n_out) > 0 ? more : nullptr);
 }
 
 extern "C" int kn_adapted_linear_backward_workspace_bytes(const kn_linear_desc *d, int32_t rank, int64_t *out_bytes)
@@ -1124,7 +1163,7 @@ extern "C" int kn_adapted_linear_backward(void *stream, const kn_linear_desc *d,
         p.lda = N; p.ldm = d->ldx; p.b_c = io ? 1 : K; p.b_j = io ? N : 1; p.o_i = K;
         p.M = down.M; p.J = d->n_in; p.C = d->n_out; p.a_rows = p.M; p.m_rows = (int32_t)d->x_rows;
         p.mask_rows = relu_in ? rows : nullptr;
-        KN_TRY(run((hipStream_t)stream, d->dtype, !io, down, p, beside, (float *)sums));
+        KN_TRY(run((hipStream_t)stream, d->dtype, !io, down, p, beside, (float *)sums, padded_bytes(d, rank, !io, d->n_in) > 0 ? sums : nullptr));
     }
     const kn_linear_desc la = layer_of(d, d->n_in, rank, d->x_rows, d->ldx), lb = layer_of(d, rank, d->n_out, d->rows, rp);
     return kn_linear_dw_low_rank(stream, &la, x, g, rp, rows, da, &lb, h, dy, N, db, offsets, sums, dw);

@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(WAVES * 64) k_reduce_small(KnProduct p, int32_
 // the long side's bytes.
 constexpr int thin_bytes(int fi, int fj) { return 16 * fi * (16 * fj + 4) * 4 > (fi + fj) * 1024 ? 16 * fi * (16 * fj + 4) * 4 : (fi + fj) * 1024; } // of a wavefront
 template <typename T, int FI, int FJ, bool TURN, int WAVES>
-__device__ __forceinline__ void reduce_thin(const KnProduct &p, const Parts &parts, int32_t block, char *lds_)
+__device__ __forceinline__ void reduce_thin(const KnProduct &p, const Parts &parts, int32_t width_a, int32_t width_b, int32_t block, char *lds_)
 {
     constexpr int W = 16 / sizeof(T), RS = 4 * W, LD = 16 * FJ + 4, OWN = thin_bytes(FI, FJ);
     typedef typename KnFrag<T>::Type Frag;
@@ -301,8 +301,8 @@ __device__ __forceinline__ void reduce_thin(const KnProduct &p, const Parts &par
     std::integral_constant<int, FI> fi;
     std::integral_constant<int, FJ> fj;
     auto load = [&](Step &x, int32_t c) {
-        ask(fi, (const T *)p.a + i0, p.lda, p.rows, p.a_rows, p.I - i0, c, x.a, x.none_a);
-        ask(fj, (const T *)p.b + j0, p.ldb, p.b_index, p.b_rows, p.J - j0, c, x.b, x.none_b);
+        ask(fi, (const T *)p.a + i0, p.lda, p.rows, p.a_rows, width_a - i0, c, x.a, x.none_a);
+        ask(fj, (const T *)p.b + j0, p.ldb, p.b_index, p.b_rows, width_b - j0, c, x.b, x.none_b);
     };
     auto multiply = [&](Step &x, int32_t c) {
         if (c >= cend) return;
@@ -356,18 +356,19 @@ __device__ __forceinline__ void reduce_thin(const KnProduct &p, const Parts &par
 struct Thin {
     KnProduct p;
     Parts parts;
+    int32_t width_a, width_b; // values that a row of a and b has: the narrower side's, which is made here, has zeros up to a whole piece
 };
 template <typename T, int FI, int FJ, bool TURN, int WAVES> __global__ void __launch_bounds__(WAVES * 64) k_reduce_thin(Thin a)
 {
     __shared__ __align__(16) char lds[WAVES * thin_bytes(FI, FJ)];
-    reduce_thin<T, FI, FJ, TURN, WAVES>(a.p, a.parts, a.p.first + kn_block(), lds);
+    reduce_thin<T, FI, FJ, TURN, WAVES>(a.p, a.parts, a.width_a, a.width_b, a.p.first + kn_block(), lds);
 }
 template <typename T, int F, bool TURN, int WAVES> __global__ void __launch_bounds__(WAVES * 64) k_reduce_thin_pair(Thin tall, Thin wide, int32_t blocks)
 {
     __shared__ __align__(16) char lds[WAVES * (thin_bytes(4, F) > thin_bytes(F, 4) ? thin_bytes(4, F) : thin_bytes(F, 4))];
     const int32_t block = tall.p.first + kn_block();
-    if (block < blocks) reduce_thin<T, 4, F, TURN, WAVES>(tall.p, tall.parts, block, lds);
-    else reduce_thin<T, F, 4, TURN, WAVES>(wide.p, wide.parts, block - blocks, lds);
+    if (block < blocks) reduce_thin<T, 4, F, TURN, WAVES>(tall.p, tall.parts, tall.width_a, tall.width_b, block, lds);
+    else reduce_thin<T, F, 4, TURN, WAVES>(wide.p, wide.parts, wide.width_a, wide.width_b, block - blocks, lds);
 }
 
 // The parts' sums of the networks that have several, in the order of the parts; `chunk` results per workgroup.  SEARCH: there are at most
@@ -650,11 +651,12 @@ Thin product_of(const kn_linear_desc *d, const void *x, const void *dy, int64_t 
     p.a_rows = (int32_t)(io ? d->x_rows : d->rows); p.b_rows = (int32_t)(io ? d->rows : d->x_rows);
     p.out = dw; p.out_bias = db; p.offsets = offsets;
     p.o_group = (int64_t)d->n_in * d->n_out; p.o_i = p.J;
-    return {p, parts};
+    const int32_t unit = 16 / kn_item(d->dtype), wa = thin && p.I <= 64 ? (int32_t)kn_align_up(p.I, unit) : p.I, wb = thin && p.J <= 64 ? (int32_t)kn_align_up(p.J, unit) : p.J;
+    return {p, parts, wa, wb};
 }
-bool whole_rows(const KnProduct &p, int64_t V)
+bool whole_rows(const KnProduct &p, int64_t V, int32_t width_a, int32_t width_b)
 {
-    return p.I % V == 0 && p.J % V == 0 && (((uintptr_t)p.a | (uintptr_t)p.b) & 15) == 0 && p.lda % V == 0 && p.ldb % V == 0;
+    return width_a % V == 0 && width_b % V == 0 && (((uintptr_t)p.a | (uintptr_t)p.b) & 15) == 0 && p.lda % V == 0 && p.ldb % V == 0;
 }
 } // namespace
 
@@ -679,7 +681,7 @@ int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const
             if (io) return direct ? launch_reduce<E_, true, SAVED_A>(st, d, p, sum, parts, exponents) : launch_reduce<E_, false, SAVED_A>(st, d, p, sum, parts, exponents);
             return direct ? launch_reduce<E_, true, SAVED_B>(st, d, p, sum, parts, exponents) : launch_reduce<E_, false, SAVED_B>(st, d, p, sum, parts, exponents);
         }
-        const bool direct = whole_rows(p, V);
+        const bool direct = whole_rows(p, V, p.I, p.J);
         return direct ? launch_reduce<E_, true, SAVED_NONE>(st, d, p, sum, parts, nullptr) : launch_reduce<E_, false, SAVED_NONE>(st, d, p, sum, parts, nullptr);
     });
 }
@@ -699,7 +701,7 @@ int kn_linear_dw_low_rank(void *stream, const kn_linear_desc *da, const void *x,
         typedef decltype(v) E_;
         constexpr int64_t V = 16 / sizeof(E_);
         constexpr bool TURNS = sizeof(E_) == 2;
-        const bool turn_a = TURNS && whole_rows(a.p, V), turn_b = TURNS && whole_rows(b.p, V);
+        const bool turn_a = TURNS && whole_rows(a.p, V, a.width_a, a.width_b), turn_b = TURNS && whole_rows(b.p, V, b.width_a, b.width_b);
         if (thin_a && thin_b && turn_a == turn_b) return turn_a ? launch_pair<E_, TURNS>(st, a, b) : launch_pair<E_, false>(st, a, b);
         if (thin_a) KN_TRY((turn_a ? launch_thin<E_, TURNS>(st, a) : launch_thin<E_, false>(st, a)));
         else KN_TRY(kn_linear_dw_run(stream, da, x, nullptr, g, ldg, offsets, rows, out_a, nullptr, workspace, na));
