@@ -529,7 +529,7 @@ template <typename T, int F, bool TURN> int launch_pair_of(hipStream_t st, const
         else hipLaunchKernelGGL((k_reduce_thin_pair<T, F, TURN, 4>), grid, dim3(256), 0, st, q, wide, (int32_t)blocks);
     });
 }
-// Two at once: a launch less, and one's last workgroups run beside the other's (8,192 rows of 16 networks 1024 x 2048, rank 16 in bf16, with the joins 34 -> 21 us)
+// Two at once: a launch less, and one's last workgroups run beside the other's (8,192 rows of 16 networks 1024 x 2048, rank 16 in bf16, with the joins 34 -> 25 us)
 template <typename T, bool TURN> int launch_pair(hipStream_t st, const Thin &a, const Thin &b)
 {
     const Thin &tall = a.p.I > a.p.J ? a : b, &wide = a.p.I > a.p.J ? b : a;
