@@ -470,14 +470,16 @@ template <int G, int V> __device__ __forceinline__ bool softmax_row(float v[V], 
 // Sums over the rows [block * per, + per): G lanes a row, whose columns' sums stay in registers from row to row and meet in the LDS at the end, in
 // the order of the groups.  A row is asked for while the one before is worked on.  ONE: these are all rows, and the results are written too; else they are
 // left for k_balance_join.  Bound by its bytes where rows are many: 32,768 rows of 128 logits in fp32 6.3 us, 2.7 TB/s, and the join 6.5; 16,385 of 1,000 in
-// bf16 14 (42 with branches around the fetches), and 6.  64 rows of 16: one launch, 3.0.
+// bf16 13 (42 with branches around the fetches, and half the threads), and 4.8; 65,536 of 300 in fp32, forward and backward, 55, with 16 values a lane instead of 8 73.
+// 64 rows of 16: one launch, 3.0; of 1,000 in bf16 with the backward call 13.6, with 256 threads 17.8.
+constexpr int balance_threads(int G) { return G == 64 ? 512 : 256; }
 template <typename T, int G, int V, bool ONE>
-__global__ void __launch_bounds__(256) k_balance(BalanceArgs a)
+__global__ void __launch_bounds__(balance_threads(G)) k_balance(BalanceArgs a)
 {
-    constexpr int GROUPS = 256 / G;
+    constexpr int THREADS = balance_threads(G), GROUPS = THREADS / G;
     typedef RowOf<T, G, V> Row;
     __shared__ float parts[GROUPS][G * V];
-    __shared__ float squares[GROUPS], terms[4];
+    __shared__ float squares[GROUPS], terms[THREADS / 64];
     __shared__ int32_t rows[GROUPS];
     const int tid = kn_thread(), lane = tid & 63, at = lane & (G - 1), group = tid / G;
     const int32_t block = a.first + kn_block();
@@ -509,7 +511,7 @@ __global__ void __launch_bounds__(256) k_balance(BalanceArgs a)
     if (!ONE && block == 0 && tid == 0) *a.ticket = 0;
     __syncthreads();
     float term = 0.0f;
-    for (int32_t e = tid; e < a.E; e += 256) {
+    for (int32_t e = tid; e < a.E; e += THREADS) {
         float y = 0.0f;
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) y += parts[g][e];
@@ -535,9 +537,11 @@ __global__ void __launch_bounds__(256) k_balance(BalanceArgs a)
         all_rows += rows[g];
     }
     if constexpr (ONE) {
+        float all_terms = 0.0f;
+        for (int w = 0; w < THREADS / 64; ++w) all_terms += terms[w];
         const float inverse = all_rows > 0 ? 1.0f / (float)all_rows : 0.0f;
         a.counts[a.E] = all_rows;
-        a.losses[0] = (terms[0] + terms[1] + terms[2] + terms[3]) * inverse * inverse * ((float)a.E / (float)a.k);
+        a.losses[0] = all_terms * inverse * inverse * ((float)a.E / (float)a.k);
         a.losses[1] = all_squares * inverse;
     } else {
         a.tail[2 * (int64_t)block] = all_squares;
@@ -616,7 +620,7 @@ __global__ void __launch_bounds__(JOIN_COLUMNS * JOIN_TURNS) k_balance_join(Bala
 }
 
 // dl_te = p_te (g_0 (s_e - sum over i of p_ti s_i) + g_1 (2 / n) Z_t), s_e = E c_e / (k n^2), and (ADD) what it is added to.  Rows as in k_balance.  The same 32,768 rows:
-// 9.0 us, 5.6 TB/s; 16,385 of 1,000 in bf16: 17, 3.9 TB/s.
+// 9.0 us, 5.6 TB/s; 16,385 of 1,000 in bf16: 15.7, 4.2 TB/s.
 template <typename T, int G, int V, bool ADD>
 __global__ void __launch_bounds__(256) k_balance_backward(BalanceArgs a)
 {
@@ -826,11 +830,20 @@ extern "C" int kn_route_backward(void *stream, const void *logits, int32_t dtype
     });
 }
 
-// Rows of a workgroup: enough workgroups for the whole chip, and no sum of more than 2,048 rows in 32 bits
+// Rows of a workgroup: enough workgroups for the whole chip, and no sum of more than 2,048 rows in 32 bits.  Long rows (us, forward and backward; 16,385 rows of 1,000 in
+// bf16): 256 threads and 1,024 parts 36.0, 512 threads and 2,048 34.0, 1,024 33.0, 512 32.5.  The backward pass has no parts to join: 1,024 workgroups 36.0, 2,048 35.0,
+// 4,096 34.3, 8,192 34.8.
 static int32_t balance_rows(int64_t T, int32_t E)
 {
-    const int64_t set = E <= 256 ? 16 : 4, per = kn_align_up(kn_div_up(T, 1024), set);
+    const int64_t per = E <= 256 ? kn_align_up(kn_div_up(T, 1024), 16) : kn_align_up(kn_div_up(T, 512), 8);
     return (int32_t)(per < 2048 ? per : 2048);
+}
+static int32_t balance_backward_rows(int64_t T, int32_t E) { return (int32_t)(E <= 256 ? kn_align_up(kn_div_up(T, 1024), 16) : kn_align_up(kn_div_up(T, 4096), 4)); }
+
+// As route_shape, with shorter rows of a wavefront
+template <typename F> static int balance_shape(int32_t E, F &&f)
+{
+    return E > 256 && E <= 512 ? f(Int<64>(), Int<8>()) : route_shape(E, f);
 }
 
 extern "C" int kn_route_balance_workspace_bytes(int64_t T, int32_t E, int64_t *out_bytes)
@@ -863,12 +876,13 @@ extern "C" int kn_route_balance(void *stream, const void *logits, int32_t dtype,
     hipStream_t st = (hipStream_t)stream;
     KN_TRY(kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
-        return route_shape(E, [&](auto g, auto n) -> int {
+        return balance_shape(E, [&](auto g, auto n) -> int {
             constexpr int G = decltype(g)::n, V = decltype(n)::n;
-            return kn_launch(a.blocks, 256, [&](dim3 grid, int32_t first) {
+            constexpr int threads = balance_threads(G);
+            return kn_launch(a.blocks, threads, [&](dim3 grid, int32_t first) {
                 a.first = first;
-                if (one) hipLaunchKernelGGL((k_balance<E_, G, V, true>), grid, dim3(256), 0, st, a);
-                else hipLaunchKernelGGL((k_balance<E_, G, V, false>), grid, dim3(256), 0, st, a);
+                if (one) hipLaunchKernelGGL((k_balance<E_, G, V, true>), grid, dim3(threads), 0, st, a);
+                else hipLaunchKernelGGL((k_balance<E_, G, V, false>), grid, dim3(threads), 0, st, a);
             });
         });
     }));
@@ -886,11 +900,11 @@ extern "C" int kn_route_balance_backward(void *stream, const void *logits, int32
     if (T == 0) return KN_OK;
     BalanceArgs a = {};
     a.logits = logits; a.add = add; a.dlogits = dlogits; a.ld = ld; a.T = (int32_t)T; a.E = E; a.k = k;
-    a.per = balance_rows(T, E);
+    a.per = balance_backward_rows(T, E);
     a.counts = const_cast<int32_t *>(counts); a.dlosses = dlosses;
     return kn_with_type(dtype, [&](auto v) -> int {
         typedef decltype(v) E_;
-        return route_shape(E, [&](auto g, auto n) -> int {
+        return balance_shape(E, [&](auto g, auto n) -> int {
             constexpr int G = decltype(g)::n, V = decltype(n)::n;
             return kn_launch(kn_div_up(T, a.per), 256, [&](dim3 grid, int32_t first) {
                 a.first = first;
