@@ -356,7 +356,7 @@ __device__ __forceinline__ void reduce_thin(const KnProduct &p, const Parts &par
 struct Thin {
     KnProduct p;
     Parts parts;
-    int32_t width_a, width_b; // values that a row of a and b has: the narrower side's, which is made here, has zeros up to a whole piece
+    int32_t width_a, width_b; // values that a row of a and b has: those of g and h have zeros up to a whole piece
 };
 template <typename T, int FI, int FJ, bool TURN, int WAVES> __global__ void __launch_bounds__(WAVES * 64) k_reduce_thin(Thin a)
 {
@@ -636,11 +636,12 @@ extern "C" int kn_grouped_linear_dw_saved(void *stream, const kn_linear_desc *d,
     return kn_linear_dw_run(stream, &whole, q, exponents ? exponents : &none, dy, d->n_out, offsets, rows, dw, db, workspace, workspace_bytes);
 }
 
-// Both operands and the result of a gradient (thin: a low-rank factor's)
+// Both operands and the result of a gradient.  LOW_..: a low-rank factor's, whose g or h (the side named) has rows with zeros up to a whole piece
 namespace {
-Thin product_of(const kn_linear_desc *d, const void *x, const void *dy, int64_t lddy, const int32_t *offsets, const int32_t *rows, void *dw, void *db, void *workspace, bool thin)
+enum Low { LOW_NO, LOW_OUT, LOW_IN };
+Thin product_of(const kn_linear_desc *d, const void *x, const void *dy, int64_t lddy, const int32_t *offsets, const int32_t *rows, void *dw, void *db, void *workspace, Low low)
 {
-    Parts parts = {part_length(d, thin && is_thin(d)), (float *)workspace, nullptr};
+    Parts parts = {part_length(d, low != LOW_NO && is_thin(d)), (float *)workspace, nullptr};
     parts.bias_sums = parts.sums + part_places(d->rows, parts.len) * (int64_t)d->n_in * d->n_out;
     KnProduct p = {};
     const bool io = d->w_layout == KN_W_IN_OUT; // (columns are what is contiguous in dw)
@@ -651,8 +652,9 @@ Thin product_of(const kn_linear_desc *d, const void *x, const void *dy, int64_t 
     p.a_rows = (int32_t)(io ? d->x_rows : d->rows); p.b_rows = (int32_t)(io ? d->rows : d->x_rows);
     p.out = dw; p.out_bias = db; p.offsets = offsets;
     p.o_group = (int64_t)d->n_in * d->n_out; p.o_i = p.J;
-    const int32_t unit = 16 / kn_item(d->dtype), wa = thin && p.I <= 64 ? (int32_t)kn_align_up(p.I, unit) : p.I, wb = thin && p.J <= 64 ? (int32_t)kn_align_up(p.J, unit) : p.J;
-    return {p, parts, wa, wb};
+    const int32_t unit = 16 / kn_item(d->dtype);
+    const int32_t in = low == LOW_IN ? (int32_t)kn_align_up(d->n_in, unit) : d->n_in, out = low == LOW_OUT ? (int32_t)kn_align_up(d->n_out, unit) : d->n_out;
+    return {p, parts, io ? in : out, io ? out : in};
 }
 bool whole_rows(const KnProduct &p, int64_t V, int32_t width_a, int32_t width_b)
 {
@@ -668,7 +670,7 @@ int kn_linear_dw_run(void *stream, const kn_linear_desc *d, const void *x, const
     KN_TRY(kn_grouped_linear_dw_workspace_bytes(d, &need));
     if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return KN_E_WORKSPACE;
     const bool io = d->w_layout == KN_W_IN_OUT;
-    const Thin t = product_of(d, x, dy, lddy, offsets, rows, dw, db, workspace, false);
+    const Thin t = product_of(d, x, dy, lddy, offsets, rows, dw, db, workspace, LOW_NO);
     const KnProduct &p = t.p;
     const Parts &parts = t.parts;
     const int32_t sum = !db ? SUM_NONE : io ? SUM_B : SUM_A;
@@ -694,7 +696,7 @@ int kn_linear_dw_low_rank(void *stream, const kn_linear_desc *da, const void *x,
     KN_TRY(kn_linear_dw_bytes(db, true, &nb));
     if (na + nb > 0 && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < na + nb)) return KN_E_WORKSPACE;
     char *ws_b = (char *)workspace + na;
-    const Thin a = product_of(da, x, g, ldg, offsets, rows, out_a, nullptr, workspace, true), b = product_of(db, h, dy, lddy, offsets, nullptr, out_b, nullptr, ws_b, true);
+    const Thin a = product_of(da, x, g, ldg, offsets, rows, out_a, nullptr, workspace, LOW_OUT), b = product_of(db, h, dy, lddy, offsets, nullptr, out_b, nullptr, ws_b, LOW_IN);
     const bool thin_a = is_thin(da), thin_b = is_thin(db);
     hipStream_t st = (hipStream_t)stream;
     return kn_with_type(da->dtype, [&](auto v) -> int {

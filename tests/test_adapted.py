@@ -85,7 +85,7 @@ SIZES = [  # rows, networks, inputs, outputs, rank
     (64, 1, 64, 64, 64), (65, 2, 63, 32, 4), (100, 100, 96, 40, 24), (129, 5, 91, 64, 7), (200, 65, 32, 33, 1), (257, 3, 72, 200, 80), (300, 130, 64, 3, 2), (500, 4, 320, 520, 16),
     (1000, 7, 129, 127, 9), (1100, 3, 512, 256, 32), (3000, 4200, 32, 32, 4), (2100, 2, 136, 264, 13), (1300, 3, 40, 72, 130), (200, 3, 24, 1, 3), (200, 3, 1, 24, 2), (90, 2, 300, 1, 8), (90, 2, 1, 300, 8), (2200, 5, 128, 128, 16), (400, 9, 100, 128, 10), (500, 3, 8, 200, 16),
     (70, 2, 3, 5, 40), (900, 3, 128, 64, 20), (3000, 3, 136, 200, 30), (2500, 2, 130, 99, 50), (1500, 2, 72, 300, 64), (700, 5, 96, 50, 70), (400, 9, 256, 136, 4), (1800, 30, 136, 264, 12), (2600, 3, 520, 256, 1),
-    (5000, 4, 64, 33, 3), (700, 9, 2000, 48, 8),
+    (5000, 4, 64, 33, 3), (700, 9, 2000, 48, 8), (300, 3, 5, 72, 100), (700, 2, 75, 9, 70), (900, 3, 67, 131, 3), (2600, 2, 141, 66, 33), (1500, 2, 13, 74, 66), (400, 2, 71, 1, 67), (2200, 3, 515, 300, 10),
 ]
 
 
