@@ -116,7 +116,6 @@ __device__ __forceinline__ kn_f32x4 kn_mfma(kn_f32x4 a, kn_f32x4 b, kn_f32x4 c)
 struct KnProduct {
     const void *a, *b, *bias, *mask; // mask: out(i, j) becomes 0 where mask(row i, j) <= 0 (a ReLU's result)
     void *out, *out_bias;            // out_bias (weight gradient): sum over the rows r of b(r, j)
-    const int8_t *mask_saved;        // the same mask from what kn_save_f8 left: a positive byte is a positive value (rows of ldm bytes)
     const int32_t *offsets, *rows, *b_index, *mask_rows; // rows: of a, b_index: of b, mask_rows: of the mask; nullable
     int64_t lda, ldb, ldm;           // row strides in elements: a, b (weight gradient), mask
     int64_t b_group, b_c, b_j;       // strides of b_e: network, contraction, column

@@ -13,7 +13,7 @@ namespace {
 // library of 8192 x 8192 x 8192 reaches 1,250.  The clock is 2.03 GHz with the matrix cores busy 44 % of the time (256 x 256: 2.30 GHz, 39 %, the
 // same time); with every fetch a hit in the L2 it would be 250 us, so that more than half of what is above the floor is the wait for what
 // the L2 does not have.
-template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB>
+template <typename T, bool SAVED, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB>
 __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int32_t blocks)
 {
     constexpr int NW = WR * WC, STAGE = (BM + BN) * 128, U = BM / WR / 16, V = BN / WC / 16, CS = 128 / sizeof(T);
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
             if (r >= 16 || i >= piece.end || j >= p.J) continue;
             const kn_f32x4 lo = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj), hi = *(const KN_LDS kn_f32x4 *)(mine + r * LD + cj + 4);
             float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            kn_finish<T>(p, some, i, j, add, y);
+            kn_finish<T, SAVED>(p, some, i, j, add, y);
         }
         kn_lanes_meet();
     }
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(WR * WC * 64) k_product_rows(KnProduct p, int3
 // product's fragment: column j of every lane's square.  16-bit squares are turned by byte permutations of register pairs, fp32
 // ones by naming.  Bound by the weights' bytes: 32 rows in about 25 of 64 networks 2048 x 1024, bf16: 24 us, 4.4 TB/s.
 constexpr int FEW_WAVES = 8;
-template <typename T>
+template <typename T, bool SAVED>
 __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p)
 {
     constexpr int R = 16 / sizeof(T), BN = 16 * R, KS = 4 * R, LD = BN + 4;
@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p)
             for (int n = 0; n < 4; ++n) { y[n] += lo[n]; y[n + 4] += hi[n]; }
         }
         kn_bias_of<T>(p, some, group, j, add);
-        kn_finish<T>(p, some, i, j, add, y);
+        kn_finish<T, SAVED>(p, some, i, j, add, y);
     }
 }
 
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(FEW_WAVES * 64) k_product_few(KnProduct p)
 // a third more lines than they fill; 44 us where each odd end is waited for); 524,291 rows, 64 x 64 in fp16, input gradient with a ReLU's mask: 59 us, 4.0 TB/s (68 where a
 // lane stores and masks 8 bytes at a time).  Pieces of 64 rows: 49 and 69, of 128: 70 and 90, of 16: 52 and 85.
 constexpr int SMALL_ROWS = 32, SMALL_WAVES = 4;
-template <typename T, bool COLS, int KF, int V, bool ODD>
+template <typename T, bool SAVED, bool COLS, int KF, int V, bool ODD>
 __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p, int32_t pieces)
 {
     constexpr int W = KnSmallFrag<T>::W, KS = KnSmallFrag<T>::KS, SUBS = SMALL_ROWS / 16;
@@ -300,23 +300,6 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
     Run add[RUNS], m[SUBS][RUNS]; // (a lane's columns are j0 + 4 W n + W g .. + W - 1)
 #pragma unroll
     for (int n = 0; n < RUNS; ++n) add[n] = some && bias ? run(bias + group * p.J, min(j0 + 4 * W * n + W * g, p.J - 1)) : Run{};
-    if (some && p.mask_saved) { // (a lane's W columns lie in a saved row's whole 16 bytes)
-#pragma unroll
-        for (int s = 0; s < SUBS; ++s) {
-            const int32_t i = min(piece.begin + 16 * s + col, piece.end - 1), src = p.mask_rows ? p.mask_rows[i] : i;
-            const bool in = (uint32_t)src < (uint32_t)p.m_rows;
-#pragma unroll
-            for (int n = 0; n < RUNS; ++n) {
-                typedef int8_t Bytes __attribute__((ext_vector_type(W)));
-                const int32_t j = j0 + 4 * W * n + W * g;
-                Bytes b = {};
-                if (in && j < p.J) b = *(const Bytes *)(p.mask_saved + (int64_t)src * p.ldm + j);
-#pragma unroll
-                for (int r = 0; r < W; ++r) m[s][n][r] = (T)(b[r] > 0 ? 1.0f : 0.0f);
-            }
-        }
-    }
-    const bool masked = some && (mask || p.mask_saved);
     if (some && mask) { // (asked for before the first result is stored, not one after the other's)
 #pragma unroll
         for (int s = 0; s < SUBS; ++s) {
@@ -325,6 +308,15 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
 #pragma unroll
             for (int n = 0; n < RUNS; ++n) {
                 m[s][n] = Run{};
+                if constexpr (SAVED) { // (a lane's W columns lie in a saved row's whole 16 bytes)
+                    typedef int8_t Bytes __attribute__((ext_vector_type(W)));
+                    const int32_t j = j0 + 4 * W * n + W * g;
+                    Bytes b = {};
+                    if (in && j < p.J) b = *(const Bytes *)((const int8_t *)p.mask + (int64_t)src * p.ldm + j);
+#pragma unroll
+                    for (int r = 0; r < W; ++r) m[s][n][r] = (T)(b[r] > 0 ? 1.0f : 0.0f);
+                    continue;
+                }
                 if (in) m[s][n] = run(mask + (int64_t)src * p.ldm, min(j0 + 4 * W * n + W * g, p.J - 1));
             }
         }
@@ -355,7 +347,7 @@ __global__ void __launch_bounds__(SMALL_WAVES * 64) k_product_small(KnProduct p,
                 float y = acc[n * PAIR + r / 4][r % 4];
                 if (some && bias) y += (float)add[n][r];
                 if (p.relu) y = y > 0.0f || y != y ? y : 0.0f; // (a NaN stays one)
-                if (masked && !((float)m[s][n][r] > 0.0f)) y = 0.0f;
+                if (some && mask && !((float)m[s][n][r] > 0.0f)) y = 0.0f;
                 o[r] = (T)y;
             }
             if (together) {
@@ -390,23 +382,23 @@ template <typename T, bool COLS> bool rows_of_pieces(const KnProduct &p)
     return ((uintptr_t)p.a | (uintptr_t)p.b) % 16 == 0 && p.C % V == 0 && p.lda % V == 0 && (!COLS || p.J % V == 0) && p.a_rows > 0;
 }
 
-template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB> int launch_rows(hipStream_t st, const KnProduct &p)
+template <typename T, bool SAVED, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB> int launch_rows(hipStream_t st, const KnProduct &p)
 {
     const int64_t blocks = kn_pieces(p.M, p.E, BM) * kn_div_up(p.J, BN);
     return kn_launch(blocks, WR * WC * 64, [&](dim3 grid, int32_t first) {
         KnProduct q = p;
         q.first = first;
-        hipLaunchKernelGGL((k_product_rows<T, COLS, DIRECT, BM, BN, WR, WC, NB>), grid, dim3(WR * WC * 64), 0, st, q, (int32_t)blocks);
+        hipLaunchKernelGGL((k_product_rows<T, SAVED, COLS, DIRECT, BM, BN, WR, WC, NB>), grid, dim3(WR * WC * 64), 0, st, q, (int32_t)blocks);
     });
 }
 
-template <typename T> int launch_few(hipStream_t st, const KnProduct &p)
+template <typename T, bool SAVED> int launch_few(hipStream_t st, const KnProduct &p)
 {
     const int64_t blocks = kn_pieces(p.M, p.E, 16) * kn_div_up(p.J, 256 / (int)sizeof(T));
     return kn_launch(blocks, FEW_WAVES * 64, [&](dim3 grid, int32_t first) {
         KnProduct q = p;
         q.first = first;
-        hipLaunchKernelGGL((k_product_few<T>), grid, dim3(FEW_WAVES * 64), 0, st, q);
+        hipLaunchKernelGGL((k_product_few<T, SAVED>), grid, dim3(FEW_WAVES * 64), 0, st, q);
     });
 }
 
@@ -431,66 +423,66 @@ template <typename T> int launch_few(hipStream_t st, const KnProduct &p)
 //   32,768, 8, 512, 1024                                               339         306         317
 //   2,048, 64, 512, 512, contraction contiguous                22       33          41          42
 //   8,192, 16, 1024, 1024                                     180      167         177         209
-template <typename T, bool COLS> int launch_pieces(hipStream_t st, const KnProduct &p)
+template <typename T, bool SAVED, bool COLS> int launch_pieces(hipStream_t st, const KnProduct &p)
 {
     const int64_t each = p.M / p.E; // rows of a network, on average
     auto tiles = [&](int64_t bm) { return (p.M + bm - 1) / bm * ((p.J + 127) / 128); };
     if constexpr (sizeof(T) == 4) {
         const bool narrow = (int64_t)p.M * p.J <= 1 << 20; // (too few tiles of 32 x 128 for the chip)
         if (!rows_of_pieces<T, COLS>(p))
-            return narrow ? launch_rows<T, COLS, false, 32, 64, 1, 4, 2>(st, p) : each < 512 ? launch_rows<T, COLS, false, 32, 128, 1, 4, 2>(st, p) : launch_rows<T, COLS, false, 64, 128, 1, 4, 2>(st, p);
+            return narrow ? launch_rows<T, SAVED, COLS, false, 32, 64, 1, 4, 2>(st, p) : each < 512 ? launch_rows<T, SAVED, COLS, false, 32, 128, 1, 4, 2>(st, p) : launch_rows<T, SAVED, COLS, false, 64, 128, 1, 4, 2>(st, p);
         if constexpr (COLS) {
-            if (narrow) return launch_few<T>(st, p);
-            if (p.J <= 64) return launch_rows<T, COLS, true, 32, 64, 1, 4, 2>(st, p);
-            return each < 512 ? launch_rows<T, COLS, true, 32, 128, 1, 4, 2>(st, p) : launch_rows<T, COLS, true, 64, 128, 1, 4, 2>(st, p);
+            if (narrow) return launch_few<T, SAVED>(st, p);
+            if (p.J <= 64) return launch_rows<T, SAVED, COLS, true, 32, 64, 1, 4, 2>(st, p);
+            return each < 512 ? launch_rows<T, SAVED, COLS, true, 32, 128, 1, 4, 2>(st, p) : launch_rows<T, SAVED, COLS, true, 64, 128, 1, 4, 2>(st, p);
         } else {
-            if (p.J <= 64 && !narrow) return launch_rows<T, COLS, true, 32, 64, 1, 4, 2>(st, p); // (two stages: more workgroups at a time)
-            return narrow ? launch_rows<T, COLS, true, 32, 64, 1, 4, 4>(st, p) : launch_rows<T, COLS, true, 32, 128, 1, 4, 2>(st, p);
+            if (p.J <= 64 && !narrow) return launch_rows<T, SAVED, COLS, true, 32, 64, 1, 4, 2>(st, p); // (two stages: more workgroups at a time)
+            return narrow ? launch_rows<T, SAVED, COLS, true, 32, 64, 1, 4, 4>(st, p) : launch_rows<T, SAVED, COLS, true, 32, 128, 1, 4, 2>(st, p);
         }
     } else {
         if (!rows_of_pieces<T, COLS>(p))
-            return each >= 64 && tiles(128) >= 256 ? launch_rows<T, COLS, false, 128, 128, 2, 4, 2>(st, p) : launch_rows<T, COLS, false, 32, 128, 1, 4, 2>(st, p);
+            return each >= 64 && tiles(128) >= 256 ? launch_rows<T, SAVED, COLS, false, 128, 128, 2, 4, 2>(st, p) : launch_rows<T, SAVED, COLS, false, 32, 128, 1, 4, 2>(st, p);
         const bool little = (int64_t)p.M * p.J <= 1 << 19;
         if constexpr (COLS) {
-            if (little && (each < 2 || (int64_t)p.E * p.C * p.J <= 1 << 25)) return launch_few<T>(st, p);
+            if (little && (each < 2 || (int64_t)p.E * p.C * p.J <= 1 << 25)) return launch_few<T, SAVED>(st, p);
         } else {
-            if (little || each < 64) return launch_rows<T, COLS, true, 32, 64, 1, 4, 4>(st, p);
+            if (little || each < 64) return launch_rows<T, SAVED, COLS, true, 32, 64, 1, 4, 4>(st, p);
         }
-        if (each >= 384 && tiles(192) >= 256 && p.C * (int64_t)sizeof(T) >= 1024) return launch_rows<T, COLS, true, 192, 128, 2, 2, 2>(st, p);
-        if (each >= 192 && tiles(128) >= 512) return launch_rows<T, COLS, true, 128, 128, 2, 4, 2>(st, p);
-        return launch_rows<T, COLS, true, 64, 128, 1, 4, 2>(st, p);
+        if (each >= 384 && tiles(192) >= 256 && p.C * (int64_t)sizeof(T) >= 1024) return launch_rows<T, SAVED, COLS, true, 192, 128, 2, 2, 2>(st, p);
+        if (each >= 192 && tiles(128) >= 512) return launch_rows<T, SAVED, COLS, true, 128, 128, 2, 4, 2>(st, p);
+        return launch_rows<T, SAVED, COLS, true, 64, 128, 1, 4, 2>(st, p);
     }
 }
 
-template <typename T, bool COLS, int KF, int V, bool ODD> int launch_small_of(hipStream_t st, const KnProduct &p)
+template <typename T, bool SAVED, bool COLS, int KF, int V, bool ODD> int launch_small_of(hipStream_t st, const KnProduct &p)
 {
     const int64_t pieces = kn_pieces(p.M, p.E, SMALL_ROWS), waves = pieces * kn_div_up(p.J, 16 * V);
     if (waves > 0x7fffffffLL) return KN_E_UNSUPPORTED;
     return kn_launch(kn_div_up(waves, SMALL_WAVES), SMALL_WAVES * 64, [&](dim3 grid, int32_t first) {
         KnProduct q = p;
         q.first = first;
-        hipLaunchKernelGGL((k_product_small<T, COLS, KF, V, ODD>), grid, dim3(SMALL_WAVES * 64), 0, st, q, (int32_t)pieces);
+        hipLaunchKernelGGL((k_product_small<T, SAVED, COLS, KF, V, ODD>), grid, dim3(SMALL_WAVES * 64), 0, st, q, (int32_t)pieces);
     });
 }
-template <typename T, bool COLS, int KF, int V> int launch_small(hipStream_t st, const KnProduct &p)
+template <typename T, bool SAVED, bool COLS, int KF, int V> int launch_small(hipStream_t st, const KnProduct &p)
 {
     if constexpr (sizeof(T) == 2) { // rows that begin between two words
-        if (((uintptr_t)p.a / 2 | p.lda | (COLS ? 0 : (uintptr_t)p.b / 2 | p.b_j)) & 1) return launch_small_of<T, COLS, KF, V, true>(st, p);
+        if (((uintptr_t)p.a / 2 | p.lda | (COLS ? 0 : (uintptr_t)p.b / 2 | p.b_j)) & 1) return launch_small_of<T, SAVED, COLS, KF, V, true>(st, p);
     }
-    return launch_small_of<T, COLS, KF, V, false>(st, p);
+    return launch_small_of<T, SAVED, COLS, KF, V, false>(st, p);
 }
 constexpr int SMALL_MOST = 128; // widest contraction and most columns that k_product_small takes
-template <typename T, bool COLS> int launch_small_widths(hipStream_t st, const KnProduct &p)
+template <typename T, bool SAVED, bool COLS> int launch_small_widths(hipStream_t st, const KnProduct &p)
 {
     const int kf = (p.C + KnSmallFrag<T>::KS - 1) / KnSmallFrag<T>::KS;
     if constexpr (sizeof(T) == 4) {
-        if (kf > 4) return launch_small<T, COLS, 8, 2>(st, p);
-        if (kf > 2) return p.J <= 32 ? launch_small<T, COLS, 4, 2>(st, p) : launch_small<T, COLS, 4, 4>(st, p);
-        return p.J <= 32 ? launch_small<T, COLS, 2, 2>(st, p) : launch_small<T, COLS, 2, 4>(st, p);
+        if (kf > 4) return launch_small<T, SAVED, COLS, 8, 2>(st, p);
+        if (kf > 2) return p.J <= 32 ? launch_small<T, SAVED, COLS, 4, 2>(st, p) : launch_small<T, SAVED, COLS, 4, 4>(st, p);
+        return p.J <= 32 ? launch_small<T, SAVED, COLS, 2, 2>(st, p) : launch_small<T, SAVED, COLS, 2, 4>(st, p);
     } else {
-        if (kf > 2) return launch_small<T, COLS, 4, 4>(st, p);
-        if (kf > 1) return p.J <= 32 ? launch_small<T, COLS, 2, 2>(st, p) : launch_small<T, COLS, 2, 4>(st, p);
-        return p.J <= 32 ? launch_small<T, COLS, 1, 2>(st, p) : launch_small<T, COLS, 1, 4>(st, p);
+        if (kf > 2) return launch_small<T, SAVED, COLS, 4, 4>(st, p);
+        if (kf > 1) return p.J <= 32 ? launch_small<T, SAVED, COLS, 2, 2>(st, p) : launch_small<T, SAVED, COLS, 2, 4>(st, p);
+        return p.J <= 32 ? launch_small<T, SAVED, COLS, 1, 2>(st, p) : launch_small<T, SAVED, COLS, 1, 4>(st, p);
     }
 }
 
@@ -522,14 +514,14 @@ template <typename T> bool small_by_tiles(const KnProduct &p, bool cols)
     if (p.J <= 64) return p.C > 64 && p.J > 32 && (cols ? each >= 96 : p.C > 96 && each >= 256);
     return p.C > 64 ? cols || each >= 64 : p.C > 32 && each >= 96;
 }
-template <typename T> int launch_forward(hipStream_t st, const KnProduct &p)
+template <typename T, bool SAVED> int launch_forward(hipStream_t st, const KnProduct &p)
 {
     const bool cols = p.b_j == 1 && p.b_c != 1; // (one column of one input: either)
     // (91 x 64, whose rows are not whole pieces, by staged tiles: 262,145 rows, 1,600 networks 43 and 71 us in bf16, 103 and 123 in fp32)
     const bool pieces = cols ? rows_of_pieces<T, true>(p) : rows_of_pieces<T, false>(p);
     if (p.C <= SMALL_MOST && p.J <= SMALL_MOST && !(pieces && small_by_tiles<T>(p, cols)))
-        return cols ? launch_small_widths<T, true>(st, p) : launch_small_widths<T, false>(st, p);
-    return cols ? launch_pieces<T, true>(st, p) : launch_pieces<T, false>(st, p);
+        return cols ? launch_small_widths<T, SAVED, true>(st, p) : launch_small_widths<T, SAVED, false>(st, p);
+    return cols ? launch_pieces<T, SAVED, true>(st, p) : launch_pieces<T, SAVED, false>(st, p);
 }
 
 } // namespace
@@ -548,26 +540,25 @@ extern "C" int kn_grouped_linear(void *stream, const kn_linear_desc *d, const vo
     p.o_i = d->n_out;
     p.M = (int32_t)d->rows; p.E = d->experts; p.J = d->n_out; p.C = d->n_in;
     p.a_rows = (int32_t)d->x_rows; p.relu = relu != 0;
-    return kn_with_type(d->dtype, [&](auto v) { return launch_forward<decltype(v)>((hipStream_t)stream, p); });
+    return kn_with_type(d->dtype, [&](auto v) { return launch_forward<decltype(v), false>((hipStream_t)stream, p); });
 }
 
 namespace {
-// The gradient of a layer's inputs; x_relu or saved: the mask of a ReLU before it
-int linear_dx(void *stream, const kn_linear_desc *d, const void *dy, const void *w, const void *x_relu, const void *saved, const int32_t *offsets,
-              const int32_t *rows, void *dx)
+// The gradient of a layer's inputs; mask: of a ReLU before it (SAVED: what kn_save_f8 left of its results)
+template <bool SAVED>
+int linear_dx(void *stream, const kn_linear_desc *d, const void *dy, const void *w, const void *mask, const int32_t *offsets, const int32_t *rows, void *dx)
 {
-    const bool masked = x_relu || saved;
-    if (!dy || !w || !offsets || !dx || (masked && !rows && d->x_rows < d->rows)) return KN_E_INVALID_ARG;
+    if (!dy || !w || !offsets || !dx || (mask && !rows && d->x_rows < d->rows)) return KN_E_INVALID_ARG;
     KnProduct p = {};
     const bool io = d->w_layout == KN_W_IN_OUT;
-    p.a = dy; p.b = w; p.mask = x_relu; p.mask_saved = (const int8_t *)saved; p.out = dx; p.offsets = offsets; p.rows = nullptr;
-    p.lda = d->n_out; p.ldm = saved ? kn_saved_bytes(d->n_in) : d->ldx;
+    p.a = dy; p.b = w; p.mask = mask; p.out = dx; p.offsets = offsets; p.rows = nullptr;
+    p.lda = d->n_out; p.ldm = SAVED ? kn_saved_bytes(d->n_in) : d->ldx;
     p.b_group = (int64_t)d->n_in * d->n_out; p.b_c = io ? 1 : d->n_in; p.b_j = io ? d->n_out : 1;
     p.o_i = d->n_in;
     p.M = (int32_t)d->rows; p.E = d->experts; p.J = d->n_in; p.C = d->n_out;
     p.a_rows = p.M; p.m_rows = (int32_t)d->x_rows;
-    p.mask_rows = masked ? rows : nullptr;
-    return kn_with_type(d->dtype, [&](auto v) { return launch_forward<decltype(v)>((hipStream_t)stream, p); });
+    p.mask_rows = mask ? rows : nullptr;
+    return kn_with_type(d->dtype, [&](auto v) { return launch_forward<decltype(v), SAVED>((hipStream_t)stream, p); });
 }
 } // namespace
 
@@ -575,7 +566,7 @@ extern "C" int kn_grouped_linear_dx(void *stream, const kn_linear_desc *d, const
                                     const int32_t *offsets, const int32_t *rows, void *dx)
 {
     KN_TRY(kn_linear_check(d));
-    return d->rows == 0 ? KN_OK : linear_dx(stream, d, dy, w, x_relu, nullptr, offsets, rows, dx);
+    return d->rows == 0 ? KN_OK : linear_dx<false>(stream, d, dy, w, x_relu, offsets, rows, dx);
 }
 
 extern "C" int kn_grouped_linear_dx_saved(void *stream, const kn_linear_desc *d, const void *dy, const void *w, const void *q, const int32_t *offsets,
@@ -584,5 +575,5 @@ extern "C" int kn_grouped_linear_dx_saved(void *stream, const kn_linear_desc *d,
     KN_TRY(kn_saved_check(d));
     if (d->rows == 0) return KN_OK;
     if (!q || ((uintptr_t)q & 15)) return KN_E_INVALID_ARG;
-    return linear_dx(stream, d, dy, w, nullptr, q, offsets, rows, dx);
+    return linear_dx<true>(stream, d, dy, w, q, offsets, rows, dx);
 }

@@ -186,8 +186,9 @@ template <typename T> __device__ __forceinline__ void kn_bias_of(const KnProduct
 #pragma unroll
     for (int q = 0; q < 8; ++q) add[q] = any ? (float)v[q] : 0.0f;
 }
-// The end of 8 neighbouring results of row i: zeros for a row that x does not have, bias, ReLU, the mask of a ReLU before; one rounding
-template <typename T>
+// The end of 8 neighbouring results of row i: zeros for a row that x does not have, bias, ReLU, the mask of a ReLU before (SAVED: from what kn_save_f8 left, where a
+// positive byte is a positive value, in rows of ldm bytes); one rounding
+template <typename T, bool SAVED = false>
 __device__ __forceinline__ void kn_finish(const KnProduct &p, bool some, int32_t i, int32_t j, const float add[8], float y[8])
 {
     if (p.rows && (uint32_t)p.rows[i] >= (uint32_t)p.a_rows) {
@@ -201,20 +202,21 @@ __device__ __forceinline__ void kn_finish(const KnProduct &p, bool some, int32_t
     }
     if (p.mask && some) {
         const int32_t src = p.mask_rows ? p.mask_rows[i] : i;
-        typename KnEight<T>::Piece m = {};
-        if ((uint32_t)src < (uint32_t)p.m_rows) m = KnEight<T>::load((const T *)p.mask + (int64_t)src * p.ldm, j, p.J);
+        const bool in = (uint32_t)src < (uint32_t)p.m_rows;
+        if constexpr (SAVED) { // (j is a multiple of eight, and saved rows are of whole 16 bytes)
+            typedef int8_t Eight __attribute__((ext_vector_type(8)));
+            Eight m = {};
+            if (in) m = *(const Eight *)((const int8_t *)p.mask + (int64_t)src * p.ldm + j);
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (!((float)m[q] > 0.0f)) y[q] = 0.0f;
-    }
-    if (p.mask_saved && some) { // (j is a multiple of eight, and saved rows are of whole 16 bytes)
-        typedef int8_t Eight __attribute__((ext_vector_type(8)));
-        const int32_t src = p.mask_rows ? p.mask_rows[i] : i;
-        Eight m = {};
-        if ((uint32_t)src < (uint32_t)p.m_rows) m = *(const Eight *)(p.mask_saved + (int64_t)src * p.ldm + j);
+            for (int q = 0; q < 8; ++q)
+                if (m[q] <= 0) y[q] = 0.0f;
+        } else {
+            typename KnEight<T>::Piece m = {};
+            if (in) m = KnEight<T>::load((const T *)p.mask + (int64_t)src * p.ldm, j, p.J);
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-            if (m[q] <= 0) y[q] = 0.0f;
+            for (int q = 0; q < 8; ++q)
+                if (!((float)m[q] > 0.0f)) y[q] = 0.0f;
+        }
     }
     typename KnEight<T>::Piece o;
 #pragma unroll
