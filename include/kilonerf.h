@@ -414,7 +414,7 @@ int kn_adapted_linear(void *stream, const kn_linear_desc *desc, int32_t rank, co
                       void *workspace, int64_t workspace_bytes);
 /* Its gradients: dx[i] = dy[i] W^T + g[i] A_e^T with g[i] = scales[e] dy[i] B_e^T (a row per row of y; relu_in: 0 where x[r] is not above 0, which is the
  * gradient before the ReLU that x is the result of), da[e] = sum of x[r]^T g[i], db[e] = sum of h[i]^T dy[i], laid out as a and b; zeros for a network
- * without rows.  g is rounded as h is.  dy is the gradient before the layer's own ReLU.  Where W and bias are trained too, their gradients are
+ * without rows.  g is rounded as h is, but for dx where M is 64 or less: sums of those are made in fp32, of a g in fp32.  dy is the gradient before the layer's own ReLU.  Where W and bias are trained too, their gradients are
  * kn_grouped_linear_dw's of one network whose rows are all M. */
 int kn_adapted_linear_backward_workspace_bytes(const kn_linear_desc *desc, int32_t rank, int64_t *out_bytes);
 int kn_adapted_linear_backward(void *stream, const kn_linear_desc *desc, int32_t rank, const void *dy, const void *x, const void *h, const void *w,

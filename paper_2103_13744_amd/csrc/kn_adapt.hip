@@ -23,11 +23,13 @@ struct Down {
     const void *next;
     int64_t values;
     int32_t *apart;
+    float *wide; // nullable: h before it is rounded, in rows of rp (few rows)
 };
 // What the shared product takes beside its own operands
 struct Beside {
     const void *h, *b;
     const int32_t *net, *apart; // apart: a network's b has infinities or NaN
+    const float *wide;          // Down's
     int64_t b_group, b_c, b_j;
     int32_t E, rank, rp;
 };
@@ -157,8 +159,8 @@ __device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v)
 __device__ __forceinline__ bool not_finite(_Float16 v) { return (__builtin_bit_cast(uint16_t, v) & 0x7c00u) == 0x7c00u; }
 __device__ __forceinline__ bool not_finite(__bf16 v) { return (__builtin_bit_cast(uint16_t, v) & 0x7f80u) == 0x7f80u; }
 
-// The h of 16 U rows of one network, 16 V values
-template <typename T, int B, int U, int V, int WAVES, int AHEAD> __device__ __forceinline__ void down_piece(const Down &p, int32_t number, float *red)
+// The h of 16 U rows of one network, 16 V values.  WIDE: in 32 bits, too, where asked for
+template <typename T, int B, int U, int V, int WAVES, int AHEAD, bool WIDE> __device__ __forceinline__ void down_piece(const Down &p, int32_t number, float *red)
 {
     typedef Sums<T, B, U, V, WAVES, AHEAD> Core;
     const int tid = kn_thread(), col = tid & 15;
@@ -190,6 +192,12 @@ template <typename T, int B, int U, int V, int WAVES, int AHEAD> __device__ __fo
 #pragma unroll
         for (int n = 0; n < 4; ++n) o[n] = j + n < p.rank ? (T)(scale * y[n]) : (T)0.0f; // (16 bits: what the matrix cores take)
         *(Four *)((T *)p.h + (int64_t)i * p.rp + j) = o;
+        if constexpr (WIDE && sizeof(T) == 2) {
+            kn_f32x4 whole;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) whole[n] = j + n < p.rank ? scale * y[n] : 0.0f;
+            if (p.wide) *(kn_f32x4 *)(p.wide + (int64_t)i * p.rp + j) = whole;
+        }
     }
 }
 // Whether the values that network `group` makes its second product with are all finite, if it has rows: a workgroup of its own, so that they are looked at while the
@@ -232,7 +240,7 @@ template <typename T, int B, int U, int V, int WAVES, int AHEAD> __global__ void
     __shared__ __align__(16) float red[Sums<T, B, U, V, WAVES, AHEAD>::WORDS];
     const int32_t block = p.first + kn_block();
     if (block < p.E) look_at<T, WAVES>(p, block, red);
-    else down_piece<T, B, U, V, WAVES, AHEAD>(p, block - p.E, red);
+    else down_piece<T, B, U, V, WAVES, AHEAD, false>(p, block - p.E, red);
 }
 
 // Few rows (16 U at most): one launch leaves h and the shared product's sums, cut into parts of the contraction so that all of w is on its way at once; the
@@ -251,7 +259,7 @@ template <typename T, int B, int U, int V, int DOWN_V> __global__ void __launch_
     __shared__ __align__(16) float red[Core::WORDS > Low::WORDS ? Core::WORDS : Low::WORDS];
     const int32_t block = kn_block();
     if (block >= few.products) {
-        down_piece<T, B, 1, DOWN_V, 8, 2>(down, block - few.products, red);
+        down_piece<T, B, 1, DOWN_V, 8, 2, true>(down, block - few.products, red);
         return;
     }
     const int tid = kn_thread(), col = tid & 15;
@@ -277,8 +285,9 @@ template <typename T, int B, int U, int V, int DOWN_V> __global__ void __launch_
                 if (j + n < p.J) to[n] = y[n];
     }
 }
-// Four results of a row per thread
-template <typename T> __global__ void __launch_bounds__(128) k_adapt_few_join(KnProduct p, Beside beside, Few few)
+// Four results of a row per thread.  H: what h is read in, T where it is what the caller gets (the result is made of that h, whose gradient the backward call takes, and is
+// the same whether h is asked for or not); else, for the backward call's g, 32 bits, which is summed in fp32 here and needs no rounding.
+template <typename T, typename H> __global__ void __launch_bounds__(128) k_adapt_few_join(KnProduct p, Beside beside, Few few)
 {
     typedef T Four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
     typedef float Sum __attribute__((ext_vector_type(4), aligned(4)));
@@ -299,7 +308,8 @@ template <typename T> __global__ void __launch_bounds__(128) k_adapt_few_join(Kn
         for (int n = 0; n < 4; ++n) y[n] += v[n];
     }
     if ((uint32_t)net < (uint32_t)beside.E && p.a_rows > 0) {
-        const T *h = (const T *)beside.h + (int64_t)i * beside.rp, *b = (const T *)beside.b + net * beside.b_group + j * beside.b_j;
+        const H *h = (const H *)(sizeof(H) == sizeof(T) ? beside.h : beside.wide) + (int64_t)i * beside.rp;
+        const T *b = (const T *)beside.b + net * beside.b_group + j * beside.b_j;
         float low[4] = {};
         if (beside.b_j == 1 && beside.b_c != 1) {
 #pragma unroll 8
@@ -316,7 +326,8 @@ template <typename T> __global__ void __launch_bounds__(128) k_adapt_few_join(Kn
         } else {
             constexpr int W = 16 / sizeof(T);
             for (int32_t c = 0; c < beside.rank; c += W) { // (h has zeros behind the rank)
-                const typename KnFrag<T>::Type a = *(const typename KnFrag<T>::Type *)(h + c);
+                typedef H Piece __attribute__((ext_vector_type(W)));
+                const Piece a = *(const Piece *)(h + c);
 #pragma unroll
                 for (int n = 0; n < 4; ++n) {
                     const typename KnFrag<T>::Type v = kn_any_piece<T>(b + min(n, p.J - 1 - j) * beside.b_j, c, beside.rank);
@@ -1022,7 +1033,9 @@ template <typename T> int launch_few(hipStream_t st, const Down &down, const KnP
     Few few = few_of(p.M, p.J, p.C, sizeof(T));
     few.sums = sums;
     KN_TRY(launch_few_b<T>(st, down, p, few, cols));
-    hipLaunchKernelGGL((k_adapt_few_join<T>), dim3((unsigned)kn_div_up((int64_t)p.M * kn_div_up(p.J, 4), 128)), dim3(128), 0, st, p, beside, few);
+    const dim3 grid((unsigned)kn_div_up((int64_t)p.M * kn_div_up(p.J, 4), 128));
+    if (sizeof(T) == 2 && beside.wide) hipLaunchKernelGGL((k_adapt_few_join<T, float>), grid, dim3(128), 0, st, p, beside, few);
+    else hipLaunchKernelGGL((k_adapt_few_join<T, T>), grid, dim3(128), 0, st, p, beside, few);
     KN_CHECK_LAUNCH();
     return KN_OK;
 }
@@ -1067,6 +1080,11 @@ int check(const kn_linear_desc *d, int32_t rank)
 int64_t net_bytes(const kn_linear_desc *d) { return kn_align_up(d->rows * 4, 256) + kn_align_up(d->experts * 4, 256); }
 int32_t *apart_of(const kn_linear_desc *d, void *workspace) { return (int32_t *)((char *)workspace + kn_align_up(d->rows * 4, 256)); }
 int64_t h_bytes(const kn_linear_desc *d, int32_t rank) { return kn_align_up(d->rows * (int64_t)padded_rank(d->dtype, rank) * kn_item(d->dtype), 256); }
+// Room for the g of few rows in 32 bits
+int64_t wide_bytes(const kn_linear_desc *d, int32_t rank)
+{
+    return d->rows > FEW_ROWS || d->dtype == KN_F32 ? 0 : kn_align_up(d->rows * (int64_t)padded_rank(d->dtype, rank) * 4, 256);
+}
 // Room for a factor of J rows of `rank` in rows of whole pieces, where its rows are contiguous and not that already (not beyond 256 MiB: then as they are)
 int64_t padded_bytes(const kn_linear_desc *d, int32_t rank, bool cols, int32_t J)
 {
@@ -1087,7 +1105,7 @@ int dw_bytes(const kn_linear_desc *d, int32_t rank, int64_t *out)
     int64_t na = 0, nb = 0;
     KN_TRY(kn_linear_dw_bytes(&a, true, &na));
     KN_TRY(kn_linear_dw_bytes(&b, true, &nb));
-    const int64_t few = few_bytes(d->rows, d->n_in, d->n_out, kn_item(d->dtype)); // (done with before the others begin)
+    const int64_t few = few_bytes(d->rows, d->n_in, d->n_out, kn_item(d->dtype)) + wide_bytes(d, rank); // (done with before the others begin)
     *out = na + nb;
     *out = few > *out ? few : *out;
     const int64_t padded = padded_bytes(d, rank, d->w_layout == KN_W_OUT_IN, d->n_in);
@@ -1119,8 +1137,8 @@ extern "C" int kn_adapted_linear(void *stream, const kn_linear_desc *d, int32_t 
     const bool io = d->w_layout == KN_W_IN_OUT;
     const int64_t K = d->n_in, N = d->n_out, R = rank;
     Down down = {x, a, scales, h ? h : (char *)workspace + net_bytes(d), (int32_t *)workspace, offsets, rows, d->ldx, K * R, io ? R : 1, io ? 1 : K,
-                 (int32_t)d->rows, d->experts, d->n_in, rank, padded_rank(d->dtype, rank), (int32_t)d->x_rows, 0, b, R * N, apart_of(d, workspace)};
-    Beside beside = {down.h, b, down.net, down.apart, R * N, io ? N : 1, io ? 1 : R, d->experts, rank, down.rp};
+                 (int32_t)d->rows, d->experts, d->n_in, rank, padded_rank(d->dtype, rank), (int32_t)d->x_rows, 0, b, R * N, apart_of(d, workspace), nullptr};
+    Beside beside = {down.h, b, down.net, down.apart, nullptr, R * N, io ? N : 1, io ? 1 : R, d->experts, rank, down.rp};
     KnProduct p = {};
     p.a = x; p.b = w; p.bias = bias; p.out = y; p.rows = rows;
     p.lda = d->ldx; p.b_c = io ? N : 1; p.b_j = io ? 1 : K; p.o_i = N;
@@ -1155,9 +1173,10 @@ extern "C" int kn_adapted_linear_backward(void *stream, const kn_linear_desc *d,
     char *g = (char *)workspace + net_bytes(d), *sums = g + h_bytes(d, rank);
     const int32_t rp = padded_rank(d->dtype, rank);
     if (d->rows > 0) {
+        float *wide = wide_bytes(d, rank) > 0 ? (float *)(sums + few_bytes(d->rows, d->n_in, d->n_out, kn_item(d->dtype))) : nullptr;
         Down down = {dy, b, scales, g, (int32_t *)workspace, offsets, nullptr, N, R * N, io ? 1 : R, io ? N : 1,
-                     (int32_t)d->rows, d->experts, d->n_out, rank, rp, (int32_t)d->rows, 0, a, K * R, apart_of(d, workspace)};
-        Beside beside = {g, a, down.net, down.apart, K * R, io ? 1 : K, io ? R : 1, d->experts, rank, rp};
+                     (int32_t)d->rows, d->experts, d->n_out, rank, rp, (int32_t)d->rows, 0, a, K * R, apart_of(d, workspace), wide};
+        Beside beside = {g, a, down.net, down.apart, wide, K * R, io ? 1 : K, io ? R : 1, d->experts, rank, rp};
         KnProduct p = {};
         p.a = dy; p.b = w; p.mask = relu_in ? (x ? x : w) : nullptr; p.out = dx; // (an x without rows may have no address)
         p.lda = N; p.ldm = d->ldx; p.b_c = io ? 1 : K; p.b_j = io ? N : 1; p.o_i = K;
