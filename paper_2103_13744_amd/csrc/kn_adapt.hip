@@ -907,9 +907,13 @@ template <typename T, int B, int U, int V, int WAVES, int AHEAD> int launch_down
         hipLaunchKernelGGL((k_adapt_down<T, B, U, V, WAVES, AHEAD>), grid, dim3(WAVES * 64), 0, st, q);
     });
 }
+// One wavefront where the contraction is short, and where one looks at a network's second factor in a single go (8 KiB); else its fetches are waited for one after
+// the other.  Measured (us, whole call, one / four / eight wavefronts): 65,536 rows of 4,096 networks 64 x 136, rank 4 in bf16, factors of 1 KiB, 33 / 76 / 76; 20,000 of 1,000
+// 128 x 256, rank 8, 4 KiB, 19 / 26 / 26, in fp32, 8 KiB, 38 / 44 / 44; 4,096 of 128 128 x 512, rank 16 in bf16, 16 KiB, 22 / 15 / 15; 16,384 of 64 128 x 1024, 32 KiB, 26 / 24 / 26; 4,096
+// of one 256 x 2048, rank 64, 256 KiB, 44 / 23 / 23.
 template <typename T, int B, int V> int launch_down_columns(hipStream_t st, const Down &p)
 {
-    if (p.C * (int64_t)sizeof(T) <= 512) return launch_down_of<T, B, 2, V, 1, 2>(st, p);
+    if (p.C * (int64_t)sizeof(T) <= 512 && p.values * (int64_t)sizeof(T) <= 8192) return launch_down_of<T, B, 2, V, 1, 2>(st, p);
     if (p.M / p.E >= 32) return launch_down_of<T, B, 2, V, 4, 2>(st, p);
     return launch_down_of<T, B, 1, V, 8, 2>(st, p);
 }
