@@ -406,7 +406,8 @@ int kn_grouped_linear_dw(void *stream, const kn_linear_desc *desc, const void *x
  * network: act(x[r] W + bias); an entry of `rows` that x does not have: act(bias).  One rank for all networks (fewer: zeros); desc's n_in, n_out are
  * W's, w_layout is that of all three: W (K, N), A (E, K, rank), B (E, rank, N), or W (N, K), A (E, rank, K), B (E, N, rank).
  * scales: dev, E, nullable (ones); bias: dev, N.  h (dev, nullable, 16-byte aligned): M rows of `rank` values and zeros up to the next 16 bytes, in desc's
- * dtype, to which the first product is rounded (16-bit matrix products take it in 16 bits); the backward call reads it.
+ * dtype, to which the first product is rounded (16-bit matrix products take it in 16 bits), and of which y is made, whether it is asked for or not; the backward call
+ * reads it.  In fp16 an h beyond 65504 is an infinity, and one below 2^-25 zero.
  * Workspace: dev, 256-byte aligned. */
 int kn_adapted_linear_workspace_bytes(const kn_linear_desc *desc, int32_t rank, int64_t *out_bytes);
 int kn_adapted_linear(void *stream, const kn_linear_desc *desc, int32_t rank, const void *x, const void *w, const void *a, const void *b,
@@ -414,7 +415,8 @@ int kn_adapted_linear(void *stream, const kn_linear_desc *desc, int32_t rank, co
                       void *workspace, int64_t workspace_bytes);
 /* Its gradients: dx[i] = dy[i] W^T + g[i] A_e^T with g[i] = scales[e] dy[i] B_e^T (a row per row of y; relu_in: 0 where x[r] is not above 0, which is the
  * gradient before the ReLU that x is the result of), da[e] = sum of x[r]^T g[i], db[e] = sum of h[i]^T dy[i], laid out as a and b; zeros for a network
- * without rows.  g is rounded as h is, but for dx where M is 64 or less: sums of those are made in fp32, of a g in fp32.  dy is the gradient before the layer's own ReLU.  Where W and bias are trained too, their gradients are
+ * without rows.  g is rounded as h is, but for dx where M is 64 or less: sums of those are made in fp32, of a g in fp32.  In fp16 dy and scales
+ * have to be such that g is in range, too (2^-24 to 65504), or what lies outside is lost from da and dx.  dy is the gradient before the layer's own ReLU.  Where W and bias are trained too, their gradients are
  * kn_grouped_linear_dw's of one network whose rows are all M. */
 int kn_adapted_linear_backward_workspace_bytes(const kn_linear_desc *desc, int32_t rank, int64_t *out_bytes);
 int kn_adapted_linear_backward(void *stream, const kn_linear_desc *desc, int32_t rank, const void *dy, const void *x, const void *h, const void *w,

@@ -664,7 +664,7 @@ def _adapted_args(x, w, a, b, offsets, rows, scales):
 
 def adapted_linear(x, w, a, b, offsets, rows=None, scales=None, bias=None, relu=False, want_h=False, out=None):
     """A layer that all networks share, with a low-rank product of each one's own: row i of the result, of network e with offsets[e] <= i < offsets[e + 1], is
-    x[rows[i]] @ w + h[i] @ b[e] + bias with h[i] = scales[e] * (x[rows[i]] @ a[e]), then a ReLU where asked for; rows from offsets[E] on have no
+    x[rows[i]] @ w + h[i] @ b[e] + bias with h[i] = scales[e] * (x[rows[i]] @ a[e]), rounded to x's dtype, then a ReLU where asked for; rows from offsets[E] on have no
     such product.  ``w``: (n_in, n_out), ``a``: (E, n_in, rank), ``b``: (E, rank, n_out), all contiguous, or all transposes of contiguous weights;
     ``scales``: (E,) float32 or None (ones).  ``want_h``: (result, h) for ``adapted_linear_backward``, h in rows of whole 16 bytes."""
     L = load_library()

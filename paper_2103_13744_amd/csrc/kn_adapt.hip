@@ -190,7 +190,7 @@ template <typename T, int B, int U, int V, int WAVES, int AHEAD, bool WIDE> __de
         typedef T Four __attribute__((ext_vector_type(4)));
         Four o;
 #pragma unroll
-        for (int n = 0; n < 4; ++n) o[n] = j + n < p.rank ? (T)(scale * y[n]) : (T)0.0f; // (16 bits: what the matrix cores take)
+        for (int n = 0; n < 4; ++n) o[n] = j + n < p.rank ? (T)(scale * y[n]) : (T)0.0f; // (16 bits: what the matrix cores take; fp16: what its range holds)
         *(Four *)((T *)p.h + (int64_t)i * p.rp + j) = o;
         if constexpr (WIDE && sizeof(T) == 2) {
             kn_f32x4 whole;
@@ -476,7 +476,9 @@ template <typename T, int R, int NW, int LIST, bool COLS, bool DIRECT> struct Lo
 // stages of the shared contraction come those of the tile's networks.  There a row meets other networks' values with zeros, and a zero times what is not finite is a
 // NaN: networks with such values are left out, and their rows get their part at the end, value by value.  COLS: the columns of w and b are contiguous (else the contraction is).  DIRECT: rows
 // of whole 16-byte pieces throughout.
-// Measured: 16,384 rows of 12 networks 2048 x 2048, rank 32 in bf16: 154 us, 906 TFLOP/s, where one product of the library of 8192 x 8192 x 8192 reaches 1,221.  Tiles of
+// Measured: 16,384 rows of 12 networks 2048 x 2048, rank 32 in bf16: 165 us, 845 TFLOP/s (150 to 167 from day to day), where one product of the library of 8192 x 8192 x 8192
+// reaches 1,221.  The networks that a tile meets add their number times the rank to the contraction: two and a rank of 32 one stage of 64, but 32 of rank 64 as much as W's 2048.  A
+// network that is left out costs its rows: one of 129 rows 175 -> 254 us, one of 14,813 816, for the whole call.  Tiles of
 // 192 x 128 (too few registers for two workgroups at a time): 222.
 // (128 x 128: registers for two workgroups at a time)
 template <typename T, bool COLS, bool DIRECT, int BM, int BN, int WR, int WC, int NB>

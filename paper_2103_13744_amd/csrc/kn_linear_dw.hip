@@ -20,7 +20,8 @@ __host__ __device__ inline int64_t part_places(int64_t M, int64_t len) { return 
 // lane, so that fragments cost twice the reads of the forward product's, and the LDS bounds it (128 x 128 by four wavefronts of 64 x
 // 64: 230 against 219 on even networks; 256 x 128: 230; 128 x 256: 246).  64 x 64 tiles: 524,291 rows, 4,096 networks 64 x 64 in fp16: 34
 // us, 4.9 TB/s (47 with 128 x 128).
-// SAVED: a, or b, is what kn_save_f8 left of x (its exponents beside it), and goes through registers: the 32,768 rows 243 us, 524,291 rows 64 x 64 in fp16 34.
+// SAVED: a, or b, is what kn_save_f8 left of x (its exponents beside it), and goes through registers: the 32,768 rows 250 us, 524,291 rows 64 x 64 in fp16 33.  Of small layers, too,
+// whose x as it was would be k_reduce_small's: widths far below a tile's cost what the tile does.
 enum { SUM_NONE, SUM_A, SUM_B };
 enum { SAVED_NONE, SAVED_A, SAVED_B };
 template <typename T, bool DIRECT, int BM, int BN, int WR, int WC, int SAVED = SAVED_NONE>
@@ -249,6 +250,7 @@ __global__ void __launch_bounds__(WAVES * 64) k_reduce_small(KnProduct p, int32_
 // takes every WAVES-th step of rows by itself, asked for while another is multiplied, and they are summed in the order of their numbers.  TURN: 16-bit rows
 // in pieces, wherever they lie, which an LDS of the wavefront's own turns into columns; else (fp32, and rows of less than a piece) value by value, 16 neighbouring
 // lanes, 16 neighbouring values.  Bound by the long side's bytes.  Rows that are not whole pieces, 20,000 of 100 networks 515 x 300, rank 10 in bf16: 20 us, value by value 45.
+// (In fp32 nothing but value by value has been measured.)
 constexpr int thin_bytes(int fi, int fj) { return 16 * fi * (16 * fj + 4) * 4 > (fi + fj) * 1024 ? 16 * fi * (16 * fj + 4) * 4 : (fi + fj) * 1024; } // of a wavefront
 template <typename T, int FI, int FJ, bool TURN, int WAVES>
 __device__ __forceinline__ void reduce_thin(const KnProduct &p, const Parts &parts, int32_t width_a, int32_t width_b, int32_t block, char *lds_)

@@ -469,8 +469,8 @@ template <int G, int V> __device__ __forceinline__ bool softmax_row(float v[V], 
 
 // Sums over the rows [block * per, + per): G lanes a row, whose columns' sums stay in registers from row to row and meet in the LDS at the end, in
 // the order of the groups.  A row is asked for while the one before is worked on.  ONE: these are all rows, and the results are written too; else they are
-// left for k_balance_join.  Bound by its bytes where rows are many: 32,768 rows of 128 logits in fp32 6.3 us, 2.7 TB/s, and the join 6.5; 16,385 of 1,000 in
-// bf16 13 (42 with branches around the fetches, and half the threads), and 4.8; 65,536 of 300 in fp32, forward and backward, 55, with 16 values a lane instead of 8 73.
+// left for k_balance_join.  32,768 rows of 128 logits in fp32 6.4 us, 2.7 TB/s, half of a copy's rate: what is asked for ahead passes the workgroup's end, so that of 48 rows
+// fetched 32 are its own; the join 6.2.  16,385 of 1,000 in bf16 12.7, 2.6 TB/s (48 fetched for 40; 42 us with branches around the fetches, and half the threads), and 4.6; 65,536 of 300 in fp32, forward and backward, 55, with 16 values a lane instead of 8 73.
 // 64 rows of 16: one launch, 3.0; of 1,000 in bf16 with the backward call 13.6, with 256 threads 17.8.
 constexpr int balance_threads(int G) { return G == 64 ? 512 : 256; }
 template <typename T, int G, int V, bool ONE>
